@@ -383,17 +383,173 @@ mpq_status mpq_multipoint_linear(const int8_t *X, int T, const mpq_packed_layout
                                  const void *packed, int32_t *Y, void *stream);
 
 /*
+ * Serving in few bits.  What follows is not of the paper: it is what a program that serves the
+ * quantized layers of a language model needs beside them -- the hardware's own 4-bit format for
+ * the linear layers (both operands), the key-value cache in 8 or 4 bits, and the attention of new
+ * tokens over that cache.
+ *
+ * Element types of inputs and outputs, where an argument takes one.
+ */
+#define MPQ_F32 0
+#define MPQ_F16 1
+#define MPQ_BF16 2
+
+/*
+ * Microscaled 4-bit floats.  A matrix [rows][d] is held as E2M1 codes (bit 3 the sign, bits 0..2
+ * the magnitude 0, 0.5, 1, 1.5, 2, 3, 4, 6) in blocks of 32 along a row, each with an E8M0 scale:
+ * one byte E that stands for 2^(E-127), 0xFF for NaN.  The value of an element is scale x code.
+ * One device buffer of layout->bytes bytes holds both:
+ *   codes   [rows][d_pad / 2] bytes from offset 0: element 2i in the low half of byte i, 2i + 1 in
+ *           the high half; d_pad is d rounded up to a multiple of 128, codes past d (and the bytes
+ *           from the last row to off_scales) are 0.
+ *   scales  from off_scales on: [row_tiles][k_tiles][512] bytes, one tile for each 128 rows x 128
+ *           elements; row m of a tile (0..127) and block b (0..3) at 16 (m % 32) + 4 (m / 32) + b
+ *           (the order the tensor cores take them in).  Rows past the last have scale bytes 0.
+ * A buffer in this layout that was made elsewhere can be used as well; it is 16-byte aligned.
+ */
+#define MPQ_MX_BLOCK 32
+#define MPQ_MX_MAX_DIM (1 << 24)
+typedef struct {
+    int rows, d;
+    int d_pad;               /* d rounded up to a multiple of 128 */
+    int row_tiles, k_tiles;  /* ceil(rows / 128), d_pad / 128 */
+    size_t off_scales;       /* rows * d_pad / 2 rounded up to a multiple of 512 */
+    size_t bytes;            /* size of the device buffer to allocate */
+} mpq_mx_matrix;
+
+/* mpq_mx_layout -- HOST only: the layout of a [rows][d] matrix; rows >= 0, 1 <= d <= MPQ_MX_MAX_DIM. */
+mpq_status mpq_mx_layout(int rows, int d, mpq_mx_matrix *layout);
+
+/*
+ * mpq_mx_quantize -- X [rows][d] to microscaled 4-bit floats.  For each block of 32 elements (the
+ * last of a row may be shorter), amax = max |x|:
+ *   e = floor(log2 amax) - 2, at least -127 (-127 for a block of zeros); the scale is 2^e;
+ *   the code is the level nearest to |x| / 2^e, halfway cases to the even code, and 6 for what is
+ *   larger (amax / 2^e is below 8).  x / 2^e is exact.
+ * A block with a NaN or an infinity gets the NaN scale and zero codes.
+ *   X       [rows][d] of type x_type (MPQ_F32, MPQ_F16 or MPQ_BF16), rows ldx elements apart
+ *           (ldx >= d); any alignment of its elements' own size (16-byte aligned rows are faster).
+ *   packed  out: layout->bytes bytes, 16-byte aligned.
+ */
+mpq_status mpq_mx_quantize(const void *X, int x_type, long long ldx, const mpq_mx_matrix *layout,
+                           void *packed, void *stream);
+
+/*
+ * mpq_mx_dequantize -- the values a packed matrix stands for, each rounded once to y_type.
+ *   Y  out [rows][d], rows ldy elements apart (ldy >= d); what lies between rows is left alone.
+ */
+mpq_status mpq_mx_dequantize(const void *packed, const mpq_mx_matrix *layout, void *Y, int y_type,
+                             long long ldy, void *stream);
+
+/*
+ * mpq_mx_linear -- Y[t][c] = sum_j x_tj w_cj + bias_c for packed X [T][d] and W [C][d]: products and
+ * sums of the tensor cores (exact products, fp32 sums), the bias added in fp32, one rounding to y_type.
+ *   x_layout, X  the inputs' layout (rows = T) and buffer;  w_layout, W  the weights' (rows = C; the
+ *                same d).
+ *   bias         [C] fp32 or NULL.
+ *   Y            out [T][C] of type y_type, rows ldy elements apart (ldy >= C).
+ * T = 0 or C = 0 is an empty call.  Equal inputs give equal bits from call to call (sums of several
+ * CTAs are joined in a fixed order).
+ */
+mpq_status mpq_mx_linear(const mpq_mx_matrix *x_layout, const void *X,
+                         const mpq_mx_matrix *w_layout, const void *W, const float *bias, void *Y,
+                         int y_type, long long ldy, void *stream);
+
+/*
+ * A paged key-value cache in few bits.  `pages` pages of `page` tokens each; a token's place is its
+ * slot, (page index) * page + (place in the page).  The row of `dim` values that a token keeps for
+ * one head (its key, or its value) is held as codes q with one fp32 scale s, the values s q:
+ *   s = max_j |x_j| (1 / Qmax) (the fp32 reciprocal, one fp32 product: within a unit in the last
+ *   place of the quotient), q_j = clamp(rint(x_j / s), -Qmax, Qmax) (Eq. 8's codes; fp32 division, ties
+ *   to even), Qmax = 2^(bits-1) - 1.
+ * A row of zeros, or one whose scale underflows to 0, has scale 0 and zero codes; one with a NaN or
+ * an infinity has a NaN scale and zero codes.
+ *   codes   [pages][2][heads][page][row_bytes] bytes (0: keys, 1: values), 16-byte aligned: q + 128
+ *           per byte for 8 bits; for 4 bits q + 8, element 2i in the low half of byte i.
+ *   scales  [pages][2][heads][page] fp32.
+ * Both are the caller's; nothing need be zeroed.
+ */
+typedef struct {
+    int pages, page, heads, dim, bits;
+    int row_bytes;           /* dim * bits / 8 */
+    size_t codes_bytes;      /* pages * 2 * heads * page * row_bytes */
+    size_t scales_bytes;     /* pages * 2 * heads * page * 4 */
+} mpq_kv_cache;
+
+/*
+ * mpq_cache_layout -- HOST only.  pages >= 0; page a multiple of 16, 16..1024; heads 1..1024; dim 64, 128
+ * or 256; bits 8 or 4 (other widths: MPQ_ERR_UNSUPPORTED).
+ */
+mpq_status mpq_cache_layout(int pages, int page, int heads, int dim, int bits, mpq_kv_cache *layout);
+
+/*
+ * mpq_cache_write -- quantises T tokens' keys and values into the cache.
+ *   K, V    [T][heads][dim] of type `type`; token t's row of head h starts ld_token * t + ld_head * h
+ *           elements after K (V), the dim values are consecutive (the three parts of one projection's
+ *           output can be given as they are).
+ *   slots   [T] int64 on the device; a negative slot, or one past the cache, is skipped.  Two tokens
+ *           with one slot leave it undefined which of them (or which parts) it holds.
+ */
+mpq_status mpq_cache_write(const void *K, const void *V, int type, long long ld_token,
+                           long long ld_head, int T, const int64_t *slots,
+                           const mpq_kv_cache *layout, void *codes, float *scales, void *stream);
+
+/*
+ * mpq_cache_read -- the values s q of T slots (one fp32 product, rounded once more to `type`).
+ *   K, V  out [T][heads][dim]; zeros for a slot outside the cache.
+ */
+mpq_status mpq_cache_read(const int64_t *slots, int T, const mpq_kv_cache *layout,
+                          const void *codes, const float *scales, void *K, void *V, int type,
+                          void *stream);
+
+/*
+ * mpq_cache_attention -- attention of one new token of each of B sequences over the cache:
+ *   o = sum_t p_t v_t / sum_t p_t,  p_t = exp(scale q . k_t),
+ * over the attended tokens t of the sequence: t < n_b (and t >= n_b - window if window > 0), in the
+ * page that the table names.  Query head h reads key head h / (q_heads / heads).  Scores, the softmax's
+ * maximum and sum and the outputs' sums are fp32; scores take the query in fp16 scaled by a power of two
+ * (exact for bf16 and fp16 queries but for elements 2^-24 of their head's largest), and weights times
+ * value scales are rounded to fp16 relative to the largest of them so far.
+ *   Q        [B][q_heads][dim] of type `type` (MPQ_F16 or MPQ_BF16), sequences q_stride elements
+ *            apart, heads consecutive.  q_heads is a multiple of layout->heads.
+ *   table    [B][table_cols] int32: the page of tokens page*i .. page*i + page - 1 in column i.  An
+ *            entry that names no page (negative, or >= pages) holds no tokens to attend to.
+ *   lens     [B] int32: n_b; taken as within 0 .. page * table_cols.
+ *   scale    finite; 1 / sqrt(dim) is usual.
+ *   window   0: the whole sequence; else the newest `window` tokens.
+ *   O        out [B][q_heads][dim] of type `type`.  A sequence with nothing to attend to gets zeros.
+ *   lse      out [B][q_heads] fp32, nullable: log sum_t p_t (-infinity where there is nothing).
+ *   workspace  16-byte aligned device memory of at least mpq_cache_attention_workspace() bytes, or
+ *            NULL to take it from the device's stream-ordered pool on `stream` (as
+ *            mpq_output_error does; MPQ_ERR_NOMEM).  It is zeroed once before its first use; every
+ *            call leaves it ready for the next.  Calls that may overlap (on different streams) need
+ *            one each.
+ * Equal inputs give equal bits from call to call.
+ */
+mpq_status mpq_cache_attention(const void *Q, int type, long long q_stride, int B, int q_heads,
+                               const mpq_kv_cache *layout, const void *codes, const float *scales,
+                               const int *table, int table_cols, const int *lens, float scale,
+                               int window, void *O, float *lse, void *workspace,
+                               size_t workspace_bytes, void *stream);
+
+/* Bytes of workspace that mpq_cache_attention takes, whatever the sizes. */
+#define MPQ_CACHE_WORKSPACE ((size_t)1 << 25)
+size_t mpq_cache_attention_workspace(void);
+
+/*
  * Bounded device-side waits.  The tensor-core kernels (mpq_output_error and its _noalloc variant,
- * mpq_clip_search, mpq_multipoint_linear) hand work between their warps through shared-memory
+ * mpq_clip_search, mpq_multipoint_linear, mpq_mx_linear) hand work between their warps through shared-memory
  * barriers, and every wait on one is bounded by a clock budget.  A kernel whose wait gives up
  * stops issuing work, waits for the copies and MMAs it has already issued to finish, releases its
- * tensor memory and returns, with NaN in its output errors (its inference outputs unspecified);
+ * tensor memory and returns, with NaN in its output errors (the outputs of mpq_multipoint_linear and
+ * mpq_mx_linear unspecified);
  * it records which kernel it was in a word kept per device.  A NaN error can therefore mean a
  * non-finite input or a timeout: mpq_device_status tells them apart.
  */
 #define MPQ_TIMEOUT_OUTPUT_ERROR 0x1u   /* mpq_output_error / mpq_output_error_noalloc */
 #define MPQ_TIMEOUT_CLIP 0x2u           /* mpq_clip_search */
 #define MPQ_TIMEOUT_INFERENCE 0x4u      /* mpq_multipoint_linear */
+#define MPQ_TIMEOUT_MX 0x8u             /* mpq_mx_linear */
 #define MPQ_TIMEOUT_DRAIN 0x100u        /* a wait for the kernel's own copies or MMAs also gave up */
 
 /*

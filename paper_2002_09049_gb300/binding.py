@@ -8,6 +8,8 @@ library is missing or fails to load, every call raises.
 from __future__ import annotations
 
 import ctypes
+import functools
+import math
 import os
 
 import torch
@@ -25,9 +27,13 @@ MPQ_ADAPTIVE_MAX_THRESHOLDS = 1 << 16  # most d * Qmax of mpq_quantize_layer_ada
 MPQ_TIMEOUT_OUTPUT_ERROR = 0x1        # timeout bits of mpq_device_status
 MPQ_TIMEOUT_CLIP = 0x2
 MPQ_TIMEOUT_INFERENCE = 0x4
+MPQ_TIMEOUT_MX = 0x8
 MPQ_TIMEOUT_DRAIN = 0x100
 MPQ_FAULT_BOUNDS = 0x10000            # mpq_device_status: the checked build skipped accesses
 MPQ_BUILD_CHECK_BOUNDS = 0x1          # mpq_build_options: the checked build
+
+MPQ_CACHE_WORKSPACE = 1 << 25         # bytes of mpq_cache_attention's workspace
+MPQ_TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}   # MPQ_F32, MPQ_F16, MPQ_BF16
 
 MPQ_STATUS = {0: "MPQ_OK", 1: "MPQ_ERR_INVALID_ARG", 2: "MPQ_ERR_NONFINITE",
               3: "MPQ_ERR_UNSUPPORTED", 4: "MPQ_ERR_CUDA", 5: "MPQ_ERR_TIMEOUT",
@@ -46,7 +52,32 @@ class PackedLayout(ctypes.Structure):
                 ("bytes", ctypes.c_size_t)]
 
 
+class MxMatrix(ctypes.Structure):
+    """mpq_mx_matrix of include/mpq.h: the layout of a matrix of microscaled 4-bit floats."""
+    _fields_ = [("rows", ctypes.c_int), ("d", ctypes.c_int), ("d_pad", ctypes.c_int),
+                ("row_tiles", ctypes.c_int), ("k_tiles", ctypes.c_int),
+                ("off_scales", ctypes.c_size_t), ("bytes", ctypes.c_size_t)]
+
+
+class KvCache(ctypes.Structure):
+    """mpq_kv_cache of include/mpq.h: the layout of a paged key-value cache in 8 or 4 bits."""
+    _fields_ = [("pages", ctypes.c_int), ("page", ctypes.c_int), ("heads", ctypes.c_int),
+                ("dim", ctypes.c_int), ("bits", ctypes.c_int), ("row_bytes", ctypes.c_int),
+                ("codes_bytes", ctypes.c_size_t), ("scales_bytes", ctypes.c_size_t)]
+
+    @property
+    def codes_shape(self):
+        return (self.pages, 2, self.heads, self.page, self.row_bytes)
+
+    @property
+    def scales_shape(self):
+        return (self.pages, 2, self.heads, self.page)
+
+
 _L = ctypes.POINTER(PackedLayout)
+_M = ctypes.POINTER(MxMatrix)
+_KV = ctypes.POINTER(KvCache)
+_LL = ctypes.c_longlong
 
 SIGNATURES = {
     "mpq_quantize_layer": ([_P, _I, _I, _I, _I, _P, _I, _P, _P, _P, _P, _P, _P], _I),
@@ -62,6 +93,16 @@ SIGNATURES = {
     "mpq_pack_layout": ([_P, _I, _I, _I, _I, _I, _I, _L], _I),
     "mpq_pack_points": ([_P, _P, _P, _P, _L, _P, _P], _I),
     "mpq_multipoint_linear": ([_P, _I, _L, _P, _P, _P], _I),
+    "mpq_mx_layout": ([_I, _I, _M], _I),
+    "mpq_mx_quantize": ([_P, _I, _LL, _M, _P, _P], _I),
+    "mpq_mx_dequantize": ([_P, _M, _P, _I, _LL, _P], _I),
+    "mpq_mx_linear": ([_M, _P, _M, _P, _P, _P, _I, _LL, _P], _I),
+    "mpq_cache_layout": ([_I, _I, _I, _I, _I, _KV], _I),
+    "mpq_cache_write": ([_P, _P, _I, _LL, _LL, _I, _P, _KV, _P, _P, _P], _I),
+    "mpq_cache_read": ([_P, _I, _KV, _P, _P, _P, _P, _I, _P], _I),
+    "mpq_cache_attention": ([_P, _I, _LL, _I, _I, _KV, _P, _P, _P, _I, _P, ctypes.c_float, _I, _P,
+                             _P, _P, ctypes.c_size_t, _P], _I),
+    "mpq_cache_attention_workspace": ([], ctypes.c_size_t),
     "mpq_device_status": ([_P, _P], _I),
     "mpq_set_wait_limit": ([ctypes.c_longlong], _I),
     "mpq_test_withhold_copies": ([_I], _I),
@@ -418,6 +459,185 @@ def mpq_center_weights(W, mode: int = MPQ_CENTER_PER_CHANNEL, center=None, Wc=No
     st = load().mpq_center_weights(_ptr(W), C, d, mode, _ptr(center), _ptr(Wc), _stream(stream))
     _check(st, "mpq_center_weights")
     return center, Wc
+
+
+# ---------------------------------------------------------------------------------------------
+# Serving in few bits
+
+
+def _type(t, name):
+    """The MPQ_* number of a floating element type."""
+    got = MPQ_TYPES.get(t)
+    if got is None:
+        raise TypeError(f"{name} must be torch.float32, torch.float16 or torch.bfloat16, got {t}")
+    return got
+
+
+def _rows(t, name, shape, dtype=None):
+    """A CUDA matrix of this shape whose rows are contiguous; returns its row stride."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    rows, d = shape
+    step, unit = t.stride()
+    if (unit != 1 and d > 1) or (step < d and rows > 1):
+        raise ValueError(f"{name} must have contiguous rows that do not overlap")
+    return max(step, d)
+
+
+def _packed(t, name, layout):
+    _dev(t, name, torch.uint8)
+    if t.numel() < layout.bytes:
+        raise ValueError(f"{name} is smaller than layout.bytes = {layout.bytes}")
+    return t.data_ptr()
+
+
+@functools.lru_cache(maxsize=256)
+def mpq_mx_layout(rows: int, d: int) -> MxMatrix:
+    """Host-side layout of a [rows][d] matrix of microscaled 4-bit floats (not to be changed)."""
+    lay = MxMatrix()
+    _check(load().mpq_mx_layout(rows, d, ctypes.byref(lay)), "mpq_mx_layout")
+    return lay
+
+
+def mpq_mx_quantize(X, layout: MxMatrix = None, packed=None, stream=None):
+    """X [rows][d] (fp32, fp16 or bf16; rows may lie apart) to microscaled 4-bit floats: the packed
+    buffer (uint8 [layout.bytes]) of mpq_mx_layout(rows, d)."""
+    layout = layout if layout is not None else mpq_mx_layout(*X.shape)
+    ld = _rows(X, "X", (layout.rows, layout.d))
+    if packed is None:
+        packed = torch.empty((layout.bytes,), dtype=torch.uint8, device=X.device)
+    to = _packed(packed, "packed", layout)
+    _check(load().mpq_mx_quantize(X.data_ptr(), _type(X.dtype, "X"), ld, layout, to,
+                                  _stream(stream)), "mpq_mx_quantize")
+    return packed
+
+
+def mpq_mx_dequantize(packed, layout: MxMatrix, dtype=torch.float32, Y=None, stream=None):
+    """The values [rows][d] of a packed matrix."""
+    at = _packed(packed, "packed", layout)
+    if Y is None:
+        Y = torch.empty((layout.rows, layout.d), dtype=dtype, device=packed.device)
+    ld = _rows(Y, "Y", (layout.rows, layout.d))
+    _check(load().mpq_mx_dequantize(at, layout, Y.data_ptr(), _type(Y.dtype, "Y"), ld,
+                                    _stream(stream)), "mpq_mx_dequantize")
+    return Y
+
+
+def mpq_mx_linear(X, x_layout: MxMatrix, W, w_layout: MxMatrix, bias=None, dtype=torch.bfloat16,
+                  Y=None, stream=None):
+    """Y [T][C] = X W^T + bias for packed inputs X [T][d] and weights W [C][d]; bias fp32 [C]."""
+    x, w = _packed(X, "X", x_layout), _packed(W, "W", w_layout)
+    T, C = x_layout.rows, w_layout.rows
+    if bias is not None:
+        _dev(bias, "bias", torch.float32, (C,))
+    if Y is None:
+        Y = torch.empty((T, C), dtype=dtype, device=X.device)
+    ld = _rows(Y, "Y", (T, C))
+    _check(load().mpq_mx_linear(x_layout, x, w_layout, w, _ptr(bias), Y.data_ptr(),
+                                _type(Y.dtype, "Y"), ld, _stream(stream)), "mpq_mx_linear")
+    return Y
+
+
+@functools.lru_cache(maxsize=256)
+def mpq_cache_layout(pages: int, page: int, heads: int, dim: int, bits: int = 8) -> KvCache:
+    """Host-side layout of a paged key-value cache (not to be changed): codes uint8
+    [pages][2][heads][page][row_bytes] and scales fp32 [pages][2][heads][page]."""
+    lay = KvCache()
+    _check(load().mpq_cache_layout(pages, page, heads, dim, bits, ctypes.byref(lay)),
+           "mpq_cache_layout")
+    return lay
+
+
+def mpq_cache_empty(layout: KvCache, device):
+    """Storage for a cache: (codes, scales), nothing in it."""
+    return (torch.empty(layout.codes_shape, dtype=torch.uint8, device=device),
+            torch.empty(layout.scales_shape, dtype=torch.float32, device=device))
+
+
+def _storage(layout, codes, scales):
+    _dev(codes, "codes", torch.uint8, layout.codes_shape)
+    _dev(scales, "scales", torch.float32, layout.scales_shape)
+
+
+def mpq_cache_write(K, V, slots, layout: KvCache, codes, scales, stream=None):
+    """Quantises K and V [T][heads][dim] (fp32, fp16 or bf16; tokens and heads may lie apart, the same
+    for both) into the slots [T] int64 of the cache; slots outside it are skipped."""
+    shape = (slots.shape[0], layout.heads, layout.dim)
+    for t, name in ((K, "K"), (V, "V")):
+        if not t.is_cuda:
+            raise ValueError(f"{name} must be a CUDA tensor")
+        if t.shape != shape:
+            raise ValueError(f"{name} must have shape {shape}, got {tuple(t.shape)}")
+        if t.stride(2) != 1:
+            raise ValueError(f"{name} must have contiguous rows")
+    if K.dtype != V.dtype or K.stride() != V.stride():
+        raise ValueError("K and V must have one type and the same strides")
+    _dev(slots, "slots", torch.int64, (shape[0],))
+    _storage(layout, codes, scales)
+    _check(load().mpq_cache_write(K.data_ptr(), V.data_ptr(), _type(K.dtype, "K"), K.stride(0),
+                                  K.stride(1), shape[0], slots.data_ptr(), layout,
+                                  codes.data_ptr(), scales.data_ptr(), _stream(stream)),
+           "mpq_cache_write")
+
+
+def mpq_cache_read(slots, layout: KvCache, codes, scales, dtype=torch.bfloat16, K=None, V=None,
+                   stream=None):
+    """The keys and values [T][heads][dim] that the cache holds in the slots [T] int64 (zeros for one
+    outside it)."""
+    _dev(slots, "slots", torch.int64, slots.shape[:1])
+    _storage(layout, codes, scales)
+    shape = (slots.shape[0], layout.heads, layout.dim)
+    if K is None:
+        K = torch.empty(shape, dtype=dtype, device=slots.device)
+    if V is None:
+        V = torch.empty(shape, dtype=K.dtype, device=slots.device)
+    _dev(K, "K", K.dtype, shape)
+    _dev(V, "V", K.dtype, shape)
+    _check(load().mpq_cache_read(slots.data_ptr(), shape[0], layout, codes.data_ptr(),
+                                 scales.data_ptr(), K.data_ptr(), V.data_ptr(),
+                                 _type(K.dtype, "K"), _stream(stream)), "mpq_cache_read")
+    return K, V
+
+
+def mpq_cache_attention(Q, table, lens, layout: KvCache, codes, scales, scale: float = None,
+                        window: int = 0, O=None, lse=None, workspace=None, stream=None):
+    """Attention of one new token of every sequence over the cache: Q [B][q_heads][dim] (fp16 or
+    bf16; sequences may lie apart), table [B][columns] int32 pages, lens [B] int32 tokens.  scale:
+    1 / sqrt(dim) by default; window: the newest tokens attended to (0: all).  lse: an fp32 [B][q_heads]
+    tensor that receives the logarithm of the softmax's sum.  workspace: MPQ_CACHE_WORKSPACE bytes,
+    zeroed before the first call and kept from call to call (by default taken from the pool)."""
+    B, cols = table.shape
+    if Q.dim() != 3 or Q.shape[0] != B or Q.shape[2] != layout.dim:
+        raise ValueError(f"Q must have shape ({B}, q_heads, {layout.dim}), got {tuple(Q.shape)}")
+    if not Q.is_cuda:
+        raise ValueError("Q must be a CUDA tensor")
+    q_heads = Q.shape[1]
+    if Q.stride(2) != 1 or (q_heads > 1 and Q.stride(1) != layout.dim):
+        raise ValueError("Q must have consecutive heads")
+    _dev(table, "table", torch.int32)
+    _dev(lens, "lens", torch.int32, (B,))
+    _storage(layout, codes, scales)
+    if O is None:
+        O = torch.empty((B, q_heads, layout.dim), dtype=Q.dtype, device=Q.device)
+    _dev(O, "O", Q.dtype, (B, q_heads, layout.dim))
+    if lse is not None:
+        _dev(lse, "lse", torch.float32, (B, q_heads))
+    if workspace is not None:
+        _dev(workspace, "workspace", torch.uint8)
+    if scale is None:
+        scale = 1.0 / math.sqrt(layout.dim)
+    _check(load().mpq_cache_attention(
+        Q.data_ptr(), _type(Q.dtype, "Q"), Q.stride(0), B, q_heads, layout, codes.data_ptr(),
+        scales.data_ptr(), table.data_ptr(), cols, lens.data_ptr(), scale, window, O.data_ptr(),
+        _ptr(lse), _ptr(workspace), 0 if workspace is None else workspace.numel(),
+        _stream(stream)), "mpq_cache_attention")
+    return O
 
 
 def mpq_status_string(status: int) -> str:

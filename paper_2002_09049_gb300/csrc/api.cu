@@ -7,10 +7,7 @@
 
 #include <mutex>
 
-#ifndef MPQ_NO_NVTX
-#include <nvtx3/nvToolsExt.h>
-#endif
-
+#include "api_common.cuh"
 #include "mpq_internal.cuh"
 
 namespace mpq {
@@ -81,28 +78,6 @@ cudaError_t allow_smem(const void *kernel, std::atomic<int> (&limit)[kMaxDevices
 }  // namespace mpq
 
 using namespace mpq;
-
-// One NVTX range per C-ABI call (named after the entry point), so that a profiler's timeline shows
-// which call enqueued which kernels; with no tool attached a range costs a few nanoseconds.
-// Build with -DMPQ_NO_NVTX to leave them out.
-namespace {
-struct CallRange {
-#ifndef MPQ_NO_NVTX
-    explicit CallRange(const char *name) { nvtxRangePushA(name); }
-    ~CallRange() { nvtxRangePop(); }
-#else
-    explicit CallRange(const char *) {}
-#endif
-};
-}  // namespace
-
-#define REQUIRE(cond, status, ...)  \
-    do {                            \
-        if (!(cond)) {              \
-            set_error(__VA_ARGS__); \
-            return (status);        \
-        }                           \
-    } while (0)
 
 static mpq_status check_common(int C, int d, int k_max)
 {

@@ -1,0 +1,125 @@
+// Inputs and outputs of the few-bit operators in fp32, fp16 or bf16: eight elements at a time, as two
+// or one 16-byte accesses where the rows are aligned, else one by one.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <stdint.h>
+
+#include "mpq_internal.cuh"
+
+namespace mpq {
+
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(__half v) { return __half2float(v); }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
+
+template <typename T>
+__device__ __forceinline__ T from_f32(float v);
+template <>
+__device__ __forceinline__ float from_f32<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v)
+{
+    return __float2bfloat16_rn(v);
+}
+
+// Two consecutive elements of one 4-byte word, the lower address first.
+__device__ __forceinline__ float2 unpack2(uint32_t w, __half)
+{
+    return __half22float2(*reinterpret_cast<const __half2 *>(&w));
+}
+__device__ __forceinline__ float2 unpack2(uint32_t w, __nv_bfloat16)
+{
+    return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&w));
+}
+__device__ __forceinline__ uint32_t pack2(float a, float b, __half)
+{
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+__device__ __forceinline__ uint32_t pack2(float a, float b, __nv_bfloat16)
+{
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+
+// Eight elements from p (16-byte aligned).  Ordinary loads: in a kernel that begins with griddep_wait
+// what they read may have been written by the kernel before.
+__device__ __forceinline__ void load8(const float *p, float (&v)[8])
+{
+    const float4 a = reinterpret_cast<const float4 *>(p)[0];
+    const float4 b = reinterpret_cast<const float4 *>(p)[1];
+    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
+    v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+}
+template <typename T>
+__device__ __forceinline__ void load8(const T *p, float (&v)[8])
+{
+    const uint4 a = *reinterpret_cast<const uint4 *>(p);
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = unpack2(w[i], T());
+        v[2 * i] = f.x;
+        v[2 * i + 1] = f.y;
+    }
+}
+
+__device__ __forceinline__ void store8(float *p, const float (&v)[8])
+{
+    reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
+template <typename T>
+__device__ __forceinline__ void store8(T *p, const float (&v)[8])
+{
+    *reinterpret_cast<uint4 *>(p) =
+        make_uint4(pack2(v[0], v[1], T()), pack2(v[2], v[3], T()), pack2(v[4], v[5], T()),
+                   pack2(v[6], v[7], T()));
+}
+
+// Host: bytes of an element type, 0 for a number that names none.
+inline int type_size(int type)
+{
+    return type == MPQ_F32 ? 4 : type == MPQ_F16 || type == MPQ_BF16 ? 2 : 0;
+}
+
+// Host: rows of `ld` elements from `p` on, each 16-byte aligned.
+inline bool rows_aligned(const void *p, int type, long long ld)
+{
+    return ((uintptr_t)p & 15) == 0 && (ld * type_size(type)) % 16 == 0;
+}
+
+// Host: fn(T()) for the element type `type` names (one that type_size knows).
+template <typename F>
+mpq_status by_type(int type, F &&fn)
+{
+    if (type == MPQ_F32) return fn(float());
+    if (type == MPQ_F16) return fn(__half());
+    return fn(__nv_bfloat16());
+}
+
+// Host: launch of a kernel that begins with griddep_wait (its blocks are resident before the kernel
+// ahead of it on the stream ends).
+template <typename... P, typename... A>
+mpq_status launch_waiting(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem,
+                          cudaStream_t stream, const char *what, A... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+    return cuda_status(e != cudaSuccess ? e : cudaGetLastError(), what);
+}
+
+}  // namespace mpq

@@ -130,4 +130,26 @@ mpq_status launch_adaptive(const float *W, int C, int d, int qmax, int k_max, do
 mpq_status launch_center(const float *W, int C, int d, int mode, float *center, float *Wc,
                          cudaStream_t stream);
 
+// Few-bit serving: microscaled 4-bit floats and their product, the key-value cache, its attention.
+mpq_status make_mx_layout(int rows, int d, mpq_mx_matrix *L);
+mpq_status launch_mx_quantize(const void *X, int x_type, long long ldx, const mpq_mx_matrix *L,
+                              void *packed, cudaStream_t stream);
+mpq_status launch_mx_dequantize(const void *packed, const mpq_mx_matrix *L, void *Y, int y_type,
+                                long long ldy, cudaStream_t stream);
+mpq_status launch_mx_linear(const mpq_mx_matrix *xl, const void *X, const mpq_mx_matrix *wl,
+                            const void *W, const float *bias, void *Y, int y_type, long long ldy,
+                            cudaStream_t stream);
+mpq_status make_cache_layout(int pages, int page, int heads, int dim, int bits, mpq_kv_cache *L);
+mpq_status launch_cache_write(const void *K, const void *V, int type, long long ld_token,
+                              long long ld_head, int T, const int64_t *slots,
+                              const mpq_kv_cache *L, void *codes, float *scales,
+                              cudaStream_t stream);
+mpq_status launch_cache_read(const int64_t *slots, int T, const mpq_kv_cache *L, const void *codes,
+                             const float *scales, void *K, void *V, int type, cudaStream_t stream);
+mpq_status launch_cache_attention(const void *Q, int type, long long q_stride, int B, int q_heads,
+                                  const mpq_kv_cache *L, const void *codes, const float *scales,
+                                  const int *table, int cols, const int *lens, float scale,
+                                  int window, void *O, float *lse, void *workspace,
+                                  cudaStream_t stream);
+
 }  // namespace mpq
