@@ -466,7 +466,7 @@ mpq_status mpq_mx_linear(const mpq_mx_matrix *x_layout, const void *X,
  * an infinity has a NaN scale and zero codes.
  *   codes   [pages][2][heads][page][row_bytes] bytes (0: keys, 1: values), 16-byte aligned: q + 128
  *           per byte for 8 bits; for 4 bits q + 8, element 2i in the low half of byte i.
- *   scales  [pages][2][heads][page] fp32.
+ *   scales  [pages][2][heads][page] fp32, 16-byte aligned.
  * Both are the caller's; nothing need be zeroed.
  */
 typedef struct {
@@ -496,7 +496,7 @@ mpq_status mpq_cache_write(const void *K, const void *V, int type, long long ld_
 
 /*
  * mpq_cache_read -- the values s q of T slots (one fp32 product, rounded once more to `type`).
- *   K, V  out [T][heads][dim]; zeros for a slot outside the cache.
+ *   K, V  out [T][heads][dim], 16-byte aligned; zeros for a slot outside the cache.
  */
 mpq_status mpq_cache_read(const int64_t *slots, int T, const mpq_kv_cache *layout,
                           const void *codes, const float *scales, void *K, void *V, int type,
@@ -517,7 +517,7 @@ mpq_status mpq_cache_read(const int64_t *slots, int T, const mpq_kv_cache *layou
  *   lens     [B] int32: n_b; taken as within 0 .. page * table_cols.
  *   scale    finite; 1 / sqrt(dim) is usual.
  *   window   0: the whole sequence; else the newest `window` tokens.
- *   O        out [B][q_heads][dim] of type `type`.  A sequence with nothing to attend to gets zeros.
+ *   O        out [B][q_heads][dim] of type `type`, 16-byte aligned.  A sequence with nothing to attend to gets zeros.
  *   lse      out [B][q_heads] fp32, nullable: log sum_t p_t (-infinity where there is nothing).
  *   workspace  16-byte aligned device memory of at least mpq_cache_attention_workspace() bytes, or
  *            NULL to take it from the device's stream-ordered pool on `stream` (as
@@ -538,7 +538,8 @@ size_t mpq_cache_attention_workspace(void);
 
 /*
  * Bounded device-side waits.  The tensor-core kernels (mpq_output_error and its _noalloc variant,
- * mpq_clip_search, mpq_multipoint_linear, mpq_mx_linear) hand work between their warps through shared-memory
+ * mpq_clip_search, mpq_multipoint_linear, mpq_mx_linear) hand work between their warps, and mpq_cache_attention's warps
+ * take their copies, through shared-memory
  * barriers, and every wait on one is bounded by a clock budget.  A kernel whose wait gives up
  * stops issuing work, waits for the copies and MMAs it has already issued to finish, releases its
  * tensor memory and returns, with NaN in its output errors (the outputs of mpq_multipoint_linear and
@@ -550,6 +551,7 @@ size_t mpq_cache_attention_workspace(void);
 #define MPQ_TIMEOUT_CLIP 0x2u           /* mpq_clip_search */
 #define MPQ_TIMEOUT_INFERENCE 0x4u      /* mpq_multipoint_linear */
 #define MPQ_TIMEOUT_MX 0x8u             /* mpq_mx_linear */
+#define MPQ_TIMEOUT_ATTENTION 0x10u     /* mpq_cache_attention */
 #define MPQ_TIMEOUT_DRAIN 0x100u        /* a wait for the kernel's own copies or MMAs also gave up */
 
 /*
@@ -591,7 +593,7 @@ mpq_status mpq_set_wait_limit(long long clocks);
  * mpq_test_withhold_copies -- TEST HOOK, process-wide: while on (1), the tile-copy thread of the
  * output-error contraction (mpq_output_error's tensor-core path) issues no copies, so that every
  * wait of that kernel runs out with nothing in flight and the call reports MPQ_TIMEOUT_OUTPUT_ERROR
- * through mpq_device_status.  Off (0) by default; never on outside tests of the timeout path.
+ * through mpq_device_status; likewise mpq_cache_attention's warps (MPQ_TIMEOUT_ATTENTION).  Off (0) by default; never on outside tests of the timeout path.
  */
 mpq_status mpq_test_withhold_copies(int on);
 

@@ -4,11 +4,12 @@
 // with s in the log2 domain, for the query heads of each key head.
 //
 // Bound by memory: a cached token's row costs dim * bits / 8 + 4 bytes and 4 dim operations for each
-// query head that shares it.  So the codes go from memory to the registers that feed the MMAs with
-// one stop: a lane copies (cp.async) exactly the chunks that its own fragments need into a ring of
-// its warp's shared memory and reads them back itself, which takes no barrier and no bank conflict,
-// and several 16-token stages are always in flight.  Codes become fp16 by setting them into the
-// mantissa of 1024 (an exact conversion in one permute and one subtraction for two).
+// query head that shares it.  A stage, 16 tokens of one page and head, is two tile copies (keys and
+// values, contiguous in the cache) and a scale for each lane into a ring that each warp has for
+// itself, so that several stages per warp are always in flight and no warp waits for another.  The
+// copies swizzle the rows' 16-byte chunks, and the order of a stage's tokens in the MMAs is chosen so
+// that both the keys' and the values' fragments are read without bank conflicts (row_of).  Codes become
+// fp16 by setting them into the mantissa of 1024 (exact; one permute and one subtraction for two).
 //
 // Tokens and elements are the long sides of the warp MMAs (m16n8k16, fp16 in, fp32 sums), query heads
 // the short one (8 or 16 of them, zero past the group), so that codes are converted once for all
@@ -22,13 +23,16 @@
 // rescale that long rows take a handful of times), so a token's precision does not hang on how large
 // its values are.  The sum of the softmax keeps an fp32 maximum and sum per lane.
 //
-// The work is the list of (sequence, key head, 64 tokens) tiles, cut into equal ranges for the
-// resident CTAs whatever the lengths are; the four warps of a CTA take every fourth stage of 16 tokens.
-// A (sequence, head) whose tiles are in one range is finished there.  Else each range leaves its
-// sums in the workspace, and the CTA that comes last joins them in the order of the ranges (so the
-// result does not depend on which one it is).
+// The work is the list of every (sequence, key head)'s stages, cut into equal ranges for the resident
+// warps whatever the lengths are.  A warp runs through its range on its own: its copies run ahead
+// across the ends of rows, and a row that lies in one range is finished from registers.  Rows that
+// several warps of a CTA share are joined in shared memory at the end; rows that several CTAs share
+// leave their sums in the workspace, and the CTA that comes last joins them.  Sums are joined in the
+// order of the ranges, so the result does not depend on who comes last.
+#include <cuda.h>
 #include <float.h>
 #include <math.h>
+#include <string.h>
 
 #include <algorithm>
 
@@ -36,6 +40,7 @@
 #include "mpq_internal.cuh"
 #include "pair_common.cuh"
 #include "sm100.cuh"
+#include "waits.cuh"
 
 MPQ_CHECKED_UNIT("cache_attention.cu");
 
@@ -44,14 +49,13 @@ namespace {
 
 using namespace sm100;
 
-constexpr int A_WARPS = 4;
-constexpr int A_THREADS = A_WARPS * 32;
-constexpr int A_STAGE = 16;                       // tokens of a warp's stage
-constexpr int A_TILE = A_WARPS * A_STAGE;         // tokens of a tile
-constexpr int A_MAX_CTAS = 2048;                  // counters at the head of the workspace
+constexpr int A_STAGE = 16;                       // tokens of a stage
+constexpr int A_ROW_COST = 2;                     // what a row costs besides its stages, in stages
+constexpr int A_LEAST = 2;                        // stages a warp is woken for
+constexpr int A_ROW = 6;                          // most stages of a warp where each CTA takes one row
+constexpr int A_MAX_CTAS = 512;                   // counters at the head of the workspace
 constexpr size_t A_COUNTERS = A_MAX_CTAS * sizeof(unsigned);
 constexpr float A_SHIFT = 6.0f, A_MARGIN = 14.0f; // r = largest / 2^6; moves past r 2^14
-constexpr int A_JOIN = 64;                        // ranges joined at a time
 
 struct AttnArgs {
     const void *Q;
@@ -80,21 +84,52 @@ struct Shape {
     static constexpr int NK = RB / 4 / CK;
     static constexpr int CV = RB / 8 < 16 ? RB / 8 : 16;      // a lane's value chunk
     static constexpr int NV = RB / 8 / CV;
-    static constexpr int K_BYTES = A_STAGE * RB;
-    static constexpr int STAGE_BYTES = 2 * K_BYTES + 2 * A_STAGE * 4;   // rows and scales
-    static constexpr int STAGES = RB <= 32 ? 8 : RB <= 64 ? 6 : RB <= 128 ? 4 : 3;
-    static constexpr int RING = A_WARPS * STAGES * STAGE_BYTES;
-    static constexpr int OUT_LD = D + 4;                      // a head's row of the warps' sums
-    static constexpr int JOIN_BYTES = A_WARPS * H * (OUT_LD + 3) * 4;
-    static constexpr int SMEM = RING > JOIN_BYTES ? RING : JOIN_BYTES;
-    static constexpr int SLOT = H * (D + 3);                  // floats a range leaves
-    static constexpr int CTAS = D * NT <= 128 ? 4 : D * NT <= 256 ? 3 : 2;   // resident per SM
+    static constexpr int K_BYTES = A_STAGE * RB;              // a stage's keys (and its values)
+    static constexpr int BOX = RB < 128 ? RB : 128;           // bytes of a copied row: one swizzle span
+    static constexpr int SCALE_BYTES = 2 * A_STAGE * 4;
+    // warps of a CTA, one CTA per SM: 128, 168 or 255 registers a thread
+    static constexpr int WARPS = D * NT <= 128 ? 16 : D * NT <= 256 ? 12 : 8;
+    static constexpr int THREADS = WARPS * 32;
+    static constexpr int ROOM = (222 * 1024 - 8192) / WARPS / (2 * K_BYTES + SCALE_BYTES + 8);
+    static constexpr int STAGES = ROOM < 8 ? ROOM : 8;
+    static_assert(STAGES >= 2, "a stage in use and one on its way");
+    static constexpr int LD = D + 4;                          // (heads 2c apart: other banks)
+    static constexpr int SUMS = H * (LD + 3);                 // floats of a row's sums: reference,
+                                                              // maximum, sum by head, then values
+    static constexpr int RING = STAGES * 2 * K_BYTES;
+    static constexpr int WARP_BYTES = ((RING > SUMS * 4 ? RING : SUMS * 4) + 1023) / 1024 * 1024;
+    static constexpr int OFF_SCALES = WARPS * WARP_BYTES;
+    static constexpr int OFF_BARS = OFF_SCALES + WARPS * STAGES * SCALE_BYTES;
+    static constexpr int SMEM = 1024 + OFF_BARS + WARPS * STAGES * 8;
 };
+
+// The token of a stage that row g (0..7) of an S^T tile stands for (row g + 8: that token + 8), and
+// so, by twos, the tokens of the values' k indices.  With the copies' swizzles the 8 (or 16) lanes of
+// one shared-memory access then read different banks: keys, g and g + 1 with all c; values, all c with
+// neighbouring g.
+__device__ __forceinline__ int row_of(int g) { return (g & 1) ? (g - 1) ^ 5 : g; }
+
+// Byte of 16-byte chunk `ch` of row r of a stage's keys or values.
+template <int RB>
+__device__ __forceinline__ int chunk_at(int r, int ch)
+{
+    if (RB == 256) return (ch >> 3) * (A_STAGE * 128) + r * 128 + (((ch & 7) ^ (r & 7)) << 4);
+    if (RB == 128) return r * 128 + ((ch ^ (r & 7)) << 4);
+    if (RB == 64) return r * 64 + ((ch ^ ((r >> 1) & 3)) << 4);
+    return r * 32 + ((ch ^ ((r >> 2) & 1)) << 4);
+}
 
 __device__ __forceinline__ float ex2(float x)
 {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+__device__ __forceinline__ float lg2(float x)
+{
+    float y;
+    asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
 
@@ -137,19 +172,6 @@ __device__ __forceinline__ uint32_t codes4(uint32_t w)
 }
 
 template <int BYTES>
-__device__ __forceinline__ void copy_chunk(uint32_t dst, const void *src)
-{
-    if constexpr (BYTES == 16) {
-        cp_async16(dst, src, 16);
-    } else if constexpr (BYTES == 8) {
-        asm volatile("cp.async.ca.shared.global [%0], [%1], 8;"
-                     :: "r"(dst), "l"(__cvta_generic_to_global(src)) : "memory");
-    } else {
-        cp_async4(dst, src, 4);
-    }
-}
-
-template <int BYTES>
 __device__ __forceinline__ void read_chunk(uint32_t src, uint32_t (&w)[BYTES / 4])
 {
     if constexpr (BYTES == 16)
@@ -162,243 +184,364 @@ __device__ __forceinline__ void read_chunk(uint32_t src, uint32_t (&w)[BYTES / 4
         w[0] = ld_shared_u32(src);
 }
 
-// Attended tokens [first, end) of a sequence and its tiles.
+// Attended tokens [first, end) of a sequence and its stages.
 struct Span {
     int first, end;
-    __device__ int tile0() const { return first / A_TILE; }
-    __device__ int tiles() const { return end > first ? (end + A_TILE - 1) / A_TILE - tile0() : 0; }
+    __device__ int stage0() const { return first / A_STAGE; }
+    __device__ int stages() const
+    {
+        return end > first ? (end + A_STAGE - 1) / A_STAGE - stage0() : 0;
+    }
 };
 
 __device__ __forceinline__ Span span_of(const AttnArgs &a, int b)
 {
-    const long long room = (long long)a.cols * a.L.page;
-    long long n = a.lens[b];
-    n = n < 0 ? 0 : n > room ? room : n;
-    const long long f = a.window > 0 && n > a.window ? n - a.window : 0;
-    return {(int)f, (int)n};
+    const int room = a.cols * a.L.page;
+    const int n = min(max(a.lens[b], 0), room);
+    return {a.window > 0 ? max(n - a.window, 0) : 0, n};
 }
 
-// Sums of one range of a (sequence, head block): per head the reference of the weighted values, the
-// maximum and the sum of the softmax, and the weighted values.
-struct Joined {
+// What one unit of a sequence of n stages counts in the work: its stages, and its own cost.
+__device__ __forceinline__ int weight(int n) { return n > 0 ? n + A_ROW_COST : 0; }
+
+// A row's place in the work: sequence, unit (key head and block of query heads), stages.
+struct Row {
+    int b, u, n;          // n: stages of each of the sequence's units
+    Span sp;
+    __device__ void next(const AttnArgs &a, int units)
+    {
+        if (++u < units) return;
+        u = 0;
+        do {
+            sp = span_of(a, ++b);
+            n = sp.stages();
+        } while (n == 0);
+    }
+};
+
+// Per head: the reference of the weighted values, the maximum and the sum of the softmax.
+struct Stat {
     float ref, top, sum;
 };
 
-__device__ __forceinline__ float natural_lse(float top, float sum)
+__device__ __forceinline__ float natural_lse(const Stat &s)
 {
-    return sum == 0.0f ? -INFINITY : (top + log2f(sum)) * 0.693147180559945f;
+    return s.sum == 0.0f ? -INFINITY : (s.top + log2f(s.sum)) * 0.693147180559945f;
 }
 
-// v 2^(ref - top) / sum, in two steps so that neither factor leaves fp32's range first.
-__device__ __forceinline__ float finish(float v, const Joined &j)
+// 2^(ref - top) / sum, which makes weighted values outputs, as two factors (so that none leaves fp32's
+// range before the product does); 0 where there was nothing to attend to.
+__device__ __forceinline__ float2 to_output(const Stat &s)
 {
-    if (j.sum == 0.0f) return 0.0f;
-    const float h = ex2(0.5f * (j.ref - j.top));
-    return v * h * h / j.sum;
+    if (s.sum == 0.0f) return make_float2(0.0f, 0.0f);
+    const float h = ex2(0.5f * (s.ref - s.top));
+    return make_float2(h, h / s.sum);
 }
+
+// What a warp leaves for the others: up to two rows that it has a part of, the one its range begins
+// in (kept in the workspace) and the one it ends in (in its shared memory).
+struct Part {
+    int b, u;             // b < 0: none
+    int starts, ends;     // it holds the row's first stage, its last
+};
+
+// A load for L1's sake (of the 2 bytes at p; the value goes nowhere).
+__device__ __forceinline__ void touch(const void *p)
+{
+    asm volatile("{\n\t.reg .u16 v;\n\tld.global.ca.u16 v, [%0];\n\t}" :: "l"(__cvta_generic_to_global(p))
+                 : "memory");
+}
+
+// The sum of two parts' statistics.
+__device__ __forceinline__ Stat add(const Stat &a, const Stat &b)
+{
+    const float t = fmaxf(a.top, b.top);
+    return {fmaxf(a.ref, b.ref), t, a.sum * ex2(a.top - t) + b.sum * ex2(b.top - t)};
+}
+
+// The sum of the lanes' statistics, in every lane (the same bits: each step adds the same two).
+__device__ __forceinline__ Stat add_lanes(Stat s)
+{
+#pragma unroll
+    for (int x = 1; x < 32; x <<= 1)
+        s = add(s, {__shfl_xor_sync(0xffffffffu, s.ref, x), __shfl_xor_sync(0xffffffffu, s.top, x),
+                    __shfl_xor_sync(0xffffffffu, s.sum, x)});
+    return s;
+}
+
+// a / b for a >= 0, b > 0: a 32-bit division where they allow it.
+__device__ __forceinline__ long long quotient(long long a, long long b)
+{
+    return ((a | b) >> 32) == 0 ? (long long)((unsigned)a / (unsigned)b) : a / b;
+}
+
+// The cut of `total` stages into ranges for `n` workers (n <= total).  Where total / n workers hold a
+// whole number of equal rows, so do their ranges.
+struct Cut {
+    long long total, n;
+    __device__ long long begin(int w) const { return quotient(total * w, n); }
+    __device__ int worker(long long stage) const { return (int)quotient((stage + 1) * n - 1, total); }
+};
 
 template <typename T, int D, int BITS, int NT>
-__global__ void __launch_bounds__(A_THREADS, Shape<D, BITS, NT>::CTAS)
-cache_attention_kernel(const AttnArgs a)
+__global__ void __launch_bounds__((Shape<D, BITS, NT>::THREADS), 1)
+cache_attention_kernel(const AttnArgs a, WaitCtl wc, const __grid_constant__ CUtensorMap tm)
 {
     using S = Shape<D, BITS, NT>;
-    constexpr int H = S::H;
-    extern __shared__ __align__(16) unsigned char smem[];
-    __shared__ long long sh_pre[A_WARPS];
-    __shared__ long long sh_first;           // tiles of the sequences before sh_b
-    __shared__ int sh_b, sh_last;
-    __shared__ Joined sh_join[H];
-    __shared__ float sh_factor[H][A_JOIN];
+    constexpr int H = S::H, W = S::WARPS, THREADS = S::THREADS;
+    constexpr int E = D / 32;                    // values of a head that a lane joins
+    extern __shared__ unsigned char raw[];
+    __shared__ long long sh_pre[THREADS];        // stages before each thread's sequences
+    __shared__ long long sh_warp[W];
+    __shared__ Part sh_part[2 * W];
+    __shared__ int sh_list[2 * W];               // the parts that there are, in order
+    __shared__ int sh_run[2 * W + 1];            // where runs of parts of one row begin in it
+    __shared__ int sh_counts[2];                 // parts, runs
+    __shared__ int sh_last[2];
+    __shared__ __align__(16) float sh_slice[W][D];
     griddep_launch();
-    griddep_wait();
+    const uint32_t raw_u32 = smem_u32(raw);
+    unsigned char *const smem = raw + ((1024u - (raw_u32 & 1023u)) & 1023u);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
+    const int kr = row_of(g);
+    unsigned char *const own = smem + warp * S::WARP_BYTES;
+    const uint32_t ring = smem_u32(own);
+    const uint32_t scales = smem_u32(smem) + (uint32_t)(S::OFF_SCALES + warp * S::STAGES * S::SCALE_BYTES);
+    uint64_t *const bars = reinterpret_cast<uint64_t *>(smem + S::OFF_BARS) + warp * S::STAGES;
+    if (!MPQ_CHECK_SMEM_END(smem - raw + S::OFF_BARS + W * S::STAGES * 8)) return;
+    if (lane == 0) {
+        for (int i = 0; i < S::STAGES; ++i) mbar_init(&bars[i], 1 + 32);   // the copies', the lanes' scales
+        fence_barrier_init();
+    }
+    if (tid == 0) prefetch_tensormap(&tm);
+    if (tid < 2 * W) sh_part[tid].b = -1;
     const int units = a.L.heads * a.blocks;
     T *const O = static_cast<T *>(a.O);
     const size_t o_size = (size_t)a.B * a.q_heads * D;
-    if (!MPQ_CHECK_SMEM_END(S::SMEM)) return;
+    griddep_wait();
 
-    // ---- sequences with nothing to attend to --------------------------------------------------
-    for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
-        if (span_of(a, b).tiles() > 0) continue;
-        for (int i = tid; i < a.q_heads * D; i += A_THREADS)
-            if (MPQ_IN((size_t)b * a.q_heads * D + i, o_size))
-                O[(size_t)b * a.q_heads * D + i] = from_f32<T>(0.0f);
-        if (a.lse)
-            for (int i = tid; i < a.q_heads; i += A_THREADS)
-                a.lse[(size_t)b * a.q_heads + i] = -INFINITY;
-    }
-
-    // ---- this CTA's range of the tiles, and the sequence it begins in -------------------------
-    const int per = (a.B + A_THREADS - 1) / A_THREADS;
+    // ---- the stages before each thread's sequences, and sequences with nothing to attend to -----------
+    const int per = (a.B + THREADS - 1) / THREADS;
     const int b_lo = min(tid * per, a.B), b_hi = min(b_lo + per, a.B);
-    long long mine = 0;
-    for (int b = b_lo; b < b_hi; ++b) mine += (long long)span_of(a, b).tiles() * units;
-    long long pre = mine;                    // inclusive prefix over the CTA's threads
+    long long pre = 0;
+    for (int b = b_lo; b < b_hi; ++b) pre += (long long)weight(span_of(a, b).stages()) * units;
+    const long long mine = pre;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
         const long long v = __shfl_up_sync(0xffffffffu, pre, o);
         if (lane >= o) pre += v;
     }
-    if (lane == 31) sh_pre[warp] = pre;
-    __syncthreads();
+    if (lane == 31) sh_warp[warp] = pre;
+    const int some = __syncthreads_count(mine > 0);       // sequences (of one thread each) that have any
     long long total = 0;
 #pragma unroll
-    for (int w = 0; w < A_WARPS; ++w) {
-        if (w < warp) pre += sh_pre[w];
-        total += sh_pre[w];
+    for (int w = 0; w < W; ++w) {
+        if (w < warp) pre += sh_warp[w];
+        total += sh_warp[w];
     }
-    const long long ctas = min((long long)gridDim.x, total);
-    if (blockIdx.x >= ctas) return;
-    const long long r0 = total * blockIdx.x / ctas, r1 = total * (blockIdx.x + 1LL) / ctas;
-    pre -= mine;
-    if (r0 >= pre && r0 < pre + mine) {
-        int b = b_lo;
-        for (;; ++b) {
-            const long long n = (long long)span_of(a, b).tiles() * units;
-            if (r0 < pre + n) break;
-            pre += n;
-        }
-        sh_b = b;
-        sh_first = pre;
+    sh_pre[tid] = pre - mine;
+    for (long long b = blockIdx.x + (long long)warp * gridDim.x; b < a.B; b += (long long)W * gridDim.x) {
+        if (span_of(a, (int)b).stages() > 0) continue;
+        const float zero[8] = {};
+        for (int i = lane * 8; i < a.q_heads * D; i += 256)
+            if (MPQ_IN(b * a.q_heads * D + i + 7, o_size)) store8(O + b * a.q_heads * D + i, zero);
+        for (int i = lane; a.lse && i < a.q_heads; i += 32) a.lse[b * a.q_heads + i] = -INFINITY;
     }
+    // the warps that take part, and this one's range.  A CTA a row where there are no more rows than CTAs
+    // and a warp then has A_ROW stages at most: joining CTAs takes longer than that.
+    const long long rows = (long long)some * units;
+    const bool by_row = per == 1 && rows <= gridDim.x && total <= rows * (W * A_ROW);
+    const int workers = by_row ? (int)min(rows * W, total)
+                               : (int)min((long long)gridDim.x * W, max(total / A_LEAST, 1LL));
+    const int me = blockIdx.x * W + warp;
+    if ((int)blockIdx.x * W >= workers || total == 0) return;
+    const Cut cut = {total, workers};
+    const long long r0 = me < workers ? cut.begin(me) : total;
+    long long left = me < workers ? cut.begin(me + 1) - r0 : 0;
     __syncthreads();
-    int b = sh_b;
-    long long first = sh_first;
-    Span sp = span_of(a, b);
 
-    const uint32_t ring = smem_u32(smem) + (uint32_t)(warp * S::STAGES * S::STAGE_BYTES);
-    float *const join = reinterpret_cast<float *>(smem);          // [warp][H][OUT_LD]
-    float *const join_stat = join + A_WARPS * H * S::OUT_LD;      // [warp][H][3]
     unsigned *const counters = reinterpret_cast<unsigned *>(a.workspace);
-    float *const slots = reinterpret_cast<float *>(a.workspace + A_COUNTERS);
+    float *const cta_sums = reinterpret_cast<float *>(a.workspace + A_COUNTERS);      // [CTA][2]
+    float *const warp_sums = cta_sums + (size_t)2 * gridDim.x * S::SUMS;             // [warp]
+    bool dead = false;                           // a wait gave up: the outputs read NaN
 
-    for (long long at = r0; at < r1;) {
-        // ---- the segment: tiles [t_lo, t_hi) of unit u of sequence b ----------------------------
-        int nt = sp.tiles();
-        while (at - first >= (long long)nt * units) {
-            first += (long long)nt * units;
-            sp = span_of(a, ++b);
-            nt = sp.tiles();
+    if (left > 0) {
+        // ---- the sequence and unit that the range begins in ---------------------------------------
+        Row at;
+        int st;                                   // next stage of the row
+        {
+            int lo = 0, hi = min(THREADS, a.B) - 1;   // the last thread whose sequences begin by r0
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) / 2;
+                if (sh_pre[mid] <= r0) lo = mid; else hi = mid - 1;
+            }
+            long long skip = r0 - sh_pre[lo];
+            at.b = lo * per;
+            for (;; ++at.b) {
+                at.sp = span_of(a, at.b);
+                at.n = at.sp.stages();
+                const long long all = (long long)weight(at.n) * units;
+                if (skip < all) break;
+                skip -= all;
+            }
+            at.u = (int)quotient(skip, weight(at.n));
+            const int in = (int)(skip - (long long)at.u * weight(at.n));
+            st = max(0, in - A_ROW_COST);         // the row's own cost comes first
+            left -= max(0, A_ROW_COST - in);
         }
-        const int u = (int)((at - first) / nt);
-        const int t_lo = (int)(at - first - (long long)u * nt);
-        const int t_hi = (int)min((long long)nt, t_lo + (r1 - at));
-        const int kvh = u / a.blocks, head0 = (u - kvh * a.blocks) * H;   // within the group
-        const int heads = min(H, a.group - head0);
-        const int tok_lo = (sp.tile0() + t_lo) * A_TILE;
-        const int tok_hi = min(sp.end, (sp.tile0() + t_hi) * A_TILE);
 
-        // ---- the warp's ring of stages: 16 tokens each, every fourth ---------------------------
-        const int *row_of_table = a.table + (size_t)b * a.cols;
-        int f_tok = tok_lo + warp * A_STAGE;                  // next stage to fetch
-        int f_col = f_tok / a.L.page, f_off = f_tok - f_col * a.L.page;
-        int f_page = f_tok < tok_hi ? row_of_table[f_col] : -1;
-        unsigned held = 0;                                    // bit per stage: it names a page
-        int f_slot = 0;
-        auto fetch = [&]() {
-            const bool ok = f_tok < tok_hi && f_page >= 0 && f_page < a.L.pages;
-            if (ok) {
-                const size_t row = ((size_t)f_page * 2 * a.L.heads + kvh) * a.L.page + f_off;
-                const size_t v_row = row + (size_t)a.L.heads * a.L.page;
-                const uint32_t st = ring + (uint32_t)(f_slot * S::STAGE_BYTES);
-                const unsigned char *kp = a.codes + row * S::RB, *vp = a.codes + v_row * S::RB;
-#pragma unroll
-                for (int r = 0; r < 2; ++r)
-#pragma unroll
-                    for (int i = 0; i < S::NK; ++i)
-                        copy_chunk<S::CK>(st + (uint32_t)(((r * S::NK + i) * 32 + lane) * S::CK),
-                                          kp + (g + 8 * r) * S::RB + (i * 4 + c) * S::CK);
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-#pragma unroll
-                    for (int i = 0; i < S::NV; ++i)
-                        copy_chunk<S::CV>(st + (uint32_t)(S::K_BYTES + ((r * S::NV + i) * 32 + lane) *
-                                                                           S::CV),
-                                          vp + (2 * c + (r & 1) + 8 * (r >> 1)) * S::RB +
-                                              (i * 8 + g) * S::CV);
-                cp_async4(st + (uint32_t)(2 * S::K_BYTES + lane * 4),
-                          a.scales + (lane < 16 ? row : v_row) + (lane & 15), 4);
+        // ---- the ring: stages on their way, ahead of the row that is being worked on ---------------
+        Row ahead = at;
+        long long f_left = left;
+        int f_st = st, f_i = 0, f_n = 0;          // next stage; place in the pages looked up, of f_n
+        int f_blk = 0, f_off = 0;                 // this lane's, of stage f_st + lane: the keys' block
+                                                  // (page x head) and place in the page
+        unsigned f_ok = 0;                        // bit per lane: its stage names a page
+        unsigned held = 0;                        // the same, bit per ring stage
+        auto fetch = [&](int to_slot) {
+            if (f_left <= 0) return;
+            if (f_i == f_n) {                     // look up the next 32 stages of the row
+                if (f_st == ahead.n) {
+                    f_left -= A_ROW_COST;
+                    if (f_left <= 0) return;
+                    ahead.next(a, units);
+                    f_st = 0;
+                    // the row's queries and the next sequence's pages on their way to L1 (unused here:
+                    // nothing waits for them)
+                    const int h0 = ahead.u % a.blocks * H, kv = ahead.u / a.blocks;
+                    const char *const q = reinterpret_cast<const char *>(
+                        static_cast<const T *>(a.Q) + a.q_stride * ahead.b + (size_t)(kv * a.group + h0) * D);
+                    const int bytes = min(H, a.group - h0) * D * (int)sizeof(T);
+                    for (int i = lane * 128; i < bytes; i += 32 * 128) touch(q + i);
+                    if (lane == 0 && ahead.u == 0 && ahead.b + 1 < a.B)
+                        touch(a.table + (size_t)(ahead.b + 1) * a.cols);
+                }
+                f_i = 0;
+                f_n = min(32, ahead.n - f_st);
+                const unsigned tok = (unsigned)(ahead.sp.stage0() + f_st + lane) * A_STAGE;
+                const unsigned col = tok / (unsigned)a.L.page;
+                const int page = lane < f_n ? a.table[(size_t)ahead.b * a.cols + col] : -1;
+                const bool there = page >= 0 && page < a.L.pages;
+                f_off = (int)(tok - col * (unsigned)a.L.page);
+                f_blk = there ? page * 2 * a.L.heads + ahead.u / a.blocks : 0;
+                f_ok = __ballot_sync(0xffffffffu, there);
             }
-            cp_async_commit();
-            held = ok ? held | (1u << f_slot) : held & ~(1u << f_slot);
-            f_slot = f_slot + 1 == S::STAGES ? 0 : f_slot + 1;
-            f_tok += A_TILE;
-            f_off += A_TILE;
-            while (f_off >= a.L.page) {
-                f_off -= a.L.page;
-                ++f_col;
+            const bool ok = (f_ok >> f_i) & 1u;
+            if (ok && !wc.withhold) {             // (warp-uniform)
+                const uint32_t to = ring + (uint32_t)(to_slot * 2 * S::K_BYTES);
+                uint64_t *const bar = &bars[to_slot];
+                const int blk = __shfl_sync(0xffffffffu, f_blk, f_i), off = __shfl_sync(0xffffffffu, f_off, f_i);
+                if (lane == 0) {
+                    mbar_arrive_expect_tx(bar, 2 * S::K_BYTES);
+                    if (MPQ_CHECK((to & 255u) == 0u && off % A_STAGE == 0 && off < a.L.page)) {
+#pragma unroll
+                        for (int x = 0; x < S::RB; x += S::BOX) {
+                            tma_load_3d(to + x * A_STAGE, &tm, x, off, blk, bar);
+                            tma_load_3d(to + S::K_BYTES + x * A_STAGE, &tm, x, off, blk + a.L.heads, bar);
+                        }
+                    }
+                }
+                cp_async4(scales + (uint32_t)(to_slot * S::SCALE_BYTES + lane * 4),
+                          a.scales + (long long)(blk + (lane < 16 ? 0 : a.L.heads)) * a.L.page + off +
+                              (lane & 15),
+                          4);
+                cp_async_arrive(bar);
             }
-            f_page = f_tok < tok_hi ? row_of_table[f_col] : -1;
+            held = (held & ~(1u << to_slot)) | ((unsigned)ok << to_slot);
+            ++f_i;
+            ++f_st;
+            --f_left;
         };
+        __syncwarp();                             // the barriers are ready
 #pragma unroll 1
-        for (int i = 0; i < S::STAGES - 1; ++i) fetch();
+        for (int i = 0; i < S::STAGES - 1; ++i) fetch(i);
 
-        // ---- the queries: fp16 times a power of two, in the keys' element order -----------------
-        constexpr int KSTEPS = D / 16;
-        uint32_t qf[NT][KSTEPS][2];
-        float qs[NT][2];                 // scale log2(e) / that power, of heads 2c and 2c + 1
+        int slot = 0, fill = S::STAGES - 1;       // ring stages: the next to be used, to be filled
+        unsigned parity = 0;                      // bit per ring stage: the phase of its next copies
+#pragma unroll 1
+        while (left > 0) {
+            // ---- the queries of the row: fp16 times a power of two, in the keys' element order ------
+            const int kvh = at.u / a.blocks, head0 = (at.u - kvh * a.blocks) * H;
+            const int heads = min(H, a.group - head0);
+            constexpr int KSTEPS = D / 16;
+            uint32_t qf[NT][KSTEPS][2];
+            float qs[NT][2];             // scale log2(e) / that power, of heads 2c and 2c + 1
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const int head = n * 8 + g;
-            const T *q = static_cast<const T *>(a.Q) + a.q_stride * b +
-                         (size_t)(kvh * a.group + head0 + head) * D;
-            constexpr int CE = S::CK * 8 / BITS;        // elements of a key chunk
-            float v[D / 4];
-            float m = 0.0f;
+            for (int n = 0; n < NT; ++n) {
+                const int head = n * 8 + g;
+                const T *q = static_cast<const T *>(a.Q) + a.q_stride * at.b +
+                             (size_t)(kvh * a.group + head0 + head) * D;
+                constexpr int CE = S::CK * 8 / BITS;    // elements of a key chunk
+                float v[D / 4];
+                float m = 0.0f;
 #pragma unroll
-            for (int i = 0; i < D / 4; i += 4) {
-                const T *p = q + (i / CE * 4 + c) * CE + i % CE;
-                if (head >= heads) {
-                    v[i] = v[i + 1] = v[i + 2] = v[i + 3] = 0.0f;
-                } else if (a.q_aligned) {
-                    const uint2 w = *reinterpret_cast<const uint2 *>(p);
-                    const float2 x = unpack2(w.x, T()), y = unpack2(w.y, T());
-                    v[i] = x.x, v[i + 1] = x.y, v[i + 2] = y.x, v[i + 3] = y.y;
-                } else {
+                for (int i = 0; i < D / 4; i += 4) {
+                    const T *p = q + (i / CE * 4 + c) * CE + i % CE;
+                    if (head >= heads) {
+                        v[i] = v[i + 1] = v[i + 2] = v[i + 3] = 0.0f;
+                    } else if (a.q_aligned) {
+                        const uint2 w = *reinterpret_cast<const uint2 *>(p);
+                        const float2 x = unpack2(w.x, T()), y = unpack2(w.y, T());
+                        v[i] = x.x, v[i + 1] = x.y, v[i + 2] = y.x, v[i + 3] = y.y;
+                    } else {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) v[i + k] = to_f32(p[k]);
+                        for (int k = 0; k < 4; ++k) v[i + k] = to_f32(p[k]);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < D / 4; ++i) m = fmaxf(m, fabsf(v[i]));
+                m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
+                m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
+                const int e = f16_scale_exp(m);
+                const float up = pow2f(e), down = a.scale_log2 * pow2f(-e);
+#pragma unroll
+                for (int k = 0; k < KSTEPS; ++k) {
+                    // 8 bits: bytes 0..3 of a word.  4 bits: nibbles 0, 4 | 1, 5, then 2, 6 | 3, 7.
+                    const int w = BITS == 8 ? 4 * k : 8 * (k / 2) + 2 * (k & 1);
+                    const int i0 = w, i1 = BITS == 8 ? w + 1 : w + 4;
+                    const int i2 = BITS == 8 ? w + 2 : w + 1, i3 = BITS == 8 ? w + 3 : w + 5;
+                    qf[n][k][0] = pack2(v[i0] * up, v[i1] * up, __half());
+                    qf[n][k][1] = pack2(v[i2] * up, v[i3] * up, __half());
+                }
+                qs[n][0] = __shfl_sync(0xffffffffu, down, 8 * c);
+                qs[n][1] = __shfl_sync(0xffffffffu, down, 8 * c + 4);
+            }
+
+            float o[NT][D / 16][4];
+            Stat sm[NT][2];
+            float top_hi[NT][2], ref_hi[NT][2];  // the maximum and the reference move past these
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i)
+                    o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.0f;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    sm[n][h] = {-FLT_MAX, -FLT_MAX, 0.0f};
+                    top_hi[n][h] = ref_hi[n][h] = -FLT_MAX;
                 }
             }
-#pragma unroll
-            for (int i = 0; i < D / 4; ++i) m = fmaxf(m, fabsf(v[i]));
-            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
-            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
-            const int e = f16_scale_exp(m);
-            const float up = pow2f(e), down = a.scale_log2 * pow2f(-e);
-#pragma unroll
-            for (int k = 0; k < KSTEPS; ++k) {
-                // 8 bits: bytes 0..3 of a word.  4 bits: nibbles 0, 4 | 1, 5, then 2, 6 | 3, 7.
-                const int w = BITS == 8 ? 4 * k : 8 * (k / 2) + 2 * (k & 1);
-                const int i0 = w, i1 = BITS == 8 ? w + 1 : w + 4;
-                const int i2 = BITS == 8 ? w + 2 : w + 1, i3 = BITS == 8 ? w + 3 : w + 5;
-                qf[n][k][0] = pack2(v[i0] * up, v[i1] * up, __half());
-                qf[n][k][1] = pack2(v[i2] * up, v[i3] * up, __half());
-            }
-            qs[n][0] = __shfl_sync(0xffffffffu, down, 8 * c);
-            qs[n][1] = __shfl_sync(0xffffffffu, down, 8 * c + 4);
-        }
-
-        float o[NT][D / 16][4], ref[NT][2], top[NT][2], sum[NT][2];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-#pragma unroll
-            for (int i = 0; i < D / 16; ++i) o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.0f;
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                ref[n][k] = top[n][k] = -FLT_MAX;
-                sum[n][k] = 0.0f;
-            }
-        }
-
-        int slot = 0;
+            const int st0 = st, st1 = (int)min((long long)at.n, st + left);
 #pragma unroll 1
-        for (int tok = tok_lo + warp * A_STAGE; tok < tok_hi; tok += A_TILE) {
-            cp_async_wait<S::STAGES - 2>();
-            __syncwarp();                // every lane's copies (the scales are read across lanes);
-            fetch();                     // all are done with the stage before, which this fills
-            const bool ok = (held >> slot) & 1u;
-            const uint32_t st = ring + (uint32_t)(slot * S::STAGE_BYTES);
-            if (ok) {                    // warp-uniform
+            for (; st < st1; ++st) {
+                __syncwarp();            // all lanes are done with the stage before, which this fills
+                fetch(fill);
+                const int at_slot = fill = slot;
+                slot = slot + 1 == S::STAGES ? 0 : slot + 1;
+                if (!((held >> at_slot) & 1u)) continue;           // (warp-uniform)
+                bool landed = !dead && mbar_wait(&bars[at_slot], (parity >> at_slot) & 1u, wc.budget);
+                if (__any_sync(0xffffffffu, !landed)) {
+                    // nothing more is asked for, and what is on its way lands before the warp goes on
+                    if (!dead) note_timeout(wc, MPQ_TIMEOUT_ATTENTION);
+                    dead = true;
+                    f_left = 0;
+                    held &= ~(1u << at_slot);
+                    if (!wc.withhold)
+                        drain_wait(&bars[at_slot], (parity >> at_slot) & 1u, wc, MPQ_TIMEOUT_ATTENTION);
+                }
+                parity ^= 1u << at_slot;
+                if (dead) continue;
+                const uint32_t from = ring + (uint32_t)(at_slot * 2 * S::K_BYTES);
                 // ---- S^T = K Q^T -----------------------------------------------------------------
                 float s[NT][4];
 #pragma unroll
@@ -406,8 +549,10 @@ cache_attention_kernel(const AttnArgs a)
 #pragma unroll
                 for (int i = 0; i < S::NK; ++i) {
                     uint32_t ka[S::CK / 4], kb[S::CK / 4];
-                    read_chunk<S::CK>(st + (uint32_t)((i * 32 + lane) * S::CK), ka);
-                    read_chunk<S::CK>(st + (uint32_t)(((S::NK + i) * 32 + lane) * S::CK), kb);
+                    const uint32_t k0 = from + (uint32_t)(chunk_at<S::RB>(kr, (i * 4 * S::CK + c * S::CK) / 16) +
+                                                          c * S::CK % 16);
+                    read_chunk<S::CK>(k0, ka);
+                    read_chunk<S::CK>(k0 + 8 * S::BOX, kb);
 #pragma unroll
                     for (int w = 0; w < S::CK / 4; ++w) {
                         if constexpr (BITS == 8) {
@@ -433,42 +578,56 @@ cache_attention_kernel(const AttnArgs a)
                     }
                 }
                 // ---- weights: rows g and g + 8 of the stage, heads 2c and 2c + 1 ----------------
-                const uint32_t sc = st + (uint32_t)(2 * S::K_BYTES);
-                float sk[2], lv[2];
-                bool in[2];
+                const uint32_t sc = scales + (uint32_t)(at_slot * S::SCALE_BYTES + kr * 4);
+                    float sk[2], lv[2];
 #pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    const int t = tok + g + 8 * r;
-                    in[r] = t >= sp.first && t < sp.end;
-                    sk[r] = __uint_as_float(ld_shared_u32(sc + (uint32_t)((g + 8 * r) * 4)));
-                    lv[r] = log2f(__uint_as_float(ld_shared_u32(sc + (uint32_t)((16 + g + 8 * r) * 4))));
-                }
-                bool move = false;
-                float w[NT][4];
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int r = k >> 1, h = k & 1;
-                        s[n][k] = in[r] ? s[n][k] * (sk[r] * qs[n][h]) : -INFINITY;
-                        w[n][k] = in[r] ? s[n][k] + lv[r] : -INFINITY;
-                        move |= s[n][k] > top[n][h] + A_MARGIN || w[n][k] > ref[n][h] + A_MARGIN;
+                    for (int r = 0; r < 2; ++r) {
+                        sk[r] = __uint_as_float(ld_shared_u32(sc + 32 * r));
+                        lv[r] = lg2(__uint_as_float(ld_shared_u32(sc + 64 + 32 * r)));
                     }
+                    float w[NT][4];
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            s[n][k] *= sk[k >> 1] * qs[n][k & 1];
+                            w[n][k] = s[n][k] + lv[k >> 1];
+                        }
+                    const int t0 = (at.sp.stage0() + st) * A_STAGE;
+                    if (t0 < at.sp.first || t0 + A_STAGE > at.sp.end) {    // tokens that are not attended to
+#pragma unroll
+                        for (int r = 0; r < 2; ++r) {
+                            const int t = t0 + kr + 8 * r;
+                            if (t >= at.sp.first && t < at.sp.end) continue;
+#pragma unroll
+                            for (int n = 0; n < NT; ++n)
+                                s[n][2 * r] = s[n][2 * r + 1] = w[n][2 * r] = w[n][2 * r + 1] = -INFINITY;
+                        }
+                    }
+                    bool move = false;
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+                            move |= fmaxf(s[n][h], s[n][2 + h]) > top_hi[n][h] ||
+                                    fmaxf(w[n][h], w[n][2 + h]) > ref_hi[n][h];
                 if (__any_sync(0xffffffffu, move)) {
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
-                            const float t1 = fmaxf(top[n][h], fmaxf(s[n][h], s[n][2 + h]));
-                            sum[n][h] *= ex2(top[n][h] - t1);
-                            top[n][h] = t1;
+                            const float t1 = fmaxf(sm[n][h].top, fmaxf(s[n][h], s[n][2 + h]));
+                            sm[n][h].sum *= ex2(sm[n][h].top - t1);
+                            sm[n][h].top = t1;
                             float m = fmaxf(w[n][h], w[n][2 + h]);
                             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
                             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
                             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
-                            const float r1_ = fmaxf(ref[n][h], m - A_SHIFT);
-                            const float f = ex2(ref[n][h] - r1_);
-                            ref[n][h] = r1_;
+                            const float r1 = fmaxf(sm[n][h].ref, m - A_SHIFT);
+                            const float f = ex2(sm[n][h].ref - r1);
+                            sm[n][h].ref = r1;
+                            top_hi[n][h] = t1 + A_MARGIN;
+                            ref_hi[n][h] = r1 + A_MARGIN;
 #pragma unroll
                             for (int i = 0; i < D / 16; ++i) {
                                 o[n][i][h] *= f;
@@ -481,21 +640,24 @@ cache_attention_kernel(const AttnArgs a)
                 for (int n = 0; n < NT; ++n) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
-                        sum[n][h] += ex2(s[n][h] - top[n][h]) + ex2(s[n][2 + h] - top[n][h]);
+                        sm[n][h].sum += ex2(s[n][h] - sm[n][h].top) + ex2(s[n][2 + h] - sm[n][h].top);
 #pragma unroll
                     for (int r = 0; r < 2; ++r)
-                        pf[n][r] = transpose_8x8(pack2(ex2(w[n][2 * r] - ref[n][0]),
-                                                       ex2(w[n][2 * r + 1] - ref[n][1]), __half()));
+                        pf[n][r] = transpose_8x8(pack2(ex2(w[n][2 * r] - sm[n][0].ref),
+                                                       ex2(w[n][2 * r + 1] - sm[n][1].ref), __half()));
                 }
                 // ---- O^T += V^T P^T --------------------------------------------------------------
 #pragma unroll
                 for (int i = 0; i < S::NV; ++i) {
                     uint32_t v[4][S::CV / 4];
 #pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        read_chunk<S::CV>(st + (uint32_t)(S::K_BYTES +
-                                                          ((r * S::NV + i) * 32 + lane) * S::CV),
-                                          v[r]);
+                    for (int r = 0; r < 2; ++r) {
+                        const int tok = r ? 2 * c ^ 5 : 2 * c;           // row_of(2c), row_of(2c + 1)
+                        const uint32_t v0 = from + (uint32_t)(S::K_BYTES + g * S::CV % 16 +
+                                                              chunk_at<S::RB>(tok, (i * 8 * S::CV + g * S::CV) / 16));
+                        read_chunk<S::CV>(v0, v[r]);
+                        read_chunk<S::CV>(v0 + 8 * S::BOX, v[2 + r]);
+                    }
 #pragma unroll
                     for (int w4 = 0; w4 < S::CV / 4; ++w4) {
 #pragma unroll
@@ -528,159 +690,238 @@ cache_attention_kernel(const AttnArgs a)
                     }
                 }
             }
-            slot = slot + 1 == S::STAGES ? 0 : slot + 1;
-        }
-        cp_async_wait_all();
+            left -= st1 - st0;
 
-        // ---- the four warps' sums ---------------------------------------------------------------
+            // ---- the end of the row, or of the range ------------------------------------------------
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                float t = top[n][h];
+                for (int h = 0; h < 2; ++h) {
+                    float t = sm[n][h].top;
 #pragma unroll
-                for (int x = 4; x < 32; x <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, x));
-                float l = sum[n][h] * ex2(top[n][h] - t);
+                    for (int x = 4; x < 32; x <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, x));
+                    float l = sm[n][h].sum * ex2(sm[n][h].top - t);
 #pragma unroll
-                for (int x = 4; x < 32; x <<= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
-                top[n][h] = t;
-                sum[n][h] = l;
-            }
-        __syncthreads();                 // the rings are free
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int head = n * 8 + 2 * c + h;
-                if (g == 0) {
-                    float *stat = join_stat + (warp * H + head) * 3;
-                    stat[0] = ref[n][h];
-                    stat[1] = top[n][h];
-                    stat[2] = sum[n][h];
+                    for (int x = 4; x < 32; x <<= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
+                    sm[n][h].top = t;
+                    sm[n][h].sum = dead ? NAN : l;
                 }
-                constexpr int CE = S::CV * 8 / BITS;    // elements of a value chunk
+            constexpr int CE = S::CV * 8 / BITS;        // elements of a value chunk, consecutive
+            const bool starts = st0 == 0, ends = st1 == at.n;
+            if (starts && ends) {
+                const size_t row = (size_t)at.b * a.q_heads + kvh * a.group + head0;
 #pragma unroll
-                for (int m = 0; m < D / 16; ++m)
+                for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int r = 0; r < 2; ++r) {
-                        const int d = (m / (CE / 2) * 8 + g) * CE + 2 * (m % (CE / 2)) + r;
-                        join[(warp * H + head) * S::OUT_LD + d] = o[n][m][2 * r + h];
+                    for (int h = 0; h < 2; ++h) {
+                        const int head = n * 8 + 2 * c + h;
+                        if (head >= heads) continue;
+                        if (a.lse && g == 0) a.lse[row + head] = natural_lse(sm[n][h]);
+                        const float2 f = to_output(sm[n][h]);
+#pragma unroll
+                        for (int i = 0; i < S::NV; ++i)
+#pragma unroll
+                            for (int k = 0; k < CE; k += 8) {
+                                float v[8];
+#pragma unroll
+                                for (int e = 0; e < 8; ++e)
+                                    v[e] = o[n][(i * CE + k + e) / 2][2 * (e & 1) + h] * f.x * f.y;
+                                const size_t to = (row + head) * D + (i * 8 + g) * CE + k;
+                                if (MPQ_IN(to + 7, o_size)) store8(O + to, v);
+                            }
                     }
-            }
-        __syncthreads();
-        const bool whole = t_lo == 0 && t_hi == nt;
-        if (tid < H) {
-            Joined j = {-FLT_MAX, -FLT_MAX, 0.0f};
+            } else {
+                const bool last = left == 0 || (st1 == at.n && left <= A_ROW_COST);     // (then the ring is free)
+                float *const to = last ? reinterpret_cast<float *>(own) : warp_sums + (size_t)me * S::SUMS;
+                if (last) __syncwarp();
 #pragma unroll
-            for (int w = 0; w < A_WARPS; ++w) {
-                j.ref = fmaxf(j.ref, join_stat[(w * H + tid) * 3]);
-                j.top = fmaxf(j.top, join_stat[(w * H + tid) * 3 + 1]);
-            }
+                for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int w = 0; w < A_WARPS; ++w)
-                j.sum += join_stat[(w * H + tid) * 3 + 2] *
-                         ex2(join_stat[(w * H + tid) * 3 + 1] - j.top);
-            sh_join[tid] = j;
-        }
-        __syncthreads();
-        const size_t out_row = (size_t)b * a.q_heads + kvh * a.group + head0;
-        float *const part = slots + (size_t)(2 * blockIdx.x + (t_lo == 0 ? 1 : 0)) * S::SLOT;
-        for (int i = tid; i < heads * D; i += A_THREADS) {
-            const int head = i / D, d = i - head * D;
-            const Joined j = sh_join[head];
-            float v = 0.0f;
-#pragma unroll
-            for (int w = 0; w < A_WARPS; ++w)
-                v += join[(w * H + head) * S::OUT_LD + d] *
-                     ex2(join_stat[(w * H + head) * 3] - j.ref);
-            if (whole && MPQ_IN(out_row * D + i, o_size))
-                O[out_row * D + i] = from_f32<T>(finish(v, j));
-            else if (!whole && MPQ_IN(part + 3 * H + i - slots, 2 * gridDim.x * S::SLOT))
-                __stcg(part + 3 * H + i, v);
-        }
-        if (whole) {
-            if (a.lse && tid < heads)
-                a.lse[out_row + tid] = natural_lse(sh_join[tid].top, sh_join[tid].sum);
-            __syncthreads();             // the rings are filled again
-        } else {
-            if (tid < heads) {
-                __stcg(part + tid, sh_join[tid].ref);
-                __stcg(part + H + tid, sh_join[tid].top);
-                __stcg(part + 2 * H + tid, sh_join[tid].sum);
-            }
-            // ---- the unit's ranges: c0 .. c1; the CTA that comes last joins them ------------------
-            const long long g0 = first + (long long)u * nt;
-            const int c0 = (int)(((g0 + 1) * ctas - 1) / total);
-            const int c1 = (int)(((g0 + nt) * ctas - 1) / total);
-            __threadfence();
-            __syncthreads();
-            if (tid == 0) {
-                const unsigned n = atomicAdd(&counters[c0], 1u);
-                sh_last = n == (unsigned)(c1 - c0);
-                if (sh_last) counters[c0] = 0;
-            }
-            __syncthreads();
-            if (sh_last) {
-                __threadfence();
-                // range i of the unit: the first leaves its sums in its second slot, the others in
-                // their first
-                auto slot_of = [&](int i) {
-                    return slots + (size_t)(2 * (c0 + i) + (i == 0 ? 1 : 0)) * S::SLOT;
-                };
-                const int n = c1 - c0 + 1;
-                for (int h = warp; h < heads; h += A_WARPS) {
-                    Joined j = {-FLT_MAX, -FLT_MAX, 0.0f};
-                    for (int i = lane; i < n; i += 32) {
-                        j.ref = fmaxf(j.ref, __ldcg(slot_of(i) + h));
-                        j.top = fmaxf(j.top, __ldcg(slot_of(i) + H + h));
-                    }
-#pragma unroll
-                    for (int x = 1; x < 32; x <<= 1) {
-                        j.ref = fmaxf(j.ref, __shfl_xor_sync(0xffffffffu, j.ref, x));
-                        j.top = fmaxf(j.top, __shfl_xor_sync(0xffffffffu, j.top, x));
-                    }
-                    for (int i = lane; i < n; i += 32)
-                        j.sum += __ldcg(slot_of(i) + 2 * H + h) *
-                                 ex2(__ldcg(slot_of(i) + H + h) - j.top);
-#pragma unroll
-                    for (int x = 1; x < 32; x <<= 1)
-                        j.sum += __shfl_xor_sync(0xffffffffu, j.sum, x);
-                    if (lane == 0) sh_join[h] = j;
-                }
-                constexpr int MINE = H * D / A_THREADS;
-                float acc[MINE];
-#pragma unroll
-                for (int k = 0; k < MINE; ++k) acc[k] = 0.0f;
-                for (int i0 = 0; i0 < n; i0 += A_JOIN) {
-                    const int m = min(A_JOIN, n - i0);
-                    __syncthreads();
-                    for (int i = tid; i < heads * A_JOIN; i += A_THREADS) {
-                        const int h = i / A_JOIN, k = i % A_JOIN;
-                        if (k < m)
-                            sh_factor[h][k] = ex2(__ldcg(slot_of(i0 + k) + h) - sh_join[h].ref);
-                    }
-                    __syncthreads();
-                    for (int k = 0; k < m; ++k) {
-                        const float *p = slot_of(i0 + k) + 3 * H;
-#pragma unroll
-                        for (int e = 0; e < MINE; ++e) {
-                            const int i = e * A_THREADS + tid;
-                            if (i < heads * D) acc[e] += __ldcg(p + i) * sh_factor[i / D][k];
+                    for (int h = 0; h < 2; ++h) {
+                        const int head = n * 8 + 2 * c + h;
+                        if (g == 0) {
+                            to[head] = sm[n][h].ref;
+                            to[H + head] = sm[n][h].top;
+                            to[2 * H + head] = sm[n][h].sum;
                         }
-                    }
-                }
 #pragma unroll
-                for (int e = 0; e < MINE; ++e) {
-                    const int i = e * A_THREADS + tid;
-                    if (i < heads * D && MPQ_IN(out_row * D + i, o_size))
-                        O[out_row * D + i] = from_f32<T>(finish(acc[e], sh_join[i / D]));
-                }
-                if (a.lse && tid < heads)
-                    a.lse[out_row + tid] = natural_lse(sh_join[tid].top, sh_join[tid].sum);
+                        for (int i = 0; i < S::NV; ++i)
+#pragma unroll
+                            for (int k = 0; k < CE; k += 4) {
+                                const int m = (i * CE + k) / 2;
+                                *reinterpret_cast<float4 *>(to + 3 * H + head * S::LD + (i * 8 + g) * CE +
+                                                            k) =
+                                    make_float4(o[n][m][h], o[n][m][2 + h], o[n][m + 1][h],
+                                                o[n][m + 1][2 + h]);
+                            }
+                    }
+                if (lane == 0) sh_part[2 * warp + (last ? 1 : 0)] = {at.b, at.u, starts, ends};
             }
-            __syncthreads();
+            if (st1 == at.n) left -= A_ROW_COST;
+            if (left > 0) {
+                at.next(a, units);
+                st = 0;
+            }
         }
-        at += t_hi - t_lo;
+    }
+    __syncthreads();
+
+    // ---- rows that several warps share: runs of parts of one row, in the order of the warps ------------
+    static_assert(2 * W <= 32, "one lane per part");
+    if (warp == 0) {
+        const Part part = lane < 2 * W ? sh_part[lane] : Part{-1, 0, 0, 0};
+        const unsigned live = __ballot_sync(0xffffffffu, part.b >= 0);
+        const unsigned lower = live & ((1u << lane) - 1u);
+        const int before = 31 - __clz((int)lower);            // the part before, or -1
+        const int prev_b = __shfl_sync(0xffffffffu, part.b, before & 31);
+        const int prev_u = __shfl_sync(0xffffffffu, part.u, before & 31);
+        const bool first = part.b >= 0 && (before < 0 || prev_b != part.b || prev_u != part.u);
+        const unsigned firsts = __ballot_sync(0xffffffffu, first);
+        if (part.b >= 0) sh_list[__popc(lower)] = lane;
+        if (first) sh_run[__popc(firsts & ((1u << lane) - 1u))] = __popc(lower);
+        if (lane == 0) {
+            sh_run[__popc(firsts)] = __popc(live);
+            sh_counts[0] = __popc(live);
+            sh_counts[1] = __popc(firsts);
+        }
+    }
+    __syncthreads();
+    const int runs = sh_counts[1];
+    const float *const kept = warp_sums + (size_t)blockIdx.x * W * S::SUMS;
+    // a warp takes a head of a run at a time, a lane the statistics of a part
+    for (int item = warp; item < runs * H; item += W) {
+        const int run = item / H, h = item % H;
+        const int p0 = sh_run[run], n = sh_run[run + 1] - p0;
+        const Part lead = sh_part[sh_list[p0]];
+        const bool starts = lead.starts, ends = sh_part[sh_list[p0 + n - 1]].ends;
+        const int head0 = lead.u % a.blocks * H;
+        if (h >= min(H, a.group - head0)) continue;
+        const int mine_p = lane < n ? sh_list[p0 + lane] : 0;
+        // a part's sums: in its warp's shared memory, or kept in the workspace
+        const float *const at = (mine_p & 1)
+                                    ? reinterpret_cast<const float *>(smem + (mine_p >> 1) * S::WARP_BYTES)
+                                    : kept + (size_t)(mine_p >> 1) * S::SUMS;
+        Stat s = {-FLT_MAX, -FLT_MAX, 0.0f};
+        if (lane < n) s = {at[h], at[H + h], at[2 * H + h]};
+        const float ref = s.ref;
+        s = add_lanes(s);
+        const float factor = ex2(ref - s.ref);
+        float acc[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] = 0.0f;
+#pragma unroll 4
+        for (int i = 0; i < n; ++i) {
+            const float f = __shfl_sync(0xffffffffu, factor, i);
+            const float *const q = reinterpret_cast<const float *>(
+                __shfl_sync(0xffffffffu, (unsigned long long)at, i)) + 3 * H + h * S::LD + lane;
+#pragma unroll
+            for (int e = 0; e < E; ++e) acc[e] += f * q[e * 32];
+        }
+        if (starts && ends) {
+            const size_t row = (size_t)lead.b * a.q_heads + (lead.u / a.blocks) * a.group + head0 + h;
+            const float2 f = to_output(s);
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (MPQ_IN(row * D + e * 32 + lane, o_size))
+                    O[row * D + e * 32 + lane] = from_f32<T>(acc[e] * f.x * f.y);
+            if (a.lse && lane == 0) a.lse[row] = natural_lse(s);
+        } else {
+            float *const to = cta_sums + (size_t)(2 * blockIdx.x + (starts ? 1 : 0)) * S::SUMS;
+            if (lane == 0) {
+                __stcg(to + h, s.ref);
+                __stcg(to + H + h, s.top);
+                __stcg(to + 2 * H + h, s.sum);
+            }
+#pragma unroll
+            for (int e = 0; e < E; ++e) __stcg(to + 3 * H + h * S::LD + e * 32 + lane, acc[e]);
+        }
+    }
+
+    // ---- rows that several CTAs share: this one's first run (begun before) and its last ---------------
+    if (runs == 0) return;
+    const Part in_first = sh_part[sh_list[0]], in_last = sh_part[sh_list[sh_run[runs - 1]]];
+    const bool last_ends = sh_part[sh_list[sh_counts[0] - 1]].ends;
+    const bool open[2] = {!in_first.starts, (bool)in_last.starts && !last_ends};
+    if (!open[0] && !open[1]) return;
+    // the row's CTAs: those of the workers of its first and last stage
+    int c0[2], c1[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        c0[k] = c1[k] = 0;
+        if (!open[k]) continue;
+        const Part p = k ? in_last : in_first;
+        long long g0 = sh_pre[p.b / per];
+        for (int b = p.b / per * per; b < p.b; ++b)
+            g0 += (long long)weight(span_of(a, b).stages()) * units;
+        const int n = span_of(a, p.b).stages();
+        g0 += (long long)p.u * weight(n) + A_ROW_COST;
+        c0[k] = cut.worker(g0) / W;
+        c1[k] = cut.worker(g0 + n - 1) / W;
+    }
+    __threadfence();
+    __syncthreads();
+    if (tid < 2) {
+        sh_last[tid] = 0;
+        if (open[tid]) {
+            sh_last[tid] = atomicAdd(&counters[c0[tid]], 1u) == (unsigned)(c1[tid] - c0[tid]);
+            if (sh_last[tid]) counters[c0[tid]] = 0;
+        }
+        __threadfence();
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (int k = 0; k < 2; ++k) {
+        if (!sh_last[k]) continue;
+        const Part p = k ? in_last : in_first;
+        const int head0 = p.u % a.blocks * H, heads = min(H, a.group - head0);
+        const int n = c1[k] - c0[k] + 1;
+        // the first CTA's sums are in its second place, the others' in their first
+        const float *const base = cta_sums + (size_t)2 * c0[k] * S::SUMS;
+        auto sums = [&](int i) { return base + (size_t)(2 * i + (i == 0 ? 1 : 0)) * S::SUMS; };
+        // several warps a head where there are more warps than heads, each a slice of the CTAs
+        const int slices = max(1, W / heads);
+        for (int i0 = 0; i0 < heads; i0 += W) {
+            const int h = i0 + warp % heads, slice = heads > W ? 0 : warp / heads;
+            const bool works = h < heads && slice < slices;
+            Stat s = {0.0f, 0.0f, 0.0f};
+            float acc[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) acc[e] = 0.0f;
+            if (works) {
+                s = {-FLT_MAX, -FLT_MAX, 0.0f};
+                for (int i = lane; i < n; i += 32) {
+                    const float *const q = sums(i) + h;
+                    s = add(s, {__ldcg(q), __ldcg(q + H), __ldcg(q + 2 * H)});
+                }
+                s = add_lanes(s);
+                const int lo = n * slice / slices, hi = n * (slice + 1) / slices;
+#pragma unroll 4
+                for (int i = lo; i < hi; ++i) {
+                    const float *const q = sums(i);
+                    const float f = ex2(__ldcg(q + h) - s.ref);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) acc[e] += f * __ldcg(q + 3 * H + h * S::LD + e * 32 + lane);
+                }
+            }
+            if (slices > 1) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) sh_slice[warp][e * 32 + lane] = acc[e];
+                __syncthreads();
+                for (int j = 1; works && slice == 0 && j < slices; ++j)
+#pragma unroll
+                    for (int e = 0; e < E; ++e) acc[e] += sh_slice[j * heads + h][e * 32 + lane];
+                __syncthreads();
+            }
+            if (works && slice == 0) {
+                const size_t row = (size_t)p.b * a.q_heads + (p.u / a.blocks) * a.group + head0 + h;
+                const float2 f = to_output(s);
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (MPQ_IN(row * D + e * 32 + lane, o_size))
+                        O[row * D + e * 32 + lane] = from_f32<T>(acc[e] * f.x * f.y);
+                if (a.lse && lane == 0) a.lse[row] = natural_lse(s);
+            }
+        }
     }
 }
 
@@ -692,18 +933,40 @@ mpq_status launch_shape(const AttnArgs &a, cudaStream_t stream)
     const cudaError_t e = allow_smem(
         reinterpret_cast<const void *>(cache_attention_kernel<T, D, BITS, NT>), limit, S::SMEM);
     if (e != cudaSuccess) return cuda_status(e, "cudaFuncSetAttribute");
-    // every tile that the tables could hold, at most as many CTAs as are resident and as the
-    // workspace has room for
+    // the codes as rows of a page and head: [pages x 2 x heads][page][row] (a cache without pages is
+    // never read; the map then names the workspace)
+    CUtensorMap tm;
+    memset(&tm, 0, sizeof(tm));
+    const bool any = a.L.pages > 0;
+    const cuuint64_t dims[3] = {(cuuint64_t)S::RB, (cuuint64_t)a.L.page,
+                                any ? (cuuint64_t)a.L.pages * 2 * a.L.heads : 1};
+    const cuuint64_t strides[2] = {(cuuint64_t)S::RB, (cuuint64_t)a.L.page * S::RB};
+    const cuuint32_t box[3] = {(cuuint32_t)S::BOX, A_STAGE, 1};
+    if (!encode_tile_map(&tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3,
+                         any ? (const void *)a.codes : (const void *)a.workspace, dims, strides, box,
+                         S::BOX == 128  ? CU_TENSOR_MAP_SWIZZLE_128B
+                         : S::BOX == 64 ? CU_TENSOR_MAP_SWIZZLE_64B
+                                        : CU_TENSOR_MAP_SWIZZLE_32B)) {
+        set_error("cache attention: tensor map encoding failed");
+        return MPQ_ERR_CUDA;
+    }
+    WaitCtl wc;
+    const mpq_status ws = wait_ctl(&wc);
+    if (ws != MPQ_OK) return ws;
+    // one CTA per SM, fewer where the tables cannot hold work for all their warps; the workspace has
+    // room for two rows' sums of each CTA and one of each warp
     const long long room = (long long)a.cols * a.L.page;
-    const long long span = a.window > 0 ? std::min<long long>(room, a.window) + A_TILE : room;
-    const long long tiles = (span + A_TILE - 1) / A_TILE;
+    const long long span = a.window > 0 ? std::min<long long>(room, a.window) + A_STAGE : room;
+    const long long stages = (span + A_STAGE - 1) / A_STAGE * a.L.heads * a.blocks;   // of a sequence
     const long long fit =
-        (long long)((MPQ_CACHE_WORKSPACE - A_COUNTERS) / (2 * S::SLOT * sizeof(float)));
-    long long ctas = std::min<long long>((long long)sm_count() * S::CTAS, std::min<long long>(fit, A_MAX_CTAS));
-    const long long most = tiles * a.L.heads * a.blocks;     // of one sequence
-    if (most < ctas) ctas = std::min(ctas, std::max<long long>(1, most * a.B));
+        (long long)((MPQ_CACHE_WORKSPACE - A_COUNTERS) / ((2 + S::WARPS) * S::SUMS * sizeof(float)));
+    const long long most = std::min<long long>(std::min<long long>(sm_count(), fit), A_MAX_CTAS);
+    const long long wake = (long long)A_LEAST * S::WARPS;                 // stages that wake a CTA
+    const long long ctas = stages >= most * wake
+                               ? most
+                               : std::min(most, std::max(1LL, (stages * a.B + wake - 1) / wake));
     return launch_waiting(cache_attention_kernel<T, D, BITS, NT>, dim3((unsigned)ctas),
-                          dim3(A_THREADS), S::SMEM, stream, "cache attention launch", a);
+                          dim3(S::THREADS), S::SMEM, stream, "cache attention launch", a, wc, tm);
 }
 
 template <typename T, int D, int BITS>

@@ -117,6 +117,8 @@ extern "C" mpq_status mpq_cache_layout(int pages, int page, int heads, int dim, 
             "page = %d must be a multiple of 16, at most 1024", page);
     REQUIRE(heads >= 1, MPQ_ERR_INVALID_ARG, "heads = %d must be >= 1", heads);
     REQUIRE(heads <= 1024, MPQ_ERR_UNSUPPORTED, "heads = %d exceeds 1024", heads);
+    REQUIRE((long long)pages * 2 * heads <= INT_MAX, MPQ_ERR_UNSUPPORTED,
+            "pages * 2 * heads = %lld too large", (long long)pages * 2 * heads);
     REQUIRE(dim >= 1, MPQ_ERR_INVALID_ARG, "dim = %d must be >= 1", dim);
     REQUIRE(dim == 64 || dim == 128 || dim == 256, MPQ_ERR_UNSUPPORTED,
             "dim = %d is not 64, 128 or 256", dim);
@@ -203,8 +205,8 @@ extern "C" mpq_status mpq_cache_attention(const void *Q, int type, long long q_s
     REQUIRE(table_cols == 0 || table, MPQ_ERR_INVALID_ARG, "table must be non-NULL");
     REQUIRE(layout->pages == 0 || (codes && scales), MPQ_ERR_INVALID_ARG,
             "codes and scales must be non-NULL");
-    REQUIRE(aligned16(codes) && aligned16(workspace), MPQ_ERR_INVALID_ARG,
-            "codes and workspace must be 16-byte aligned");
+    REQUIRE(aligned16(codes) && aligned16(scales) && aligned16(O) && aligned16(workspace),
+            MPQ_ERR_INVALID_ARG, "codes, scales, O and workspace must be 16-byte aligned");
     REQUIRE(!workspace || workspace_bytes >= MPQ_CACHE_WORKSPACE, MPQ_ERR_INVALID_ARG,
             "workspace of %zu bytes: %zu are needed", workspace_bytes, MPQ_CACHE_WORKSPACE);
     return launch_cache_attention(Q, type, q_stride, B, q_heads, layout, codes, scales, table,

@@ -342,6 +342,26 @@ def test_attention_offsets_beyond_32_bits(gpu):
         assert (np.abs(o[0, h].cpu().double().numpy() - r) <= tol).all()
 
 
+def test_attention_withheld_copies_time_out(gpu):
+    """With the test hook on, the kernel's waits run out with nothing in flight: outputs read NaN,
+    the status says so, and the same call is right again after."""
+    s = Scene([40, 700], 1, 4, 64, 8, 16, "bf16", 21)
+    good, lse = s.run()
+    assert binding.mpq_device_status() == 0
+    try:
+        binding.mpq_set_wait_limit(1 << 18)
+        binding.mpq_test_withhold_copies(True)
+        bad, _ = s.run()
+        flags = binding.mpq_device_status()
+    finally:
+        binding.mpq_test_withhold_copies(False)
+        binding.mpq_set_wait_limit(0)
+    assert flags == binding.MPQ_TIMEOUT_ATTENTION
+    assert bool(torch.isnan(bad).all())
+    o, l = s.run()
+    assert torch.equal(o, good) and torch.equal(l, lse) and binding.mpq_device_status() == 0
+
+
 def test_refusals(gpu):
     lay = binding.mpq_cache_layout(4, 16, 2, 64, 8)
     codes, scales = binding.mpq_cache_empty(lay, DEV)
