@@ -297,7 +297,7 @@ cache_attention_kernel(const AttnArgs a, WaitCtl wc, const __grid_constant__ CUt
     __shared__ int sh_list[2 * W];               // the parts that there are, in order
     __shared__ int sh_run[2 * W + 1];            // where runs of parts of one row begin in it
     __shared__ int sh_counts[2];                 // parts, runs
-    __shared__ int sh_last[2];
+    __shared__ int sh_open[2], sh_c0[2], sh_c1[2], sh_last[2];
     __shared__ __align__(16) float sh_slice[W][D];
     griddep_launch();
     const uint32_t raw_u32 = smem_u32(raw);
@@ -398,6 +398,15 @@ cache_attention_kernel(const AttnArgs a, WaitCtl wc, const __grid_constant__ CUt
                                                   // (page x head) and place in the page
         unsigned f_ok = 0;                        // bit per lane: its stage names a page
         unsigned held = 0;                        // the same, bit per ring stage
+        // A row's queries on their way to L1, before its stages are asked for (which they would wait
+        // behind); nothing waits for them here.
+        auto touch_queries = [&](const Row &r) {
+            const int h0 = r.u % a.blocks * H, kv = r.u / a.blocks;
+            const char *const q = reinterpret_cast<const char *>(
+                static_cast<const T *>(a.Q) + a.q_stride * r.b + (size_t)(kv * a.group + h0) * D);
+            const int bytes = min(H, a.group - h0) * D * (int)sizeof(T);
+            for (int i = lane * 128; i < bytes; i += 32 * 128) touch(q + i);
+        };
         auto fetch = [&](int to_slot) {
             if (f_left <= 0) return;
             if (f_i == f_n) {                     // look up the next 32 stages of the row
@@ -406,13 +415,7 @@ cache_attention_kernel(const AttnArgs a, WaitCtl wc, const __grid_constant__ CUt
                     if (f_left <= 0) return;
                     ahead.next(a, units);
                     f_st = 0;
-                    // the row's queries and the next sequence's pages on their way to L1 (unused here:
-                    // nothing waits for them)
-                    const int h0 = ahead.u % a.blocks * H, kv = ahead.u / a.blocks;
-                    const char *const q = reinterpret_cast<const char *>(
-                        static_cast<const T *>(a.Q) + a.q_stride * ahead.b + (size_t)(kv * a.group + h0) * D);
-                    const int bytes = min(H, a.group - h0) * D * (int)sizeof(T);
-                    for (int i = lane * 128; i < bytes; i += 32 * 128) touch(q + i);
+                    touch_queries(ahead);
                     if (lane == 0 && ahead.u == 0 && ahead.b + 1 < a.B)
                         touch(a.table + (size_t)(ahead.b + 1) * a.cols);
                 }
@@ -452,6 +455,7 @@ cache_attention_kernel(const AttnArgs a, WaitCtl wc, const __grid_constant__ CUt
             ++f_st;
             --f_left;
         };
+        touch_queries(at);
         __syncwarp();                             // the barriers are ready
 #pragma unroll 1
         for (int i = 0; i < S::STAGES - 1; ++i) fetch(i);
@@ -787,6 +791,21 @@ cache_attention_kernel(const AttnArgs a, WaitCtl wc, const __grid_constant__ CUt
     }
     __syncthreads();
     const int runs = sh_counts[1];
+    // the rows that other CTAs have parts of, the first run's (begun before) and the last one's, and
+    // their CTAs: those of the workers of the row's first and last stage
+    if (warp == W - 1 && lane < 2) {
+        const Part p = runs > 0 ? sh_part[sh_list[lane ? sh_run[runs - 1] : 0]] : Part{-1, 0, 0, 0};
+        sh_open[lane] = runs > 0 && (lane ? p.starts && !sh_part[sh_list[sh_counts[0] - 1]].ends : !p.starts);
+        if (sh_open[lane]) {
+            long long g0 = sh_pre[p.b / per];
+            for (int b = p.b / per * per; b < p.b; ++b)
+                g0 += (long long)weight(span_of(a, b).stages()) * units;
+            const int n = span_of(a, p.b).stages();
+            g0 += (long long)p.u * weight(n) + A_ROW_COST;
+            sh_c0[lane] = cut.worker(g0) / W;
+            sh_c1[lane] = cut.worker(g0 + n - 1) / W;
+        }
+    }
     const float *const kept = warp_sums + (size_t)blockIdx.x * W * S::SUMS;
     // a warp takes a head of a run at a time, a lane the statistics of a part
     for (int item = warp; item < runs * H; item += W) {
@@ -838,45 +857,27 @@ cache_attention_kernel(const AttnArgs a, WaitCtl wc, const __grid_constant__ CUt
     }
 
     // ---- rows that several CTAs share: this one's first run (begun before) and its last ---------------
-    if (runs == 0) return;
-    const Part in_first = sh_part[sh_list[0]], in_last = sh_part[sh_list[sh_run[runs - 1]]];
-    const bool last_ends = sh_part[sh_list[sh_counts[0] - 1]].ends;
-    const bool open[2] = {!in_first.starts, (bool)in_last.starts && !last_ends};
-    if (!open[0] && !open[1]) return;
-    // the row's CTAs: those of the workers of its first and last stage
-    int c0[2], c1[2];
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        c0[k] = c1[k] = 0;
-        if (!open[k]) continue;
-        const Part p = k ? in_last : in_first;
-        long long g0 = sh_pre[p.b / per];
-        for (int b = p.b / per * per; b < p.b; ++b)
-            g0 += (long long)weight(span_of(a, b).stages()) * units;
-        const int n = span_of(a, p.b).stages();
-        g0 += (long long)p.u * weight(n) + A_ROW_COST;
-        c0[k] = cut.worker(g0) / W;
-        c1[k] = cut.worker(g0 + n - 1) / W;
-    }
-    __threadfence();
     __syncthreads();
     if (tid < 2) {
         sh_last[tid] = 0;
-        if (open[tid]) {
-            sh_last[tid] = atomicAdd(&counters[c0[tid]], 1u) == (unsigned)(c1[tid] - c0[tid]);
-            if (sh_last[tid]) counters[c0[tid]] = 0;
+        if (sh_open[tid]) {
+            // (releases the CTA's sums, which the barrier ordered before it, and acquires the others')
+            unsigned n;
+            asm volatile("atom.add.acq_rel.gpu.u32 %0, [%1], 1;"
+                         : "=r"(n) : "l"(&counters[sh_c0[tid]]) : "memory");
+            sh_last[tid] = n == (unsigned)(sh_c1[tid] - sh_c0[tid]);
+            if (sh_last[tid]) counters[sh_c0[tid]] = 0;
         }
-        __threadfence();
     }
     __syncthreads();
 #pragma unroll 1
     for (int k = 0; k < 2; ++k) {
         if (!sh_last[k]) continue;
-        const Part p = k ? in_last : in_first;
+        const Part p = sh_part[sh_list[k ? sh_run[runs - 1] : 0]];
         const int head0 = p.u % a.blocks * H, heads = min(H, a.group - head0);
-        const int n = c1[k] - c0[k] + 1;
+        const int n = sh_c1[k] - sh_c0[k] + 1;
         // the first CTA's sums are in its second place, the others' in their first
-        const float *const base = cta_sums + (size_t)2 * c0[k] * S::SUMS;
+        const float *const base = cta_sums + (size_t)2 * sh_c0[k] * S::SUMS;
         auto sums = [&](int i) { return base + (size_t)(2 * i + (i == 0 ? 1 : 0)) * S::SUMS; };
         // several warps a head where there are more warps than heads, each a slice of the CTAs
         const int slices = max(1, W / heads);
