@@ -9,7 +9,6 @@ from __future__ import annotations
 
 import ctypes
 import functools
-import math
 import os
 
 import torch
@@ -66,11 +65,11 @@ class KvCache(ctypes.Structure):
                 ("dim", ctypes.c_int), ("bits", ctypes.c_int), ("row_bytes", ctypes.c_int),
                 ("codes_bytes", ctypes.c_size_t), ("scales_bytes", ctypes.c_size_t)]
 
-    @property
+    @functools.cached_property
     def codes_shape(self):
         return (self.pages, 2, self.heads, self.page, self.row_bytes)
 
-    @property
+    @functools.cached_property
     def scales_shape(self):
         return (self.pages, 2, self.heads, self.page)
 
@@ -463,7 +462,22 @@ def mpq_center_weights(W, mode: int = MPQ_CENTER_PER_CHANNEL, center=None, Wc=No
 
 
 # ---------------------------------------------------------------------------------------------
-# Serving in few bits
+# Serving in few bits.  A decode step makes these calls one after another with little work in each,
+# so what a call costs on the host counts: a tensor that is as it should be is seen so in one
+# expression, and outputs allocated here are not looked at again.
+
+
+def _is(t, dtype, shape):
+    """t is a contiguous CUDA tensor of this type and shape."""
+    try:
+        return t.dtype is dtype and t.shape == shape and t.is_cuda and t.is_contiguous()
+    except AttributeError:
+        return False
+
+
+def _need(t, name, dtype, shape):
+    if not _is(t, dtype, shape):
+        _dev(t, name, dtype, shape)
 
 
 def _type(t, name):
@@ -474,24 +488,22 @@ def _type(t, name):
     return got
 
 
-def _rows(t, name, shape, dtype=None):
-    """A CUDA matrix of this shape whose rows are contiguous; returns its row stride."""
+def _rows(t, name, rows, d):
+    """A CUDA matrix [rows][d] whose rows are contiguous and do not overlap; returns its row stride."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch tensor")
     if not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor")
-    if dtype is not None and t.dtype != dtype:
-        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.shape != shape:
-        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    rows, d = shape
+    if t.shape != (rows, d):
+        raise ValueError(f"{name} must have shape {(rows, d)}, got {tuple(t.shape)}")
     step, unit = t.stride()
     if (unit != 1 and d > 1) or (step < d and rows > 1):
         raise ValueError(f"{name} must have contiguous rows that do not overlap")
-    return max(step, d)
+    return step if step > d else d
 
 
 def _packed(t, name, layout):
+    """The address of a packed matrix's buffer."""
     _dev(t, name, torch.uint8)
     if t.numel() < layout.bytes:
         raise ValueError(f"{name} is smaller than layout.bytes = {layout.bytes}")
@@ -509,13 +521,17 @@ def mpq_mx_layout(rows: int, d: int) -> MxMatrix:
 def mpq_mx_quantize(X, layout: MxMatrix = None, packed=None, stream=None):
     """X [rows][d] (fp32, fp16 or bf16; rows may lie apart) to microscaled 4-bit floats: the packed
     buffer (uint8 [layout.bytes]) of mpq_mx_layout(rows, d)."""
-    layout = layout if layout is not None else mpq_mx_layout(*X.shape)
-    ld = _rows(X, "X", (layout.rows, layout.d))
+    if layout is None:
+        layout = mpq_mx_layout(*X.shape)
+    ld = _rows(X, "X", layout.rows, layout.d)
     if packed is None:
-        packed = torch.empty((layout.bytes,), dtype=torch.uint8, device=X.device)
-    to = _packed(packed, "packed", layout)
-    _check(load().mpq_mx_quantize(X.data_ptr(), _type(X.dtype, "X"), ld, layout, to,
-                                  _stream(stream)), "mpq_mx_quantize")
+        packed = torch.empty(layout.bytes, dtype=torch.uint8, device=X.device)
+        to = packed.data_ptr()
+    else:
+        to = _packed(packed, "packed", layout)
+    st = load().mpq_mx_quantize(X.data_ptr(), _type(X.dtype, "X"), ld, layout, to, _stream(stream))
+    if st:
+        _check(st, "mpq_mx_quantize")
     return packed
 
 
@@ -523,10 +539,14 @@ def mpq_mx_dequantize(packed, layout: MxMatrix, dtype=torch.float32, Y=None, str
     """The values [rows][d] of a packed matrix."""
     at = _packed(packed, "packed", layout)
     if Y is None:
-        Y = torch.empty((layout.rows, layout.d), dtype=dtype, device=packed.device)
-    ld = _rows(Y, "Y", (layout.rows, layout.d))
-    _check(load().mpq_mx_dequantize(at, layout, Y.data_ptr(), _type(Y.dtype, "Y"), ld,
-                                    _stream(stream)), "mpq_mx_dequantize")
+        ld = layout.d
+        Y = torch.empty((layout.rows, ld), dtype=dtype, device=packed.device)
+    else:
+        ld = _rows(Y, "Y", layout.rows, layout.d)
+    st = load().mpq_mx_dequantize(at, layout, Y.data_ptr(), _type(Y.dtype, "Y"), ld,
+                                  _stream(stream))
+    if st:
+        _check(st, "mpq_mx_dequantize")
     return Y
 
 
@@ -535,13 +555,19 @@ def mpq_mx_linear(X, x_layout: MxMatrix, W, w_layout: MxMatrix, bias=None, dtype
     """Y [T][C] = X W^T + bias for packed inputs X [T][d] and weights W [C][d]; bias fp32 [C]."""
     x, w = _packed(X, "X", x_layout), _packed(W, "W", w_layout)
     T, C = x_layout.rows, w_layout.rows
+    add = None      # (bias keeps its name: the last reference to it may be this one)
     if bias is not None:
-        _dev(bias, "bias", torch.float32, (C,))
+        _need(bias, "bias", torch.float32, (C,))
+        add = bias.data_ptr()
     if Y is None:
+        ld = C
         Y = torch.empty((T, C), dtype=dtype, device=X.device)
-    ld = _rows(Y, "Y", (T, C))
-    _check(load().mpq_mx_linear(x_layout, x, w_layout, w, _ptr(bias), Y.data_ptr(),
-                                _type(Y.dtype, "Y"), ld, _stream(stream)), "mpq_mx_linear")
+    else:
+        ld = _rows(Y, "Y", T, C)
+    st = load().mpq_mx_linear(x_layout, x, w_layout, w, add, Y.data_ptr(), _type(Y.dtype, "Y"), ld,
+                              _stream(stream))
+    if st:
+        _check(st, "mpq_mx_linear")
     return Y
 
 
@@ -562,47 +588,53 @@ def mpq_cache_empty(layout: KvCache, device):
 
 
 def _storage(layout, codes, scales):
-    _dev(codes, "codes", torch.uint8, layout.codes_shape)
-    _dev(scales, "scales", torch.float32, layout.scales_shape)
+    """The addresses of a cache's codes and scales."""
+    _need(codes, "codes", torch.uint8, layout.codes_shape)
+    _need(scales, "scales", torch.float32, layout.scales_shape)
+    return codes.data_ptr(), scales.data_ptr()
 
 
 def mpq_cache_write(K, V, slots, layout: KvCache, codes, scales, stream=None):
     """Quantises K and V [T][heads][dim] (fp32, fp16 or bf16; tokens and heads may lie apart, the same
     for both) into the slots [T] int64 of the cache; slots outside it are skipped."""
+    _need(slots, "slots", torch.int64, slots.shape[:1])
     shape = (slots.shape[0], layout.heads, layout.dim)
+    steps = K.stride()
     for t, name in ((K, "K"), (V, "V")):
         if not t.is_cuda:
             raise ValueError(f"{name} must be a CUDA tensor")
         if t.shape != shape:
             raise ValueError(f"{name} must have shape {shape}, got {tuple(t.shape)}")
-        if t.stride(2) != 1:
-            raise ValueError(f"{name} must have contiguous rows")
-    if K.dtype != V.dtype or K.stride() != V.stride():
+    if K.dtype != V.dtype or steps != V.stride():
         raise ValueError("K and V must have one type and the same strides")
-    _dev(slots, "slots", torch.int64, (shape[0],))
-    _storage(layout, codes, scales)
-    _check(load().mpq_cache_write(K.data_ptr(), V.data_ptr(), _type(K.dtype, "K"), K.stride(0),
-                                  K.stride(1), shape[0], slots.data_ptr(), layout,
-                                  codes.data_ptr(), scales.data_ptr(), _stream(stream)),
-           "mpq_cache_write")
+    if steps[2] != 1:
+        raise ValueError("K and V must have contiguous rows")
+    at, sc = _storage(layout, codes, scales)
+    st = load().mpq_cache_write(K.data_ptr(), V.data_ptr(), _type(K.dtype, "K"), steps[0], steps[1],
+                                shape[0], slots.data_ptr(), layout, at, sc, _stream(stream))
+    if st:
+        _check(st, "mpq_cache_write")
 
 
 def mpq_cache_read(slots, layout: KvCache, codes, scales, dtype=torch.bfloat16, K=None, V=None,
                    stream=None):
     """The keys and values [T][heads][dim] that the cache holds in the slots [T] int64 (zeros for one
     outside it)."""
-    _dev(slots, "slots", torch.int64, slots.shape[:1])
-    _storage(layout, codes, scales)
+    _need(slots, "slots", torch.int64, slots.shape[:1])
+    at, sc = _storage(layout, codes, scales)
     shape = (slots.shape[0], layout.heads, layout.dim)
     if K is None:
         K = torch.empty(shape, dtype=dtype, device=slots.device)
+    else:
+        _need(K, "K", K.dtype, shape)
     if V is None:
         V = torch.empty(shape, dtype=K.dtype, device=slots.device)
-    _dev(K, "K", K.dtype, shape)
-    _dev(V, "V", K.dtype, shape)
-    _check(load().mpq_cache_read(slots.data_ptr(), shape[0], layout, codes.data_ptr(),
-                                 scales.data_ptr(), K.data_ptr(), V.data_ptr(),
-                                 _type(K.dtype, "K"), _stream(stream)), "mpq_cache_read")
+    else:
+        _need(V, "V", K.dtype, shape)
+    st = load().mpq_cache_read(slots.data_ptr(), shape[0], layout, at, sc, K.data_ptr(),
+                               V.data_ptr(), _type(K.dtype, "K"), _stream(stream))
+    if st:
+        _check(st, "mpq_cache_read")
     return K, V
 
 
@@ -614,30 +646,34 @@ def mpq_cache_attention(Q, table, lens, layout: KvCache, codes, scales, scale: f
     tensor that receives the logarithm of the softmax's sum.  workspace: MPQ_CACHE_WORKSPACE bytes,
     zeroed before the first call and kept from call to call (by default taken from the pool)."""
     B, cols = table.shape
-    if Q.dim() != 3 or Q.shape[0] != B or Q.shape[2] != layout.dim:
-        raise ValueError(f"Q must have shape ({B}, q_heads, {layout.dim}), got {tuple(Q.shape)}")
+    shape, dim = Q.shape, layout.dim
+    if len(shape) != 3 or shape[0] != B or shape[2] != dim:
+        raise ValueError(f"Q must have shape ({B}, q_heads, {dim}), got {tuple(shape)}")
     if not Q.is_cuda:
         raise ValueError("Q must be a CUDA tensor")
-    q_heads = Q.shape[1]
-    if Q.stride(2) != 1 or (q_heads > 1 and Q.stride(1) != layout.dim):
+    q_heads, steps = shape[1], Q.stride()
+    if steps[2] != 1 or (q_heads > 1 and steps[1] != dim):
         raise ValueError("Q must have consecutive heads")
-    _dev(table, "table", torch.int32)
-    _dev(lens, "lens", torch.int32, (B,))
-    _storage(layout, codes, scales)
+    _need(table, "table", torch.int32, (B, cols))
+    _need(lens, "lens", torch.int32, (B,))
+    at, sc = _storage(layout, codes, scales)
     if O is None:
-        O = torch.empty((B, q_heads, layout.dim), dtype=Q.dtype, device=Q.device)
-    _dev(O, "O", Q.dtype, (B, q_heads, layout.dim))
+        O = torch.empty(shape, dtype=Q.dtype, device=Q.device)
+    else:
+        _need(O, "O", Q.dtype, shape)
+    ws = size = log = None
     if lse is not None:
-        _dev(lse, "lse", torch.float32, (B, q_heads))
+        _need(lse, "lse", torch.float32, (B, q_heads))
+        log = lse.data_ptr()
     if workspace is not None:
         _dev(workspace, "workspace", torch.uint8)
-    if scale is None:
-        scale = 1.0 / math.sqrt(layout.dim)
-    _check(load().mpq_cache_attention(
-        Q.data_ptr(), _type(Q.dtype, "Q"), Q.stride(0), B, q_heads, layout, codes.data_ptr(),
-        scales.data_ptr(), table.data_ptr(), cols, lens.data_ptr(), scale, window, O.data_ptr(),
-        _ptr(lse), _ptr(workspace), 0 if workspace is None else workspace.numel(),
-        _stream(stream)), "mpq_cache_attention")
+        ws, size = workspace.data_ptr(), workspace.numel()
+    st = load().mpq_cache_attention(
+        Q.data_ptr(), _type(Q.dtype, "Q"), steps[0], B, q_heads, layout, at, sc, table.data_ptr(),
+        cols, lens.data_ptr(), dim ** -0.5 if scale is None else scale, window, O.data_ptr(), log,
+        ws, size or 0, _stream(stream))
+    if st:
+        _check(st, "mpq_cache_attention")
     return O
 
 

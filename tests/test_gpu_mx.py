@@ -228,6 +228,18 @@ def test_chain_of_dependent_calls(gpu):
         assert torch.equal(y, want)
 
 
+def test_linear_keeps_a_temporary_bias(gpu):
+    """A bias that nothing but the call refers to is not overwritten by the output allocated in it."""
+    T, C = 1, 600
+    lay, wl = binding.mpq_mx_layout(T, 64), binding.mpq_mx_layout(C, 64)
+    x = binding.mpq_mx_quantize(torch.zeros(T, 64, device=DEV), lay)
+    w = binding.mpq_mx_quantize(torch.zeros(C, 64, device=DEV), wl)
+    for i in range(20):
+        y = binding.mpq_mx_linear(x, lay, w, wl, bias=torch.full((C,), float(i), device=DEV),
+                                  dtype=torch.float32)
+        assert bool((y == i).all())
+
+
 def test_refusals(gpu):
     x = torch.zeros(4, 64, device=DEV)
     lay = binding.mpq_mx_layout(4, 64)
