@@ -1,5 +1,5 @@
-// Inputs and outputs of the few-bit operators in fp32, fp16 or bf16: eight elements at a time, as two
-// or one 16-byte accesses where the rows are aligned, else one by one.
+// Inputs and outputs of the few-bit operators in fp32, fp16 or bf16: eight elements at a time, as one
+// access of 32 or 16 bytes (two of 16) where the rows are aligned, else one by one.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -50,6 +50,13 @@ __device__ __forceinline__ uint32_t pack2(float a, float b, __nv_bfloat16)
 // what they read may have been written by the kernel before.
 __device__ __forceinline__ void load8(const float *p, float (&v)[8])
 {
+    if (((uintptr_t)p & 31) == 0) {      // one 32-byte access
+        asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]),
+                       "=f"(v[6]), "=f"(v[7])
+                     : "l"(__cvta_generic_to_global(p)) : "memory");
+        return;
+    }
     const float4 a = reinterpret_cast<const float4 *>(p)[0];
     const float4 b = reinterpret_cast<const float4 *>(p)[1];
     v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
@@ -68,8 +75,25 @@ __device__ __forceinline__ void load8(const T *p, float (&v)[8])
     }
 }
 
+// max |x| of eight elements as fp32 bits: the order of non-negative floats, infinities and NaN above
+// every finite value.
+__device__ __forceinline__ uint32_t top8(const float (&v)[8])
+{
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
+    return top;
+}
+
 __device__ __forceinline__ void store8(float *p, const float (&v)[8])
 {
+    if (((uintptr_t)p & 31) == 0) {
+        asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                     :: "l"(__cvta_generic_to_global(p)), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]),
+                        "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7])
+                     : "memory");
+        return;
+    }
     reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
     reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
 }

@@ -2,10 +2,18 @@
 // slots back (mpq_cache_read).
 //
 // A row is what one token keeps for one head (its key, or its value): s = max|x| (1 / Qmax), one fp32
-// product, codes clamp(rint(x / s)) as Eq. 8's, by one correctly rounded division each.  A thread takes 8 elements
-// of a row, so dim / 8 threads (8, 16 or 32 of a warp) share its maximum by shuffles, and its codes
-// leave in one store of 8 or 4 bytes a thread.  Memory-bound: an element's own bytes on one side,
-// bits / 8 + 4 / dim bytes on the other; slots scatter rows of 32 to 256 bytes, whole sectors.
+// product, codes clamp(rint(x / s)) as Eq. 8's.  A thread takes 8 elements of a token's key and value
+// row of one head (both are on their way before either is used), so dim / 8 threads (8, 16 or 32 of
+// a warp) share the rows' maxima by shuffles, and their codes leave in one store of 8 or 4 bytes a
+// thread and row.
+//
+// Codes are screened by the reciprocal: with r = fl(1 / s) normal, y = fl(x r) is within 2^-15 of the
+// quotient x / s (|x / s| <= 127 (1 + 2^-22), two roundings of 2^-24 and the division's own), so rint(y)
+// is the code unless y lies within 2^-14 of halfway between two integers; those elements, and rows
+// whose scale has no normal reciprocal, are divided.
+//
+// Memory-bound: an element's own bytes on one side, bits / 8 + 4 / dim bytes on the other; slots scatter
+// rows of 32 to 256 bytes, whole sectors.
 #include <math.h>
 #include <string.h>
 
@@ -20,82 +28,136 @@ namespace {
 
 constexpr int KV_THREADS = 256;
 
-// A thread's row: token, key or value, head, and its first element.
+// A thread's place: token, head (blockIdx.y), and its first element of both rows.
 struct RowAt {
-    int t, kv, h, j0;
+    int t, h, j0;
 };
 __device__ __forceinline__ bool row_at(int T, const mpq_kv_cache &L, RowAt &at)
 {
-    const unsigned per = (unsigned)L.dim / 8;
-    const unsigned r = blockIdx.x * (KV_THREADS / per) + threadIdx.x / per;
-    const unsigned of_token = 2u * (unsigned)L.heads;
-    at.t = (int)(r / of_token);
-    const unsigned rest = r - (unsigned)at.t * of_token;
-    at.kv = rest >= (unsigned)L.heads;
-    at.h = (int)rest - at.kv * L.heads;
-    at.j0 = (int)(threadIdx.x & (per - 1)) * 8;
+    const int shift = L.dim == 64 ? 3 : L.dim == 128 ? 4 : 5;       // of dim / 8 threads a row
+    at.t = (int)(blockIdx.x * (unsigned)(KV_THREADS >> shift) + (threadIdx.x >> shift));
+    at.h = (int)blockIdx.y;
+    at.j0 = (int)(threadIdx.x & ((1u << shift) - 1u)) * 8;
     return at.t < T;
 }
 
-// Index of a slot's row among the cache's rows, or -1 for a slot outside it.
-__device__ __forceinline__ long long cache_row(long long slot, const mpq_kv_cache &L, int kv, int h)
+// Index of a slot's key row among the cache's rows (its value row is heads * page further), or -1 for
+// a slot outside the cache.
+__device__ __forceinline__ long long cache_row(long long slot, const mpq_kv_cache &L, int h)
 {
     if (slot < 0 || slot >= (long long)L.pages * L.page) return -1;
-    const long long page = slot / L.page;
-    return ((page * 2 + kv) * L.heads + h) * L.page + (slot - page * L.page);
+    const long long page = (slot >> 32) == 0 ? (long long)((unsigned)slot / (unsigned)L.page)
+                                             : slot / L.page;
+    return (page * 2 * L.heads + h) * L.page + (slot - page * L.page);
+}
+
+// max |x| of a row as bits (infinities and NaN above every finite value), over its `per` threads.
+__device__ __forceinline__ uint32_t row_top(const float (&v)[8], unsigned per, unsigned lanes)
+{
+    uint32_t top = top8(v);
+    for (unsigned o = 1; o < per; o <<= 1) top = max(top, __shfl_xor_sync(lanes, top, o));
+    return top;
+}
+
+// The codes of 8 elements, offset by Qmax + 1, in the low bits of each word, and the row's scale.
+__device__ __forceinline__ float row_codes(const float (&v)[8], uint32_t top, int qmax,
+                                           float inv_qmax, uint32_t (&u)[8])
+{
+    const bool bad = top >= 0x7f800000u;
+    const float s = bad ? NAN : __fmul_rn(__uint_as_float(top), inv_qmax);
+    const int zero = qmax + 1;
+    if (!(s > 0.0f)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) u[i] = (uint32_t)zero;
+        return s;
+    }
+    const float r = __frcp_rn(s);
+    bool near = s < 0x1p-120f || r < 0x1p-120f;
+    const float magic = 12582912.0f + (float)zero;      // 3 2^22 + offset: the sum's low bits are the code
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float y = __fmul_rn(v[i], r), t = __fadd_rn(y, magic);
+        near |= fabsf(__fsub_rn(y, __fsub_rn(t, magic))) > 0.5f - 0x1p-14f;
+        u[i] = __float_as_uint(t);
+    }
+    if (near) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            u[i] = (uint32_t)(min(max(__float2int_rn(__fdiv_rn(v[i], s)), -qmax), qmax) + zero);
+    }
+    return s;
+}
+
+__device__ __forceinline__ uint32_t low_bytes(const uint32_t *u)
+{
+    return __byte_perm(__byte_perm(u[0], u[1], 0x0040), __byte_perm(u[2], u[3], 0x0040), 0x5410);
+}
+
+// Stores a thread's 8 codes and, by the row's first thread, its scale.
+__device__ __forceinline__ void store_row(const uint32_t (&u)[8], float s, long long row, int j0,
+                                          const mpq_kv_cache &L, unsigned char *codes, float *scales)
+{
+    if (!MPQ_IN(row, (size_t)L.pages * 2 * L.heads * L.page)) return;
+    unsigned char *const out = codes + row * L.row_bytes;
+    if (L.bits == 8) {
+        *reinterpret_cast<uint2 *>(out + j0) = make_uint2(low_bytes(u), low_bytes(u + 4));
+    } else {
+        uint32_t w = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w |= (u[i] & 15u) << (4 * i);
+        *reinterpret_cast<uint32_t *>(out + j0 / 2) = w;
+    }
+    if (j0 == 0) scales[row] = s;
 }
 
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(KV_THREADS)
 cache_write_kernel(const T *K, const T *V, long long ld_token, long long ld_head, int n,
-                   const int64_t *slots, mpq_kv_cache L, unsigned char *codes, float *scales)
+                   const int64_t *slots, mpq_kv_cache L, float inv_qmax, unsigned char *codes,
+                   float *scales)
 {
     sm100::griddep_launch();
     sm100::griddep_wait();
     RowAt at;
     if (!row_at(n, L, at)) return;   // whole rows (dim / 8 threads) leave together
-    const long long row = cache_row(slots[at.t], L, at.kv, at.h);
-    if (row < 0) return;
-    const T *x = (at.kv ? V : K) + ld_token * at.t + ld_head * at.h + at.j0;
-    float v[8];
+    const long long slot = slots[at.t];
+    const long long from = ld_token * at.t + ld_head * at.h + at.j0;
+    float k[8], v[8];
     if (VEC) {
-        load8(x, v);
+        load8(K + from, k);
+        load8(V + from, v);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = to_f32(x[i]);
+        for (int i = 0; i < 8; ++i) {
+            k[i] = to_f32(K[from + i]);
+            v[i] = to_f32(V[from + i]);
+        }
     }
-    // max |x| as bits (infinities and NaN above every finite value), over the row's threads
-    uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
+    const long long row = cache_row(slot, L, at.h);
+    if (row < 0) return;
     const unsigned per = (unsigned)L.dim / 8;
     const unsigned lanes = per == 32 ? 0xffffffffu : ((1u << per) - 1u)
                                                          << (threadIdx.x & 31 & ~(per - 1));
-    for (unsigned o = 1; o < per; o <<= 1) top = max(top, __shfl_xor_sync(lanes, top, o));
     const int qmax = (1 << (L.bits - 1)) - 1;
-    const bool bad = top >= 0x7f800000u;
-    const float s = bad ? NAN : __fmul_rn(__uint_as_float(top), __fdiv_rn(1.0f, (float)qmax));
+    const uint32_t k_top = row_top(k, per, lanes), v_top = row_top(v, per, lanes);
     uint32_t u[8];
+    float s = row_codes(k, k_top, qmax, inv_qmax, u);
+    store_row(u, s, row, at.j0, L, codes, scales);
+    s = row_codes(v, v_top, qmax, inv_qmax, u);
+    store_row(u, s, row + (long long)L.heads * L.page, at.j0, L, codes, scales);
+}
+
+// The values of 8 codes (in one or two words) with a scale.
+__device__ __forceinline__ void row_values(uint2 w, float s, int bits, float (&v)[8])
+{
+    if (bits == 8) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        int q = 0;
-        if (s > 0.0f) q = min(max(__float2int_rn(__fdiv_rn(v[i], s)), -qmax), qmax);
-        u[i] = (uint32_t)(q + qmax + 1);
-    }
-    const size_t rows = (size_t)L.pages * 2 * L.heads * L.page;
-    if (!MPQ_IN(row, rows)) return;
-    unsigned char *out = codes + row * L.row_bytes;
-    if (L.bits == 8) {
-        *reinterpret_cast<uint2 *>(out + at.j0) =
-            make_uint2(u[0] | u[1] << 8 | u[2] << 16 | u[3] << 24,
-                       u[4] | u[5] << 8 | u[6] << 16 | u[7] << 24);
+        for (int i = 0; i < 8; ++i)
+            v[i] = s * (float)((int)(((i < 4 ? w.x : w.y) >> (8 * (i & 3))) & 255u) - 128);
     } else {
-        uint32_t w = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w |= u[i] << (4 * i);
-        *reinterpret_cast<uint32_t *>(out + at.j0 / 2) = w;
+        for (int i = 0; i < 8; ++i) v[i] = s * (float)((int)((w.x >> (4 * i)) & 15u) - 8);
     }
-    if (at.j0 == 0) scales[row] = s;
 }
 
 template <typename T>
@@ -107,34 +169,35 @@ cache_read_kernel(const int64_t *slots, int n, mpq_kv_cache L, const unsigned ch
     sm100::griddep_wait();
     RowAt at;
     if (!row_at(n, L, at)) return;
-    const long long row = cache_row(slots[at.t], L, at.kv, at.h);
-    float v[8];
-    if (row < 0) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = 0.0f;
-    } else {
-        const float s = scales[row];
-        const unsigned char *in = codes + row * L.row_bytes;
+    const long long row = cache_row(slots[at.t], L, at.h);
+    const long long v_row = row + (long long)L.heads * L.page;
+    uint2 kw = make_uint2(0, 0), vw = make_uint2(0, 0);
+    float ks = 0.0f, vs = 0.0f;      // (a slot outside the cache: zeros)
+    if (row >= 0) {
+        ks = scales[row];
+        vs = scales[v_row];
         if (L.bits == 8) {
-            const uint2 w = *reinterpret_cast<const uint2 *>(in + at.j0);
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                v[i] = s * (float)((int)(((i < 4 ? w.x : w.y) >> (8 * (i & 3))) & 255u) - 128);
+            kw = *reinterpret_cast<const uint2 *>(codes + row * L.row_bytes + at.j0);
+            vw = *reinterpret_cast<const uint2 *>(codes + v_row * L.row_bytes + at.j0);
         } else {
-            const uint32_t w = *reinterpret_cast<const uint32_t *>(in + at.j0 / 2);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = s * (float)((int)((w >> (4 * i)) & 15u) - 8);
+            kw.x = *reinterpret_cast<const uint32_t *>(codes + row * L.row_bytes + at.j0 / 2);
+            vw.x = *reinterpret_cast<const uint32_t *>(codes + v_row * L.row_bytes + at.j0 / 2);
         }
     }
+    float v[8];
     const size_t to = ((size_t)at.t * L.heads + at.h) * L.dim + at.j0;
-    if (MPQ_IN(to + 7, (size_t)n * L.heads * L.dim)) store8((at.kv ? V : K) + to, v);
+    if (!MPQ_IN(to + 7, (size_t)n * L.heads * L.dim)) return;
+    row_values(kw, ks, L.bits, v);
+    store8(K + to, v);
+    row_values(vw, vs, L.bits, v);
+    store8(V + to, v);
 }
 
-// Blocks of KV_THREADS threads for T tokens' rows.
-unsigned kv_blocks(int T, const mpq_kv_cache *L)
+// Blocks of KV_THREADS threads for T tokens' rows, by head.
+dim3 kv_grid(int T, const mpq_kv_cache *L)
 {
     const long long per_block = KV_THREADS / (L->dim / 8);
-    return (unsigned)(((long long)T * 2 * L->heads + per_block - 1) / per_block);
+    return dim3((unsigned)((T + per_block - 1) / per_block), (unsigned)L->heads, 1);
 }
 
 }  // namespace
@@ -163,9 +226,10 @@ mpq_status launch_cache_write(const void *K, const void *V, int type, long long 
     return by_type(type, [&](auto t) {
         using E = decltype(t);
         return launch_waiting(vec ? cache_write_kernel<E, true> : cache_write_kernel<E, false>,
-                              dim3(kv_blocks(T, L)), dim3(KV_THREADS), 0, stream,
+                              kv_grid(T, L), dim3(KV_THREADS), 0, stream,
                               "cache write launch", static_cast<const E *>(K),
                               static_cast<const E *>(V), ld_token, ld_head, T, slots, *L,
+                              1.0f / (float)((1 << (L->bits - 1)) - 1),
                               static_cast<unsigned char *>(codes), scales);
     });
 }
@@ -175,7 +239,7 @@ mpq_status launch_cache_read(const int64_t *slots, int T, const mpq_kv_cache *L,
 {
     return by_type(type, [&](auto t) {
         using E = decltype(t);
-        return launch_waiting(cache_read_kernel<E>, dim3(kv_blocks(T, L)), dim3(KV_THREADS), 0,
+        return launch_waiting(cache_read_kernel<E>, kv_grid(T, L), dim3(KV_THREADS), 0,
                               stream, "cache read launch", slots, T, *L,
                               static_cast<const unsigned char *>(codes), scales,
                               static_cast<E *>(K), static_cast<E *>(V));

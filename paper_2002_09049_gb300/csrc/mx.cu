@@ -5,9 +5,8 @@
 // range is far below half the smallest level), so the one rounding of an element is the conversion to
 // E2M1.  amax / 2^e lies in [4, 8): nothing but (6, 8) saturates.
 //
-// A thread takes 8 consecutive elements, 4 threads a block, 16 threads the 128 elements of a scale
-// tile's row, so that a tile row's 4 scale bytes leave in one store.  Memory-bound: an element costs
-// its own bytes in and 17/32 of a byte out; the arithmetic is about 4 instructions an element.
+// A thread takes 8 consecutive elements, 4 threads a block of 32, 16 threads the 128 elements of a
+// scale tile's row.  Memory-bound: an element costs its own bytes in and 17/32 of a byte out.
 #include <math.h>
 #include <string.h>
 
@@ -60,15 +59,21 @@ __device__ __forceinline__ void e2m1x8_values(uint32_t w, float (&v)[8])
     }
 }
 
-// The thread's place: row and 8-element group of the row (d_pad / 8 groups); rows past the matrix
+// Rows a thread takes, blockDim.y apart: their loads are all on their way before the first is used
+// (16 bytes a thread and row of 16-bit elements; one row is as much in fp32).
+template <typename T>
+constexpr int MX_ROWS = sizeof(T) == 4 ? 1 : 2;
+
+// The thread's first row and its 8-element group of the rows (d_pad / 8 groups); rows past the matrix
 // belong to its last row tile.
 struct Place {
     long long row;
     int group;
 };
+template <int ROWS>
 __device__ __forceinline__ Place place()
 {
-    return {(long long)blockIdx.x * blockDim.y + threadIdx.y,
+    return {(long long)blockIdx.x * (blockDim.y * ROWS) + threadIdx.y,
             (int)(blockIdx.y * blockDim.x + threadIdx.x)};
 }
 
@@ -78,48 +83,50 @@ mx_quantize_kernel(const T *X, long long ldx, mpq_mx_matrix L, unsigned char *pa
 {
     sm100::griddep_launch();
     sm100::griddep_wait();
-    const Place at = place();
+    constexpr int ROWS = MX_ROWS<T>;
+    const Place at = place<ROWS>();
+    const int j0 = at.group * 8;
     // d_pad / 8 is a multiple of 16: the 16 threads of a tile row leave together
-    if (at.group * 8 >= L.d_pad || at.row >= (long long)L.row_tiles * 128) return;
+    if (j0 >= L.d_pad) return;
     const unsigned half = (threadIdx.y * blockDim.x + threadIdx.x) & 16;   // of the warp
     const unsigned part = 0xffffu << half;
-    const bool real = at.row < L.rows;
-    const int j0 = at.group * 8;
-    float v[8];
-    const T *x = X + at.row * ldx + j0;
-    if (VEC && real && j0 + 8 <= L.d) {
-        load8(x, v);
-    } else {
+    float v[ROWS][8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = real && j0 + i < L.d ? to_f32(x[i]) : 0.0f;
+    for (int r = 0; r < ROWS; ++r) {
+        const long long row = at.row + r * (int)blockDim.y;
+        const bool real = row < L.rows;
+        const T *x = X + row * ldx + j0;
+        if (VEC && real && j0 + 8 <= L.d) {
+            load8(x, v[r]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[r][i] = real && j0 + i < L.d ? to_f32(x[i]) : 0.0f;
+        }
     }
-    // amax as bits: the order of non-negative floats, infinities and NaN above every finite value
-    uint32_t top = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
-    top = max(top, __shfl_xor_sync(part, top, 1));
-    top = max(top, __shfl_xor_sync(part, top, 2));
-    const bool bad = top >= 0x7f800000u;
-    // E = e + 127: the exponent field less 2; below 2^-125 (subnormal or nearly) e stays at -127
-    const int field = (int)(top >> 23);
-    const int E = bad ? 255 : (field > 2 ? field - 2 : 0);
-    const float inv = bad ? 0.0f : __uint_as_float((uint32_t)(254 - E) << 23);   // 2^-e, e <= 125
+    for (int r = 0; r < ROWS; ++r) {
+        const long long row = at.row + r * (int)blockDim.y;
+        if (row >= (long long)L.row_tiles * 128) return;
+        uint32_t top = top8(v[r]);
+        top = max(top, __shfl_xor_sync(part, top, 1));
+        top = max(top, __shfl_xor_sync(part, top, 2));
+        const bool bad = top >= 0x7f800000u;
+        // E = e + 127: the exponent field less 2; below 2^-125 (subnormal or nearly) e stays at -127
+        const int field = (int)(top >> 23);
+        const int E = bad ? 255 : (field > 2 ? field - 2 : 0);
+        const float inv = __uint_as_float((uint32_t)(254 - E) << 23);   // 2^-e, e <= 125
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = bad ? 0.0f : v[i] * inv;
-    // (rows past the last fill what is left up to the scales with zero codes)
-    const size_t to_codes = (size_t)at.row * (L.d_pad / 2) + j0 / 2;
-    if (to_codes < L.off_scales) *reinterpret_cast<uint32_t *>(packed + to_codes) = e2m1x8(v);
-    // the tile row's four scales, from threads 0, 4, 8 and 12 of its 16
-    const uint32_t b0 = (uint32_t)E;
-    const uint32_t b1 = __shfl_sync(part, b0, half + 4), b2 = __shfl_sync(part, b0, half + 8),
-                   b3 = __shfl_sync(part, b0, half + 12);
-    if ((threadIdx.x & 15) == 0) {
-        const size_t to = L.off_scales +
-                          ((size_t)(at.row >> 7) * L.k_tiles + (at.group >> 4)) * 512 +
-                          scale_at((int)(at.row & 127));
-        if (MPQ_IN(to + 3, L.bytes))
-            *reinterpret_cast<uint32_t *>(packed + to) =
-                real ? b0 | (b1 << 8) | (b2 << 16) | (b3 << 24) : 0u;
+        for (int i = 0; i < 8; ++i) v[r][i] *= inv;
+        // (rows past the last fill what is left up to the scales with zero codes)
+        const size_t to_codes = (size_t)row * (L.d_pad / 2) + j0 / 2;
+        if (to_codes < L.off_scales)
+            *reinterpret_cast<uint32_t *>(packed + to_codes) = bad ? 0u : e2m1x8(v[r]);
+        if ((threadIdx.x & 3) == 0) {    // the block's scale: a tile row's four are consecutive bytes
+            const size_t to = L.off_scales +
+                              ((size_t)(row >> 7) * L.k_tiles + (at.group >> 4)) * 512 +
+                              scale_at((int)(row & 127)) + ((at.group >> 2) & 3);
+            if (MPQ_IN(to, L.bytes)) packed[to] = (unsigned char)(row < L.rows ? E : 0);
+        }
     }
 }
 
@@ -129,7 +136,7 @@ mx_dequantize_kernel(const unsigned char *packed, mpq_mx_matrix L, T *Y, long lo
 {
     sm100::griddep_launch();
     sm100::griddep_wait();
-    const Place at = place();
+    const Place at = place<1>();
     const int j0 = at.group * 8;
     if (j0 >= L.d || at.row >= L.rows) return;
     const uint32_t w = sm100::ld_after_wait(
@@ -192,9 +199,10 @@ mpq_status launch_mx_quantize(const void *X, int x_type, long long ldx, const mp
 {
     const bool vec = rows_aligned(X, x_type, ldx);
     unsigned char *out = static_cast<unsigned char *>(packed);
-    const dim3 block = mx_block(L), grid = mx_grid(L, (long long)L->row_tiles * 128, block);
+    const dim3 block = mx_block(L);
     return by_type(x_type, [&](auto t) {
         using T = decltype(t);
+        const dim3 grid = mx_grid(L, ((long long)L->row_tiles * 128 + MX_ROWS<T> - 1) / MX_ROWS<T>, block);
         return launch_waiting(vec ? mx_quantize_kernel<T, true> : mx_quantize_kernel<T, false>, grid,
                               block, 0, stream, "mx quantize launch", static_cast<const T *>(X), ldx,
                               *L, out);
