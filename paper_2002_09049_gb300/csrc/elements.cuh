@@ -75,14 +75,23 @@ __device__ __forceinline__ void load8(const T *p, float (&v)[8])
     }
 }
 
-// max |x| of eight elements as fp32 bits: the order of non-negative floats, infinities and NaN above
-// every finite value.
-__device__ __forceinline__ uint32_t top8(const float (&v)[8])
+// max(|a|, |b|, |c|); NaN if any is.
+__device__ __forceinline__ float max_abs(float a, float b, float c)
 {
-    uint32_t top = 0;
+    float r;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+
+// max |x| of N elements (even) as fp32 bits: the order of non-negative floats, infinities and NaN above
+// every finite value.
+template <int N>
+__device__ __forceinline__ uint32_t top_bits(const float (&v)[N])
+{
+    float m = max_abs(v[0], v[1], v[1]);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
-    return top;
+    for (int i = 2; i < N; i += 2) m = max_abs(m, v[i], v[i + 1]);
+    return __float_as_uint(m);
 }
 
 __device__ __forceinline__ void store8(float *p, const float (&v)[8])
@@ -103,6 +112,63 @@ __device__ __forceinline__ void store8(T *p, const float (&v)[8])
     *reinterpret_cast<uint4 *>(p) =
         make_uint4(pack2(v[0], v[1], T()), pack2(v[2], v[3], T()), pack2(v[4], v[5], T()),
                    pack2(v[6], v[7], T()));
+}
+
+// Sixteen elements from p on, to p on (16-byte aligned): 32-byte accesses where p is 32-byte aligned.
+template <typename T>
+__device__ __forceinline__ void load16(const T *p, float (&v)[16])
+{
+    if constexpr (sizeof(T) == 4) {
+        float a[8], b[8];
+        load8(p, a);
+        load8(p + 8, b);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = a[i], v[8 + i] = b[i];
+    } else {
+        uint32_t w[8];
+        if (((uintptr_t)p & 31) == 0) {
+            asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                         : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]),
+                           "=r"(w[6]), "=r"(w[7])
+                         : "l"(__cvta_generic_to_global(p)) : "memory");
+        } else {
+            const uint4 a = reinterpret_cast<const uint4 *>(p)[0];
+            const uint4 b = reinterpret_cast<const uint4 *>(p)[1];
+            w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w;
+            w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float2 f = unpack2(w[i], T());
+            v[2 * i] = f.x;
+            v[2 * i + 1] = f.y;
+        }
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void store16(T *p, const float (&v)[16])
+{
+    if constexpr (sizeof(T) == 4) {
+        float a[8], b[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) a[i] = v[i], b[i] = v[8 + i];
+        store8(p, a);
+        store8(p + 8, b);
+    } else {
+        uint32_t w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = pack2(v[2 * i], v[2 * i + 1], T());
+        if (((uintptr_t)p & 31) == 0) {
+            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                         :: "l"(__cvta_generic_to_global(p)), "r"(w[0]), "r"(w[1]), "r"(w[2]),
+                            "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                         : "memory");
+        } else {
+            reinterpret_cast<uint4 *>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+            reinterpret_cast<uint4 *>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+        }
+    }
 }
 
 // Host: bytes of an element type, 0 for a number that names none.

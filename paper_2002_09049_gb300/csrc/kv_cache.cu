@@ -54,7 +54,7 @@ __device__ __forceinline__ long long cache_row(long long slot, const mpq_kv_cach
 // max |x| of a row as bits (infinities and NaN above every finite value), over its `per` threads.
 __device__ __forceinline__ uint32_t row_top(const float (&v)[8], unsigned per, unsigned lanes)
 {
-    uint32_t top = top8(v);
+    uint32_t top = top_bits(v);
     for (unsigned o = 1; o < per; o <<= 1) top = max(top, __shfl_xor_sync(lanes, top, o));
     return top;
 }
@@ -72,17 +72,13 @@ __device__ __forceinline__ float row_codes(const float (&v)[8], uint32_t top, in
         return s;
     }
     const float r = __frcp_rn(s);
-    bool near = s < 0x1p-120f || r < 0x1p-120f;
+    const bool tiny = s < 0x1p-120f || r < 0x1p-120f;
     const float magic = 12582912.0f + (float)zero;      // 3 2^22 + offset: the sum's low bits are the code
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const float y = __fmul_rn(v[i], r), t = __fadd_rn(y, magic);
-        near |= fabsf(__fsub_rn(y, __fsub_rn(t, magic))) > 0.5f - 0x1p-14f;
         u[i] = __float_as_uint(t);
-    }
-    if (near) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
+        if (tiny || fabsf(__fsub_rn(y, __fsub_rn(t, magic))) > 0.5f - 0x1p-14f)
             u[i] = (uint32_t)(min(max(__float2int_rn(__fdiv_rn(v[i], s)), -qmax), qmax) + zero);
     }
     return s;

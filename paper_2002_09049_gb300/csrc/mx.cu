@@ -5,8 +5,8 @@
 // range is far below half the smallest level), so the one rounding of an element is the conversion to
 // E2M1.  amax / 2^e lies in [4, 8): nothing but (6, 8) saturates.
 //
-// A thread takes 8 consecutive elements, 4 threads a block of 32, 16 threads the 128 elements of a
-// scale tile's row.  Memory-bound: an element costs its own bytes in and 17/32 of a byte out.
+// A thread takes 16 consecutive elements (one 32-byte access of 16-bit ones), two threads a block.
+// Memory-bound: an element costs its own bytes in and 17/32 of a byte out.
 #include <math.h>
 #include <string.h>
 
@@ -59,22 +59,23 @@ __device__ __forceinline__ void e2m1x8_values(uint32_t w, float (&v)[8])
     }
 }
 
-// Rows a thread takes, blockDim.y apart: their loads are all on their way before the first is used
-// (16 bytes a thread and row of 16-bit elements; one row is as much in fp32).
-template <typename T>
-constexpr int MX_ROWS = sizeof(T) == 4 ? 1 : 2;
-
-// The thread's first row and its 8-element group of the rows (d_pad / 8 groups); rows past the matrix
-// belong to its last row tile.
+// The thread's row and its 16-element group of the row (d_pad / 16 groups); rows past the matrix belong
+// to its last row tile.
 struct Place {
     long long row;
     int group;
 };
-template <int ROWS>
 __device__ __forceinline__ Place place()
 {
-    return {(long long)blockIdx.x * (blockDim.y * ROWS) + threadIdx.y,
+    return {(long long)blockIdx.x * blockDim.y + threadIdx.y,
             (int)(blockIdx.y * blockDim.x + threadIdx.x)};
+}
+
+// Byte of the scale of a group's block in the packed buffer.
+__device__ __forceinline__ size_t scale_byte(const mpq_mx_matrix &L, const Place &at)
+{
+    return L.off_scales + ((size_t)(at.row >> 7) * L.k_tiles + (at.group >> 3)) * 512 +
+           scale_at((int)(at.row & 127)) + ((at.group >> 1) & 3);
 }
 
 template <typename T, bool VEC>
@@ -83,50 +84,38 @@ mx_quantize_kernel(const T *X, long long ldx, mpq_mx_matrix L, unsigned char *pa
 {
     sm100::griddep_launch();
     sm100::griddep_wait();
-    constexpr int ROWS = MX_ROWS<T>;
-    const Place at = place<ROWS>();
-    const int j0 = at.group * 8;
-    // d_pad / 8 is a multiple of 16: the 16 threads of a tile row leave together
-    if (j0 >= L.d_pad) return;
-    const unsigned half = (threadIdx.y * blockDim.x + threadIdx.x) & 16;   // of the warp
-    const unsigned part = 0xffffu << half;
-    float v[ROWS][8];
+    const Place at = place();
+    const int j0 = at.group * 16;
+    // d_pad / 16 is even: the two threads of a block leave together
+    if (j0 >= L.d_pad || at.row >= (long long)L.row_tiles * 128) return;
+    const unsigned pair = 3u << ((threadIdx.y * blockDim.x + threadIdx.x) & 30);
+    const bool real = at.row < L.rows;
+    float v[16];
+    const T *x = X + at.row * ldx + j0;
+    if (VEC && real && j0 + 16 <= L.d) {
+        load16(x, v);
+    } else {
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-        const long long row = at.row + r * (int)blockDim.y;
-        const bool real = row < L.rows;
-        const T *x = X + row * ldx + j0;
-        if (VEC && real && j0 + 8 <= L.d) {
-            load8(x, v[r]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[r][i] = real && j0 + i < L.d ? to_f32(x[i]) : 0.0f;
-        }
+        for (int i = 0; i < 16; ++i) v[i] = real && j0 + i < L.d ? to_f32(x[i]) : 0.0f;
     }
+    uint32_t top = top_bits(v);
+    top = max(top, __shfl_xor_sync(pair, top, 1));
+    const bool bad = top >= 0x7f800000u;
+    // E = e + 127: the exponent field less 2; below 2^-125 (subnormal or nearly) e stays at -127
+    const int field = (int)(top >> 23);
+    const int E = bad ? 255 : (field > 2 ? field - 2 : 0);
+    const float inv = __uint_as_float((uint32_t)(254 - E) << 23);   // 2^-e, e <= 125
+    float lo[8], hi[8];
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-        const long long row = at.row + r * (int)blockDim.y;
-        if (row >= (long long)L.row_tiles * 128) return;
-        uint32_t top = top8(v[r]);
-        top = max(top, __shfl_xor_sync(part, top, 1));
-        top = max(top, __shfl_xor_sync(part, top, 2));
-        const bool bad = top >= 0x7f800000u;
-        // E = e + 127: the exponent field less 2; below 2^-125 (subnormal or nearly) e stays at -127
-        const int field = (int)(top >> 23);
-        const int E = bad ? 255 : (field > 2 ? field - 2 : 0);
-        const float inv = __uint_as_float((uint32_t)(254 - E) << 23);   // 2^-e, e <= 125
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[r][i] *= inv;
-        // (rows past the last fill what is left up to the scales with zero codes)
-        const size_t to_codes = (size_t)row * (L.d_pad / 2) + j0 / 2;
-        if (to_codes < L.off_scales)
-            *reinterpret_cast<uint32_t *>(packed + to_codes) = bad ? 0u : e2m1x8(v[r]);
-        if ((threadIdx.x & 3) == 0) {    // the block's scale: a tile row's four are consecutive bytes
-            const size_t to = L.off_scales +
-                              ((size_t)(row >> 7) * L.k_tiles + (at.group >> 4)) * 512 +
-                              scale_at((int)(row & 127)) + ((at.group >> 2) & 3);
-            if (MPQ_IN(to, L.bytes)) packed[to] = (unsigned char)(row < L.rows ? E : 0);
-        }
+    for (int i = 0; i < 8; ++i) lo[i] = v[i] * inv, hi[i] = v[8 + i] * inv;
+    // (rows past the last fill what is left up to the scales with zero codes)
+    const size_t to = (size_t)at.row * (L.d_pad / 2) + j0 / 2;
+    if (to < L.off_scales)
+        *reinterpret_cast<uint2 *>(packed + to) =
+            bad ? make_uint2(0, 0) : make_uint2(e2m1x8(lo), e2m1x8(hi));
+    if ((at.group & 1) == 0) {
+        const size_t sc = scale_byte(L, at);
+        if (MPQ_IN(sc, L.bytes)) packed[sc] = (unsigned char)(real ? E : 0);
     }
 }
 
@@ -136,47 +125,41 @@ mx_dequantize_kernel(const unsigned char *packed, mpq_mx_matrix L, T *Y, long lo
 {
     sm100::griddep_launch();
     sm100::griddep_wait();
-    const Place at = place<1>();
-    const int j0 = at.group * 8;
+    const Place at = place();
+    const int j0 = at.group * 16;
     if (j0 >= L.d || at.row >= L.rows) return;
-    const uint32_t w = sm100::ld_after_wait(
-        reinterpret_cast<const unsigned *>(packed + at.row * (L.d_pad / 2) + j0 / 2));
-    const uint32_t s = sm100::ld_after_wait(reinterpret_cast<const unsigned *>(
-        packed + L.off_scales + ((size_t)(at.row >> 7) * L.k_tiles + (at.group >> 4)) * 512 +
-        scale_at((int)(at.row & 127))));
-    const int E = (int)((s >> (8 * ((at.group >> 2) & 3))) & 255u);
-    float v[8];
-    e2m1x8_values(w, v);
-    // 2^(E-127) as two normal factors (E = 0 is subnormal, and 6 x 2^127 overflows in one step only
-    // where the value does)
-    const int h = E >> 1;
-    const float f0 = E == 255 ? NAN : __uint_as_float((uint32_t)(h + 64) << 23);
-    const float f1 = __uint_as_float((uint32_t)(E - h + 63) << 23);
+    const uint2 w = *reinterpret_cast<const uint2 *>(packed + at.row * (L.d_pad / 2) + j0 / 2);
+    const int E = packed[scale_byte(L, at)];
+    float lo[8], hi[8], v[16];
+    e2m1x8_values(w.x, lo);
+    e2m1x8_values(w.y, hi);
+    // 2^(E-127): subnormal for E = 0
+    const float scale = __uint_as_float(E == 255 ? 0x7fffffffu : E == 0 ? 0x00400000u : (uint32_t)E << 23);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = __fmul_rn(__fmul_rn(v[i], f0), f1);
+    for (int i = 0; i < 8; ++i) v[i] = __fmul_rn(lo[i], scale), v[8 + i] = __fmul_rn(hi[i], scale);
     T *y = Y + at.row * ldy + j0;
-    if (!MPQ_IN(at.row * ldy + j0 + min(8, L.d - j0) - 1, (L.rows - 1) * ldy + L.d)) return;
-    if (VEC && j0 + 8 <= L.d) {
-        store8(y, v);
+    if (!MPQ_IN(at.row * ldy + j0 + min(16, L.d - j0) - 1, (L.rows - 1) * ldy + L.d)) return;
+    if (VEC && j0 + 16 <= L.d) {
+        store16(y, v);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < 16; ++i)
             if (j0 + i < L.d) y[i] = from_f32<T>(v[i]);
     }
 }
 
-// Threads across a row (a multiple of 16, at most 256), the rest down the rows.
+// Threads across a row (a power of two, 8 to 256), the rest down the rows.
 dim3 mx_block(const mpq_mx_matrix *L)
 {
-    int tx = 16;
-    while (tx < MX_THREADS && tx < L->d_pad / 8) tx *= 2;
+    int tx = 8;
+    while (tx < MX_THREADS && tx < L->d_pad / 16) tx *= 2;
     return dim3((unsigned)tx, (unsigned)(MX_THREADS / tx), 1);
 }
 
 dim3 mx_grid(const mpq_mx_matrix *L, long long rows, dim3 block)
 {
     return dim3((unsigned)((rows + block.y - 1) / block.y),
-                (unsigned)((L->d_pad / 8 + (int)block.x - 1) / (int)block.x), 1);
+                (unsigned)((L->d_pad / 16 + (int)block.x - 1) / (int)block.x), 1);
 }
 
 }  // namespace
@@ -199,10 +182,9 @@ mpq_status launch_mx_quantize(const void *X, int x_type, long long ldx, const mp
 {
     const bool vec = rows_aligned(X, x_type, ldx);
     unsigned char *out = static_cast<unsigned char *>(packed);
-    const dim3 block = mx_block(L);
+    const dim3 block = mx_block(L), grid = mx_grid(L, (long long)L->row_tiles * 128, block);
     return by_type(x_type, [&](auto t) {
         using T = decltype(t);
-        const dim3 grid = mx_grid(L, ((long long)L->row_tiles * 128 + MX_ROWS<T> - 1) / MX_ROWS<T>, block);
         return launch_waiting(vec ? mx_quantize_kernel<T, true> : mx_quantize_kernel<T, false>, grid,
                               block, 0, stream, "mx quantize launch", static_cast<const T *>(X), ldx,
                               *L, out);
