@@ -2,15 +2,17 @@
 // slots back (mpq_cache_read).
 //
 // A row is what one token keeps for one head (its key, or its value): s = max|x| (1 / Qmax), one fp32
-// product, codes clamp(rint(x / s)) as Eq. 8's.  A thread takes 8 elements of a token's key and value
-// row of one head (both are on their way before either is used), so dim / 8 threads (8, 16 or 32 of
-// a warp) share the rows' maxima by shuffles, and their codes leave in one store of 8 or 4 bytes a
+// product, codes clamp(rint(x / s)) as Eq. 8's.  A thread takes 16 elements of a token's key and value
+// row of one head (both are on their way before either is used), so dim / 16 threads (4, 8 or 16 of
+// a warp) share the rows' maxima by shuffles, and their codes leave in one store of 16 or 8 bytes a
 // thread and row.
 //
-// Codes are screened by the reciprocal: with r = fl(1 / s) normal, y = fl(x r) is within 2^-15 of the
-// quotient x / s (|x / s| <= 127 (1 + 2^-22), two roundings of 2^-24 and the division's own), so rint(y)
-// is the code unless y lies within 2^-14 of halfway between two integers; those elements, and rows
-// whose scale has no normal reciprocal, are divided.
+// The quotient x / s has to be the correctly rounded one: 16-bit inputs meet near-ties all the time
+// (elements whose ratio to the row's largest is a simple fraction).  One correctly rounded reciprocal r
+// a row, and Markstein's theorem (IBM J. Res. Dev. 34(1), 1990): a y within a unit in the last place of
+// x / s gives RN(x / s) as RN(y + r (x - s y)), the remainder exact by a fused multiply-add.  RN(x r) is
+// within 1.5 units, one such step brings it within one, the next is the quotient.  Rows whose scale is
+// so small or large that r or a remainder could leave the normal range are divided.
 //
 // Memory-bound: an element's own bytes on one side, bits / 8 + 4 / dim bytes on the other; slots scatter
 // rows of 32 to 256 bytes, whole sectors.
@@ -34,10 +36,10 @@ struct RowAt {
 };
 __device__ __forceinline__ bool row_at(int T, const mpq_kv_cache &L, RowAt &at)
 {
-    const int shift = L.dim == 64 ? 3 : L.dim == 128 ? 4 : 5;       // of dim / 8 threads a row
+    const int shift = L.dim == 64 ? 2 : L.dim == 128 ? 3 : 4;       // of dim / 16 threads a row
     at.t = (int)(blockIdx.x * (unsigned)(KV_THREADS >> shift) + (threadIdx.x >> shift));
     at.h = (int)blockIdx.y;
-    at.j0 = (int)(threadIdx.x & ((1u << shift) - 1u)) * 8;
+    at.j0 = (int)(threadIdx.x & ((1u << shift) - 1u)) * 16;
     return at.t < T;
 }
 
@@ -52,34 +54,44 @@ __device__ __forceinline__ long long cache_row(long long slot, const mpq_kv_cach
 }
 
 // max |x| of a row as bits (infinities and NaN above every finite value), over its `per` threads.
-__device__ __forceinline__ uint32_t row_top(const float (&v)[8], unsigned per, unsigned lanes)
+__device__ __forceinline__ uint32_t row_top(const float (&v)[16], unsigned per, unsigned lanes)
 {
     uint32_t top = top_bits(v);
     for (unsigned o = 1; o < per; o <<= 1) top = max(top, __shfl_xor_sync(lanes, top, o));
     return top;
 }
 
-// The codes of 8 elements, offset by Qmax + 1, in the low bits of each word, and the row's scale.
-__device__ __forceinline__ float row_codes(const float (&v)[8], uint32_t top, int qmax,
-                                           float inv_qmax, uint32_t (&u)[8])
+// Scales whose reciprocal, and whose quotients' remainders where the code is not 0, are normal.
+constexpr float KV_LEAST = 0x1p-100f, KV_MOST = 0x1p100f;
+
+// The codes of 16 elements, offset by Qmax + 1, in the low bits of each word, and the row's scale.
+__device__ __forceinline__ float row_codes(const float (&v)[16], uint32_t top, int qmax,
+                                           float inv_qmax, uint32_t (&u)[16])
 {
-    const bool bad = top >= 0x7f800000u;
-    const float s = bad ? NAN : __fmul_rn(__uint_as_float(top), inv_qmax);
+    const float s = top >= 0x7f800000u ? NAN : __fmul_rn(__uint_as_float(top), inv_qmax);
     const int zero = qmax + 1;
-    if (!(s > 0.0f)) {
+    if (s >= KV_LEAST && s <= KV_MOST) {
+        const float r = __frcp_rn(s);
+        const float magic = 12582912.0f + (float)zero;  // 3 2^22 + offset: the sum's low bits are the code
 #pragma unroll
-        for (int i = 0; i < 8; ++i) u[i] = (uint32_t)zero;
-        return s;
-    }
-    const float r = __frcp_rn(s);
-    const bool tiny = s < 0x1p-120f || r < 0x1p-120f;
-    const float magic = 12582912.0f + (float)zero;      // 3 2^22 + offset: the sum's low bits are the code
+        for (int i = 0; i < 16; ++i) {
+            float y = __fmul_rn(v[i], r);
+            y = __fmaf_rn(__fmaf_rn(-y, s, v[i]), r, y);
+            y = __fmaf_rn(__fmaf_rn(-y, s, v[i]), r, y);
+            u[i] = __float_as_uint(__fadd_rn(y, magic));
+        }
+    } else {
+#pragma unroll 1
+        for (int i = 0; i < 16; ++i) {
+            float x = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float y = __fmul_rn(v[i], r), t = __fadd_rn(y, magic);
-        u[i] = __float_as_uint(t);
-        if (tiny || fabsf(__fsub_rn(y, __fsub_rn(t, magic))) > 0.5f - 0x1p-14f)
-            u[i] = (uint32_t)(min(max(__float2int_rn(__fdiv_rn(v[i], s)), -qmax), qmax) + zero);
+            for (int k = 0; k < 16; ++k) x = k == i ? v[k] : x;
+            int q = 0;
+            if (s > 0.0f) q = min(max(__float2int_rn(__fdiv_rn(x, s)), -qmax), qmax);
+#pragma unroll
+            for (int k = 0; k < 16; ++k)
+                if (k == i) u[k] = (uint32_t)(q + zero);
+        }
     }
     return s;
 }
@@ -89,19 +101,20 @@ __device__ __forceinline__ uint32_t low_bytes(const uint32_t *u)
     return __byte_perm(__byte_perm(u[0], u[1], 0x0040), __byte_perm(u[2], u[3], 0x0040), 0x5410);
 }
 
-// Stores a thread's 8 codes and, by the row's first thread, its scale.
-__device__ __forceinline__ void store_row(const uint32_t (&u)[8], float s, long long row, int j0,
+// Stores a thread's 16 codes and, by the row's first thread, its scale.
+__device__ __forceinline__ void store_row(const uint32_t (&u)[16], float s, long long row, int j0,
                                           const mpq_kv_cache &L, unsigned char *codes, float *scales)
 {
     if (!MPQ_IN(row, (size_t)L.pages * 2 * L.heads * L.page)) return;
     unsigned char *const out = codes + row * L.row_bytes;
     if (L.bits == 8) {
-        *reinterpret_cast<uint2 *>(out + j0) = make_uint2(low_bytes(u), low_bytes(u + 4));
+        *reinterpret_cast<uint4 *>(out + j0) = make_uint4(low_bytes(u), low_bytes(u + 4),
+                                                          low_bytes(u + 8), low_bytes(u + 12));
     } else {
-        uint32_t w = 0;
+        uint32_t w[2] = {0, 0};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w |= (u[i] & 15u) << (4 * i);
-        *reinterpret_cast<uint32_t *>(out + j0 / 2) = w;
+        for (int i = 0; i < 16; ++i) w[i >> 3] |= (u[i] & 15u) << (4 * (i & 7));
+        *reinterpret_cast<uint2 *>(out + j0 / 2) = make_uint2(w[0], w[1]);
     }
     if (j0 == 0) scales[row] = s;
 }
@@ -115,45 +128,52 @@ cache_write_kernel(const T *K, const T *V, long long ld_token, long long ld_head
     sm100::griddep_launch();
     sm100::griddep_wait();
     RowAt at;
-    if (!row_at(n, L, at)) return;   // whole rows (dim / 8 threads) leave together
+    if (!row_at(n, L, at)) return;   // whole rows (dim / 16 threads) leave together
     const long long slot = slots[at.t];
     const long long from = ld_token * at.t + ld_head * at.h + at.j0;
-    float k[8], v[8];
+    float k[16], v[16];
     if (VEC) {
-        load8(K + from, k);
-        load8(V + from, v);
+        load16(K + from, k);
+        load16(V + from, v);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < 16; ++i) {
             k[i] = to_f32(K[from + i]);
             v[i] = to_f32(V[from + i]);
         }
     }
     const long long row = cache_row(slot, L, at.h);
     if (row < 0) return;
-    const unsigned per = (unsigned)L.dim / 8;
-    const unsigned lanes = per == 32 ? 0xffffffffu : ((1u << per) - 1u)
-                                                         << (threadIdx.x & 31 & ~(per - 1));
+    const unsigned per = (unsigned)L.dim / 16;
+    const unsigned lanes = ((1u << per) - 1u) << (threadIdx.x & 31 & ~(per - 1));
     const int qmax = (1 << (L.bits - 1)) - 1;
     const uint32_t k_top = row_top(k, per, lanes), v_top = row_top(v, per, lanes);
-    uint32_t u[8];
+    uint32_t u[16];
     float s = row_codes(k, k_top, qmax, inv_qmax, u);
     store_row(u, s, row, at.j0, L, codes, scales);
     s = row_codes(v, v_top, qmax, inv_qmax, u);
     store_row(u, s, row + (long long)L.heads * L.page, at.j0, L, codes, scales);
 }
 
-// The values of 8 codes (in one or two words) with a scale.
-__device__ __forceinline__ void row_values(uint2 w, float s, int bits, float (&v)[8])
+// The values of 16 codes (four words, or two) with a scale.
+__device__ __forceinline__ void row_values(uint4 w, float s, int bits, float (&v)[16])
 {
+    const uint32_t q[4] = {w.x, w.y, w.z, w.w};
     if (bits == 8) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            v[i] = s * (float)((int)(((i < 4 ? w.x : w.y) >> (8 * (i & 3))) & 255u) - 128);
+        for (int i = 0; i < 16; ++i)
+            v[i] = s * (float)((int)((q[i >> 2] >> (8 * (i & 3))) & 255u) - 128);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = s * (float)((int)((w.x >> (4 * i)) & 15u) - 8);
+        for (int i = 0; i < 16; ++i) v[i] = s * (float)((int)((q[i >> 3] >> (4 * (i & 7))) & 15u) - 8);
     }
+}
+
+__device__ __forceinline__ uint4 load_codes(const unsigned char *row, int j0, int bits)
+{
+    if (bits == 8) return *reinterpret_cast<const uint4 *>(row + j0);
+    const uint2 w = *reinterpret_cast<const uint2 *>(row + j0 / 2);
+    return make_uint4(w.x, w.y, 0, 0);
 }
 
 template <typename T>
@@ -167,32 +187,27 @@ cache_read_kernel(const int64_t *slots, int n, mpq_kv_cache L, const unsigned ch
     if (!row_at(n, L, at)) return;
     const long long row = cache_row(slots[at.t], L, at.h);
     const long long v_row = row + (long long)L.heads * L.page;
-    uint2 kw = make_uint2(0, 0), vw = make_uint2(0, 0);
+    uint4 kw = make_uint4(0, 0, 0, 0), vw = make_uint4(0, 0, 0, 0);
     float ks = 0.0f, vs = 0.0f;      // (a slot outside the cache: zeros)
     if (row >= 0) {
         ks = scales[row];
         vs = scales[v_row];
-        if (L.bits == 8) {
-            kw = *reinterpret_cast<const uint2 *>(codes + row * L.row_bytes + at.j0);
-            vw = *reinterpret_cast<const uint2 *>(codes + v_row * L.row_bytes + at.j0);
-        } else {
-            kw.x = *reinterpret_cast<const uint32_t *>(codes + row * L.row_bytes + at.j0 / 2);
-            vw.x = *reinterpret_cast<const uint32_t *>(codes + v_row * L.row_bytes + at.j0 / 2);
-        }
+        kw = load_codes(codes + row * L.row_bytes, at.j0, L.bits);
+        vw = load_codes(codes + v_row * L.row_bytes, at.j0, L.bits);
     }
-    float v[8];
+    float v[16];
     const size_t to = ((size_t)at.t * L.heads + at.h) * L.dim + at.j0;
-    if (!MPQ_IN(to + 7, (size_t)n * L.heads * L.dim)) return;
+    if (!MPQ_IN(to + 15, (size_t)n * L.heads * L.dim)) return;
     row_values(kw, ks, L.bits, v);
-    store8(K + to, v);
+    store16(K + to, v);
     row_values(vw, vs, L.bits, v);
-    store8(V + to, v);
+    store16(V + to, v);
 }
 
 // Blocks of KV_THREADS threads for T tokens' rows, by head.
 dim3 kv_grid(int T, const mpq_kv_cache *L)
 {
-    const long long per_block = KV_THREADS / (L->dim / 8);
+    const long long per_block = KV_THREADS / (L->dim / 16);
     return dim3((unsigned)((T + per_block - 1) / per_block), (unsigned)L->heads, 1);
 }
 
