@@ -1,22 +1,28 @@
 // Linear layer of microscaled 4-bit floats (mpq_mx_linear): Y[t][c] = sum_j x_tj w_cj + bias_c on the
 // tensor cores' block-scaled MMAs (tcgen05.mma kind::mxf4).
 //
-// The weights' 128-channel row tiles are the MMA's A (M = 128), the tokens its B (N = 16 .. 256), so a
-// handful of tokens costs no padding to 128.  A K stage is 256 elements: 128-byte rows of codes, as
-// they lie in memory, by TMA into 128-byte-swizzled K-major tiles, and the scales of both, 512
-// contiguous bytes per 128 rows x 128 elements, by bulk copies; one thread moves the scales from
-// shared to tensor memory (each stage has columns of its own, reused when its MMAs are done) and
-// issues the MMAs.  Accumulators are fp32 in tensor memory, one rounding (after the bias) on the way
-// out.
+// A K stage is 256 elements: 128-byte rows of codes, as they lie in memory, by TMA into 128-byte-
+// swizzled K-major tiles, and the scales of both operands, 512 contiguous bytes per 128 rows x 128
+// elements, by bulk copies.  Four warps move the scales from shared to tensor memory (each stage has
+// columns of its own, written anew when its MMAs are done) a stage or more ahead of the thread that
+// issues the MMAs: as tensor-core copies (tcgen05.cp) they would take 72 cycles each in line with the
+// MMAs, 545 a stage beside the 513 of four 128 x 256 x 64 MMAs.  Accumulators are fp32 in tensor memory,
+// one rounding (after the bias) on the way out.
 //
-// With few tokens the weights' bytes bound it (d / 2 + d / 32 a channel), and with few row tiles most
-// SMs would idle: the K stages of a tile are then split over the CTAs of a cluster, which leave their
-// sums in shared memory and join them there in the order of the ranks (so equal inputs give equal
-// bits).  With many tokens shared-memory reads of the MMAs bound it: 128 + N rows of 32 bytes for 64
-// elements of K, which 128 x 256 tiles bring to 3/4 of the 128 x 128 ones' per product.
+// Few tokens (or few tiles): the weights' rows are the MMA's A (M = 128 channels on the accumulator's
+// lanes), the tokens its B (N = 16 .. 256), so a handful of tokens costs no padding to 128.  The weights'
+// bytes bound it (d / 2 + d / 32 a channel), and with few row tiles most SMs would idle: the K stages of a
+// tile are split over the CTAs of a cluster, which leave their sums in shared memory and join them there
+// in the order of the ranks (so equal inputs give equal bits).
 //
-// Roles: warp 0 copies, warp 1 issues MMAs, warps 2..5 (TMEM lane quarter warp % 4) write the outputs.
-// Every wait is bounded.
+// Many tokens: tokens on the lanes (a lane then writes runs of consecutive outputs), tiles of 128 tokens
+// x 256 channels.  What L2 can deliver bounds a CTA that loads its own operands (52 KB a stage take about
+// 1,200 cycles at the 43 bytes per SM and cycle measured, the MMAs 513), so a cluster of 4 x 2 tiles
+// shares them: each CTA loads an eighth of the cluster's rows and sends them to the CTAs that need
+// them (multicast), 17.5 KB a stage and CTA.
+//
+// Roles: warp 0 copies, warp 1 issues MMAs, warps 2..5 (TMEM lane quarter warp % 4) move scales, then write
+// the outputs.  Every wait is bounded.
 #include <cuda.h>
 #include <math.h>
 #include <string.h>
@@ -36,18 +42,20 @@ namespace {
 
 using namespace sm100;
 
-constexpr int X_M = 128;                 // channels of a tile
-constexpr int X_N = 256;                 // most tokens of a tile
+constexpr int X_M = 128;                 // rows of A in a tile (accumulator lanes)
+constexpr int X_N = 256;                 // most rows of B in a tile (accumulator columns)
 constexpr int X_ROW = 128;               // bytes of a row's codes in a stage: 256 elements
 constexpr int X_SF = 512;                // bytes of a scale tile (128 rows x 128 elements)
 constexpr int X_A_BYTES = X_M * X_ROW;
 constexpr int X_MAX_STAGES = 8;
 constexpr int X_THREADS = 192;
-constexpr int X_MAX_SPLIT = 8;           // CTAs of a cluster
+constexpr int X_MAX_SPLIT = 8;           // CTAs of a cluster that splits K
+constexpr int X_CM = 4, X_CN = 2;        // tiles of a cluster that shares operands: along A, along B
 
 struct MxCtrl {
     uint64_t full[X_MAX_STAGES];         // a stage's tiles and scales have landed
-    uint64_t empty[X_MAX_STAGES];        // the MMAs that read a stage completed
+    uint64_t scaled[X_MAX_STAGES];       // its scales are in tensor memory
+    uint64_t empty[X_MAX_STAGES];        // the MMAs that read what this CTA loads completed
     uint64_t done;                       // every MMA completed
     uint32_t tmem_base;
     int abort;
@@ -55,28 +63,37 @@ struct MxCtrl {
 constexpr int X_CTRL_BYTES = 1024;
 static_assert(sizeof(MxCtrl) <= X_CTRL_BYTES, "control block");
 
+// The operands by their place in the MMA: A's rows on the accumulator's lanes, B's on its columns.
 struct MxArgs {
-    int T, C;
-    int n_tile;                          // tokens of a tile, a multiple of 16
+    int a_rows, b_rows;
+    int a_tiles, b_tiles;                // row tiles of their scales (128 rows)
+    int n_tile;                          // rows of B in a tile, a multiple of 16
     int stages, k_stages, k_tiles;       // ring, K stages of a row, scale tiles of a row
     int split;                           // CTAs that share a tile's K stages
     int acc_cols, cols;                  // TMEM columns: the accumulator's (scales follow), all
-    const unsigned char *w_scales, *x_scales;
+    int b_clusters;                      // clusters along B (shared operands)
+    int wide;                            // output rows take 32-byte stores
+    const unsigned char *a_scales, *b_scales;
     const float *bias;
     long long ldy;
 };
 
 __host__ __device__ inline int sf_b_bytes(int n_tile) { return n_tile > 128 ? 4 * X_SF : 2 * X_SF; }
+__host__ __device__ inline int sf_b_cols(int n_tile) { return n_tile > 128 ? 8 : 4; }  // of a k tile
+__host__ __device__ inline int sf_cols(int n_tile) { return 8 + 2 * sf_b_cols(n_tile); }
 __host__ __device__ inline int stage_bytes(int n_tile)
 {
     return X_A_BYTES + n_tile * X_ROW + 2 * X_SF + sf_b_bytes(n_tile);
 }
 
-template <typename T>
+// MANY: A is the inputs, B the weights, operands shared in clusters of X_CM x X_CN tiles.  Else A is the
+// weights, B the inputs, K split over clusters of a.split.
+template <typename T, bool MANY>
 __global__ void __launch_bounds__(X_THREADS)
-mx_linear_kernel(const MxArgs a, T *Y, WaitCtl wc, const __grid_constant__ CUtensorMap tmW,
-                 const __grid_constant__ CUtensorMap tmX)
+mx_linear_kernel(const MxArgs a, T *Y, WaitCtl wc, const __grid_constant__ CUtensorMap tmA,
+                 const __grid_constant__ CUtensorMap tmB)
 {
+    constexpr int CM = MANY ? X_CM : 1, CN = MANY ? X_CN : 1;
     extern __shared__ unsigned char raw[];
     const uint32_t raw_u32 = smem_u32(raw);
     unsigned char *const base = raw + ((1024u - (raw_u32 & 1023u)) & 1023u);
@@ -86,29 +103,41 @@ mx_linear_kernel(const MxArgs a, T *Y, WaitCtl wc, const __grid_constant__ CUten
     volatile int *const abort_flag = &ctl.abort;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int sb = stage_bytes(a.n_tile);
-    const int rank = a.split > 1 ? (int)cluster_ctarank() : 0;
-    const int tile = (int)blockIdx.x / a.split;
-    const long long n0 = (long long)blockIdx.y * a.n_tile;
-    const int n_real = (int)min((long long)a.n_tile, a.T - n0);      // tokens of this tile
-    const int k0 = (int)((long long)a.k_stages * rank / a.split);
-    const int k1 = (int)((long long)a.k_stages * (rank + 1) / a.split);
+    const bool cluster = MANY || a.split > 1;
+    const int rank = cluster ? (int)cluster_ctarank() : 0;
+    // the tile: row tile of A, first row of B; the cluster's tiles lie X_CM along A, X_CN along B
+    const int cm = MANY ? rank % CM : 0, cn = MANY ? rank / CM : 0;
+    const int group = (int)blockIdx.x / (MANY ? CM * CN : a.split);
+    const int tile = MANY ? group / a.b_clusters * CM + cm : group;
+    const long long n0 = MANY ? (long long)(group % a.b_clusters * CN + cn) * X_N
+                              : (long long)blockIdx.y * a.n_tile;
+    const int n_real = (int)max(0LL, min((long long)a.n_tile, a.b_rows - n0));   // rows of B that there are
+    const int a_sf = tile < a.a_tiles ? 1 : 0;                       // scale tiles (per k tile) of A, of B
+    const int b_sf = (n_real + 127) / 128;
+    const int k0 = MANY ? 0 : (int)((long long)a.k_stages * rank / a.split);
+    const int k1 = MANY ? a.k_stages : (int)((long long)a.k_stages * (rank + 1) / a.split);
+    // the CTAs that take what this one loads of A (those along B), of B (those along A)
+    const uint16_t mask_a = (uint16_t)((1u << cm) * (CN == 2 ? 1u | (1u << CM) : 1u));
+    const uint16_t mask_b = (uint16_t)(((1u << CM) - 1u) << (cn * CM));
 
     griddep_launch();
     if (threadIdx.x == 0) {
         for (int i = 0; i < a.stages; ++i) {
             mbar_init(&ctl.full[i], 1);
-            mbar_init(&ctl.empty[i], 1);
+            mbar_init(&ctl.scaled[i], 4);
+            mbar_init(&ctl.empty[i], CM + CN - 1);
         }
         mbar_init(&ctl.done, 1);
         ctl.abort = 0;
         fence_barrier_init();
         if (!MPQ_CHECK_SMEM_END(ring - raw + (size_t)a.stages * sb)) ctl.abort = 1;
-        prefetch_tensormap(&tmW);
-        prefetch_tensormap(&tmX);
+        prefetch_tensormap(&tmA);
+        prefetch_tensormap(&tmB);
     }
     if (warp == 1) tmem_alloc(&ctl.tmem_base, (uint32_t)a.cols);
     tc_fence_before();
     __syncthreads();
+    if (MANY) cluster_sync();            // the barriers that other CTAs arrive on are ready
     tc_fence_after();
     const uint32_t tmem = ctl.tmem_base;
     griddep_wait();
@@ -116,76 +145,97 @@ mx_linear_kernel(const MxArgs a, T *Y, WaitCtl wc, const __grid_constant__ CUten
     if (warp == 0) {
         // ---------------------------------------------------------------- copies
         if (lane == 0) {
-            const int row_tiles = (n_real + 127) / 128;              // of the tokens' scales
             const size_t sf_a = (size_t)tile * a.k_tiles * X_SF;
             const size_t sf_b = (size_t)(n0 / 128) * a.k_tiles * X_SF;
             int issued = k0;
             for (int k = k0; k < k1; ++k) {
                 const int i = k - k0, s = i % a.stages;
                 if (i >= a.stages &&
-                    !mbar_wait(&ctl.empty[s], (uint32_t)(i / a.stages - 1) & 1u, wc.budget)) {
+                    !mbar_wait_cluster(&ctl.empty[s], (uint32_t)(i / a.stages - 1) & 1u, wc.budget)) {
                     *abort_flag = 1;
                     note_timeout(wc, MPQ_TIMEOUT_MX);
                 }
                 if (*abort_flag) break;
                 const uint32_t at = ring_u32 + (uint32_t)(s * sb);
-                const int kt = min(2, a.k_tiles - 2 * k);            // scale tiles of this stage
+                const int kt = min(2, a.k_tiles - 2 * k);            // scale tiles (along K) of this stage
                 if (!MPQ_CHECK(((k * X_ROW) & 15) == 0 && (at & 1023u) == 0u && kt > 0)) {
                     *abort_flag = 1;
                     break;
                 }
                 const uint32_t sfs = at + (uint32_t)(X_A_BYTES + a.n_tile * X_ROW);
-                mbar_arrive_expect_tx(&ctl.full[s], (uint32_t)(X_A_BYTES + a.n_tile * X_ROW +
-                                                               (1 + row_tiles) * kt * X_SF));
-                tma_load_2d(at, &tmW, k * X_ROW, tile * X_M, &ctl.full[s]);
-                tma_load_2d(at + X_A_BYTES, &tmX, k * X_ROW, (int)n0, &ctl.full[s]);
-                bulk_load(sfs, a.w_scales + sf_a + (size_t)(2 * k) * X_SF, (uint32_t)(kt * X_SF),
-                          &ctl.full[s]);
-                for (int r = 0; r < row_tiles; ++r)
-                    bulk_load(sfs + (uint32_t)((2 + 2 * r) * X_SF),
-                              a.x_scales + sf_b + ((size_t)r * a.k_tiles + 2 * k) * X_SF,
-                              (uint32_t)(kt * X_SF), &ctl.full[s]);
+                uint64_t *const bar = &ctl.full[s];
+                mbar_arrive_expect_tx(bar, (uint32_t)(X_A_BYTES + a.n_tile * X_ROW +
+                                                      (a_sf + b_sf) * kt * X_SF));
+                if constexpr (MANY) {
+                    constexpr int RA = X_M / CN, RB = X_N / CM;      // rows that this CTA loads
+                    tma_load_2d_multicast(at + cn * RA * X_ROW, &tmA, k * X_ROW, tile * X_M + cn * RA,
+                                          bar, mask_a);
+                    tma_load_2d_multicast(at + X_A_BYTES + cm * RB * X_ROW, &tmB, k * X_ROW,
+                                          (int)n0 + cm * RB, bar, mask_b);
+                    // scale tiles: A's k tile cn; B's (row tile, k tile) number cm
+                    static_assert(CN == 2 && CM == 4, "one scale tile of A and one of B for each CTA");
+                    if (cn < kt && a_sf)
+                        bulk_load_multicast(sfs + cn * X_SF, a.a_scales + sf_a + (size_t)(2 * k + cn) * X_SF,
+                                            X_SF, bar, mask_a);
+                    if ((cm & 1) < kt && (cm >> 1) < b_sf)
+                        bulk_load_multicast(sfs + (2 + cm) * X_SF,
+                                            a.b_scales + sf_b +
+                                                ((size_t)(cm >> 1) * a.k_tiles + 2 * k + (cm & 1)) * X_SF,
+                                            X_SF, bar, mask_b);
+                } else {
+                    tma_load_2d(at, &tmA, k * X_ROW, tile * X_M, bar);
+                    tma_load_2d(at + X_A_BYTES, &tmB, k * X_ROW, (int)n0, bar);
+                    bulk_load(sfs, a.a_scales + sf_a + (size_t)(2 * k) * X_SF, (uint32_t)(kt * X_SF), bar);
+                    for (int r = 0; r < b_sf; ++r)
+                        bulk_load(sfs + (uint32_t)((2 + 2 * r) * X_SF),
+                                  a.b_scales + sf_b + ((size_t)r * a.k_tiles + 2 * k) * X_SF,
+                                  (uint32_t)(kt * X_SF), bar);
+                }
                 issued = k + 1;
             }
             // no copy may land after the CTA is gone
             for (int k = max(k0, issued - a.stages); k < issued; ++k)
                 drain_wait(&ctl.full[(k - k0) % a.stages], (uint32_t)((k - k0) / a.stages) & 1u, wc,
                            MPQ_TIMEOUT_MX);
+            // ... nor an arrival of another CTA's MMAs
+            for (int k = max(k0, issued - a.stages); MANY && k < issued && !*abort_flag; ++k)
+                drain_wait_cluster(&ctl.empty[(k - k0) % a.stages], (uint32_t)((k - k0) / a.stages) & 1u,
+                                   wc, MPQ_TIMEOUT_MX);
         }
         __syncwarp();
     } else if (warp == 1) {
         // ---------------------------------------------------------------- MMAs
         if (lane == 0) {
-            const int n = (n_real + 15) / 16 * 16;
-            const int row_tiles = (n_real + 127) / 128;
+            const int n = MANY ? X_N : (n_real + 15) / 16 * 16;
             const uint32_t id0 = idesc_mxf4(X_M, n, 0), id2 = idesc_mxf4(X_M, n, 2);
-            const int sf_cols = 8 + 8 * (a.n_tile > 128 ? 2 : 1);    // of a stage
+            const int bc = sf_b_cols(a.n_tile);
+            int s = 0;
+            uint32_t phase = 0;
             for (int k = k0; k < k1 && !*abort_flag; ++k) {
-                const int i = k - k0, s = i % a.stages;
-                if (!mbar_wait(&ctl.full[s], (uint32_t)(i / a.stages) & 1u, wc.budget)) {
+                if (!mbar_wait(&ctl.full[s], phase, wc.budget) ||
+                    !mbar_wait(&ctl.scaled[s], phase, wc.budget)) {
                     *abort_flag = 1;
                     note_timeout(wc, MPQ_TIMEOUT_MX);
                     break;
                 }
                 tc_fence_after();
                 const uint32_t at = ring_u32 + (uint32_t)(s * sb);
-                const uint32_t sfs = at + (uint32_t)(X_A_BYTES + a.n_tile * X_ROW);
-                const uint32_t ta = tmem + (uint32_t)(a.acc_cols + s * sf_cols), tb = ta + 8;
-                const int kt = min(2, a.k_tiles - 2 * k);
-                for (int j = 0; j < kt; ++j) {
-                    tmem_copy_scales(ta + 4 * j, sfs + (uint32_t)(j * X_SF));
-                    for (int r = 0; r < row_tiles; ++r)
-                        tmem_copy_scales(tb + (uint32_t)((a.n_tile > 128 ? 8 : 4) * j + 4 * r),
-                                         sfs + (uint32_t)((2 + 2 * r + j) * X_SF));
-                }
+                const uint32_t ta = tmem + (uint32_t)(a.acc_cols + s * sf_cols(a.n_tile)), tb = ta + 8;
                 const uint64_t ad = smem_desc_sw128(at), bd = smem_desc_sw128(at + X_A_BYTES);
-                for (int j = 0; j < 2 * kt; ++j) {
+                const int steps = 2 * min(2, a.k_tiles - 2 * k);
+                for (int j = 0; j < steps; ++j) {
                     const uint64_t o = (uint64_t)(j * 2);            // 32 bytes, in 16 B units
                     mma_mxf4(tmem, ad + o, bd + o, (j & 1) ? id2 : id0, ta + 4 * (j >> 1),
-                             tb + (uint32_t)((a.n_tile > 128 ? 8 : 4) * (j >> 1)),
-                             i > 0 || j > 0 ? 1u : 0u);
+                             tb + (uint32_t)(bc * (j >> 1)), k > k0 || j > 0 ? 1u : 0u);
                 }
-                mma_commit(&ctl.empty[s]);
+                if (MANY)
+                    mma_commit_multicast(&ctl.empty[s], mask_a | mask_b);
+                else
+                    mma_commit(&ctl.empty[s]);
+                if (++s == a.stages) {
+                    s = 0;
+                    phase ^= 1u;
+                }
             }
             // every MMA issued above completes before its sums are read or tensor memory released
             mma_commit(&ctl.done);
@@ -193,26 +243,79 @@ mx_linear_kernel(const MxArgs a, T *Y, WaitCtl wc, const __grid_constant__ CUten
         }
         __syncwarp();
     } else {
+        // ---------------------------------------------------------------- scales
+        const int q = warp & 3;
+        const uint32_t quarter = tmem + ((uint32_t)(q * 32) << 16);
+        {
+            const int bc = sf_b_cols(a.n_tile);
+            int s = 0;
+            uint32_t phase = 0;
+            for (int k = k0; k < k1; ++k) {
+                // (a slot lands anew only when the MMAs that read its columns are done)
+                if (!mbar_wait(&ctl.full[s], phase, wc.budget)) {
+                    *abort_flag = 1;
+                    note_timeout(wc, MPQ_TIMEOUT_MX);
+                }
+                if (__any_sync(0xffffffffu, *abort_flag)) break;
+                const uint32_t sfs = ring_u32 + (uint32_t)(s * sb + X_A_BYTES + a.n_tile * X_ROW) +
+                                     (uint32_t)(lane * 16);
+                const uint32_t ta = quarter + (uint32_t)(a.acc_cols + s * sf_cols(a.n_tile));
+                const int kt = min(2, a.k_tiles - 2 * k);
+                // lane r of every quarter holds the words of rows r, 32 + r, 64 + r and 96 + r
+                auto move = [&](uint32_t to, uint32_t from) {
+                    const float4 w = ld_shared_v4(from);
+                    const float v[4] = {w.x, w.y, w.z, w.w};
+                    tmem_st_32x32b_x4(to, v);
+                };
+                for (int j = 0; j < kt; ++j) {
+                    move(ta + 4 * j, sfs + (uint32_t)(j * X_SF));
+                    for (int r = 0; r < b_sf; ++r)
+                        move(ta + 8 + (uint32_t)(bc * j + 4 * r), sfs + (uint32_t)((2 + 2 * r + j) * X_SF));
+                }
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&ctl.scaled[s]);
+                if (++s == a.stages) {
+                    s = 0;
+                    phase ^= 1u;
+                }
+            }
+        }
         // ---------------------------------------------------------------- outputs
-        const int q = warp & 3, c = tile * X_M + q * 32 + lane;
+        const int i = tile * X_M + q * 32 + lane;                    // this lane's row of A
         if (!drain_wait(&ctl.done, 0, wc, MPQ_TIMEOUT_MX)) *abort_flag = 1;
         if (!__any_sync(0xffffffffu, *abort_flag)) {
             tc_fence_after();
-            const uint32_t from = tmem + ((uint32_t)(q * 32) << 16);
-            const float bias = a.bias && c < a.C && a.split == 1 ? a.bias[c] : 0.0f;
+            const float bias = !MANY && a.bias && i < a.a_rows && a.split == 1 ? a.bias[i] : 0.0f;
             float *const part = reinterpret_cast<float *>(ring) + q * 32 + lane;
+            const size_t size = (MANY ? a.a_rows - 1 : a.b_rows - 1) * a.ldy + (MANY ? a.b_rows : a.a_rows);
             for (int j0 = 0; j0 < n_real; j0 += 16) {
                 float v[16];
-                tmem_ld_32x32b_x16(from + (uint32_t)j0, v);
-                if (a.split > 1) {       // [token][128 channels]; the ring's copies have been read
+                __syncwarp();
+                tmem_ld_32x32b_x16(quarter + (uint32_t)j0, v);
+                if (MANY && i < a.a_rows) {   // row i of the inputs, 16 consecutive channels
+                    const int c = (int)n0 + j0;
+                    if (a.bias) {
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) v[j] += c + j < a.b_rows ? a.bias[c + j] : 0.0f;
+                    }
+                    T *const y = Y + i * a.ldy + c;
+                    if (a.wide && c + 16 <= a.b_rows) {
+                        if (MPQ_IN(i * a.ldy + c + 15, size)) store16(y, v);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 16; ++j)
+                            if (c + j < a.b_rows && MPQ_IN(i * a.ldy + c + j, size)) y[j] = from_f32<T>(v[j]);
+                    }
+                } else if (!MANY && a.split > 1) {   // [token][128 channels]; the ring's copies have been read
 #pragma unroll
                     for (int j = 0; j < 16; ++j) part[(j0 + j) * X_M] = v[j];
-                } else if (c < a.C) {
-                    T *y = Y + (n0 + j0) * a.ldy + c;
+                } else if (!MANY && i < a.a_rows) {  // channel i of 16 tokens
+                    T *y = Y + (n0 + j0) * a.ldy + i;
 #pragma unroll
                     for (int j = 0; j < 16; ++j)
-                        if (j0 + j < n_real &&
-                            MPQ_IN((n0 + j0 + j) * a.ldy + c, (a.T - 1) * a.ldy + a.C))
+                        if (j0 + j < n_real && MPQ_IN((n0 + j0 + j) * a.ldy + i, size))
                             y[j * a.ldy] = from_f32<T>(v[j] + bias);
                 }
             }
@@ -220,13 +323,13 @@ mx_linear_kernel(const MxArgs a, T *Y, WaitCtl wc, const __grid_constant__ CUten
         }
     }
 
-    if (a.split > 1) {
+    if (!MANY && a.split > 1) {
         cluster_sync();                  // every rank's sums are in its shared memory
         const float *const part = reinterpret_cast<const float *>(ring);
         const int quads = n_real * (X_M / 4);
         for (int i = (int)threadIdx.x + rank * X_THREADS; i < quads; i += a.split * X_THREADS) {
             const int t = i / (X_M / 4), cc = (i % (X_M / 4)) * 4, c = tile * X_M + cc;
-            if (c >= a.C) continue;
+            if (c >= a.a_rows) continue;
             float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
             for (int r = 0; r < a.split; ++r) {
                 const float4 p = ld_dsmem_f32x4(part + t * X_M + cc, (uint32_t)r);
@@ -235,13 +338,14 @@ mx_linear_kernel(const MxArgs a, T *Y, WaitCtl wc, const __grid_constant__ CUten
             T *y = Y + (n0 + t) * a.ldy + c;
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                if (c + e < a.C && MPQ_IN((n0 + t) * a.ldy + c + e, (a.T - 1) * a.ldy + a.C))
+                if (c + e < a.a_rows && MPQ_IN((n0 + t) * a.ldy + c + e, (a.b_rows - 1) * a.ldy + a.a_rows))
                     y[e] = from_f32<T>(v[e] + (a.bias ? a.bias[c + e] : 0.0f));
         }
-        cluster_sync();                  // no rank leaves while its sums are read
-    } else {
-        __syncthreads();
     }
+    if (cluster)
+        cluster_sync();                  // no rank leaves while its sums are read, or copies to it land
+    else
+        __syncthreads();
     if (warp == 1) {
         tc_fence_after();
         tmem_dealloc(tmem, (uint32_t)a.cols);
@@ -255,52 +359,54 @@ int pow2_at_least(int n, int least)
     return r;
 }
 
-template <typename T>
-mpq_status launch_typed(MxArgs &a, const mpq_mx_matrix *xl, const void *X, const mpq_mx_matrix *wl,
-                        const void *W, void *Y, cudaStream_t stream)
+template <typename T, bool MANY>
+mpq_status launch_typed(const MxArgs &a, const void *A, const void *B, int row_bytes, dim3 grid,
+                        int cluster, void *Y, cudaStream_t stream)
 {
-    CUtensorMap tmW, tmX;
-    memset(&tmW, 0, sizeof(tmW));
-    memset(&tmX, 0, sizeof(tmX));
-    const cuuint64_t row = (cuuint64_t)(wl->d_pad / 2);
-    const cuuint64_t dw[2] = {row, (cuuint64_t)a.C}, dx[2] = {row, (cuuint64_t)a.T}, st[1] = {row};
-    const cuuint32_t bw[2] = {X_ROW, X_M}, bx[2] = {X_ROW, (cuuint32_t)a.n_tile};
-    if (!encode_tile_map(&tmW, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, W, dw, st, bw,
+    CUtensorMap tmA, tmB;
+    memset(&tmA, 0, sizeof(tmA));
+    memset(&tmB, 0, sizeof(tmB));
+    const cuuint64_t row = (cuuint64_t)row_bytes;
+    const cuuint64_t da[2] = {row, (cuuint64_t)a.a_rows}, db[2] = {row, (cuuint64_t)a.b_rows}, st[1] = {row};
+    const cuuint32_t ba[2] = {X_ROW, MANY ? X_M / X_CN : X_M};
+    const cuuint32_t bb[2] = {X_ROW, MANY ? (cuuint32_t)(X_N / X_CM) : (cuuint32_t)a.n_tile};
+    if (!encode_tile_map(&tmA, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, A, da, st, ba,
                          CU_TENSOR_MAP_SWIZZLE_128B) ||
-        !encode_tile_map(&tmX, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, X, dx, st, bx,
+        !encode_tile_map(&tmB, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, B, db, st, bb,
                          CU_TENSOR_MAP_SWIZZLE_128B)) {
         set_error("mx linear: tensor map encoding failed");
         return MPQ_ERR_CUDA;
     }
     const size_t smem = 1024 + X_CTRL_BYTES + (size_t)a.stages * stage_bytes(a.n_tile);
     static std::atomic<int> limit[kMaxDevices];
-    cudaError_t e = allow_smem(reinterpret_cast<const void *>(mx_linear_kernel<T>), limit, smem);
+    cudaError_t e = allow_smem(reinterpret_cast<const void *>(mx_linear_kernel<T, MANY>), limit, smem);
     if (e != cudaSuccess) return cuda_status(e, "cudaFuncSetAttribute");
     WaitCtl wc;
     const mpq_status ws = wait_ctl(&wc);
     if (ws != MPQ_OK) return ws;
-    const long long tiles = ((long long)a.C + X_M - 1) / X_M;
-    const long long token_tiles = ((long long)a.T + a.n_tile - 1) / a.n_tile;
-    if (token_tiles > 65535) {
-        set_error("mx linear: T = %d is too large", a.T);
-        return MPQ_ERR_UNSUPPORTED;
-    }
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(tiles * a.split), (unsigned)token_tiles, 1);
+    cfg.gridDim = grid;
     cfg.blockDim = dim3(X_THREADS, 1, 1);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     attr[0] = after_previous_kernel();
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = (unsigned)a.split;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
     attr[1].val.clusterDim.y = 1;
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    e = cudaLaunchKernelEx(&cfg, mx_linear_kernel<T>, (const MxArgs)a, static_cast<T *>(Y), wc, tmW,
-                           tmX);
+    e = cudaLaunchKernelEx(&cfg, mx_linear_kernel<T, MANY>, a, static_cast<T *>(Y), wc, tmA, tmB);
     return cuda_status(e != cudaSuccess ? e : cudaGetLastError(), "mx linear launch");
+}
+
+// Stages that fit into `room` bytes of shared memory, and the tensor memory columns.
+void size_ring(MxArgs &a, int room)
+{
+    a.stages = std::min(X_MAX_STAGES, (room - 1024 - X_CTRL_BYTES) / stage_bytes(a.n_tile));
+    a.acc_cols = pow2_at_least(a.n_tile, 32);
+    a.cols = pow2_at_least(a.acc_cols + a.stages * sf_cols(a.n_tile), 32);
 }
 
 }  // namespace
@@ -310,31 +416,64 @@ mpq_status launch_mx_linear(const mpq_mx_matrix *xl, const void *X, const mpq_mx
                             cudaStream_t stream)
 {
     MxArgs a = {};
-    a.T = xl->rows;
-    a.C = wl->rows;
-    a.n_tile = a.T >= X_N ? X_N : (a.T + 15) / 16 * 16;
     a.k_tiles = wl->k_tiles;
     a.k_stages = (wl->k_tiles + 1) / 2;
-    a.w_scales = static_cast<const unsigned char *>(W) + wl->off_scales;
-    a.x_scales = static_cast<const unsigned char *>(X) + xl->off_scales;
     a.bias = bias;
     a.ldy = ldy;
+    const unsigned char *const x = static_cast<const unsigned char *>(X);
+    const unsigned char *const w = static_cast<const unsigned char *>(W);
+    const int T = xl->rows, C = wl->rows, sms = sm_count();
+    // Tiles of 128 tokens x 256 channels in clusters of 4 x 2 where they fill half the SMs or more
+    const long long m_cl = (((long long)T + X_M - 1) / X_M + X_CM - 1) / X_CM;
+    const long long n_cl = (((long long)C + X_N - 1) / X_N + X_CN - 1) / X_CN;
+    if (m_cl * n_cl * X_CM * X_CN * 2 >= sms && T > X_N) {
+        a.a_rows = T;
+        a.b_rows = C;
+        a.a_tiles = xl->row_tiles;
+        a.b_tiles = wl->row_tiles;
+        a.a_scales = x + xl->off_scales;
+        a.b_scales = w + wl->off_scales;
+        a.n_tile = X_N;
+        a.split = 1;
+        a.b_clusters = (int)n_cl;
+        a.wide = rows_aligned(Y, y_type, ldy);
+        size_ring(a, max_smem_optin());
+        const long long ctas = m_cl * n_cl * X_CM * X_CN;
+        if (ctas > 0x7fffffffLL) {
+            set_error("mx linear: T = %d, C = %d are too large", T, C);
+            return MPQ_ERR_UNSUPPORTED;
+        }
+        return by_type(y_type, [&](auto t) {
+            return launch_typed<decltype(t), true>(a, X, W, wl->d_pad / 2, dim3((unsigned)ctas),
+                                                   X_CM * X_CN, Y, stream);
+        });
+    }
+    a.a_rows = C;
+    a.b_rows = T;
+    a.a_tiles = wl->row_tiles;
+    a.b_tiles = xl->row_tiles;
+    a.a_scales = w + wl->off_scales;
+    a.b_scales = x + xl->off_scales;
+    a.n_tile = T >= X_N ? X_N : (T + 15) / 16 * 16;
     // two CTAs share an SM where a ring of four stages leaves room for it (up to 64 tokens)
-    const int sb = stage_bytes(a.n_tile);
     const bool two = a.n_tile <= 64;
-    const int room = two ? 112 * 1024 : max_smem_optin();
-    a.stages = std::min(X_MAX_STAGES, (room - 2048) / sb);
-    a.acc_cols = pow2_at_least(a.n_tile, 32);
-    a.cols = pow2_at_least(a.acc_cols + a.stages * (a.n_tile > 128 ? 24 : 16), 32);
+    size_ring(a, two ? 112 * 1024 : max_smem_optin());
     // clusters split the K stages while every CTA stays resident and has two stages or more
-    const long long tiles = ((long long)a.C + X_M - 1) / X_M * ((a.T + a.n_tile - 1LL) / a.n_tile);
-    const long long resident = (long long)sm_count() * (two ? 2 : 1);
+    const long long m_tiles = ((long long)C + X_M - 1) / X_M;
+    const long long n_tiles = ((long long)T + a.n_tile - 1) / a.n_tile;
+    const long long resident = (long long)sms * (two ? 2 : 1);
     a.split = 1;
-    while (a.split < X_MAX_SPLIT && tiles * a.split * 2 <= resident &&
+    while (a.split < X_MAX_SPLIT && m_tiles * n_tiles * a.split * 2 <= resident &&
            a.k_stages >= a.split * 4)
         a.split *= 2;
+    if (n_tiles > 65535 || m_tiles * a.split > 0x7fffffffLL) {
+        set_error("mx linear: T = %d, C = %d are too large", T, C);
+        return MPQ_ERR_UNSUPPORTED;
+    }
     return by_type(y_type, [&](auto t) {
-        return launch_typed<decltype(t)>(a, xl, X, wl, W, Y, stream);
+        return launch_typed<decltype(t), false>(a, W, X, wl->d_pad / 2,
+                                                dim3((unsigned)(m_tiles * a.split), (unsigned)n_tiles),
+                                                a.split, Y, stream);
     });
 }
 

@@ -544,19 +544,6 @@ __host__ __device__ constexpr uint32_t idesc_mxf4(int M, int N, int sf)
            | ((uint32_t)sf << 29);        // A's scale bytes
 }
 
-// 32 rows of 16 bytes (contiguous shared memory) into 4 columns of tensor memory, the same in each
-// of its four lane quarters: the scales of 128 rows x 4 blocks.  Issued by one thread; MMAs that it
-// issues later see them.
-__device__ __forceinline__ void tmem_copy_scales(uint32_t taddr, uint32_t saddr)
-{
-    uint64_t d = 0;
-    d |= (uint64_t)((saddr & 0x3FFFF) >> 4);          // start address
-    d |= (uint64_t)(128 >> 4) << 32;                  // stride byte offset: next 8 rows
-    d |= (uint64_t)1 << 46;                           // descriptor version (tcgen05)
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(d)
-                 : "memory");
-}
-
 // `bytes` (a multiple of 16) of global memory into shared memory at dst, both 16-byte aligned,
 // counted on `bar`.
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes,
@@ -565,6 +552,39 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_
     asm volatile(
         "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
         ::"r"(dst), "l"(__cvta_generic_to_global(src)), "r"(bytes), "r"(smem_u32(bar))
+        : "memory");
+}
+
+// The same copies to every CTA of `cta_mask` (of the cluster): at dst's offset in its shared memory,
+// counted on the barrier at bar's offset there.
+__device__ __forceinline__ void tma_load_2d_multicast(uint32_t dst, const void *tmap, int x, int y,
+                                                      uint64_t *bar, uint16_t cta_mask)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+        ".multicast::cluster [%0], [%1, {%2, %3}], [%4], %5;" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(tmap)), "r"(x), "r"(y), "r"(smem_u32(bar)), "h"(cta_mask)
+        : "memory");
+}
+
+__device__ __forceinline__ void bulk_load_multicast(uint32_t dst, const void *src, uint32_t bytes,
+                                                    uint64_t *bar, uint16_t cta_mask)
+{
+    asm volatile(
+        "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.multicast::cluster [%0], [%1], "
+        "%2, [%3], %4;" ::"r"(dst),
+        "l"(__cvta_generic_to_global(src)), "r"(bytes), "r"(smem_u32(bar)), "h"(cta_mask)
+        : "memory");
+}
+
+// Arrives on the barrier at `bar`'s offset in every CTA of `cta_mask` once every tcgen05.mma issued so
+// far by this thread has completed.
+__device__ __forceinline__ void mma_commit_multicast(uint64_t *bar, uint16_t cta_mask)
+{
+    asm volatile(
+        "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64"
+        " [%0], %1;" ::"r"(smem_u32(bar)),
+        "h"(cta_mask)
         : "memory");
 }
 
