@@ -15,14 +15,16 @@
 // tile are split over the CTAs of a cluster, which leave their sums in shared memory and join them there
 // in the order of the ranks (so equal inputs give equal bits).
 //
-// Many tokens: tokens on the lanes (a lane then writes runs of consecutive outputs), tiles of 128 tokens
-// x 256 channels.  What L2 can deliver bounds a CTA that loads its own operands (52 KB a stage take about
-// 1,200 cycles at the 43 bytes per SM and cycle measured, the MMAs 513), so a cluster of 4 x 2 tiles
-// shares them: each CTA loads an eighth of the cluster's rows and sends them to the CTAs that need
-// them (multicast), 17.5 KB a stage and CTA.
+// Many tokens: tokens on the lanes (a lane then writes runs of consecutive outputs), tiles of 256 tokens
+// x 256 channels by CTA pairs (cta_group::2: each CTA holds 128 tokens and half of the channels), two
+// pairs a cluster on the same channels.  One CTA alone with a 128 x 256 tile is bound by shared memory
+// (52 KB a stage in and 48 KB read by the MMAs, 784 cycles at 128 bytes each beside the MMAs' 513) and by
+// what L2 delivers (43 bytes per SM and cycle measured: 1,200 cycles).  The pair halves B's share of
+// both, the cluster sends each quarter of B to the two CTAs that need it and each scale tile of B to all
+// four (multicast): 35 KB in and 32 KB read a stage, 25.5 KB from L2.
 //
-// Roles: warp 0 copies, warp 1 issues MMAs, warps 2..5 (TMEM lane quarter warp % 4) move scales, then write
-// the outputs.  Every wait is bounded.
+// Roles: warp 0 copies, warp 1 issues MMAs (the even CTA's, for a pair), warps 2..5 (TMEM lane quarter
+// warp % 4) move scales, then write the outputs.  Every wait is bounded.
 #include <cuda.h>
 #include <math.h>
 #include <string.h>
@@ -50,7 +52,8 @@ constexpr int X_A_BYTES = X_M * X_ROW;
 constexpr int X_MAX_STAGES = 8;
 constexpr int X_THREADS = 192;
 constexpr int X_MAX_SPLIT = 8;           // CTAs of a cluster that splits K
-constexpr int X_CM = 4, X_CN = 2;        // tiles of a cluster that shares operands: along A, along B
+constexpr int X_PAIRS = 2;               // CTA pairs of a cluster that shares B
+constexpr int X_SHARE = 2 * X_PAIRS;     // its CTAs
 
 struct MxCtrl {
     uint64_t full[X_MAX_STAGES];         // a stage's tiles and scales have landed
@@ -66,12 +69,13 @@ static_assert(sizeof(MxCtrl) <= X_CTRL_BYTES, "control block");
 // The operands by their place in the MMA: A's rows on the accumulator's lanes, B's on its columns.
 struct MxArgs {
     int a_rows, b_rows;
-    int a_tiles, b_tiles;                // row tiles of their scales (128 rows)
+    int a_tiles;                         // row tiles of A (128 rows)
     int n_tile;                          // rows of B in a tile, a multiple of 16
+    int b_held;                          // of them, in one CTA's shared memory
     int stages, k_stages, k_tiles;       // ring, K stages of a row, scale tiles of a row
     int split;                           // CTAs that share a tile's K stages
     int acc_cols, cols;                  // TMEM columns: the accumulator's (scales follow), all
-    int b_clusters;                      // clusters along B (shared operands)
+    int n_tiles;                         // tiles along B (MANY)
     int wide;                            // output rows take 32-byte stores
     const unsigned char *a_scales, *b_scales;
     const float *bias;
@@ -81,19 +85,18 @@ struct MxArgs {
 __host__ __device__ inline int sf_b_bytes(int n_tile) { return n_tile > 128 ? 4 * X_SF : 2 * X_SF; }
 __host__ __device__ inline int sf_b_cols(int n_tile) { return n_tile > 128 ? 8 : 4; }  // of a k tile
 __host__ __device__ inline int sf_cols(int n_tile) { return 8 + 2 * sf_b_cols(n_tile); }
-__host__ __device__ inline int stage_bytes(int n_tile)
+__host__ __device__ inline int stage_bytes(const MxArgs &a)
 {
-    return X_A_BYTES + n_tile * X_ROW + 2 * X_SF + sf_b_bytes(n_tile);
+    return X_A_BYTES + a.b_held * X_ROW + 2 * X_SF + sf_b_bytes(a.n_tile);
 }
 
-// MANY: A is the inputs, B the weights, operands shared in clusters of X_CM x X_CN tiles.  Else A is the
-// weights, B the inputs, K split over clusters of a.split.
+// MANY: A is the inputs, B the weights; clusters of X_PAIRS CTA pairs, one below the other along A.  Else A
+// is the weights, B the inputs, K split over clusters of a.split.
 template <typename T, bool MANY>
 __global__ void __launch_bounds__(X_THREADS)
 mx_linear_kernel(const MxArgs a, T *Y, WaitCtl wc, const __grid_constant__ CUtensorMap tmA,
                  const __grid_constant__ CUtensorMap tmB)
 {
-    constexpr int CM = MANY ? X_CM : 1, CN = MANY ? X_CN : 1;
     extern __shared__ unsigned char raw[];
     const uint32_t raw_u32 = smem_u32(raw);
     unsigned char *const base = raw + ((1024u - (raw_u32 & 1023u)) & 1023u);
@@ -102,30 +105,26 @@ mx_linear_kernel(const MxArgs a, T *Y, WaitCtl wc, const __grid_constant__ CUten
     const uint32_t ring_u32 = smem_u32(ring);
     volatile int *const abort_flag = &ctl.abort;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int sb = stage_bytes(a.n_tile);
+    const int sb = stage_bytes(a);
     const bool cluster = MANY || a.split > 1;
     const int rank = cluster ? (int)cluster_ctarank() : 0;
-    // the tile: row tile of A, first row of B; the cluster's tiles lie X_CM along A, X_CN along B
-    const int cm = MANY ? rank % CM : 0, cn = MANY ? rank / CM : 0;
-    const int group = (int)blockIdx.x / (MANY ? CM * CN : a.split);
-    const int tile = MANY ? group / a.b_clusters * CM + cm : group;
-    const long long n0 = MANY ? (long long)(group % a.b_clusters * CN + cn) * X_N
-                              : (long long)blockIdx.y * a.n_tile;
-    const int n_real = (int)max(0LL, min((long long)a.n_tile, a.b_rows - n0));   // rows of B that there are
+    // the tile: this CTA's row tile of A, the first row of B
+    const int pair = MANY ? rank >> 1 : 0, half = MANY ? rank & 1 : 0;
+    const int group = (int)blockIdx.x / (MANY ? X_SHARE : a.split);
+    const int tile = MANY ? (group / a.n_tiles) * X_SHARE + rank : group;
+    const long long n0 = MANY ? (long long)(group % a.n_tiles) * X_N : (long long)blockIdx.y * a.n_tile;
+    const int n_real = (int)min((long long)a.n_tile, a.b_rows - n0);         // rows of B that there are
     const int a_sf = tile < a.a_tiles ? 1 : 0;                       // scale tiles (per k tile) of A, of B
     const int b_sf = (n_real + 127) / 128;
     const int k0 = MANY ? 0 : (int)((long long)a.k_stages * rank / a.split);
     const int k1 = MANY ? a.k_stages : (int)((long long)a.k_stages * (rank + 1) / a.split);
-    // the CTAs that take what this one loads of A (those along B), of B (those along A)
-    const uint16_t mask_a = (uint16_t)((1u << cm) * (CN == 2 ? 1u | (1u << CM) : 1u));
-    const uint16_t mask_b = (uint16_t)(((1u << CM) - 1u) << (cn * CM));
 
     griddep_launch();
     if (threadIdx.x == 0) {
         for (int i = 0; i < a.stages; ++i) {
             mbar_init(&ctl.full[i], 1);
-            mbar_init(&ctl.scaled[i], 4);
-            mbar_init(&ctl.empty[i], CM + CN - 1);
+            mbar_init(&ctl.scaled[i], MANY ? 8 : 4);         // warps of this CTA (even CTA: of the pair)
+            mbar_init(&ctl.empty[i], MANY ? X_PAIRS : 1);
         }
         mbar_init(&ctl.done, 1);
         ctl.abort = 0;
@@ -134,7 +133,12 @@ mx_linear_kernel(const MxArgs a, T *Y, WaitCtl wc, const __grid_constant__ CUten
         prefetch_tensormap(&tmA);
         prefetch_tensormap(&tmB);
     }
-    if (warp == 1) tmem_alloc(&ctl.tmem_base, (uint32_t)a.cols);
+    if (warp == 1) {
+        if (MANY)
+            tmem_alloc_pair(&ctl.tmem_base, (uint32_t)a.cols);
+        else
+            tmem_alloc(&ctl.tmem_base, (uint32_t)a.cols);
+    }
     tc_fence_before();
     __syncthreads();
     if (MANY) cluster_sync();            // the barriers that other CTAs arrive on are ready
@@ -162,26 +166,25 @@ mx_linear_kernel(const MxArgs a, T *Y, WaitCtl wc, const __grid_constant__ CUten
                     *abort_flag = 1;
                     break;
                 }
-                const uint32_t sfs = at + (uint32_t)(X_A_BYTES + a.n_tile * X_ROW);
+                const uint32_t sfs = at + (uint32_t)(X_A_BYTES + a.b_held * X_ROW);
                 uint64_t *const bar = &ctl.full[s];
-                mbar_arrive_expect_tx(bar, (uint32_t)(X_A_BYTES + a.n_tile * X_ROW +
+                mbar_arrive_expect_tx(bar, (uint32_t)(X_A_BYTES + a.b_held * X_ROW +
                                                       (a_sf + b_sf) * kt * X_SF));
                 if constexpr (MANY) {
-                    constexpr int RA = X_M / CN, RB = X_N / CM;      // rows that this CTA loads
-                    tma_load_2d_multicast(at + cn * RA * X_ROW, &tmA, k * X_ROW, tile * X_M + cn * RA,
-                                          bar, mask_a);
-                    tma_load_2d_multicast(at + X_A_BYTES + cm * RB * X_ROW, &tmB, k * X_ROW,
-                                          (int)n0 + cm * RB, bar, mask_b);
-                    // scale tiles: A's k tile cn; B's (row tile, k tile) number cm
-                    static_assert(CN == 2 && CM == 4, "one scale tile of A and one of B for each CTA");
-                    if (cn < kt && a_sf)
-                        bulk_load_multicast(sfs + cn * X_SF, a.a_scales + sf_a + (size_t)(2 * k + cn) * X_SF,
-                                            X_SF, bar, mask_a);
-                    if ((cm & 1) < kt && (cm >> 1) < b_sf)
-                        bulk_load_multicast(sfs + (2 + cm) * X_SF,
-                                            a.b_scales + sf_b +
-                                                ((size_t)(cm >> 1) * a.k_tiles + 2 * k + (cm & 1)) * X_SF,
-                                            X_SF, bar, mask_b);
+                    // this CTA's rows of A; a quarter of B: of its half, the slice of its pair, for the CTAs
+                    // of the same half; one scale tile of B (row tile, k tile) for all
+                    constexpr int SLICE = X_N / X_SHARE;
+                    static_assert(X_PAIRS == 2, "two slices of a half, four scale tiles");
+                    tma_load_2d(at, &tmA, k * X_ROW, tile * X_M, bar);
+                    tma_load_2d_multicast(at + X_A_BYTES + pair * SLICE * X_ROW, &tmB, k * X_ROW,
+                                          (int)n0 + half * (X_N / 2) + pair * SLICE, bar,
+                                          (uint16_t)(5u << half));
+                    if (a_sf)
+                        bulk_load(sfs, a.a_scales + sf_a + (size_t)(2 * k) * X_SF, (uint32_t)(kt * X_SF), bar);
+                    if (half < kt && pair < b_sf)
+                        bulk_load_multicast(sfs + (2 + rank) * X_SF,
+                                            a.b_scales + sf_b + ((size_t)pair * a.k_tiles + 2 * k + half) * X_SF,
+                                            X_SF, bar, (uint16_t)((1u << X_SHARE) - 1u));
                 } else {
                     tma_load_2d(at, &tmA, k * X_ROW, tile * X_M, bar);
                     tma_load_2d(at + X_A_BYTES, &tmB, k * X_ROW, (int)n0, bar);
@@ -197,7 +200,7 @@ mx_linear_kernel(const MxArgs a, T *Y, WaitCtl wc, const __grid_constant__ CUten
             for (int k = max(k0, issued - a.stages); k < issued; ++k)
                 drain_wait(&ctl.full[(k - k0) % a.stages], (uint32_t)((k - k0) / a.stages) & 1u, wc,
                            MPQ_TIMEOUT_MX);
-            // ... nor an arrival of another CTA's MMAs
+            // ... nor an arrival for another pair's MMAs
             for (int k = max(k0, issued - a.stages); MANY && k < issued && !*abort_flag; ++k)
                 drain_wait_cluster(&ctl.empty[(k - k0) % a.stages], (uint32_t)((k - k0) / a.stages) & 1u,
                                    wc, MPQ_TIMEOUT_MX);
@@ -205,15 +208,15 @@ mx_linear_kernel(const MxArgs a, T *Y, WaitCtl wc, const __grid_constant__ CUten
         __syncwarp();
     } else if (warp == 1) {
         // ---------------------------------------------------------------- MMAs
-        if (lane == 0) {
-            const int n = MANY ? X_N : (n_real + 15) / 16 * 16;
-            const uint32_t id0 = idesc_mxf4(X_M, n, 0), id2 = idesc_mxf4(X_M, n, 2);
+        if (lane == 0 && half == 0) {
+            const int n = MANY ? X_N : (n_real + 15) / 16 * 16, m = MANY ? 2 * X_M : X_M;
+            const uint32_t id0 = idesc_mxf4(m, n, 0), id2 = idesc_mxf4(m, n, 2);
             const int bc = sf_b_cols(a.n_tile);
             int s = 0;
             uint32_t phase = 0;
             for (int k = k0; k < k1 && !*abort_flag; ++k) {
-                if (!mbar_wait(&ctl.full[s], phase, wc.budget) ||
-                    !mbar_wait(&ctl.scaled[s], phase, wc.budget)) {
+                // (moved by warps that saw the stage land: both CTAs' have, for a pair)
+                if (!mbar_wait_cluster(&ctl.scaled[s], phase, wc.budget)) {
                     *abort_flag = 1;
                     note_timeout(wc, MPQ_TIMEOUT_MX);
                     break;
@@ -225,11 +228,15 @@ mx_linear_kernel(const MxArgs a, T *Y, WaitCtl wc, const __grid_constant__ CUten
                 const int steps = 2 * min(2, a.k_tiles - 2 * k);
                 for (int j = 0; j < steps; ++j) {
                     const uint64_t o = (uint64_t)(j * 2);            // 32 bytes, in 16 B units
-                    mma_mxf4(tmem, ad + o, bd + o, (j & 1) ? id2 : id0, ta + 4 * (j >> 1),
-                             tb + (uint32_t)(bc * (j >> 1)), k > k0 || j > 0 ? 1u : 0u);
+                    const uint32_t id = (j & 1) ? id2 : id0, more = k > k0 || j > 0 ? 1u : 0u;
+                    const uint32_t sfa = ta + 4 * (j >> 1), sfb = tb + (uint32_t)(bc * (j >> 1));
+                    if (MANY)
+                        mma_mxf4_pair(tmem, ad + o, bd + o, id, sfa, sfb, more);
+                    else
+                        mma_mxf4(tmem, ad + o, bd + o, id, sfa, sfb, more);
                 }
-                if (MANY)
-                    mma_commit_multicast(&ctl.empty[s], mask_a | mask_b);
+                if (MANY)                // every CTA of the cluster loads for this pair
+                    mma_commit_pair(&ctl.empty[s], (uint16_t)((1u << X_SHARE) - 1u));
                 else
                     mma_commit(&ctl.empty[s]);
                 if (++s == a.stages) {
@@ -238,8 +245,11 @@ mx_linear_kernel(const MxArgs a, T *Y, WaitCtl wc, const __grid_constant__ CUten
                 }
             }
             // every MMA issued above completes before its sums are read or tensor memory released
-            mma_commit(&ctl.done);
-            drain_wait(&ctl.done, 0, wc, MPQ_TIMEOUT_MX);
+            if (MANY)
+                mma_commit_pair(&ctl.done, (uint16_t)(3u << (2 * pair)));
+            else
+                mma_commit(&ctl.done);
+            drain_wait_cluster(&ctl.done, 0, wc, MPQ_TIMEOUT_MX);
         }
         __syncwarp();
     } else {
@@ -257,7 +267,7 @@ mx_linear_kernel(const MxArgs a, T *Y, WaitCtl wc, const __grid_constant__ CUten
                     note_timeout(wc, MPQ_TIMEOUT_MX);
                 }
                 if (__any_sync(0xffffffffu, *abort_flag)) break;
-                const uint32_t sfs = ring_u32 + (uint32_t)(s * sb + X_A_BYTES + a.n_tile * X_ROW) +
+                const uint32_t sfs = ring_u32 + (uint32_t)(s * sb + X_A_BYTES + a.b_held * X_ROW) +
                                      (uint32_t)(lane * 16);
                 const uint32_t ta = quarter + (uint32_t)(a.acc_cols + s * sf_cols(a.n_tile));
                 const int kt = min(2, a.k_tiles - 2 * k);
@@ -275,7 +285,12 @@ mx_linear_kernel(const MxArgs a, T *Y, WaitCtl wc, const __grid_constant__ CUten
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&ctl.scaled[s]);
+                if (lane == 0) {
+                    if (MANY)
+                        mbar_arrive_cluster(&ctl.scaled[s], (uint32_t)(rank & ~1));
+                    else
+                        mbar_arrive(&ctl.scaled[s]);
+                }
                 if (++s == a.stages) {
                     s = 0;
                     phase ^= 1u;
@@ -284,7 +299,7 @@ mx_linear_kernel(const MxArgs a, T *Y, WaitCtl wc, const __grid_constant__ CUten
         }
         // ---------------------------------------------------------------- outputs
         const int i = tile * X_M + q * 32 + lane;                    // this lane's row of A
-        if (!drain_wait(&ctl.done, 0, wc, MPQ_TIMEOUT_MX)) *abort_flag = 1;
+        if (!drain_wait_cluster(&ctl.done, 0, wc, MPQ_TIMEOUT_MX)) *abort_flag = 1;
         if (!__any_sync(0xffffffffu, *abort_flag)) {
             tc_fence_after();
             const float bias = !MANY && a.bias && i < a.a_rows && a.split == 1 ? a.bias[i] : 0.0f;
@@ -348,7 +363,10 @@ mx_linear_kernel(const MxArgs a, T *Y, WaitCtl wc, const __grid_constant__ CUten
         __syncthreads();
     if (warp == 1) {
         tc_fence_after();
-        tmem_dealloc(tmem, (uint32_t)a.cols);
+        if (MANY)
+            tmem_dealloc_pair(tmem, (uint32_t)a.cols);
+        else
+            tmem_dealloc(tmem, (uint32_t)a.cols);
     }
 }
 
@@ -368,8 +386,8 @@ mpq_status launch_typed(const MxArgs &a, const void *A, const void *B, int row_b
     memset(&tmB, 0, sizeof(tmB));
     const cuuint64_t row = (cuuint64_t)row_bytes;
     const cuuint64_t da[2] = {row, (cuuint64_t)a.a_rows}, db[2] = {row, (cuuint64_t)a.b_rows}, st[1] = {row};
-    const cuuint32_t ba[2] = {X_ROW, MANY ? X_M / X_CN : X_M};
-    const cuuint32_t bb[2] = {X_ROW, MANY ? (cuuint32_t)(X_N / X_CM) : (cuuint32_t)a.n_tile};
+    const cuuint32_t ba[2] = {X_ROW, X_M};
+    const cuuint32_t bb[2] = {X_ROW, MANY ? (cuuint32_t)(X_N / X_SHARE) : (cuuint32_t)a.n_tile};
     if (!encode_tile_map(&tmA, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, A, da, st, ba,
                          CU_TENSOR_MAP_SWIZZLE_128B) ||
         !encode_tile_map(&tmB, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, B, db, st, bb,
@@ -377,7 +395,7 @@ mpq_status launch_typed(const MxArgs &a, const void *A, const void *B, int row_b
         set_error("mx linear: tensor map encoding failed");
         return MPQ_ERR_CUDA;
     }
-    const size_t smem = 1024 + X_CTRL_BYTES + (size_t)a.stages * stage_bytes(a.n_tile);
+    const size_t smem = 1024 + X_CTRL_BYTES + (size_t)a.stages * stage_bytes(a);
     static std::atomic<int> limit[kMaxDevices];
     cudaError_t e = allow_smem(reinterpret_cast<const void *>(mx_linear_kernel<T, MANY>), limit, smem);
     if (e != cudaSuccess) return cuda_status(e, "cudaFuncSetAttribute");
@@ -404,7 +422,7 @@ mpq_status launch_typed(const MxArgs &a, const void *A, const void *B, int row_b
 // Stages that fit into `room` bytes of shared memory, and the tensor memory columns.
 void size_ring(MxArgs &a, int room)
 {
-    a.stages = std::min(X_MAX_STAGES, (room - 1024 - X_CTRL_BYTES) / stage_bytes(a.n_tile));
+    a.stages = std::min(X_MAX_STAGES, (room - 1024 - X_CTRL_BYTES) / stage_bytes(a));
     a.acc_cols = pow2_at_least(a.n_tile, 32);
     a.cols = pow2_at_least(a.acc_cols + a.stages * sf_cols(a.n_tile), 32);
 }
@@ -423,38 +441,37 @@ mpq_status launch_mx_linear(const mpq_mx_matrix *xl, const void *X, const mpq_mx
     const unsigned char *const x = static_cast<const unsigned char *>(X);
     const unsigned char *const w = static_cast<const unsigned char *>(W);
     const int T = xl->rows, C = wl->rows, sms = sm_count();
-    // Tiles of 128 tokens x 256 channels in clusters of 4 x 2 where they fill half the SMs or more
-    const long long m_cl = (((long long)T + X_M - 1) / X_M + X_CM - 1) / X_CM;
-    const long long n_cl = (((long long)C + X_N - 1) / X_N + X_CN - 1) / X_CN;
-    if (m_cl * n_cl * X_CM * X_CN * 2 >= sms && T > X_N) {
+    // pairs' tiles of 256 tokens x 256 channels where their clusters fill half the SMs or more
+    const long long m_cl = ((long long)T + X_SHARE * X_M - 1) / (X_SHARE * X_M);
+    const long long n_cl = ((long long)C + X_N - 1) / X_N;
+    const long long ctas = m_cl * n_cl * X_SHARE;
+    if (2 * ctas >= sms && T > X_N) {
         a.a_rows = T;
         a.b_rows = C;
         a.a_tiles = xl->row_tiles;
-        a.b_tiles = wl->row_tiles;
         a.a_scales = x + xl->off_scales;
         a.b_scales = w + wl->off_scales;
         a.n_tile = X_N;
+        a.b_held = X_N / 2;
         a.split = 1;
-        a.b_clusters = (int)n_cl;
+        a.n_tiles = (int)n_cl;
         a.wide = rows_aligned(Y, y_type, ldy);
         size_ring(a, max_smem_optin());
-        const long long ctas = m_cl * n_cl * X_CM * X_CN;
         if (ctas > 0x7fffffffLL) {
             set_error("mx linear: T = %d, C = %d are too large", T, C);
             return MPQ_ERR_UNSUPPORTED;
         }
         return by_type(y_type, [&](auto t) {
-            return launch_typed<decltype(t), true>(a, X, W, wl->d_pad / 2, dim3((unsigned)ctas),
-                                                   X_CM * X_CN, Y, stream);
+            return launch_typed<decltype(t), true>(a, X, W, wl->d_pad / 2, dim3((unsigned)ctas), X_SHARE, Y,
+                                                   stream);
         });
     }
     a.a_rows = C;
     a.b_rows = T;
     a.a_tiles = wl->row_tiles;
-    a.b_tiles = xl->row_tiles;
     a.a_scales = w + wl->off_scales;
     a.b_scales = x + xl->off_scales;
-    a.n_tile = T >= X_N ? X_N : (T + 15) / 16 * 16;
+    a.n_tile = a.b_held = T >= X_N ? X_N : (T + 15) / 16 * 16;
     // two CTAs share an SM where a ring of four stages leaves room for it (up to 64 tokens)
     const bool two = a.n_tile <= 64;
     size_ring(a, two ? 112 * 1024 : max_smem_optin());

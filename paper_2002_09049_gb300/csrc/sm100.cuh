@@ -531,6 +531,21 @@ __device__ __forceinline__ void mma_mxf4(uint32_t d_tmem, uint64_t a_desc, uint6
         : "memory");
 }
 
+// The CTA-pair form, as mma_f16_pair's: A is M = 256 rows, 128 in each CTA; B is N rows, N/2 in each; each
+// CTA's tensor memory holds the scales of its own rows of A at sfa and of all rows of B at sfb.
+__device__ __forceinline__ void mma_mxf4_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc,
+                                              uint32_t idesc, uint32_t sfa, uint32_t sfb,
+                                              uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], "
+        "p;\n\t}" ::"r"(d_tmem),
+        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate)
+        : "memory");
+}
+
 // Instruction descriptor, kind::mxf4: A and B E2M1, E8M0 scales, both K-major; the scales of this
 // K = 64 are bytes sf, sf + 1 (sf 0 or 2) of the 4-byte words in tensor memory.
 __host__ __device__ constexpr uint32_t idesc_mxf4(int M, int N, int sf)
@@ -574,17 +589,6 @@ __device__ __forceinline__ void bulk_load_multicast(uint32_t dst, const void *sr
         "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.multicast::cluster [%0], [%1], "
         "%2, [%3], %4;" ::"r"(dst),
         "l"(__cvta_generic_to_global(src)), "r"(bytes), "r"(smem_u32(bar)), "h"(cta_mask)
-        : "memory");
-}
-
-// Arrives on the barrier at `bar`'s offset in every CTA of `cta_mask` once every tcgen05.mma issued so
-// far by this thread has completed.
-__device__ __forceinline__ void mma_commit_multicast(uint64_t *bar, uint16_t cta_mask)
-{
-    asm volatile(
-        "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64"
-        " [%0], %1;" ::"r"(smem_u32(bar)),
-        "h"(cta_mask)
         : "memory");
 }
 
