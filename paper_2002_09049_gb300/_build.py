@@ -1,7 +1,8 @@
 """Builds libmpq.so (the C-ABI library) in-tree from csrc/*.cu with nvcc for sm_103a.
 
 Translation units compile in parallel, then link into one shared library with the CUDA runtime
-linked statically.  Run ``python -m paper_2002_09049_gb300._build`` or call ``build()``.
+linked statically.  The native marshalling of the serving calls (csrc/bind/) is a Python extension of its
+own, _serve_binding.so, compiled against the torch that imports it.  Run ``python -m paper_2002_09049_gb300._build`` or call ``build()``.
 ``build(checked=True)`` (``--checked``) builds the checked library, libmpq_checked.so: the same
 sources with -DMPQ_CHECK_BOUNDS, whose kernels count and skip out-of-range accesses.
 """
@@ -20,6 +21,7 @@ CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libmpq.so")
 CHECKED_LIB = os.path.join(PKG, "libmpq_checked.so")
+BINDING = os.path.join(PKG, "_serve_binding.so")
 ROOT = os.path.dirname(PKG)
 INCLUDE = os.path.join(ROOT, "include")
 
@@ -51,6 +53,36 @@ def up_to_date(lib: str = LIB) -> bool:
     return all(os.path.getmtime(p) <= t for p in _deps())
 
 
+def _binding_up_to_date() -> bool:
+    src = os.path.join(CSRC, "bind", "serve_binding.cpp")
+    return os.path.exists(BINDING) and all(
+        os.path.getmtime(p) <= os.path.getmtime(BINDING)
+        for p in (src, os.path.join(INCLUDE, "mpq.h")))
+
+
+def _build_binding(exe: str) -> None:
+    """Compile csrc/bind/serve_binding.cpp -> _serve_binding.so with the host compiler."""
+    import sysconfig
+
+    import torch
+    home = os.path.dirname(torch.__file__)
+    inc = [os.path.join(home, "include"),
+           os.path.join(home, "include", "torch", "csrc", "api", "include"),
+           os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(exe))), "include"),
+           sysconfig.get_paths()["include"], INCLUDE]
+    libs = os.path.join(home, "lib")
+    tmp = BINDING + f".{os.getpid()}.tmp"
+    cmd = [shutil.which("g++") or "c++", "-O2", "-std=c++17", "-fPIC", "-shared",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           *[f"-I{p}" for p in inc], os.path.join(CSRC, "bind", "serve_binding.cpp"), "-o", tmp,
+           f"-L{libs}", f"-Wl,-rpath,{libs}", "-ltorch_python", "-ltorch", "-ltorch_cpu",
+           "-ltorch_cuda", "-lc10", "-lc10_cuda"]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError(f"compiling the serving calls' binding failed:\n{res.stdout}\n{res.stderr}")
+    os.replace(tmp, BINDING)
+
+
 def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False,
           checked: bool = False) -> str:
     """Compile csrc/*.cu -> libmpq.so, or with checked=True -> libmpq_checked.so (skipped when
@@ -58,10 +90,14 @@ def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False,
     lib = CHECKED_LIB if checked else LIB
     obj_dir = os.path.join(BUILD, "checked") if checked else BUILD
     with _lock:
-        if not force and up_to_date(lib):
+        exe = nvcc()
+        stale = force or not up_to_date(lib)
+        bind = force or not _binding_up_to_date()
+        if not stale:
+            if bind:
+                _build_binding(exe)
             return lib
         os.makedirs(obj_dir, exist_ok=True)
-        exe = nvcc()
         extra = ["-Xptxas", "-v"] if ptxas_info else []
         if checked:
             extra += ["-DMPQ_CHECK_BOUNDS"]
@@ -77,7 +113,10 @@ def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False,
             return obj
 
         with ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 4)) as ex:
+            extension = ex.submit(_build_binding, exe) if bind else None
             objs = list(ex.map(compile_one, _sources()))
+            if extension:
+                extension.result()
         tmp = lib + f".{os.getpid()}.tmp"
         cmd = [exe, *ARCH, "-shared", "-cudart", "static", "-o", tmp, *objs]
         res = subprocess.run(cmd, capture_output=True, text=True)

@@ -33,7 +33,6 @@ MPQ_FAULT_BOUNDS = 0x10000            # mpq_device_status: the checked build ski
 MPQ_BUILD_CHECK_BOUNDS = 0x1          # mpq_build_options: the checked build
 
 MPQ_CACHE_WORKSPACE = 1 << 25         # bytes of mpq_cache_attention's workspace
-MPQ_TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}   # MPQ_F32, MPQ_F16, MPQ_BF16
 
 MPQ_STATUS = {0: "MPQ_OK", 1: "MPQ_ERR_INVALID_ARG", 2: "MPQ_ERR_NONFINITE",
               3: "MPQ_ERR_UNSUPPORTED", 4: "MPQ_ERR_CUDA", 5: "MPQ_ERR_TIMEOUT",
@@ -462,52 +461,30 @@ def mpq_center_weights(W, mode: int = MPQ_CENTER_PER_CHANNEL, center=None, Wc=No
 
 
 # ---------------------------------------------------------------------------------------------
-# Serving in few bits.  A decode step makes these calls one after another with little work in each,
-# so what a call costs on the host counts: a tensor that is as it should be is seen so in one
-# expression, and outputs allocated here are not looked at again.
+# Serving in few bits.  A decode step makes these calls one after another with little work in each, so
+# their tensors are checked and their outputs allocated by a native extension (csrc/bind/), which calls
+# the loaded library by address.
 
 
-def _is(t, dtype, shape):
-    """t is a contiguous CUDA tensor of this type and shape."""
-    try:
-        return t.dtype is dtype and t.shape == shape and t.is_cuda and t.is_contiguous()
-    except AttributeError:
-        return False
+class _Unloaded:
+    """Stands for the extension until the first call."""
+
+    def __getattr__(self, name):
+        global _native
+        lib = load()
+        try:
+            from . import _serve_binding
+        except ImportError as e:
+            raise RuntimeError(f"{_build.BINDING} is missing or was built for another Python or torch: "
+                               "build it with paper_2002_09049_gb300._build.build() (there is no "
+                               "fallback)") from e
+        _serve_binding.init(_check, {f: ctypes.cast(getattr(lib, f), ctypes.c_void_p).value
+                                     for f in SIGNATURES if f.startswith(("mpq_mx_", "mpq_cache_"))})
+        _native = _serve_binding
+        return getattr(_native, name)
 
 
-def _need(t, name, dtype, shape):
-    if not _is(t, dtype, shape):
-        _dev(t, name, dtype, shape)
-
-
-def _type(t, name):
-    """The MPQ_* number of a floating element type."""
-    got = MPQ_TYPES.get(t)
-    if got is None:
-        raise TypeError(f"{name} must be torch.float32, torch.float16 or torch.bfloat16, got {t}")
-    return got
-
-
-def _rows(t, name, rows, d):
-    """A CUDA matrix [rows][d] whose rows are contiguous and do not overlap; returns its row stride."""
-    if not isinstance(t, torch.Tensor):
-        raise TypeError(f"{name} must be a torch tensor")
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a CUDA tensor")
-    if t.shape != (rows, d):
-        raise ValueError(f"{name} must have shape {(rows, d)}, got {tuple(t.shape)}")
-    step, unit = t.stride()
-    if (unit != 1 and d > 1) or (step < d and rows > 1):
-        raise ValueError(f"{name} must have contiguous rows that do not overlap")
-    return step if step > d else d
-
-
-def _packed(t, name, layout):
-    """The address of a packed matrix's buffer."""
-    _dev(t, name, torch.uint8)
-    if t.numel() < layout.bytes:
-        raise ValueError(f"{name} is smaller than layout.bytes = {layout.bytes}")
-    return t.data_ptr()
+_native = _Unloaded()
 
 
 @functools.lru_cache(maxsize=256)
@@ -523,52 +500,18 @@ def mpq_mx_quantize(X, layout: MxMatrix = None, packed=None, stream=None):
     buffer (uint8 [layout.bytes]) of mpq_mx_layout(rows, d)."""
     if layout is None:
         layout = mpq_mx_layout(*X.shape)
-    ld = _rows(X, "X", layout.rows, layout.d)
-    if packed is None:
-        packed = torch.empty(layout.bytes, dtype=torch.uint8, device=X.device)
-        to = packed.data_ptr()
-    else:
-        to = _packed(packed, "packed", layout)
-    st = load().mpq_mx_quantize(X.data_ptr(), _type(X.dtype, "X"), ld, layout, to, _stream(stream))
-    if st:
-        _check(st, "mpq_mx_quantize")
-    return packed
+    return _native.mx_quantize(X, layout, packed, stream)
 
 
 def mpq_mx_dequantize(packed, layout: MxMatrix, dtype=torch.float32, Y=None, stream=None):
     """The values [rows][d] of a packed matrix."""
-    at = _packed(packed, "packed", layout)
-    if Y is None:
-        ld = layout.d
-        Y = torch.empty((layout.rows, ld), dtype=dtype, device=packed.device)
-    else:
-        ld = _rows(Y, "Y", layout.rows, layout.d)
-    st = load().mpq_mx_dequantize(at, layout, Y.data_ptr(), _type(Y.dtype, "Y"), ld,
-                                  _stream(stream))
-    if st:
-        _check(st, "mpq_mx_dequantize")
-    return Y
+    return _native.mx_dequantize(packed, layout, dtype, Y, stream)
 
 
 def mpq_mx_linear(X, x_layout: MxMatrix, W, w_layout: MxMatrix, bias=None, dtype=torch.bfloat16,
                   Y=None, stream=None):
     """Y [T][C] = X W^T + bias for packed inputs X [T][d] and weights W [C][d]; bias fp32 [C]."""
-    x, w = _packed(X, "X", x_layout), _packed(W, "W", w_layout)
-    T, C = x_layout.rows, w_layout.rows
-    add = None      # (bias keeps its name: the last reference to it may be this one)
-    if bias is not None:
-        _need(bias, "bias", torch.float32, (C,))
-        add = bias.data_ptr()
-    if Y is None:
-        ld = C
-        Y = torch.empty((T, C), dtype=dtype, device=X.device)
-    else:
-        ld = _rows(Y, "Y", T, C)
-    st = load().mpq_mx_linear(x_layout, x, w_layout, w, add, Y.data_ptr(), _type(Y.dtype, "Y"), ld,
-                              _stream(stream))
-    if st:
-        _check(st, "mpq_mx_linear")
-    return Y
+    return _native.mx_linear(X, x_layout, W, w_layout, bias, dtype, Y, stream)
 
 
 @functools.lru_cache(maxsize=256)
@@ -587,55 +530,17 @@ def mpq_cache_empty(layout: KvCache, device):
             torch.empty(layout.scales_shape, dtype=torch.float32, device=device))
 
 
-def _storage(layout, codes, scales):
-    """The addresses of a cache's codes and scales."""
-    _need(codes, "codes", torch.uint8, layout.codes_shape)
-    _need(scales, "scales", torch.float32, layout.scales_shape)
-    return codes.data_ptr(), scales.data_ptr()
-
-
 def mpq_cache_write(K, V, slots, layout: KvCache, codes, scales, stream=None):
     """Quantises K and V [T][heads][dim] (fp32, fp16 or bf16; tokens and heads may lie apart, the same
     for both) into the slots [T] int64 of the cache; slots outside it are skipped."""
-    _need(slots, "slots", torch.int64, slots.shape[:1])
-    shape = (slots.shape[0], layout.heads, layout.dim)
-    steps = K.stride()
-    for t, name in ((K, "K"), (V, "V")):
-        if not t.is_cuda:
-            raise ValueError(f"{name} must be a CUDA tensor")
-        if t.shape != shape:
-            raise ValueError(f"{name} must have shape {shape}, got {tuple(t.shape)}")
-    if K.dtype != V.dtype or steps != V.stride():
-        raise ValueError("K and V must have one type and the same strides")
-    if steps[2] != 1:
-        raise ValueError("K and V must have contiguous rows")
-    at, sc = _storage(layout, codes, scales)
-    st = load().mpq_cache_write(K.data_ptr(), V.data_ptr(), _type(K.dtype, "K"), steps[0], steps[1],
-                                shape[0], slots.data_ptr(), layout, at, sc, _stream(stream))
-    if st:
-        _check(st, "mpq_cache_write")
+    _native.cache_write(K, V, slots, layout, codes, scales, stream)
 
 
 def mpq_cache_read(slots, layout: KvCache, codes, scales, dtype=torch.bfloat16, K=None, V=None,
                    stream=None):
     """The keys and values [T][heads][dim] that the cache holds in the slots [T] int64 (zeros for one
     outside it)."""
-    _need(slots, "slots", torch.int64, slots.shape[:1])
-    at, sc = _storage(layout, codes, scales)
-    shape = (slots.shape[0], layout.heads, layout.dim)
-    if K is None:
-        K = torch.empty(shape, dtype=dtype, device=slots.device)
-    else:
-        _need(K, "K", K.dtype, shape)
-    if V is None:
-        V = torch.empty(shape, dtype=K.dtype, device=slots.device)
-    else:
-        _need(V, "V", K.dtype, shape)
-    st = load().mpq_cache_read(slots.data_ptr(), shape[0], layout, at, sc, K.data_ptr(),
-                               V.data_ptr(), _type(K.dtype, "K"), _stream(stream))
-    if st:
-        _check(st, "mpq_cache_read")
-    return K, V
+    return _native.cache_read(slots, layout, codes, scales, dtype, K, V, stream)
 
 
 def mpq_cache_attention(Q, table, lens, layout: KvCache, codes, scales, scale: float = None,
@@ -645,36 +550,8 @@ def mpq_cache_attention(Q, table, lens, layout: KvCache, codes, scales, scale: f
     1 / sqrt(dim) by default; window: the newest tokens attended to (0: all).  lse: an fp32 [B][q_heads]
     tensor that receives the logarithm of the softmax's sum.  workspace: MPQ_CACHE_WORKSPACE bytes,
     zeroed before the first call and kept from call to call (by default taken from the pool)."""
-    B, cols = table.shape
-    shape, dim = Q.shape, layout.dim
-    if len(shape) != 3 or shape[0] != B or shape[2] != dim:
-        raise ValueError(f"Q must have shape ({B}, q_heads, {dim}), got {tuple(shape)}")
-    if not Q.is_cuda:
-        raise ValueError("Q must be a CUDA tensor")
-    q_heads, steps = shape[1], Q.stride()
-    if steps[2] != 1 or (q_heads > 1 and steps[1] != dim):
-        raise ValueError("Q must have consecutive heads")
-    _need(table, "table", torch.int32, (B, cols))
-    _need(lens, "lens", torch.int32, (B,))
-    at, sc = _storage(layout, codes, scales)
-    if O is None:
-        O = torch.empty(shape, dtype=Q.dtype, device=Q.device)
-    else:
-        _need(O, "O", Q.dtype, shape)
-    ws = size = log = None
-    if lse is not None:
-        _need(lse, "lse", torch.float32, (B, q_heads))
-        log = lse.data_ptr()
-    if workspace is not None:
-        _dev(workspace, "workspace", torch.uint8)
-        ws, size = workspace.data_ptr(), workspace.numel()
-    st = load().mpq_cache_attention(
-        Q.data_ptr(), _type(Q.dtype, "Q"), steps[0], B, q_heads, layout, at, sc, table.data_ptr(),
-        cols, lens.data_ptr(), dim ** -0.5 if scale is None else scale, window, O.data_ptr(), log,
-        ws, size or 0, _stream(stream))
-    if st:
-        _check(st, "mpq_cache_attention")
-    return O
+    return _native.cache_attention(Q, table, lens, layout, codes, scales, scale, window, O, lse,
+                                   workspace, stream)
 
 
 def mpq_status_string(status: int) -> str:
