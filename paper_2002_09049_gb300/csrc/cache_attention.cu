@@ -294,9 +294,6 @@ cache_attention_kernel(const AttnArgs a, WaitCtl wc, const __grid_constant__ CUt
     __shared__ long long sh_pre[THREADS];        // stages before each thread's sequences
     __shared__ long long sh_warp[W];
     __shared__ Part sh_part[2 * W];
-    __shared__ int sh_list[2 * W];               // the parts that there are, in order
-    __shared__ int sh_run[2 * W + 1];            // where runs of parts of one row begin in it
-    __shared__ int sh_counts[2];                 // parts, runs
     __shared__ int sh_open[2], sh_c0[2], sh_c1[2], sh_last[2];
     __shared__ __align__(16) float sh_slice[W][D];
     griddep_launch();
@@ -320,7 +317,7 @@ cache_attention_kernel(const AttnArgs a, WaitCtl wc, const __grid_constant__ CUt
     const size_t o_size = (size_t)a.B * a.q_heads * D;
     griddep_wait();
 
-    // ---- the stages before each thread's sequences, and sequences with nothing to attend to -----------
+    // ---- the stages before each thread's sequences ------------------------------------------------
     const int per = (a.B + THREADS - 1) / THREADS;
     const int b_lo = min(tid * per, a.B), b_hi = min(b_lo + per, a.B);
     long long pre = 0;
@@ -340,13 +337,17 @@ cache_attention_kernel(const AttnArgs a, WaitCtl wc, const __grid_constant__ CUt
         total += sh_warp[w];
     }
     sh_pre[tid] = pre - mine;
-    for (long long b = blockIdx.x + (long long)warp * gridDim.x; b < a.B; b += (long long)W * gridDim.x) {
-        if (span_of(a, (int)b).stages() > 0) continue;
-        const float zero[8] = {};
-        for (int i = lane * 8; i < a.q_heads * D; i += 256)
-            if (MPQ_IN(b * a.q_heads * D + i + 7, o_size)) store8(O + b * a.q_heads * D + i, zero);
-        for (int i = lane; a.lse && i < a.q_heads; i += 32) a.lse[b * a.q_heads + i] = -INFINITY;
-    }
+    // sequences with nothing to attend to: a warp each
+    auto empty_rows = [&]() {
+        for (long long b = blockIdx.x + (long long)warp * gridDim.x; b < a.B;
+             b += (long long)W * gridDim.x) {
+            if (span_of(a, (int)b).stages() > 0) continue;
+            const float zero[8] = {};
+            for (int i = lane * 8; i < a.q_heads * D; i += 256)
+                if (MPQ_IN(b * a.q_heads * D + i + 7, o_size)) store8(O + b * a.q_heads * D + i, zero);
+            for (int i = lane; a.lse && i < a.q_heads; i += 32) a.lse[b * a.q_heads + i] = -INFINITY;
+        }
+    };
     // the warps that take part, and this one's range.  A CTA a row where there are no more rows than CTAs
     // and a warp then has A_ROW stages at most: joining CTAs takes longer than that.
     const long long rows = (long long)some * units;
@@ -354,7 +355,10 @@ cache_attention_kernel(const AttnArgs a, WaitCtl wc, const __grid_constant__ CUt
     const int workers = by_row ? (int)min(rows * W, total)
                                : (int)min((long long)gridDim.x * W, max(total / A_LEAST, 1LL));
     const int me = blockIdx.x * W + warp;
-    if ((int)blockIdx.x * W >= workers || total == 0) return;
+    if ((int)blockIdx.x * W >= workers || total == 0) {
+        empty_rows();
+        return;
+    }
     const Cut cut = {total, workers};
     const long long r0 = me < workers ? cut.begin(me) : total;
     long long left = me < workers ? cut.begin(me + 1) - r0 : 0;
@@ -768,34 +772,27 @@ cache_attention_kernel(const AttnArgs a, WaitCtl wc, const __grid_constant__ CUt
             }
         }
     }
+    empty_rows();
     __syncthreads();
 
     // ---- rows that several warps share: runs of parts of one row, in the order of the warps ------------
+    // (every warp finds them for itself: lane p looks at part p)
     static_assert(2 * W <= 32, "one lane per part");
-    if (warp == 0) {
-        const Part part = lane < 2 * W ? sh_part[lane] : Part{-1, 0, 0, 0};
-        const unsigned live = __ballot_sync(0xffffffffu, part.b >= 0);
-        const unsigned lower = live & ((1u << lane) - 1u);
-        const int before = 31 - __clz((int)lower);            // the part before, or -1
-        const int prev_b = __shfl_sync(0xffffffffu, part.b, before & 31);
-        const int prev_u = __shfl_sync(0xffffffffu, part.u, before & 31);
-        const bool first = part.b >= 0 && (before < 0 || prev_b != part.b || prev_u != part.u);
-        const unsigned firsts = __ballot_sync(0xffffffffu, first);
-        if (part.b >= 0) sh_list[__popc(lower)] = lane;
-        if (first) sh_run[__popc(firsts & ((1u << lane) - 1u))] = __popc(lower);
-        if (lane == 0) {
-            sh_run[__popc(firsts)] = __popc(live);
-            sh_counts[0] = __popc(live);
-            sh_counts[1] = __popc(firsts);
-        }
-    }
-    __syncthreads();
-    const int runs = sh_counts[1];
+    const Part part = lane < 2 * W ? sh_part[lane] : Part{-1, 0, 0, 0};
+    const unsigned live = __ballot_sync(0xffffffffu, part.b >= 0);
+    if (live == 0) return;
+    const int before = 31 - __clz((int)(live & ((1u << lane) - 1u)));       // the part before, or -1
+    const int prev_b = __shfl_sync(0xffffffffu, part.b, before & 31);
+    const int prev_u = __shfl_sync(0xffffffffu, part.u, before & 31);
+    const unsigned firsts = __ballot_sync(
+        0xffffffffu, part.b >= 0 && (before < 0 || prev_b != part.b || prev_u != part.u));
+    const int first_part = __ffs((int)firsts) - 1, last_run = 31 - __clz((int)firsts);
+    const int last_part = 31 - __clz((int)live);
     // the rows that other CTAs have parts of, the first run's (begun before) and the last one's, and
     // their CTAs: those of the workers of the row's first and last stage
     if (warp == W - 1 && lane < 2) {
-        const Part p = runs > 0 ? sh_part[sh_list[lane ? sh_run[runs - 1] : 0]] : Part{-1, 0, 0, 0};
-        sh_open[lane] = runs > 0 && (lane ? p.starts && !sh_part[sh_list[sh_counts[0] - 1]].ends : !p.starts);
+        const Part p = sh_part[lane ? last_run : first_part];
+        sh_open[lane] = lane ? p.starts && !sh_part[last_part].ends : !p.starts;
         if (sh_open[lane]) {
             long long g0 = sh_pre[p.b / per];
             for (int b = p.b / per * per; b < p.b; ++b)
@@ -807,52 +804,57 @@ cache_attention_kernel(const AttnArgs a, WaitCtl wc, const __grid_constant__ CUt
         }
     }
     const float *const kept = warp_sums + (size_t)blockIdx.x * W * S::SUMS;
-    // a warp takes a head of a run at a time, a lane the statistics of a part
-    for (int item = warp; item < runs * H; item += W) {
-        const int run = item / H, h = item % H;
-        const int p0 = sh_run[run], n = sh_run[run + 1] - p0;
-        const Part lead = sh_part[sh_list[p0]];
-        const bool starts = lead.starts, ends = sh_part[sh_list[p0 + n - 1]].ends;
-        const int head0 = lead.u % a.blocks * H;
-        if (h >= min(H, a.group - head0)) continue;
-        const int mine_p = lane < n ? sh_list[p0 + lane] : 0;
-        // a part's sums: in its warp's shared memory, or kept in the workspace
-        const float *const at = (mine_p & 1)
-                                    ? reinterpret_cast<const float *>(smem + (mine_p >> 1) * S::WARP_BYTES)
-                                    : kept + (size_t)(mine_p >> 1) * S::SUMS;
-        Stat s = {-FLT_MAX, -FLT_MAX, 0.0f};
-        if (lane < n) s = {at[h], at[H + h], at[2 * H + h]};
-        const float ref = s.ref;
-        s = add_lanes(s);
-        const float factor = ex2(ref - s.ref);
-        float acc[E];
+    // a warp takes a head of a run at a time, a lane the statistics of its part
+    const float *const at = (lane & 1) ? reinterpret_cast<const float *>(smem + (lane >> 1) * S::WARP_BYTES)
+                                       : kept + (size_t)(lane >> 1) * S::SUMS;
+    int item = 0;
+    for (unsigned rest = firsts; rest;) {
+        const int p0 = __ffs((int)rest) - 1;
+        rest &= rest - 1;
+        const unsigned run = live & ~((1u << p0) - 1u) & (rest ? (rest & (0u - rest)) - 1u : ~0u);
+        const Part lead = sh_part[p0];
+        const bool starts = lead.starts, ends = sh_part[31 - __clz((int)run)].ends;
+        const int head0 = lead.u % a.blocks * H, heads = min(H, a.group - head0);
+        const int h0 = (warp + W - item % W) % W;        // this warp's first head of the run
+        item += heads;
+        for (int h = h0; h < heads; h += W) {
+            Stat s = {-FLT_MAX, -FLT_MAX, 0.0f};
+            if ((run >> lane) & 1u) s = {at[h], at[H + h], at[2 * H + h]};
+            const float ref = s.ref;
+            s = add_lanes(s);
+            const float factor = ex2(ref - s.ref);
+            float acc[E];
 #pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] = 0.0f;
+            for (int e = 0; e < E; ++e) acc[e] = 0.0f;
+            unsigned left = run;
 #pragma unroll 4
-        for (int i = 0; i < n; ++i) {
-            const float f = __shfl_sync(0xffffffffu, factor, i);
-            const float *const q = reinterpret_cast<const float *>(
-                __shfl_sync(0xffffffffu, (unsigned long long)at, i)) + 3 * H + h * S::LD + lane;
+            for (int n = __popc(run); n > 0; --n) {
+                const int i = __ffs((int)left) - 1;
+                left &= left - 1;
+                const float f = __shfl_sync(0xffffffffu, factor, i);
+                const float *const q = reinterpret_cast<const float *>(
+                    __shfl_sync(0xffffffffu, (unsigned long long)at, i)) + 3 * H + h * S::LD + lane;
 #pragma unroll
-            for (int e = 0; e < E; ++e) acc[e] += f * q[e * 32];
-        }
-        if (starts && ends) {
-            const size_t row = (size_t)lead.b * a.q_heads + (lead.u / a.blocks) * a.group + head0 + h;
-            const float2 f = to_output(s);
-#pragma unroll
-            for (int e = 0; e < E; ++e)
-                if (MPQ_IN(row * D + e * 32 + lane, o_size))
-                    O[row * D + e * 32 + lane] = from_f32<T>(acc[e] * f.x * f.y);
-            if (a.lse && lane == 0) a.lse[row] = natural_lse(s);
-        } else {
-            float *const to = cta_sums + (size_t)(2 * blockIdx.x + (starts ? 1 : 0)) * S::SUMS;
-            if (lane == 0) {
-                __stcg(to + h, s.ref);
-                __stcg(to + H + h, s.top);
-                __stcg(to + 2 * H + h, s.sum);
+                for (int e = 0; e < E; ++e) acc[e] += f * q[e * 32];
             }
+            if (starts && ends) {
+                const size_t row = (size_t)lead.b * a.q_heads + (lead.u / a.blocks) * a.group + head0 + h;
+                const float2 f = to_output(s);
 #pragma unroll
-            for (int e = 0; e < E; ++e) __stcg(to + 3 * H + h * S::LD + e * 32 + lane, acc[e]);
+                for (int e = 0; e < E; ++e)
+                    if (MPQ_IN(row * D + e * 32 + lane, o_size))
+                        O[row * D + e * 32 + lane] = from_f32<T>(acc[e] * f.x * f.y);
+                if (a.lse && lane == 0) a.lse[row] = natural_lse(s);
+            } else {
+                float *const to = cta_sums + (size_t)(2 * blockIdx.x + (starts ? 1 : 0)) * S::SUMS;
+                if (lane == 0) {
+                    __stcg(to + h, s.ref);
+                    __stcg(to + H + h, s.top);
+                    __stcg(to + 2 * H + h, s.sum);
+                }
+#pragma unroll
+                for (int e = 0; e < E; ++e) __stcg(to + 3 * H + h * S::LD + e * 32 + lane, acc[e]);
+            }
         }
     }
 
@@ -873,7 +875,7 @@ cache_attention_kernel(const AttnArgs a, WaitCtl wc, const __grid_constant__ CUt
 #pragma unroll 1
     for (int k = 0; k < 2; ++k) {
         if (!sh_last[k]) continue;
-        const Part p = sh_part[sh_list[k ? sh_run[runs - 1] : 0]];
+        const Part p = sh_part[k ? last_run : first_part];
         const int head0 = p.u % a.blocks * H, heads = min(H, a.group - head0);
         const int n = sh_c1[k] - sh_c0[k] + 1;
         // the first CTA's sums are in its second place, the others' in their first
