@@ -150,25 +150,26 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t v)
     return r;
 }
 
-// A pair of 16-bit halves 0x6400 | u (1024 + u in fp16) less 1024 + bias: the codes as fp16, exactly.
-template <int BITS>
-__device__ __forceinline__ uint32_t unbias(uint32_t v)
-{
-    const __half2 b = __float2half2_rn(BITS == 8 ? 1152.0f : 1032.0f);
-    const __half2 r = __hsub2(*reinterpret_cast<const __half2 *>(&v), b);
-    return *reinterpret_cast<const uint32_t *>(&r);
-}
-
-// 8 bits: codes of bytes 0, 1 (HI: 2, 3) of w.  4 bits: of nibbles J and J + 4.
+// Codes as fp16, exactly: set into the mantissa of 1024, less 1024 and their offset.
+// 8 bits: codes of bytes 0, 1 (HI: 2, 3) of w.
 template <int HI>
 __device__ __forceinline__ uint32_t codes8(uint32_t w)
 {
-    return unbias<8>(__byte_perm(w, 0x64646464u, HI ? 0x4342 : 0x4140));
+    const uint32_t v = __byte_perm(w, 0x64646464u, HI ? 0x4342 : 0x4140);
+    const __half2 r = __hsub2(*reinterpret_cast<const __half2 *>(&v), __float2half2_rn(1152.0f));
+    return *reinterpret_cast<const uint32_t *>(&r);
 }
+
+// 4 bits: of nibbles J and J + 4 (an odd J sets 16 times the code: 1024 + 16 u, one fma from u - 8).
 template <int J>
 __device__ __forceinline__ uint32_t codes4(uint32_t w)
 {
-    return unbias<4>(((w >> (4 * J)) & 0x000f000fu) | 0x64006400u);
+    const uint32_t x = J >= 2 ? w >> 8 : w;
+    const uint32_t v = (x & (J & 1 ? 0x00f000f0u : 0x000f000fu)) | 0x64006400u;
+    const __half2 h = *reinterpret_cast<const __half2 *>(&v);
+    const __half2 r = J & 1 ? __hfma2(h, __float2half2_rn(0.0625f), __float2half2_rn(-72.0f))
+                            : __hsub2(h, __float2half2_rn(1032.0f));
+    return *reinterpret_cast<const uint32_t *>(&r);
 }
 
 template <int BYTES>
