@@ -61,6 +61,7 @@ struct AttnArgs {
     const void *Q;
     long long q_stride;
     int q_aligned;               // 8-byte aligned rows
+    int page_shift;              // log2 of the page, -1 where it is no power of two
     int B, q_heads, group, blocks;   // blocks of query heads of a key head
     mpq_kv_cache L;
     const unsigned char *codes;
@@ -312,34 +313,58 @@ cache_attention_kernel(const AttnArgs a, WaitCtl wc, const __grid_constant__ CUt
         fence_barrier_init();
     }
     if (tid == 0) prefetch_tensormap(&tm);
-    if (tid < 2 * W) sh_part[tid].b = -1;
+    if (lane < 2) sh_part[2 * warp + lane].b = -1;
     const int units = a.L.heads * a.blocks;
     T *const O = static_cast<T *>(a.O);
     const size_t o_size = (size_t)a.B * a.q_heads * D;
     griddep_wait();
 
-    // ---- the stages before each thread's sequences ------------------------------------------------
-    const int per = (a.B + THREADS - 1) / THREADS;
-    const int b_lo = min(tid * per, a.B), b_hi = min(b_lo + per, a.B);
-    long long pre = 0;
-    for (int b = b_lo; b < b_hi; ++b) pre += (long long)weight(span_of(a, b).stages()) * units;
-    const long long mine = pre;
+    // ---- the work: the stages before each sequence ------------------------------------------------
+    // Up to 32 sequences: every warp looks at all of them, one a lane, and waits for no other.  More: each
+    // thread at `per` of them.
+    const bool few = a.B <= 32;
+    const int per = few ? 1 : (a.B + THREADS - 1) / THREADS;
+    Span lane_span = {0, 0};                     // (few) of sequence `lane`
+    unsigned lane_pre = 0, lane_all = 0;         // (few) weight of a unit, before it and up to its end
+    long long total;
+    int some;                                    // sequences (threads' of them) that have any
+    if (few) {
+        if (lane < a.B) lane_span = span_of(a, lane);
+        const unsigned mine = (unsigned)weight(lane_span.stages());      // (32 of at most 2^26 + 2)
+        lane_all = mine;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long v = __shfl_up_sync(0xffffffffu, pre, o);
-        if (lane >= o) pre += v;
-    }
-    if (lane == 31) sh_warp[warp] = pre;
-    const int some = __syncthreads_count(mine > 0);       // sequences (of one thread each) that have any
-    long long total = 0;
+        for (int o = 1; o < 32; o <<= 1) {
+            const unsigned v = __shfl_up_sync(0xffffffffu, lane_all, o);
+            if (lane >= o) lane_all += v;
+        }
+        lane_pre = lane_all - mine;
+        total = (long long)__shfl_sync(0xffffffffu, lane_all, 31) * units;
+        some = __popc(__ballot_sync(0xffffffffu, mine > 0));
+        if (warp == 0) sh_pre[lane] = (long long)lane_pre * units;       // (read after a barrier)
+    } else {
+        const int b_lo = min(tid * per, a.B), b_hi = min(b_lo + per, a.B);
+        long long pre = 0;
+        for (int b = b_lo; b < b_hi; ++b) pre += (long long)weight(span_of(a, b).stages()) * units;
+        const long long mine = pre;
 #pragma unroll
-    for (int w = 0; w < W; ++w) {
-        if (w < warp) pre += sh_warp[w];
-        total += sh_warp[w];
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long v = __shfl_up_sync(0xffffffffu, pre, o);
+            if (lane >= o) pre += v;
+        }
+        if (lane == 31) sh_warp[warp] = pre;
+        some = __syncthreads_count(mine > 0);
+        total = 0;
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            if (w < warp) pre += sh_warp[w];
+            total += sh_warp[w];
+        }
+        sh_pre[tid] = pre - mine;
+        __syncthreads();
     }
-    sh_pre[tid] = pre - mine;
     // sequences with nothing to attend to: a warp each
     auto empty_rows = [&]() {
+        if (per == 1 && some == a.B) return;
         for (long long b = blockIdx.x + (long long)warp * gridDim.x; b < a.B;
              b += (long long)W * gridDim.x) {
             if (span_of(a, (int)b).stages() > 0) continue;
@@ -363,7 +388,6 @@ cache_attention_kernel(const AttnArgs a, WaitCtl wc, const __grid_constant__ CUt
     const Cut cut = {total, workers};
     const long long r0 = me < workers ? cut.begin(me) : total;
     long long left = me < workers ? cut.begin(me + 1) - r0 : 0;
-    __syncthreads();
 
     unsigned *const counters = reinterpret_cast<unsigned *>(a.workspace);
     float *const cta_sums = reinterpret_cast<float *>(a.workspace + A_COUNTERS);      // [CTA][2]
@@ -374,7 +398,15 @@ cache_attention_kernel(const AttnArgs a, WaitCtl wc, const __grid_constant__ CUt
         // ---- the sequence and unit that the range begins in ---------------------------------------
         Row at;
         int st;                                   // next stage of the row
-        {
+        if (few) {
+            at.b = __ffs((int)__ballot_sync(0xffffffffu, (long long)lane_all * units > r0)) - 1;
+            at.sp.first = __shfl_sync(0xffffffffu, lane_span.first, at.b);
+            at.sp.end = __shfl_sync(0xffffffffu, lane_span.end, at.b);
+            at.n = at.sp.stages();
+            const long long skip = r0 - (long long)__shfl_sync(0xffffffffu, lane_pre, at.b) * units;
+            at.u = (int)quotient(skip, weight(at.n));
+            st = (int)(skip - (long long)at.u * weight(at.n));
+        } else {
             int lo = 0, hi = min(THREADS, a.B) - 1;   // the last thread whose sequences begin by r0
             while (lo < hi) {
                 const int mid = (lo + hi + 1) / 2;
@@ -390,10 +422,10 @@ cache_attention_kernel(const AttnArgs a, WaitCtl wc, const __grid_constant__ CUt
                 skip -= all;
             }
             at.u = (int)quotient(skip, weight(at.n));
-            const int in = (int)(skip - (long long)at.u * weight(at.n));
-            st = max(0, in - A_ROW_COST);         // the row's own cost comes first
-            left -= max(0, A_ROW_COST - in);
+            st = (int)(skip - (long long)at.u * weight(at.n));
         }
+        left -= max(0, A_ROW_COST - st);          // the row's own cost comes first
+        st = max(0, st - A_ROW_COST);
 
         // ---- the ring: stages on their way, ahead of the row that is being worked on ---------------
         Row ahead = at;
@@ -427,7 +459,7 @@ cache_attention_kernel(const AttnArgs a, WaitCtl wc, const __grid_constant__ CUt
                 f_i = 0;
                 f_n = min(32, ahead.n - f_st);
                 const unsigned tok = (unsigned)(ahead.sp.stage0() + f_st + lane) * A_STAGE;
-                const unsigned col = tok / (unsigned)a.L.page;
+                const unsigned col = a.page_shift >= 0 ? tok >> a.page_shift : tok / (unsigned)a.L.page;
                 const int page = lane < f_n ? a.table[(size_t)ahead.b * a.cols + col] : -1;
                 const bool there = page >= 0 && page < a.L.pages;
                 f_off = (int)(tok - col * (unsigned)a.L.page);
@@ -1009,6 +1041,9 @@ mpq_status launch_cache_attention(const void *Q, int type, long long q_stride, i
     a.Q = Q;
     a.q_stride = q_stride;
     a.q_aligned = ((uintptr_t)Q & 7) == 0 && q_stride % 4 == 0;
+    a.page_shift = -1;
+    for (int i = 4; i <= 10; ++i)
+        if (L->page == 1 << i) a.page_shift = i;
     a.B = B;
     a.q_heads = q_heads;
     a.group = q_heads / L->heads;
