@@ -119,7 +119,14 @@ mx_quantize_kernel(const T *X, long long ldx, mpq_mx_matrix L, unsigned char *pa
     }
 }
 
-template <typename T, bool VEC>
+// 2^(E-127): subnormal for E = 0, NaN for 255.
+__device__ __forceinline__ float scale_value(int E)
+{
+    return __uint_as_float(E == 255 ? 0x7fffffffu : E == 0 ? 0x00400000u : (uint32_t)E << 23);
+}
+
+// Aligned rows: 16 consecutive elements a thread.
+template <typename T>
 __global__ void __launch_bounds__(MX_THREADS)
 mx_dequantize_kernel(const unsigned char *packed, mpq_mx_matrix L, T *Y, long long ldy)
 {
@@ -129,22 +136,45 @@ mx_dequantize_kernel(const unsigned char *packed, mpq_mx_matrix L, T *Y, long lo
     const int j0 = at.group * 16;
     if (j0 >= L.d || at.row >= L.rows) return;
     const uint2 w = *reinterpret_cast<const uint2 *>(packed + at.row * (L.d_pad / 2) + j0 / 2);
-    const int E = packed[scale_byte(L, at)];
+    const float scale = scale_value(packed[scale_byte(L, at)]);
     float lo[8], hi[8], v[16];
     e2m1x8_values(w.x, lo);
     e2m1x8_values(w.y, hi);
-    // 2^(E-127): subnormal for E = 0
-    const float scale = __uint_as_float(E == 255 ? 0x7fffffffu : E == 0 ? 0x00400000u : (uint32_t)E << 23);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = __fmul_rn(lo[i], scale), v[8 + i] = __fmul_rn(hi[i], scale);
     T *y = Y + at.row * ldy + j0;
     if (!MPQ_IN(at.row * ldy + j0 + min(16, L.d - j0) - 1, (L.rows - 1) * ldy + L.d)) return;
-    if (VEC && j0 + 16 <= L.d) {
+    if (j0 + 16 <= L.d) {
         store16(y, v);
     } else {
 #pragma unroll
         for (int i = 0; i < 16; ++i)
             if (j0 + i < L.d) y[i] = from_f32<T>(v[i]);
+    }
+}
+
+// Other rows: a warp takes 512 elements of a row, 32 consecutive ones (a block) at a time, one a lane,
+// so that its stores are consecutive (16 of them a thread 32 bytes apart take 15 times as long).
+template <typename T>
+__global__ void __launch_bounds__(MX_THREADS)
+mx_dequantize_odd_kernel(const unsigned char *packed, mpq_mx_matrix L, T *Y, long long ldy)
+{
+    sm100::griddep_launch();
+    sm100::griddep_wait();
+    const int lane = threadIdx.x & 31;
+    const long long row = blockIdx.x;
+    const int j0 = ((int)blockIdx.y * (MX_THREADS / 32) + (int)(threadIdx.x >> 5)) * 512;
+    const unsigned char *const codes = packed + row * (L.d_pad / 2);
+    T *const y = Y + row * ldy;
+#pragma unroll 4
+    for (int j = j0 + lane; j < min(j0 + 512, L.d); j += 32) {
+        const unsigned code = (codes[j >> 1] >> (4 * (j & 1))) & 15u;
+        const float scale = scale_value(packed[scale_byte(L, {row, j >> 4})]);
+        // the level as an integer number of halves: m for m < 2, else (2 + (m & 1)) 2^(m/2 - 1)
+        const unsigned m = code & 7u;
+        const float v = 0.5f * (float)(m < 2 ? m : (2u + (m & 1u)) << ((m >> 1) - 1));
+        if (MPQ_IN(row * ldy + j, (L.rows - 1) * ldy + L.d))
+            y[j] = from_f32<T>(__fmul_rn(code & 8u ? -v : v, scale));
     }
 }
 
@@ -196,12 +226,17 @@ mpq_status launch_mx_dequantize(const void *packed, const mpq_mx_matrix *L, void
 {
     const bool vec = rows_aligned(Y, y_type, ldy);
     const unsigned char *in = static_cast<const unsigned char *>(packed);
-    const dim3 block = mx_block(L), grid = mx_grid(L, L->rows, block);
     return by_type(y_type, [&](auto t) {
         using T = decltype(t);
-        return launch_waiting(vec ? mx_dequantize_kernel<T, true> : mx_dequantize_kernel<T, false>,
-                              grid, block, 0, stream, "mx dequantize launch", in, *L,
-                              static_cast<T *>(Y), ldy);
+        if (!vec)
+            return launch_waiting(mx_dequantize_odd_kernel<T>,
+                                  dim3((unsigned)L->rows, (unsigned)((L->d + MX_THREADS * 16 - 1) /
+                                                                     (MX_THREADS * 16))),
+                                  dim3(MX_THREADS), 0, stream, "mx dequantize launch", in, *L,
+                                  static_cast<T *>(Y), ldy);
+        const dim3 block = mx_block(L), grid = mx_grid(L, L->rows, block);
+        return launch_waiting(mx_dequantize_kernel<T>, grid, block, 0, stream, "mx dequantize launch", in,
+                              *L, static_cast<T *>(Y), ldy);
     });
 }
 
