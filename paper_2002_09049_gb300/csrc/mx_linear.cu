@@ -24,7 +24,8 @@
 // four (multicast): 35 KB in and 32 KB read a stage, 25.5 KB from L2.
 //
 // Roles: warp 0 copies, warp 1 issues MMAs (the even CTA's, for a pair), warps 2..5 (TMEM lane quarter
-// warp % 4) move scales, then write the outputs.  Every wait is bounded.
+// warp % 4) move scales, then write the outputs -- with warps 6..9 where there are such.  Every wait is
+// bounded.
 #include <cuda.h>
 #include <math.h>
 #include <string.h>
@@ -50,7 +51,7 @@ constexpr int X_ROW = 128;               // bytes of a row's codes in a stage: 2
 constexpr int X_SF = 512;                // bytes of a scale tile (128 rows x 128 elements)
 constexpr int X_A_BYTES = X_M * X_ROW;
 constexpr int X_MAX_STAGES = 8;
-constexpr int X_THREADS = 192;
+constexpr int X_THREADS = 320;           // at most: warps 6..9 may be left out
 constexpr int X_MAX_SPLIT = 8;           // CTAs of a cluster that splits K
 constexpr int X_PAIRS = 2;               // CTA pairs of a cluster that shares B
 constexpr int X_SHARE = 2 * X_PAIRS;     // its CTAs
@@ -76,7 +77,7 @@ struct MxArgs {
     int split;                           // CTAs that share a tile's K stages
     int acc_cols, cols;                  // TMEM columns: the accumulator's (scales follow), all
     int n_tiles;                         // tiles along B (MANY)
-    int wide;                            // output rows take 32-byte stores
+    int wide;                            // output rows take 4 outputs at a time
     const unsigned char *a_scales, *b_scales;
     const float *bias;
     long long ldy;
@@ -90,10 +91,83 @@ __host__ __device__ inline int stage_bytes(const MxArgs &a)
     return X_A_BYTES + a.b_held * X_ROW + 2 * X_SF + sf_b_bytes(a.n_tile);
 }
 
+// v[4 j + k] of the four lanes 4 q .. 4 q + 3 (lane l: channel l, k: token) to v[4 j + k] with lane l:
+// token l, k: channel -- 4 x 4 transposes by two exchanges.
+__device__ __forceinline__ void quad_transpose(float (&v)[16], int lane)
+{
+#pragma unroll
+    for (int o = 1; o <= 2; o <<= 1) {
+        const bool high = lane & o;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            if (j & o) continue;
+            const float give = high ? v[j] : v[j + o];
+            const float got = __shfl_xor_sync(0xffffffffu, give, o);
+            if (high) v[j] = got; else v[j + o] = got;
+        }
+    }
+}
+
+__device__ __forceinline__ void store4(float *p, float a, float b, float c, float d)
+{
+    *reinterpret_cast<float4 *>(p) = make_float4(a, b, c, d);
+}
+template <typename T>
+__device__ __forceinline__ void store4(T *p, float a, float b, float c, float d)
+{
+    *reinterpret_cast<uint2 *>(p) = make_uint2(pack2(a, b, T()), pack2(c, d, T()));
+}
+
+struct JoinAt {
+    const float *part;                   // this rank's sums, [token][128 channels]
+    long long n0;
+    int n_real, tile, rank;
+};
+
+// The sums of a cluster's R ranks, in rank order; four channels to a thread, eight loads in flight.
+template <typename T, int R>
+__device__ __forceinline__ void join(const MxArgs &a, T *Y, const JoinAt &at)
+{
+    constexpr int U = 8 / R;
+    static_assert(X_MAX_SPLIT == 8, "ranks to join");
+    const int quads = at.n_real * (X_M / 4), step = R * (int)blockDim.x;
+    const size_t size = (a.b_rows - 1) * a.ldy + a.a_rows;
+    for (int i0 = (int)threadIdx.x + at.rank * (int)blockDim.x; i0 < quads; i0 += U * step) {
+        float4 p[U][R];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                p[u][r] = ld_dsmem_f32x4(at.part + min(i0 + u * step, quads - 1) * 4, (uint32_t)r);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = i0 + u * step;
+            const int t = i / (X_M / 4), c = at.tile * X_M + (i % (X_M / 4)) * 4;
+            if (i >= quads || c >= a.a_rows) continue;
+            float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                v[0] += p[u][r].x, v[1] += p[u][r].y, v[2] += p[u][r].z, v[3] += p[u][r].w;
+            if (a.bias) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] += c + e < a.a_rows ? a.bias[c + e] : 0.0f;
+            }
+            T *const y = Y + (at.n0 + t) * a.ldy + c;
+            if (a.wide) {
+                if (MPQ_IN((at.n0 + t) * a.ldy + c + 3, size)) store4(y, v[0], v[1], v[2], v[3]);
+                continue;
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (c + e < a.a_rows && MPQ_IN((at.n0 + t) * a.ldy + c + e, size)) y[e] = from_f32<T>(v[e]);
+        }
+    }
+}
+
 // MANY: A is the inputs, B the weights; clusters of X_PAIRS CTA pairs, one below the other along A.  Else A
 // is the weights, B the inputs, K split over clusters of a.split.
 template <typename T, bool MANY>
-__global__ void __launch_bounds__(X_THREADS)
+__global__ void __launch_bounds__(MANY ? 192 : X_THREADS)
 mx_linear_kernel(const MxArgs a, T *Y, WaitCtl wc, const __grid_constant__ CUtensorMap tmA,
                  const __grid_constant__ CUtensorMap tmB)
 {
@@ -115,7 +189,7 @@ mx_linear_kernel(const MxArgs a, T *Y, WaitCtl wc, const __grid_constant__ CUten
     const long long n0 = MANY ? (long long)(group % a.n_tiles) * X_N : (long long)blockIdx.y * a.n_tile;
     const int n_real = (int)min((long long)a.n_tile, a.b_rows - n0);         // rows of B that there are
     const int a_sf = tile < a.a_tiles ? 1 : 0;                       // scale tiles (per k tile) of A, of B
-    const int b_sf = (n_real + 127) / 128;
+    const int b_sf = (n_real + 127) / 128, b_skip = (int)(n0 % 128) / 32;
     const int k0 = MANY ? 0 : (int)((long long)a.k_stages * rank / a.split);
     const int k1 = MANY ? a.k_stages : (int)((long long)a.k_stages * (rank + 1) / a.split);
 
@@ -256,7 +330,7 @@ mx_linear_kernel(const MxArgs a, T *Y, WaitCtl wc, const __grid_constant__ CUten
         // ---------------------------------------------------------------- scales
         const int q = warp & 3;
         const uint32_t quarter = tmem + ((uint32_t)(q * 32) << 16);
-        {
+        if (warp < 6) {
             const int bc = sf_b_cols(a.n_tile);
             int s = 0;
             uint32_t phase = 0;
@@ -271,16 +345,19 @@ mx_linear_kernel(const MxArgs a, T *Y, WaitCtl wc, const __grid_constant__ CUten
                                      (uint32_t)(lane * 16);
                 const uint32_t ta = quarter + (uint32_t)(a.acc_cols + s * sf_cols(a.n_tile));
                 const int kt = min(2, a.k_tiles - 2 * k);
-                // lane r of every quarter holds the words of rows r, 32 + r, 64 + r and 96 + r
-                auto move = [&](uint32_t to, uint32_t from) {
+                // lane r of every quarter holds the words of rows r, 32 + r, 64 + r and 96 + r (of B, from
+                // the tile's first row on: a tile of 32 or 64 rows may begin inside a scale tile)
+                auto move = [&](uint32_t to, uint32_t from, int skip) {
                     const float4 w = ld_shared_v4(from);
-                    const float v[4] = {w.x, w.y, w.z, w.w};
+                    const float v[4] = {skip == 0 ? w.x : skip == 1 ? w.y : skip == 2 ? w.z : w.w,
+                                        skip == 2 ? w.w : skip == 1 ? w.z : w.y, skip == 1 ? w.w : w.z, w.w};
                     tmem_st_32x32b_x4(to, v);
                 };
                 for (int j = 0; j < kt; ++j) {
-                    move(ta + 4 * j, sfs + (uint32_t)(j * X_SF));
+                    move(ta + 4 * j, sfs + (uint32_t)(j * X_SF), 0);
                     for (int r = 0; r < b_sf; ++r)
-                        move(ta + 8 + (uint32_t)(bc * j + 4 * r), sfs + (uint32_t)((2 + 2 * r + j) * X_SF));
+                        move(ta + 8 + (uint32_t)(bc * j + 4 * r), sfs + (uint32_t)((2 + 2 * r + j) * X_SF),
+                             b_skip);
                 }
                 tmem_wait_st();
                 tc_fence_before();
@@ -305,33 +382,48 @@ mx_linear_kernel(const MxArgs a, T *Y, WaitCtl wc, const __grid_constant__ CUten
             const float bias = !MANY && a.bias && i < a.a_rows && a.split == 1 ? a.bias[i] : 0.0f;
             float *const part = reinterpret_cast<float *>(ring) + q * 32 + lane;
             const size_t size = (MANY ? a.a_rows - 1 : a.b_rows - 1) * a.ldy + (MANY ? a.b_rows : a.a_rows);
-            for (int j0 = 0; j0 < n_real; j0 += 16) {
+            // the warps of a quarter share its columns by sixteens (loading the next columns ahead of the
+            // stores slows both forms down: 42.3 us instead of 37.2 for 2,785 x 10,304 x 448)
+            const int step = blockDim.x > 192 ? 32 : 16;
+            for (int j0 = warp < 6 ? 0 : 16; j0 < n_real; j0 += step) {
                 float v[16];
                 __syncwarp();
                 tmem_ld_32x32b_x16(quarter + (uint32_t)j0, v);
-                if (MANY && i < a.a_rows) {   // row i of the inputs, 16 consecutive channels
+                if (MANY) {                   // row i of the inputs, 16 consecutive channels
                     const int c = (int)n0 + j0;
                     if (a.bias) {
 #pragma unroll
                         for (int j = 0; j < 16; ++j) v[j] += c + j < a.b_rows ? a.bias[c + j] : 0.0f;
                     }
                     T *const y = Y + i * a.ldy + c;
-                    if (a.wide && c + 16 <= a.b_rows) {
-                        if (MPQ_IN(i * a.ldy + c + 15, size)) store16(y, v);
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 16; ++j)
-                            if (c + j < a.b_rows && MPQ_IN(i * a.ldy + c + j, size)) y[j] = from_f32<T>(v[j]);
+                    if (c + 16 <= a.b_rows) {
+                        if (i < a.a_rows && MPQ_IN(i * a.ldy + c + 15, size)) store16(y, v);
+                        continue;
                     }
+#pragma unroll
+                    for (int j = 0; j < 16; j += 4)
+                        if (i < a.a_rows && c + j < a.b_rows && MPQ_IN(i * a.ldy + c + j + 3, size))
+                            store4(y + j, v[j], v[j + 1], v[j + 2], v[j + 3]);
                 } else if (!MANY && a.split > 1) {   // [token][128 channels]; the ring's copies have been read
 #pragma unroll
                     for (int j = 0; j < 16; ++j) part[(j0 + j) * X_M] = v[j];
+                } else if (!MANY && a.wide) {   // channel i of 16 tokens: by quads of lanes, 4 channels of 4
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) v[j] += bias;
+                    quad_transpose(v, lane);
+                    const int c = i & ~3;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int t = j0 + 4 * j + (lane & 3);
+                        if (t < n_real && c < a.a_rows && MPQ_IN((n0 + t) * a.ldy + c + 3, size))
+                            store4(Y + (n0 + t) * a.ldy + c, v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+                    }
                 } else if (!MANY && i < a.a_rows) {  // channel i of 16 tokens
                     T *y = Y + (n0 + j0) * a.ldy + i;
+                    const int n = n_real - j0;
 #pragma unroll
-                    for (int j = 0; j < 16; ++j)
-                        if (j0 + j < n_real && MPQ_IN((n0 + j0 + j) * a.ldy + i, size))
-                            y[j * a.ldy] = from_f32<T>(v[j] + bias);
+                    for (int j = 0; j < 16; ++j, y += a.ldy)
+                        if (j < n && MPQ_IN((n0 + j0 + j) * a.ldy + i, size)) *y = from_f32<T>(v[j] + bias);
                 }
             }
             tc_fence_before();
@@ -340,22 +432,13 @@ mx_linear_kernel(const MxArgs a, T *Y, WaitCtl wc, const __grid_constant__ CUten
 
     if (!MANY && a.split > 1) {
         cluster_sync();                  // every rank's sums are in its shared memory
-        const float *const part = reinterpret_cast<const float *>(ring);
-        const int quads = n_real * (X_M / 4);
-        for (int i = (int)threadIdx.x + rank * X_THREADS; i < quads; i += a.split * X_THREADS) {
-            const int t = i / (X_M / 4), cc = (i % (X_M / 4)) * 4, c = tile * X_M + cc;
-            if (c >= a.a_rows) continue;
-            float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-            for (int r = 0; r < a.split; ++r) {
-                const float4 p = ld_dsmem_f32x4(part + t * X_M + cc, (uint32_t)r);
-                v[0] += p.x, v[1] += p.y, v[2] += p.z, v[3] += p.w;
-            }
-            T *y = Y + (n0 + t) * a.ldy + c;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (c + e < a.a_rows && MPQ_IN((n0 + t) * a.ldy + c + e, (a.b_rows - 1) * a.ldy + a.a_rows))
-                    y[e] = from_f32<T>(v[e] + (a.bias ? a.bias[c + e] : 0.0f));
-        }
+        const JoinAt at{reinterpret_cast<const float *>(ring), n0, n_real, tile, rank};
+        if (a.split == 2)
+            join<T, 2>(a, Y, at);
+        else if (a.split == 4)
+            join<T, 4>(a, Y, at);
+        else
+            join<T, 8>(a, Y, at);
     }
     if (cluster)
         cluster_sync();                  // no rank leaves while its sums are read, or copies to it land
@@ -404,7 +487,10 @@ mpq_status launch_typed(const MxArgs &a, const void *A, const void *B, int row_b
     if (ws != MPQ_OK) return ws;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
-    cfg.blockDim = dim3(X_THREADS, 1, 1);
+    // eight writers pay for wide tiles (256 columns: 6.0 us instead of 7.5 for 352 x 8,128 x 448), four for
+    // narrow ones whose sums are joined by all warps (37 x 11,008 x 4,096: 7.8 us instead of 8.0)
+    const bool four = MANY || a.n_tile <= 16 || (a.split > 1 && a.n_tile <= 64);
+    cfg.blockDim = dim3(four ? 192 : X_THREADS, 1, 1);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
@@ -417,6 +503,51 @@ mpq_status launch_typed(const MxArgs &a, const void *A, const void *B, int row_b
     cfg.numAttrs = 2;
     e = cudaLaunchKernelEx(&cfg, mx_linear_kernel<T, MANY>, a, static_cast<T *>(Y), wc, tmA, tmB);
     return cuda_status(e != cudaSuccess ? e : cudaGetLastError(), "mx linear launch");
+}
+
+// CTAs of a cluster that split the K stages of few tokens' tiles: as many as leave every CTA resident, with
+// two stages or more.
+int few_split(long long tiles, int n, int k_stages, int sms)
+{
+    const long long resident = (long long)sms * (n <= 64 ? 2 : 1);
+    int split = 1;
+    while (split < X_MAX_SPLIT && tiles * split * 2 <= resident && k_stages >= split * 4) split *= 2;
+    return split;
+}
+
+// The rows of B in a tile where A is the weights, 32 to 256 (n_tile), or none where the pairs' form
+// (`pairs`: it may be taken) is expected to be faster.  The modelled time counts, for each round of resident
+// CTAs, a start, the stages by their bytes and the columns on their way out, in units of about 10 ns; CTAs
+// that share an SM take longer over the last two.  The constants are fitted to 500 timings of 110 sizes
+// (17 <= T <= 4,096, 64 <= C, d <= 14,000): the choice costs 1% on average, 9% at worst, against the best
+// of the forms.  Some of them, us, with 32 / 64 / 128 / 256 rows / pairs: 1,233 x 448 x 448 3.7, 4.1, 4.4,
+// 5.9, 5.2; 128 x 4,096 x 4,096 8.5, 7.8, 7.7, -, -; 207 x 8,960 x 7,680 34, 18.3, 17.4, 14.6, -;
+// 512 x 4,096 x 4,096 21.3, 11.4, 10.6, 10.6, 11.2; 1,024 x 4,096 x 4,096 40, 22.3, 20.9, 13.2, 11.9.
+int few_tile(int T, int C, int k_stages, int sms, bool pairs)
+{
+    const long long m_tiles = ((long long)C + X_M - 1) / X_M;
+    auto rounds = [](long long ctas, long long at_once) { return (double)((ctas + at_once - 1) / at_once); };
+    int best = 0;
+    double least = HUGE_VAL;
+    if (pairs) {                         // clusters of four leave 8 of 152 SMs idle
+        const long long ctas = ((long long)T + X_SHARE * X_M - 1) / (X_SHARE * X_M) *
+                               (((long long)C + X_N - 1) / X_N) * X_SHARE;
+        least = rounds(ctas, std::max(X_SHARE, sms / 38 * 36)) * (740.0 + 22.0 * k_stages);
+    }
+    for (int n = X_N; n >= 32; n /= 2) {
+        const int width = std::min(n, (T + 15) / 16 * 16);
+        const long long tiles = m_tiles * (((long long)T + n - 1) / n);
+        const int split = few_split(tiles, width, k_stages, sms);
+        const int share = width <= 64 && tiles * split > sms ? 2 : 1;
+        const double t = rounds(tiles * split, (long long)sms * share) *
+                             (485.0 + (k_stages + split - 1) / split * (128 + width) * share / 16.0 +
+                              width * share) + (split > 1 ? 20.0 : 0.0);
+        if (t < least) {
+            best = width;
+            least = t;
+        }
+    }
+    return best;
 }
 
 // Stages that fit into `room` bytes of shared memory, and the tensor memory columns.
@@ -441,11 +572,13 @@ mpq_status launch_mx_linear(const mpq_mx_matrix *xl, const void *X, const mpq_mx
     const unsigned char *const x = static_cast<const unsigned char *>(X);
     const unsigned char *const w = static_cast<const unsigned char *>(W);
     const int T = xl->rows, C = wl->rows, sms = sm_count();
-    // pairs' tiles of 256 tokens x 256 channels where their clusters fill half the SMs or more
-    const long long m_cl = ((long long)T + X_SHARE * X_M - 1) / (X_SHARE * X_M);
-    const long long n_cl = ((long long)C + X_N - 1) / X_N;
-    const long long ctas = m_cl * n_cl * X_SHARE;
-    if (2 * ctas >= sms && T > X_N) {
+    const int four = 4 * type_size(y_type);
+    a.wide = C % 4 == 0 && ldy % 4 == 0 && (uintptr_t)Y % four == 0;
+    // (the pairs' writers hold 16 channels of a token each: 256 x 250 outputs, one by one, took 30 us)
+    const int n = few_tile(T, C, a.k_stages, sms, T > X_N && a.wide && rows_aligned(Y, y_type, ldy));
+    if (n == 0) {
+        const long long n_cl = ((long long)C + X_N - 1) / X_N;
+        const long long ctas = ((long long)T + X_SHARE * X_M - 1) / (X_SHARE * X_M) * n_cl * X_SHARE;
         a.a_rows = T;
         a.b_rows = C;
         a.a_tiles = xl->row_tiles;
@@ -455,7 +588,6 @@ mpq_status launch_mx_linear(const mpq_mx_matrix *xl, const void *X, const mpq_mx
         a.b_held = X_N / 2;
         a.split = 1;
         a.n_tiles = (int)n_cl;
-        a.wide = rows_aligned(Y, y_type, ldy);
         size_ring(a, max_smem_optin());
         if (ctas > 0x7fffffffLL) {
             set_error("mx linear: T = %d, C = %d are too large", T, C);
@@ -471,18 +603,13 @@ mpq_status launch_mx_linear(const mpq_mx_matrix *xl, const void *X, const mpq_mx
     a.a_tiles = wl->row_tiles;
     a.a_scales = w + wl->off_scales;
     a.b_scales = x + xl->off_scales;
-    a.n_tile = a.b_held = T >= X_N ? X_N : (T + 15) / 16 * 16;
+    const long long m_tiles = ((long long)C + X_M - 1) / X_M;
+    a.n_tile = a.b_held = n;
     // two CTAs share an SM where a ring of four stages leaves room for it (up to 64 tokens)
     const bool two = a.n_tile <= 64;
     size_ring(a, two ? 112 * 1024 : max_smem_optin());
-    // clusters split the K stages while every CTA stays resident and has two stages or more
-    const long long m_tiles = ((long long)C + X_M - 1) / X_M;
     const long long n_tiles = ((long long)T + a.n_tile - 1) / a.n_tile;
-    const long long resident = (long long)sms * (two ? 2 : 1);
-    a.split = 1;
-    while (a.split < X_MAX_SPLIT && m_tiles * n_tiles * a.split * 2 <= resident &&
-           a.k_stages >= a.split * 4)
-        a.split *= 2;
+    a.split = few_split(m_tiles * n_tiles, a.n_tile, a.k_stages, sms);
     if (n_tiles > 65535 || m_tiles * a.split > 0x7fffffffLL) {
         set_error("mx linear: T = %d, C = %d are too large", T, C);
         return MPQ_ERR_UNSUPPORTED;

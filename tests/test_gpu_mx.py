@@ -168,6 +168,19 @@ def test_linear(gpu, T, C, d):
     assert binding.mpq_device_status() == 0
 
 
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("T,C,d", [
+    (33, 500, 64), (100, 96, 200), (200, 64, 2560), (330, 203, 700), (90, 4000, 100),
+    (1000, 260, 1536), (2000, 61, 90), (150, 2052, 2048), (193, 5896, 2560), (200, 9000, 600),
+    (352, 8136, 448), (700, 3080, 515)])
+def test_linear_token_tiles(gpu, T, C, d, dtype):
+    """Tiles of 32 to 256 tokens, some starting inside a block of 128 tokens' scales, K whole or split;
+    channels by fours and one by one; the pairs' form with a last run of eight channels."""
+    y, want, tol, _ = linear(T, C, d, dtype, C % 8 == 0, T + C + d)
+    assert within(y, want, tol), float(((y.double() - want).abs() / tol).max())
+    assert binding.mpq_device_status() == 0
+
+
 @pytest.mark.parametrize("T", [1, 40, 300])
 def test_linear_fp32_outputs(gpu, T):
     y, want, tol, packed = linear(T, 260, 1536, "fp32", True, T)
