@@ -146,6 +146,20 @@ __device__ __forceinline__ void load16(const T *p, float (&v)[16])
     }
 }
 
+// Eight words to p on (16-byte aligned).
+__device__ __forceinline__ void store_words(uint32_t *p, const uint32_t (&w)[8])
+{
+    if (((uintptr_t)p & 31) == 0) {
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                     :: "l"(__cvta_generic_to_global(p)), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
+                        "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                     : "memory");
+    } else {
+        reinterpret_cast<uint4 *>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        reinterpret_cast<uint4 *>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    }
+}
+
 template <typename T>
 __device__ __forceinline__ void store16(T *p, const float (&v)[16])
 {
@@ -159,16 +173,19 @@ __device__ __forceinline__ void store16(T *p, const float (&v)[16])
         uint32_t w[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) w[i] = pack2(v[2 * i], v[2 * i + 1], T());
-        if (((uintptr_t)p & 31) == 0) {
-            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
-                         :: "l"(__cvta_generic_to_global(p)), "r"(w[0]), "r"(w[1]), "r"(w[2]),
-                            "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
-                         : "memory");
-        } else {
-            reinterpret_cast<uint4 *>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
-            reinterpret_cast<uint4 *>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
-        }
+        store_words(reinterpret_cast<uint32_t *>(p), w);
     }
+}
+
+// 32 consecutive elements, as load16's.
+template <typename T>
+__device__ __forceinline__ void load32(const T *p, float (&v)[32])
+{
+    float a[16], b[16];
+    load16(p, a);
+    load16(p + 16, b);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = a[i], v[16 + i] = b[i];
 }
 
 // Host: bytes of an element type, 0 for a number that names none.

@@ -56,6 +56,22 @@ def test_quantize_bits(gpu, rows, d, dtype):
 
 
 @pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("rows,d", [(1, 716), (300, 230), (5, 1025), (129, 127), (2, 9525), (700, 31)])
+def test_odd_rows_there_and_back(gpu, rows, d, dtype):
+    """Rows off the 16-byte boundary: the bits of the same rows laid out on it, both ways."""
+    x = inputs(rows, d, rows + d, dtype).to(DEV)
+    wide = torch.zeros((rows, (d + 15) // 16 * 16 + 16), dtype=TYPES[dtype], device=DEV)
+    wide[:, :d] = x
+    lay = binding.mpq_mx_layout(rows, d)
+    odd, even = binding.mpq_mx_quantize(x, lay), binding.mpq_mx_quantize(wide[:, :d], lay)
+    assert torch.equal(odd, even)
+    y = binding.mpq_mx_dequantize(odd, lay, dtype=TYPES[dtype])
+    wide.fill_(7)
+    binding.mpq_mx_dequantize(odd, lay, Y=wide[:, :d])
+    assert torch.equal(torch.nan_to_num(wide[:, :d]), torch.nan_to_num(y)) and bool((wide[:, d:] == 7).all())
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
 @pytest.mark.parametrize("pad,shift", [(8, 0), (3, 0), (8, 1), (0, 3)])
 def test_quantize_strided_rows(gpu, dtype, pad, shift):
     """Rows further apart than d, bases off the 16-byte boundary."""
