@@ -2,17 +2,20 @@
 // slots back (mpq_cache_read).
 //
 // A row is what one token keeps for one head (its key, or its value): s = max|x| (1 / Qmax), one fp32
-// product, codes clamp(rint(x / s)) as Eq. 8's.  A thread takes 16 elements of a token's key and value
-// row of one head (both are on their way before either is used), so dim / 16 threads (4, 8 or 16 of
-// a warp) share the rows' maxima by shuffles, and their codes leave in one store of 16 or 8 bytes a
-// thread and row.
+// product, codes clamp(rint(x / s)) as Eq. 8's.  A thread takes 16 elements of a row, so dim / 16 threads
+// (4, 8 or 16 of a warp) share its maximum by shuffles, and their codes leave in one store of 16 or 8 bytes
+// a thread.  Writing, keys and values are rows of threads of their own (1,999 tokens, 4 heads x 64, fp32 to 4 bits: 2.7 us,
+// 3.5 with a key and a value row a thread; 32 elements a thread leave too few warps: 22.9 us instead of
+// 15.7 for 8,192 tokens); reading, a thread takes both.
 //
 // The quotient x / s has to be the correctly rounded one: 16-bit inputs meet near-ties all the time
 // (elements whose ratio to the row's largest is a simple fraction).  One correctly rounded reciprocal r
-// a row, and Markstein's theorem (IBM J. Res. Dev. 34(1), 1990): a y within a unit in the last place of
-// x / s gives RN(x / s) as RN(y + r (x - s y)), the remainder exact by a fused multiply-add.  RN(x r) is
-// within 1.5 units, one such step brings it within one, the next is the quotient.  Rows whose scale is
-// so small or large that r or a remainder could leave the normal range are divided.
+// a row: x r is within 2^-24 of x / s, relatively, so its distance from rint(x r), which one fused
+// multiply-add gives, shows the code to be that of x / s unless it is within 2^-15 of a half.  Threads with
+// such an element take all their quotients by Markstein's theorem (IBM J. Res. Dev. 34(1), 1990): a y within
+// a unit in the last place of x / s gives RN(x / s) as RN(y + r (x - s y)), the remainder exact by a fused
+// multiply-add.  RN(x r) is within 1.5 units, one such step brings it within one, the next is the quotient.
+// Rows whose scale is so small or large that r or a remainder could leave the normal range are divided.
 //
 // Memory-bound: an element's own bytes on one side, bits / 8 + 4 / dim bytes on the other; slots scatter
 // rows of 32 to 256 bytes, whole sectors.
@@ -30,7 +33,8 @@ namespace {
 
 constexpr int KV_THREADS = 256;
 
-// A thread's place: token, head (blockIdx.y), and its first element of both rows.
+// A thread's place: token, head (blockIdx.y; writing, the heads' keys, then their values), and its first
+// element of the row.
 struct RowAt {
     int t, h, j0;
 };
@@ -43,8 +47,8 @@ __device__ __forceinline__ bool row_at(int T, const mpq_kv_cache &L, RowAt &at)
     return at.t < T;
 }
 
-// Index of a slot's key row among the cache's rows (its value row is heads * page further), or -1 for
-// a slot outside the cache.
+// Index of a slot's key row among the cache's rows (its value row is heads * page further: head h + heads),
+// or -1 for a slot outside the cache.
 __device__ __forceinline__ long long cache_row(long long slot, const mpq_kv_cache &L, int h)
 {
     if (slot < 0 || slot >= (long long)L.pages * L.page) return -1;
@@ -73,12 +77,23 @@ __device__ __forceinline__ float row_codes(const float (&v)[16], uint32_t top, i
     if (s >= KV_LEAST && s <= KV_MOST) {
         const float r = __frcp_rn(s);
         const float magic = 12582912.0f + (float)zero;  // 3 2^22 + offset: the sum's low bits are the code
+        float off = 0.0f;                               // the most that x r lies from its rounding
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            float y = __fmul_rn(v[i], r);
-            y = __fmaf_rn(__fmaf_rn(-y, s, v[i]), r, y);
-            y = __fmaf_rn(__fmaf_rn(-y, s, v[i]), r, y);
-            u[i] = __float_as_uint(__fadd_rn(y, magic));
+        for (int i = 0; i < 16; i += 2) {
+            const float t0 = __fmaf_rn(v[i], r, magic), t1 = __fmaf_rn(v[i + 1], r, magic);
+            u[i] = __float_as_uint(t0);
+            u[i + 1] = __float_as_uint(t1);
+            off = max_abs(off, __fmaf_rn(v[i], r, __fsub_rn(magic, t0)),
+                          __fmaf_rn(v[i + 1], r, __fsub_rn(magic, t1)));
+        }
+        if (off > 0.5f - 0x1p-15f) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                float y = __fmul_rn(v[i], r);
+                y = __fmaf_rn(__fmaf_rn(-y, s, v[i]), r, y);
+                y = __fmaf_rn(__fmaf_rn(-y, s, v[i]), r, y);
+                u[i] = __float_as_uint(__fadd_rn(y, magic));
+            }
         }
     } else {
 #pragma unroll 1
@@ -120,7 +135,7 @@ __device__ __forceinline__ void store_row(const uint32_t (&u)[16], float s, long
 }
 
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(KV_THREADS)
+__global__ void __launch_bounds__(KV_THREADS, 5)
 cache_write_kernel(const T *K, const T *V, long long ld_token, long long ld_head, int n,
                    const int64_t *slots, mpq_kv_cache L, float inv_qmax, unsigned char *codes,
                    float *scales)
@@ -129,30 +144,24 @@ cache_write_kernel(const T *K, const T *V, long long ld_token, long long ld_head
     sm100::griddep_wait();
     RowAt at;
     if (!row_at(n, L, at)) return;   // whole rows (dim / 16 threads) leave together
+    const bool value = at.h >= L.heads;
+    const T *const x = (value ? V : K) + ld_token * at.t + ld_head * (value ? at.h - L.heads : at.h) + at.j0;
     const long long slot = slots[at.t];
-    const long long from = ld_token * at.t + ld_head * at.h + at.j0;
-    float k[16], v[16];
+    float v[16];
     if (VEC) {
-        load16(K + from, k);
-        load16(V + from, v);
+        load16(x, v);
     } else {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            k[i] = to_f32(K[from + i]);
-            v[i] = to_f32(V[from + i]);
-        }
+        for (int i = 0; i < 16; ++i) v[i] = to_f32(x[i]);
     }
     const long long row = cache_row(slot, L, at.h);
     if (row < 0) return;
     const unsigned per = (unsigned)L.dim / 16;
     const unsigned lanes = ((1u << per) - 1u) << (threadIdx.x & 31 & ~(per - 1));
     const int qmax = (1 << (L.bits - 1)) - 1;
-    const uint32_t k_top = row_top(k, per, lanes), v_top = row_top(v, per, lanes);
     uint32_t u[16];
-    float s = row_codes(k, k_top, qmax, inv_qmax, u);
+    const float s = row_codes(v, row_top(v, per, lanes), qmax, inv_qmax, u);
     store_row(u, s, row, at.j0, L, codes, scales);
-    s = row_codes(v, v_top, qmax, inv_qmax, u);
-    store_row(u, s, row + (long long)L.heads * L.page, at.j0, L, codes, scales);
 }
 
 // The values of 16 codes (four words, or two) with a scale.
@@ -205,10 +214,10 @@ cache_read_kernel(const int64_t *slots, int n, mpq_kv_cache L, const unsigned ch
 }
 
 // Blocks of KV_THREADS threads for T tokens' rows, by head.
-dim3 kv_grid(int T, const mpq_kv_cache *L)
+dim3 kv_grid(int T, const mpq_kv_cache *L, int heads)
 {
     const long long per_block = KV_THREADS / (L->dim / 16);
-    return dim3((unsigned)((T + per_block - 1) / per_block), (unsigned)L->heads, 1);
+    return dim3((unsigned)((T + per_block - 1) / per_block), (unsigned)heads, 1);
 }
 
 }  // namespace
@@ -237,7 +246,7 @@ mpq_status launch_cache_write(const void *K, const void *V, int type, long long 
     return by_type(type, [&](auto t) {
         using E = decltype(t);
         return launch_waiting(vec ? cache_write_kernel<E, true> : cache_write_kernel<E, false>,
-                              kv_grid(T, L), dim3(KV_THREADS), 0, stream,
+                              kv_grid(T, L, 2 * L->heads), dim3(KV_THREADS), 0, stream,
                               "cache write launch", static_cast<const E *>(K),
                               static_cast<const E *>(V), ld_token, ld_head, T, slots, *L,
                               1.0f / (float)((1 << (L->bits - 1)) - 1),
@@ -250,7 +259,7 @@ mpq_status launch_cache_read(const int64_t *slots, int T, const mpq_kv_cache *L,
 {
     return by_type(type, [&](auto t) {
         using E = decltype(t);
-        return launch_waiting(cache_read_kernel<E>, kv_grid(T, L), dim3(KV_THREADS), 0,
+        return launch_waiting(cache_read_kernel<E>, kv_grid(T, L, L->heads), dim3(KV_THREADS), 0,
                               stream, "cache read launch", slots, T, *L,
                               static_cast<const unsigned char *>(codes), scales,
                               static_cast<E *>(K), static_cast<E *>(V));

@@ -122,6 +122,34 @@ def test_slots_outside_and_special_rows(gpu, bits):
     assert np.array_equal(K[3, 0].cpu().numpy(), q_ref[1].astype(np.float32) * s_ref[1])
 
 
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("dtype", ["fp32", "fp16"])
+def test_write_quotients_near_halves(gpu, bits, dtype):
+    """Elements a few units around every half of the scale, and simple fractions of the largest: the
+    codes are those of the correctly rounded fp32 quotients."""
+    dim, T, qmax = 256, 600, 2 ** (bits - 1) - 1
+    rng = np.random.default_rng(bits)
+    top = np.exp(rng.uniform(-9, 9, (T, 1))).astype(np.float32)
+    if dtype == "fp16":
+        top = top.astype(np.float16).astype(np.float32)
+    s = top * (np.float32(1) / np.float32(qmax))
+    half = rng.integers(0, qmax, (T, dim)) + 0.5
+    x = (s * half).astype(np.float32)
+    x = (x.view(np.int32) + rng.integers(-3, 4, (T, dim))).astype(np.int32).view(np.float32)
+    x[:, ::5] = (top * rng.integers(0, 2 * qmax, (T, dim)) / (2 * qmax)).astype(np.float32)[:, ::5]
+    x = np.minimum(x, top) * rng.choice([-1, 1], (T, dim)).astype(np.float32)
+    x[:, 0] = top[:, 0]
+    x = torch.from_numpy(x).to(TYPES[dtype])
+    lay = binding.mpq_cache_layout(-(-T // 16), 16, 1, dim, bits)
+    codes, scales = binding.mpq_cache_empty(lay, DEV)
+    kv = x.to(DEV).view(T, 1, dim)
+    binding.mpq_cache_write(kv, -kv, torch.arange(T, device=DEV), lay, codes, scales)
+    q, sc = stored(codes, scales, np.arange(T), lay)
+    q_ref, s_ref = ref.cache_rows(x.float().numpy(), bits)
+    assert np.array_equal(sc[:, 0, 0], s_ref) and np.array_equal(sc[:, 1, 0], s_ref)
+    assert np.array_equal(q[:, 0, 0], q_ref) and np.array_equal(q[:, 1, 0], -q_ref)
+
+
 class Scene:
     """A cache filled at random (NaN scales wherever no sequence looks), its tables, and the queries."""
 
