@@ -4,21 +4,23 @@
 // A row is what one token keeps for one head (its key, or its value): s = max|x| (1 / Qmax), one fp32
 // product, codes clamp(rint(x / s)) as Eq. 8's.  A thread takes 16 elements of a row, so dim / 16 threads
 // (4, 8 or 16 of a warp) share its maximum by shuffles, and their codes leave in one store of 16 or 8 bytes
-// a thread.  Writing, keys and values are rows of threads of their own (1,999 tokens, 4 heads x 64, fp32 to 4 bits: 2.7 us,
+// a thread.  Writing, keys and values have threads of their own (1,999 tokens of 4 x 64 fp32 to 4 bits: 2.7 us,
 // 3.5 with a key and a value row a thread; 32 elements a thread leave too few warps: 22.9 us instead of
-// 15.7 for 8,192 tokens); reading, a thread takes both.
+// 15.7 for 8,192 tokens of 8 x 128 bf16, before the quotients below took one step); reading, a thread takes
+// both.
 //
 // The quotient x / s has to be the correctly rounded one: 16-bit inputs meet near-ties all the time
-// (elements whose ratio to the row's largest is a simple fraction).  One correctly rounded reciprocal r
-// a row: x r is within 2^-24 of x / s, relatively, so its distance from rint(x r), which one fused
-// multiply-add gives, shows the code to be that of x / s unless it is within 2^-15 of a half.  Threads with
-// such an element take all their quotients by Markstein's theorem (IBM J. Res. Dev. 34(1), 1990): a y within
-// a unit in the last place of x / s gives RN(x / s) as RN(y + r (x - s y)), the remainder exact by a fused
-// multiply-add.  RN(x r) is within 1.5 units, one such step brings it within one, the next is the quotient.
+// (elements whose ratio to the row's largest is a simple fraction: in 70% of a warp's 512 bf16 elements
+// there is one, so that a screen with an exact way out gains nothing).  One correctly rounded reciprocal r
+// a row, and Markstein's theorem (IBM J. Res. Dev. 34(1), 1990): a y within a unit in the last place of
+// x / s gives RN(x / s) as RN(y + r (x - s y)), the remainder exact by a fused multiply-add.  RN(x r) is
+// within 1.5 units, one such step brings it within one, the next is the quotient.  For elements and maxima
+// of 11 bits or fewer the first step gives it already (all of them tried: tests/test_cache_quotients.py).
 // Rows whose scale is so small or large that r or a remainder could leave the normal range are divided.
 //
 // Memory-bound: an element's own bytes on one side, bits / 8 + 4 / dim bytes on the other; slots scatter
-// rows of 32 to 256 bytes, whole sectors.
+// rows of 32 to 256 bytes, whole sectors.  8,192 tokens of 8 x 128 bf16 to 8 bits: written in 12.6 us (51 MB,
+// 4.0 TB/s; issue slots 70% busy), read back in 9.9 us (5.1 TB/s).
 #include <math.h>
 #include <string.h>
 
@@ -49,11 +51,10 @@ __device__ __forceinline__ bool row_at(int T, const mpq_kv_cache &L, RowAt &at)
 
 // Index of a slot's key row among the cache's rows (its value row is heads * page further: head h + heads),
 // or -1 for a slot outside the cache.
-__device__ __forceinline__ long long cache_row(long long slot, const mpq_kv_cache &L, int h)
+__device__ __forceinline__ long long cache_row(long long slot, const mpq_kv_cache &L, int page_shift, int h)
 {
     if (slot < 0 || slot >= (long long)L.pages * L.page) return -1;
-    const long long page = (slot >> 32) == 0 ? (long long)((unsigned)slot / (unsigned)L.page)
-                                             : slot / L.page;
+    const long long page = page_shift >= 0 ? slot >> page_shift : slot / L.page;
     return (page * 2 * L.heads + h) * L.page + (slot - page * L.page);
 }
 
@@ -68,7 +69,9 @@ __device__ __forceinline__ uint32_t row_top(const float (&v)[16], unsigned per, 
 // Scales whose reciprocal, and whose quotients' remainders where the code is not 0, are normal.
 constexpr float KV_LEAST = 0x1p-100f, KV_MOST = 0x1p100f;
 
-// The codes of 16 elements, offset by Qmax + 1, in the low bits of each word, and the row's scale.
+// The codes of 16 elements, offset by Qmax + 1, in the low bits of each word, and the row's scale; STEPS
+// corrections of a quotient.
+template <int STEPS>
 __device__ __forceinline__ float row_codes(const float (&v)[16], uint32_t top, int qmax,
                                            float inv_qmax, uint32_t (&u)[16])
 {
@@ -77,32 +80,23 @@ __device__ __forceinline__ float row_codes(const float (&v)[16], uint32_t top, i
     if (s >= KV_LEAST && s <= KV_MOST) {
         const float r = __frcp_rn(s);
         const float magic = 12582912.0f + (float)zero;  // 3 2^22 + offset: the sum's low bits are the code
-        float off = 0.0f;                               // the most that x r lies from its rounding
 #pragma unroll
-        for (int i = 0; i < 16; i += 2) {
-            const float t0 = __fmaf_rn(v[i], r, magic), t1 = __fmaf_rn(v[i + 1], r, magic);
-            u[i] = __float_as_uint(t0);
-            u[i + 1] = __float_as_uint(t1);
-            off = max_abs(off, __fmaf_rn(v[i], r, __fsub_rn(magic, t0)),
-                          __fmaf_rn(v[i + 1], r, __fsub_rn(magic, t1)));
-        }
-        if (off > 0.5f - 0x1p-15f) {
+        for (int i = 0; i < 16; ++i) {
+            float y = __fmul_rn(v[i], r);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                float y = __fmul_rn(v[i], r);
-                y = __fmaf_rn(__fmaf_rn(-y, s, v[i]), r, y);
-                y = __fmaf_rn(__fmaf_rn(-y, s, v[i]), r, y);
-                u[i] = __float_as_uint(__fadd_rn(y, magic));
-            }
+            for (int k = 0; k < STEPS; ++k) y = __fmaf_rn(__fmaf_rn(-y, s, v[i]), r, y);
+            u[i] = __float_as_uint(__fadd_rn(y, magic));
         }
     } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) u[i] = __float_as_uint(v[i]);
 #pragma unroll 1
         for (int i = 0; i < 16; ++i) {
-            float x = 0.0f;
+            uint32_t x = 0;
 #pragma unroll
-            for (int k = 0; k < 16; ++k) x = k == i ? v[k] : x;
+            for (int k = 0; k < 16; ++k) x = k == i ? u[k] : x;
             int q = 0;
-            if (s > 0.0f) q = min(max(__float2int_rn(__fdiv_rn(x, s)), -qmax), qmax);
+            if (s > 0.0f) q = min(max(__float2int_rn(__fdiv_rn(__uint_as_float(x), s)), -qmax), qmax);
 #pragma unroll
             for (int k = 0; k < 16; ++k)
                 if (k == i) u[k] = (uint32_t)(q + zero);
@@ -135,9 +129,9 @@ __device__ __forceinline__ void store_row(const uint32_t (&u)[16], float s, long
 }
 
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(KV_THREADS, 5)
+__global__ void __launch_bounds__(KV_THREADS)
 cache_write_kernel(const T *K, const T *V, long long ld_token, long long ld_head, int n,
-                   const int64_t *slots, mpq_kv_cache L, float inv_qmax, unsigned char *codes,
+                   const int64_t *slots, mpq_kv_cache L, int page_shift, float inv_qmax, unsigned char *codes,
                    float *scales)
 {
     sm100::griddep_launch();
@@ -154,13 +148,13 @@ cache_write_kernel(const T *K, const T *V, long long ld_token, long long ld_head
 #pragma unroll
         for (int i = 0; i < 16; ++i) v[i] = to_f32(x[i]);
     }
-    const long long row = cache_row(slot, L, at.h);
+    const long long row = cache_row(slot, L, page_shift, at.h);
     if (row < 0) return;
     const unsigned per = (unsigned)L.dim / 16;
     const unsigned lanes = ((1u << per) - 1u) << (threadIdx.x & 31 & ~(per - 1));
     const int qmax = (1 << (L.bits - 1)) - 1;
     uint32_t u[16];
-    const float s = row_codes(v, row_top(v, per, lanes), qmax, inv_qmax, u);
+    const float s = row_codes<sizeof(T) == 2 ? 1 : 2>(v, row_top(v, per, lanes), qmax, inv_qmax, u);
     store_row(u, s, row, at.j0, L, codes, scales);
 }
 
@@ -187,14 +181,14 @@ __device__ __forceinline__ uint4 load_codes(const unsigned char *row, int j0, in
 
 template <typename T>
 __global__ void __launch_bounds__(KV_THREADS)
-cache_read_kernel(const int64_t *slots, int n, mpq_kv_cache L, const unsigned char *codes,
-                  const float *scales, T *K, T *V)
+cache_read_kernel(const int64_t *slots, int n, mpq_kv_cache L, int page_shift,
+                  const unsigned char *codes, const float *scales, T *K, T *V)
 {
     sm100::griddep_launch();
     sm100::griddep_wait();
     RowAt at;
     if (!row_at(n, L, at)) return;
-    const long long row = cache_row(slots[at.t], L, at.h);
+    const long long row = cache_row(slots[at.t], L, page_shift, at.h);
     const long long v_row = row + (long long)L.heads * L.page;
     uint4 kw = make_uint4(0, 0, 0, 0), vw = make_uint4(0, 0, 0, 0);
     float ks = 0.0f, vs = 0.0f;      // (a slot outside the cache: zeros)
@@ -218,6 +212,14 @@ dim3 kv_grid(int T, const mpq_kv_cache *L, int heads)
 {
     const long long per_block = KV_THREADS / (L->dim / 16);
     return dim3((unsigned)((T + per_block - 1) / per_block), (unsigned)heads, 1);
+}
+
+// log2 of the page, -1 where it is no power of two.
+int page_shift(const mpq_kv_cache *L)
+{
+    int s = 0;
+    while (1 << s < L->page) ++s;
+    return 1 << s == L->page ? s : -1;
 }
 
 }  // namespace
@@ -249,7 +251,7 @@ mpq_status launch_cache_write(const void *K, const void *V, int type, long long 
                               kv_grid(T, L, 2 * L->heads), dim3(KV_THREADS), 0, stream,
                               "cache write launch", static_cast<const E *>(K),
                               static_cast<const E *>(V), ld_token, ld_head, T, slots, *L,
-                              1.0f / (float)((1 << (L->bits - 1)) - 1),
+                              page_shift(L), 1.0f / (float)((1 << (L->bits - 1)) - 1),
                               static_cast<unsigned char *>(codes), scales);
     });
 }
@@ -260,7 +262,7 @@ mpq_status launch_cache_read(const int64_t *slots, int T, const mpq_kv_cache *L,
     return by_type(type, [&](auto t) {
         using E = decltype(t);
         return launch_waiting(cache_read_kernel<E>, kv_grid(T, L, L->heads), dim3(KV_THREADS), 0,
-                              stream, "cache read launch", slots, T, *L,
+                              stream, "cache read launch", slots, T, *L, page_shift(L),
                               static_cast<const unsigned char *>(codes), scales,
                               static_cast<E *>(K), static_cast<E *>(V));
     });
