@@ -34,6 +34,7 @@
 
 #include "elements.cuh"
 #include "mpq_internal.cuh"
+#include "mx_ops.cuh"
 #include "pair_common.cuh"
 #include "sm100.cuh"
 #include "waits.cuh"
