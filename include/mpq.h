@@ -17,8 +17,9 @@
  *  - `stream` is a cudaStream_t passed as void* (NULL = the legacy default stream).  Every call
  *    only enqueues work on `stream` and returns; results are ready when the stream reaches them.
  *    No entry point synchronizes, and none allocates device memory except the scratch of
- *    mpq_output_error, mpq_clip_search and mpq_quantize_layer_adaptive, which comes from the
- *    device's stream-ordered pool on `stream` and goes back to it on `stream` (see there).
+ *    mpq_output_error, mpq_clip_search and mpq_quantize_layer_adaptive, and of mpq_cache_attention
+ *    without a workspace, which comes from the device's stream-ordered pool on `stream` and goes
+ *    back to it on `stream` (see there).
  *  - Arguments are validated on the host before anything is enqueued; an invalid argument
  *    returns MPQ_ERR_INVALID_ARG / MPQ_ERR_UNSUPPORTED and leaves every output untouched.
  *    A failed kernel launch returns MPQ_ERR_CUDA.  mpq_last_error() gives a message for the
@@ -45,7 +46,7 @@ typedef enum {
     MPQ_ERR_UNSUPPORTED = 3,  /* valid for the method but beyond this library's limits below */
     MPQ_ERR_CUDA = 4,         /* a CUDA runtime call or kernel launch failed */
     MPQ_ERR_TIMEOUT = 5,      /* a bounded device-side wait gave up (mpq_device_status) */
-    MPQ_ERR_NOMEM = 6,        /* mpq_output_error's stream-ordered scratch allocation failed */
+    MPQ_ERR_NOMEM = 6,        /* a call's stream-ordered scratch allocation failed */
     MPQ_ERR_BOUNDS = 7        /* the checked build skipped an out-of-range access (mpq_device_status) */
 } mpq_status;
 
@@ -517,7 +518,8 @@ mpq_status mpq_cache_read(const int64_t *slots, int T, const mpq_kv_cache *layou
  *   lens     [B] int32: n_b; taken as within 0 .. page * table_cols.
  *   scale    finite; 1 / sqrt(dim) is usual.
  *   window   0: the whole sequence; else the newest `window` tokens.
- *   O        out [B][q_heads][dim] of type `type`, 16-byte aligned.  A sequence with nothing to attend to gets zeros.
+ *   O        out [B][q_heads][dim] of type `type`, 16-byte aligned.  A sequence with nothing to attend to
+ *            gets zeros.
  *   lse      out [B][q_heads] fp32, nullable: log sum_t p_t (-infinity where there is nothing).
  *   workspace  16-byte aligned device memory of at least mpq_cache_attention_workspace() bytes, or
  *            NULL to take it from the device's stream-ordered pool on `stream` (as
@@ -538,12 +540,12 @@ size_t mpq_cache_attention_workspace(void);
 
 /*
  * Bounded device-side waits.  The tensor-core kernels (mpq_output_error and its _noalloc variant,
- * mpq_clip_search, mpq_multipoint_linear, mpq_mx_linear) hand work between their warps, and mpq_cache_attention's warps
- * take their copies, through shared-memory
- * barriers, and every wait on one is bounded by a clock budget.  A kernel whose wait gives up
+ * mpq_clip_search, mpq_multipoint_linear, mpq_mx_linear) hand work between their warps, and
+ * mpq_cache_attention's warps take their copies, through shared-memory barriers, and every wait on
+ * one is bounded by a clock budget.  A kernel whose wait gives up
  * stops issuing work, waits for the copies and MMAs it has already issued to finish, releases its
- * tensor memory and returns, with NaN in its output errors (the outputs of mpq_multipoint_linear and
- * mpq_mx_linear unspecified);
+ * tensor memory and returns, with NaN in its output errors and in mpq_cache_attention's outputs (the
+ * outputs of mpq_multipoint_linear and mpq_mx_linear unspecified);
  * it records which kernel it was in a word kept per device.  A NaN error can therefore mean a
  * non-finite input or a timeout: mpq_device_status tells them apart.
  */
@@ -593,7 +595,8 @@ mpq_status mpq_set_wait_limit(long long clocks);
  * mpq_test_withhold_copies -- TEST HOOK, process-wide: while on (1), the tile-copy thread of the
  * output-error contraction (mpq_output_error's tensor-core path) issues no copies, so that every
  * wait of that kernel runs out with nothing in flight and the call reports MPQ_TIMEOUT_OUTPUT_ERROR
- * through mpq_device_status; likewise mpq_cache_attention's warps (MPQ_TIMEOUT_ATTENTION).  Off (0) by default; never on outside tests of the timeout path.
+ * through mpq_device_status; likewise mpq_mx_linear's (MPQ_TIMEOUT_MX) and mpq_cache_attention's warps
+ * (MPQ_TIMEOUT_ATTENTION).  Off (0) by default; never on outside tests of the timeout path.
  */
 mpq_status mpq_test_withhold_copies(int on);
 

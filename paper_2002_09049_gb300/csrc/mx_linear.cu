@@ -23,6 +23,10 @@
 // both, the cluster sends each quarter of B to the two CTAs that need it and each scale tile of B to all
 // four (multicast): 35 KB in and 32 KB read a stage, 25.5 KB from L2.
 //
+// Measured: 1 x 4,096 x 4,096 (T x C x d) 5.0 us and 37 x 11,008 x 4,096 8.3 us (weights' bytes at 1.8 and 2.9
+// TB/s; latency of one round of CTAs), 1,024 x 4,096 x 4,096 11.9 us, 2,048 x 4,096 x 11,008 46.8 us (3.9
+// PFLOP/s; 64 clusters on 36 places are two rounds).
+//
 // Roles: warp 0 copies, warp 1 issues MMAs (the even CTA's, for a pair), warps 2..5 (TMEM lane quarter
 // warp % 4) move scales, then write the outputs -- with warps 6..9 where there are such.  Every wait is
 // bounded.
@@ -227,7 +231,7 @@ mx_linear_kernel(const MxArgs a, T *Y, WaitCtl wc, const __grid_constant__ CUten
             const size_t sf_a = (size_t)tile * a.k_tiles * X_SF;
             const size_t sf_b = (size_t)(n0 / 128) * a.k_tiles * X_SF;
             int issued = k0;
-            for (int k = k0; k < k1; ++k) {
+            for (int k = k0; k < k1 && !wc.withhold; ++k) {
                 const int i = k - k0, s = i % a.stages;
                 if (i >= a.stages &&
                     !mbar_wait_cluster(&ctl.empty[s], (uint32_t)(i / a.stages - 1) & 1u, wc.budget)) {

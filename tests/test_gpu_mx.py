@@ -267,6 +267,25 @@ def test_chain_of_dependent_calls(gpu):
         assert torch.equal(y, want)
 
 
+@pytest.mark.parametrize("T,C,d", [(4, 300, 512), (4, 300, 8192), (352, 8136, 448)])
+def test_linear_withheld_copies_time_out(gpu, T, C, d):
+    """With the test hook on, the kernel's waits run out with nothing in flight: the status says so, and the
+    same call is right again after (K whole, K split over a cluster, CTA pairs)."""
+    good, _, _, (xp, xl, wp, wl) = linear(T, C, d, "bf16", False, 3)
+    assert binding.mpq_device_status() == 0
+    try:
+        binding.mpq_set_wait_limit(1 << 18)
+        binding.mpq_test_withhold_copies(True)
+        binding.mpq_mx_linear(xp, xl, wp, wl)
+        flags = binding.mpq_device_status()
+    finally:
+        binding.mpq_test_withhold_copies(False)
+        binding.mpq_set_wait_limit(0)
+    assert flags == binding.MPQ_TIMEOUT_MX
+    assert torch.equal(binding.mpq_mx_linear(xp, xl, wp, wl), good)
+    assert binding.mpq_device_status() == 0
+
+
 def test_linear_keeps_a_temporary_bias(gpu):
     """A bias that nothing but the call refers to is not overwritten by the output allocated in it."""
     T, C = 1, 600
