@@ -31,8 +31,9 @@
 // order of the ranges, so the result does not depend on who comes last.
 //
 // Measured, 8 key heads x 4 query heads of 128, 8 bits: 2 sequences of 131,072 tokens 91 us (554 MB, 6.1 TB/s;
-// 4 bits: also 91 us, bound by 500 warp instructions a stage); 96 sequences of 0 to 4,096, 35 us (a row's start
-// and end cost two stages' time, ranges are ten stages long); one of 777 tokens 11.1 us (latency).
+// 4 bits: also 91 us, bound by 500 warp instructions a stage); 96 sequences of 0 to 4,096, 32 us (a row's start
+// and end cost four stages' time, ranges are ten stages long); one of 777 tokens 11.2 us, one of 64 6.6
+// (latency).
 #include <cuda.h>
 #include <float.h>
 #include <math.h>
@@ -54,9 +55,11 @@ namespace {
 using namespace sm100;
 
 constexpr int A_STAGE = 16;                       // tokens of a stage
-constexpr int A_ROW_COST = 2;                     // what a row costs besides its stages, in stages
+constexpr int A_ROW_COST = 4;                     // what a row costs besides its stages, in stages: 96 ragged
+                                                  // sequences 34.7, 32.9, 31.9, 32.1 us with 2, 3, 4, 5
 constexpr int A_LEAST = 2;                        // stages a warp is woken for
 constexpr int A_ROW = 6;                          // most stages of a warp where each CTA takes one row
+constexpr int A_WHOLE = 10;                       // most stages (and costs) of a row that a warp takes alone
 constexpr int A_MAX_CTAS = 512;                   // counters at the head of the workspace
 constexpr size_t A_COUNTERS = A_MAX_CTAS * sizeof(unsigned);
 constexpr float A_SHIFT = 6.0f, A_MARGIN = 14.0f; // r = largest / 2^6; moves past r 2^14
@@ -379,11 +382,16 @@ cache_attention_kernel(const AttnArgs a, WaitCtl wc, const __grid_constant__ CUt
         }
     };
     // the warps that take part, and this one's range.  A CTA a row where there are no more rows than CTAs
-    // and a warp then has A_ROW stages at most: joining CTAs takes longer than that.
+    // and a warp then has A_ROW stages at most: joining CTAs takes longer than that (1 x 500 tokens 9.7 us,
+    // 12.6 for the 1,024 that CTAs share).  A warp a row where there are more and they are short: nothing is
+    // joined (96 x 64 tokens 11.3 us, 12.9 in ranges of two stages; 12 stages a row are too many: a case of 13 us
+    // took 18).
     const long long rows = (long long)some * units;
     const bool by_row = per == 1 && rows <= gridDim.x && total <= rows * (W * A_ROW);
-    const int workers = by_row ? (int)min(rows * W, total)
-                               : (int)min((long long)gridDim.x * W, max(total / A_LEAST, 1LL));
+    const bool whole = rows > gridDim.x && rows <= (long long)gridDim.x * W && total <= rows * A_WHOLE;
+    const int workers = by_row  ? (int)(rows * W)
+                        : whole ? (int)rows
+                                : (int)min((long long)gridDim.x * W, max(total / A_LEAST, 1LL));
     const int me = blockIdx.x * W + warp;
     if ((int)blockIdx.x * W >= workers || total == 0) {
         empty_rows();
@@ -993,8 +1001,9 @@ mpq_status launch_shape(const AttnArgs &a, cudaStream_t stream)
     WaitCtl wc;
     const mpq_status ws = wait_ctl(&wc);
     if (ws != MPQ_OK) return ws;
-    // one CTA per SM, fewer where the tables cannot hold work for all their warps; the workspace has
-    // room for two rows' sums of each CTA and one of each warp
+    // one CTA per SM, fewer where the tables cannot hold work for all their warps, but no fewer than rows (1 and
+    // 4 sequences of 64 tokens 6.6 and 6.8 us, 8.2 and 10.0 with the CTAs that their stages wake); the
+    // workspace has room for two rows' sums of each CTA and one of each warp
     const long long room = (long long)a.cols * a.L.page;
     const long long span = a.window > 0 ? std::min<long long>(room, a.window) + A_STAGE : room;
     const long long stages = (span + A_STAGE - 1) / A_STAGE * a.L.heads * a.blocks;   // of a sequence
@@ -1002,9 +1011,10 @@ mpq_status launch_shape(const AttnArgs &a, cudaStream_t stream)
         (long long)((MPQ_CACHE_WORKSPACE - A_COUNTERS) / ((2 + S::WARPS) * S::SUMS * sizeof(float)));
     const long long most = std::min<long long>(std::min<long long>(sm_count(), fit), A_MAX_CTAS);
     const long long wake = (long long)A_LEAST * S::WARPS;                 // stages that wake a CTA
+    const long long rows = (long long)a.B * a.L.heads * a.blocks;
     const long long ctas = stages >= most * wake
                                ? most
-                               : std::min(most, std::max(1LL, (stages * a.B + wake - 1) / wake));
+                               : std::min(most, std::max(rows, (stages * a.B + wake - 1) / wake));
     return launch_waiting(cache_attention_kernel<T, D, BITS, NT>, dim3((unsigned)ctas),
                           dim3(S::THREADS), S::SMEM, stream, "cache attention launch", a, wc, tm);
 }
