@@ -16,16 +16,16 @@
 // in the order of the ranks (so equal inputs give equal bits).
 //
 // Many tokens: tokens on the lanes (a lane then writes runs of consecutive outputs), tiles of 256 tokens
-// x 256 channels by CTA pairs (cta_group::2: each CTA holds 128 tokens and half of the channels), two
-// pairs a cluster on the same channels.  One CTA alone with a 128 x 256 tile is bound by shared memory
-// (52 KB a stage in and 48 KB read by the MMAs, 784 cycles at 128 bytes each beside the MMAs' 513) and by
-// what L2 delivers (43 bytes per SM and cycle measured: 1,200 cycles).  The pair halves B's share of
-// both, the cluster sends each quarter of B to the two CTAs that need it and each scale tile of B to all
-// four (multicast): 35 KB in and 32 KB read a stage, 25.5 KB from L2.
+// x 256 channels by CTA pairs (cta_group::2: each CTA holds 128 tokens and half of the channels).  One CTA
+// alone with a 128 x 256 tile is bound by shared memory (52 KB a stage in and 48 KB read by the MMAs, 784
+// cycles at 128 bytes each beside the MMAs' 513) and by what L2 delivers (43 bytes per SM and cycle measured:
+// 1,200 cycles).  The pair halves B's share of both: 35 KB in and 32 KB read a stage, 0.5 us of it.  Each CTA
+// loads all that it holds: a load for several CTAs at once would want its source in this GPU's own memory,
+// which a pointer does not say.
 //
-// Measured: 1 x 4,096 x 4,096 (T x C x d) 5.0 us and 37 x 11,008 x 4,096 8.3 us (weights' bytes at 1.8 and 2.9
-// TB/s; latency of one round of CTAs), 1,024 x 4,096 x 4,096 11.9 us, 2,048 x 4,096 x 11,008 46.8 us (3.9
-// PFLOP/s; 64 clusters on 36 places are two rounds).
+// Measured: 1 x 4,096 x 4,096 (T x C x d) 5.1 us and 37 x 11,008 x 4,096 8.4 us (weights' bytes at 1.7 and 2.8
+// TB/s; latency of one round of CTAs), 1,024 x 4,096 x 4,096 13.2 us, 2,048 x 4,096 x 11,008 51.9 us (3.6
+// PFLOP/s; 128 tiles on 76 pairs are two rounds).
 //
 // Roles: warp 0 copies, warp 1 issues MMAs (the even CTA's, for a pair), warps 2..5 (TMEM lane quarter
 // warp % 4) move scales, then write the outputs -- with warps 6..9 where there are such.  Every wait is
@@ -58,8 +58,6 @@ constexpr int X_A_BYTES = X_M * X_ROW;
 constexpr int X_MAX_STAGES = 8;
 constexpr int X_THREADS = 320;           // at most: warps 6..9 may be left out
 constexpr int X_MAX_SPLIT = 8;           // CTAs of a cluster that splits K
-constexpr int X_PAIRS = 2;               // CTA pairs of a cluster that shares B
-constexpr int X_SHARE = 2 * X_PAIRS;     // its CTAs
 
 struct MxCtrl {
     uint64_t full[X_MAX_STAGES];         // a stage's tiles and scales have landed
@@ -169,8 +167,8 @@ __device__ __forceinline__ void join(const MxArgs &a, T *Y, const JoinAt &at)
     }
 }
 
-// MANY: A is the inputs, B the weights; clusters of X_PAIRS CTA pairs, one below the other along A.  Else A
-// is the weights, B the inputs, K split over clusters of a.split.
+// MANY: A is the inputs, B the weights; a cluster is a CTA pair.  Else A is the weights, B the inputs, K split
+// over clusters of a.split.
 template <typename T, bool MANY>
 __global__ void __launch_bounds__(MANY ? 192 : X_THREADS)
 mx_linear_kernel(const MxArgs a, T *Y, WaitCtl wc, const __grid_constant__ CUtensorMap tmA,
@@ -188,9 +186,9 @@ mx_linear_kernel(const MxArgs a, T *Y, WaitCtl wc, const __grid_constant__ CUten
     const bool cluster = MANY || a.split > 1;
     const int rank = cluster ? (int)cluster_ctarank() : 0;
     // the tile: this CTA's row tile of A, the first row of B
-    const int pair = MANY ? rank >> 1 : 0, half = MANY ? rank & 1 : 0;
-    const int group = (int)blockIdx.x / (MANY ? X_SHARE : a.split);
-    const int tile = MANY ? (group / a.n_tiles) * X_SHARE + rank : group;
+    const int half = MANY ? rank : 0;    // of the pair: which half of B's rows it holds
+    const int group = (int)blockIdx.x / (MANY ? 2 : a.split);
+    const int tile = MANY ? (group / a.n_tiles) * 2 + rank : group;
     const long long n0 = MANY ? (long long)(group % a.n_tiles) * X_N : (long long)blockIdx.y * a.n_tile;
     const int n_real = (int)min((long long)a.n_tile, a.b_rows - n0);         // rows of B that there are
     const int a_sf = tile < a.a_tiles ? 1 : 0;                       // scale tiles (per k tile) of A, of B
@@ -203,7 +201,7 @@ mx_linear_kernel(const MxArgs a, T *Y, WaitCtl wc, const __grid_constant__ CUten
         for (int i = 0; i < a.stages; ++i) {
             mbar_init(&ctl.full[i], 1);
             mbar_init(&ctl.scaled[i], MANY ? 8 : 4);         // warps of this CTA (even CTA: of the pair)
-            mbar_init(&ctl.empty[i], MANY ? X_PAIRS : 1);
+            mbar_init(&ctl.empty[i], 1);
         }
         mbar_init(&ctl.done, 1);
         ctl.abort = 0;
@@ -249,37 +247,21 @@ mx_linear_kernel(const MxArgs a, T *Y, WaitCtl wc, const __grid_constant__ CUten
                 uint64_t *const bar = &ctl.full[s];
                 mbar_arrive_expect_tx(bar, (uint32_t)(X_A_BYTES + a.b_held * X_ROW +
                                                       (a_sf + b_sf) * kt * X_SF));
-                if constexpr (MANY) {
-                    // this CTA's rows of A; a quarter of B: of its half, the slice of its pair, for the CTAs
-                    // of the same half; one scale tile of B (row tile, k tile) for all
-                    constexpr int SLICE = X_N / X_SHARE;
-                    static_assert(X_PAIRS == 2, "two slices of a half, four scale tiles");
-                    tma_load_2d(at, &tmA, k * X_ROW, tile * X_M, bar);
-                    tma_load_2d_multicast(at + X_A_BYTES + pair * SLICE * X_ROW, &tmB, k * X_ROW,
-                                          (int)n0 + half * (X_N / 2) + pair * SLICE, bar,
-                                          (uint16_t)(5u << half));
-                    if (a_sf)
-                        bulk_load(sfs, a.a_scales + sf_a + (size_t)(2 * k) * X_SF, (uint32_t)(kt * X_SF), bar);
-                    if (half < kt && pair < b_sf)
-                        bulk_load_multicast(sfs + (2 + rank) * X_SF,
-                                            a.b_scales + sf_b + ((size_t)pair * a.k_tiles + 2 * k + half) * X_SF,
-                                            X_SF, bar, (uint16_t)((1u << X_SHARE) - 1u));
-                } else {
-                    tma_load_2d(at, &tmA, k * X_ROW, tile * X_M, bar);
-                    tma_load_2d(at + X_A_BYTES, &tmB, k * X_ROW, (int)n0, bar);
+                tma_load_2d(at, &tmA, k * X_ROW, tile * X_M, bar);
+                tma_load_2d(at + X_A_BYTES, &tmB, k * X_ROW, (int)n0 + half * (X_N / 2), bar);
+                if (a_sf)
                     bulk_load(sfs, a.a_scales + sf_a + (size_t)(2 * k) * X_SF, (uint32_t)(kt * X_SF), bar);
-                    for (int r = 0; r < b_sf; ++r)
-                        bulk_load(sfs + (uint32_t)((2 + 2 * r) * X_SF),
-                                  a.b_scales + sf_b + ((size_t)r * a.k_tiles + 2 * k) * X_SF,
-                                  (uint32_t)(kt * X_SF), bar);
-                }
+                for (int r = 0; r < b_sf; ++r)
+                    bulk_load(sfs + (uint32_t)((2 + 2 * r) * X_SF),
+                              a.b_scales + sf_b + ((size_t)r * a.k_tiles + 2 * k) * X_SF,
+                              (uint32_t)(kt * X_SF), bar);
                 issued = k + 1;
             }
             // no copy may land after the CTA is gone
             for (int k = max(k0, issued - a.stages); k < issued; ++k)
                 drain_wait(&ctl.full[(k - k0) % a.stages], (uint32_t)((k - k0) / a.stages) & 1u, wc,
                            MPQ_TIMEOUT_MX);
-            // ... nor an arrival for another pair's MMAs
+            // ... nor an arrival for the pair's MMAs
             for (int k = max(k0, issued - a.stages); MANY && k < issued && !*abort_flag; ++k)
                 drain_wait_cluster(&ctl.empty[(k - k0) % a.stages], (uint32_t)((k - k0) / a.stages) & 1u,
                                    wc, MPQ_TIMEOUT_MX);
@@ -314,8 +296,8 @@ mx_linear_kernel(const MxArgs a, T *Y, WaitCtl wc, const __grid_constant__ CUten
                     else
                         mma_mxf4(tmem, ad + o, bd + o, id, sfa, sfb, more);
                 }
-                if (MANY)                // every CTA of the cluster loads for this pair
-                    mma_commit_pair(&ctl.empty[s], (uint16_t)((1u << X_SHARE) - 1u));
+                if (MANY)                // both CTAs load for the pair
+                    mma_commit_pair(&ctl.empty[s], (uint16_t)3);
                 else
                     mma_commit(&ctl.empty[s]);
                 if (++s == a.stages) {
@@ -325,7 +307,7 @@ mx_linear_kernel(const MxArgs a, T *Y, WaitCtl wc, const __grid_constant__ CUten
             }
             // every MMA issued above completes before its sums are read or tensor memory released
             if (MANY)
-                mma_commit_pair(&ctl.done, (uint16_t)(3u << (2 * pair)));
+                mma_commit_pair(&ctl.done, (uint16_t)3);
             else
                 mma_commit(&ctl.done);
             drain_wait_cluster(&ctl.done, 0, wc, MPQ_TIMEOUT_MX);
@@ -369,7 +351,7 @@ mx_linear_kernel(const MxArgs a, T *Y, WaitCtl wc, const __grid_constant__ CUten
                 __syncwarp();
                 if (lane == 0) {
                     if (MANY)
-                        mbar_arrive_cluster(&ctl.scaled[s], (uint32_t)(rank & ~1));
+                        mbar_arrive_cluster(&ctl.scaled[s], 0);
                     else
                         mbar_arrive(&ctl.scaled[s]);
                 }
@@ -475,7 +457,7 @@ mpq_status launch_typed(const MxArgs &a, const void *A, const void *B, int row_b
     const cuuint64_t row = (cuuint64_t)row_bytes;
     const cuuint64_t da[2] = {row, (cuuint64_t)a.a_rows}, db[2] = {row, (cuuint64_t)a.b_rows}, st[1] = {row};
     const cuuint32_t ba[2] = {X_ROW, X_M};
-    const cuuint32_t bb[2] = {X_ROW, MANY ? (cuuint32_t)(X_N / X_SHARE) : (cuuint32_t)a.n_tile};
+    const cuuint32_t bb[2] = {X_ROW, (cuuint32_t)a.b_held};
     if (!encode_tile_map(&tmA, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, A, da, st, ba,
                          CU_TENSOR_MAP_SWIZZLE_128B) ||
         !encode_tile_map(&tmB, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, B, db, st, bb,
@@ -525,19 +507,19 @@ int few_split(long long tiles, int n, int k_stages, int sms)
 // CTAs, a start, the stages by their bytes and the columns on their way out, in units of about 10 ns; CTAs
 // that share an SM take longer over the last two.  The constants are fitted to 500 timings of 110 sizes
 // (17 <= T <= 4,096, 64 <= C, d <= 14,000): the choice costs 1% on average, 9% at worst, against the best
-// of the forms.  Some of them, us, with 32 / 64 / 128 / 256 rows / pairs: 1,233 x 448 x 448 3.7, 4.1, 4.4,
-// 5.9, 5.2; 128 x 4,096 x 4,096 8.5, 7.8, 7.7, -, -; 207 x 8,960 x 7,680 34, 18.3, 17.4, 14.6, -;
-// 512 x 4,096 x 4,096 21.3, 11.4, 10.6, 10.6, 11.2; 1,024 x 4,096 x 4,096 40, 22.3, 20.9, 13.2, 11.9.
+// of the forms.  Some of them, us, with 32 / 64 / 128 / 256 rows / pairs: 1,233 x 448 x 448 3.9, 4.1, 4.5,
+// 6.2, 5.5; 128 x 4,096 x 4,096 8.5, 7.8, 7.7, -, -; 207 x 8,960 x 7,680 34, 18.3, 17.4, 14.6, -;
+// 512 x 4,096 x 4,096 21.5, 11.6, 10.9, 10.9, 12.4; 1,024 x 4,096 x 4,096 41, 22.6, 21.3, 13.5, 13.2;
+// 2,785 x 10,304 x 448 90, 51, 55, 37.4, 35.5.
 int few_tile(int T, int C, int k_stages, int sms, bool pairs)
 {
     const long long m_tiles = ((long long)C + X_M - 1) / X_M;
     auto rounds = [](long long ctas, long long at_once) { return (double)((ctas + at_once - 1) / at_once); };
     int best = 0;
     double least = HUGE_VAL;
-    if (pairs) {                         // clusters of four leave 8 of 152 SMs idle
-        const long long ctas = ((long long)T + X_SHARE * X_M - 1) / (X_SHARE * X_M) *
-                               (((long long)C + X_N - 1) / X_N) * X_SHARE;
-        least = rounds(ctas, std::max(X_SHARE, sms / 38 * 36)) * (740.0 + 22.0 * k_stages);
+    if (pairs) {
+        const long long ctas = ((long long)T + 2 * X_M - 1) / (2 * X_M) * (((long long)C + X_N - 1) / X_N) * 2;
+        least = rounds(ctas, std::max(2, sms / 2 * 2)) * (740.0 + 22.0 * k_stages);
     }
     for (int n = X_N; n >= 32; n /= 2) {
         const int width = std::min(n, (T + 15) / 16 * 16);
@@ -583,7 +565,7 @@ mpq_status launch_mx_linear(const mpq_mx_matrix *xl, const void *X, const mpq_mx
     const int n = few_tile(T, C, a.k_stages, sms, T > X_N && a.wide && rows_aligned(Y, y_type, ldy));
     if (n == 0) {
         const long long n_cl = ((long long)C + X_N - 1) / X_N;
-        const long long ctas = ((long long)T + X_SHARE * X_M - 1) / (X_SHARE * X_M) * n_cl * X_SHARE;
+        const long long ctas = ((long long)T + 2 * X_M - 1) / (2 * X_M) * n_cl * 2;
         a.a_rows = T;
         a.b_rows = C;
         a.a_tiles = xl->row_tiles;
@@ -599,7 +581,7 @@ mpq_status launch_mx_linear(const mpq_mx_matrix *xl, const void *X, const mpq_mx
             return MPQ_ERR_UNSUPPORTED;
         }
         return by_type(y_type, [&](auto t) {
-            return launch_typed<decltype(t), true>(a, X, W, wl->d_pad / 2, dim3((unsigned)ctas), X_SHARE, Y,
+            return launch_typed<decltype(t), true>(a, X, W, wl->d_pad / 2, dim3((unsigned)ctas), 2, Y,
                                                    stream);
         });
     }

@@ -1,5 +1,5 @@
-// Instructions of the microscaled linear layer beside those of sm100.cuh: block-scaled MMAs, untiled and
-// multicast copies, wide reads of another CTA's shared memory.
+// Instructions of the microscaled linear layer beside those of sm100.cuh: block-scaled MMAs, untiled
+// copies, wide reads of another CTA's shared memory.
 #pragma once
 
 #include "sm100.cuh"
@@ -59,28 +59,6 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_
     asm volatile(
         "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
         ::"r"(dst), "l"(__cvta_generic_to_global(src)), "r"(bytes), "r"(smem_u32(bar))
-        : "memory");
-}
-
-// The same copies to every CTA of `cta_mask` (of the cluster): at dst's offset in its shared memory,
-// counted on the barrier at bar's offset there.
-__device__ __forceinline__ void tma_load_2d_multicast(uint32_t dst, const void *tmap, int x, int y,
-                                                      uint64_t *bar, uint16_t cta_mask)
-{
-    asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
-        ".multicast::cluster [%0], [%1, {%2, %3}], [%4], %5;" ::"r"(dst),
-        "l"(reinterpret_cast<uint64_t>(tmap)), "r"(x), "r"(y), "r"(smem_u32(bar)), "h"(cta_mask)
-        : "memory");
-}
-
-__device__ __forceinline__ void bulk_load_multicast(uint32_t dst, const void *src, uint32_t bytes,
-                                                    uint64_t *bar, uint16_t cta_mask)
-{
-    asm volatile(
-        "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.multicast::cluster [%0], [%1], "
-        "%2, [%3], %4;" ::"r"(dst),
-        "l"(__cvta_generic_to_global(src)), "r"(bytes), "r"(smem_u32(bar)), "h"(cta_mask)
         : "memory");
 }
 
