@@ -8,6 +8,7 @@
 
 #include <ATen/core/Tensor.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -49,13 +50,41 @@ const char *dtype_name(at::ScalarType t)
     }
 }
 
-const at::Tensor &tensor(PyObject *o, const char *name)
-{
-    if (!THPVariable_Check(o)) refuse(PyExc_TypeError, "%s must be a torch tensor", name);
-    const at::Tensor &t = THPVariable_Unpack(o);
-    if (!t.is_cuda()) refuse(PyExc_ValueError, "%s must be a CUDA tensor", name);
-    return t;
-}
+// What the tensors of one call have in common: they lie on one device, which is the current one when the
+// call is made (stream).
+class Call {
+public:
+    const at::Tensor &tensor(PyObject *o, const char *name)
+    {
+        if (!THPVariable_Check(o)) refuse(PyExc_TypeError, "%s must be a torch tensor", name);
+        const at::Tensor &t = THPVariable_Unpack(o);
+        if (!t.is_cuda()) refuse(PyExc_ValueError, "%s must be a CUDA tensor", name);
+        const int device = t.device().index();
+        if (device_ < 0) device_ = device;
+        if (device != device_)
+            refuse(PyExc_ValueError, "%s must lie on the other tensors' device, %s", name,
+                   ("cuda:" + std::to_string(device_) + ", is on cuda:" + std::to_string(device)).c_str());
+        return t;
+    }
+    // The stream argument's handle (None: the current stream's).
+    void *stream(PyObject *o) const
+    {
+        const int current = c10::cuda::current_device();
+        if (device_ != current)
+            refuse(PyExc_ValueError, "the tensors lie on %s, the current device is %s",
+                   ("cuda:" + std::to_string(device_)).c_str(), ("cuda:" + std::to_string(current)).c_str());
+        if (o == Py_None) return c10::cuda::getCurrentCUDAStream().stream();
+        PyObject *h = PyObject_GetAttrString(o, "cuda_stream");
+        if (!h) throw Refused();
+        void *s = PyLong_AsVoidPtr(h);
+        Py_DECREF(h);
+        if (PyErr_Occurred()) throw Refused();
+        return s;
+    }
+
+private:
+    int device_ = -1;
+};
 
 std::string text(at::IntArrayRef s)
 {
@@ -72,18 +101,18 @@ void need_shape(const at::Tensor &t, const char *name, at::IntArrayRef shape)
 }
 
 // A contiguous CUDA tensor of a type (and, where there is one, a shape).
-const at::Tensor &dense(PyObject *o, const char *name, at::ScalarType type)
+const at::Tensor &dense(Call &call, PyObject *o, const char *name, at::ScalarType type)
 {
-    const at::Tensor &t = tensor(o, name);
+    const at::Tensor &t = call.tensor(o, name);
     if (t.scalar_type() != type)
         refuse(PyExc_TypeError, "%s must be %s", name,
                (std::string(dtype_name(type)) + ", got " + dtype_name(t.scalar_type())).c_str());
     if (!t.is_contiguous()) refuse(PyExc_ValueError, "%s must be contiguous", name);
     return t;
 }
-const at::Tensor &dense(PyObject *o, const char *name, at::ScalarType type, at::IntArrayRef shape)
+const at::Tensor &dense(Call &call, PyObject *o, const char *name, at::ScalarType type, at::IntArrayRef shape)
 {
-    const at::Tensor &t = dense(o, name, type);
+    const at::Tensor &t = dense(call, o, name, type);
     need_shape(t, name, shape);
     return t;
 }
@@ -117,17 +146,6 @@ const L &layout(PyObject *o, const char *name)
     return *p;
 }
 
-void *stream_arg(PyObject *o)
-{
-    if (o == Py_None) return c10::cuda::getCurrentCUDAStream().stream();
-    PyObject *h = PyObject_GetAttrString(o, "cuda_stream");
-    if (!h) throw Refused();
-    void *s = PyLong_AsVoidPtr(h);
-    Py_DECREF(h);
-    if (PyErr_Occurred()) throw Refused();
-    return s;
-}
-
 long long integer(PyObject *o)
 {
     const long long v = PyLong_AsLongLong(o);
@@ -152,9 +170,9 @@ long long rows_of(const at::Tensor &t, const char *name, long long rows, long lo
     return step > d ? step : d;
 }
 
-const at::Tensor &packed(PyObject *o, const char *name, const mpq_mx_matrix &L)
+const at::Tensor &packed(Call &call, PyObject *o, const char *name, const mpq_mx_matrix &L)
 {
-    const at::Tensor &t = dense(o, name, at::kByte);
+    const at::Tensor &t = dense(call, o, name, at::kByte);
     if ((size_t)t.numel() < L.bytes)
         refuse(PyExc_ValueError, "%s is smaller than layout.bytes = %s", name,
                std::to_string(L.bytes).c_str());
@@ -185,60 +203,65 @@ PyObject *same(PyObject *o)
 
 PyObject *mx_quantize(PyObject *const *v)     // X, layout, packed, stream
 {
-    const at::Tensor &X = tensor(v[0], "X");
+    Call call;
+    const at::Tensor &X = call.tensor(v[0], "X");
     const mpq_mx_matrix &L = layout<mpq_mx_matrix>(v[1], "layout");
     const long long ld = rows_of(X, "X", L.rows, L.d);
     const int type = type_of(X.scalar_type(), "X");
     const bool own = v[2] == Py_None;
-    const at::Tensor out = own ? empty({(long long)L.bytes}, at::kByte, X) : packed(v[2], "packed", L);
-    done(f_mx_quantize(X.data_ptr(), type, ld, &L, out.data_ptr(), stream_arg(v[3])), "mpq_mx_quantize");
+    if (!own) packed(call, v[2], "packed", L);
+    void *const stream = call.stream(v[3]);
+    const at::Tensor out = own ? empty({(long long)L.bytes}, at::kByte, X) : THPVariable_Unpack(v[2]);
+    done(f_mx_quantize(X.data_ptr(), type, ld, &L, out.data_ptr(), stream), "mpq_mx_quantize");
     return own ? THPVariable_Wrap(out) : same(v[2]);
 }
 
 PyObject *mx_dequantize(PyObject *const *v)   // packed, layout, dtype, Y, stream
 {
+    Call call;
     const mpq_mx_matrix &L = layout<mpq_mx_matrix>(v[1], "layout");
-    const at::Tensor &p = packed(v[0], "packed", L);
+    const at::Tensor &p = packed(call, v[0], "packed", L);
     const bool own = v[3] == Py_None;
-    const at::Tensor Y = own ? empty({L.rows, L.d}, dtype_arg(v[2]), p) : tensor(v[3], "Y");
+    if (!own) call.tensor(v[3], "Y");
+    void *const stream = call.stream(v[4]);
+    const at::Tensor Y = own ? empty({L.rows, L.d}, dtype_arg(v[2]), p) : THPVariable_Unpack(v[3]);
     const long long ld = rows_of(Y, "Y", L.rows, L.d);
-    done(f_mx_dequantize(p.data_ptr(), &L, Y.data_ptr(), type_of(Y.scalar_type(), "Y"), ld,
-                         stream_arg(v[4])),
+    done(f_mx_dequantize(p.data_ptr(), &L, Y.data_ptr(), type_of(Y.scalar_type(), "Y"), ld, stream),
          "mpq_mx_dequantize");
     return own ? THPVariable_Wrap(Y) : same(v[3]);
 }
 
 PyObject *mx_linear(PyObject *const *v)       // X, x_layout, W, w_layout, bias, dtype, Y, stream
 {
+    Call call;
     const mpq_mx_matrix &xl = layout<mpq_mx_matrix>(v[1], "x_layout");
     const mpq_mx_matrix &wl = layout<mpq_mx_matrix>(v[3], "w_layout");
-    const at::Tensor &X = packed(v[0], "X", xl), &W = packed(v[2], "W", wl);
-    const float *bias = nullptr;
-    if (v[4] != Py_None)
-        bias = dense(v[4], "bias", at::kFloat, {wl.rows}).data_ptr<float>();
+    const at::Tensor &X = packed(call, v[0], "X", xl), &W = packed(call, v[2], "W", wl);
+    const at::Tensor *const bias = v[4] == Py_None ? nullptr : &dense(call, v[4], "bias", at::kFloat, {wl.rows});
     const bool own = v[6] == Py_None;
-    const at::Tensor Y = own ? empty({xl.rows, wl.rows}, dtype_arg(v[5]), X) : tensor(v[6], "Y");
+    if (!own) call.tensor(v[6], "Y");
+    void *const stream = call.stream(v[7]);
+    const at::Tensor Y = own ? empty({xl.rows, wl.rows}, dtype_arg(v[5]), X) : THPVariable_Unpack(v[6]);
     const long long ld = rows_of(Y, "Y", xl.rows, wl.rows);
-    done(f_mx_linear(&xl, X.data_ptr(), &wl, W.data_ptr(), bias, Y.data_ptr(),
-                     type_of(Y.scalar_type(), "Y"), ld, stream_arg(v[7])),
+    done(f_mx_linear(&xl, X.data_ptr(), &wl, W.data_ptr(), bias ? bias->data_ptr<float>() : nullptr, Y.data_ptr(),
+                     type_of(Y.scalar_type(), "Y"), ld, stream),
          "mpq_mx_linear");
     return own ? THPVariable_Wrap(Y) : same(v[6]);
 }
 
 // A cache's codes and scales.
 struct Storage {
-    void *codes;
-    float *scales;
-    Storage(const mpq_kv_cache &L, PyObject *c, PyObject *s)
-        : codes(dense(c, "codes", at::kByte, {L.pages, 2, L.heads, L.page, L.row_bytes}).data_ptr()),
-          scales(dense(s, "scales", at::kFloat, {L.pages, 2, L.heads, L.page}).data_ptr<float>())
+    const at::Tensor &codes, &scales;
+    Storage(Call &call, const mpq_kv_cache &L, PyObject *c, PyObject *s)
+        : codes(dense(call, c, "codes", at::kByte, {L.pages, 2, L.heads, L.page, L.row_bytes})),
+          scales(dense(call, s, "scales", at::kFloat, {L.pages, 2, L.heads, L.page}))
     {
     }
 };
 
-const at::Tensor &slots_arg(PyObject *o)
+const at::Tensor &slots_arg(Call &call, PyObject *o)
 {
-    const at::Tensor &t = dense(o, "slots", at::kLong);
+    const at::Tensor &t = dense(call, o, "slots", at::kLong);
     if (t.dim() != 1) refuse(PyExc_ValueError, "%s must be [T]", "slots");
     if (t.numel() > INT32_MAX) refuse(PyExc_ValueError, "%s has too many entries", "slots");
     return t;
@@ -246,7 +269,8 @@ const at::Tensor &slots_arg(PyObject *o)
 
 PyObject *cache_write(PyObject *const *v)     // K, V, slots, layout, codes, scales, stream
 {
-    const at::Tensor &K = tensor(v[0], "K"), &V = tensor(v[1], "V"), &slots = slots_arg(v[2]);
+    Call call;
+    const at::Tensor &K = call.tensor(v[0], "K"), &V = call.tensor(v[1], "V"), &slots = slots_arg(call, v[2]);
     const mpq_kv_cache &L = layout<mpq_kv_cache>(v[3], "layout");
     const long long T = slots.numel();
     need_shape(K, "K", {T, L.heads, L.dim});
@@ -254,26 +278,31 @@ PyObject *cache_write(PyObject *const *v)     // K, V, slots, layout, codes, sca
     if (K.scalar_type() != V.scalar_type() || K.strides() != V.strides())
         refuse(PyExc_ValueError, "K and V must have one type and the same strides%s", "");
     if (K.stride(2) != 1) refuse(PyExc_ValueError, "%s must have contiguous rows", "K and V");
-    const Storage s(L, v[4], v[5]);
+    const Storage s(call, L, v[4], v[5]);
+    void *const stream = call.stream(v[6]);
     done(f_cache_write(K.data_ptr(), V.data_ptr(), type_of(K.scalar_type(), "K"), K.stride(0), K.stride(1),
-                       (int)T, slots.data_ptr<int64_t>(), &L, s.codes, s.scales, stream_arg(v[6])),
+                       (int)T, slots.data_ptr<int64_t>(), &L, s.codes.data_ptr(), s.scales.data_ptr<float>(), stream),
          "mpq_cache_write");
     Py_RETURN_NONE;
 }
 
 PyObject *cache_read(PyObject *const *v)      // slots, layout, codes, scales, dtype, K, V, stream
 {
-    const at::Tensor &slots = slots_arg(v[0]);
+    Call call;
+    const at::Tensor &slots = slots_arg(call, v[0]);
     const mpq_kv_cache &L = layout<mpq_kv_cache>(v[1], "layout");
     const int64_t shape[3] = {slots.numel(), L.heads, L.dim};
-    const Storage s(L, v[2], v[3]);
-    at::Tensor out[2];
-    at::ScalarType type = v[5] == Py_None ? dtype_arg(v[4]) : tensor(v[5], "K").scalar_type();
+    const Storage s(call, L, v[2], v[3]);
+    const at::ScalarType type = v[5] == Py_None ? dtype_arg(v[4]) : call.tensor(v[5], "K").scalar_type();
     const int number = type_of(type, "K");
     for (int i = 0; i < 2; ++i)
-        out[i] = v[5 + i] == Py_None ? empty(shape, type, slots) : dense(v[5 + i], i ? "V" : "K", type, shape);
-    done(f_cache_read(slots.data_ptr<int64_t>(), (int)shape[0], &L, s.codes, s.scales, out[0].data_ptr(),
-                      out[1].data_ptr(), number, stream_arg(v[7])),
+        if (v[5 + i] != Py_None) dense(call, v[5 + i], i ? "V" : "K", type, shape);
+    void *const stream = call.stream(v[7]);
+    at::Tensor out[2];
+    for (int i = 0; i < 2; ++i)
+        out[i] = v[5 + i] == Py_None ? empty(shape, type, slots) : THPVariable_Unpack(v[5 + i]);
+    done(f_cache_read(slots.data_ptr<int64_t>(), (int)shape[0], &L, s.codes.data_ptr(), s.scales.data_ptr<float>(),
+                      out[0].data_ptr(), out[1].data_ptr(), number, stream),
          "mpq_cache_read");
     PyObject *k = v[5] == Py_None ? THPVariable_Wrap(out[0]) : same(v[5]);
     PyObject *w = k ? (v[6] == Py_None ? THPVariable_Wrap(out[1]) : same(v[6])) : nullptr;
@@ -286,7 +315,8 @@ PyObject *cache_read(PyObject *const *v)      // slots, layout, codes, scales, d
 // Q, table, lens, layout, codes, scales, scale, window, O, lse, workspace, stream
 PyObject *cache_attention(PyObject *const *v)
 {
-    const at::Tensor &Q = tensor(v[0], "Q"), &table = dense(v[1], "table", at::kInt);
+    Call call;
+    const at::Tensor &Q = call.tensor(v[0], "Q"), &table = dense(call, v[1], "table", at::kInt);
     const mpq_kv_cache &L = layout<mpq_kv_cache>(v[3], "layout");
     if (table.dim() != 2) refuse(PyExc_ValueError, "%s must be [B][columns]", "table");
     const long long B = table.size(0), cols = table.size(1);
@@ -299,29 +329,25 @@ PyObject *cache_attention(PyObject *const *v)
         refuse(PyExc_ValueError, "%s must have consecutive heads", "Q");
     if (B > INT32_MAX || cols > INT32_MAX || q_heads > INT32_MAX)
         refuse(PyExc_ValueError, "%s is too large", "table or Q");
-    const at::Tensor &lens = dense(v[2], "lens", at::kInt, {B});
-    const Storage s(L, v[4], v[5]);
+    const at::Tensor &lens = dense(call, v[2], "lens", at::kInt, {B});
+    const Storage s(call, L, v[4], v[5]);
     const int type = type_of(Q.scalar_type(), "Q");
     const bool own = v[8] == Py_None;
-    const at::Tensor O = own ? empty(Q.sizes(), Q.scalar_type(), Q)
-                             : dense(v[8], "O", Q.scalar_type(), Q.sizes());
-    float *const lse = v[9] == Py_None ? nullptr
-                                       : dense(v[9], "lse", at::kFloat, {B, q_heads}).data_ptr<float>();
-    void *ws = nullptr;
-    size_t ws_bytes = 0;
-    if (v[10] != Py_None) {
-        const at::Tensor &w = dense(v[10], "workspace", at::kByte);
-        ws = w.data_ptr();
-        ws_bytes = (size_t)w.numel();
-    }
+    if (!own) dense(call, v[8], "O", Q.scalar_type(), Q.sizes());
+    const at::Tensor *const lse = v[9] == Py_None ? nullptr : &dense(call, v[9], "lse", at::kFloat, {B, q_heads});
+    const at::Tensor *const ws = v[10] == Py_None ? nullptr : &dense(call, v[10], "workspace", at::kByte);
     double scale = 1.0 / std::sqrt((double)L.dim);
     if (v[6] != Py_None) {
         scale = PyFloat_AsDouble(v[6]);
         if (scale == -1.0 && PyErr_Occurred()) throw Refused();
     }
-    done(f_cache_attention(Q.data_ptr(), type, Q.stride(0), (int)B, (int)q_heads, &L, s.codes, s.scales,
-                           table.data_ptr<int>(), (int)cols, lens.data_ptr<int>(), (float)scale,
-                           integer32(v[7], "window"), O.data_ptr(), lse, ws, ws_bytes, stream_arg(v[11])),
+    const int window = integer32(v[7], "window");
+    void *const stream = call.stream(v[11]);
+    const at::Tensor O = own ? empty(Q.sizes(), Q.scalar_type(), Q) : THPVariable_Unpack(v[8]);
+    done(f_cache_attention(Q.data_ptr(), type, Q.stride(0), (int)B, (int)q_heads, &L, s.codes.data_ptr(),
+                           s.scales.data_ptr<float>(), table.data_ptr<int>(), (int)cols, lens.data_ptr<int>(),
+                           (float)scale, window, O.data_ptr(), lse ? lse->data_ptr<float>() : nullptr,
+                           ws ? ws->data_ptr() : nullptr, ws ? (size_t)ws->numel() : 0, stream),
          "mpq_cache_attention");
     return own ? THPVariable_Wrap(O) : same(v[8]);
 }
