@@ -463,7 +463,9 @@ def mpq_center_weights(W, mode: int = MPQ_CENTER_PER_CHANNEL, center=None, Wc=No
 # ---------------------------------------------------------------------------------------------
 # Serving in few bits.  A decode step makes these calls one after another with little work in each, so
 # their tensors are checked and their outputs allocated by a native extension (csrc/bind/), which calls
-# the loaded library by address.
+# the loaded library by address.  All tensors of a call lie on the current device.  With a stream of its own a
+# call runs on that stream, its outputs are allocated there, and the caller orders it after what writes its
+# inputs and keeps them until it is done, as for any work on a side stream.
 
 
 class _Unloaded:

@@ -9,6 +9,7 @@
 #include <ATen/core/Tensor.h>
 #include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAFunctions.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -51,7 +52,7 @@ const char *dtype_name(at::ScalarType t)
 }
 
 // What the tensors of one call have in common: they lie on one device, which is the current one when the
-// call is made (stream).
+// call is made (stream), and those that it makes belong to the stream it runs on.
 class Call {
 public:
     const at::Tensor &tensor(PyObject *o, const char *name)
@@ -67,23 +68,41 @@ public:
         return t;
     }
     // The stream argument's handle (None: the current stream's).
-    void *stream(PyObject *o) const
+    void *stream(PyObject *o)
     {
         const int current = c10::cuda::current_device();
         if (device_ != current)
             refuse(PyExc_ValueError, "the tensors lie on %s, the current device is %s",
                    ("cuda:" + std::to_string(device_)).c_str(), ("cuda:" + std::to_string(current)).c_str());
-        if (o == Py_None) return c10::cuda::getCurrentCUDAStream().stream();
+        cudaStream_t const here = c10::cuda::getCurrentCUDAStream().stream();
+        if (o == Py_None) return here;
         PyObject *h = PyObject_GetAttrString(o, "cuda_stream");
         if (!h) throw Refused();
         void *s = PyLong_AsVoidPtr(h);
         Py_DECREF(h);
         if (PyErr_Occurred()) throw Refused();
+        stream_ = static_cast<cudaStream_t>(s);
+        elsewhere_ = stream_ != here;
         return s;
+    }
+    // An output, after stream: in memory of that stream (a block of the current stream's may still be in use
+    // there), not given out again before what the current stream has been asked by then is done with it either.
+    at::Tensor empty(at::IntArrayRef shape, at::ScalarType type) const
+    {
+        const c10::Device device(c10::kCUDA, (c10::DeviceIndex)device_);
+        if (!elsewhere_) return at::Tensor(at::detail::empty_cuda(shape, type, device, std::nullopt));
+        const c10::cuda::CUDAStream here = c10::cuda::getCurrentCUDAStream();
+        const c10::cuda::CUDAStreamGuard guard(
+            c10::cuda::getStreamFromExternal(stream_, (c10::DeviceIndex)device_));
+        at::Tensor t(at::detail::empty_cuda(shape, type, device, std::nullopt));
+        t.record_stream(here);
+        return t;
     }
 
 private:
     int device_ = -1;
+    cudaStream_t stream_ = nullptr;      // where it is not the current one
+    bool elsewhere_ = false;
 };
 
 std::string text(at::IntArrayRef s)
@@ -179,11 +198,6 @@ const at::Tensor &packed(Call &call, PyObject *o, const char *name, const mpq_mx
     return t;
 }
 
-at::Tensor empty(at::IntArrayRef shape, at::ScalarType type, const at::Tensor &like)
-{
-    return at::Tensor(at::detail::empty_cuda(shape, type, like.device(), std::nullopt));
-}
-
 void done(mpq_status st, const char *name)
 {
     if (st == MPQ_OK) return;
@@ -211,7 +225,7 @@ PyObject *mx_quantize(PyObject *const *v)     // X, layout, packed, stream
     const bool own = v[2] == Py_None;
     if (!own) packed(call, v[2], "packed", L);
     void *const stream = call.stream(v[3]);
-    const at::Tensor out = own ? empty({(long long)L.bytes}, at::kByte, X) : THPVariable_Unpack(v[2]);
+    const at::Tensor out = own ? call.empty({(long long)L.bytes}, at::kByte) : THPVariable_Unpack(v[2]);
     done(f_mx_quantize(X.data_ptr(), type, ld, &L, out.data_ptr(), stream), "mpq_mx_quantize");
     return own ? THPVariable_Wrap(out) : same(v[2]);
 }
@@ -224,7 +238,7 @@ PyObject *mx_dequantize(PyObject *const *v)   // packed, layout, dtype, Y, strea
     const bool own = v[3] == Py_None;
     if (!own) call.tensor(v[3], "Y");
     void *const stream = call.stream(v[4]);
-    const at::Tensor Y = own ? empty({L.rows, L.d}, dtype_arg(v[2]), p) : THPVariable_Unpack(v[3]);
+    const at::Tensor Y = own ? call.empty({L.rows, L.d}, dtype_arg(v[2])) : THPVariable_Unpack(v[3]);
     const long long ld = rows_of(Y, "Y", L.rows, L.d);
     done(f_mx_dequantize(p.data_ptr(), &L, Y.data_ptr(), type_of(Y.scalar_type(), "Y"), ld, stream),
          "mpq_mx_dequantize");
@@ -241,7 +255,7 @@ PyObject *mx_linear(PyObject *const *v)       // X, x_layout, W, w_layout, bias,
     const bool own = v[6] == Py_None;
     if (!own) call.tensor(v[6], "Y");
     void *const stream = call.stream(v[7]);
-    const at::Tensor Y = own ? empty({xl.rows, wl.rows}, dtype_arg(v[5]), X) : THPVariable_Unpack(v[6]);
+    const at::Tensor Y = own ? call.empty({xl.rows, wl.rows}, dtype_arg(v[5])) : THPVariable_Unpack(v[6]);
     const long long ld = rows_of(Y, "Y", xl.rows, wl.rows);
     done(f_mx_linear(&xl, X.data_ptr(), &wl, W.data_ptr(), bias ? bias->data_ptr<float>() : nullptr, Y.data_ptr(),
                      type_of(Y.scalar_type(), "Y"), ld, stream),
@@ -300,7 +314,7 @@ PyObject *cache_read(PyObject *const *v)      // slots, layout, codes, scales, d
     void *const stream = call.stream(v[7]);
     at::Tensor out[2];
     for (int i = 0; i < 2; ++i)
-        out[i] = v[5 + i] == Py_None ? empty(shape, type, slots) : THPVariable_Unpack(v[5 + i]);
+        out[i] = v[5 + i] == Py_None ? call.empty(shape, type) : THPVariable_Unpack(v[5 + i]);
     done(f_cache_read(slots.data_ptr<int64_t>(), (int)shape[0], &L, s.codes.data_ptr(), s.scales.data_ptr<float>(),
                       out[0].data_ptr(), out[1].data_ptr(), number, stream),
          "mpq_cache_read");
@@ -343,7 +357,7 @@ PyObject *cache_attention(PyObject *const *v)
     }
     const int window = integer32(v[7], "window");
     void *const stream = call.stream(v[11]);
-    const at::Tensor O = own ? empty(Q.sizes(), Q.scalar_type(), Q) : THPVariable_Unpack(v[8]);
+    const at::Tensor O = own ? call.empty(Q.sizes(), Q.scalar_type()) : THPVariable_Unpack(v[8]);
     done(f_cache_attention(Q.data_ptr(), type, Q.stride(0), (int)B, (int)q_heads, &L, s.codes.data_ptr(),
                            s.scales.data_ptr<float>(), table.data_ptr<int>(), (int)cols, lens.data_ptr<int>(),
                            (float)scale, window, O.data_ptr(), lse ? lse->data_ptr<float>() : nullptr,

@@ -1,0 +1,52 @@
+"""The few-bit serving calls on a stream that is not the current one: what a call allocates belongs to the
+stream that writes it."""
+import pytest
+import torch
+
+from paper_2002_09049_gb300 import binding
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+
+
+def owner(t):
+    """The stream that the allocator keeps t's memory for."""
+    for seg in torch.cuda.memory_snapshot():
+        if seg["address"] <= t.data_ptr() < seg["address"] + seg["total_size"]:
+            return seg["stream"]
+    raise AssertionError("not the allocator's memory")
+
+
+def test_outputs_belong_to_the_stream_given(gpu):
+    lay = binding.mpq_mx_layout(40, 256)
+    kv = binding.mpq_cache_layout(3, 16, 2, 64, 8)
+    codes, scales = binding.mpq_cache_empty(kv, DEV)
+    x = torch.randn(40, 256, device=DEV)
+    k = torch.randn(40, 2, 64, device=DEV)
+    slots = torch.arange(40, device=DEV)
+    binding.mpq_cache_write(k, k, slots, kv, codes, scales)
+    q = torch.randn(1, 4, 64, device=DEV).half()
+    table = torch.arange(3, dtype=torch.int32, device=DEV).view(1, 3)
+    lens = torch.tensor([40], dtype=torch.int32, device=DEV)
+    packed = binding.mpq_mx_quantize(x, lay)
+    side = torch.cuda.Stream()
+
+    def calls(stream):
+        return [binding.mpq_mx_quantize(x, lay, stream=stream),
+                binding.mpq_mx_dequantize(packed, lay, stream=stream),
+                binding.mpq_mx_linear(packed, lay, packed, lay, stream=stream),
+                *binding.mpq_cache_read(slots, kv, codes, scales, stream=stream),
+                binding.mpq_cache_attention(q, table, lens, kv, codes, scales, stream=stream)]
+
+    want = calls(None)
+    torch.cuda.synchronize()
+    got = calls(side)
+    side.synchronize()
+    assert [owner(t) for t in got] == [side.cuda_stream] * len(got)
+    with torch.cuda.stream(side):
+        inside = calls(None) + calls(torch.cuda.default_stream())
+    torch.cuda.synchronize()
+    assert [owner(t) for t in inside] == [side.cuda_stream] * len(got) + [0] * len(got)
+    for a, b in zip(got + inside, want * 3):
+        assert torch.equal(a, b)
