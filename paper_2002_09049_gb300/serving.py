@@ -10,9 +10,20 @@ replay (``capture``).  ``prompt`` enters whole prompts into the cache, ``tokens`
 """
 from __future__ import annotations
 
+import contextlib
+
 import torch
 
 from . import binding
+
+
+def _on(stream, device):
+    """Makes `stream` the current one (None: it stays): what is allocated meanwhile belongs to it."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if not hasattr(stream, "wait_stream"):           # a handle that is not torch's
+        stream = torch.cuda.ExternalStream(stream.cuda_stream, device)
+    return torch.cuda.stream(stream)
 
 
 class FewBitAttention:
@@ -60,9 +71,10 @@ class FewBitAttention:
 
     def prompt(self, x, slots, stream=None):
         """Enters tokens x [T][d] into the cache at slots [T] (int64).  Its buffers are allocated for the
-        call, on the current stream."""
-        _, k, v = self._project(x, self._make_buffers(x.shape[0]), stream)
-        binding.mpq_cache_write(k, v, slots, self.cache, self.codes, self.scales, stream=stream)
+        call, on the stream that it runs on."""
+        with _on(stream, self.device):
+            _, k, v = self._project(x, self._make_buffers(x.shape[0]), None)
+            binding.mpq_cache_write(k, v, slots, self.cache, self.codes, self.scales)
 
     def step(self, x, slots, table, lens, window: int = 0, stream=None):
         """One new token of every sequence: x [B][d], its slot in the cache (int64 [B]), the

@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from paper_2002_09049_gb300 import binding
+from paper_2002_09049_gb300.serving import FewBitAttention
 
 pytestmark = pytest.mark.gpu
 
@@ -50,3 +51,32 @@ def test_outputs_belong_to_the_stream_given(gpu):
     assert [owner(t) for t in inside] == [side.cuda_stream] * len(got) + [0] * len(got)
     for a, b in zip(got + inside, want * 3):
         assert torch.equal(a, b)
+
+
+def block(bits=8):
+    gen = torch.Generator(device=DEV).manual_seed(5)
+    w = lambda r, c: torch.randn(r, c, generator=gen, device=DEV) / c ** 0.5
+    return FewBitAttention(w(12 * 64, 512), w(512, 8 * 64), 8, 2, 64, pages=20, page=16, bits=bits), gen
+
+
+def test_prompt_on_a_side_stream(gpu):
+    """The current stream allocates and writes while the prompt has not yet begun on its own: the cache holds
+    what it holds when nothing else runs."""
+    blk, gen = block()
+    x = torch.randn(300, 512, generator=gen, device=DEV).to(blk.dtype)
+    slots = torch.arange(300, device=DEV)
+    blk.prompt(x, slots)
+    want = blk.tokens(slots)
+    blk.codes.zero_()
+    blk.scales.zero_()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(50_000_000)
+    blk.prompt(x, slots, stream=side)
+    spoil = [torch.full((n,), 0x7F, dtype=torch.uint8, device=DEV)
+             for n in (300 * 512, 300 * 768 * 2, 300 * 512 * 2) for _ in range(8)]
+    torch.cuda.synchronize()
+    for a, b in zip(blk.tokens(slots), want):
+        assert torch.equal(a, b)
+    del spoil
