@@ -1,8 +1,8 @@
 """An attention block served in few bits: the projections as microscaled 4-bit layers, keys and values in a
 quantized paged cache, and the attention of new tokens over it.
 
-``FewBitAttention`` owns the packed weights, the cache and the buffers of a decode step, so that a step
-allocates nothing: quantise the inputs, project (queries, keys and values in one product), write the
+``FewBitAttention`` owns the packed weights, the cache and the buffers of a decode step (kept for every batch
+size and stream that it has met), so that a step allocates nothing: quantise the inputs, project (queries, keys and values in one product), write the
 new tokens' keys and values, attend, quantise, project back -- six calls on one stream, or one graph
 replay (``capture``).  ``prompt`` enters whole prompts into the cache, ``tokens`` reads slots back.
 
@@ -43,9 +43,7 @@ class FewBitAttention:
         self.w_out = binding.mpq_mx_quantize(w_out, self.out_layout)
         self.cache = binding.mpq_cache_layout(pages, page, heads, dim, bits)
         self.codes, self.scales = binding.mpq_cache_empty(self.cache, self.device)
-        self.workspace = torch.zeros(binding.MPQ_CACHE_WORKSPACE, dtype=torch.uint8,
-                                     device=self.device)
-        self._buffers = {}
+        self._buffers, self._workspaces = {}, {}
 
     def _make_buffers(self, B):
         """What a step of B tokens writes on its way."""
@@ -55,17 +53,25 @@ class FewBitAttention:
         return dict(x=x, o=o, x_packed=packed[0], o_packed=packed[1], qkv=mk(B, self.qkv_layout.rows),
                     attended=mk(B, self.q_heads, self.dim), y=mk(B, self.out_layout.rows))
 
-    def _step_buffers(self, B):
-        """Those of steps, kept by B."""
-        if B not in self._buffers:
-            self._buffers[B] = self._make_buffers(B)
-        return self._buffers[B]
+    def _make_workspace(self):
+        return torch.zeros(binding.MPQ_CACHE_WORKSPACE, dtype=torch.uint8, device=self.device)
 
-    def _project(self, x, b, stream):
+    def _step_buffers(self, B):
+        """The buffers of steps of B tokens on the current stream and its workspace, kept by stream (steps of
+        one stream follow one another; those of two may overlap).  A graph being captured gets its own."""
+        if torch.cuda.is_current_stream_capturing():
+            return self._make_buffers(B), self._make_workspace()
+        stream = torch._C._cuda_getCurrentRawStream(self.device.index)
+        if stream not in self._workspaces:
+            self._workspaces[stream] = self._make_workspace()
+        if (B, stream) not in self._buffers:
+            self._buffers[B, stream] = self._make_buffers(B)
+        return self._buffers[B, stream], self._workspaces[stream]
+
+    def _project(self, x, b):
         """Queries, keys and values [B][heads of each][dim] of inputs x [B][d] (views of one buffer)."""
-        binding.mpq_mx_quantize(x, b["x"], b["x_packed"], stream=stream)
-        binding.mpq_mx_linear(b["x_packed"], b["x"], self.w_qkv, self.qkv_layout, Y=b["qkv"],
-                              stream=stream)
+        binding.mpq_mx_quantize(x, b["x"], b["x_packed"])
+        binding.mpq_mx_linear(b["x_packed"], b["x"], self.w_qkv, self.qkv_layout, Y=b["qkv"])
         rows = b["qkv"].view(x.shape[0], self.q_heads + 2 * self.heads, self.dim)
         return rows.split((self.q_heads, self.heads, self.heads), 1)
 
@@ -73,23 +79,23 @@ class FewBitAttention:
         """Enters tokens x [T][d] into the cache at slots [T] (int64).  Its buffers are allocated for the
         call, on the stream that it runs on."""
         with _on(stream, self.device):
-            _, k, v = self._project(x, self._make_buffers(x.shape[0]), None)
+            _, k, v = self._project(x, self._make_buffers(x.shape[0]))
             binding.mpq_cache_write(k, v, slots, self.cache, self.codes, self.scales)
 
     def step(self, x, slots, table, lens, window: int = 0, stream=None):
         """One new token of every sequence: x [B][d], its slot in the cache (int64 [B]), the
         sequences' pages (int32 [B][columns]) and lengths with the new token (int32 [B]).  Returns the
-        block's outputs [B][d] (a buffer that the next step of B tokens overwrites)."""
-        b = self._step_buffers(x.shape[0])
-        q, k, v = self._project(x, b, stream)
-        binding.mpq_cache_write(k, v, slots, self.cache, self.codes, self.scales, stream=stream)
+        block's outputs [B][d] (a buffer that the next step of B tokens on the same stream overwrites)."""
+        with _on(stream, self.device):
+            return self._step(x, slots, table, lens, window, *self._step_buffers(x.shape[0]))
+
+    def _step(self, x, slots, table, lens, window, b, workspace):
+        q, k, v = self._project(x, b)
+        binding.mpq_cache_write(k, v, slots, self.cache, self.codes, self.scales)
         binding.mpq_cache_attention(q, table, lens, self.cache, self.codes, self.scales,
-                                    window=window, O=b["attended"], workspace=self.workspace,
-                                    stream=stream)
-        binding.mpq_mx_quantize(b["attended"].view(x.shape[0], -1), b["o"], b["o_packed"],
-                                stream=stream)
-        return binding.mpq_mx_linear(b["o_packed"], b["o"], self.w_out, self.out_layout, Y=b["y"],
-                                     stream=stream)
+                                    window=window, O=b["attended"], workspace=workspace)
+        binding.mpq_mx_quantize(b["attended"].view(x.shape[0], -1), b["o"], b["o_packed"])
+        return binding.mpq_mx_linear(b["o_packed"], b["o"], self.w_out, self.out_layout, Y=b["y"])
 
     def tokens(self, slots, stream=None):
         """The keys and values [T][heads][dim] that the cache holds at slots [T]."""

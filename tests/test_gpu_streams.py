@@ -80,3 +80,35 @@ def test_prompt_on_a_side_stream(gpu):
     for a, b in zip(blk.tokens(slots), want):
         assert torch.equal(a, b)
     del spoil
+
+
+def batch(blk, gen, first, lens):
+    """Sequences of lens cached tokens on pages from `first` on: the next step's arguments."""
+    table = torch.full((len(lens), 4), -1, dtype=torch.int32, device=DEV)
+    slots = []
+    for b, n in enumerate(lens):
+        need = -(-n // 16)
+        table[b, :need] = torch.arange(first, first + need, device=DEV)
+        x = torch.randn(n, blk.d, generator=gen, device=DEV).to(blk.dtype)
+        blk.prompt(x, torch.arange(n, device=DEV) + first * 16)
+        slots.append(first * 16 + n - 1)
+        first += need
+    x = torch.randn(len(lens), blk.d, generator=gen, device=DEV).to(blk.dtype)
+    return (x, torch.tensor(slots, device=DEV), table, torch.tensor(lens, dtype=torch.int32, device=DEV))
+
+
+def test_overlapping_steps(gpu):
+    """Steps of two streams at once, of the same number of tokens: each as alone."""
+    blk, gen = block()
+    one, two = batch(blk, gen, 0, [40, 3, 60]), batch(blk, gen, 8, [17, 64, 33])
+    want = blk.step(*one).clone(), blk.step(*two).clone()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(30):
+        y = blk.step(*one).clone()
+        z = blk.step(*two, stream=side)
+        with torch.cuda.stream(side):
+            got.append((y, z.clone()))
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, want[0]) and torch.equal(z, want[1]) for y, z in got)
