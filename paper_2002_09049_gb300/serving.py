@@ -104,7 +104,8 @@ class FewBitAttention:
 
     def capture(self, B: int, columns: int, window: int = 0):
         """A CUDA graph of one step for B sequences of up to `columns` pages: its inputs are the
-        returned object's x, slots, table and lens, filled before replay()."""
+        returned object's x, slots, table and lens, filled before replay().  It has buffers and a workspace
+        of its own and keeps the block; one graph's replays follow one another."""
         return CapturedStep(self, B, columns, window)
 
 
@@ -115,15 +116,17 @@ class CapturedStep:
         self.slots = mk((B,), torch.int64).fill_(-1)      # no slot, no tokens: the warm-up writes nothing
         self.table = mk((B, columns), torch.int32)
         self.lens = mk((B,), torch.int32)
-        args = (self.x, self.slots, self.table, self.lens, window)
+        self.block = block                # the graph reads its weights and its cache
+        self._buffers, self._workspace = block._make_buffers(B), block._make_workspace()
+        args = (self.x, self.slots, self.table, self.lens, window, self._buffers, self._workspace)
         side = torch.cuda.Stream(block.device)
         side.wait_stream(torch.cuda.current_stream(block.device))
         with torch.cuda.stream(side):
-            block.step(*args)
+            block._step(*args)
         torch.cuda.current_stream(block.device).wait_stream(side)
         self.graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(self.graph):
-            self.y = block.step(*args)
+            self.y = block._step(*args)
 
     def replay(self):
         """Enqueues the step on the current stream; returns its outputs' buffer."""

@@ -1,5 +1,8 @@
 """The few-bit serving calls on a stream that is not the current one: what a call allocates belongs to the
 stream that writes it."""
+import gc
+import weakref
+
 import pytest
 import torch
 
@@ -112,3 +115,46 @@ def test_overlapping_steps(gpu):
             got.append((y, z.clone()))
     torch.cuda.synchronize()
     assert all(torch.equal(y, want[0]) and torch.equal(z, want[1]) for y, z in got)
+
+
+def replayed(cap, args):
+    for name, t in zip(("x", "slots", "table", "lens"), args):
+        getattr(cap, name).copy_(t)
+    return cap.replay()
+
+
+def test_captured_step_keeps_its_block(gpu):
+    blk, gen = block()
+    args = batch(blk, gen, 0, [40, 3, 60])
+    want = blk.step(*args).clone()
+    cap = blk.capture(3, 4)
+    gone = weakref.ref(blk)
+    del blk
+    gc.collect()
+    assert gone() is not None            # (else the replay would read memory that is free)
+    torch.cuda.empty_cache()
+    spoil = torch.full((1 << 26,), 0x7F, dtype=torch.uint8, device=DEV)
+    assert torch.equal(replayed(cap, args), want)
+    del spoil
+
+
+def test_captured_steps_share_nothing(gpu):
+    """Two graphs of one size, replayed at once on two streams, and steps between them."""
+    blk, gen = block()
+    one, two, three = (batch(blk, gen, f, n) for f, n in ((0, [40, 3]), (6, [17, 60]), (14, [33, 20])))
+    want = [blk.step(*a).clone() for a in (one, two, three)]
+    caps = [blk.capture(2, 4), blk.capture(2, 4)]
+    outs = [c.y.data_ptr() for c in caps] + [blk.step(*three).data_ptr()]
+    assert len(set(outs)) == 3
+    for c, a in zip(caps, (one, two)):
+        replayed(c, a)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(30):
+        caps[0].replay()
+        with torch.cuda.stream(side):
+            caps[1].replay()
+        y = blk.step(*three)
+    torch.cuda.synchronize()
+    for got, ref in zip((caps[0].y, caps[1].y, y), want):
+        assert torch.equal(got, ref)
