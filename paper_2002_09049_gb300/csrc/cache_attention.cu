@@ -302,6 +302,7 @@ cache_attention_kernel(const AttnArgs a, WaitCtl wc, const __grid_constant__ CUt
     extern __shared__ unsigned char raw[];
     __shared__ long long sh_pre[THREADS];        // stages before each thread's sequences
     __shared__ long long sh_warp[W];
+    __shared__ int sh_some[W];
     __shared__ Part sh_part[2 * W];
     __shared__ int sh_open[2], sh_c0[2], sh_c1[2], sh_last[2];
     __shared__ __align__(16) float sh_slice[W][D];
@@ -334,7 +335,7 @@ cache_attention_kernel(const AttnArgs a, WaitCtl wc, const __grid_constant__ CUt
     Span lane_span = {0, 0};                     // (few) of sequence `lane`
     unsigned lane_pre = 0, lane_all = 0;         // (few) weight of a unit, before it and up to its end
     long long total;
-    int some;                                    // sequences (threads' of them) that have any
+    int some;                                    // sequences that have any
     if (few) {
         if (lane < a.B) lane_span = span_of(a, lane);
         const unsigned mine = (unsigned)weight(lane_span.stages());      // (32 of at most 2^26 + 2)
@@ -351,27 +352,38 @@ cache_attention_kernel(const AttnArgs a, WaitCtl wc, const __grid_constant__ CUt
     } else {
         const int b_lo = min(tid * per, a.B), b_hi = min(b_lo + per, a.B);
         long long pre = 0;
-        for (int b = b_lo; b < b_hi; ++b) pre += (long long)weight(span_of(a, b).stages()) * units;
+        int live = 0;
+        for (int b = b_lo; b < b_hi; ++b) {
+            const int n = span_of(a, b).stages();
+            pre += (long long)weight(n) * units;
+            live += n > 0;
+        }
         const long long mine = pre;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const long long v = __shfl_up_sync(0xffffffffu, pre, o);
             if (lane >= o) pre += v;
         }
-        if (lane == 31) sh_warp[warp] = pre;
-        some = __syncthreads_count(mine > 0);
+        live = __reduce_add_sync(0xffffffffu, live);
+        if (lane == 31) {
+            sh_warp[warp] = pre;
+            sh_some[warp] = live;
+        }
+        __syncthreads();
         total = 0;
+        some = 0;
 #pragma unroll
         for (int w = 0; w < W; ++w) {
             if (w < warp) pre += sh_warp[w];
             total += sh_warp[w];
+            some += sh_some[w];
         }
         sh_pre[tid] = pre - mine;
         __syncthreads();
     }
     // sequences with nothing to attend to: a warp each
     auto empty_rows = [&]() {
-        if (per == 1 && some == a.B) return;
+        if (some == a.B) return;
         for (long long b = blockIdx.x + (long long)warp * gridDim.x; b < a.B;
              b += (long long)W * gridDim.x) {
             if (span_of(a, (int)b).stages() > 0) continue;
@@ -387,7 +399,7 @@ cache_attention_kernel(const AttnArgs a, WaitCtl wc, const __grid_constant__ CUt
     // joined (96 x 64 tokens 11.3 us, 12.9 in ranges of two stages; 12 stages a row are too many: a case of 13 us
     // took 18).
     const long long rows = (long long)some * units;
-    const bool by_row = per == 1 && rows <= gridDim.x && total <= rows * (W * A_ROW);
+    const bool by_row = rows <= gridDim.x && total <= rows * (W * A_ROW);
     const bool whole = rows > gridDim.x && rows <= (long long)gridDim.x * W && total <= rows * A_WHOLE;
     const int workers = by_row  ? (int)(rows * W)
                         : whole ? (int)rows
