@@ -90,12 +90,13 @@ def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False,
     lib = CHECKED_LIB if checked else LIB
     obj_dir = os.path.join(BUILD, "checked") if checked else BUILD
     with _lock:
-        exe = nvcc()
         stale = force or not up_to_date(lib)
         bind = force or not _binding_up_to_date()
+        if not (stale or bind):
+            return lib
+        exe = nvcc()
         if not stale:
-            if bind:
-                _build_binding(exe)
+            _build_binding(exe)
             return lib
         os.makedirs(obj_dir, exist_ok=True)
         extra = ["-Xptxas", "-v"] if ptxas_info else []
