@@ -2,7 +2,9 @@
 
 Translation units compile in parallel, then link into one shared library with the CUDA runtime
 linked statically.  The native marshalling of the serving calls (csrc/bind/) is a Python extension of its
-own, _serve_binding.so, compiled against the torch that imports it.  Run ``python -m paper_2002_09049_gb300._build`` or call ``build()``.
+own, _serve_binding.so, compiled (by the host compiler that nvcc uses too) against the torch that imports it,
+and again when that torch or the Python changes.  Run ``python -m paper_2002_09049_gb300._build`` or call
+``build()``.
 ``build(checked=True)`` (``--checked``) builds the checked library, libmpq_checked.so: the same
 sources with -DMPQ_CHECK_BOUNDS, whose kernels count and skip out-of-range accesses.
 """
@@ -13,6 +15,7 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 import threading
 from concurrent.futures import ThreadPoolExecutor
 
@@ -22,6 +25,7 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libmpq.so")
 CHECKED_LIB = os.path.join(PKG, "libmpq_checked.so")
 BINDING = os.path.join(PKG, "_serve_binding.so")
+BINDING_FOR = os.path.join(BUILD, "serve_binding.for")   # what it was compiled against
 ROOT = os.path.dirname(PKG)
 INCLUDE = os.path.join(ROOT, "include")
 
@@ -53,17 +57,31 @@ def up_to_date(lib: str = LIB) -> bool:
     return all(os.path.getmtime(p) <= t for p in _deps())
 
 
+def _binding_against() -> str:
+    """What the extension depends on besides its sources: this Python's and this torch's C++ interfaces."""
+    import torch
+    return "\n".join((sysconfig.get_config_var("SOABI") or sys.version, torch.__version__,
+                      str(int(torch._C._GLIBCXX_USE_CXX11_ABI))))
+
+
+def binding_fits() -> bool:
+    """Whether the extension was compiled against this Python and this torch."""
+    try:
+        with open(BINDING_FOR) as f:
+            return f.read() == _binding_against()
+    except FileNotFoundError:
+        return False
+
+
 def _binding_up_to_date() -> bool:
     src = os.path.join(CSRC, "bind", "serve_binding.cpp")
-    return os.path.exists(BINDING) and all(
+    return os.path.exists(BINDING) and binding_fits() and all(
         os.path.getmtime(p) <= os.path.getmtime(BINDING)
         for p in (src, os.path.join(INCLUDE, "mpq.h")))
 
 
 def _build_binding(exe: str) -> None:
     """Compile csrc/bind/serve_binding.cpp -> _serve_binding.so with the host compiler."""
-    import sysconfig
-
     import torch
     home = os.path.dirname(torch.__file__)
     inc = [os.path.join(home, "include"),
@@ -81,6 +99,11 @@ def _build_binding(exe: str) -> None:
     if res.returncode != 0:
         raise RuntimeError(f"compiling the serving calls' binding failed:\n{res.stdout}\n{res.stderr}")
     os.replace(tmp, BINDING)
+    os.makedirs(BUILD, exist_ok=True)
+    tmp = BINDING_FOR + f".{os.getpid()}.tmp"
+    with open(tmp, "w") as f:
+        f.write(_binding_against())
+    os.replace(tmp, BINDING_FOR)
 
 
 def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False,

@@ -475,6 +475,9 @@ class _Unloaded:
         global _native
         lib = load()
         try:
+            # (it might load all the same, and crash; one that came without its record is tried)
+            if os.path.exists(_build.BINDING_FOR) and not _build.binding_fits():
+                raise ImportError("compiled against another Python or torch")
             from . import _serve_binding
         except ImportError as e:
             raise RuntimeError(f"{_build.BINDING} is missing or was built for another Python or torch: "
