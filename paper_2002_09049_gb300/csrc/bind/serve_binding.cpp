@@ -289,12 +289,18 @@ PyObject *cache_write(PyObject *const *v)     // K, V, slots, layout, codes, sca
     const long long T = slots.numel();
     need_shape(K, "K", {T, L.heads, L.dim});
     need_shape(V, "V", {T, L.heads, L.dim});
-    if (K.scalar_type() != V.scalar_type() || K.strides() != V.strides())
-        refuse(PyExc_ValueError, "K and V must have one type and the same strides%s", "");
-    if (K.stride(2) != 1) refuse(PyExc_ValueError, "%s must have contiguous rows", "K and V");
+    // (a dimension of one entry has no stride to speak of)
+    long long ld[2];
+    bool same_rows = K.scalar_type() == V.scalar_type();
+    for (int i = 0; i < 2; ++i) {
+        ld[i] = K.size(i) > 1 ? K.stride(i) : 0;
+        same_rows = same_rows && ld[i] == (V.size(i) > 1 ? V.stride(i) : 0);
+    }
+    if (!same_rows) refuse(PyExc_ValueError, "K and V must have one type and the same strides%s", "");
+    if (K.stride(2) != 1 || V.stride(2) != 1) refuse(PyExc_ValueError, "%s must have contiguous rows", "K and V");
     const Storage s(call, L, v[4], v[5]);
     void *const stream = call.stream(v[6]);
-    done(f_cache_write(K.data_ptr(), V.data_ptr(), type_of(K.scalar_type(), "K"), K.stride(0), K.stride(1),
+    done(f_cache_write(K.data_ptr(), V.data_ptr(), type_of(K.scalar_type(), "K"), ld[0], ld[1],
                        (int)T, slots.data_ptr<int64_t>(), &L, s.codes.data_ptr(), s.scales.data_ptr<float>(), stream),
          "mpq_cache_write");
     Py_RETURN_NONE;
