@@ -389,6 +389,8 @@ mpq_status mpq_multipoint_linear(const int8_t *X, int T, const mpq_packed_layout
  * the linear layers (both operands), the key-value cache in 8 or 4 bits, and the attention of new
  * tokens over that cache.
  *
+ * Every pointer is aligned to its elements at least; one that is not is refused (MPQ_ERR_INVALID_ARG).
+ *
  * Element types of inputs and outputs, where an argument takes one.
  */
 #define MPQ_F32 0

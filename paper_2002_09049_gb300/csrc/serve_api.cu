@@ -41,7 +41,8 @@ static mpq_status check_cache(const mpq_kv_cache *L)
     return MPQ_OK;
 }
 
-static bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
+static bool on(const void *p, size_t bytes) { return (uintptr_t)p % bytes == 0; }
+static bool aligned16(const void *p) { return on(p, 16); }
 
 extern "C" mpq_status mpq_mx_layout(int rows, int d, mpq_mx_matrix *layout)
 {
@@ -67,6 +68,7 @@ extern "C" mpq_status mpq_mx_quantize(const void *X, int x_type, long long ldx,
     REQUIRE(ldx >= layout->d, MPQ_ERR_INVALID_ARG, "ldx = %lld must be >= d = %d", ldx, layout->d);
     if (layout->rows == 0) return MPQ_OK;
     REQUIRE(X && packed, MPQ_ERR_INVALID_ARG, "X and packed must be non-NULL");
+    REQUIRE(on(X, type_size(x_type)), MPQ_ERR_INVALID_ARG, "X must be aligned to its elements");
     REQUIRE(aligned16(packed), MPQ_ERR_INVALID_ARG, "packed must be 16-byte aligned");
     return launch_mx_quantize(X, x_type, ldx, layout, packed, (cudaStream_t)stream);
 }
@@ -82,6 +84,7 @@ extern "C" mpq_status mpq_mx_dequantize(const void *packed, const mpq_mx_matrix 
     REQUIRE(ldy >= layout->d, MPQ_ERR_INVALID_ARG, "ldy = %lld must be >= d = %d", ldy, layout->d);
     if (layout->rows == 0) return MPQ_OK;
     REQUIRE(packed && Y, MPQ_ERR_INVALID_ARG, "packed and Y must be non-NULL");
+    REQUIRE(on(Y, type_size(y_type)), MPQ_ERR_INVALID_ARG, "Y must be aligned to its elements");
     REQUIRE(aligned16(packed), MPQ_ERR_INVALID_ARG, "packed must be 16-byte aligned");
     return launch_mx_dequantize(packed, layout, Y, y_type, ldy, (cudaStream_t)stream);
 }
@@ -103,6 +106,8 @@ extern "C" mpq_status mpq_mx_linear(const mpq_mx_matrix *x_layout, const void *X
     if (x_layout->rows == 0 || w_layout->rows == 0) return MPQ_OK;
     REQUIRE(X && W && Y, MPQ_ERR_INVALID_ARG, "X, W and Y must be non-NULL");
     REQUIRE(aligned16(X) && aligned16(W), MPQ_ERR_INVALID_ARG, "X and W must be 16-byte aligned");
+    REQUIRE(on(bias, sizeof(float)) && on(Y, type_size(y_type)), MPQ_ERR_INVALID_ARG,
+            "bias and Y must be aligned to their elements");
     return launch_mx_linear(x_layout, X, w_layout, W, bias, Y, y_type, ldy, (cudaStream_t)stream);
 }
 
@@ -154,6 +159,9 @@ extern "C" mpq_status mpq_cache_write(const void *K, const void *V, int type, lo
     REQUIRE(K && V && slots && codes && scales, MPQ_ERR_INVALID_ARG,
             "K, V, slots, codes and scales must be non-NULL");
     REQUIRE(aligned16(codes), MPQ_ERR_INVALID_ARG, "codes must be 16-byte aligned");
+    REQUIRE(on(K, type_size(type)) && on(V, type_size(type)) && on(slots, sizeof(int64_t)) &&
+                on(scales, sizeof(float)),
+            MPQ_ERR_INVALID_ARG, "K, V, slots and scales must be aligned to their elements");
     return launch_cache_write(K, V, type, ld_token, ld_head, T, slots, layout, codes, scales,
                               (cudaStream_t)stream);
 }
@@ -172,6 +180,8 @@ extern "C" mpq_status mpq_cache_read(const int64_t *slots, int T, const mpq_kv_c
             "codes and scales must be non-NULL");
     REQUIRE(aligned16(codes) && aligned16(K) && aligned16(V), MPQ_ERR_INVALID_ARG,
             "codes, K and V must be 16-byte aligned");
+    REQUIRE(on(slots, sizeof(int64_t)) && on(scales, sizeof(float)), MPQ_ERR_INVALID_ARG,
+            "slots and scales must be aligned to their elements");
     return launch_cache_read(slots, T, layout, codes, scales, K, V, type, (cudaStream_t)stream);
 }
 
@@ -207,6 +217,8 @@ extern "C" mpq_status mpq_cache_attention(const void *Q, int type, long long q_s
             "codes and scales must be non-NULL");
     REQUIRE(aligned16(codes) && aligned16(scales) && aligned16(O) && aligned16(workspace),
             MPQ_ERR_INVALID_ARG, "codes, scales, O and workspace must be 16-byte aligned");
+    REQUIRE(on(Q, type_size(type)) && on(table, sizeof(int)) && on(lens, sizeof(int)) && on(lse, sizeof(float)),
+            MPQ_ERR_INVALID_ARG, "Q, table, lens and lse must be aligned to their elements");
     REQUIRE(!workspace || workspace_bytes >= MPQ_CACHE_WORKSPACE, MPQ_ERR_INVALID_ARG,
             "workspace of %zu bytes: %zu are needed", workspace_bytes, MPQ_CACHE_WORKSPACE);
     return launch_cache_attention(Q, type, q_stride, B, q_heads, layout, codes, scales, table,
