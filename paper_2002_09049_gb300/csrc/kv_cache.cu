@@ -14,8 +14,9 @@
 // there is one, so that a screen with an exact way out gains nothing).  One correctly rounded reciprocal r
 // a row, and Markstein's theorem (IBM J. Res. Dev. 34(1), 1990): a y within a unit in the last place of
 // x / s gives RN(x / s) as RN(y + r (x - s y)), the remainder exact by a fused multiply-add.  RN(x r) is
-// within 1.5 units, one such step brings it within one, the next is the quotient.  For elements and maxima
-// of 11 bits or fewer the first step gives it already (all of them tried: tests/test_cache_quotients.py).
+// within 1.5 units, so one step (its remainder may have a bit too many, and is rounded) brings it within one,
+// and the next is the quotient.  For elements and maxima of 11 bits or fewer the first step gives it already
+// (all of them tried, with every rounding: tests/test_cache_quotient_steps.py).
 // Rows whose scale is so small or large that r or a remainder could leave the normal range are divided.
 //
 // Memory-bound: an element's own bytes on one side, bits / 8 + 4 / dim bytes on the other; slots scatter
