@@ -198,8 +198,15 @@ const at::Tensor &packed(Call &call, PyObject *o, const char *name, const mpq_mx
     return t;
 }
 
-void done(mpq_status st, const char *name)
+// One call of the library, other Python threads running meanwhile (a launch waits while its stream's queue is
+// full, and what is ahead in the queue may need Python).
+template <typename F, typename... A>
+void run(const char *name, F f, A... args)
 {
+    mpq_status st;
+    Py_BEGIN_ALLOW_THREADS
+    st = f(args...);
+    Py_END_ALLOW_THREADS
     if (st == MPQ_OK) return;
     PyObject *r = PyObject_CallFunction(raise_status, "is", (int)st, name);
     Py_XDECREF(r);
@@ -226,7 +233,7 @@ PyObject *mx_quantize(PyObject *const *v)     // X, layout, packed, stream
     if (!own) packed(call, v[2], "packed", L);
     void *const stream = call.stream(v[3]);
     const at::Tensor out = own ? call.empty({(long long)L.bytes}, at::kByte) : THPVariable_Unpack(v[2]);
-    done(f_mx_quantize(X.data_ptr(), type, ld, &L, out.data_ptr(), stream), "mpq_mx_quantize");
+    run("mpq_mx_quantize", f_mx_quantize, X.data_ptr(), type, ld, &L, out.data_ptr(), stream);
     return own ? THPVariable_Wrap(out) : same(v[2]);
 }
 
@@ -240,8 +247,8 @@ PyObject *mx_dequantize(PyObject *const *v)   // packed, layout, dtype, Y, strea
     void *const stream = call.stream(v[4]);
     const at::Tensor Y = own ? call.empty({L.rows, L.d}, dtype_arg(v[2])) : THPVariable_Unpack(v[3]);
     const long long ld = rows_of(Y, "Y", L.rows, L.d);
-    done(f_mx_dequantize(p.data_ptr(), &L, Y.data_ptr(), type_of(Y.scalar_type(), "Y"), ld, stream),
-         "mpq_mx_dequantize");
+    run("mpq_mx_dequantize", f_mx_dequantize, p.data_ptr(), &L, Y.data_ptr(), type_of(Y.scalar_type(), "Y"),
+        ld, stream);
     return own ? THPVariable_Wrap(Y) : same(v[3]);
 }
 
@@ -257,9 +264,8 @@ PyObject *mx_linear(PyObject *const *v)       // X, x_layout, W, w_layout, bias,
     void *const stream = call.stream(v[7]);
     const at::Tensor Y = own ? call.empty({xl.rows, wl.rows}, dtype_arg(v[5])) : THPVariable_Unpack(v[6]);
     const long long ld = rows_of(Y, "Y", xl.rows, wl.rows);
-    done(f_mx_linear(&xl, X.data_ptr(), &wl, W.data_ptr(), bias ? bias->data_ptr<float>() : nullptr, Y.data_ptr(),
-                     type_of(Y.scalar_type(), "Y"), ld, stream),
-         "mpq_mx_linear");
+    run("mpq_mx_linear", f_mx_linear, &xl, X.data_ptr(), &wl, W.data_ptr(), bias ? bias->data_ptr<float>() :
+        nullptr, Y.data_ptr(), type_of(Y.scalar_type(), "Y"), ld, stream);
     return own ? THPVariable_Wrap(Y) : same(v[6]);
 }
 
@@ -300,9 +306,8 @@ PyObject *cache_write(PyObject *const *v)     // K, V, slots, layout, codes, sca
     if (K.stride(2) != 1 || V.stride(2) != 1) refuse(PyExc_ValueError, "%s must have contiguous rows", "K and V");
     const Storage s(call, L, v[4], v[5]);
     void *const stream = call.stream(v[6]);
-    done(f_cache_write(K.data_ptr(), V.data_ptr(), type_of(K.scalar_type(), "K"), ld[0], ld[1],
-                       (int)T, slots.data_ptr<int64_t>(), &L, s.codes.data_ptr(), s.scales.data_ptr<float>(), stream),
-         "mpq_cache_write");
+    run("mpq_cache_write", f_cache_write, K.data_ptr(), V.data_ptr(), type_of(K.scalar_type(), "K"), ld[0],
+        ld[1], (int)T, slots.data_ptr<int64_t>(), &L, s.codes.data_ptr(), s.scales.data_ptr<float>(), stream);
     Py_RETURN_NONE;
 }
 
@@ -321,9 +326,8 @@ PyObject *cache_read(PyObject *const *v)      // slots, layout, codes, scales, d
     at::Tensor out[2];
     for (int i = 0; i < 2; ++i)
         out[i] = v[5 + i] == Py_None ? call.empty(shape, type) : THPVariable_Unpack(v[5 + i]);
-    done(f_cache_read(slots.data_ptr<int64_t>(), (int)shape[0], &L, s.codes.data_ptr(), s.scales.data_ptr<float>(),
-                      out[0].data_ptr(), out[1].data_ptr(), number, stream),
-         "mpq_cache_read");
+    run("mpq_cache_read", f_cache_read, slots.data_ptr<int64_t>(), (int)shape[0], &L, s.codes.data_ptr(),
+        s.scales.data_ptr<float>(), out[0].data_ptr(), out[1].data_ptr(), number, stream);
     PyObject *k = v[5] == Py_None ? THPVariable_Wrap(out[0]) : same(v[5]);
     PyObject *w = k ? (v[6] == Py_None ? THPVariable_Wrap(out[1]) : same(v[6])) : nullptr;
     PyObject *both = w ? PyTuple_Pack(2, k, w) : nullptr;
@@ -364,11 +368,10 @@ PyObject *cache_attention(PyObject *const *v)
     const int window = integer32(v[7], "window");
     void *const stream = call.stream(v[11]);
     const at::Tensor O = own ? call.empty(Q.sizes(), Q.scalar_type()) : THPVariable_Unpack(v[8]);
-    done(f_cache_attention(Q.data_ptr(), type, Q.stride(0), (int)B, (int)q_heads, &L, s.codes.data_ptr(),
-                           s.scales.data_ptr<float>(), table.data_ptr<int>(), (int)cols, lens.data_ptr<int>(),
-                           (float)scale, window, O.data_ptr(), lse ? lse->data_ptr<float>() : nullptr,
-                           ws ? ws->data_ptr() : nullptr, ws ? (size_t)ws->numel() : 0, stream),
-         "mpq_cache_attention");
+    run("mpq_cache_attention", f_cache_attention, Q.data_ptr(), type, Q.stride(0), (int)B, (int)q_heads, &L,
+        s.codes.data_ptr(), s.scales.data_ptr<float>(), table.data_ptr<int>(), (int)cols, lens.data_ptr<int>(),
+        (float)scale, window, O.data_ptr(), lse ? lse->data_ptr<float>() : nullptr, ws ? ws->data_ptr() :
+        nullptr, ws ? (size_t)ws->numel() : 0, stream);
     return own ? THPVariable_Wrap(O) : same(v[8]);
 }
 
