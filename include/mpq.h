@@ -451,7 +451,8 @@ mpq_status mpq_mx_dequantize(const void *packed, const mpq_mx_matrix *layout, vo
  *                same d).
  *   bias         [C] fp32 or NULL.
  *   Y            out [T][C] of type y_type, rows ldy elements apart (ldy >= C).
- * T = 0 or C = 0 is an empty call.  Equal inputs give equal bits from call to call (sums of several
+ * T = 0 or C = 0 is an empty call; more tiles than one launch holds (T of many millions) are
+ * MPQ_ERR_UNSUPPORTED.  Equal inputs give equal bits from call to call (sums of several
  * CTAs are joined in a fixed order).
  */
 mpq_status mpq_mx_linear(const mpq_mx_matrix *x_layout, const void *X,

@@ -30,10 +30,12 @@
 // leave their sums in the workspace, and the CTA that comes last joins them.  Sums are joined in the
 // order of the ranges, so the result does not depend on who comes last.
 //
-// Measured, 8 key heads x 4 query heads of 128, 8 bits: 2 sequences of 131,072 tokens 91 us (554 MB, 6.1 TB/s;
-// 4 bits: also 91 us, bound by 500 warp instructions a stage); 96 sequences of 0 to 4,096, 32 us (a row's start
-// and end cost four stages' time, ranges are ten stages long); one of 777 tokens 11.2 us, one of 64 6.6
-// (latency).
+// Measured, 8 key heads x 4 query heads of 128, 8 bits: 2 sequences of 131,072 tokens 93 us (554 MB, 6.0 TB/s;
+// 4 bits: 92 us with half the bytes -- a stage is one chain of dependent steps, 565 warp instructions, and four
+// warps a scheduler fill 0.58 of its issue slots); 96 sequences of 0 to 4,096, 32 us (a row's start and end cost
+// four stages' time, ranges are ten stages long); one of 777 tokens 11.3 us, one of 64 6.6 (latency).  With 16
+// query heads a key head 76 us instead of 54 (16 sequences of 8,192, 8 key heads of 128); with heads of 256 (4 key
+// heads) 57, and 87 with 16 query heads.
 #include <cuda.h>
 #include <float.h>
 #include <math.h>
@@ -55,8 +57,10 @@ namespace {
 using namespace sm100;
 
 constexpr int A_STAGE = 16;                       // tokens of a stage
-constexpr int A_ROW_COST = 4;                     // what a row costs besides its stages, in stages: 96 ragged
-                                                  // sequences 34.7, 32.9, 31.9, 32.1 us with 2, 3, 4, 5
+// Cuts of the work.  The geometric mean over 64 random batches (1 to 700 sequences of 8 to 60,000 tokens, all
+// heads, widths and bits) is 16.2 us with these; A_ROW_COST 1, 2, 3, 5, 6, 8: 17.2, 16.4, 16.3, 16.1, 16.1, 16.2;
+// A_WHOLE 6, 8, 14: 16.1, 16.2, 16.5; A_ROW 4, 9: 16.2; A_LEAST 1, 3: 16.1, 16.3 (two runs differ by 0.03).
+constexpr int A_ROW_COST = 4;                     // what a row costs besides its stages, in stages
 constexpr int A_LEAST = 2;                        // stages a warp is woken for
 constexpr int A_ROW = 6;                          // most stages of a warp where each CTA takes one row
 constexpr int A_WHOLE = 10;                       // most stages (and costs) of a row that a warp takes alone
@@ -338,7 +342,7 @@ cache_attention_kernel(const AttnArgs a, WaitCtl wc, const __grid_constant__ CUt
     int some;                                    // sequences that have any
     if (few) {
         if (lane < a.B) lane_span = span_of(a, lane);
-        const unsigned mine = (unsigned)weight(lane_span.stages());      // (32 of at most 2^26 + 2)
+        const unsigned mine = (unsigned)weight(lane_span.stages());      // (32 of at most 2^26 + 4)
         lane_all = mine;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {

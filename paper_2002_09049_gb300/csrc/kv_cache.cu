@@ -21,7 +21,7 @@
 //
 // Memory-bound: an element's own bytes on one side, bits / 8 + 4 / dim bytes on the other; slots scatter
 // rows of 32 to 256 bytes, whole sectors.  8,192 tokens of 8 x 128 bf16 to 8 bits: written in 12.6 us (51 MB,
-// 4.0 TB/s; issue slots 70% busy), read back in 9.9 us (5.1 TB/s).
+// 4.0 TB/s; issue slots 74% busy), read back in 9.9 us (5.1 TB/s).
 #include <math.h>
 #include <string.h>
 

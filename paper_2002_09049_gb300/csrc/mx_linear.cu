@@ -19,12 +19,12 @@
 // x 256 channels by CTA pairs (cta_group::2: each CTA holds 128 tokens and half of the channels).  One CTA
 // alone with a 128 x 256 tile is bound by shared memory (52 KB a stage in and 48 KB read by the MMAs, 784
 // cycles at 128 bytes each beside the MMAs' 513) and by what L2 delivers (43 bytes per SM and cycle measured:
-// 1,200 cycles).  The pair halves B's share of both: 35 KB in and 32 KB read a stage, 0.5 us of it.  Each CTA
-// loads all that it holds: a load for several CTAs at once would want its source in this GPU's own memory,
-// which a pointer does not say.
+// 1,200 cycles).  The pair halves B's share of both, 35 KB in and 32 KB read a stage: 0.5 us a stage, 0.25 of it
+// the MMAs', and 5 us a tile for its start and its way out.  Each CTA loads all that it holds: a load for several
+// CTAs at once would want its source in this GPU's own memory, which a pointer does not say.
 //
-// Measured: 1 x 4,096 x 4,096 (T x C x d) 5.1 us and 37 x 11,008 x 4,096 8.4 us (weights' bytes at 1.7 and 2.8
-// TB/s; latency of one round of CTAs), 1,024 x 4,096 x 4,096 13.2 us, 2,048 x 4,096 x 11,008 51.9 us (3.6
+// Measured: 1 x 4,096 x 4,096 (T x C x d) 5.0 us and 37 x 11,008 x 4,096 8.4 us (weights' bytes at 1.8 and 2.9
+// TB/s; latency of one round of CTAs), 1,024 x 4,096 x 4,096 13.2 us, 2,048 x 4,096 x 11,008 51.7 us (3.6
 // PFLOP/s; 128 tiles on 76 pairs are two rounds).
 //
 // Roles: warp 0 copies, warp 1 issues MMAs (the even CTA's, for a pair), warps 2..5 (TMEM lane quarter
