@@ -542,6 +542,155 @@ mpq_status mpq_cache_attention(const void *Q, int type, long long q_stride, int 
 size_t mpq_cache_attention_workspace(void);
 
 /*
+ * Weights in 4-bit integers.  A matrix [rows][d] is held as codes q (0..15) with a scale s, and a zero point z,
+ * for each group of 32, 64 or 128 elements of a row: the value of an element is s (q - z).  s is bf16; z is 8
+ * in every group of a matrix without zero points, else one of 0..15 a group.  The last group of a row may be
+ * shorter.  One device buffer of layout->bytes bytes holds tiles of 16 rows x 128 elements, [row_tiles]
+ * [k_tiles] of them, tile_bytes each:
+ *   codes   [16][64] bytes from offset 0: the 4-byte word 4 i + m of a row (i, m = 0..3) holds elements
+ *           32 m + 8 i + e, e = 0..7, in bits 4 (e / 2) + 16 (e % 2) and the three above;
+ *   scales  [16][128 / group] bf16 from offset 1024;
+ *   zeros   [16][128 / group] bytes behind them (layout->zeros alone).
+ * Elements past the row's end and rows past the last have the value 0 (of a group of zeros, below).  A buffer
+ * in this layout that was made elsewhere can be used as well; it is 16-byte aligned.
+ */
+typedef struct {
+    int rows, d;
+    int group;               /* 32, 64 or 128 */
+    int zeros;               /* 1: a zero point a group, 0: all are 8 */
+    int row_tiles, k_tiles;  /* ceil(rows / 16), ceil(d / 128) */
+    int tile_bytes;          /* 1024 + (zeros ? 48 : 32) * (128 / group) */
+    size_t bytes;            /* size of the device buffer to allocate */
+} mpq_g4_matrix;
+
+/*
+ * mpq_g4_layout -- HOST only: the layout of a [rows][d] matrix; rows >= 0, 1 <= d <= MPQ_MX_MAX_DIM, group 32, 64
+ * or 128 (others: MPQ_ERR_UNSUPPORTED), zeros 0 or 1.
+ */
+mpq_status mpq_g4_layout(int rows, int d, int group, int zeros, mpq_g4_matrix *layout);
+
+/*
+ * mpq_g4_quantize -- X [rows][d] to 4-bit integers.  For each group (fp32 division, ties to even):
+ *   without zero points  s = bf16(max |x| (1/7)) (the fp32 reciprocal, one fp32 product, one rounding to
+ *                        bf16), z = 8, q = clamp(rint(x / s), -7, 7) + 8 (Eq. 8's codes);
+ *   with them            lo = min(x, 0), hi = max(x, 0) over the group, s = bf16(hi (1/15) - lo (1/15)) (fp32
+ *                        products, an fp32 difference), z = clamp(rint(-lo / s), 0, 15),
+ *                        q = clamp(rint(x / s) + z, 0, 15).
+ * A group of zeros, or one whose scale underflows to 0, has scale 0 and q = z = 8; one with a NaN or an
+ * infinity has a NaN scale and q = z = 8.
+ *   X       [rows][d] of type x_type, rows ldx elements apart (ldx >= d); any alignment of its elements'
+ *           own size (16-byte aligned rows are faster).
+ *   packed  out: layout->bytes bytes, 16-byte aligned.
+ */
+mpq_status mpq_g4_quantize(const void *X, int x_type, long long ldx, const mpq_g4_matrix *layout,
+                           void *packed, void *stream);
+
+/*
+ * mpq_g4_dequantize -- the values a packed matrix stands for, each rounded once to y_type.
+ *   Y  out [rows][d], rows ldy elements apart (ldy >= d); what lies between rows is left alone.
+ */
+mpq_status mpq_g4_dequantize(const void *packed, const mpq_g4_matrix *layout, void *Y, int y_type,
+                             long long ldy, void *stream);
+
+/*
+ * mpq_g4_linear -- Y[t][c] = sum_j x_tj w_cj + bias_c for inputs X [T][d] and packed weights W [C][d]: exact products
+ * x (q - z), fp32 sums of each group, times its scale and added in fp32, the bias added in fp32, one rounding
+ * to y_type.
+ *   X     [T][d] of type x_type (MPQ_F16 or MPQ_BF16), rows ldx elements apart (ldx >= d; 16-byte aligned rows of a
+ *         multiple of 8 elements are faster).
+ *   bias  [C] fp32 or NULL.
+ *   Y     out [T][C] of type y_type, rows ldy elements apart (ldy >= C).
+ * T = 0 or C = 0 is an empty call; T above 2^20 is MPQ_ERR_UNSUPPORTED.  Equal inputs give equal bits from call
+ * to call (sums of several CTAs are joined in a fixed order); another T may take another order of the sums.
+ */
+mpq_status mpq_g4_linear(const void *X, int x_type, long long ldx, int T, const mpq_g4_matrix *w_layout,
+                         const void *W, const float *bias, void *Y, int y_type, long long ldy, void *stream);
+
+/*
+ * Positions.  mpq_rotation_turns -- HOST only: the frequencies freq[n] (radians a position, finite) as turns a
+ * position in 64 binary places, rounded, whole turns dropped: turns[i] = round(2^64 freq[i] / 2 pi) mod 2^64.  A
+ * position times it, in wrapping 64-bit arithmetic, is the angle's fraction of a turn to within
+ * (|position| / 2 + 1) 2^-64 turns and the frequency's own rounding.
+ */
+mpq_status mpq_rotation_turns(const double *freq, int n, uint64_t *turns);
+
+/*
+ * mpq_rotate -- norms of queries and keys for each head and the position rotation, in one pass:
+ *   with norm  x <- x w / sqrt(sum_j x_j^2 / dim + eps)  over the head's dim elements;
+ *   then, for i < rot / 2 with the angle a_i = position * freq_i,
+ *     (x_i, x_j) <- (x_i cos a_i - x_j sin a_i, x_j cos a_i + x_i sin a_i),
+ *   j = i + rot / 2, or with neighbours the pair (x_2i, x_2i+1); elements from rot on stay (normed).
+ * fp32 throughout, cosine and sine of the reduced angle within 2^-22; one rounding to `type`.
+ *   Q, K       [T][q_heads][dim] and [T][heads][dim] of type `type`: token t's row of head h starts
+ *              ld_token * t + ld_head * h elements after Q (K), the dim values consecutive (the parts
+ *              of one projection's output can be given as they are).  K NULL: queries alone (heads = 0).
+ *   positions  [T] int32 on the device; `shift` is added to each (64-bit: nothing overflows).
+ *   turns      [rot / 2] of mpq_rotation_turns on the device.
+ *   norm       0: no norm (weights NULL); 1: eps > 0, weights [dim] fp32 or NULL (ones).
+ *   Yq, Yk     out, laid out by ldy_token, ldy_head (the queries' and the keys' own strides: q_..., k_...); Q
+ *              and K themselves with their strides, or memory that does not overlap Q or K.
+ * dim even, 2..512; rot even, 0..dim.
+ */
+typedef struct {
+    const void *x;                     /* in */
+    void *y;                           /* out */
+    const float *weight;               /* [dim] or NULL */
+    int heads;
+    long long ld_token, ld_head;       /* of x, in elements */
+    long long ldy_token, ldy_head;     /* of y */
+} mpq_rotate_rows;
+
+mpq_status mpq_rotate(const mpq_rotate_rows *q, const mpq_rotate_rows *k, int type, int T, int dim,
+                      const int *positions, int shift, const uint64_t *turns, int rot, int neighbours,
+                      int norm, float eps, void *stream);
+
+/*
+ * The pages of a cache's requests, kept on the device, so that a serving step needs no word from the host.  The state
+ * of B requests:
+ *   lens   [B] int32: the tokens that each holds;
+ *   table  [B][cols] int32: the page of tokens page * i .. page * i + page - 1 in column i (what
+ *          mpq_cache_attention takes);
+ *   pool   [pages] int32: the pages that no request holds are pool[0 .. count[0] - 1];
+ *   count  [2] int32: how many, and a word of the calls' own, zero between them.
+ * Calls on one state follow one another on a stream.  Page numbers are the caller's: they are moved, not looked
+ * at.  page >= 1; any power of two or other; B up to MPQ_PAGES_MAX_REQUESTS, page * cols up to 2^30.
+ */
+#define MPQ_PAGES_MAX_REQUESTS 8192
+
+/*
+ * mpq_pages_extend -- room for add[b] new tokens (none if negative) of every request b, their slots and positions.  The
+ * new tokens lie packed in the order of the requests: token i of request b is number start_b + i, start_b =
+ * sum_{c<b} add_c, of the N that slots and positions have room for.  A request is served whole or not at all: it
+ * needs need_b = ceil((len_b + add_b) / page) - ceil(len_b / page) pages, and is served if its tokens' numbers
+ * are all below N, len_b is not negative, len_b + add_b <= page * cols, and need_b = 0 or the pages that are
+ * needed by it and the requests before it (served or not; those that the first three conditions refuse need
+ * none) are no more than count[0].  Pages are taken from the pool's end, in the order of requests and columns.
+ *   add        [B] int32.
+ *   slots      out [N] int64: (page) * page + place, for mpq_cache_write; -1 for a token of a request that was
+ *              not served, one whose table entry is negative, and numbers past the last token.
+ *   positions  out [N] int32: len_b + i, served or not; 0 past the last token.
+ *   taken      out [B] int32: add_b, or 0 where the request was not served.
+ *   new_lens   out [B] int32: len_b + taken_b; lens itself or other memory.
+ *   new_count  out [2] int32: the pages left, and 0; count itself or other memory.
+ * The pool's entries stay as they are.  count[0] is taken as within 0 .. pages.  Sums of add_b stop at 2^31 - 1
+ * (above every N).  An output that overlaps another array is MPQ_ERR_INVALID_ARG.
+ */
+mpq_status mpq_pages_extend(const int *add, int B, int page, int cols, const int *lens, int *new_lens,
+                            int *table, const int *pool, int pages, int *count, int *new_count,
+                            int64_t *slots, int *positions, long long N, int *taken, void *stream);
+
+/*
+ * mpq_pages_trim -- requests cut back to keep[b] tokens (none if negative; len_b or more: it stays): their pages
+ * beyond return to the pool, in the order in which mpq_pages_extend would give them out again (a step that is
+ * taken back whole leaves the pool as it was).  Table entries past a request's end are left as they were.  If
+ * more pages return than the pool has room for, those past its end are dropped (and its count is `pages`):
+ * a state that extend and trim alone have changed has room for all.  Lengths are taken as within 0 .. page *
+ * cols; new_lens and new_count as mpq_pages_extend's.
+ */
+mpq_status mpq_pages_trim(const int *keep, int B, int page, int cols, const int *lens, int *new_lens,
+                          const int *table, int *pool, int pages, int *count, int *new_count, void *stream);
+
+/*
  * Bounded device-side waits.  The tensor-core kernels (mpq_output_error and its _noalloc variant,
  * mpq_clip_search, mpq_multipoint_linear, mpq_mx_linear) hand work between their warps, and
  * mpq_cache_attention's warps take their copies, through shared-memory barriers, and every wait on

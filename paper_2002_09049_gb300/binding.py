@@ -11,6 +11,7 @@ import ctypes
 import functools
 import os
 
+import numpy as np
 import torch
 
 from . import _build
@@ -33,6 +34,7 @@ MPQ_FAULT_BOUNDS = 0x10000            # mpq_device_status: the checked build ski
 MPQ_BUILD_CHECK_BOUNDS = 0x1          # mpq_build_options: the checked build
 
 MPQ_CACHE_WORKSPACE = 1 << 25         # bytes of mpq_cache_attention's workspace
+MPQ_PAGES_MAX_REQUESTS = 8192         # most requests of mpq_pages_extend and mpq_pages_trim
 
 MPQ_STATUS = {0: "MPQ_OK", 1: "MPQ_ERR_INVALID_ARG", 2: "MPQ_ERR_NONFINITE",
               3: "MPQ_ERR_UNSUPPORTED", 4: "MPQ_ERR_CUDA", 5: "MPQ_ERR_TIMEOUT",
@@ -73,9 +75,25 @@ class KvCache(ctypes.Structure):
         return (self.pages, 2, self.heads, self.page)
 
 
+class G4Matrix(ctypes.Structure):
+    """mpq_g4_matrix of include/mpq.h: the layout of a matrix of 4-bit integers with a scale a group."""
+    _fields_ = [("rows", ctypes.c_int), ("d", ctypes.c_int), ("group", ctypes.c_int),
+                ("zeros", ctypes.c_int), ("row_tiles", ctypes.c_int), ("k_tiles", ctypes.c_int),
+                ("tile_bytes", ctypes.c_int), ("bytes", ctypes.c_size_t)]
+
+
+class RotateRows(ctypes.Structure):
+    """mpq_rotate_rows of include/mpq.h: the queries, or the keys, of a rotation."""
+    _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("weight", ctypes.c_void_p),
+                ("heads", ctypes.c_int), ("ld_token", ctypes.c_longlong), ("ld_head", ctypes.c_longlong),
+                ("ldy_token", ctypes.c_longlong), ("ldy_head", ctypes.c_longlong)]
+
+
 _L = ctypes.POINTER(PackedLayout)
 _M = ctypes.POINTER(MxMatrix)
 _KV = ctypes.POINTER(KvCache)
+_G4 = ctypes.POINTER(G4Matrix)
+_R = ctypes.POINTER(RotateRows)
 _LL = ctypes.c_longlong
 
 SIGNATURES = {
@@ -102,6 +120,14 @@ SIGNATURES = {
     "mpq_cache_attention": ([_P, _I, _LL, _I, _I, _KV, _P, _P, _P, _I, _P, ctypes.c_float, _I, _P,
                              _P, _P, ctypes.c_size_t, _P], _I),
     "mpq_cache_attention_workspace": ([], ctypes.c_size_t),
+    "mpq_g4_layout": ([_I, _I, _I, _I, _G4], _I),
+    "mpq_g4_quantize": ([_P, _I, _LL, _G4, _P, _P], _I),
+    "mpq_g4_dequantize": ([_P, _G4, _P, _I, _LL, _P], _I),
+    "mpq_g4_linear": ([_P, _I, _LL, _I, _G4, _P, _P, _P, _I, _LL, _P], _I),
+    "mpq_rotation_turns": ([_P, _I, _P], _I),
+    "mpq_rotate": ([_R, _R, _I, _I, _I, _P, _I, _P, _I, _I, _I, ctypes.c_float, _P], _I),
+    "mpq_pages_extend": ([_P, _I, _I, _I, _P, _P, _P, _P, _I, _P, _P, _P, _P, _LL, _P, _P], _I),
+    "mpq_pages_trim": ([_P, _I, _I, _I, _P, _P, _P, _P, _I, _P, _P, _P], _I),
     "mpq_device_status": ([_P, _P], _I),
     "mpq_set_wait_limit": ([ctypes.c_longlong], _I),
     "mpq_test_withhold_copies": ([_I], _I),
@@ -484,7 +510,8 @@ class _Unloaded:
                                "build it with paper_2002_09049_gb300._build.build() (there is no "
                                "fallback)") from e
         _serve_binding.init(_check, {f: ctypes.cast(getattr(lib, f), ctypes.c_void_p).value
-                                     for f in SIGNATURES if f.startswith(("mpq_mx_", "mpq_cache_"))})
+                                     for f in SIGNATURES if f.startswith(("mpq_mx_", "mpq_cache_", "mpq_g4_", "mpq_rotat",
+                                                                   "mpq_pages_"))})
         _native = _serve_binding
         return getattr(_native, name)
 
@@ -557,6 +584,69 @@ def mpq_cache_attention(Q, table, lens, layout: KvCache, codes, scales, scale: f
     zeroed before the first call and kept from call to call (by default taken from the pool)."""
     return _native.cache_attention(Q, table, lens, layout, codes, scales, scale, window, O, lse,
                                    workspace, stream)
+
+
+@functools.lru_cache(maxsize=256)
+def mpq_g4_layout(rows: int, d: int, group: int = 128, zeros: bool = False) -> G4Matrix:
+    """Host-side layout of a [rows][d] matrix of 4-bit integers with a scale (and, with zeros, a zero
+    point) for each group of 32, 64 or 128 elements of a row (not to be changed)."""
+    lay = G4Matrix()
+    _check(load().mpq_g4_layout(rows, d, group, int(bool(zeros)), ctypes.byref(lay)), "mpq_g4_layout")
+    return lay
+
+
+def mpq_g4_quantize(X, layout: G4Matrix, packed=None, stream=None):
+    """X [rows][d] (fp32, fp16 or bf16; rows may lie apart) to 4-bit integers: the packed buffer (uint8
+    [layout.bytes]) of mpq_g4_layout(rows, d, ..)."""
+    return _native.g4_quantize(X, layout, packed, stream)
+
+
+def mpq_g4_dequantize(packed, layout: G4Matrix, dtype=torch.float32, Y=None, stream=None):
+    """The values [rows][d] of a packed matrix."""
+    return _native.g4_dequantize(packed, layout, dtype, Y, stream)
+
+
+def mpq_g4_linear(X, W, w_layout: G4Matrix, bias=None, dtype=None, Y=None, stream=None):
+    """Y [T][C] = X W^T + bias for inputs X [T][d] (fp16 or bf16; rows may lie apart) and packed weights W
+    [C][d]; bias fp32 [C].  dtype: that of Y, X's by default."""
+    return _native.g4_linear(X, W, w_layout, bias, dtype, Y, stream)
+
+
+def mpq_rotation(freq, device="cuda"):
+    """Frequencies (radians a position; base ** (-2 i / rot) for i < rot / 2 is usual) as mpq_rotate takes
+    them: int64 [rot / 2], turns a position in 64 binary places."""
+    f = np.ascontiguousarray(freq, dtype=np.float64).reshape(-1)
+    turns = np.empty(f.size, dtype=np.int64)
+    _check(load().mpq_rotation_turns(f.ctypes.data, f.size, turns.ctypes.data), "mpq_rotation_turns")
+    return torch.from_numpy(turns).to(device)
+
+
+def mpq_rotate(Q, K, positions, turns, norm: bool = False, q_weight=None, k_weight=None, eps: float = 1e-6,
+               neighbours: bool = False, shift: int = 0, Yq=None, Yk=None, stream=None):
+    """Queries Q [T][q_heads][dim] and keys K [T][heads][dim] (or None) normed for each head (norm: by the root
+    of the mean square, times the fp32 weights [dim] where given) and rotated by their positions [T] int32 +
+    shift, in one pass.  turns: mpq_rotation's, of the rotated rot <= dim elements; neighbours: pairs are (0, 1),
+    (2, 3), .. instead of (i, i + rot / 2).  Tokens and heads may lie apart; Yq and Yk may be Q and K.
+    Returns (Yq, Yk)."""
+    return _native.rotate(Q, K, positions, turns, norm, q_weight, k_weight, eps, neighbours, shift, Yq, Yk,
+                          stream)
+
+
+def mpq_pages_extend(add, lens, table, pool, count, page: int, N: int, new_lens=None, new_count=None,
+                     slots=None, positions=None, taken=None, stream=None):
+    """Room for add [B] new tokens of the requests whose lengths are lens [B] and pages table [B][columns]:
+    pages are taken from the end of pool [pages], of which the first count[0] are free (count [2]; all
+    int32).  Returns (slots [N] int64, positions [N] int32, taken [B] int32) of the new tokens, packed in the
+    order of the requests; a request that finds no room is not served (slots of -1, taken 0).  Lengths and
+    count are updated in place, or written to new_lens and new_count."""
+    return _native.pages_extend(add, lens, table, pool, count, page, N, new_lens, new_count, slots, positions,
+                                taken, stream)
+
+
+def mpq_pages_trim(keep, lens, table, pool, count, page: int, new_lens=None, new_count=None, stream=None):
+    """The requests cut back to keep [B] tokens (where they are longer), their pages beyond returned to the pool.
+    Lengths and count are updated in place, or written to new_lens and new_count."""
+    _native.pages_trim(keep, lens, table, pool, count, page, new_lens, new_count, stream)
 
 
 def mpq_status_string(status: int) -> str:

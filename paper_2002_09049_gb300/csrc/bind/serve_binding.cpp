@@ -27,6 +27,12 @@ decltype(&mpq_mx_linear) f_mx_linear;
 decltype(&mpq_cache_write) f_cache_write;
 decltype(&mpq_cache_read) f_cache_read;
 decltype(&mpq_cache_attention) f_cache_attention;
+decltype(&mpq_g4_quantize) f_g4_quantize;
+decltype(&mpq_g4_dequantize) f_g4_dequantize;
+decltype(&mpq_g4_linear) f_g4_linear;
+decltype(&mpq_rotate) f_rotate;
+decltype(&mpq_pages_extend) f_pages_extend;
+decltype(&mpq_pages_trim) f_pages_trim;
 PyObject *raise_status;      // raise_status(status, name): the exception of a refused call
 
 // An argument was refused: the Python error is set.
@@ -189,7 +195,8 @@ long long rows_of(const at::Tensor &t, const char *name, long long rows, long lo
     return step > d ? step : d;
 }
 
-const at::Tensor &packed(Call &call, PyObject *o, const char *name, const mpq_mx_matrix &L)
+template <typename L_>
+const at::Tensor &packed(Call &call, PyObject *o, const char *name, const L_ &L)
 {
     const at::Tensor &t = dense(call, o, name, at::kByte);
     if ((size_t)t.numel() < L.bytes)
@@ -375,6 +382,208 @@ PyObject *cache_attention(PyObject *const *v)
     return own ? THPVariable_Wrap(O) : same(v[8]);
 }
 
+PyObject *g4_quantize(PyObject *const *v)     // X, layout, packed, stream
+{
+    Call call;
+    const at::Tensor &X = call.tensor(v[0], "X");
+    const mpq_g4_matrix &L = layout<mpq_g4_matrix>(v[1], "layout");
+    const long long ld = rows_of(X, "X", L.rows, L.d);
+    const int type = type_of(X.scalar_type(), "X");
+    const bool own = v[2] == Py_None;
+    if (!own) packed(call, v[2], "packed", L);
+    void *const stream = call.stream(v[3]);
+    const at::Tensor out = own ? call.empty({(long long)L.bytes}, at::kByte) : THPVariable_Unpack(v[2]);
+    run("mpq_g4_quantize", f_g4_quantize, X.data_ptr(), type, ld, &L, out.data_ptr(), stream);
+    return own ? THPVariable_Wrap(out) : same(v[2]);
+}
+
+PyObject *g4_dequantize(PyObject *const *v)   // packed, layout, dtype, Y, stream
+{
+    Call call;
+    const mpq_g4_matrix &L = layout<mpq_g4_matrix>(v[1], "layout");
+    const at::Tensor &p = packed(call, v[0], "packed", L);
+    const bool own = v[3] == Py_None;
+    if (!own) call.tensor(v[3], "Y");
+    void *const stream = call.stream(v[4]);
+    const at::Tensor Y = own ? call.empty({L.rows, L.d}, dtype_arg(v[2])) : THPVariable_Unpack(v[3]);
+    const long long ld = rows_of(Y, "Y", L.rows, L.d);
+    run("mpq_g4_dequantize", f_g4_dequantize, p.data_ptr(), &L, Y.data_ptr(), type_of(Y.scalar_type(), "Y"), ld,
+        stream);
+    return own ? THPVariable_Wrap(Y) : same(v[3]);
+}
+
+PyObject *g4_linear(PyObject *const *v)       // X, W, w_layout, bias, dtype, Y, stream
+{
+    Call call;
+    const at::Tensor &X = call.tensor(v[0], "X");
+    const mpq_g4_matrix &L = layout<mpq_g4_matrix>(v[2], "w_layout");
+    if (X.dim() != 2) refuse(PyExc_ValueError, "%s must be [T][d]", "X");
+    const long long T = X.size(0), ldx = rows_of(X, "X", T, L.d);
+    if (T > INT32_MAX) refuse(PyExc_ValueError, "%s has too many rows", "X");
+    const int type = type_of(X.scalar_type(), "X");
+    const at::Tensor &W = packed(call, v[1], "W", L);
+    const at::Tensor *const bias = v[3] == Py_None ? nullptr : &dense(call, v[3], "bias", at::kFloat, {L.rows});
+    const bool own = v[5] == Py_None;
+    if (!own) call.tensor(v[5], "Y");
+    void *const stream = call.stream(v[6]);
+    const at::Tensor Y = own ? call.empty({T, L.rows}, v[4] == Py_None ? X.scalar_type() : dtype_arg(v[4]))
+                             : THPVariable_Unpack(v[5]);
+    const long long ldy = rows_of(Y, "Y", T, L.rows);
+    run("mpq_g4_linear", f_g4_linear, X.data_ptr(), type, ldx, (int)T, &L, W.data_ptr(),
+        bias ? bias->data_ptr<float>() : nullptr, Y.data_ptr(), type_of(Y.scalar_type(), "Y"), ldy, stream);
+    return own ? THPVariable_Wrap(Y) : same(v[5]);
+}
+
+bool flag(PyObject *o)
+{
+    const int r = PyObject_IsTrue(o);
+    if (r < 0) throw Refused();
+    return r != 0;
+}
+
+// Q or K [T][heads][dim] of a rotation, and where its output goes (None: allocated later).
+struct Turned {
+    const at::Tensor *x = nullptr;
+    at::Tensor y;
+    bool own = false;
+    mpq_rotate_rows rows = {};
+
+    Turned(Call &call, PyObject *in, PyObject *out, PyObject *weight, const char *name, const char *out_name,
+           const char *weight_name)
+    {
+        if (in == Py_None) {
+            if (out != Py_None || weight != Py_None)
+                refuse(PyExc_ValueError, "%s or %s without what they are for", out_name, weight_name);
+            return;
+        }
+        x = &call.tensor(in, name);
+        if (x->dim() != 3) refuse(PyExc_ValueError, "%s must be [T][heads][dim]", name);
+        if (x->size(2) > 1 && x->stride(2) != 1) refuse(PyExc_ValueError, "%s must have contiguous rows", name);
+        if (x->size(1) > INT32_MAX) refuse(PyExc_ValueError, "%s has too many heads", name);
+        if (weight != Py_None)
+            rows.weight = dense(call, weight, weight_name, at::kFloat, {x->size(2)}).data_ptr<float>();
+        own = out == Py_None;
+        if (own) return;
+        y = call.tensor(out, out_name);
+        need_shape(y, out_name, x->sizes());
+        if (y.scalar_type() != x->scalar_type())
+            refuse(PyExc_TypeError, "%s must have the type of its input, %s", out_name, dtype_name(x->scalar_type()));
+        if (y.size(2) > 1 && y.stride(2) != 1) refuse(PyExc_ValueError, "%s must have contiguous rows", out_name);
+    }
+    void finish(Call &call)
+    {
+        if (!x) return;
+        if (own) y = call.empty(x->sizes(), x->scalar_type());
+        rows.x = x->data_ptr();
+        rows.y = y.data_ptr();
+        rows.heads = (int)x->size(1);
+        rows.ld_token = x->size(0) > 1 ? x->stride(0) : 0;
+        rows.ld_head = x->size(1) > 1 ? x->stride(1) : 0;
+        rows.ldy_token = y.size(0) > 1 ? y.stride(0) : 0;
+        rows.ldy_head = y.size(1) > 1 ? y.stride(1) : 0;
+    }
+    PyObject *result(PyObject *out) const { return x && own ? THPVariable_Wrap(y) : same(out); }
+};
+
+// Q, K, positions, turns, norm, q_weight, k_weight, eps, neighbours, shift, Yq, Yk, stream
+PyObject *rotate(PyObject *const *v)
+{
+    Call call;
+    Turned q(call, v[0], v[10], v[5], "Q", "Yq", "q_weight"), k(call, v[1], v[11], v[6], "K", "Yk", "k_weight");
+    if (!q.x) refuse(PyExc_TypeError, "%s must be a torch tensor", "Q");
+    const long long T = q.x->size(0), dim = q.x->size(2);
+    if (T > INT32_MAX || dim > INT32_MAX) refuse(PyExc_ValueError, "%s is too large", "Q");
+    if (k.x && (k.x->size(0) != T || k.x->size(2) != dim || k.x->scalar_type() != q.x->scalar_type()))
+        refuse(PyExc_ValueError, "K must have Q's tokens, dim and type%s", "");
+    const at::Tensor &positions = dense(call, v[2], "positions", at::kInt, {T});
+    const at::Tensor &turns = dense(call, v[3], "turns", at::kLong);
+    if (turns.dim() != 1 || turns.numel() > INT32_MAX / 2) refuse(PyExc_ValueError, "%s must be [rot / 2]", "turns");
+    const int type = type_of(q.x->scalar_type(), "Q");
+    const double eps = PyFloat_AsDouble(v[7]);
+    if (eps == -1.0 && PyErr_Occurred()) throw Refused();
+    const int norm = flag(v[4]), neighbours = flag(v[8]), shift = integer32(v[9], "shift");
+    void *const stream = call.stream(v[12]);
+    q.finish(call);
+    k.finish(call);
+    run("mpq_rotate", f_rotate, &q.rows, k.x ? &k.rows : nullptr, type, (int)T, (int)dim, positions.data_ptr<int>(),
+        shift, reinterpret_cast<const uint64_t *>(turns.data_ptr<int64_t>()), 2 * (int)turns.numel(), neighbours,
+        norm, (float)eps, stream);
+    PyObject *a = q.result(v[10]), *b = a ? k.result(v[11]) : nullptr, *both = b ? PyTuple_Pack(2, a, b) : nullptr;
+    Py_XDECREF(a);
+    Py_XDECREF(b);
+    return both;
+}
+
+// The state of a cache's requests: want (add or keep), lens, table, pool, count, and where new lengths and the new
+// count go (None: in place).
+struct Requests {
+    const at::Tensor &want, &lens, &table, &pool, &count;
+    const at::Tensor &new_lens, &new_count;
+
+    Requests(Call &call, const char *name, PyObject *w, PyObject *l, PyObject *t, PyObject *p, PyObject *c,
+             PyObject *nl, PyObject *nc)
+        : want(dense(call, w, name, at::kInt)), lens(dense(call, l, "lens", at::kInt, want.sizes())),
+          table(dense(call, t, "table", at::kInt)), pool(dense(call, p, "pool", at::kInt)),
+          count(dense(call, c, "count", at::kInt, {2})),
+          new_lens(nl == Py_None ? lens : dense(call, nl, "new_lens", at::kInt, want.sizes())),
+          new_count(nc == Py_None ? count : dense(call, nc, "new_count", at::kInt, {2}))
+    {
+        if (want.dim() != 1) refuse(PyExc_ValueError, "%s must be [B]", name);
+        if (table.dim() != 2 || table.size(0) != want.size(0))
+            refuse(PyExc_ValueError, "table must have shape (%s, columns), got %s",
+                   std::to_string(want.size(0)).c_str(), text(table.sizes()).c_str());
+        if (pool.dim() != 1) refuse(PyExc_ValueError, "%s must be [pages]", "pool");
+        if (want.size(0) > INT32_MAX || table.size(1) > INT32_MAX || pool.size(0) > INT32_MAX)
+            refuse(PyExc_ValueError, "%s is too large", "table or pool");
+    }
+};
+
+// add, lens, table, pool, count, page, N, new_lens, new_count, slots, positions, taken, stream
+PyObject *pages_extend(PyObject *const *v)
+{
+    Call call;
+    const Requests r(call, "add", v[0], v[1], v[2], v[3], v[4], v[7], v[8]);
+    const int page = integer32(v[5], "page");
+    const long long N = integer(v[6]), B = r.want.size(0);
+    if (N < 0) refuse(PyExc_ValueError, "%s must not be negative", "N");
+    const char *const names[3] = {"slots", "positions", "taken"};
+    const at::ScalarType types[3] = {at::kLong, at::kInt, at::kInt};
+    const long long sizes[3] = {N, N, B};
+    for (int i = 0; i < 3; ++i)
+        if (v[9 + i] != Py_None) dense(call, v[9 + i], names[i], types[i], {sizes[i]});
+    void *const stream = call.stream(v[12]);
+    at::Tensor out[3];
+    for (int i = 0; i < 3; ++i)
+        out[i] = v[9 + i] == Py_None ? call.empty({sizes[i]}, types[i]) : THPVariable_Unpack(v[9 + i]);
+    run("mpq_pages_extend", f_pages_extend, r.want.data_ptr<int>(), (int)B, page, (int)r.table.size(1),
+        r.lens.data_ptr<int>(), r.new_lens.data_ptr<int>(), r.table.data_ptr<int>(), r.pool.data_ptr<int>(),
+        (int)r.pool.size(0), r.count.data_ptr<int>(), r.new_count.data_ptr<int>(), out[0].data_ptr<int64_t>(),
+        out[1].data_ptr<int>(), N, out[2].data_ptr<int>(), stream);
+    PyObject *all = PyTuple_New(3);
+    for (int i = 0; all && i < 3; ++i) {
+        PyObject *o = v[9 + i] == Py_None ? THPVariable_Wrap(out[i]) : same(v[9 + i]);
+        if (!o) {
+            Py_DECREF(all);
+            return nullptr;
+        }
+        PyTuple_SET_ITEM(all, i, o);
+    }
+    return all;
+}
+
+// keep, lens, table, pool, count, page, new_lens, new_count, stream
+PyObject *pages_trim(PyObject *const *v)
+{
+    Call call;
+    const Requests r(call, "keep", v[0], v[1], v[2], v[3], v[4], v[6], v[7]);
+    const int page = integer32(v[5], "page");
+    void *const stream = call.stream(v[8]);
+    run("mpq_pages_trim", f_pages_trim, r.want.data_ptr<int>(), (int)r.want.size(0), page, (int)r.table.size(1),
+        r.lens.data_ptr<int>(), r.new_lens.data_ptr<int>(), r.table.data_ptr<int>(), r.pool.data_ptr<int>(),
+        (int)r.pool.size(0), r.count.data_ptr<int>(), r.new_count.data_ptr<int>(), stream);
+    Py_RETURN_NONE;
+}
+
 // No C++ exception leaves a call: refusals have their Python error set, others become RuntimeError.
 template <PyObject *(*F)(PyObject *const *), Py_ssize_t N>
 PyObject *guarded(PyObject *, PyObject *const *v, Py_ssize_t n)
@@ -407,6 +616,12 @@ PyObject *init(PyObject *, PyObject *args)
     take(f_cache_write, "mpq_cache_write");
     take(f_cache_read, "mpq_cache_read");
     take(f_cache_attention, "mpq_cache_attention");
+    take(f_g4_quantize, "mpq_g4_quantize");
+    take(f_g4_dequantize, "mpq_g4_dequantize");
+    take(f_g4_linear, "mpq_g4_linear");
+    take(f_rotate, "mpq_rotate");
+    take(f_pages_extend, "mpq_pages_extend");
+    take(f_pages_trim, "mpq_pages_trim");
     if (!ok) {
         if (!PyErr_Occurred()) PyErr_SetString(PyExc_KeyError, "an entry point is missing");
         return nullptr;
@@ -431,6 +646,12 @@ PyMethodDef methods[] = {{"init", init, METH_VARARGS, nullptr},
                          method<cache_write, 7>("cache_write"),
                          method<cache_read, 8>("cache_read"),
                          method<cache_attention, 12>("cache_attention"),
+                         method<g4_quantize, 4>("g4_quantize"),
+                         method<g4_dequantize, 5>("g4_dequantize"),
+                         method<g4_linear, 7>("g4_linear"),
+                         method<rotate, 13>("rotate"),
+                         method<pages_extend, 13>("pages_extend"),
+                         method<pages_trim, 9>("pages_trim"),
                          {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_serve_binding", nullptr, -1, methods,

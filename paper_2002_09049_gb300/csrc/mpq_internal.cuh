@@ -152,4 +152,23 @@ mpq_status launch_cache_attention(const void *Q, int type, long long q_stride, i
                                   int window, void *O, float *lse, void *workspace,
                                   cudaStream_t stream);
 
+mpq_status make_g4_layout(int rows, int d, int group, int zeros, mpq_g4_matrix *L);
+mpq_status launch_g4_quantize(const void *X, int x_type, long long ldx, const mpq_g4_matrix *L,
+                              void *packed, cudaStream_t stream);
+mpq_status launch_g4_dequantize(const void *packed, const mpq_g4_matrix *L, void *Y, int y_type,
+                                long long ldy, cudaStream_t stream);
+mpq_status launch_g4_linear(const void *X, int x_type, long long ldx, int T, const mpq_g4_matrix *L,
+                            const void *W, const float *bias, void *Y, int y_type, long long ldy,
+                            cudaStream_t stream);
+mpq_status launch_rotate(const mpq_rotate_rows *q, const mpq_rotate_rows *k, int type, int T, int dim,
+                         const int *positions, int shift, const uint64_t *turns, int rot, int neighbours,
+                         int norm, float eps, cudaStream_t stream);
+mpq_status launch_pages_extend(const int *add, int B, int page, int cols, const int *lens, int *new_lens,
+                               int *table, const int *pool, int pages, int *count, int *new_count,
+                               int64_t *slots, int *positions, long long N, int *taken,
+                               cudaStream_t stream);
+mpq_status launch_pages_trim(const int *keep, int B, int page, int cols, const int *lens, int *new_lens,
+                             const int *table, int *pool, int pages, int *count, int *new_count,
+                             cudaStream_t stream);
+
 }  // namespace mpq
