@@ -593,9 +593,9 @@ mpq_status mpq_g4_dequantize(const void *packed, const mpq_g4_matrix *layout, vo
                              long long ldy, void *stream);
 
 /*
- * mpq_g4_linear -- Y[t][c] = sum_j x_tj w_cj + bias_c for inputs X [T][d] and packed weights W [C][d]: exact products
- * x (q - z), fp32 sums of each group, times its scale and added in fp32, the bias added in fp32, one rounding
- * to y_type.
+ * mpq_g4_linear -- Y[t][c] = sum_j x_tj w_cj + bias_c for inputs X [T][d] and packed weights W [C][d]: w is a weight's
+ * value s (q - z) rounded once to X's type, what mpq_g4_dequantize gives in it (bf16: by 2^-9 of it at most; fp16: by
+ * 2^-12, infinite from 65,520 on); exact products, fp32 sums, the bias added in fp32, one rounding to y_type.
  *   X     [T][d] of type x_type (MPQ_F16 or MPQ_BF16), rows ldx elements apart (ldx >= d; 16-byte aligned rows of a
  *         multiple of 8 elements are faster).
  *   bias  [C] fp32 or NULL.
@@ -692,12 +692,12 @@ mpq_status mpq_pages_trim(const int *keep, int B, int page, int cols, const int 
 
 /*
  * Bounded device-side waits.  The tensor-core kernels (mpq_output_error and its _noalloc variant,
- * mpq_clip_search, mpq_multipoint_linear, mpq_mx_linear) hand work between their warps, and
+ * mpq_clip_search, mpq_multipoint_linear, mpq_mx_linear, mpq_g4_linear) hand work between their warps, and
  * mpq_cache_attention's warps take their copies, through shared-memory barriers, and every wait on
  * one is bounded by a clock budget.  A kernel whose wait gives up
  * stops issuing work, waits for the copies and MMAs it has already issued to finish, releases its
  * tensor memory and returns, with NaN in its output errors and in mpq_cache_attention's outputs (the
- * outputs of mpq_multipoint_linear and mpq_mx_linear unspecified);
+ * outputs of mpq_multipoint_linear, mpq_mx_linear and mpq_g4_linear unspecified);
  * it records which kernel it was in a word kept per device.  A NaN error can therefore mean a
  * non-finite input or a timeout: mpq_device_status tells them apart.
  */
@@ -706,6 +706,7 @@ mpq_status mpq_pages_trim(const int *keep, int B, int page, int cols, const int 
 #define MPQ_TIMEOUT_INFERENCE 0x4u      /* mpq_multipoint_linear */
 #define MPQ_TIMEOUT_MX 0x8u             /* mpq_mx_linear */
 #define MPQ_TIMEOUT_ATTENTION 0x10u     /* mpq_cache_attention */
+#define MPQ_TIMEOUT_G4 0x20u            /* mpq_g4_linear */
 #define MPQ_TIMEOUT_DRAIN 0x100u        /* a wait for the kernel's own copies or MMAs also gave up */
 
 /*
@@ -747,8 +748,8 @@ mpq_status mpq_set_wait_limit(long long clocks);
  * mpq_test_withhold_copies -- TEST HOOK, process-wide: while on (1), the tile-copy thread of the
  * output-error contraction (mpq_output_error's tensor-core path) issues no copies, so that every
  * wait of that kernel runs out with nothing in flight and the call reports MPQ_TIMEOUT_OUTPUT_ERROR
- * through mpq_device_status; likewise mpq_mx_linear's (MPQ_TIMEOUT_MX) and mpq_cache_attention's warps
- * (MPQ_TIMEOUT_ATTENTION).  Off (0) by default; never on outside tests of the timeout path.
+ * through mpq_device_status; likewise mpq_mx_linear's (MPQ_TIMEOUT_MX), mpq_g4_linear's
+ * (MPQ_TIMEOUT_G4) and mpq_cache_attention's warps (MPQ_TIMEOUT_ATTENTION).  Off (0) by default; never on outside tests of the timeout path.
  */
 mpq_status mpq_test_withhold_copies(int on);
 

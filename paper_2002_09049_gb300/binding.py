@@ -29,6 +29,7 @@ MPQ_TIMEOUT_CLIP = 0x2
 MPQ_TIMEOUT_INFERENCE = 0x4
 MPQ_TIMEOUT_MX = 0x8
 MPQ_TIMEOUT_ATTENTION = 0x10
+MPQ_TIMEOUT_G4 = 0x20
 MPQ_TIMEOUT_DRAIN = 0x100
 MPQ_FAULT_BOUNDS = 0x10000            # mpq_device_status: the checked build skipped accesses
 MPQ_BUILD_CHECK_BOUNDS = 0x1          # mpq_build_options: the checked build

@@ -1,5 +1,5 @@
-// Weights in 4-bit integers (include/mpq.h: mpq_g4_matrix): where things lie in a tile, and eight codes as
-// eight 16-bit floats.
+// Weights in 4-bit integers (include/mpq.h: mpq_g4_matrix): where things lie in a tile, and eight codes' values
+// as eight 16-bit floats.
 #pragma once
 
 #include "elements.cuh"
@@ -18,42 +18,75 @@ __host__ __device__ __forceinline__ int g4_shift(int e) { return 4 * (e >> 1) + 
 
 __device__ __forceinline__ float bf16_bits(uint32_t low) { return __uint_as_float(low << 16); }
 
-// q - z of a word's eight codes, exact, as four pairs of T in order (elements 0 and 1, 2 and 3, ..): a code in the low
-// bits of the bits of 2^k, the power whose last place is 1, is 2^k + q, and `from` holds 2^k + z twice.
+// A word's eight values s (q - z), each rounded once to T, as four pairs in order (elements 0 and 1, 2 and 3, ..).  A code
+// in the low bits of the bits of 2^k, the power whose last place is 1, is 2^k + q, so q - z is one exact difference;
+// s is a bf16, which bf16 takes as it is, and fp16 from 2^-17 (the last place of its subnormals is 2^-24) to its
+// largest number: there a product in T is the rounded value.  Other scales' go through fp32.
 template <typename T>
 struct G4Pairs;
 template <>
 struct G4Pairs<__nv_bfloat16> {
+    static constexpr bool kBf16 = true;
     static constexpr uint32_t kPower = 0x43004300u;      // 128
-    __device__ static __forceinline__ uint32_t less(uint32_t w, uint32_t from)
+    // s twice; its bits are a bf16's
+    __device__ static __forceinline__ uint32_t scale(uint32_t bits) { return __byte_perm(bits, 0, 0x1010); }
+    __device__ static __forceinline__ bool plain(uint32_t) { return true; }
+    __device__ static __forceinline__ uint32_t value(uint32_t v, uint32_t from, uint32_t s)
     {
-        const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&w),
-                                         *reinterpret_cast<const __nv_bfloat162 *>(&from));
+        const __nv_bfloat162 r = __hmul2(__hsub2(as(v), as(from)), as(s));
         return *reinterpret_cast<const uint32_t *>(&r);
     }
+    __device__ static __forceinline__ __nv_bfloat162 as(uint32_t v) { return *reinterpret_cast<__nv_bfloat162 *>(&v); }
 };
 template <>
 struct G4Pairs<__half> {
+    static constexpr bool kBf16 = false;
     static constexpr uint32_t kPower = 0x64006400u;      // 1024
-    __device__ static __forceinline__ uint32_t less(uint32_t w, uint32_t from)
+    __device__ static __forceinline__ uint32_t scale(uint32_t bits)
     {
-        const __half2 r = __hsub2(*reinterpret_cast<const __half2 *>(&w),
-                                  *reinterpret_cast<const __half2 *>(&from));
+        const __half2 h = __float2half2_rn(bf16_bits(bits));
+        return *reinterpret_cast<const uint32_t *>(&h);
+    }
+    __device__ static __forceinline__ bool plain(uint32_t bits)      // |s| in [2^-17, 2^15], or 0
+    {
+        const uint32_t m = bits & 0x7fffu;
+        return m - 0x3700u <= 0x4700u - 0x3700u || m == 0;
+    }
+    __device__ static __forceinline__ uint32_t value(uint32_t v, uint32_t from, uint32_t s)
+    {
+        const __half2 r = __hmul2(__hsub2(as(v), as(from)), as(s));
         return *reinterpret_cast<const uint32_t *>(&r);
     }
+    __device__ static __forceinline__ __half2 as(uint32_t v) { return *reinterpret_cast<__half2 *>(&v); }
 };
 
+// A group's scale and zero point as g4_values takes them.
+struct G4Scale {
+    uint32_t s, from, bits;
+};
 template <typename T>
-__device__ __forceinline__ uint32_t g4_from(uint32_t z) { return G4Pairs<T>::kPower | z | z << 16; }
+__device__ __forceinline__ G4Scale g4_scale(uint32_t bits, uint32_t z)
+{
+    return {G4Pairs<T>::scale(bits), G4Pairs<T>::kPower | z | z << 16, bits};
+}
 
 template <typename T>
-__device__ __forceinline__ void g4_pairs(uint32_t w, uint32_t from, uint32_t (&p)[4])
+__device__ __forceinline__ void g4_values(uint32_t w, const G4Scale &g, uint32_t (&p)[4])
 {
+    if (G4Pairs<T>::plain(g.bits)) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        uint32_t v;                          // (w >> 4 j) & 0x000f000f | the power: one operation of three inputs
-        asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(v) : "r"(w >> (4 * j)), "n"(0x000f000f), "n"(G4Pairs<T>::kPower));
-        p[j] = G4Pairs<T>::less(v, from);
+        for (int j = 0; j < 4; ++j) {
+            uint32_t v;                      // (w >> 4 j) & 0x000f000f | the power: one operation of three inputs
+            asm("lop3.b32 %0, %1, %2, %3, 0xea;"
+                : "=r"(v) : "r"(w >> (4 * j)), "n"(0x000f000f), "n"(G4Pairs<T>::kPower));
+            p[j] = G4Pairs<T>::value(v, g.from, g.s);
+        }
+    } else {
+        const float s = bf16_bits(g.bits);
+        const int z = (int)(g.from & 255u);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            p[j] = pack2((float)((int)(w >> (4 * j) & 15u) - z) * s, (float)((int)(w >> (4 * j + 16) & 15u) - z) * s, T());
     }
 }
 

@@ -1,12 +1,10 @@
-// Linear layer of weights in 4-bit integers (mpq_g4_linear): Y[t][c] = sum_j x_tj w_cj + bias_c,
-// w = s (q - z) with s and z by groups of a row.
+// Linear layer of weights in 4-bit integers (mpq_g4_linear): Y[t][c] = sum_j x_tj w_cj + bias_c, w = s (q - z) with
+// s and z by groups of a row, rounded once to x's type.  (bf16 rounds the weight by 2^-9 of it at most, fp16 by
+// 2^-12, beside the 1/30 of a group's largest that its codes are apart: what that buys is one sum over all of K, in
+// the tensor cores' fp32.)  Many tokens: g4_tiles.cu.
 //
-// q - z is a whole number of at most 5 bits, exact in either 16-bit type, so the weights' scales need not be
-// rounded into an operand: a group's products are summed as x (q - z), in fp32, and its sum times s is added to
-// the output's.
-//
-// Few tokens, warp-level MMAs (m16n8k16): a tile's 16 rows are A, eight tokens B.  A lane's 16 bytes of a row hold, for
-// each 32 elements, the eight that it multiplies in two MMAs: the codes become A's registers where they are,
+// A few tokens, warp-level MMAs (m16n8k16): a tile's 16 rows are A, eight tokens B.  A lane's 16 bytes of a row hold,
+// for each 32 elements, the eight that it multiplies in two MMAs: the codes become A's registers where they are,
 // and x's registers are 16 consecutive bytes of its row.  Warps of a CTA take a row tile's tiles in turn and
 // their sums are joined in shared memory in the warps' order.
 #include <math.h>
@@ -22,12 +20,13 @@ namespace mpq {
 namespace {
 
 constexpr int FEW_WARPS = 8;
+constexpr int FEW_TOKENS = 16;
 
 template <typename T>
 __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
                                          uint32_t b0, uint32_t b1)
 {
-    if constexpr (sizeof(T) == 2 && G4Pairs<T>::kPower == G4Pairs<__nv_bfloat16>::kPower)
+    if constexpr (G4Pairs<T>::kBf16)
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
                      "{%8, %9}, {%0, %1, %2, %3};"
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
@@ -91,37 +90,24 @@ g4_few_kernel(const G4Args a, const T *X, void *Y)
         const uint32_t qa[4] = {wa.x, wa.y, wa.z, wa.w}, qb[4] = {wb.x, wb.y, wb.z, wb.w};
         const uint16_t *const sc = reinterpret_cast<const uint16_t *>(tile + G4_CODES);
         const unsigned char *const zs = tile + G4_CODES + 32 * N;
-        float sum[NT][4];
+        G4Scale ga, gb;
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
-            const int grp = m * 32 / GROUP;
             if (m * 32 % GROUP == 0) {
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) sum[n][e] = 0.0f;
+                const int at = m * 32 / GROUP;
+                ga = g4_scale<T>(sc[g * N + at], a.L.zeros ? zs[g * N + at] : G4_ZERO);
+                gb = g4_scale<T>(sc[(g + 8) * N + at], a.L.zeros ? zs[(g + 8) * N + at] : G4_ZERO);
             }
-            const uint32_t za = a.L.zeros ? zs[g * N + grp] : G4_ZERO, zb = a.L.zeros ? zs[(g + 8) * N + grp] : G4_ZERO;
             uint32_t pa[4], pb[4];
-            g4_pairs<T>(qa[m], g4_from<T>(za), pa);
-            g4_pairs<T>(qb[m], g4_from<T>(zb), pb);
+            g4_values<T>(qa[m], ga, pa);
+            g4_values<T>(qb[m], gb, pb);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 const long long t = n0 + n * 8 + g;
                 uint4 x = make_uint4(0, 0, 0, 0);
                 if (t < a.T) x = load_x<T, VEC>(X + t * a.ldx, kt * 128 + m * 32 + i * 8, a.L.d);
-                mma16816<T>(sum[n], pa[0], pb[0], pa[1], pb[1], x.x, x.y);
-                mma16816<T>(sum[n], pa[2], pb[2], pa[3], pb[3], x.z, x.w);
-            }
-            if ((m + 1) * 32 % GROUP == 0) {
-                const float sa = bf16_bits(sc[g * N + grp]), sb = bf16_bits(sc[(g + 8) * N + grp]);
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    acc[n][0] = fmaf(sum[n][0], sa, acc[n][0]);
-                    acc[n][1] = fmaf(sum[n][1], sa, acc[n][1]);
-                    acc[n][2] = fmaf(sum[n][2], sb, acc[n][2]);
-                    acc[n][3] = fmaf(sum[n][3], sb, acc[n][3]);
-                }
+                mma16816<T>(acc[n], pa[0], pb[0], pa[1], pb[1], x.x, x.y);
+                mma16816<T>(acc[n], pa[2], pb[2], pa[3], pb[3], x.z, x.w);
             }
         }
     }
@@ -167,6 +153,7 @@ mpq_status launch_g4_linear(const void *X, int x_type, long long ldx, int T, con
                             const void *W, const float *bias, void *Y, int y_type, long long ldy,
                             cudaStream_t stream)
 {
+    if (T > FEW_TOKENS) return launch_g4_tiles(X, x_type, ldx, T, L, W, bias, Y, y_type, ldy, stream);
     const G4Args a = {*L, static_cast<const unsigned char *>(W), bias, ldx, ldy, T, y_type};
     if (x_type == MPQ_F16) return launch_typed(a, static_cast<const __half *>(X), x_type, Y, stream);
     return launch_typed(a, static_cast<const __nv_bfloat16 *>(X), x_type, Y, stream);

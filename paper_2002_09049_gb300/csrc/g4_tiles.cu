@@ -1,0 +1,584 @@
+// Linear layer of weights in 4-bit integers for more than a few tokens (mpq_g4_linear), on tcgen05 MMAs.
+//
+// 128 channels of weights, s (q - z) rounded to x's type, are the MMA's A (the accumulator's lanes), up to 256
+// tokens its B (columns).  Packed weights come by bulk copies as they lie in memory (a ring of their own, tiles
+// ahead), three groups of four warps turn them by turns into 128-byte-swizzled K-major operands of 64 elements of K, x
+// comes by TMA, and four warps write the outputs.  Roles run over their CTA's tiles without a pause, two
+// accumulators in turn: a tile's outputs leave while the next one is summed.
+//
+// PAIR: CTA pairs (cta_group::2) take 256 channels x 256 tokens, each CTA its own channels and half of the
+// tokens' operand: shared memory takes 64 KB in and out per 64 elements of K, a CTA alone 96 (at 128 bytes a
+// cycle, beside 512 cycles of MMAs).  Else K may be split over the CTAs of a cluster, whose sums are joined in
+// shared memory in the order of the ranks (equal inputs give equal bits).
+//
+// Warps: 0 copies x, 1 issues MMAs (the even CTA's, of a pair), 2 copies weights, 3 tells the MMAs' warp that x has
+// landed, 4..15 make operands, 16..19 (lane quarter warp % 4) write outputs.  Every wait is bounded.
+#include <cuda.h>
+#include <string.h>
+
+#include <algorithm>
+
+#include "g4.cuh"
+#include "pair_common.cuh"
+#include "sm100.cuh"
+#include "token_tiles.cuh"
+#include "waits.cuh"
+
+MPQ_CHECKED_UNIT("g4_tiles.cu");
+
+namespace mpq {
+namespace {
+
+using namespace sm100;
+
+constexpr int H_M = TOKEN_M;             // channels of a CTA's tile
+constexpr int H_K = 64;                  // elements of K in a stage, half a packed tile
+constexpr int H_A_BYTES = H_M * H_K * 2; // A of a stage, rows of 128 bytes
+constexpr int H_MAX_STAGES = 8;
+constexpr int H_MAX_PACKED = 8;
+constexpr int H_MAKERS = 3;              // groups of four warps that make operands
+constexpr int H_MAKE0 = 4, H_OUT0 = H_MAKE0 + 4 * H_MAKERS;          // first warps of the roles
+constexpr int H_THREADS = (H_OUT0 + 4) * 32;
+
+struct TileCtrl {
+    uint64_t x_full[H_MAX_STAGES];       // a stage's x has landed
+    uint64_t ready[H_MAX_STAGES];        // ... and its weights are operands
+    uint64_t empty[H_MAX_STAGES];        // the MMAs that read it completed
+    uint64_t p_full[H_MAX_PACKED];       // packed weights have landed
+    uint64_t p_empty[H_MAX_PACKED];      // and been read
+    uint64_t d_full[2];                  // a tile's MMAs completed
+    uint64_t d_empty[2];                 // its sums have been read
+    uint64_t done;                       // every MMA completed
+    uint32_t tmem_base;
+    int abort;
+};
+constexpr int H_CTRL_BYTES = 1024;
+static_assert(sizeof(TileCtrl) <= H_CTRL_BYTES, "control block");
+
+struct TileArgs {
+    mpq_g4_matrix L;
+    const unsigned char *w;
+    TokenRows rows;
+    int y_type;
+    int n_tile, held;                    // tokens of a tile; of them, in one CTA's shared memory
+    int n_tiles, tiles;                  // tiles along the tokens; all (of a pair, or a cluster)
+    int split;                           // CTAs that share a tile's K
+    int stages, packed;                  // depths of the rings
+    int acc_cols;                        // TMEM columns of one accumulator
+};
+
+__host__ __device__ inline int tile_stage_bytes(int held) { return H_A_BYTES + held * H_K * 2; }
+__host__ __device__ inline int packed_bytes(const mpq_g4_matrix &L) { return 8 * L.tile_bytes; }
+
+// A place in a ring: the slot, and the parity of the phase in which it is filled (emptied: the other).
+struct Place {
+    int at = 0;
+    uint32_t phase = 0;
+    __device__ __forceinline__ void pass(int slots, int count = 1)   // count <= slots
+    {
+        at += count;
+        if (at >= slots) {
+            at -= slots;
+            phase ^= 1u;
+        }
+    }
+};
+
+// D[tmem] (+)= A B^T, kind::f16, one CTA's.
+__device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t more)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(more)
+        : "memory");
+}
+
+// Outputs of channel i (of the lane), 16 tokens from column j0 of n_real on.
+template <typename O>
+__device__ __forceinline__ void store_columns(const TokenRows &r, O *Y, float (&v)[16], int i, int lane,
+                                              long long n0, int j0, int n_real)
+{
+    const size_t size = (r.tokens - 1) * r.ldy + r.channels;
+    if (r.wide) {                        // by quads of lanes, 4 channels of 4 tokens
+        quad_transpose(v, lane);
+        const int c = i & ~3;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int t = j0 + 4 * j + (lane & 3);
+            if (t < n_real && c < r.channels && MPQ_IN((n0 + t) * r.ldy + c + 3, size))
+                store4(Y + (n0 + t) * r.ldy + c, v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+        }
+    } else if (i < r.channels) {
+        O *y = Y + (n0 + j0) * r.ldy + i;
+#pragma unroll
+        for (int j = 0; j < 16; ++j, y += r.ldy)
+            if (j0 + j < n_real && MPQ_IN((n0 + j0 + j) * r.ldy + i, size)) *y = from_f32<O>(v[j]);
+    }
+}
+
+template <typename T, bool PAIR>
+__global__ void __launch_bounds__(H_THREADS, 1)
+g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ CUtensorMap tmX)
+{
+    extern __shared__ unsigned char raw[];
+    unsigned char *const base = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
+    TileCtrl &ctl = *reinterpret_cast<TileCtrl *>(base);
+    unsigned char *const ring = base + H_CTRL_BYTES;
+    const uint32_t ring_u32 = smem_u32(ring);
+    const int sb = tile_stage_bytes(a.held), pb = packed_bytes(a.L);
+    unsigned char *const packed = ring + a.stages * sb;
+    volatile int *const abort_flag = &ctl.abort;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const bool cluster = PAIR || a.split > 1;
+    const int rank = cluster ? (int)cluster_ctarank() : 0, size = PAIR ? 2 : a.split;
+    const int first = (int)blockIdx.x / size, step = (int)gridDim.x / size;
+    const int k_tiles = a.L.k_tiles;
+    // this CTA's share of the row: tiles of 128, stages of 64 (the last tile may have one)
+    const int k0 = PAIR ? 0 : (int)((long long)k_tiles * rank / a.split);
+    const int k1 = PAIR ? k_tiles : (int)((long long)k_tiles * (rank + 1) / a.split);
+    const int halves = min(2 * k1, (a.L.d + H_K - 1) / H_K) - 2 * k0;
+    auto row_tile = [&](int tile) { return PAIR ? tile / a.n_tiles * 2 + rank : tile / a.n_tiles; };
+    auto token0 = [&](int tile) { return (long long)(tile % a.n_tiles) * a.n_tile; };
+    // A wait that gave up, or that another role has given up: true.  (Cluster-scope acquires only where one
+    // thread takes arrivals of the other CTA's warps.)
+    auto failed = [&](uint64_t *bar, uint32_t parity, bool other = false) {
+        auto reached = [&] { return PAIR && other ? mbar_try_wait_cluster(bar, parity) : mbar_try_wait(bar, parity); };
+        if (reached()) return false;
+        const long long t0 = clock64();
+        while (!reached()) {
+            if (*abort_flag) return true;
+            if (clock64() - t0 <= wc.budget) continue;
+            *abort_flag = 1;
+            note_timeout(wc, MPQ_TIMEOUT_G4);
+            return true;
+        }
+        return false;
+    };
+    auto warp_failed = [&](uint64_t *bar, uint32_t parity) { return __any_sync(0xffffffffu, failed(bar, parity)) != 0; };
+    auto arrive = [&](uint64_t *bar) {   // at the CTA whose thread issues MMAs
+        if (PAIR) mbar_arrive_cluster(bar, 0); else mbar_arrive(bar);
+    };
+    auto commit = [&](uint64_t *bar) {
+        if (PAIR) mma_commit_pair(bar, (uint16_t)3); else mma_commit(bar);
+    };
+
+    griddep_launch();
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < a.stages; ++i) {
+            mbar_init(&ctl.x_full[i], 1);
+            mbar_init(&ctl.ready[i], PAIR ? 10 : 5);
+            mbar_init(&ctl.empty[i], 1);
+        }
+        for (int i = 0; i < a.packed; ++i) {
+            mbar_init(&ctl.p_full[i], 1);
+            mbar_init(&ctl.p_empty[i], 4);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&ctl.d_full[i], 1);
+            mbar_init(&ctl.d_empty[i], PAIR ? 8 : 4);
+        }
+        mbar_init(&ctl.done, 1);
+        ctl.abort = 0;
+        fence_barrier_init();
+        if (!MPQ_CHECK_SMEM_END(packed - raw + (size_t)a.packed * pb)) ctl.abort = 1;
+        prefetch_tensormap(&tmX);
+    }
+    if (warp == 1) {
+        if (PAIR)
+            tmem_alloc_pair(&ctl.tmem_base, (uint32_t)(2 * a.acc_cols));
+        else
+            tmem_alloc(&ctl.tmem_base, (uint32_t)(2 * a.acc_cols));
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (PAIR) cluster_sync();            // the barriers that the other CTA arrives on are ready
+    tc_fence_after();
+    const uint32_t tmem = ctl.tmem_base;
+    griddep_wait();
+
+    if (warp == 0) {
+        // -------------------------------------------------------------------- copies of x
+        if (lane == 0 && !wc.withhold) {
+            int n = 0;
+            Place s;
+            bool stop = *abort_flag != 0;
+            for (int tile = first; tile < a.tiles && !stop; tile += step) {
+                const int y0 = (int)token0(tile) + (PAIR ? rank * a.held : 0);
+                for (int h = 0; h < halves; ++h, ++n, s.pass(a.stages)) {
+                    const uint32_t at = ring_u32 + (uint32_t)(s.at * sb + H_A_BYTES);
+                    if ((n >= a.stages && failed(&ctl.empty[s.at], s.phase ^ 1u)) ||
+                        !MPQ_CHECK((at & 1023u) == 0u)) {
+                        stop = true;
+                        break;
+                    }
+                    mbar_arrive_expect_tx(&ctl.x_full[s.at], (uint32_t)(a.held * H_K * 2));
+                    tma_load_2d(at, &tmX, k0 * 128 + h * H_K, y0, &ctl.x_full[s.at]);
+                }
+            }
+            // no copy may land after the CTA is gone
+            for (int i = max(0, n - a.stages); i < n; ++i)
+                drain_wait(&ctl.x_full[i % a.stages], (uint32_t)(i / a.stages) & 1u, wc, MPQ_TIMEOUT_G4);
+        }
+        __syncwarp();
+    } else if (warp == 2) {
+        // -------------------------------------------------------------------- copies of weights
+        int n = 0;
+        Place p;
+        bool stop = wc.withhold || *abort_flag;
+        for (int tile = first; tile < a.tiles && !stop; tile += step) {
+            const int r0 = row_tile(tile) * 8, strips = max(0, min(8, a.L.row_tiles - r0));
+            for (int k = k0; k < k1; ++k, ++n, p.pass(a.packed)) {
+                if (n >= a.packed && warp_failed(&ctl.p_empty[p.at], p.phase ^ 1u)) {
+                    stop = true;
+                    break;
+                }
+                // (a pair's odd CTA may have no channels: it makes what it finds into operands)
+                if (lane == 0) mbar_arrive_expect_tx(&ctl.p_full[p.at], (uint32_t)(strips * a.L.tile_bytes));
+                __syncwarp();
+                if (lane < strips)
+                    bulk_load(smem_u32(packed + p.at * pb + lane * a.L.tile_bytes),
+                              a.w + ((size_t)(r0 + lane) * k_tiles + k) * a.L.tile_bytes, (uint32_t)a.L.tile_bytes,
+                              &ctl.p_full[p.at]);
+            }
+        }
+        for (int i = max(0, n - a.packed); lane == 0 && i < n; ++i)
+            drain_wait(&ctl.p_full[i % a.packed], (uint32_t)(i / a.packed) & 1u, wc, MPQ_TIMEOUT_G4);
+        __syncwarp();
+    } else if (warp == 3) {
+        // -------------------------------------------------------------------- x has landed
+        if (lane == 0) {
+            Place s;
+            bool stop = false;
+            for (int tile = first; tile < a.tiles && !stop; tile += step)
+                for (int h = 0; h < halves && !stop; ++h, s.pass(a.stages)) {
+                    stop = failed(&ctl.x_full[s.at], s.phase);
+                    if (!stop) arrive(&ctl.ready[s.at]);
+                }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        // -------------------------------------------------------------------- MMAs
+        if (lane == 0 && (!PAIR || rank == 0)) {
+            int t = 0;                   // tiles so far
+            Place s;
+            bool stop = false;
+            for (int tile = first; tile < a.tiles && !stop; tile += step, ++t) {
+                const int real = (int)min((long long)a.n_tile, a.rows.tokens - token0(tile));
+                const int m = PAIR ? 2 * H_M : H_M, cols = PAIR ? 256 : (real + 15) / 16 * 16, b = t & 1;
+                const uint32_t id = G4Pairs<T>::kBf16 ? idesc_bf16(m, cols) : idesc_f16(m, cols);
+                const uint32_t d = tmem + (uint32_t)(b * a.acc_cols);
+                if (t >= 2 && failed(&ctl.d_empty[b], (uint32_t)((t >> 1) - 1) & 1u, true)) break;
+                for (int h = 0; h < halves; ++h, s.pass(a.stages)) {
+                    if (failed(&ctl.ready[s.at], s.phase, true)) {
+                        stop = true;
+                        break;
+                    }
+                    tc_fence_after();
+                    const uint32_t at = ring_u32 + (uint32_t)(s.at * sb);
+                    const uint64_t ad = smem_desc_sw128(at), bd = smem_desc_sw128(at + H_A_BYTES);
+#pragma unroll
+                    for (int j = 0; j < H_K / 16; ++j) {             // 32 bytes a step, in 16 B units
+                        const uint32_t more = h > 0 || j > 0 ? 1u : 0u;
+                        if (PAIR)
+                            mma_f16_pair(d, ad + 2 * j, bd + 2 * j, id, more);
+                        else
+                            mma_f16(d, ad + 2 * j, bd + 2 * j, id, more);
+                    }
+                    commit(&ctl.empty[s.at]);
+                }
+                if (!stop) commit(&ctl.d_full[b]);
+            }
+            // every MMA issued above completes before tensor memory is released
+            commit(&ctl.done);
+        }
+        if (lane == 0) drain_wait_cluster(&ctl.done, 0, wc, MPQ_TIMEOUT_G4);
+        __syncwarp();
+    } else if (warp < H_OUT0) {
+        // -------------------------------------------------------------------- operands from packed weights
+        // Lanes by eights (what shared memory serves at once): rows r and r ^ 5, four words each -- r and r ^ 5
+        // begin in different halves of the packed rows' 64 bytes and of the operand's swizzled 128.
+        const int own = (warp - H_MAKE0) >> 2, i = lane & 3, r8 = (lane >> 3) ^ ((lane & 4) ? 5 : 0);
+        const int row0 = (warp & 3) * 32 + r8, groups = 128 / a.L.group;
+        int turn = 0;                    // of the groups
+        bool again = false;              // every stage has been filled once
+        Place p, s;
+        bool stop = false;
+        for (int tile = first; tile < a.tiles && !stop; tile += step) {
+            for (int k = k0; k < k1; ++k, p.pass(a.packed)) {
+                const int count = min(2, halves - 2 * (k - k0));
+                const bool mine = turn == own;
+                turn = turn == H_MAKERS - 1 ? 0 : turn + 1;
+                if (!mine) {
+                    again |= s.at + count >= a.stages;
+                    s.pass(a.stages, count);
+                    continue;
+                }
+                if (warp_failed(&ctl.p_full[p.at], p.phase)) {
+                    stop = true;
+                    break;
+                }
+                uint4 w[4];
+                uint2 sc[4];             // the row's scales, two a word
+                uint32_t z[4];           // and zero points, of the tile's quarters
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const int row = row0 + 8 * u;
+                    const unsigned char *const t = packed + p.at * pb + (row >> 4) * a.L.tile_bytes;
+                    w[u] = *reinterpret_cast<const uint4 *>(t + (row & 15) * 64 + i * 16);
+                    const unsigned char *const ss = t + G4_CODES + (row & 15) * 2 * groups;
+                    if (groups == 1) {
+                        sc[u].x = *reinterpret_cast<const uint16_t *>(ss) * 0x10001u;
+                        sc[u].y = sc[u].x;
+                    } else if (groups == 2) {
+                        const uint32_t two = *reinterpret_cast<const uint32_t *>(ss);
+                        sc[u] = make_uint2(__byte_perm(two, 0, 0x1010), __byte_perm(two, 0, 0x3232));
+                    } else {
+                        sc[u] = *reinterpret_cast<const uint2 *>(ss);
+                    }
+                    z[u] = 0x08080808u;
+                    if (a.L.zeros) {
+                        const unsigned char *const zs = t + G4_CODES + 32 * groups + (row & 15) * groups;
+                        z[u] = groups == 4   ? *reinterpret_cast<const uint32_t *>(zs)
+                               : groups == 2 ? __byte_perm(*reinterpret_cast<const uint16_t *>(zs), 0, 0x1100)
+                                             : __byte_perm(*zs, 0, 0x0000);
+                    }
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&ctl.p_empty[p.at]);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (h >= count) break;
+                    if (again && warp_failed(&ctl.empty[s.at], s.phase ^ 1u)) {
+                        stop = true;
+                        break;
+                    }
+                    const uint32_t at = ring_u32 + (uint32_t)(s.at * sb);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        const uint32_t q[4] = {w[u].x, w[u].y, w[u].z, w[u].w}, two = h ? sc[u].y : sc[u].x;
+                        const uint32_t to = at + (uint32_t)((row0 + 8 * u) * 128);
+#pragma unroll
+                        for (int m = 0; m < 2; ++m) {
+                            const G4Scale g = g4_scale<T>(m ? two >> 16 : two & 0xffffu, z[u] >> (8 * (2 * h + m)) & 255u);
+                            uint32_t v[4];
+                            g4_values<T>(q[2 * h + m], g, v);
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
+                                         :: "r"(to + (uint32_t)(((4 * m + i) ^ r8) * 16)), "r"(v[0]), "r"(v[1]),
+                                            "r"(v[2]), "r"(v[3])
+                                         : "memory");
+                        }
+                    }
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) arrive(&ctl.ready[s.at]);
+                    again |= s.at + 1 == a.stages;
+                    s.pass(a.stages);
+                }
+                if (stop) break;
+            }
+        }
+    } else {
+        // -------------------------------------------------------------------- outputs
+        const int q = warp & 3, row = q * 32 + lane;
+        int t = 0;
+        for (int tile = first; tile < a.tiles; tile += step, ++t) {
+            const long long n0 = token0(tile);
+            const int real = (int)min((long long)a.n_tile, a.rows.tokens - n0), b = t & 1;
+            const int c = row_tile(tile) * H_M + row;
+            const float bias = a.split == 1 && a.rows.bias && c < a.rows.channels ? a.rows.bias[c] : 0.0f;
+            if (warp_failed(&ctl.d_full[b], (uint32_t)(t >> 1) & 1u)) break;
+            tc_fence_after();
+            const uint32_t from = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(b * a.acc_cols);
+            for (int j0 = 0; j0 < real; j0 += 16) {
+                float v[16];
+                __syncwarp();
+                tmem_ld_32x32b_x16(from + (uint32_t)j0, v);
+                if (!PAIR && a.split > 1) {          // [token][128 channels]; the MMAs have read the ring
+                    float *const part = reinterpret_cast<float *>(ring) + row;
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) part[(j0 + j) * H_M] = v[j];
+                    continue;
+                }
+#pragma unroll
+                for (int j = 0; j < 16; ++j) v[j] += bias;
+                if (a.y_type == MPQ_F32)
+                    store_columns(a.rows, static_cast<float *>(Y), v, c, lane, n0, j0, real);
+                else if (a.y_type == MPQ_F16)
+                    store_columns(a.rows, static_cast<__half *>(Y), v, c, lane, n0, j0, real);
+                else
+                    store_columns(a.rows, static_cast<__nv_bfloat16 *>(Y), v, c, lane, n0, j0, real);
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) arrive(&ctl.d_empty[b]);
+        }
+    }
+
+    if (!PAIR && a.split > 1) {
+        cluster_sync();                  // every rank's sums are in its shared memory
+        const long long n0 = token0(first);
+        const JoinAt at{reinterpret_cast<const float *>(ring), n0,
+                        (int)min((long long)a.n_tile, a.rows.tokens - n0), row_tile(first), rank};
+        if (a.y_type == MPQ_F32)
+            join_split(a.rows, static_cast<float *>(Y), at, a.split);
+        else if (a.y_type == MPQ_F16)
+            join_split(a.rows, static_cast<__half *>(Y), at, a.split);
+        else
+            join_split(a.rows, static_cast<__nv_bfloat16 *>(Y), at, a.split);
+    }
+    if (cluster)
+        cluster_sync();                  // no CTA leaves while its sums are read, or arrivals to it are on their way
+    else
+        __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        if (PAIR)
+            tmem_dealloc_pair(tmem, (uint32_t)(2 * a.acc_cols));
+        else
+            tmem_dealloc(tmem, (uint32_t)(2 * a.acc_cols));
+    }
+}
+
+// Rows of x where a tile copy cannot read them, `to` elements apart and 16-byte aligned, the rest zeros.
+__global__ void __launch_bounds__(256)
+g4_rows_kernel(const uint16_t *X, long long ldx, int T, int d, uint16_t *to, int dp)
+{
+    griddep_launch();
+    griddep_wait();
+    const long long n = (long long)T * (dp / 8), step = (long long)gridDim.x * blockDim.x;
+    for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += step) {
+        const long long t = i / (dp / 8);
+        const int j = (int)(i - t * (dp / 8)) * 8;
+        const uint16_t *const x = X + t * ldx;
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            w[e] = (j + 2 * e < d ? x[j + 2 * e] : 0u) | (j + 2 * e + 1 < d ? (uint32_t)x[j + 2 * e + 1] : 0u) << 16;
+        if (MPQ_IN(t * dp + j + 7, (long long)T * dp))
+            *reinterpret_cast<uint4 *>(to + t * dp + j) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+template <typename T, bool PAIR>
+mpq_status launch_tiles(const TileArgs &a, const CUtensorMap &tmX, void *Y, int ctas, cudaStream_t stream)
+{
+    const size_t smem = 1024 + H_CTRL_BYTES + (size_t)a.stages * tile_stage_bytes(a.held) +
+                        (size_t)a.packed * packed_bytes(a.L);
+    static std::atomic<int> limit[kMaxDevices];
+    cudaError_t e = allow_smem(reinterpret_cast<const void *>(g4_tiles_kernel<T, PAIR>), limit, smem);
+    if (e != cudaSuccess) return cuda_status(e, "cudaFuncSetAttribute");
+    WaitCtl wc;
+    const mpq_status ws = wait_ctl(&wc);
+    if (ws != MPQ_OK) return ws;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)ctas);
+    cfg.blockDim = dim3(H_THREADS);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0] = after_previous_kernel();
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = PAIR ? 2u : (unsigned)a.split;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    e = cudaLaunchKernelEx(&cfg, g4_tiles_kernel<T, PAIR>, a, Y, wc, tmX);
+    return cuda_status(e != cudaSuccess ? e : cudaGetLastError(), "g4 linear launch");
+}
+
+template <typename T>
+mpq_status launch_form(const TileArgs &a, bool pair, const CUtensorMap &tmX, void *Y, int ctas, cudaStream_t stream)
+{
+    return pair ? launch_tiles<T, true>(a, tmX, Y, ctas, stream) : launch_tiles<T, false>(a, tmX, Y, ctas, stream);
+}
+
+struct Form {
+    int n;                               // tokens of a tile
+    bool pair;
+    int split;
+};
+
+// Pairs for more than a tile of tokens; else as many CTAs share a tile's K as leave each one an SM, with four tiles
+// of 128 or more.
+Form choose_form(int T, int C, int k_tiles, int sms)
+{
+    Form f = {std::min(256, (T + 15) / 16 * 16), T > 256, 1};
+    const long long tiles = ((long long)C + H_M - 1) / H_M * ((T + f.n - 1) / f.n);
+    while (!f.pair && f.split < TOKEN_MAX_SPLIT && tiles * f.split * 2 <= sms && k_tiles >= f.split * 4) f.split *= 2;
+    return f;
+}
+
+}  // namespace
+
+mpq_status launch_g4_tiles(const void *X, int x_type, long long ldx, int T, const mpq_g4_matrix *L, const void *W,
+                           const float *bias, void *Y, int y_type, long long ldy, cudaStream_t stream)
+{
+    TileArgs a = {};
+    a.L = *L;
+    a.w = static_cast<const unsigned char *>(W);
+    a.y_type = y_type;
+    const int C = L->rows, four = 4 * type_size(y_type), sms = sm_count();
+    a.rows = {T, C, C % 4 == 0 && ldy % 4 == 0 && (uintptr_t)Y % four == 0, bias, ldy};
+    const Form f = choose_form(T, C, L->k_tiles, sms);
+    a.n_tile = f.n;
+    a.held = f.pair ? f.n / 2 : f.n;
+    a.split = f.pair ? 1 : f.split;
+    a.acc_cols = 32;
+    while (a.acc_cols < f.n) a.acc_cols *= 2;
+    a.n_tiles = (T + f.n - 1) / f.n;
+    const long long tiles = ((long long)C + (f.pair ? 2 : 1) * H_M - 1) / ((f.pair ? 2 : 1) * H_M) * a.n_tiles;
+    if (tiles > (1 << 28)) {
+        set_error("g4 linear: T = %d, C = %d are too large", T, C);
+        return MPQ_ERR_UNSUPPORTED;
+    }
+    a.tiles = (int)tiles;
+    // two tiles' packed weights or more, as many stages as fit beside them, then more packed tiles
+    const int room = max_smem_optin() - 1024 - H_CTRL_BYTES, pb = packed_bytes(*L), sb = tile_stage_bytes(a.held);
+    a.stages = std::min(H_MAX_STAGES, (room - 3 * pb) / sb);
+    a.packed = std::min(H_MAX_PACKED, (room - a.stages * sb) / pb);
+    const int ctas = f.pair      ? 2 * std::min(a.tiles, sms / 2)
+                     : f.split > 1 ? a.tiles * f.split
+                                   : std::min(a.tiles, sms);
+
+    void *scratch = nullptr;
+    int dp = L->d;
+    if (!rows_aligned(X, x_type, T > 1 ? ldx : 0)) {
+        dp = (L->d + 7) / 8 * 8;
+        const mpq_status st = pool_scratch(&scratch, (size_t)T * dp * 2, stream);
+        if (st != MPQ_OK) return st;
+        const long long n = (long long)T * (dp / 8);
+        const mpq_status ls = launch_waiting(g4_rows_kernel, dim3((unsigned)std::min((n + 255) / 256, 16LL * sms)),
+                                             dim3(256), 0, stream, "g4 rows launch", static_cast<const uint16_t *>(X),
+                                             ldx, T, L->d, static_cast<uint16_t *>(scratch), dp);
+        if (ls != MPQ_OK) {
+            cudaFreeAsync(scratch, stream);
+            return ls;
+        }
+        X = scratch;
+        ldx = dp;
+    }
+    CUtensorMap tmX;
+    memset(&tmX, 0, sizeof(tmX));
+    const cuuint64_t dims[2] = {(cuuint64_t)dp, (cuuint64_t)T};
+    const cuuint64_t strides[1] = {(cuuint64_t)(T > 1 ? ldx : (dp + 7) / 8 * 8) * 2};
+    const cuuint32_t box[2] = {64, (cuuint32_t)a.held};
+    mpq_status st = MPQ_OK;
+    if (!encode_tile_map(&tmX, x_type == MPQ_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
+                         X, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B)) {
+        set_error("g4 linear: tensor map encoding failed");
+        st = MPQ_ERR_CUDA;
+    } else if (x_type == MPQ_F16) {
+        st = launch_form<__half>(a, f.pair, tmX, Y, ctas, stream);
+    } else {
+        st = launch_form<__nv_bfloat16>(a, f.pair, tmX, Y, ctas, stream);
+    }
+    if (scratch) {
+        const cudaError_t e = cudaFreeAsync(scratch, stream);
+        if (st == MPQ_OK) st = cuda_status(e, "cudaFreeAsync");
+    }
+    return st;
+}
+
+}  // namespace mpq

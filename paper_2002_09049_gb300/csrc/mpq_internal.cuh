@@ -160,6 +160,10 @@ mpq_status launch_g4_dequantize(const void *packed, const mpq_g4_matrix *L, void
 mpq_status launch_g4_linear(const void *X, int x_type, long long ldx, int T, const mpq_g4_matrix *L,
                             const void *W, const float *bias, void *Y, int y_type, long long ldy,
                             cudaStream_t stream);
+// The form for many tokens (g4_tiles.cu).
+mpq_status launch_g4_tiles(const void *X, int x_type, long long ldx, int T, const mpq_g4_matrix *L,
+                           const void *W, const float *bias, void *Y, int y_type, long long ldy,
+                           cudaStream_t stream);
 mpq_status launch_rotate(const mpq_rotate_rows *q, const mpq_rotate_rows *k, int type, int T, int dim,
                          const int *positions, int shift, const uint64_t *turns, int rot, int neighbours,
                          int norm, float eps, cudaStream_t stream);

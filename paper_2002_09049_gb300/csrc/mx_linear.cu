@@ -41,6 +41,7 @@
 #include "mx_ops.cuh"
 #include "pair_common.cuh"
 #include "sm100.cuh"
+#include "token_tiles.cuh"
 #include "waits.cuh"
 
 MPQ_CHECKED_UNIT("mx_linear.cu");
@@ -57,7 +58,7 @@ constexpr int X_SF = 512;                // bytes of a scale tile (128 rows x 12
 constexpr int X_A_BYTES = X_M * X_ROW;
 constexpr int X_MAX_STAGES = 8;
 constexpr int X_THREADS = 320;           // at most: warps 6..9 may be left out
-constexpr int X_MAX_SPLIT = 8;           // CTAs of a cluster that splits K
+constexpr int X_MAX_SPLIT = TOKEN_MAX_SPLIT;    // CTAs of a cluster that splits K
 
 struct MxCtrl {
     uint64_t full[X_MAX_STAGES];         // a stage's tiles and scales have landed
@@ -92,79 +93,6 @@ __host__ __device__ inline int sf_cols(int n_tile) { return 8 + 2 * sf_b_cols(n_
 __host__ __device__ inline int stage_bytes(const MxArgs &a)
 {
     return X_A_BYTES + a.b_held * X_ROW + 2 * X_SF + sf_b_bytes(a.n_tile);
-}
-
-// v[4 j + k] of the four lanes 4 q .. 4 q + 3 (lane l: channel l, k: token) to v[4 j + k] with lane l:
-// token l, k: channel -- 4 x 4 transposes by two exchanges.
-__device__ __forceinline__ void quad_transpose(float (&v)[16], int lane)
-{
-#pragma unroll
-    for (int o = 1; o <= 2; o <<= 1) {
-        const bool high = lane & o;
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            if (j & o) continue;
-            const float give = high ? v[j] : v[j + o];
-            const float got = __shfl_xor_sync(0xffffffffu, give, o);
-            if (high) v[j] = got; else v[j + o] = got;
-        }
-    }
-}
-
-__device__ __forceinline__ void store4(float *p, float a, float b, float c, float d)
-{
-    *reinterpret_cast<float4 *>(p) = make_float4(a, b, c, d);
-}
-template <typename T>
-__device__ __forceinline__ void store4(T *p, float a, float b, float c, float d)
-{
-    *reinterpret_cast<uint2 *>(p) = make_uint2(pack2(a, b, T()), pack2(c, d, T()));
-}
-
-struct JoinAt {
-    const float *part;                   // this rank's sums, [token][128 channels]
-    long long n0;
-    int n_real, tile, rank;
-};
-
-// The sums of a cluster's R ranks, in rank order; four channels to a thread, eight loads in flight.
-template <typename T, int R>
-__device__ __forceinline__ void join(const MxArgs &a, T *Y, const JoinAt &at)
-{
-    constexpr int U = 8 / R;
-    static_assert(X_MAX_SPLIT == 8, "ranks to join");
-    const int quads = at.n_real * (X_M / 4), step = R * (int)blockDim.x;
-    const size_t size = (a.b_rows - 1) * a.ldy + a.a_rows;
-    for (int i0 = (int)threadIdx.x + at.rank * (int)blockDim.x; i0 < quads; i0 += U * step) {
-        float4 p[U][R];
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-                p[u][r] = ld_dsmem_f32x4(at.part + min(i0 + u * step, quads - 1) * 4, (uint32_t)r);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int i = i0 + u * step;
-            const int t = i / (X_M / 4), c = at.tile * X_M + (i % (X_M / 4)) * 4;
-            if (i >= quads || c >= a.a_rows) continue;
-            float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-                v[0] += p[u][r].x, v[1] += p[u][r].y, v[2] += p[u][r].z, v[3] += p[u][r].w;
-            if (a.bias) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] += c + e < a.a_rows ? a.bias[c + e] : 0.0f;
-            }
-            T *const y = Y + (at.n0 + t) * a.ldy + c;
-            if (a.wide) {
-                if (MPQ_IN((at.n0 + t) * a.ldy + c + 3, size)) store4(y, v[0], v[1], v[2], v[3]);
-                continue;
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (c + e < a.a_rows && MPQ_IN((at.n0 + t) * a.ldy + c + e, size)) y[e] = from_f32<T>(v[e]);
-        }
-    }
 }
 
 // MANY: A is the inputs, B the weights; a cluster is a CTA pair.  Else A is the weights, B the inputs, K split
@@ -419,13 +347,9 @@ mx_linear_kernel(const MxArgs a, T *Y, WaitCtl wc, const __grid_constant__ CUten
 
     if (!MANY && a.split > 1) {
         cluster_sync();                  // every rank's sums are in its shared memory
+        const TokenRows rows{a.b_rows, a.a_rows, a.wide, a.bias, a.ldy};
         const JoinAt at{reinterpret_cast<const float *>(ring), n0, n_real, tile, rank};
-        if (a.split == 2)
-            join<T, 2>(a, Y, at);
-        else if (a.split == 4)
-            join<T, 4>(a, Y, at);
-        else
-            join<T, 8>(a, Y, at);
+        join_split(rows, Y, at, a.split);
     }
     if (cluster)
         cluster_sync();                  // no rank leaves while its sums are read, or copies to it land

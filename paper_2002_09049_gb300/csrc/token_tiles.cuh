@@ -1,0 +1,108 @@
+// The way out of a linear layer's tiles whose accumulators hold 128 channels on the tensor memory's lanes and
+// tokens on its columns (mx_linear.cu, g4_tiles.cu): outputs by quads of channels, and the sums of a cluster
+// that shares a tile's K, joined in the order of its ranks.
+#pragma once
+
+#include <algorithm>
+
+#include "elements.cuh"
+#include "mpq_internal.cuh"
+#include "mx_ops.cuh"
+
+namespace mpq {
+
+constexpr int TOKEN_M = 128;             // channels of a tile
+constexpr int TOKEN_MAX_SPLIT = 8;       // CTAs of a cluster that splits K
+
+// Outputs [tokens][channels], rows ldy apart; wide: they take 4 at a time.
+struct TokenRows {
+    int tokens, channels, wide;
+    const float *bias;
+    long long ldy;
+};
+
+// v[4 j + k] of the four lanes 4 q .. 4 q + 3 (lane l: channel l, k: token) to v[4 j + k] with lane l:
+// token l, k: channel -- 4 x 4 transposes by two exchanges.
+__device__ __forceinline__ void quad_transpose(float (&v)[16], int lane)
+{
+#pragma unroll
+    for (int o = 1; o <= 2; o <<= 1) {
+        const bool high = lane & o;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            if (j & o) continue;
+            const float give = high ? v[j] : v[j + o];
+            const float got = __shfl_xor_sync(0xffffffffu, give, o);
+            if (high) v[j] = got; else v[j + o] = got;
+        }
+    }
+}
+
+__device__ __forceinline__ void store4(float *p, float a, float b, float c, float d)
+{
+    *reinterpret_cast<float4 *>(p) = make_float4(a, b, c, d);
+}
+template <typename T>
+__device__ __forceinline__ void store4(T *p, float a, float b, float c, float d)
+{
+    *reinterpret_cast<uint2 *>(p) = make_uint2(pack2(a, b, T()), pack2(c, d, T()));
+}
+
+struct JoinAt {
+    const float *part;                   // this rank's sums, [token][128 channels]
+    long long n0;
+    int n_real, tile, rank;
+};
+
+// The sums of a cluster's R ranks, in rank order; four channels to a thread, eight loads in flight.
+template <typename T, int R>
+__device__ __forceinline__ void join(const TokenRows &a, T *Y, const JoinAt &at)
+{
+    constexpr int U = 8 / R;
+    static_assert(TOKEN_MAX_SPLIT == 8, "ranks to join");
+    const int quads = at.n_real * (TOKEN_M / 4), step = R * (int)blockDim.x;
+    const size_t size = (a.tokens - 1) * a.ldy + a.channels;
+    for (int i0 = (int)threadIdx.x + at.rank * (int)blockDim.x; i0 < quads; i0 += U * step) {
+        float4 p[U][R];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                p[u][r] = sm100::ld_dsmem_f32x4(at.part + min(i0 + u * step, quads - 1) * 4, (uint32_t)r);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = i0 + u * step;
+            const int t = i / (TOKEN_M / 4), c = at.tile * TOKEN_M + (i % (TOKEN_M / 4)) * 4;
+            if (i >= quads || c >= a.channels) continue;
+            float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                v[0] += p[u][r].x, v[1] += p[u][r].y, v[2] += p[u][r].z, v[3] += p[u][r].w;
+            if (a.bias) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] += c + e < a.channels ? a.bias[c + e] : 0.0f;
+            }
+            T *const y = Y + (at.n0 + t) * a.ldy + c;
+            if (a.wide) {
+                if (MPQ_IN((at.n0 + t) * a.ldy + c + 3, size)) store4(y, v[0], v[1], v[2], v[3]);
+                continue;
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (c + e < a.channels && MPQ_IN((at.n0 + t) * a.ldy + c + e, size)) y[e] = from_f32<T>(v[e]);
+        }
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void join_split(const TokenRows &a, T *Y, const JoinAt &at, int split)
+{
+    if (split == 2)
+        join<T, 2>(a, Y, at);
+    else if (split == 4)
+        join<T, 4>(a, Y, at);
+    else
+        join<T, 8>(a, Y, at);
+}
+
+}  // namespace mpq

@@ -1,11 +1,11 @@
 """4-bit integer weights on the GPU: codes, zero points and scales bit for bit against the definition, the
 values they stand for, and the linear layer against 64-bit sums of the same values.
 
-The linear layer's bound: products are exact, and each fp32 addition or product of a sum -- d of a group's products, one
-of each group, up to 12 where CTAs' and warps' sums are joined -- is off by at most one unit in the last place of a
-partial sum, which the sum of magnitudes bounds: |y - exact| <= (d + ceil(d / 32) + 12) 2^-23 sum_j |x_j w_j| (+
-the bias's addition, 2^-23 (|y| + |bias|)); the output's rounding adds 2^-24, 2^-11 or 2^-8 of |y| (fp32,
-fp16, bf16; fp16 also 2^-25 absolutely, and infinities past its range)."""
+The linear layer's bound: products of x and the weights' values in x's type are exact, and each fp32 addition of a
+sum -- d products, up to 16 where CTAs' and warps' sums are joined -- is off by at most one unit in the last place of a
+partial sum, which the sum of magnitudes bounds: |y - exact| <= (d + 16) 2^-23 sum_j |x_j w_j| (+ the bias's
+addition, 2^-23 (|y| + |bias|)); the output's rounding adds 2^-24, 2^-11 or 2^-8 of |y| (fp32, fp16, bf16;
+fp16 also 2^-25 absolutely, and infinities past its range)."""
 import numpy as np
 import pytest
 import torch
@@ -116,8 +116,8 @@ def test_every_code(gpu, group, zeros):
     for T in (3, 40, 300):
         x = torch.randn(T, d, generator=torch.Generator().manual_seed(T)).to(torch.bfloat16)
         y = binding.mpq_g4_linear(x.to(DEV), packed, lay, dtype=torch.float32)
-        w = torch.from_numpy(values)
-        tol = (d + d // 32 + 12) * 2.0 ** -23 * (x.double().abs() @ w.abs().T)
+        w = torch.from_numpy(values).to(torch.float32).to(torch.bfloat16).double()     # (exact in fp32)
+        tol = (d + 16) * 2.0 ** -23 * (x.double().abs() @ w.abs().T)
         assert bool(((y.cpu().double() - x.double() @ w.T).abs() <= tol).all())
 
 
@@ -131,9 +131,9 @@ def layer(T, C, d, group, zeros, dtype, out, bias, seed, pad=0, shift=0):
     rows = flat[shift:shift + T * (d + pad)].view(T, d + pad)[:, :d]
     rows.copy_(x)
     b = torch.randn(C, generator=torch.Generator().manual_seed(seed)).to(DEV) if bias else None
-    xv, wv = x.to(DEV).double(), binding.mpq_g4_dequantize(packed, lay).double()
+    xv, wv = x.to(DEV).double(), binding.mpq_g4_dequantize(packed, lay, dtype=TYPES[dtype]).double()
     want = xv @ wv.T
-    tol = (d + -(-d // 32) + 12) * 2.0 ** -23 * (xv.abs() @ wv.abs().T)
+    tol = (d + 16) * 2.0 ** -23 * (xv.abs() @ wv.abs().T)
     if bias:
         want = want + b.double()
         tol = tol + 2.0 ** -23 * (want.abs() + b.double().abs())
@@ -198,6 +198,31 @@ def test_linear_repeats_bits_and_leaves_the_rest(gpu, T, C, d):
             call(Y=buf[:T, :C])
             assert torch.equal(buf[:T, :C], y)
         assert bool((buf[:, C:] == 3.0).all()) and bool((buf[T] == 3.0).all())
+
+
+@pytest.mark.parametrize("T", [3, 30, 300])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_weights_of_every_size(gpu, T, dtype):
+    """Scales over the range of bf16, in fp16 too those whose values are subnormal, vanish or overflow: the values
+    that the matrix stands for in x's type, bit for bit (x is one row of the identity at a time)."""
+    d = 64
+    s = np.exp2(np.arange(-140, 126, dtype=np.float64)).astype(np.float32)
+    s = ref.bf16(np.concatenate([s, s * 1.5078125, -s * 1.9921875]))[:, None].repeat(d // 32, 1)
+    q = np.random.default_rng(1).integers(0, 16, (len(s), d)).astype(np.uint8)
+    z = np.random.default_rng(2).integers(0, 16, s.shape).astype(np.uint8)
+    pad = lambda a, n: np.concatenate([a, np.zeros((len(a), n), a.dtype)], 1)
+    packed = packed_of(pad(q, 64), pad(z, 2), pad(s, 2), True).to(DEV)
+    lay = binding.mpq_g4_layout(len(s), d, 32, True)
+    want = binding.mpq_g4_dequantize(packed, lay, dtype=TYPES[dtype])
+    x = torch.zeros(T, d, dtype=TYPES[dtype], device=DEV)
+    rows = torch.arange(T, device=DEV) % d
+    x[torch.arange(T, device=DEV), rows] = 1
+    finite = torch.isfinite(want).all(1)                            # (0 times infinity is NaN)
+    y = binding.mpq_g4_linear(x, packed, lay, dtype=torch.float32)
+    small = want.abs() < 2.0 ** -126                                # (fp32 sums may drop their subnormals)
+    got = y[:, finite].T
+    assert torch.equal(torch.where(small[finite][:, rows], 0.0, got),
+                       torch.where(small, torch.zeros_like(want), want)[finite][:, rows].float())
 
 
 @pytest.mark.parametrize("T", [5, 24, 130, 1500])
@@ -294,3 +319,23 @@ def test_refusals(gpu):
         binding.mpq_g4_linear(b, p, lay, Y=torch.zeros(4, 4, device=DEV, dtype=torch.int32))
     with pytest.raises(binding.MPQError):
         binding.mpq_g4_layout(4, 64, 48)
+
+
+@pytest.mark.parametrize("T,C,d", [(40, 300, 512), (40, 300, 4096), (200, 500, 300), (700, 4000, 300)])
+def test_linear_withheld_copies_time_out(gpu, T, C, d):
+    """With the test hook on, the kernel's waits run out with nothing in flight: the status says so, and the
+    same call is right again after (K whole, K split over a cluster, CTA pairs)."""
+    call, _, _ = layer(T, C, d, 64, False, "bf16", "bf16", False, 3)
+    good = call()
+    assert binding.mpq_device_status() == 0
+    try:
+        binding.mpq_set_wait_limit(1 << 18)
+        binding.mpq_test_withhold_copies(True)
+        call()
+        flags = binding.mpq_device_status()
+    finally:
+        binding.mpq_test_withhold_copies(False)
+        binding.mpq_set_wait_limit(0)
+    assert flags == binding.MPQ_TIMEOUT_G4
+    assert torch.equal(call(), good)
+    assert binding.mpq_device_status() == 0
