@@ -2,17 +2,18 @@
 //
 // 128 channels of weights, s (q - z) rounded to x's type, are the MMA's A (the accumulator's lanes), up to 256
 // tokens its B (columns).  Packed weights come by bulk copies as they lie in memory (a ring of their own, tiles
-// ahead), three groups of four warps turn them by turns into 128-byte-swizzled K-major operands of 64 elements of K, x
-// comes by TMA, and four warps write the outputs.  Roles run over their CTA's tiles without a pause, two
-// accumulators in turn: a tile's outputs leave while the next one is summed.
+// ahead), and three groups of four warps turn them by turns into operands of 64 elements of K in tensor memory, a
+// channel to a lane; x comes by TMA into 128-byte-swizzled shared memory.  (Operands in shared memory too, 141 us
+// for 2,048 x 11,008 x 4,096: 64 KB in and out per 64 elements of K of a pair's CTA are 512 cycles at 128 bytes each,
+// as many as the MMAs take.)  Eight warps write the outputs.  Roles run over their CTA's tiles without a
+// pause; up to 128 tokens two accumulators take turns, and a tile's outputs leave while the next one is summed.
 //
 // PAIR: CTA pairs (cta_group::2) take 256 channels x 256 tokens, each CTA its own channels and half of the
-// tokens' operand: shared memory takes 64 KB in and out per 64 elements of K, a CTA alone 96 (at 128 bytes a
-// cycle, beside 512 cycles of MMAs).  Else K may be split over the CTAs of a cluster, whose sums are joined in
-// shared memory in the order of the ranks (equal inputs give equal bits).
+// tokens' operand.  Else K may be split over the CTAs of a cluster, whose sums are joined in shared memory in the
+// order of the ranks (equal inputs give equal bits).
 //
 // Warps: 0 copies x, 1 issues MMAs (the even CTA's, of a pair), 2 copies weights, 3 tells the MMAs' warp that x has
-// landed, 4..15 make operands, 16..19 (lane quarter warp % 4) write outputs.  Every wait is bounded.
+// landed, 4..15 make operands, 16..23 write outputs (these two by lane quarters, warp % 4).  Every wait is bounded.
 #include <cuda.h>
 #include <string.h>
 
@@ -33,12 +34,16 @@ using namespace sm100;
 
 constexpr int H_M = TOKEN_M;             // channels of a CTA's tile
 constexpr int H_K = 64;                  // elements of K in a stage, half a packed tile
-constexpr int H_A_BYTES = H_M * H_K * 2; // A of a stage, rows of 128 bytes
+constexpr int H_A_COLS = H_K / 2;        // TMEM columns of a stage's weights, two elements each
 constexpr int H_MAX_STAGES = 8;
 constexpr int H_MAX_PACKED = 8;
 constexpr int H_MAKERS = 3;              // groups of four warps that make operands
 constexpr int H_MAKE0 = 4, H_OUT0 = H_MAKE0 + 4 * H_MAKERS;          // first warps of the roles
-constexpr int H_THREADS = (H_OUT0 + 4) * 32;
+constexpr int H_OUTS = 8;
+constexpr int H_THREADS = (H_OUT0 + H_OUTS) * 32;
+// Shared memory of a CTA, at least: more than half of an SM's, since each takes all tensor memory (a second one would
+// wait for it, and two clusters whose CTAs wait on each other's SMs would never begin)
+constexpr size_t H_MIN_SMEM = 120 * 1024;
 
 struct TileCtrl {
     uint64_t x_full[H_MAX_STAGES];       // a stage's x has landed
@@ -64,10 +69,10 @@ struct TileArgs {
     int n_tiles, tiles;                  // tiles along the tokens; all (of a pair, or a cluster)
     int split;                           // CTAs that share a tile's K
     int stages, packed;                  // depths of the rings
-    int acc_cols;                        // TMEM columns of one accumulator
+    int acc_cols, accs;                  // TMEM columns of an accumulator; accumulators: 1 or 2
 };
 
-__host__ __device__ inline int tile_stage_bytes(int held) { return H_A_BYTES + held * H_K * 2; }
+__host__ __device__ inline int tile_stage_bytes(int held) { return held * H_K * 2; }
 __host__ __device__ inline int packed_bytes(const mpq_g4_matrix &L) { return 8 * L.tile_bytes; }
 
 // A place in a ring: the slot, and the parity of the phase in which it is filled (emptied: the other).
@@ -84,13 +89,70 @@ struct Place {
     }
 };
 
-// D[tmem] (+)= A B^T, kind::f16, one CTA's.
-__device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t more)
+// D[tmem] (+)= A[tmem] B[smem]^T, kind::f16: A's rows on the lanes, two elements of K a column; PAIR: a CTA pair's,
+// each CTA with its own rows of A (and D) and half of B's.
+template <bool PAIR>
+__device__ __forceinline__ void mma_f16_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t more)
+{
+    if constexpr (PAIR)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "setp.ne.b32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc),
+            "r"(more)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "setp.ne.b32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc),
+            "r"(more)
+            : "memory");
+}
+
+// True in one thread of a warp that is here as one.
+__device__ __forceinline__ bool elected()
+{
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
+}
+
+// A wait that is not over at once: true if it or another role's gave up.  (Out of line: with this loop in its place a
+// wait that is over at once costs its thread 190 cycles instead of 70, on the way of every stage.)
+__device__ __noinline__ bool wait_failed(uint64_t *bar, uint32_t parity, bool other, long long budget, unsigned *status,
+                                         volatile int *abort)
+{
+    const long long t0 = clock64();
+    while (!(other ? mbar_try_wait_cluster(bar, parity) : mbar_try_wait(bar, parity))) {
+        if (*abort) return true;
+        if (clock64() - t0 <= budget) continue;
+        *abort = 1;
+        atomicOr(status, MPQ_TIMEOUT_G4);
+        return true;
+    }
+    return false;
+}
+
+__device__ __forceinline__ void swap_if(bool c, uint4 &a, uint4 &b)
+{
+    const uint4 x = c ? b : a, y = c ? a : b;
+    a = x;
+    b = y;
+}
+
+// 32 columns of a warp's lane quarter, a lane per thread.
+__device__ __forceinline__ void tmem_st_32(uint32_t taddr, const uint32_t (&v)[32])
 {
     asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(more)
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+        "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+        "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(taddr),
+        "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
+        "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]),
+        "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]),
+        "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]),
+        "r"(v[29]), "r"(v[30]), "r"(v[31])
         : "memory");
 }
 
@@ -143,31 +205,25 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
     // A wait that gave up, or that another role has given up: true.  (Cluster-scope acquires only where one
     // thread takes arrivals of the other CTA's warps.)
     auto failed = [&](uint64_t *bar, uint32_t parity, bool other = false) {
-        auto reached = [&] { return PAIR && other ? mbar_try_wait_cluster(bar, parity) : mbar_try_wait(bar, parity); };
-        if (reached()) return false;
-        const long long t0 = clock64();
-        while (!reached()) {
-            if (*abort_flag) return true;
-            if (clock64() - t0 <= wc.budget) continue;
-            *abort_flag = 1;
-            note_timeout(wc, MPQ_TIMEOUT_G4);
-            return true;
-        }
-        return false;
+        if (__builtin_expect(PAIR && other ? mbar_try_wait_cluster(bar, parity) : mbar_try_wait(bar, parity), 1))
+            return false;
+        return wait_failed(bar, parity, PAIR && other, wc.budget, wc.status, &ctl.abort);
     };
-    auto warp_failed = [&](uint64_t *bar, uint32_t parity) { return __any_sync(0xffffffffu, failed(bar, parity)) != 0; };
+    auto warp_failed = [&](uint64_t *bar, uint32_t parity, bool other = false) {
+        return __any_sync(0xffffffffu, failed(bar, parity, other)) != 0;
+    };
     auto arrive = [&](uint64_t *bar) {   // at the CTA whose thread issues MMAs
         if (PAIR) mbar_arrive_cluster(bar, 0); else mbar_arrive(bar);
     };
-    auto commit = [&](uint64_t *bar) {
-        if (PAIR) mma_commit_pair(bar, (uint16_t)3); else mma_commit(bar);
+    auto commit = [&](uint64_t *bar, int ctas = 3) {
+        if (PAIR) mma_commit_pair(bar, (uint16_t)ctas); else mma_commit(bar);
     };
 
     griddep_launch();
     if (threadIdx.x == 0) {
         for (int i = 0; i < a.stages; ++i) {
             mbar_init(&ctl.x_full[i], 1);
-            mbar_init(&ctl.ready[i], PAIR ? 10 : 5);
+            mbar_init(&ctl.ready[i], PAIR ? 10 : 4);
             mbar_init(&ctl.empty[i], 1);
         }
         for (int i = 0; i < a.packed; ++i) {
@@ -176,7 +232,7 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&ctl.d_full[i], 1);
-            mbar_init(&ctl.d_empty[i], PAIR ? 8 : 4);
+            mbar_init(&ctl.d_empty[i], PAIR ? 2 * H_OUTS : H_OUTS);
         }
         mbar_init(&ctl.done, 1);
         ctl.abort = 0;
@@ -186,40 +242,40 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
     }
     if (warp == 1) {
         if (PAIR)
-            tmem_alloc_pair(&ctl.tmem_base, (uint32_t)(2 * a.acc_cols));
+            tmem_alloc_pair(&ctl.tmem_base, 512u);
         else
-            tmem_alloc(&ctl.tmem_base, (uint32_t)(2 * a.acc_cols));
+            tmem_alloc(&ctl.tmem_base, 512u);
     }
     tc_fence_before();
     __syncthreads();
     if (PAIR) cluster_sync();            // the barriers that the other CTA arrives on are ready
     tc_fence_after();
-    const uint32_t tmem = ctl.tmem_base;
+    const uint32_t tmem = ctl.tmem_base, operands = tmem + (uint32_t)(a.accs * a.acc_cols);
     griddep_wait();
 
     if (warp == 0) {
         // -------------------------------------------------------------------- copies of x
-        if (lane == 0 && !wc.withhold) {
-            int n = 0;
-            Place s;
-            bool stop = *abort_flag != 0;
-            for (int tile = first; tile < a.tiles && !stop; tile += step) {
-                const int y0 = (int)token0(tile) + (PAIR ? rank * a.held : 0);
-                for (int h = 0; h < halves; ++h, ++n, s.pass(a.stages)) {
-                    const uint32_t at = ring_u32 + (uint32_t)(s.at * sb + H_A_BYTES);
-                    if ((n >= a.stages && failed(&ctl.empty[s.at], s.phase ^ 1u)) ||
-                        !MPQ_CHECK((at & 1023u) == 0u)) {
-                        stop = true;
-                        break;
-                    }
+        int n = 0;
+        Place s;
+        bool stop = wc.withhold || *abort_flag;
+        for (int tile = first; tile < a.tiles && !stop; tile += step) {
+            const int y0 = (int)token0(tile) + (PAIR ? rank * a.held : 0);
+            for (int h = 0; h < halves; ++h, ++n, s.pass(a.stages)) {
+                const uint32_t at = ring_u32 + (uint32_t)(s.at * sb);
+                if ((n >= a.stages && warp_failed(&ctl.empty[s.at], s.phase ^ 1u)) || !MPQ_CHECK((at & 1023u) == 0u)) {
+                    stop = true;
+                    break;
+                }
+                if (elected()) {
                     mbar_arrive_expect_tx(&ctl.x_full[s.at], (uint32_t)(a.held * H_K * 2));
                     tma_load_2d(at, &tmX, k0 * 128 + h * H_K, y0, &ctl.x_full[s.at]);
                 }
+                __syncwarp();
             }
-            // no copy may land after the CTA is gone
-            for (int i = max(0, n - a.stages); i < n; ++i)
-                drain_wait(&ctl.x_full[i % a.stages], (uint32_t)(i / a.stages) & 1u, wc, MPQ_TIMEOUT_G4);
         }
+        // no copy may land after the CTA is gone
+        for (int i = max(0, n - a.stages); lane == 0 && i < n; ++i)
+            drain_wait(&ctl.x_full[i % a.stages], (uint32_t)(i / a.stages) & 1u, wc, MPQ_TIMEOUT_G4);
         __syncwarp();
     } else if (warp == 2) {
         // -------------------------------------------------------------------- copies of weights
@@ -234,7 +290,7 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
                     break;
                 }
                 // (a pair's odd CTA may have no channels: it makes what it finds into operands)
-                if (lane == 0) mbar_arrive_expect_tx(&ctl.p_full[p.at], (uint32_t)(strips * a.L.tile_bytes));
+                if (elected()) mbar_arrive_expect_tx(&ctl.p_full[p.at], (uint32_t)(strips * a.L.tile_bytes));
                 __syncwarp();
                 if (lane < strips)
                     bulk_load(smem_u32(packed + p.at * pb + lane * a.L.tile_bytes),
@@ -247,59 +303,64 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
         __syncwarp();
     } else if (warp == 3) {
         // -------------------------------------------------------------------- x has landed
-        if (lane == 0) {
-            Place s;
-            bool stop = false;
-            for (int tile = first; tile < a.tiles && !stop; tile += step)
-                for (int h = 0; h < halves && !stop; ++h, s.pass(a.stages)) {
-                    stop = failed(&ctl.x_full[s.at], s.phase);
-                    if (!stop) arrive(&ctl.ready[s.at]);
-                }
-        }
-        __syncwarp();
+        Place s;
+        bool stop = !PAIR;
+        for (int tile = first; tile < a.tiles && !stop; tile += step)
+            for (int h = 0; h < halves; ++h, s.pass(a.stages)) {
+                stop = warp_failed(&ctl.x_full[s.at], s.phase);
+                if (stop) break;
+                if (elected()) arrive(&ctl.ready[s.at]);
+                __syncwarp();
+            }
     } else if (warp == 1) {
         // -------------------------------------------------------------------- MMAs
-        if (lane == 0 && (!PAIR || rank == 0)) {
+        // (the warp waits as one; a thread that waits alone keeps its warp's others at the next meeting point, which
+        // costs it a hundred cycles a wait)
+        if (!PAIR || rank == 0) {
             int t = 0;                   // tiles so far
             Place s;
             bool stop = false;
             for (int tile = first; tile < a.tiles && !stop; tile += step, ++t) {
                 const int real = (int)min((long long)a.n_tile, a.rows.tokens - token0(tile));
-                const int m = PAIR ? 2 * H_M : H_M, cols = PAIR ? 256 : (real + 15) / 16 * 16, b = t & 1;
+                const int m = PAIR ? 2 * H_M : H_M, cols = PAIR ? 256 : (real + 15) / 16 * 16;
+                const int b = t & (a.accs - 1), use = a.accs == 2 ? t >> 1 : t;
                 const uint32_t id = G4Pairs<T>::kBf16 ? idesc_bf16(m, cols) : idesc_f16(m, cols);
                 const uint32_t d = tmem + (uint32_t)(b * a.acc_cols);
-                if (t >= 2 && failed(&ctl.d_empty[b], (uint32_t)((t >> 1) - 1) & 1u, true)) break;
+                if (use > 0 && warp_failed(&ctl.d_empty[b], (uint32_t)(use - 1) & 1u, true)) break;
                 for (int h = 0; h < halves; ++h, s.pass(a.stages)) {
-                    if (failed(&ctl.ready[s.at], s.phase, true)) {
+                    if ((!PAIR && warp_failed(&ctl.x_full[s.at], s.phase)) ||
+                        warp_failed(&ctl.ready[s.at], s.phase, true)) {
                         stop = true;
                         break;
                     }
                     tc_fence_after();
-                    const uint32_t at = ring_u32 + (uint32_t)(s.at * sb);
-                    const uint64_t ad = smem_desc_sw128(at), bd = smem_desc_sw128(at + H_A_BYTES);
+                    const uint64_t bd = smem_desc_sw128(ring_u32 + (uint32_t)(s.at * sb));
+                    const uint32_t at = operands + (uint32_t)(s.at * H_A_COLS);
+                    if (elected()) {
 #pragma unroll
-                    for (int j = 0; j < H_K / 16; ++j) {             // 32 bytes a step, in 16 B units
-                        const uint32_t more = h > 0 || j > 0 ? 1u : 0u;
-                        if (PAIR)
-                            mma_f16_pair(d, ad + 2 * j, bd + 2 * j, id, more);
-                        else
-                            mma_f16(d, ad + 2 * j, bd + 2 * j, id, more);
+                        for (int j = 0; j < H_K / 16; ++j)           // 32 bytes of B a step, in 16 B units
+                            mma_f16_ts<PAIR>(d, at + 8 * j, bd + 2 * j, id, h > 0 || j > 0 ? 1u : 0u);
+                        commit(&ctl.empty[s.at]);
+                        if (h == halves - 1) commit(&ctl.d_full[b]);
                     }
-                    commit(&ctl.empty[s.at]);
+                    __syncwarp();
                 }
-                if (!stop) commit(&ctl.d_full[b]);
             }
             // every MMA issued above completes before tensor memory is released
-            commit(&ctl.done);
+            if (elected()) {
+                commit(&ctl.done, 1);
+                drain_wait_cluster(&ctl.done, 0, wc, MPQ_TIMEOUT_G4);
+            }
         }
-        if (lane == 0) drain_wait_cluster(&ctl.done, 0, wc, MPQ_TIMEOUT_G4);
         __syncwarp();
     } else if (warp < H_OUT0) {
         // -------------------------------------------------------------------- operands from packed weights
-        // Lanes by eights (what shared memory serves at once): rows r and r ^ 5, four words each -- r and r ^ 5
-        // begin in different halves of the packed rows' 64 bytes and of the operand's swizzled 128.
-        const int own = (warp - H_MAKE0) >> 2, i = lane & 3, r8 = (lane >> 3) ^ ((lane & 4) ? 5 : 0);
-        const int row0 = (warp & 3) * 32 + r8, groups = 128 / a.L.group;
+        // A thread has a channel: its 64 bytes of a packed tile, by quarters in an order in which eight lanes
+        // (what shared memory serves at once) meet no bank twice, put right in registers.
+        const int own = (warp - H_MAKE0) >> 2, q = warp & 3, row = q * 32 + lane, x = (lane >> 1) & 3;
+        const int groups = 128 / a.L.group;
+        const uint32_t to = operands + ((uint32_t)(q * 32) << 16);
+        const unsigned char *const mine_at = packed + (row >> 4) * a.L.tile_bytes;
         int turn = 0;                    // of the groups
         bool again = false;              // every stage has been filled once
         Place p, s;
@@ -318,60 +379,59 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
                     stop = true;
                     break;
                 }
+                const unsigned char *const t = mine_at + p.at * pb;
                 uint4 w[4];
-                uint2 sc[4];             // the row's scales, two a word
-                uint32_t z[4];           // and zero points, of the tile's quarters
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const int row = row0 + 8 * u;
-                    const unsigned char *const t = packed + p.at * pb + (row >> 4) * a.L.tile_bytes;
-                    w[u] = *reinterpret_cast<const uint4 *>(t + (row & 15) * 64 + i * 16);
-                    const unsigned char *const ss = t + G4_CODES + (row & 15) * 2 * groups;
-                    if (groups == 1) {
-                        sc[u].x = *reinterpret_cast<const uint16_t *>(ss) * 0x10001u;
-                        sc[u].y = sc[u].x;
-                    } else if (groups == 2) {
-                        const uint32_t two = *reinterpret_cast<const uint32_t *>(ss);
-                        sc[u] = make_uint2(__byte_perm(two, 0, 0x1010), __byte_perm(two, 0, 0x3232));
-                    } else {
-                        sc[u] = *reinterpret_cast<const uint2 *>(ss);
-                    }
-                    z[u] = 0x08080808u;
-                    if (a.L.zeros) {
-                        const unsigned char *const zs = t + G4_CODES + 32 * groups + (row & 15) * groups;
-                        z[u] = groups == 4   ? *reinterpret_cast<const uint32_t *>(zs)
-                               : groups == 2 ? __byte_perm(*reinterpret_cast<const uint16_t *>(zs), 0, 0x1100)
-                                             : __byte_perm(*zs, 0, 0x0000);
-                    }
+                for (int i = 0; i < 4; ++i)
+                    w[i] = *reinterpret_cast<const uint4 *>(t + (row & 15) * 64 + (i ^ x) * 16);
+                uint2 sc;                // the row's scales of the tile's quarters, two a word
+                uint32_t z = 0x08080808u;            // and zero points
+                const unsigned char *const ss = t + G4_CODES + (row & 15) * 2 * groups;
+                const unsigned char *const zs = t + G4_CODES + 32 * groups + (row & 15) * groups;
+                if (groups == 1) {
+                    sc.x = sc.y = *reinterpret_cast<const uint16_t *>(ss) * 0x10001u;
+                    if (a.L.zeros) z = __byte_perm(*zs, 0, 0x0000);
+                } else if (groups == 2) {
+                    const uint32_t two = *reinterpret_cast<const uint32_t *>(ss);
+                    sc = make_uint2(__byte_perm(two, 0, 0x1010), __byte_perm(two, 0, 0x3232));
+                    if (a.L.zeros) z = __byte_perm(*reinterpret_cast<const uint16_t *>(zs), 0, 0x1100);
+                } else {
+                    sc = *reinterpret_cast<const uint2 *>(ss);
+                    if (a.L.zeros) z = *reinterpret_cast<const uint32_t *>(zs);
                 }
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&ctl.p_empty[p.at]);
+                if (elected()) mbar_arrive(&ctl.p_empty[p.at]);
+                swap_if(x & 1, w[0], w[1]);
+                swap_if(x & 1, w[2], w[3]);
+                swap_if(x & 2, w[0], w[2]);
+                swap_if(x & 2, w[1], w[3]);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     if (h >= count) break;
+                    uint32_t v[H_A_COLS];
+#pragma unroll
+                    for (int m = 0; m < 2; ++m) {
+                        const uint32_t two = h ? sc.y : sc.x;
+                        const G4Scale g = g4_scale<T>(m ? two >> 16 : two & 0xffffu, z >> (8 * (2 * h + m)) & 255u);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const uint32_t word = h ? (m ? w[i].w : w[i].z) : (m ? w[i].y : w[i].x);
+                            uint32_t p4[4];
+                            g4_values<T>(word, g, p4);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) v[16 * m + 4 * i + e] = p4[e];
+                        }
+                    }
                     if (again && warp_failed(&ctl.empty[s.at], s.phase ^ 1u)) {
                         stop = true;
                         break;
                     }
-                    const uint32_t at = ring_u32 + (uint32_t)(s.at * sb);
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        const uint32_t q[4] = {w[u].x, w[u].y, w[u].z, w[u].w}, two = h ? sc[u].y : sc[u].x;
-                        const uint32_t to = at + (uint32_t)((row0 + 8 * u) * 128);
-#pragma unroll
-                        for (int m = 0; m < 2; ++m) {
-                            const G4Scale g = g4_scale<T>(m ? two >> 16 : two & 0xffffu, z[u] >> (8 * (2 * h + m)) & 255u);
-                            uint32_t v[4];
-                            g4_values<T>(q[2 * h + m], g, v);
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
-                                         :: "r"(to + (uint32_t)(((4 * m + i) ^ r8) * 16)), "r"(v[0]), "r"(v[1]),
-                                            "r"(v[2]), "r"(v[3])
-                                         : "memory");
-                        }
-                    }
-                    fence_proxy_async_smem();
+                    tc_fence_after();
+                    tmem_st_32(to + (uint32_t)(s.at * H_A_COLS), v);
+                    tmem_wait_st();
+                    tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) arrive(&ctl.ready[s.at]);
+                    if (elected()) arrive(&ctl.ready[s.at]);
                     again |= s.at + 1 == a.stages;
                     s.pass(a.stages);
                 }
@@ -380,17 +440,18 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
         }
     } else {
         // -------------------------------------------------------------------- outputs
-        const int q = warp & 3, row = q * 32 + lane;
+        const int q = warp & 3, row = q * 32 + lane, j_first = (warp - H_OUT0) / 4 * 16;
         int t = 0;
         for (int tile = first; tile < a.tiles; tile += step, ++t) {
             const long long n0 = token0(tile);
-            const int real = (int)min((long long)a.n_tile, a.rows.tokens - n0), b = t & 1;
+            const int real = (int)min((long long)a.n_tile, a.rows.tokens - n0);
+            const int b = t & (a.accs - 1), use = a.accs == 2 ? t >> 1 : t;
             const int c = row_tile(tile) * H_M + row;
             const float bias = a.split == 1 && a.rows.bias && c < a.rows.channels ? a.rows.bias[c] : 0.0f;
-            if (warp_failed(&ctl.d_full[b], (uint32_t)(t >> 1) & 1u)) break;
+            if (warp_failed(&ctl.d_full[b], (uint32_t)use & 1u)) break;
             tc_fence_after();
             const uint32_t from = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(b * a.acc_cols);
-            for (int j0 = 0; j0 < real; j0 += 16) {
+            for (int j0 = j_first; j0 < real; j0 += H_OUTS / 4 * 16) {
                 float v[16];
                 __syncwarp();
                 tmem_ld_32x32b_x16(from + (uint32_t)j0, v);
@@ -411,7 +472,7 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
             }
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) arrive(&ctl.d_empty[b]);
+            if (elected()) arrive(&ctl.d_empty[b]);
         }
     }
 
@@ -434,9 +495,9 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
     if (warp == 1) {
         tc_fence_after();
         if (PAIR)
-            tmem_dealloc_pair(tmem, (uint32_t)(2 * a.acc_cols));
+            tmem_dealloc_pair(tmem, 512u);
         else
-            tmem_dealloc(tmem, (uint32_t)(2 * a.acc_cols));
+            tmem_dealloc(tmem, 512u);
     }
 }
 
@@ -463,8 +524,8 @@ g4_rows_kernel(const uint16_t *X, long long ldx, int T, int d, uint16_t *to, int
 template <typename T, bool PAIR>
 mpq_status launch_tiles(const TileArgs &a, const CUtensorMap &tmX, void *Y, int ctas, cudaStream_t stream)
 {
-    const size_t smem = 1024 + H_CTRL_BYTES + (size_t)a.stages * tile_stage_bytes(a.held) +
-                        (size_t)a.packed * packed_bytes(a.L);
+    const size_t smem = std::max(H_MIN_SMEM, 1024 + H_CTRL_BYTES + (size_t)a.stages * tile_stage_bytes(a.held) +
+                                                 (size_t)a.packed * packed_bytes(a.L));
     static std::atomic<int> limit[kMaxDevices];
     cudaError_t e = allow_smem(reinterpret_cast<const void *>(g4_tiles_kernel<T, PAIR>), limit, smem);
     if (e != cudaSuccess) return cuda_status(e, "cudaFuncSetAttribute");
@@ -527,6 +588,7 @@ mpq_status launch_g4_tiles(const void *X, int x_type, long long ldx, int T, cons
     a.split = f.pair ? 1 : f.split;
     a.acc_cols = 32;
     while (a.acc_cols < f.n) a.acc_cols *= 2;
+    a.accs = a.acc_cols <= 128 ? 2 : 1;      // 256 columns stay for eight stages of weights
     a.n_tiles = (T + f.n - 1) / f.n;
     const long long tiles = ((long long)C + (f.pair ? 2 : 1) * H_M - 1) / ((f.pair ? 2 : 1) * H_M) * a.n_tiles;
     if (tiles > (1 << 28)) {
@@ -534,7 +596,7 @@ mpq_status launch_g4_tiles(const void *X, int x_type, long long ldx, int T, cons
         return MPQ_ERR_UNSUPPORTED;
     }
     a.tiles = (int)tiles;
-    // two tiles' packed weights or more, as many stages as fit beside them, then more packed tiles
+    // three tiles' packed weights or more, as many stages as fit beside them, then more packed tiles
     const int room = max_smem_optin() - 1024 - H_CTRL_BYTES, pb = packed_bytes(*L), sb = tile_stage_bytes(a.held);
     a.stages = std::min(H_MAX_STAGES, (room - 3 * pb) / sb);
     a.packed = std::min(H_MAX_PACKED, (room - a.stages * sb) / pb);
