@@ -1,9 +1,9 @@
 // Linear layer of weights in 4-bit integers for more than a few tokens (mpq_g4_linear), on tcgen05 MMAs.
 //
 // 128 channels of weights, s (q - z) rounded to x's type, are the MMA's A (the accumulator's lanes), up to 256
-// tokens its B (columns).  Packed weights come by bulk copies as they lie in memory (a ring of their own, tiles
-// ahead), and three groups of four warps turn them by turns into operands of 64 elements of K in tensor memory, a
-// channel to a lane; x comes by TMA into 128-byte-swizzled shared memory.  (Operands in shared memory too, 141 us
+// tokens its B (columns).  Packed weights come by TMA as they lie in memory (a ring of their own, tiles
+// ahead), and groups of four warps turn them by turns into operands in tensor memory, a channel to a
+// lane; x comes by TMA into 128-byte-swizzled shared memory.  (Operands in shared memory too, 141 us
 // for 2,048 x 11,008 x 4,096: 64 KB in and out per 64 elements of K of a pair's CTA are 512 cycles at 128 bytes each,
 // as many as the MMAs take.)  Eight warps write the outputs.  Roles run over their CTA's tiles without a
 // pause; up to 128 tokens two accumulators take turns, and a tile's outputs leave while the next one is summed.
@@ -13,7 +13,7 @@
 // order of the ranks (equal inputs give equal bits).
 //
 // Warps: 0 copies x, 1 issues MMAs (the even CTA's, of a pair), 2 copies weights, 3 tells the MMAs' warp that x has
-// landed, 4..15 make operands, 16..23 write outputs (these two by lane quarters, warp % 4).  Every wait is bounded.
+// landed, 4 .. make operands, the last eight write outputs (these two by lane quarters, warp % 4).  Every wait is bounded.
 #include <cuda.h>
 #include <string.h>
 
@@ -33,14 +33,15 @@ namespace {
 using namespace sm100;
 
 constexpr int H_M = TOKEN_M;             // channels of a CTA's tile
-constexpr int H_K = 64;                  // elements of K in a stage, half a packed tile
+constexpr int H_K = 128;                 // elements of K in a stage: a packed tile's
 constexpr int H_A_COLS = H_K / 2;        // TMEM columns of a stage's weights, two elements each
-constexpr int H_MAX_STAGES = 8;
+constexpr int H_MAX_STAGES = 4;
 constexpr int H_MAX_PACKED = 8;
-constexpr int H_MAKERS = 3;              // groups of four warps that make operands
-constexpr int H_MAKE0 = 4, H_OUT0 = H_MAKE0 + 4 * H_MAKERS;          // first warps of the roles
-constexpr int H_OUTS = 8;
-constexpr int H_THREADS = (H_OUT0 + H_OUTS) * 32;
+constexpr int H_MAKE0 = 4;               // first of the warps that make operands, in groups of four
+constexpr int H_OUTS = 8;                // warps that write outputs, behind them
+__host__ __device__ constexpr int makers(bool pair) { return pair ? 2 : 3; }
+__host__ __device__ constexpr int first_out(bool pair) { return H_MAKE0 + 4 * makers(pair); }
+__host__ __device__ constexpr int tile_threads(bool pair) { return (first_out(pair) + H_OUTS) * 32; }
 // Shared memory of a CTA, at least: more than half of an SM's, since each takes all tensor memory (a second one would
 // wait for it, and two clusters whose CTAs wait on each other's SMs would never begin)
 constexpr size_t H_MIN_SMEM = 120 * 1024;
@@ -79,11 +80,10 @@ __host__ __device__ inline int packed_bytes(const mpq_g4_matrix &L) { return 8 *
 struct Place {
     int at = 0;
     uint32_t phase = 0;
-    __device__ __forceinline__ void pass(int slots, int count = 1)   // count <= slots
+    __device__ __forceinline__ void pass(int slots)
     {
-        at += count;
-        if (at >= slots) {
-            at -= slots;
+        if (++at == slots) {
+            at = 0;
             phase ^= 1u;
         }
     }
@@ -156,32 +156,48 @@ __device__ __forceinline__ void tmem_st_32(uint32_t taddr, const uint32_t (&v)[3
         : "memory");
 }
 
-// Outputs of channel i (of the lane), 16 tokens from column j0 of n_real on.
-template <typename O>
-__device__ __forceinline__ void store_columns(const TokenRows &r, O *Y, float (&v)[16], int i, int lane,
-                                              long long n0, int j0, int n_real)
+// Where a lane's channel's outputs go: tokens j0 .. of n_real, n0 the first of the tile.
+struct Column {
+    int i, lane;
+    long long n0;
+    int n_real;
+};
+
+// Two tokens' outputs in 16 bits.  Where rows take them by twos, neighbouring lanes exchange, and the even one stores
+// two channels of token j, the odd one of j + 1 (a warp's store is whole sectors either way).
+__device__ __forceinline__ void store_two(const TokenRows &r, uint16_t *Y, uint32_t own, const Column &at, int j)
 {
     const size_t size = (r.tokens - 1) * r.ldy + r.channels;
-    if (r.wide) {                        // by quads of lanes, 4 channels of 4 tokens
-        quad_transpose(v, lane);
-        const int c = i & ~3;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int t = j0 + 4 * j + (lane & 3);
-            if (t < n_real && c < r.channels && MPQ_IN((n0 + t) * r.ldy + c + 3, size))
-                store4(Y + (n0 + t) * r.ldy + c, v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-        }
-    } else if (i < r.channels) {
-        O *y = Y + (n0 + j0) * r.ldy + i;
-#pragma unroll
-        for (int j = 0; j < 16; ++j, y += r.ldy)
-            if (j0 + j < n_real && MPQ_IN((n0 + j0 + j) * r.ldy + i, size)) *y = from_f32<O>(v[j]);
+    if (r.wide) {
+        const int odd = at.lane & 1, c = at.i - odd;
+        const uint32_t other = __shfl_xor_sync(0xffffffffu, own, 1);
+        const uint32_t two = odd ? __byte_perm(other, own, 0x7632) : __byte_perm(own, other, 0x5410);
+        if (j + odd < at.n_real && c < r.channels && MPQ_IN((at.n0 + j + odd) * r.ldy + c + 1, size))
+            *reinterpret_cast<uint32_t *>(Y + (at.n0 + j + odd) * r.ldy + c) = two;
+        return;
     }
+    if (at.i >= r.channels) return;
+    uint16_t *const y = Y + (at.n0 + j) * r.ldy + at.i;
+    if (j < at.n_real && MPQ_IN((at.n0 + j) * r.ldy + at.i, size)) *y = (uint16_t)own;
+    if (j + 1 < at.n_real && MPQ_IN((at.n0 + j + 1) * r.ldy + at.i, size)) y[r.ldy] = (uint16_t)(own >> 16);
+}
+
+__device__ __forceinline__ void store_one(const TokenRows &r, float *Y, float v, const Column &at, int j)
+{
+    if (at.i < r.channels && j < at.n_real &&
+        MPQ_IN((at.n0 + j) * r.ldy + at.i, (r.tokens - 1) * r.ldy + r.channels))
+        Y[(at.n0 + j) * r.ldy + at.i] = v;
+}
+
+__device__ __forceinline__ uint32_t pack16(int type, float a, float b)
+{
+    return type == MPQ_F16 ? pack2(a, b, __half()) : pack2(a, b, __nv_bfloat16());
 }
 
 template <typename T, bool PAIR>
-__global__ void __launch_bounds__(H_THREADS, 1)
-g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ CUtensorMap tmX)
+__global__ void __launch_bounds__(tile_threads(PAIR), 1)
+g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ CUtensorMap tmX,
+                const __grid_constant__ CUtensorMap tmW)
 {
     extern __shared__ unsigned char raw[];
     unsigned char *const base = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
@@ -196,10 +212,11 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
     const int rank = cluster ? (int)cluster_ctarank() : 0, size = PAIR ? 2 : a.split;
     const int first = (int)blockIdx.x / size, step = (int)gridDim.x / size;
     const int k_tiles = a.L.k_tiles;
-    // this CTA's share of the row: tiles of 128, stages of 64 (the last tile may have one)
+    // this CTA's share of the row
     const int k0 = PAIR ? 0 : (int)((long long)k_tiles * rank / a.split);
     const int k1 = PAIR ? k_tiles : (int)((long long)k_tiles * (rank + 1) / a.split);
-    const int halves = min(2 * k1, (a.L.d + H_K - 1) / H_K) - 2 * k0;
+    // halves of a stage (64 elements, a row of the swizzle) that the row reaches
+    auto halves = [&](int k) { return k * H_K + 64 < a.L.d ? 2 : 1; };
     auto row_tile = [&](int tile) { return PAIR ? tile / a.n_tiles * 2 + rank : tile / a.n_tiles; };
     auto token0 = [&](int tile) { return (long long)(tile % a.n_tiles) * a.n_tile; };
     // A wait that gave up, or that another role has given up: true.  (Cluster-scope acquires only where one
@@ -239,6 +256,7 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
         fence_barrier_init();
         if (!MPQ_CHECK_SMEM_END(packed - raw + (size_t)a.packed * pb)) ctl.abort = 1;
         prefetch_tensormap(&tmX);
+        prefetch_tensormap(&tmW);
     }
     if (warp == 1) {
         if (PAIR)
@@ -260,15 +278,17 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
         bool stop = wc.withhold || *abort_flag;
         for (int tile = first; tile < a.tiles && !stop; tile += step) {
             const int y0 = (int)token0(tile) + (PAIR ? rank * a.held : 0);
-            for (int h = 0; h < halves; ++h, ++n, s.pass(a.stages)) {
+            for (int k = k0; k < k1; ++k, ++n, s.pass(a.stages)) {
                 const uint32_t at = ring_u32 + (uint32_t)(s.at * sb);
                 if ((n >= a.stages && warp_failed(&ctl.empty[s.at], s.phase ^ 1u)) || !MPQ_CHECK((at & 1023u) == 0u)) {
                     stop = true;
                     break;
                 }
                 if (elected()) {
-                    mbar_arrive_expect_tx(&ctl.x_full[s.at], (uint32_t)(a.held * H_K * 2));
-                    tma_load_2d(at, &tmX, k0 * 128 + h * H_K, y0, &ctl.x_full[s.at]);
+                    const int count = halves(k);
+                    mbar_arrive_expect_tx(&ctl.x_full[s.at], (uint32_t)(count * a.held * 128));
+                    for (int h = 0; h < count; ++h)
+                        tma_load_2d(at + (uint32_t)(h * a.held * 128), &tmX, k * H_K + h * 64, y0, &ctl.x_full[s.at]);
                 }
                 __syncwarp();
             }
@@ -283,19 +303,22 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
         Place p;
         bool stop = wc.withhold || *abort_flag;
         for (int tile = first; tile < a.tiles && !stop; tile += step) {
-            const int r0 = row_tile(tile) * 8, strips = max(0, min(8, a.L.row_tiles - r0));
+            const int r0 = row_tile(tile) * 8;
             for (int k = k0; k < k1; ++k, ++n, p.pass(a.packed)) {
                 if (n >= a.packed && warp_failed(&ctl.p_empty[p.at], p.phase ^ 1u)) {
                     stop = true;
                     break;
                 }
-                // (a pair's odd CTA may have no channels: it makes what it finds into operands)
-                if (elected()) mbar_arrive_expect_tx(&ctl.p_full[p.at], (uint32_t)(strips * a.L.tile_bytes));
+                const uint32_t at = smem_u32(packed + p.at * pb);
+                if (!MPQ_CHECK((at & 127u) == 0u)) {
+                    stop = true;
+                    break;
+                }
+                if (elected()) {         // (strips of 16 channels past the last are filled with zeros)
+                    mbar_arrive_expect_tx(&ctl.p_full[p.at], (uint32_t)pb);
+                    tma_load_3d(at, &tmW, 0, k, r0, &ctl.p_full[p.at]);
+                }
                 __syncwarp();
-                if (lane < strips)
-                    bulk_load(smem_u32(packed + p.at * pb + lane * a.L.tile_bytes),
-                              a.w + ((size_t)(r0 + lane) * k_tiles + k) * a.L.tile_bytes, (uint32_t)a.L.tile_bytes,
-                              &ctl.p_full[p.at]);
             }
         }
         for (int i = max(0, n - a.packed); lane == 0 && i < n; ++i)
@@ -306,7 +329,7 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
         Place s;
         bool stop = !PAIR;
         for (int tile = first; tile < a.tiles && !stop; tile += step)
-            for (int h = 0; h < halves; ++h, s.pass(a.stages)) {
+            for (int k = k0; k < k1; ++k, s.pass(a.stages)) {
                 stop = warp_failed(&ctl.x_full[s.at], s.phase);
                 if (stop) break;
                 if (elected()) arrive(&ctl.ready[s.at]);
@@ -327,7 +350,7 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
                 const uint32_t id = G4Pairs<T>::kBf16 ? idesc_bf16(m, cols) : idesc_f16(m, cols);
                 const uint32_t d = tmem + (uint32_t)(b * a.acc_cols);
                 if (use > 0 && warp_failed(&ctl.d_empty[b], (uint32_t)(use - 1) & 1u, true)) break;
-                for (int h = 0; h < halves; ++h, s.pass(a.stages)) {
+                for (int k = k0; k < k1; ++k, s.pass(a.stages)) {
                     if ((!PAIR && warp_failed(&ctl.x_full[s.at], s.phase)) ||
                         warp_failed(&ctl.ready[s.at], s.phase, true)) {
                         stop = true;
@@ -337,11 +360,15 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
                     const uint64_t bd = smem_desc_sw128(ring_u32 + (uint32_t)(s.at * sb));
                     const uint32_t at = operands + (uint32_t)(s.at * H_A_COLS);
                     if (elected()) {
+                        const int count = halves(k);
+                        for (int h = 0; h < count; ++h) {
+                            const uint64_t bh = bd + (uint64_t)(h * a.held * 8);     // in 16 B units
 #pragma unroll
-                        for (int j = 0; j < H_K / 16; ++j)           // 32 bytes of B a step, in 16 B units
-                            mma_f16_ts<PAIR>(d, at + 8 * j, bd + 2 * j, id, h > 0 || j > 0 ? 1u : 0u);
+                            for (int j = 0; j < 4; ++j)
+                                mma_f16_ts<PAIR>(d, at + 32 * h + 8 * j, bh + 2 * j, id, k > k0 || h + j > 0 ? 1u : 0u);
+                        }
                         commit(&ctl.empty[s.at]);
-                        if (h == halves - 1) commit(&ctl.d_full[b]);
+                        if (k == k1 - 1) commit(&ctl.d_full[b]);
                     }
                     __syncwarp();
                 }
@@ -353,7 +380,7 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
             }
         }
         __syncwarp();
-    } else if (warp < H_OUT0) {
+    } else if (warp < first_out(PAIR)) {
         // -------------------------------------------------------------------- operands from packed weights
         // A thread has a channel: its 64 bytes of a packed tile, by quarters in an order in which eight lanes
         // (what shared memory serves at once) meet no bank twice, put right in registers.
@@ -367,12 +394,11 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
         bool stop = false;
         for (int tile = first; tile < a.tiles && !stop; tile += step) {
             for (int k = k0; k < k1; ++k, p.pass(a.packed)) {
-                const int count = min(2, halves - 2 * (k - k0));
                 const bool mine = turn == own;
-                turn = turn == H_MAKERS - 1 ? 0 : turn + 1;
+                turn = turn == makers(PAIR) - 1 ? 0 : turn + 1;
                 if (!mine) {
-                    again |= s.at + count >= a.stages;
-                    s.pass(a.stages, count);
+                    again |= s.at + 1 == a.stages;
+                    s.pass(a.stages);
                     continue;
                 }
                 if (warp_failed(&ctl.p_full[p.at], p.phase)) {
@@ -406,9 +432,8 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
                 swap_if(x & 2, w[0], w[2]);
                 swap_if(x & 2, w[1], w[3]);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    if (h >= count) break;
-                    uint32_t v[H_A_COLS];
+                for (int h = 0; h < 2; ++h) {            // (behind the row's end: zeros, whose MMAs are left out)
+                    uint32_t v[32];
 #pragma unroll
                     for (int m = 0; m < 2; ++m) {
                         const uint32_t two = h ? sc.y : sc.x;
@@ -422,25 +447,27 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
                             for (int e = 0; e < 4; ++e) v[16 * m + 4 * i + e] = p4[e];
                         }
                     }
-                    if (again && warp_failed(&ctl.empty[s.at], s.phase ^ 1u)) {
-                        stop = true;
-                        break;
+                    if (h == 0) {
+                        if (again && warp_failed(&ctl.empty[s.at], s.phase ^ 1u)) {
+                            stop = true;
+                            break;
+                        }
+                        tc_fence_after();
                     }
-                    tc_fence_after();
-                    tmem_st_32(to + (uint32_t)(s.at * H_A_COLS), v);
-                    tmem_wait_st();
-                    tc_fence_before();
-                    __syncwarp();
-                    if (elected()) arrive(&ctl.ready[s.at]);
-                    again |= s.at + 1 == a.stages;
-                    s.pass(a.stages);
+                    tmem_st_32(to + (uint32_t)(s.at * H_A_COLS + 32 * h), v);
                 }
                 if (stop) break;
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (elected()) arrive(&ctl.ready[s.at]);
+                again |= s.at + 1 == a.stages;
+                s.pass(a.stages);
             }
         }
     } else {
         // -------------------------------------------------------------------- outputs
-        const int q = warp & 3, row = q * 32 + lane, j_first = (warp - H_OUT0) / 4 * 16;
+        const int q = warp & 3, row = q * 32 + lane, half = (warp - first_out(PAIR)) >> 2;
         int t = 0;
         for (int tile = first; tile < a.tiles; tile += step, ++t) {
             const long long n0 = token0(tile);
@@ -451,7 +478,31 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
             if (warp_failed(&ctl.d_full[b], (uint32_t)use & 1u)) break;
             tc_fence_after();
             const uint32_t from = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(b * a.acc_cols);
-            for (int j0 = j_first; j0 < real; j0 += H_OUTS / 4 * 16) {
+            const Column at{c, lane, n0, real};
+            uint16_t *const y16 = static_cast<uint16_t *>(Y);
+            if constexpr (PAIR) {
+                // 16 bits: all of the sums to registers, so that the next tile's MMAs go on (8,300 cycles earlier)
+                if (a.y_type != MPQ_F32) {
+                    uint32_t two[64];
+                    const int j0 = half * 128;
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        float v[32];
+                        tmem_ld_32x32b_x32(from + (uint32_t)(j0 + 32 * u), v);
+#pragma unroll
+                        for (int j = 0; j < 16; ++j)
+                            two[16 * u + j] = pack16(a.y_type, v[2 * j] + bias, v[2 * j + 1] + bias);
+                    }
+                    tc_fence_before();
+                    __syncwarp();
+                    if (elected()) arrive(&ctl.d_empty[b]);
+#pragma unroll
+                    for (int j = 0; j < 64; ++j)
+                        if (j0 + 2 * j < real) store_two(a.rows, y16, two[j], at, j0 + 2 * j);
+                    continue;
+                }
+            }
+            for (int j0 = half * 16; j0 < real; j0 += H_OUTS / 4 * 16) {
                 float v[16];
                 __syncwarp();
                 tmem_ld_32x32b_x16(from + (uint32_t)j0, v);
@@ -463,12 +514,14 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
                 }
 #pragma unroll
                 for (int j = 0; j < 16; ++j) v[j] += bias;
-                if (a.y_type == MPQ_F32)
-                    store_columns(a.rows, static_cast<float *>(Y), v, c, lane, n0, j0, real);
-                else if (a.y_type == MPQ_F16)
-                    store_columns(a.rows, static_cast<__half *>(Y), v, c, lane, n0, j0, real);
-                else
-                    store_columns(a.rows, static_cast<__nv_bfloat16 *>(Y), v, c, lane, n0, j0, real);
+                if (a.y_type == MPQ_F32) {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) store_one(a.rows, static_cast<float *>(Y), v[j], at, j0 + j);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 16; j += 2)
+                        store_two(a.rows, y16, pack16(a.y_type, v[j], v[j + 1]), at, j0 + j);
+                }
             }
             tc_fence_before();
             __syncwarp();
@@ -522,7 +575,7 @@ g4_rows_kernel(const uint16_t *X, long long ldx, int T, int d, uint16_t *to, int
 }
 
 template <typename T, bool PAIR>
-mpq_status launch_tiles(const TileArgs &a, const CUtensorMap &tmX, void *Y, int ctas, cudaStream_t stream)
+mpq_status launch_tiles(const TileArgs &a, const CUtensorMap &tmX, const CUtensorMap &tmW, void *Y, int ctas, cudaStream_t stream)
 {
     const size_t smem = std::max(H_MIN_SMEM, 1024 + H_CTRL_BYTES + (size_t)a.stages * tile_stage_bytes(a.held) +
                                                  (size_t)a.packed * packed_bytes(a.L));
@@ -534,7 +587,7 @@ mpq_status launch_tiles(const TileArgs &a, const CUtensorMap &tmX, void *Y, int 
     if (ws != MPQ_OK) return ws;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)ctas);
-    cfg.blockDim = dim3(H_THREADS);
+    cfg.blockDim = dim3(tile_threads(PAIR));
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
@@ -545,14 +598,16 @@ mpq_status launch_tiles(const TileArgs &a, const CUtensorMap &tmX, void *Y, int 
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    e = cudaLaunchKernelEx(&cfg, g4_tiles_kernel<T, PAIR>, a, Y, wc, tmX);
+    e = cudaLaunchKernelEx(&cfg, g4_tiles_kernel<T, PAIR>, a, Y, wc, tmX, tmW);
     return cuda_status(e != cudaSuccess ? e : cudaGetLastError(), "g4 linear launch");
 }
 
 template <typename T>
-mpq_status launch_form(const TileArgs &a, bool pair, const CUtensorMap &tmX, void *Y, int ctas, cudaStream_t stream)
+mpq_status launch_form(const TileArgs &a, bool pair, const CUtensorMap &tmX, const CUtensorMap &tmW, void *Y, int ctas,
+                       cudaStream_t stream)
 {
-    return pair ? launch_tiles<T, true>(a, tmX, Y, ctas, stream) : launch_tiles<T, false>(a, tmX, Y, ctas, stream);
+    return pair ? launch_tiles<T, true>(a, tmX, tmW, Y, ctas, stream)
+                : launch_tiles<T, false>(a, tmX, tmW, Y, ctas, stream);
 }
 
 struct Form {
@@ -588,7 +643,7 @@ mpq_status launch_g4_tiles(const void *X, int x_type, long long ldx, int T, cons
     a.split = f.pair ? 1 : f.split;
     a.acc_cols = 32;
     while (a.acc_cols < f.n) a.acc_cols *= 2;
-    a.accs = a.acc_cols <= 128 ? 2 : 1;      // 256 columns stay for eight stages of weights
+    a.accs = a.acc_cols <= 128 ? 2 : 1;      // 256 columns stay for four stages of weights
     a.n_tiles = (T + f.n - 1) / f.n;
     const long long tiles = ((long long)C + (f.pair ? 2 : 1) * H_M - 1) / ((f.pair ? 2 : 1) * H_M) * a.n_tiles;
     if (tiles > (1 << 28)) {
@@ -621,20 +676,27 @@ mpq_status launch_g4_tiles(const void *X, int x_type, long long ldx, int T, cons
         X = scratch;
         ldx = dp;
     }
-    CUtensorMap tmX;
+    CUtensorMap tmX, tmW;
     memset(&tmX, 0, sizeof(tmX));
+    memset(&tmW, 0, sizeof(tmW));
+    // packed weights by words of 8 bytes: [strips of 16 channels][tiles of 128][a tile]; a copy takes eight strips
+    const cuuint64_t tile = (cuuint64_t)L->tile_bytes;
+    const cuuint64_t w_dims[3] = {tile / 8, (cuuint64_t)L->k_tiles, (cuuint64_t)L->row_tiles};
+    const cuuint64_t w_strides[2] = {tile, tile * (cuuint64_t)L->k_tiles};
+    const cuuint32_t w_box[3] = {(cuuint32_t)L->tile_bytes / 8, 1, 8};
     const cuuint64_t dims[2] = {(cuuint64_t)dp, (cuuint64_t)T};
     const cuuint64_t strides[1] = {(cuuint64_t)(T > 1 ? ldx : (dp + 7) / 8 * 8) * 2};
     const cuuint32_t box[2] = {64, (cuuint32_t)a.held};
     mpq_status st = MPQ_OK;
     if (!encode_tile_map(&tmX, x_type == MPQ_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
-                         X, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B)) {
+                         X, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B) ||
+        !encode_tile_map(&tmW, CU_TENSOR_MAP_DATA_TYPE_FLOAT64, 3, W, w_dims, w_strides, w_box)) {
         set_error("g4 linear: tensor map encoding failed");
         st = MPQ_ERR_CUDA;
     } else if (x_type == MPQ_F16) {
-        st = launch_form<__half>(a, f.pair, tmX, Y, ctas, stream);
+        st = launch_form<__half>(a, f.pair, tmX, tmW, Y, ctas, stream);
     } else {
-        st = launch_form<__nv_bfloat16>(a, f.pair, tmX, Y, ctas, stream);
+        st = launch_form<__nv_bfloat16>(a, f.pair, tmX, tmW, Y, ctas, stream);
     }
     if (scratch) {
         const cudaError_t e = cudaFreeAsync(scratch, stream);
