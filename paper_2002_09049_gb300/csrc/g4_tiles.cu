@@ -13,7 +13,7 @@
 // order of the ranks (equal inputs give equal bits).
 //
 // Warps: 0 copies x, 1 issues MMAs (the even CTA's, of a pair), 2 copies weights, 3 tells the MMAs' warp that x has
-// landed, 4 .. make operands, the last eight write outputs (these two by lane quarters, warp % 4).  Every wait is bounded.
+// landed, 4 .. make operands, the last write outputs (these two by lane quarters, warp % 4).  Every wait is bounded.
 #include <cuda.h>
 #include <string.h>
 
@@ -35,11 +35,11 @@ using namespace sm100;
 constexpr int H_M = TOKEN_M;             // channels of a CTA's tile
 constexpr int H_K = 128;                 // elements of K in a stage: a packed tile's
 constexpr int H_A_COLS = H_K / 2;        // TMEM columns of a stage's weights, two elements each
-constexpr int H_MAX_STAGES = 4;
+constexpr int H_MAX_STAGES = 8;
 constexpr int H_MAX_PACKED = 8;
 constexpr int H_MAKE0 = 4;               // first of the warps that make operands, in groups of four
-constexpr int H_OUTS = 8;                // warps that write outputs, behind them
 __host__ __device__ constexpr int makers(bool pair) { return pair ? 2 : 3; }
+constexpr int H_OUTS = 8;                // warps that write outputs, behind them
 __host__ __device__ constexpr int first_out(bool pair) { return H_MAKE0 + 4 * makers(pair); }
 __host__ __device__ constexpr int tile_threads(bool pair) { return (first_out(pair) + H_OUTS) * 32; }
 // Shared memory of a CTA, at least: more than half of an SM's, since each takes all tensor memory (a second one would
@@ -47,8 +47,8 @@ __host__ __device__ constexpr int tile_threads(bool pair) { return (first_out(pa
 constexpr size_t H_MIN_SMEM = 120 * 1024;
 
 struct TileCtrl {
-    uint64_t x_full[H_MAX_STAGES];       // a stage's x has landed
-    uint64_t ready[H_MAX_STAGES];        // ... and its weights are operands
+    uint64_t x_full[H_MAX_STAGES];       // PAIR: a stage's x has landed in this CTA
+    uint64_t ready[H_MAX_STAGES];        // a stage's x has landed and its weights are operands (PAIR: in both CTAs)
     uint64_t empty[H_MAX_STAGES];        // the MMAs that read it completed
     uint64_t p_full[H_MAX_PACKED];       // packed weights have landed
     uint64_t p_empty[H_MAX_PACKED];      // and been read
@@ -221,7 +221,7 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
     auto token0 = [&](int tile) { return (long long)(tile % a.n_tiles) * a.n_tile; };
     // A wait that gave up, or that another role has given up: true.  (Cluster-scope acquires only where one
     // thread takes arrivals of the other CTA's warps.)
-    auto failed = [&](uint64_t *bar, uint32_t parity, bool other = false) {
+    auto failed = [&](uint64_t *bar, uint32_t parity, bool other) {
         if (__builtin_expect(PAIR && other ? mbar_try_wait_cluster(bar, parity) : mbar_try_wait(bar, parity), 1))
             return false;
         return wait_failed(bar, parity, PAIR && other, wc.budget, wc.status, &ctl.abort);
@@ -240,7 +240,7 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
     if (threadIdx.x == 0) {
         for (int i = 0; i < a.stages; ++i) {
             mbar_init(&ctl.x_full[i], 1);
-            mbar_init(&ctl.ready[i], PAIR ? 10 : 4);
+            mbar_init(&ctl.ready[i], PAIR ? 10 : 5);
             mbar_init(&ctl.empty[i], 1);
         }
         for (int i = 0; i < a.packed; ++i) {
@@ -249,7 +249,7 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&ctl.d_full[i], 1);
-            mbar_init(&ctl.d_empty[i], PAIR ? 2 * H_OUTS : H_OUTS);
+            mbar_init(&ctl.d_empty[i], (PAIR ? 2 : 1) * H_OUTS);
         }
         mbar_init(&ctl.done, 1);
         ctl.abort = 0;
@@ -286,16 +286,18 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
                 }
                 if (elected()) {
                     const int count = halves(k);
-                    mbar_arrive_expect_tx(&ctl.x_full[s.at], (uint32_t)(count * a.held * 128));
+                    uint64_t *const bar = PAIR ? &ctl.x_full[s.at] : &ctl.ready[s.at];
+                    mbar_arrive_expect_tx(bar, (uint32_t)(count * a.held * 128));
                     for (int h = 0; h < count; ++h)
-                        tma_load_2d(at + (uint32_t)(h * a.held * 128), &tmX, k * H_K + h * 64, y0, &ctl.x_full[s.at]);
+                        tma_load_2d(at + (uint32_t)(h * a.held * 128), &tmX, k * H_K + h * 64, y0, bar);
                 }
                 __syncwarp();
             }
         }
-        // no copy may land after the CTA is gone
+        // no copy may land after the CTA is gone (a stage that has weights too is full when they are made)
         for (int i = max(0, n - a.stages); lane == 0 && i < n; ++i)
-            drain_wait(&ctl.x_full[i % a.stages], (uint32_t)(i / a.stages) & 1u, wc, MPQ_TIMEOUT_G4);
+            drain_wait(PAIR ? &ctl.x_full[i % a.stages] : &ctl.ready[i % a.stages], (uint32_t)(i / a.stages) & 1u, wc,
+                       MPQ_TIMEOUT_G4);
         __syncwarp();
     } else if (warp == 2) {
         // -------------------------------------------------------------------- copies of weights
@@ -351,8 +353,7 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
                 const uint32_t d = tmem + (uint32_t)(b * a.acc_cols);
                 if (use > 0 && warp_failed(&ctl.d_empty[b], (uint32_t)(use - 1) & 1u, true)) break;
                 for (int k = k0; k < k1; ++k, s.pass(a.stages)) {
-                    if ((!PAIR && warp_failed(&ctl.x_full[s.at], s.phase)) ||
-                        warp_failed(&ctl.ready[s.at], s.phase, true)) {
+                    if (warp_failed(&ctl.ready[s.at], s.phase, true)) {
                         stop = true;
                         break;
                     }
@@ -643,7 +644,6 @@ mpq_status launch_g4_tiles(const void *X, int x_type, long long ldx, int T, cons
     a.split = f.pair ? 1 : f.split;
     a.acc_cols = 32;
     while (a.acc_cols < f.n) a.acc_cols *= 2;
-    a.accs = a.acc_cols <= 128 ? 2 : 1;      // 256 columns stay for four stages of weights
     a.n_tiles = (T + f.n - 1) / f.n;
     const long long tiles = ((long long)C + (f.pair ? 2 : 1) * H_M - 1) / ((f.pair ? 2 : 1) * H_M) * a.n_tiles;
     if (tiles > (1 << 28)) {
@@ -651,13 +651,26 @@ mpq_status launch_g4_tiles(const void *X, int x_type, long long ldx, int T, cons
         return MPQ_ERR_UNSUPPORTED;
     }
     a.tiles = (int)tiles;
-    // three tiles' packed weights or more, as many stages as fit beside them, then more packed tiles
-    const int room = max_smem_optin() - 1024 - H_CTRL_BYTES, pb = packed_bytes(*L), sb = tile_stage_bytes(a.held);
-    a.stages = std::min(H_MAX_STAGES, (room - 3 * pb) / sb);
-    a.packed = std::min(H_MAX_PACKED, (room - a.stages * sb) / pb);
     const int ctas = f.pair      ? 2 * std::min(a.tiles, sms / 2)
                      : f.split > 1 ? a.tiles * f.split
                                    : std::min(a.tiles, sms);
+
+    // an accumulator, or two that take turns where a CTA has several tiles of up to 128 tokens; the other columns are
+    // stages of operands
+    a.accs = a.acc_cols <= 128 && f.split == 1 && a.tiles > ctas ? 2 : 1;
+    // three tiles' packed weights or more, as many stages as fit beside them, then more packed tiles
+    const int room = max_smem_optin() - 1024 - H_CTRL_BYTES, pb = packed_bytes(*L), sb = tile_stage_bytes(a.held);
+    a.stages = std::min({H_MAX_STAGES, (room - 3 * pb) / sb, (512 - a.accs * a.acc_cols) / H_A_COLS});
+    // A barrier's parity tells two phases apart, not more.  A group of makers that has made a stage knows that the MMAs
+    // took the stage `stages` before it, and its next one is `groups` on: it meets a phase that is at most one behind if
+    // there are as many stages as groups.  Packed tiles may land out of order, so that a group knows only of its
+    // own: a slot is always the same group's.
+    const int groups = makers(f.pair);
+    a.packed = std::min(H_MAX_PACKED, (room - a.stages * sb) / pb) / groups * groups;
+    if (a.stages < groups || a.packed < groups) {
+        set_error("g4 linear: shared memory has no room for %d stages", groups);
+        return MPQ_ERR_UNSUPPORTED;
+    }
 
     void *scratch = nullptr;
     int dp = L->d;

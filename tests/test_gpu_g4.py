@@ -154,7 +154,8 @@ def within(y, want, tol):
     (1, 1, 1), (1, 16, 128), (1, 300, 4096), (2, 17, 129), (7, 129, 257), (8, 500, 640), (9, 33, 1000),
     (16, 4096, 512), (17, 640, 1000), (33, 500, 64), (31, 127, 2176), (63, 256, 384), (65, 130, 512),
     (75, 520, 4096), (128, 128, 256), (129, 384, 640), (200, 64, 2560), (256, 256, 1024), (257, 129, 136),
-    (700, 300, 776), (1030, 1030, 304), (3, 20000, 128), (513, 3001, 1000), (2100, 2050, 512), (5000, 300, 128)])
+    (700, 300, 776), (1030, 1030, 304), (3, 20000, 128), (513, 3001, 1000), (2100, 2050, 512), (5000, 300, 128),
+    (256, 4096, 4096), (208, 200, 9000), (250, 2000, 11008), (30, 600, 11000), (600, 700, 8200)])
 @pytest.mark.parametrize("group,zeros", [(32, True), (64, False), (128, True)])
 def test_linear(gpu, T, C, d, group, zeros):
     dtype, out = ("bf16", "fp16")[(T + C) % 2], list(TYPES)[(T + C + group // 32) % 3]
