@@ -70,24 +70,37 @@ __device__ __forceinline__ G4Scale g4_scale(uint32_t bits, uint32_t z)
     return {G4Pairs<T>::scale(bits), G4Pairs<T>::kPower | z | z << 16, bits};
 }
 
-template <typename T>
+// FAR: scales that G4Pairs<T>::plain does not hold for are among a warp's (hardly a matrix has such), so all of them
+// go through fp32.  (A test at every word cost fp16 9.1 -> 16.2 us for 5 x 11,008 x 4,096.)
+template <typename T, bool FAR>
 __device__ __forceinline__ void g4_values(uint32_t w, const G4Scale &g, uint32_t (&p)[4])
 {
-    if (G4Pairs<T>::plain(g.bits)) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            uint32_t v;                      // (w >> 4 j) & 0x000f000f | the power: one operation of three inputs
-            asm("lop3.b32 %0, %1, %2, %3, 0xea;"
-                : "=r"(v) : "r"(w >> (4 * j)), "n"(0x000f000f), "n"(G4Pairs<T>::kPower));
-            p[j] = G4Pairs<T>::value(v, g.from, g.s);
-        }
-    } else {
+    if constexpr (FAR) {
         const float s = bf16_bits(g.bits);
         const int z = (int)(g.from & 255u);
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             p[j] = pack2((float)((int)(w >> (4 * j) & 15u) - z) * s, (float)((int)(w >> (4 * j + 16) & 15u) - z) * s, T());
+        return;
     }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        uint32_t v;                          // (w >> 4 j) & 0x000f000f | the power: one operation of three inputs
+        asm("lop3.b32 %0, %1, %2, %3, 0xea;"
+            : "=r"(v) : "r"(w >> (4 * j)), "n"(0x000f000f), "n"(G4Pairs<T>::kPower));
+        p[j] = G4Pairs<T>::value(v, g.from, g.s);
+    }
+}
+
+// Whether a warp has a scale, two a word, that asks for FAR.
+template <typename T, int W>
+__device__ __forceinline__ bool g4_far(const uint32_t (&words)[W])
+{
+    if (G4Pairs<T>::kBf16) return false;
+    bool far = false;
+#pragma unroll
+    for (int i = 0; i < W; ++i) far |= !G4Pairs<T>::plain(words[i] & 0xffffu) || !G4Pairs<T>::plain(words[i] >> 16);
+    return __any_sync(0xffffffffu, far) != 0;
 }
 
 }  // namespace mpq

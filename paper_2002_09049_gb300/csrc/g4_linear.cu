@@ -10,6 +10,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "g4.cuh"
 #include "sm100.cuh"
@@ -20,7 +21,6 @@ namespace mpq {
 namespace {
 
 constexpr int FEW_WARPS = 8;
-constexpr int FEW_TOKENS = 16;
 
 template <typename T>
 __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
@@ -66,6 +66,34 @@ __device__ __forceinline__ uint4 load_x(const T *p, int j, int d)
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// The scales and zero points of a row's N groups in a tile, as they lie in memory.
+template <int N>
+struct Groups {
+    uint32_t s[(N + 1) / 2], z;
+    __device__ __forceinline__ void load(const unsigned char *scales, int row, int zeros)
+    {
+        const unsigned char *const ss = scales + row * 2 * N, *const zs = scales + 32 * N + row * N;
+        z = 0x08080808u;
+        if constexpr (N == 1) {
+            s[0] = *reinterpret_cast<const uint16_t *>(ss);
+            if (zeros) z = *zs;
+        } else if constexpr (N == 2) {
+            s[0] = *reinterpret_cast<const uint32_t *>(ss);
+            if (zeros) z = *reinterpret_cast<const uint16_t *>(zs);
+        } else {
+            const uint2 w = *reinterpret_cast<const uint2 *>(ss);
+            s[0] = w.x;
+            s[1] = w.y;
+            if (zeros) z = *reinterpret_cast<const uint32_t *>(zs);
+        }
+    }
+    template <typename T>
+    __device__ __forceinline__ G4Scale scale(int i) const
+    {
+        return g4_scale<T>(i & 1 ? s[i >> 1] >> 16 : s[i >> 1] & 0xffffu, z >> (8 * i) & 255u);
+    }
+};
+
 // NT: tiles of eight tokens; GROUP: elements of a group; VEC: x's rows are 16-byte aligned, d a multiple of 8.
 template <typename T, int NT, int GROUP, bool VEC>
 __global__ void __launch_bounds__(FEW_WARPS * 32)
@@ -83,32 +111,50 @@ g4_few_kernel(const G4Args a, const T *X, void *Y)
     for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[n][e] = 0.0f;
-    for (int kt = warp; kt < a.L.k_tiles; kt += FEW_WARPS) {
-        const unsigned char *const tile = strip + (size_t)kt * a.L.tile_bytes;
-        const uint4 wa = *reinterpret_cast<const uint4 *>(tile + g * 64 + i * 16);
-        const uint4 wb = *reinterpret_cast<const uint4 *>(tile + (g + 8) * 64 + i * 16);
-        const uint32_t qa[4] = {wa.x, wa.y, wa.z, wa.w}, qb[4] = {wb.x, wb.y, wb.z, wb.w};
-        const uint16_t *const sc = reinterpret_cast<const uint16_t *>(tile + G4_CODES);
-        const unsigned char *const zs = tile + G4_CODES + 32 * N;
-        G4Scale ga, gb;
+    // U tiles' codes, scales and zero points are on their way before the first is used
+    constexpr int U = NT == 1 ? 4 : 2;
+    const unsigned char *const codes = strip + g * 64 + i * 16;
+    for (int k0 = warp; k0 < a.L.k_tiles; k0 += U * FEW_WARPS) {
+        uint4 wa[U], wb[U];
+        Groups<N> ga[U], gb[U];
 #pragma unroll
-        for (int m = 0; m < 4; ++m) {
-            if (m * 32 % GROUP == 0) {
-                const int at = m * 32 / GROUP;
-                ga = g4_scale<T>(sc[g * N + at], a.L.zeros ? zs[g * N + at] : G4_ZERO);
-                gb = g4_scale<T>(sc[(g + 8) * N + at], a.L.zeros ? zs[(g + 8) * N + at] : G4_ZERO);
-            }
-            uint32_t pa[4], pb[4];
-            g4_values<T>(qa[m], ga, pa);
-            g4_values<T>(qb[m], gb, pb);
+        for (int u = 0; u < U; ++u) {
+            const size_t at = (size_t)min(k0 + u * FEW_WARPS, a.L.k_tiles - 1) * a.L.tile_bytes;
+            wa[u] = *reinterpret_cast<const uint4 *>(codes + at);
+            wb[u] = *reinterpret_cast<const uint4 *>(codes + at + 8 * 64);
+            ga[u].load(strip + at + G4_CODES, g, a.L.zeros);
+            gb[u].load(strip + at + G4_CODES, g + 8, a.L.zeros);
+        }
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const long long t = n0 + n * 8 + g;
-                uint4 x = make_uint4(0, 0, 0, 0);
-                if (t < a.T) x = load_x<T, VEC>(X + t * a.ldx, kt * 128 + m * 32 + i * 8, a.L.d);
-                mma16816<T>(acc[n], pa[0], pb[0], pa[1], pb[1], x.x, x.y);
-                mma16816<T>(acc[n], pa[2], pb[2], pa[3], pb[3], x.z, x.w);
-            }
+        for (int u = 0; u < U; ++u) {
+            const int kt = k0 + u * FEW_WARPS;
+            if (kt >= a.L.k_tiles) break;
+            const uint32_t qa[4] = {wa[u].x, wa[u].y, wa[u].z, wa[u].w}, qb[4] = {wb[u].x, wb[u].y, wb[u].z, wb[u].w};
+            auto tile = [&](auto far) {
+                G4Scale sa, sb;
+#pragma unroll
+                for (int m = 0; m < 4; ++m) {
+                    if (m * 32 % GROUP == 0) {
+                        sa = ga[u].template scale<T>(m * 32 / GROUP);
+                        sb = gb[u].template scale<T>(m * 32 / GROUP);
+                    }
+                    uint32_t pa[4], pb[4];
+                    g4_values<T, decltype(far)::value>(qa[m], sa, pa);
+                    g4_values<T, decltype(far)::value>(qb[m], sb, pb);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        const long long t = n0 + n * 8 + g;
+                        uint4 x = make_uint4(0, 0, 0, 0);
+                        if (t < a.T) x = load_x<T, VEC>(X + t * a.ldx, kt * 128 + m * 32 + i * 8, a.L.d);
+                        mma16816<T>(acc[n], pa[0], pb[0], pa[1], pb[1], x.x, x.y);
+                        mma16816<T>(acc[n], pa[2], pb[2], pa[3], pb[3], x.z, x.w);
+                    }
+                }
+            };
+            if (g4_far<T>(ga[u].s) || g4_far<T>(gb[u].s))
+                tile(std::true_type());
+            else
+                tile(std::false_type());
         }
     }
     // rows g and g + 8 of tokens 2 i and 2 i + 1
@@ -144,7 +190,22 @@ mpq_status launch_typed(const G4Args &a, const T *X, int x_type, void *Y, cudaSt
 {
     const bool vec = rows_aligned(X, x_type, a.T > 1 ? a.ldx : 0) && a.L.d % 8 == 0;
     if (a.T <= 8) return vec ? launch_few<T, 1, true>(a, X, Y, stream) : launch_few<T, 1, false>(a, X, Y, stream);
+    if (a.T <= 16) return vec ? launch_few<T, 2, true>(a, X, Y, stream) : launch_few<T, 2, false>(a, X, Y, stream);
     return vec ? launch_few<T, 4, true>(a, X, Y, stream) : launch_few<T, 4, false>(a, X, Y, stream);
+}
+
+// Whether this kernel's modelled time (us) is less than the tiles': a start, and what is longer of a warp's tiles one
+// after another and of all tiles and CTAs, by the tokens of a CTA (8, 16 or 32).  Some timings, us, this kernel's and
+// the tiles': 8 x 4,096 x 4,096 (T x C x d) 4.9, 8.7; 32 x 4,096 x 4,096 8.2, 9.4; 48 x 4,096 x 4,096 13.4, 9.9;
+// 16 x 11,008 x 4,096 13.4, 16.5; 128 x 1,024 x 1,024 4.1, 7.2; 24 x 448 x 8,064 9.1, 9.0; 16 x 14,000 x 500 9.5, 7.7.
+bool few_tokens(int T, const mpq_g4_matrix *L)
+{
+    if (T > 128) return false;
+    const int c = T <= 8 ? 0 : T <= 16 ? 1 : 2;
+    constexpr double one[3] = {0.4, 0.6, 0.9}, tile[3] = {0.25e-3, 0.4e-3, 0.45e-3}, cta[3] = {3.4e-3, 6.2e-3, 12e-3};
+    const double ctas = (double)L->row_tiles * ((T + 31) / 32);
+    const double t = 2.0 + std::max((L->k_tiles + FEW_WARPS - 1) / FEW_WARPS * one[c], ctas * (L->k_tiles * tile[c] + cta[c]));
+    return t < g4_tiles_time(T, L->rows, L->d);
 }
 
 }  // namespace
@@ -153,7 +214,7 @@ mpq_status launch_g4_linear(const void *X, int x_type, long long ldx, int T, con
                             const void *W, const float *bias, void *Y, int y_type, long long ldy,
                             cudaStream_t stream)
 {
-    if (T > FEW_TOKENS) return launch_g4_tiles(X, x_type, ldx, T, L, W, bias, Y, y_type, ldy, stream);
+    if (!few_tokens(T, L)) return launch_g4_tiles(X, x_type, ldx, T, L, W, bias, Y, y_type, ldy, stream);
     const G4Args a = {*L, static_cast<const unsigned char *>(W), bias, ldx, ldy, T, y_type};
     if (x_type == MPQ_F16) return launch_typed(a, static_cast<const __half *>(X), x_type, Y, stream);
     return launch_typed(a, static_cast<const __nv_bfloat16 *>(X), x_type, Y, stream);

@@ -15,9 +15,11 @@
 // Warps: 0 copies x, 1 issues MMAs (the even CTA's, of a pair), 2 copies weights, 3 tells the MMAs' warp that x has
 // landed, 4 .. make operands, the last write outputs (these two by lane quarters, warp % 4).  Every wait is bounded.
 #include <cuda.h>
+#include <math.h>
 #include <string.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "g4.cuh"
 #include "pair_common.cuh"
@@ -432,22 +434,30 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
                 swap_if(x & 1, w[2], w[3]);
                 swap_if(x & 2, w[0], w[2]);
                 swap_if(x & 2, w[1], w[3]);
+                const uint32_t scales[2] = {sc.x, sc.y};
+                const bool far = g4_far<T>(scales);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {            // (behind the row's end: zeros, whose MMAs are left out)
                     uint32_t v[32];
+                    auto convert = [&](auto f) {
 #pragma unroll
-                    for (int m = 0; m < 2; ++m) {
-                        const uint32_t two = h ? sc.y : sc.x;
-                        const G4Scale g = g4_scale<T>(m ? two >> 16 : two & 0xffffu, z >> (8 * (2 * h + m)) & 255u);
+                        for (int m = 0; m < 2; ++m) {
+                            const uint32_t two = scales[h];
+                            const G4Scale g = g4_scale<T>(m ? two >> 16 : two & 0xffffu, z >> (8 * (2 * h + m)) & 255u);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const uint32_t word = h ? (m ? w[i].w : w[i].z) : (m ? w[i].y : w[i].x);
-                            uint32_t p4[4];
-                            g4_values<T>(word, g, p4);
+                            for (int i = 0; i < 4; ++i) {
+                                const uint32_t word = h ? (m ? w[i].w : w[i].z) : (m ? w[i].y : w[i].x);
+                                uint32_t p4[4];
+                                g4_values<T, decltype(f)::value>(word, g, p4);
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) v[16 * m + 4 * i + e] = p4[e];
+                                for (int e = 0; e < 4; ++e) v[16 * m + 4 * i + e] = p4[e];
+                            }
                         }
-                    }
+                    };
+                    if (far)
+                        convert(std::true_type());
+                    else
+                        convert(std::false_type());
                     if (h == 0) {
                         if (again && warp_failed(&ctl.empty[s.at], s.phase ^ 1u)) {
                             stop = true;
@@ -617,17 +627,49 @@ struct Form {
     int split;
 };
 
-// Pairs for more than a tile of tokens; else as many CTAs share a tile's K as leave each one an SM, with four tiles
-// of 128 or more.
-Form choose_form(int T, int C, int k_tiles, int sms)
+// CTAs (clusters of `split`) that are resident at once: one CTA an SM; what whole clusters leave of the GPCs' SMs was
+// measured (a cluster more than these takes a second round).
+int resident(int split, int sms) { return split == 1 ? sms : split == 2 ? sms / 2 : split == 4 ? sms * 36 / 152 : sms * 14 / 152; }
+
+// The form with the least modelled time (us): a start, and for each round of resident CTAs its stages, by their tokens
+// (up to 128 the operands' making bounds them, 0.37 to 0.41 us; from 192 on the MMAs), the tile's way out, and the
+// joining of a split.  Fitted to 960 timings of 102 sizes (8 <= T <= 2,048, 448 <= C <= 14,000, 500 <= d <= 11,008): the
+// choice costs 2% on average against the best form; 14,000 x 500 with 2,048 tokens 8%, and 1,024 x 1,024 up to 30%,
+// where a few tokens' kernel is taken.  Some of them, us, with 32 / 64 / 128 / 256 tokens a tile, pairs:
+// 40 x 4,096 x 4,096 (T x C x d; split by 4) 9.3, -, -, -, -; 256 x 11,008 x 4,096 45, 31, 33, 25.5, 27.7;
+// 2,048 x 11,008 x 4,096 -, 254, 145, 121, 107; 512 x 4,096 x 11,008 -, -, 41, 33 (split by 2), 55.
+Form choose_form(int T, int C, int k_tiles, int sms, double &least)
 {
-    Form f = {std::min(256, (T + 15) / 16 * 16), T > 256, 1};
-    const long long tiles = ((long long)C + H_M - 1) / H_M * ((T + f.n - 1) / f.n);
-    while (!f.pair && f.split < TOKEN_MAX_SPLIT && tiles * f.split * 2 <= sms && k_tiles >= f.split * 4) f.split *= 2;
-    return f;
+    auto rounds = [](long long n, long long at_once) { return (double)((n + at_once - 1) / at_once); };
+    Form best = {256, true, 1};
+    least = 6.8 + rounds((C + 255LL) / 256 * ((T + 255LL) / 256), std::max(1, sms / 2)) * (0.512 * k_tiles + 3.7);
+    if (T <= 128) least = HUGE_VAL;
+    for (int most = 32; most <= 256; most += most < 128 ? 32 : 64) {
+        const int n = std::min(most, (T + 15) / 16 * 16);
+        const long long tiles = (C + H_M - 1LL) / H_M * ((T + n - 1LL) / n);
+        for (int split = 1; split <= TOKEN_MAX_SPLIT && split * 2 <= std::max(2, k_tiles); split *= 2) {
+            const int stages = (k_tiles + split - 1) / split;
+            const double r = rounds(tiles, std::max(1, resident(split, sms)));
+            const double t = 2.3 + r * (stages * std::max(0.374 + 0.0003 * n, 0.002 * n) + 0.54 +
+                                        (n > 128 ? 0.0226 : 0.0187) * n + (split > 1 ? 2.7 - 0.008 * n : 0.0));
+            if (t < least) {
+                best = {n, false, split};
+                least = t;
+            }
+            if (split == 1 && tiles > 4LL * sms) break;
+        }
+    }
+    return best;
 }
 
 }  // namespace
+
+double g4_tiles_time(int T, int C, int d)
+{
+    double t;
+    choose_form(T, C, (d + H_K - 1) / H_K, sm_count(), t);
+    return t;
+}
 
 mpq_status launch_g4_tiles(const void *X, int x_type, long long ldx, int T, const mpq_g4_matrix *L, const void *W,
                            const float *bias, void *Y, int y_type, long long ldy, cudaStream_t stream)
@@ -638,7 +680,8 @@ mpq_status launch_g4_tiles(const void *X, int x_type, long long ldx, int T, cons
     a.y_type = y_type;
     const int C = L->rows, four = 4 * type_size(y_type), sms = sm_count();
     a.rows = {T, C, C % 4 == 0 && ldy % 4 == 0 && (uintptr_t)Y % four == 0, bias, ldy};
-    const Form f = choose_form(T, C, L->k_tiles, sms);
+    double modelled;
+    const Form f = choose_form(T, C, L->k_tiles, sms, modelled);
     a.n_tile = f.n;
     a.held = f.pair ? f.n / 2 : f.n;
     a.split = f.pair ? 1 : f.split;

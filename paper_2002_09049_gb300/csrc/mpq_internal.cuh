@@ -160,7 +160,8 @@ mpq_status launch_g4_dequantize(const void *packed, const mpq_g4_matrix *L, void
 mpq_status launch_g4_linear(const void *X, int x_type, long long ldx, int T, const mpq_g4_matrix *L,
                             const void *W, const float *bias, void *Y, int y_type, long long ldy,
                             cudaStream_t stream);
-// The form for many tokens (g4_tiles.cu).
+// The form for many tokens (g4_tiles.cu), and the time (us) that its model gives a call.
+double g4_tiles_time(int T, int C, int d);
 mpq_status launch_g4_tiles(const void *X, int x_type, long long ldx, int T, const mpq_g4_matrix *L,
                            const void *W, const float *bias, void *Y, int y_type, long long ldy,
                            cudaStream_t stream);

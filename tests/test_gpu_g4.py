@@ -322,7 +322,7 @@ def test_refusals(gpu):
         binding.mpq_g4_layout(4, 64, 48)
 
 
-@pytest.mark.parametrize("T,C,d", [(40, 300, 512), (40, 300, 4096), (200, 500, 300), (700, 4000, 300)])
+@pytest.mark.parametrize("T,C,d", [(140, 300, 512), (140, 300, 4096), (200, 500, 300), (700, 4000, 300)])
 def test_linear_withheld_copies_time_out(gpu, T, C, d):
     """With the test hook on, the kernel's waits run out with nothing in flight: the status says so, and the
     same call is right again after (K whole, K split over a cluster, CTA pairs)."""
