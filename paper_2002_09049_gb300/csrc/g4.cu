@@ -3,9 +3,9 @@
 //
 // A thread has eight consecutive elements, a word of codes; 4, 8 or 16 threads share a group's range by
 // shuffles; 256 threads make a tile of 16 rows x 128 elements, whose codes leave in order.  The quotient x / s has
-// to be the correctly rounded one: two steps of Markstein's correction with the correctly rounded reciprocal (IBM
-// J. Res. Dev. 34(1), 1990; kv_cache.cu has the argument), a division where the scale is so small or large
-// that a remainder could leave the normal range.
+// to be the correctly rounded one: a step of Markstein's correction with the correctly rounded reciprocal (IBM J.
+// Res. Dev. 34(1), 1990), a division where the scale is so small or large that a remainder could leave the
+// normal range.
 //
 // Memory-bound: an element's own bytes on one side, half a byte and its share of the scales on the other.
 #include <math.h>
@@ -24,11 +24,13 @@ constexpr int G4_PITCH = 132;                // floats of a staged row: rows apa
 
 __device__ __forceinline__ float bf16_rn(float v) { return __bfloat162float(__float2bfloat16_rn(v)); }
 
-// RN(x / s), r = RN(1 / s).
+// RN(x / s), r = RN(1 / s), for an s of 8 significant bits.  x r is off by 2^-23 of it at most, its remainder x - y s is
+// exact, and y + (x - y s) r by 2^-47 of it before its rounding.  With X and M whole numbers of 24 and 25 bits, M odd, and
+// S of 8, X / S differs from M, a midpoint between two floats, by a multiple of 1 / S, and not by 0 (M S has an odd part
+// of 25 bits or more): by 2^-33 of it or more, so the rounding is that of x / s.
 __device__ __forceinline__ float quotient(float x, float s, float r)
 {
-    float y = __fmul_rn(x, r);
-    y = __fmaf_rn(__fmaf_rn(-y, s, x), r, y);
+    const float y = __fmul_rn(x, r);
     return __fmaf_rn(__fmaf_rn(-y, s, x), r, y);
 }
 
@@ -47,16 +49,18 @@ struct G4Group {
 __device__ __forceinline__ G4Group group_of(const float (&v)[8], int threads, int zeros)
 {
     float hi = 0.0f, lo = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        hi = fmaxf(hi, v[i]);
-        lo = fminf(lo, v[i]);
-    }
     uint32_t top = top_bits(v);
-    for (int o = 1; o < threads; o <<= 1) {
-        hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-        lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+    for (int o = 1; o < threads; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+    if (zeros) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            hi = fmaxf(hi, v[i]);
+            lo = fminf(lo, v[i]);
+        }
+        for (int o = 1; o < threads; o <<= 1) {
+            hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+            lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+        }
     }
     constexpr float seventh = 1.0f / 7.0f, fifteenth = 1.0f / 15.0f;
     G4Group g;
@@ -68,115 +72,161 @@ __device__ __forceinline__ G4Group group_of(const float (&v)[8], int threads, in
     return g;
 }
 
-// The word of a thread's eight codes.
+// The word of a thread's eight codes.  A quotient is clamped to the codes' range, and 1.5 * 2^23 added, which rounds it
+// to the whole number in the sum's low bits; the word is the sum of those bits in their places, less what the bits of
+// 1.5 * 2^23 themselves and z come to (all modulo 2^32).
 __device__ __forceinline__ uint32_t codes_of(const float (&v)[8], const G4Group &g, int zeros)
 {
-    const int least = zeros ? 0 : 1;
-    const bool plain = g.s >= 0x1p-100f && g.s <= 0x1p100f;
-    const float r = plain ? __frcp_rn(g.s) : 0.0f;
-    uint32_t w = 0;
+    constexpr float big = 12582912.0f;
+    const float least = zeros ? (float)-g.z : -7.0f, most = zeros ? (float)(15 - g.z) : 7.0f;
+    const uint32_t base = (uint32_t)(g.z - __float_as_int(big)) * 0x11111111u;
+    uint32_t w = base;
+    if (g.s >= 0x1p-100f && g.s <= 0x1p100f) {
+        const float r = __frcp_rn(g.s);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float q = fminf(fmaxf(quotient(v[i], g.s, r), least), most);
+            w += __float_as_uint(__fadd_rn(q, big)) << g4_shift(i);
+        }
+        return w;
+    }
+    if (!(g.s > 0.0f)) return (uint32_t)g.z * 0x11111111u;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        int q = g.z;
-        if (plain)
-            q = min(max(whole(quotient(v[i], g.s, r)) + g.z, least), 15);
-        else if (g.s > 0.0f)
-            q = min(max(whole(fminf(fmaxf(__fdiv_rn(v[i], g.s), -32.0f), 32.0f)) + g.z, least), 15);
-        w |= (uint32_t)q << g4_shift(i);
+        const float q = fminf(fmaxf(__fdiv_rn(v[i], g.s), least), most);
+        w += __float_as_uint(__fadd_rn(q, big)) << g4_shift(i);
     }
     return w;
 }
 
-// VEC: rows are 16-byte aligned; else they pass through shared memory, a warp's accesses consecutive.
-template <typename T, bool VEC>
+// What a CTA has of a matrix: `most` tiles of 16 rows x 128 elements along a row from tile kt0 on, `here` of them there.
+struct TileRun {
+    int rt, kt0, here;
+    long long row0;
+};
+__device__ __forceinline__ TileRun tile_run(const mpq_g4_matrix &L, int most)
+{
+    const int runs = (L.k_tiles + most - 1) / most, rt = (int)blockIdx.x / runs;
+    const int kt0 = ((int)blockIdx.x - rt * runs) * most;
+    return {rt, kt0, min(most, L.k_tiles - kt0), (long long)rt * 16};
+}
+
+// VEC: rows are 16-byte aligned, and a thread's words of U tiles are on their way before the first is used; else (U =
+// 1) rows pass through shared memory, a warp's accesses consecutive.
+template <typename T, bool VEC, int U>
 __global__ void __launch_bounds__(G4_THREADS)
 g4_quantize_kernel(const T *X, long long ldx, mpq_g4_matrix L, unsigned char *packed)
 {
+    static_assert(VEC || U == 1, "one staged tile");
     __shared__ float stage[VEC ? 1 : 16 * G4_PITCH];
     sm100::griddep_launch();
     sm100::griddep_wait();
-    const int rt = (int)blockIdx.x / L.k_tiles, kt = (int)blockIdx.x - rt * L.k_tiles;
+    const TileRun run = tile_run(L, U);
     const int n = threadIdx.x & 15, in_tile = (int)threadIdx.x >> 4;
-    const long long row0 = (long long)rt * 16;
-    const int j0 = kt * 128 + n * 8;
-    float v[8];
+    float v[U][8];
     if constexpr (VEC) {
-        const long long row = row0 + in_tile;
+        const long long row = run.row0 + in_tile;
         const bool real = row < L.rows;
-        const T *const x = X + (real ? row : 0) * ldx + j0;
-        if (real && j0 + 8 <= L.d) {
-            load8(x, v);
-        } else {
+        const T *const x = X + (real ? row : 0) * ldx;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = real && j0 + i < L.d ? to_f32(x[i]) : 0.0f;
+        for (int u = 0; u < U; ++u) {
+            const int j = (run.kt0 + u) * 128 + n * 8;
+            if (real && j + 8 <= L.d) {
+                load8(x + j, v[u]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[u][i] = real && j + i < L.d ? to_f32(x[j + i]) : 0.0f;
+            }
         }
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int e = (int)threadIdx.x + i * G4_THREADS, r = e >> 7, j = e & 127;
-            const bool real = row0 + r < L.rows && kt * 128 + j < L.d;
-            stage[r * G4_PITCH + j] = real ? to_f32(X[(row0 + r) * ldx + kt * 128 + j]) : 0.0f;
+            const int e = (int)threadIdx.x + i * G4_THREADS, r = e >> 7, j = run.kt0 * 128 + (e & 127);
+            const bool real = run.row0 + r < L.rows && j < L.d;
+            stage[r * G4_PITCH + (e & 127)] = real ? to_f32(X[(run.row0 + r) * ldx + j]) : 0.0f;
         }
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = stage[in_tile * G4_PITCH + n * 8 + i];
+        for (int i = 0; i < 8; ++i) v[0][i] = stage[in_tile * G4_PITCH + n * 8 + i];
     }
     const int threads = L.group >> 3, groups = 128 / L.group;
-    const G4Group g = group_of(v, threads, L.zeros);
-    const uint32_t w = codes_of(v, g, L.zeros);
-    const size_t at = (size_t)blockIdx.x * L.tile_bytes;
-    unsigned char *const tile = packed + at;
-    if (!MPQ_IN(at + L.tile_bytes - 1, L.bytes)) return;
-    *reinterpret_cast<uint32_t *>(tile + in_tile * 64 + g4_word(n)) = w;
-    if ((n & (threads - 1)) == 0) {
-        const int i = in_tile * groups + n / threads;
-        reinterpret_cast<__nv_bfloat16 *>(tile + G4_CODES)[i] = __float2bfloat16_rn(g.s);
-        if (L.zeros) tile[G4_CODES + 32 * groups + i] = (unsigned char)g.z;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const G4Group g = group_of(v[u], threads, L.zeros);
+        const uint32_t w = codes_of(v[u], g, L.zeros);
+        const size_t at = ((size_t)run.rt * L.k_tiles + run.kt0 + u) * L.tile_bytes;
+        if (u >= run.here || !MPQ_IN(at + L.tile_bytes - 1, L.bytes)) return;
+        unsigned char *const tile = packed + at;
+        *reinterpret_cast<uint32_t *>(tile + in_tile * 64 + g4_word(n)) = w;
+        if ((n & (threads - 1)) == 0) {
+            const int i = in_tile * groups + n / threads;
+            reinterpret_cast<__nv_bfloat16 *>(tile + G4_CODES)[i] = __float2bfloat16_rn(g.s);
+            if (L.zeros) tile[G4_CODES + 32 * groups + i] = (unsigned char)g.z;
+        }
     }
 }
 
-template <typename T, bool VEC>
+template <typename T, bool VEC, int U>
 __global__ void __launch_bounds__(G4_THREADS)
 g4_dequantize_kernel(const unsigned char *packed, mpq_g4_matrix L, T *Y, long long ldy)
 {
+    static_assert(VEC || U == 1, "one staged tile");
     __shared__ float stage[VEC ? 1 : 16 * G4_PITCH];
     sm100::griddep_launch();
     sm100::griddep_wait();
-    const int rt = (int)blockIdx.x / L.k_tiles, kt = (int)blockIdx.x - rt * L.k_tiles;
-    const int n = threadIdx.x & 15, in_tile = (int)threadIdx.x >> 4;
-    const long long row0 = (long long)rt * 16, row = row0 + in_tile;
-    const int j0 = kt * 128 + n * 8, groups = 128 / L.group;
-    const unsigned char *const tile = packed + (size_t)blockIdx.x * L.tile_bytes;
-    const uint32_t w = *reinterpret_cast<const uint32_t *>(tile + in_tile * 64 + g4_word(n));
+    const TileRun run = tile_run(L, U);
+    const int n = threadIdx.x & 15, in_tile = (int)threadIdx.x >> 4, groups = 128 / L.group;
+    const long long row = run.row0 + in_tile;
     const int at = in_tile * groups + n * 8 / L.group;
-    const float s = bf16_bits(reinterpret_cast<const uint16_t *>(tile + G4_CODES)[at]);
-    const int z = L.zeros ? tile[G4_CODES + 32 * groups + at] : G4_ZERO;
-    float v[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = __fmul_rn((float)((int)(w >> g4_shift(i) & 15u) - z), s);
     const size_t size = (L.rows - 1) * ldy + L.d;
-    if constexpr (VEC) {
-        if (row >= L.rows || j0 >= L.d) return;
-        T *const y = Y + row * ldy + j0;
-        if (!MPQ_IN(row * ldy + min(j0 + 8, L.d) - 1, size)) return;
-        if (j0 + 8 <= L.d) {
-            store8(y, v);
+    uint32_t w[U];
+    float s[U];
+    int z[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const unsigned char *const tile = packed + ((size_t)run.rt * L.k_tiles + run.kt0 + min(u, run.here - 1)) * L.tile_bytes;
+        w[u] = *reinterpret_cast<const uint32_t *>(tile + in_tile * 64 + g4_word(n));
+        s[u] = bf16_bits(reinterpret_cast<const uint16_t *>(tile + G4_CODES)[at]);
+        z[u] = L.zeros ? tile[G4_CODES + 32 * groups + at] : G4_ZERO;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = __fmul_rn((float)((int)(w[u] >> g4_shift(i) & 15u) - z[u]), s[u]);
+        if constexpr (VEC) {
+            const int j = (run.kt0 + u) * 128 + n * 8;
+            if (row >= L.rows || j >= L.d || !MPQ_IN(row * ldy + min(j + 8, L.d) - 1, size)) return;
+            T *const y = Y + row * ldy + j;
+            if (j + 8 <= L.d) {
+                store8(y, v);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (j + i < L.d) y[i] = from_f32<T>(v[i]);
+            }
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (j0 + i < L.d) y[i] = from_f32<T>(v[i]);
-        }
-    } else {
+            for (int i = 0; i < 8; ++i) stage[in_tile * G4_PITCH + n * 8 + i] = v[i];
+            __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 8; ++i) stage[in_tile * G4_PITCH + n * 8 + i] = v[i];
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int e = (int)threadIdx.x + i * G4_THREADS, r = e >> 7, j = e & 127;
-            if (row0 + r < L.rows && kt * 128 + j < L.d && MPQ_IN((row0 + r) * ldy + kt * 128 + j, size))
-                Y[(row0 + r) * ldy + kt * 128 + j] = from_f32<T>(stage[r * G4_PITCH + j]);
+            for (int i = 0; i < 8; ++i) {
+                const int e = (int)threadIdx.x + i * G4_THREADS, r = e >> 7, j = run.kt0 * 128 + (e & 127);
+                if (run.row0 + r < L.rows && j < L.d && MPQ_IN((run.row0 + r) * ldy + j, size))
+                    Y[(run.row0 + r) * ldy + j] = from_f32<T>(stage[r * G4_PITCH + (e & 127)]);
+            }
         }
     }
+}
+
+// Tiles of a CTA: four where that leaves every SM its fill of CTAs (eight), one otherwise.
+int tiles_each(const mpq_g4_matrix *L, bool vec)
+{
+    return vec && (long long)L->row_tiles * ((L->k_tiles + 3) / 4) >= 8LL * sm_count() ? 4 : 1;
+}
+dim3 tile_grid(const mpq_g4_matrix *L, int each)
+{
+    return dim3((unsigned)L->row_tiles * (unsigned)((L->k_tiles + each - 1) / each));
 }
 
 bool aligned(const void *p, int type, long long ld, int rows) { return rows_aligned(p, type, rows > 1 ? ld : 0); }
@@ -203,8 +253,11 @@ mpq_status launch_g4_quantize(const void *X, int x_type, long long ldx, const mp
     const bool vec = aligned(X, x_type, ldx, L->rows);
     return by_type(x_type, [&](auto t) {
         using T = decltype(t);
-        return launch_waiting(vec ? g4_quantize_kernel<T, true> : g4_quantize_kernel<T, false>,
-                              dim3((unsigned)L->row_tiles * (unsigned)L->k_tiles), dim3(G4_THREADS), 0, stream,
+        const int each = tiles_each(L, vec);
+        return launch_waiting(each > 1 ? g4_quantize_kernel<T, true, 4>
+                              : vec    ? g4_quantize_kernel<T, true, 1>
+                                       : g4_quantize_kernel<T, false, 1>,
+                              tile_grid(L, each), dim3(G4_THREADS), 0, stream,
                               "g4 quantize launch", static_cast<const T *>(X), ldx, *L,
                               static_cast<unsigned char *>(packed));
     });
@@ -216,8 +269,11 @@ mpq_status launch_g4_dequantize(const void *packed, const mpq_g4_matrix *L, void
     const bool vec = aligned(Y, y_type, ldy, L->rows);
     return by_type(y_type, [&](auto t) {
         using T = decltype(t);
-        return launch_waiting(vec ? g4_dequantize_kernel<T, true> : g4_dequantize_kernel<T, false>,
-                              dim3((unsigned)L->row_tiles * (unsigned)L->k_tiles), dim3(G4_THREADS), 0, stream,
+        const int each = tiles_each(L, vec);
+        return launch_waiting(each > 1 ? g4_dequantize_kernel<T, true, 4>
+                              : vec    ? g4_dequantize_kernel<T, true, 1>
+                                       : g4_dequantize_kernel<T, false, 1>,
+                              tile_grid(L, each), dim3(G4_THREADS), 0, stream,
                               "g4 dequantize launch", static_cast<const unsigned char *>(packed), *L,
                               static_cast<T *>(Y), ldy);
     });

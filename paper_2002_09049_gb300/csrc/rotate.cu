@@ -6,10 +6,11 @@
 // is taken off before it is rounded to fp32 (24 bits of an angle below pi / 4: 2^-25 of a radian), and put back
 // by exchanging cosine and sine.
 //
-// A CTA takes a token (several where a token has few rows): cosines and sines are made once, in shared memory,
-// while the rows are on their way, and used by all heads (made by every row's own threads they cost more
-// than the rows' traffic).  A row has dim / 16 threads of 16 elements: eight and the eight that they are paired
-// with (their neighbours' form: sixteen consecutive ones), so a pair never leaves its thread.
+// A row has dim / 16 threads of 16 elements: eight and the eight that they are paired with (their neighbours' form:
+// sixteen consecutive ones), so a pair never leaves its thread.  A CTA takes a token's rows at a time (those of
+// several where a token has few), one token after another: the next one's elements are on their way while the
+// last one is turned, and its cosines and sines -- made once for all heads, by every row's own threads they cost
+// more than the rows' traffic -- are left in shared memory for it.
 #include <math.h>
 
 #include <algorithm>
@@ -30,7 +31,8 @@ struct RotateArgs {
     const int *positions;
     const uint64_t *turns;
     int T, dim, rot, shift, norm;
-    int tokens;                          // of a CTA
+    int tokens, rows;                    // of a CTA at a time: tokens, a token's rows
+    int groups;                          // of `tokens` tokens
     int per;                             // threads of a row, a power of two
     float eps, inv_dim;
 };
@@ -88,45 +90,99 @@ __device__ __forceinline__ void unit_at(int u, int rot, bool neighbours, int &ia
     }
 }
 
+// Where pair i's cosine and sine lie: eights 80 bytes apart, so that eight threads that read eight each, 16 bytes at a
+// time, meet no bank twice.
+template <int V>
+__host__ __device__ constexpr int place(int i) { return V == 8 ? (i >> 3) * 10 + (i & 7) : i; }
+
+template <int V>
+__device__ __forceinline__ void take(const float2 *p, float2 (&cs)[V])
+{
+    if constexpr (V == 1) {
+        cs[0] = *p;
+    } else {
+#pragma unroll
+        for (int e = 0; e < V; e += 2) {
+            const float4 f = *reinterpret_cast<const float4 *>(p + e);
+            cs[e] = make_float2(f.x, f.y);
+            cs[e + 1] = make_float2(f.z, f.w);
+        }
+    }
+}
+
 template <typename T, int V, int U, bool NEIGHBOURS, bool VEC>
 __global__ void __launch_bounds__(512)
 rotate_kernel(const RotateArgs a)
 {
-    extern __shared__ float2 turned[];   // [tokens][rot / 2]
+    extern __shared__ __align__(16) float2 turned[];     // [2][tokens][rot / 2], by place
     sm100::griddep_launch();
     sm100::griddep_wait();
-    const int t0 = (int)blockIdx.x * a.tokens, half = a.rot / 2, units = a.dim / (2 * V);
-    const int tokens = min(a.tokens, a.T - t0);
-    const int heads = a.part[0].heads + a.part[1].heads, rows = tokens * heads;
-    const int slots = (int)blockDim.x / a.per, lane = (int)threadIdx.x & (a.per - 1);
-    const int steps = (rows + slots - 1) / slots;        // (every thread takes part in every step's shuffles)
-    for (int step = 0; step < steps; ++step) {
-        const int row = step * slots + (int)threadIdx.x / a.per;
-        const bool real = row < rows;
-        const int tok = real ? row / heads : 0, h = real ? row - tok * heads : 0;
-        const bool key = h >= a.part[0].heads;
-        const mpq_rotate_rows &p = a.part[key ? 1 : 0];
-        const int head = key ? h - a.part[0].heads : h;
-        const T *const x = static_cast<const T *>(p.x) + p.ld_token * (t0 + tok) + p.ld_head * head;
-        float va[U][V], vb[U][V];
+    const int half = a.rot / 2, units = a.dim / (2 * V), entries = a.tokens * half, size = place<V>(entries);
+    const int lane = (int)threadIdx.x & (a.per - 1), slot = (int)threadIdx.x / a.per;
+    const int tok = slot / a.rows, row = (int)blockIdx.y * a.rows + slot - tok * a.rows;
+    const int heads = a.part[0].heads + a.part[1].heads;
+    const bool mine = tok < a.tokens && row < heads, key = row >= a.part[0].heads;
+    const mpq_rotate_rows &p = a.part[key ? 1 : 0];
+    const int head = key ? row - a.part[0].heads : row;
+    const T *const x = static_cast<const T *>(p.x) + p.ld_head * head;
+    T *const y = static_cast<T *>(p.y) + p.ldy_head * head;
+    int ia[U], ib[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) unit_at<V>(lane + i * a.per, a.rot, NEIGHBOURS, ia[i], ib[i]);
+    float va[U][V], vb[U][V], na[U][V], nb[U][V];        // this group's elements, the next one's
+    auto fetch = [&](long long t) {
 #pragma unroll
         for (int i = 0; i < U; ++i) {
-            const int u = lane + i * a.per;
 #pragma unroll
-            for (int e = 0; e < V; ++e) va[i][e] = vb[i][e] = 0.0f;
-            if (!real || u >= units) continue;
-            int ia, ib;
-            unit_at<V>(u, a.rot, NEIGHBOURS, ia, ib);
-            load_v<VEC>(x + ia, va[i]);
-            load_v<VEC>(x + ib, vb[i]);
+            for (int e = 0; e < V; ++e) na[i][e] = nb[i][e] = 0.0f;
+            if (!mine || t >= a.T || lane + i * a.per >= units) continue;
+            load_v<VEC>(x + p.ld_token * t + ia[i], na[i]);
+            load_v<VEC>(x + p.ld_token * t + ib[i], nb[i]);
         }
-        if (step == 0) {
-            for (int i = (int)threadIdx.x; i < tokens * half; i += (int)blockDim.x) {
-                const int tok = i / half, f = i - tok * half;
-                const long long pos = (long long)a.positions[t0 + tok] + a.shift;
-                turned[i] = cos_sin((uint64_t)pos * a.turns[f]);
-            }
-            __syncthreads();
+    };
+    // a thread makes the same frequency's turns of every group (and others', where there are more than threads)
+    const int own = (int)threadIdx.x, own_tok = half ? own / half : 0;
+    const uint64_t own_turn = own < entries ? a.turns[own - own_tok * half] : 0;
+    auto position = [&](int group) {
+        const long long t = (long long)group * a.tokens + own_tok;
+        return own < entries && t < a.T ? a.positions[t] : 0;
+    };
+    auto turn = [&](int group, int buffer, int at) {
+        if (own < entries) turned[buffer * size + place<V>(own)] = cos_sin((uint64_t)((long long)at + a.shift) * own_turn);
+        for (int i = own + (int)blockDim.x; i < entries; i += (int)blockDim.x) {
+            const int k = i / half;
+            const long long t = (long long)group * a.tokens + k;
+            if (t >= a.T) continue;
+            turned[buffer * size + place<V>(i)] =
+                cos_sin((uint64_t)((long long)a.positions[t] + a.shift) * a.turns[i - k * half]);
+        }
+    };
+    float wa[U][V], wb[U][V];            // the norm's weights
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            const bool has = mine && p.weight && lane + i * a.per < units;
+            wa[i][e] = has ? p.weight[ia[i] + e] : 1.0f;
+            wb[i][e] = has ? p.weight[ib[i] + e] : 1.0f;
+        }
+    fetch((long long)blockIdx.x * a.tokens + tok);
+    turn((int)blockIdx.x, 0, position((int)blockIdx.x));
+    int ahead = position((int)(blockIdx.x + gridDim.x));
+    int buffer = 0;
+    for (int group = (int)blockIdx.x; group < a.groups; group += (int)gridDim.x, buffer ^= 1) {
+        const long long t = (long long)group * a.tokens + tok;
+        const bool real = mine && t < a.T;
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+#pragma unroll
+            for (int e = 0; e < V; ++e) va[i][e] = na[i][e], vb[i][e] = nb[i][e];
+        __syncthreads();                 // the group's turns are there; the other buffer's have been used
+        const int next = group + (int)gridDim.x;
+        if (next < a.groups) {
+            fetch((long long)next * a.tokens + tok);
+            turn(next, buffer ^ 1, ahead);
+            ahead = position(next + (int)gridDim.x);
         }
         float scale = 1.0f;
         if (a.norm) {
@@ -153,27 +209,20 @@ rotate_kernel(const RotateArgs a)
             }
         }
         if (!real) continue;
-        const long long to = p.ldy_token * (t0 + tok) + p.ldy_head * head;
-        T *const y = static_cast<T *>(p.y) + to;
 #pragma unroll
         for (int i = 0; i < U; ++i) {
             const int u = lane + i * a.per;
             if (u >= units) continue;
-            int ia, ib;
-            unit_at<V>(u, a.rot, NEIGHBOURS, ia, ib);
             if (a.norm) {
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    va[i][e] *= scale;
-                    vb[i][e] *= scale;
-                    if (p.weight) {
-                        va[i][e] *= p.weight[ia + e];
-                        vb[i][e] *= p.weight[ib + e];
-                    }
+                    va[i][e] = va[i][e] * scale * wa[i][e];
+                    vb[i][e] = vb[i][e] * scale * wb[i][e];
                 }
             }
             if (u < half / V) {
-                const float2 *const cs = turned + tok * half + u * V;
+                float2 cs[V];
+                take<V>(turned + buffer * size + place<V>(tok * half + u * V), cs);
                 if (NEIGHBOURS && V > 1) {
                     // pairs (va[0], va[1]), .., (vb[0], vb[1]), ..
 #pragma unroll
@@ -196,9 +245,9 @@ rotate_kernel(const RotateArgs a)
                     }
                 }
             }
-            if (!MPQ_CHECK(tok < tokens && ia + V <= a.dim && ib + V <= a.dim)) continue;
-            store_v<VEC>(y + ia, va[i]);
-            store_v<VEC>(y + ib, vb[i]);
+            if (!MPQ_CHECK(t < a.T && ia[i] + V <= a.dim && ib[i] + V <= a.dim)) continue;
+            store_v<VEC>(y + p.ldy_token * t + ia[i], va[i]);
+            store_v<VEC>(y + p.ldy_token * t + ib[i], vb[i]);
         }
     }
 }
@@ -236,11 +285,14 @@ mpq_status launch_rotate(const mpq_rotate_rows *q, const mpq_rotate_rows *k, int
     if (wide)
         for (a.per = 1; a.per < dim / 16;) a.per *= 2;
     const int heads = a.part[0].heads + a.part[1].heads;
-    const long long row_threads = (long long)heads * a.per;
-    a.tokens = (int)std::max(1LL, std::min<long long>(256 / row_threads, T));
-    const int threads = (int)std::min<long long>(512, (a.tokens * row_threads + 31) / 32 * 32);
-    const dim3 grid((unsigned)((T + (long long)a.tokens - 1) / a.tokens));
-    const size_t smem = (size_t)a.tokens * (rot / 2) * sizeof(float2);
+    // rows of up to 512 threads; a token of fewer than 256 shares its CTA
+    a.rows = std::min(heads, 512 / a.per);
+    a.tokens = (int)std::max(1LL, std::min<long long>(256 / (a.rows * a.per), T));
+    a.groups = (int)((T + (long long)a.tokens - 1) / a.tokens);
+    const int threads = (a.tokens * a.rows * a.per + 31) / 32 * 32, ys = (heads + a.rows - 1) / a.rows;
+    const int resident = std::max(1, 1536 / threads) * sm_count();
+    const dim3 grid((unsigned)std::min(a.groups, std::max(1, resident / ys)), (unsigned)ys);
+    const size_t smem = 2 * (size_t)(wide ? place<8>(a.tokens * (rot / 2)) : a.tokens * (rot / 2)) * sizeof(float2);
     return by_type(type, [&](auto t) {
         using E = decltype(t);
         auto *const kernel =
