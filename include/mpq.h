@@ -629,7 +629,7 @@ mpq_status mpq_rotation_turns(const double *freq, int n, uint64_t *turns);
  *   norm       0: no norm (weights NULL); 1: eps > 0, weights [dim] fp32 or NULL (ones).
  *   Yq, Yk     out, laid out by ldy_token, ldy_head (the queries' and the keys' own strides: q_..., k_...); Q
  *              and K themselves with their strides, or memory that does not overlap Q or K.
- * dim even, 2..512; rot even, 0..dim.
+ * T up to 2^30; dim even, 2..512; rot even, 0..dim.
  */
 typedef struct {
     const void *x;                     /* in */

@@ -1,8 +1,8 @@
 // Weights in 4-bit integers (mpq_g4_quantize, mpq_g4_dequantize): groups of 32, 64 or 128 elements of a row, a bf16
 // scale and a zero point each.
 //
-// A thread has eight consecutive elements, a word of codes; 4, 8 or 16 threads share a group's range by
-// shuffles; 256 threads make a tile of 16 rows x 128 elements, whose codes leave in order.  The quotient x / s has
+// Quantising, a thread has 16 consecutive elements, two words of codes; 2, 4 or 8 threads share a group's range by
+// shuffles.  Back, a thread has a word.  The quotient x / s has
 // to be the correctly rounded one: a step of Markstein's correction with the correctly rounded reciprocal (IBM J.
 // Res. Dev. 34(1), 1990), a division where the scale is so small or large that a remainder could leave the
 // normal range.
@@ -24,14 +24,21 @@ constexpr int G4_PITCH = 132;                // floats of a staged row: rows apa
 
 __device__ __forceinline__ float bf16_rn(float v) { return __bfloat162float(__float2bfloat16_rn(v)); }
 
-// RN(x / s), r = RN(1 / s), for an s of 8 significant bits.  x r is off by 2^-23 of it at most, its remainder x - y s is
-// exact, and y + (x - y s) r by 2^-47 of it before its rounding.  With X and M whole numbers of 24 and 25 bits, M odd, and
-// S of 8, X / S differs from M, a midpoint between two floats, by a multiple of 1 / S, and not by 0 (M S has an odd part
-// of 25 bits or more): by 2^-33 of it or more, so the rounding is that of x / s.
+// RN(x / s) for an s of 8 significant bits, r = 1 / s to within 2^-22 of it.  x r is off by 2^-21 of it at most, its remainder
+// x - y s is exact, and y + (x - y s) r by 2^-43 of it before its rounding.  With X and M whole numbers of 24 and 25 bits,
+// M odd, and S of 8, X / S differs from M, a midpoint between two floats, by a multiple of 1 / S, and not by 0 (M S
+// has an odd part of 25 bits or more): by 2^-33 of it or more, so the rounding is that of x / s.
 __device__ __forceinline__ float quotient(float x, float s, float r)
 {
     const float y = __fmul_rn(x, r);
     return __fmaf_rn(__fmaf_rn(-y, s, x), r, y);
+}
+
+__device__ __forceinline__ float near_reciprocal(float s)
+{
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
+    return r;
 }
 
 // The nearest whole number (|y| below 2^22, ties to even).
@@ -41,60 +48,66 @@ __device__ __forceinline__ int whole(float y)
 }
 
 struct G4Group {
-    float s;
+    float s, r;
     int z;
+    bool plain;                              // s lies where quotient() is exact; r is its reciprocal
 };
 
-// The scale and zero point of a group of `threads` threads (4, 8 or 16 lanes of a warp).
-__device__ __forceinline__ G4Group group_of(const float (&v)[8], int threads, int zeros)
+// The scale and zero point of a group of `threads` threads (2, 4 or 8 lanes of a warp) of 16 elements.
+template <bool ZEROS>
+__device__ __forceinline__ G4Group group_of(const float (&v)[16], int threads)
 {
-    float hi = 0.0f, lo = 0.0f;
     uint32_t top = top_bits(v);
-    for (int o = 1; o < threads; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-    if (zeros) {
+    float hi = 0.0f, lo = 0.0f;
+    if (ZEROS) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < 16; ++i) {
             hi = fmaxf(hi, v[i]);
             lo = fminf(lo, v[i]);
         }
-        for (int o = 1; o < threads; o <<= 1) {
+    }
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) {
+        if (o >= threads) break;
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+        if (ZEROS) {
             hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
             lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
         }
     }
     constexpr float seventh = 1.0f / 7.0f, fifteenth = 1.0f / 15.0f;
     G4Group g;
-    g.z = G4_ZERO;
-    g.s = bf16_rn(zeros ? __fsub_rn(__fmul_rn(hi, fifteenth), __fmul_rn(lo, fifteenth))
+    g.s = bf16_rn(ZEROS ? __fsub_rn(__fmul_rn(hi, fifteenth), __fmul_rn(lo, fifteenth))
                         : __fmul_rn(__uint_as_float(top), seventh));
     if (top >= 0x7f800000u) g.s = NAN;
-    if (zeros && g.s > 0.0f) g.z = min(max(whole(fminf(__fdiv_rn(-lo, g.s), 32.0f)), 0), 15);
+    g.plain = g.s >= 0x1p-100f && g.s <= 0x1p100f;
+    g.r = near_reciprocal(g.s);
+    g.z = G4_ZERO;
+    if (ZEROS && g.s > 0.0f) {
+        const float z = g.plain ? quotient(-lo, g.s, g.r) : __fdiv_rn(-lo, g.s);
+        g.z = min(max(whole(fminf(z, 32.0f)), 0), 15);
+    }
     return g;
 }
 
-// The word of a thread's eight codes.  A quotient is clamped to the codes' range, and 1.5 * 2^23 added, which rounds it
-// to the whole number in the sum's low bits; the word is the sum of those bits in their places, less what the bits of
+// The word of eight codes.  A quotient is clamped to the codes' range, and 1.5 * 2^23 added, which rounds it to the
+// whole number in the sum's low bits; the word is the sum of those bits in their places, less what the bits of
 // 1.5 * 2^23 themselves and z come to (all modulo 2^32).
-__device__ __forceinline__ uint32_t codes_of(const float (&v)[8], const G4Group &g, int zeros)
+template <bool ZEROS>
+__device__ __forceinline__ uint32_t codes_of(const float *v, const G4Group &g)
 {
     constexpr float big = 12582912.0f;
-    const float least = zeros ? (float)-g.z : -7.0f, most = zeros ? (float)(15 - g.z) : 7.0f;
-    const uint32_t base = (uint32_t)(g.z - __float_as_int(big)) * 0x11111111u;
-    uint32_t w = base;
-    if (g.s >= 0x1p-100f && g.s <= 0x1p100f) {
-        const float r = __frcp_rn(g.s);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float q = fminf(fmaxf(quotient(v[i], g.s, r), least), most);
-            w += __float_as_uint(__fadd_rn(q, big)) << g4_shift(i);
-        }
-        return w;
-    }
     if (!(g.s > 0.0f)) return (uint32_t)g.z * 0x11111111u;
+    const float least = ZEROS ? (float)-g.z : -7.0f, most = ZEROS ? (float)(15 - g.z) : 7.0f;
+    uint32_t w = (uint32_t)(g.z - __float_as_int(big)) * 0x11111111u;
+    if (g.plain) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float q = fminf(fmaxf(__fdiv_rn(v[i], g.s), least), most);
-        w += __float_as_uint(__fadd_rn(q, big)) << g4_shift(i);
+        for (int i = 0; i < 8; ++i)
+            w += __float_as_uint(__fadd_rn(fminf(fmaxf(quotient(v[i], g.s, g.r), least), most), big)) << g4_shift(i);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            w += __float_as_uint(__fadd_rn(fminf(fmaxf(__fdiv_rn(v[i], g.s), least), most), big)) << g4_shift(i);
     }
     return w;
 }
@@ -111,57 +124,61 @@ __device__ __forceinline__ TileRun tile_run(const mpq_g4_matrix &L, int most)
     return {rt, kt0, min(most, L.k_tiles - kt0), (long long)rt * 16};
 }
 
-// VEC: rows are 16-byte aligned, and a thread's words of U tiles are on their way before the first is used; else (U =
-// 1) rows pass through shared memory, a warp's accesses consecutive.
-template <typename T, bool VEC, int U>
+// A thread has 16 elements of U tiles, and 128 threads a tile's 16 rows; the CTA's two halves take U tiles each.  VEC: rows
+// are 16-byte aligned, and all of a thread's elements are on their way before the first is used; else (U = 1) rows
+// pass through shared memory, a warp's accesses consecutive.
+template <typename T, bool VEC, bool ZEROS, int U>
 __global__ void __launch_bounds__(G4_THREADS)
 g4_quantize_kernel(const T *X, long long ldx, mpq_g4_matrix L, unsigned char *packed)
 {
-    static_assert(VEC || U == 1, "one staged tile");
-    __shared__ float stage[VEC ? 1 : 16 * G4_PITCH];
+    static_assert(VEC || U == 1, "one staged tile of a half");
+    __shared__ float stage[VEC ? 1 : 2 * 16 * G4_PITCH];
     sm100::griddep_launch();
     sm100::griddep_wait();
-    const TileRun run = tile_run(L, U);
-    const int n = threadIdx.x & 15, in_tile = (int)threadIdx.x >> 4;
-    float v[U][8];
+    const TileRun run = tile_run(L, 2 * U);
+    const int part = (int)threadIdx.x >> 7, in_tile = ((int)threadIdx.x >> 3) & 15, n = 2 * (threadIdx.x & 7);
+    const int k0 = run.kt0 + part * U;
+    float v[U][16];
     if constexpr (VEC) {
         const long long row = run.row0 + in_tile;
         const bool real = row < L.rows;
         const T *const x = X + (real ? row : 0) * ldx;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int j = (run.kt0 + u) * 128 + n * 8;
-            if (real && j + 8 <= L.d) {
-                load8(x + j, v[u]);
+            const int j = (k0 + u) * 128 + n * 8;
+            if (real && j + 16 <= L.d) {
+                load16(x + j, v[u]);
             } else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[u][i] = real && j + i < L.d ? to_f32(x[j + i]) : 0.0f;
+                for (int i = 0; i < 16; ++i) v[u][i] = real && j + i < L.d ? to_f32(x[j + i]) : 0.0f;
             }
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int e = (int)threadIdx.x + i * G4_THREADS, r = e >> 7, j = run.kt0 * 128 + (e & 127);
-            const bool real = run.row0 + r < L.rows && j < L.d;
-            stage[r * G4_PITCH + (e & 127)] = real ? to_f32(X[(run.row0 + r) * ldx + j]) : 0.0f;
+        for (int i = 0; i < 16; ++i) {
+            const int e = (int)threadIdx.x + i * G4_THREADS, r = e >> 8, j = e & 255;        // a row of both tiles
+            const bool real = run.row0 + r < L.rows && run.kt0 * 128 + j < L.d;
+            stage[((j >> 7) * 16 + r) * G4_PITCH + (j & 127)] =
+                real ? to_f32(X[(run.row0 + r) * ldx + run.kt0 * 128 + j]) : 0.0f;
         }
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[0][i] = stage[in_tile * G4_PITCH + n * 8 + i];
+        for (int i = 0; i < 16; ++i) v[0][i] = stage[(part * 16 + in_tile) * G4_PITCH + n * 8 + i];
     }
-    const int threads = L.group >> 3, groups = 128 / L.group;
+    const int threads = L.group >> 4, groups = 128 / L.group;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const G4Group g = group_of(v[u], threads, L.zeros);
-        const uint32_t w = codes_of(v[u], g, L.zeros);
-        const size_t at = ((size_t)run.rt * L.k_tiles + run.kt0 + u) * L.tile_bytes;
-        if (u >= run.here || !MPQ_IN(at + L.tile_bytes - 1, L.bytes)) return;
+        const G4Group g = group_of<ZEROS>(v[u], threads);
+        const uint32_t w0 = codes_of<ZEROS>(v[u], g), w1 = codes_of<ZEROS>(v[u] + 8, g);
+        const size_t at = ((size_t)run.rt * L.k_tiles + k0 + u) * L.tile_bytes;
+        if (part * U + u >= run.here || !MPQ_IN(at + L.tile_bytes - 1, L.bytes)) return;
         unsigned char *const tile = packed + at;
-        *reinterpret_cast<uint32_t *>(tile + in_tile * 64 + g4_word(n)) = w;
-        if ((n & (threads - 1)) == 0) {
-            const int i = in_tile * groups + n / threads;
+        *reinterpret_cast<uint32_t *>(tile + in_tile * 64 + g4_word(n)) = w0;
+        *reinterpret_cast<uint32_t *>(tile + in_tile * 64 + g4_word(n + 1)) = w1;
+        if (((n >> 1) & (threads - 1)) == 0) {
+            const int i = in_tile * groups + (n >> 1) / threads;
             reinterpret_cast<__nv_bfloat16 *>(tile + G4_CODES)[i] = __float2bfloat16_rn(g.s);
-            if (L.zeros) tile[G4_CODES + 32 * groups + i] = (unsigned char)g.z;
+            if (ZEROS) tile[G4_CODES + 32 * groups + i] = (unsigned char)g.z;
         }
     }
 }
@@ -219,14 +236,25 @@ g4_dequantize_kernel(const unsigned char *packed, mpq_g4_matrix L, T *Y, long lo
     }
 }
 
-// Tiles of a CTA: four where that leaves every SM its fill of CTAs (eight), one otherwise.
-int tiles_each(const mpq_g4_matrix *L, bool vec)
+// Whether four tiles to a CTA leave every SM its fill of CTAs (eight).
+bool by_fours(const mpq_g4_matrix *L, bool vec)
 {
-    return vec && (long long)L->row_tiles * ((L->k_tiles + 3) / 4) >= 8LL * sm_count() ? 4 : 1;
+    return vec && (long long)L->row_tiles * ((L->k_tiles + 3) / 4) >= 8LL * sm_count();
 }
 dim3 tile_grid(const mpq_g4_matrix *L, int each)
 {
     return dim3((unsigned)L->row_tiles * (unsigned)((L->k_tiles + each - 1) / each));
+}
+
+template <typename T, bool ZEROS>
+mpq_status quantize_typed(const void *X, bool vec, long long ldx, const mpq_g4_matrix *L, void *packed, cudaStream_t stream)
+{
+    const bool four = by_fours(L, vec);
+    return launch_waiting(four  ? g4_quantize_kernel<T, true, ZEROS, 2>
+                          : vec ? g4_quantize_kernel<T, true, ZEROS, 1>
+                                : g4_quantize_kernel<T, false, ZEROS, 1>,
+                          tile_grid(L, four ? 4 : 2), dim3(G4_THREADS), 0, stream, "g4 quantize launch",
+                          static_cast<const T *>(X), ldx, *L, static_cast<unsigned char *>(packed));
 }
 
 bool aligned(const void *p, int type, long long ld, int rows) { return rows_aligned(p, type, rows > 1 ? ld : 0); }
@@ -253,13 +281,8 @@ mpq_status launch_g4_quantize(const void *X, int x_type, long long ldx, const mp
     const bool vec = aligned(X, x_type, ldx, L->rows);
     return by_type(x_type, [&](auto t) {
         using T = decltype(t);
-        const int each = tiles_each(L, vec);
-        return launch_waiting(each > 1 ? g4_quantize_kernel<T, true, 4>
-                              : vec    ? g4_quantize_kernel<T, true, 1>
-                                       : g4_quantize_kernel<T, false, 1>,
-                              tile_grid(L, each), dim3(G4_THREADS), 0, stream,
-                              "g4 quantize launch", static_cast<const T *>(X), ldx, *L,
-                              static_cast<unsigned char *>(packed));
+        return L->zeros ? quantize_typed<T, true>(X, vec, ldx, L, packed, stream)
+                        : quantize_typed<T, false>(X, vec, ldx, L, packed, stream);
     });
 }
 
@@ -269,7 +292,7 @@ mpq_status launch_g4_dequantize(const void *packed, const mpq_g4_matrix *L, void
     const bool vec = aligned(Y, y_type, ldy, L->rows);
     return by_type(y_type, [&](auto t) {
         using T = decltype(t);
-        const int each = tiles_each(L, vec);
+        const int each = by_fours(L, vec) ? 4 : 1;
         return launch_waiting(each > 1 ? g4_dequantize_kernel<T, true, 4>
                               : vec    ? g4_dequantize_kernel<T, true, 1>
                                        : g4_dequantize_kernel<T, false, 1>,

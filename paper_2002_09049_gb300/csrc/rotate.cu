@@ -53,28 +53,6 @@ __device__ __forceinline__ float2 cos_sin(uint64_t turn)
     return q & 2 ? make_float2(-c, -s) : make_float2(c, s);
 }
 
-// V elements from p on, to p on; VEC: 16-byte aligned.
-template <bool VEC, int V, typename T>
-__device__ __forceinline__ void load_v(const T *p, float (&v)[V])
-{
-    if constexpr (VEC) {
-        load8(p, v);
-    } else {
-#pragma unroll
-        for (int e = 0; e < V; ++e) v[e] = to_f32(p[e]);
-    }
-}
-template <bool VEC, int V, typename T>
-__device__ __forceinline__ void store_v(T *p, const float (&v)[V])
-{
-    if constexpr (VEC) {
-        store8(p, v);
-    } else {
-#pragma unroll
-        for (int e = 0; e < V; ++e) p[e] = from_f32<T>(v[e]);
-    }
-}
-
 // A thread's U units of a row, each of V elements (a) and V more (b): rotated units first, their pairs
 // numbered from V * unit on.
 template <int V>
@@ -90,34 +68,50 @@ __device__ __forceinline__ void unit_at(int u, int rot, bool neighbours, int &ia
     }
 }
 
-// Where pair i's cosine and sine lie: eights 80 bytes apart, so that eight threads that read eight each, 16 bytes at a
-// time, meet no bank twice.
+// Where pair i's cosine lies, in floats, and how far its sine: eight cosines and eight sines, such eights 80 bytes apart, so
+// that eight threads that read theirs, 16 bytes at a time, meet no bank twice.
 template <int V>
-__host__ __device__ constexpr int place(int i) { return V == 8 ? (i >> 3) * 10 + (i & 7) : i; }
+__host__ __device__ constexpr int place(int i) { return V == 8 ? (i >> 3) * 20 + (i & 7) : 2 * i; }
+template <int V>
+constexpr int kSine = V == 8 ? 8 : 1;
 
-template <int V>
-__device__ __forceinline__ void take(const float2 *p, float2 (&cs)[V])
+// Two floats at once, each rounded as one alone.
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
 {
-    if constexpr (V == 1) {
-        cs[0] = *p;
-    } else {
-#pragma unroll
-        for (int e = 0; e < V; e += 2) {
-            const float4 f = *reinterpret_cast<const float4 *>(p + e);
-            cs[e] = make_float2(f.x, f.y);
-            cs[e + 1] = make_float2(f.z, f.w);
-        }
-    }
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(*reinterpret_cast<const uint64_t *>(&a)),
+        "l"(*reinterpret_cast<const uint64_t *>(&b)));
+    return *reinterpret_cast<const float2 *>(&r);
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(*reinterpret_cast<const uint64_t *>(&a)),
+        "l"(*reinterpret_cast<const uint64_t *>(&b)), "l"(*reinterpret_cast<const uint64_t *>(&c)));
+    return *reinterpret_cast<const float2 *>(&r);
 }
 
+// (l, r) -> (l c - r s, r c + l s)
+__device__ __forceinline__ void turn_pair(float &l, float &r, float c, float s)
+{
+    const float a = __fmaf_rn(r, -s, __fmul_rn(l, c));
+    r = __fmaf_rn(l, s, __fmul_rn(r, c));
+    l = a;
+}
+
+constexpr int ROT_DEPTH = 4;             // tokens of a thread's elements that are on their way or being turned (VEC)
+
 template <typename T, int V, int U, bool NEIGHBOURS, bool VEC>
-__global__ void __launch_bounds__(512)
+__global__ void __launch_bounds__(512, VEC && sizeof(T) == 2 ? 2 : 1)
 rotate_kernel(const RotateArgs a)
 {
-    extern __shared__ __align__(16) float2 turned[];     // [2][tokens][rot / 2], by place
+    static_assert(!VEC || (V == 8 && U == 1), "the wide form");
+    constexpr int CHUNKS = VEC ? 2 * V * (int)sizeof(T) / 16 : 1;        // of a thread and token, 16 bytes each
+    extern __shared__ __align__(16) float turned[];      // cosines and sines [2][tokens][rot / 2], by place
+    const int half = a.rot / 2, units = a.dim / (2 * V), entries = a.tokens * half, size = place<V>(entries);
+    uint4 *const staged = reinterpret_cast<uint4 *>(turned + 2 * size);  // VEC: [ROT_DEPTH][CHUNKS][threads]
     sm100::griddep_launch();
     sm100::griddep_wait();
-    const int half = a.rot / 2, units = a.dim / (2 * V), entries = a.tokens * half, size = place<V>(entries);
     const int lane = (int)threadIdx.x & (a.per - 1), slot = (int)threadIdx.x / a.per;
     const int tok = slot / a.rows, row = (int)blockIdx.y * a.rows + slot - tok * a.rows;
     const int heads = a.part[0].heads + a.part[1].heads;
@@ -129,15 +123,50 @@ rotate_kernel(const RotateArgs a)
     int ia[U], ib[U];
 #pragma unroll
     for (int i = 0; i < U; ++i) unit_at<V>(lane + i * a.per, a.rot, NEIGHBOURS, ia[i], ib[i]);
-    float va[U][V], vb[U][V], na[U][V], nb[U][V];        // this group's elements, the next one's
-    auto fetch = [&](long long t) {
+    float va[U][V], vb[U][V];            // the group's elements
+    // a token's elements on their way to shared memory (nothing where there is no such token)
+    auto fetch = [&](int group, int slot_at) {
+        if constexpr (VEC) {
+            const long long t = (long long)group * a.tokens + tok;
+            const uint32_t bytes = mine && lane < units && t < a.T ? 16u : 0u;
+            const T *const from = bytes ? x + p.ld_token * t : static_cast<const T *>(p.x);
 #pragma unroll
-        for (int i = 0; i < U; ++i) {
+            for (int c = 0; c < CHUNKS; ++c) {
+                const int at = (c < CHUNKS / 2 ? ia[0] : ib[0]) + c % (CHUNKS / 2) * (16 / (int)sizeof(T));
+                sm100::cp_async16(sm100::smem_u32(staged + (slot_at * CHUNKS + c) * (int)blockDim.x + (int)threadIdx.x),
+                                  bytes ? from + at : from, bytes);
+            }
+            sm100::cp_async_commit();
+        }
+    };
+    auto take = [&](int group, int slot_at) {
+        if constexpr (VEC) {
+            sm100::cp_async_wait<ROT_DEPTH - 2>();
+            const uint4 *const q = staged + slot_at * CHUNKS * (int)blockDim.x + (int)threadIdx.x;
+            if constexpr (sizeof(T) == 2) {
+                load8(reinterpret_cast<const T *>(q), va[0]);
+                load8(reinterpret_cast<const T *>(q + blockDim.x), vb[0]);
+            } else {
 #pragma unroll
-            for (int e = 0; e < V; ++e) na[i][e] = nb[i][e] = 0.0f;
-            if (!mine || t >= a.T || lane + i * a.per >= units) continue;
-            load_v<VEC>(x + p.ld_token * t + ia[i], na[i]);
-            load_v<VEC>(x + p.ld_token * t + ib[i], nb[i]);
+                for (int c = 0; c < CHUNKS; ++c) {
+                    const float4 f = *reinterpret_cast<const float4 *>(q + c * (int)blockDim.x);
+                    float *const v = c < 2 ? va[0] + 4 * c : vb[0] + 4 * (c - 2);
+                    v[0] = f.x, v[1] = f.y, v[2] = f.z, v[3] = f.w;
+                }
+            }
+        } else {
+            const long long t = (long long)group * a.tokens + tok;
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+#pragma unroll
+                for (int e = 0; e < V; ++e) va[i][e] = vb[i][e] = 0.0f;
+                if (!mine || t >= a.T || lane + i * a.per >= units) continue;
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    va[i][e] = to_f32(x[p.ld_token * t + ia[i] + e]);
+                    vb[i][e] = to_f32(x[p.ld_token * t + ib[i] + e]);
+                }
+            }
         }
     };
     // a thread makes the same frequency's turns of every group (and others', where there are more than threads)
@@ -147,14 +176,18 @@ rotate_kernel(const RotateArgs a)
         const long long t = (long long)group * a.tokens + own_tok;
         return own < entries && t < a.T ? a.positions[t] : 0;
     };
+    auto keep = [&](int buffer, int i, uint64_t turn) {
+        const float2 c = cos_sin(turn);
+        float *const to = turned + buffer * size + place<V>(i);
+        to[0] = c.x;
+        to[kSine<V>] = c.y;
+    };
     auto turn = [&](int group, int buffer, int at) {
-        if (own < entries) turned[buffer * size + place<V>(own)] = cos_sin((uint64_t)((long long)at + a.shift) * own_turn);
+        if (own < entries) keep(buffer, own, (uint64_t)((long long)at + a.shift) * own_turn);
         for (int i = own + (int)blockDim.x; i < entries; i += (int)blockDim.x) {
             const int k = i / half;
             const long long t = (long long)group * a.tokens + k;
-            if (t >= a.T) continue;
-            turned[buffer * size + place<V>(i)] =
-                cos_sin((uint64_t)((long long)a.positions[t] + a.shift) * a.turns[i - k * half]);
+            if (t < a.T) keep(buffer, i, (uint64_t)((long long)a.positions[t] + a.shift) * a.turns[i - k * half]);
         }
     };
     float wa[U][V], wb[U][V];            // the norm's weights
@@ -166,38 +199,46 @@ rotate_kernel(const RotateArgs a)
             wa[i][e] = has ? p.weight[ia[i] + e] : 1.0f;
             wb[i][e] = has ? p.weight[ib[i] + e] : 1.0f;
         }
-    fetch((long long)blockIdx.x * a.tokens + tok);
+    const int stride = (int)gridDim.x;
+    int coming = (int)blockIdx.x;        // the group that is fetched next
+#pragma unroll
+    for (int i = 0; i < ROT_DEPTH - 1; ++i, coming += stride) fetch(coming, i);
     turn((int)blockIdx.x, 0, position((int)blockIdx.x));
-    int ahead = position((int)(blockIdx.x + gridDim.x));
-    int buffer = 0;
-    for (int group = (int)blockIdx.x; group < a.groups; group += (int)gridDim.x, buffer ^= 1) {
+    int ahead = position((int)blockIdx.x + stride);
+    int buffer = 0, at = 0;
+    for (int group = (int)blockIdx.x; group < a.groups; group += stride, buffer ^= 1, at = (at + 1) % ROT_DEPTH) {
         const long long t = (long long)group * a.tokens + tok;
-        const bool real = mine && t < a.T;
-#pragma unroll
-        for (int i = 0; i < U; ++i)
-#pragma unroll
-            for (int e = 0; e < V; ++e) va[i][e] = na[i][e], vb[i][e] = nb[i][e];
+        take(group, at);
+        fetch(coming, (at + ROT_DEPTH - 1) % ROT_DEPTH);
+        coming += stride;
         __syncthreads();                 // the group's turns are there; the other buffer's have been used
-        const int next = group + (int)gridDim.x;
-        if (next < a.groups) {
-            fetch((long long)next * a.tokens + tok);
-            turn(next, buffer ^ 1, ahead);
-            ahead = position(next + (int)gridDim.x);
+        if (group + stride < a.groups) {
+            turn(group + stride, buffer ^ 1, ahead);
+            ahead = position(group + 2 * stride);
         }
         float scale = 1.0f;
         if (a.norm) {
             auto squares = [&](float by) {
-                float s = 0.0f;
+                float2 s = make_float2(0.0f, 0.0f);
 #pragma unroll
-                for (int i = 0; i < U; ++i)
+                for (int i = 0; i < U; ++i) {
+                    if constexpr (V == 8) {
 #pragma unroll
-                    for (int e = 0; e < V; ++e) {
-                        const float fa = va[i][e] * by, fb = vb[i][e] * by;
-                        s = fmaf(fa, fa, s);
-                        s = fmaf(fb, fb, s);
+                        for (int e = 0; e < V; e += 2) {
+                            const float2 k = make_float2(by, by);
+                            const float2 fa = mul2(make_float2(va[i][e], va[i][e + 1]), k);
+                            const float2 fb = mul2(make_float2(vb[i][e], vb[i][e + 1]), k);
+                            s = fma2(fa, fa, s);
+                            s = fma2(fb, fb, s);
+                        }
+                    } else {
+                        s.x = __fmaf_rn(va[i][0] * by, va[i][0] * by, s.x);
+                        s.y = __fmaf_rn(vb[i][0] * by, vb[i][0] * by, s.y);
                     }
-                for (int o = 1; o < a.per; o <<= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-                return s;
+                }
+                float sum = s.x + s.y;
+                for (int o = 1; o < a.per; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                return sum;
             };
             const float mean = fmaf(squares(1.0f), a.inv_dim, a.eps);
             scale = __frsqrt_rn(mean);
@@ -208,7 +249,7 @@ rotate_kernel(const RotateArgs a)
                 if (big) scale = __frsqrt_rn(small) * 0x1p-80f;
             }
         }
-        if (!real) continue;
+        if (!mine || t >= a.T) continue;
 #pragma unroll
         for (int i = 0; i < U; ++i) {
             const int u = lane + i * a.per;
@@ -216,40 +257,60 @@ rotate_kernel(const RotateArgs a)
             if (a.norm) {
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    va[i][e] = va[i][e] * scale * wa[i][e];
-                    vb[i][e] = vb[i][e] * scale * wb[i][e];
+                    va[i][e] = __fmul_rn(__fmul_rn(va[i][e], scale), wa[i][e]);
+                    vb[i][e] = __fmul_rn(__fmul_rn(vb[i][e], scale), wb[i][e]);
                 }
             }
             if (u < half / V) {
-                float2 cs[V];
-                take<V>(turned + buffer * size + place<V>(tok * half + u * V), cs);
-                if (NEIGHBOURS && V > 1) {
+                const float *const cs = turned + buffer * size + place<V>(tok * half + u * V);
+                float c[V], sn[V];
+                if constexpr (V == 8) {
+#pragma unroll
+                    for (int e = 0; e < 8; e += 4) {
+                        const float4 f = *reinterpret_cast<const float4 *>(cs + e);
+                        const float4 h = *reinterpret_cast<const float4 *>(cs + 8 + e);
+                        c[e] = f.x, c[e + 1] = f.y, c[e + 2] = f.z, c[e + 3] = f.w;
+                        sn[e] = h.x, sn[e + 1] = h.y, sn[e + 2] = h.z, sn[e + 3] = h.w;
+                    }
+                } else {
+                    c[0] = cs[0];
+                    sn[0] = cs[1];
+                }
+                if constexpr (NEIGHBOURS && V > 1) {
                     // pairs (va[0], va[1]), .., (vb[0], vb[1]), ..
 #pragma unroll
                     for (int e = 0; e < V; e += 2) {
-                        const float2 ca = cs[e / 2], cb = cs[V / 2 + e / 2];
-                        float l = va[i][e], r = va[i][e + 1];
-                        va[i][e] = l * ca.x - r * ca.y;
-                        va[i][e + 1] = r * ca.x + l * ca.y;
-                        l = vb[i][e], r = vb[i][e + 1];
-                        vb[i][e] = l * cb.x - r * cb.y;
-                        vb[i][e + 1] = r * cb.x + l * cb.y;
+                        turn_pair(va[i][e], va[i][e + 1], c[e / 2], sn[e / 2]);
+                        turn_pair(vb[i][e], vb[i][e + 1], c[V / 2 + e / 2], sn[V / 2 + e / 2]);
+                    }
+                } else if constexpr (V > 1) {
+#pragma unroll
+                    for (int e = 0; e < V; e += 2) {     // turn_pair's roundings, two at once
+                        const float2 l = make_float2(va[i][e], va[i][e + 1]), r = make_float2(vb[i][e], vb[i][e + 1]);
+                        const float2 k = make_float2(c[e], c[e + 1]), h = make_float2(sn[e], sn[e + 1]);
+                        const float2 m = fma2(r, make_float2(-h.x, -h.y), mul2(l, k)), n = fma2(l, h, mul2(r, k));
+                        va[i][e] = m.x, va[i][e + 1] = m.y;
+                        vb[i][e] = n.x, vb[i][e + 1] = n.y;
                     }
                 } else {
-#pragma unroll
-                    for (int e = 0; e < V; ++e) {
-                        const float2 c = cs[e];
-                        const float l = va[i][e], r = vb[i][e];
-                        va[i][e] = l * c.x - r * c.y;
-                        vb[i][e] = r * c.x + l * c.y;
-                    }
+                    turn_pair(va[i][0], vb[i][0], c[0], sn[0]);
                 }
             }
             if (!MPQ_CHECK(t < a.T && ia[i] + V <= a.dim && ib[i] + V <= a.dim)) continue;
-            store_v<VEC>(y + p.ldy_token * t + ia[i], va[i]);
-            store_v<VEC>(y + p.ldy_token * t + ib[i], vb[i]);
+            T *const to = y + p.ldy_token * t;
+            if constexpr (VEC) {
+                store8(to + ia[i], va[i]);
+                store8(to + ib[i], vb[i]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    to[ia[i] + e] = from_f32<T>(va[i][e]);
+                    to[ib[i] + e] = from_f32<T>(vb[i][e]);
+                }
+            }
         }
     }
+    sm100::cp_async_wait_all();
 }
 
 // Strides and bases of rows that take 16-byte accesses.
@@ -292,15 +353,20 @@ mpq_status launch_rotate(const mpq_rotate_rows *q, const mpq_rotate_rows *k, int
     const int threads = (a.tokens * a.rows * a.per + 31) / 32 * 32, ys = (heads + a.rows - 1) / a.rows;
     const int resident = std::max(1, 1536 / threads) * sm_count();
     const dim3 grid((unsigned)std::min(a.groups, std::max(1, resident / ys)), (unsigned)ys);
-    const size_t smem = 2 * (size_t)(wide ? place<8>(a.tokens * (rot / 2)) : a.tokens * (rot / 2)) * sizeof(float2);
+    const int entries = a.tokens * (rot / 2);
+    size_t smem = 2 * (size_t)(wide ? place<8>(entries) : place<1>(entries)) * sizeof(float);
+    if (wide && vec) smem += (size_t)ROT_DEPTH * threads * 16 * type_size(type);
     return by_type(type, [&](auto t) {
         using E = decltype(t);
         auto *const kernel =
             !wide ? (neighbours ? rotate_kernel<E, 1, 8, true, false> : rotate_kernel<E, 1, 8, false, false>)
             : vec ? (neighbours ? rotate_kernel<E, 8, 1, true, true> : rotate_kernel<E, 8, 1, false, true>)
                   : (neighbours ? rotate_kernel<E, 8, 1, true, false> : rotate_kernel<E, 8, 1, false, false>);
-        return launch_waiting(kernel,
-                              grid, dim3((unsigned)threads), smem, stream, "rotate launch", a);
+        static std::atomic<int> limit[6][kMaxDevices];
+        const cudaError_t e = allow_smem(reinterpret_cast<const void *>(kernel),
+                                         limit[(wide ? vec ? 2 : 1 : 0) * 2 + neighbours], smem);
+        if (e != cudaSuccess) return cuda_status(e, "cudaFuncSetAttribute");
+        return launch_waiting(kernel, grid, dim3((unsigned)threads), smem, stream, "rotate launch", a);
     });
 }
 

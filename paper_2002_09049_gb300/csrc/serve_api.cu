@@ -363,6 +363,7 @@ extern "C" mpq_status mpq_rotate(const mpq_rotate_rows *q, const mpq_rotate_rows
     if (st != MPQ_OK) return st;
     REQUIRE(q, MPQ_ERR_INVALID_ARG, "q must be non-NULL");
     REQUIRE(T >= 0, MPQ_ERR_INVALID_ARG, "T = %d must be >= 0", T);
+    REQUIRE(T <= 1 << 30, MPQ_ERR_UNSUPPORTED, "T = %d exceeds 2^30", T);
     REQUIRE(dim >= 2 && dim % 2 == 0, MPQ_ERR_INVALID_ARG, "dim = %d must be even, >= 2", dim);
     REQUIRE(dim <= 512, MPQ_ERR_UNSUPPORTED, "dim = %d exceeds 512", dim);
     REQUIRE(rot >= 0 && rot % 2 == 0 && rot <= dim, MPQ_ERR_INVALID_ARG, "rot = %d must be even, 0..dim", rot);

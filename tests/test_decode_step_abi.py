@@ -124,7 +124,7 @@ def test_rotate_refuses(lib):
                 dict(positions=None), dict(turns=None), dict(positions=FAKE + 2), dict(turns=FAKE + 4)):
         assert f(**bad) == 1, bad
     assert f(norm=1, eps=float("nan")) == 2 and f(norm=1, eps=float("inf")) == 2
-    assert f(dim=514, rot=0) == 3 and f(q=rows(heads=65537)) == 3
+    assert f(T=(1 << 30) + 1) == 3 and f(dim=514, rot=0) == 3 and f(q=rows(heads=65537)) == 3
     for bad in (dict(x=None), dict(y=None), dict(heads=-1), dict(ld_token=-1), dict(ld_head=-1),
                 dict(x=FAKE + 1), dict(y=FAKE + 1), dict(weight=FAKE),             # weights without a norm
                 dict(ldy_head=63), dict(ldy_token=255),                            # output rows overlap
