@@ -14,6 +14,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "elements.cuh"
 #include "mpq_internal.cuh"
@@ -24,7 +25,6 @@ MPQ_CHECKED_UNIT("rotate.cu");
 namespace mpq {
 namespace {
 
-constexpr int ROT_MAX_DIM = 512;
 
 struct RotateArgs {
     mpq_rotate_rows part[2];             // queries, keys (heads 0: none)
@@ -68,10 +68,10 @@ __device__ __forceinline__ void unit_at(int u, int rot, bool neighbours, int &ia
     }
 }
 
-// Where pair i's cosine lies, in floats, and how far its sine: eight cosines and eight sines, such eights 80 bytes apart, so
-// that eight threads that read theirs, 16 bytes at a time, meet no bank twice.
+// Where pair i's cosine lies, in floats, and how far its sine: eight cosines, eight sines and their negatives, such eights
+// 112 bytes apart, so that eight threads that read theirs, 16 bytes at a time, meet no bank twice.
 template <int V>
-__host__ __device__ constexpr int place(int i) { return V == 8 ? (i >> 3) * 20 + (i & 7) : 2 * i; }
+__host__ __device__ constexpr int place(int i) { return V == 8 ? (i >> 3) * 28 + (i & 7) : 2 * i; }
 template <int V>
 constexpr int kSine = V == 8 ? 8 : 1;
 
@@ -118,28 +118,34 @@ rotate_kernel(const RotateArgs a)
     const bool mine = tok < a.tokens && row < heads, key = row >= a.part[0].heads;
     const mpq_rotate_rows &p = a.part[key ? 1 : 0];
     const int head = key ? row - a.part[0].heads : row;
-    const T *const x = static_cast<const T *>(p.x) + p.ld_head * head;
-    T *const y = static_cast<T *>(p.y) + p.ldy_head * head;
+    const int stride = (int)gridDim.x;
+    // the token that is fetched next and the one that is turned, by addresses: both go on by a group of every CTA
+    int t = (int)blockIdx.x * a.tokens + tok, t_next = t;
+    const int t_step = stride * a.tokens;
+    const T *x = static_cast<const T *>(p.x) + p.ld_head * head + p.ld_token * t;
+    T *y = static_cast<T *>(p.y) + p.ldy_head * head + p.ldy_token * t;
+    const long long x_step = p.ld_token * t_step, y_step = p.ldy_token * t_step;
+    const float *const weight = p.weight;
     int ia[U], ib[U];
 #pragma unroll
     for (int i = 0; i < U; ++i) unit_at<V>(lane + i * a.per, a.rot, NEIGHBOURS, ia[i], ib[i]);
     float va[U][V], vb[U][V];            // the group's elements
     // a token's elements on their way to shared memory (nothing where there is no such token)
-    auto fetch = [&](int group, int slot_at) {
+    auto fetch = [&](int slot_at) {
         if constexpr (VEC) {
-            const long long t = (long long)group * a.tokens + tok;
-            const uint32_t bytes = mine && lane < units && t < a.T ? 16u : 0u;
-            const T *const from = bytes ? x + p.ld_token * t : static_cast<const T *>(p.x);
+            const uint32_t bytes = mine && lane < units && t_next < a.T ? 16u : 0u;
 #pragma unroll
             for (int c = 0; c < CHUNKS; ++c) {
                 const int at = (c < CHUNKS / 2 ? ia[0] : ib[0]) + c % (CHUNKS / 2) * (16 / (int)sizeof(T));
                 sm100::cp_async16(sm100::smem_u32(staged + (slot_at * CHUNKS + c) * (int)blockDim.x + (int)threadIdx.x),
-                                  bytes ? from + at : from, bytes);
+                                  x + at, bytes);
             }
             sm100::cp_async_commit();
+            x += x_step;
+            t_next += t_step;
         }
     };
-    auto take = [&](int group, int slot_at) {
+    auto take = [&](int slot_at) {
         if constexpr (VEC) {
             sm100::cp_async_wait<ROT_DEPTH - 2>();
             const uint4 *const q = staged + slot_at * CHUNKS * (int)blockDim.x + (int)threadIdx.x;
@@ -155,7 +161,6 @@ rotate_kernel(const RotateArgs a)
                 }
             }
         } else {
-            const long long t = (long long)group * a.tokens + tok;
 #pragma unroll
             for (int i = 0; i < U; ++i) {
 #pragma unroll
@@ -163,10 +168,11 @@ rotate_kernel(const RotateArgs a)
                 if (!mine || t >= a.T || lane + i * a.per >= units) continue;
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    va[i][e] = to_f32(x[p.ld_token * t + ia[i] + e]);
-                    vb[i][e] = to_f32(x[p.ld_token * t + ib[i] + e]);
+                    va[i][e] = to_f32(x[ia[i] + e]);
+                    vb[i][e] = to_f32(x[ib[i] + e]);
                 }
             }
+            x += x_step;
         }
     };
     // a thread makes the same frequency's turns of every group (and others', where there are more than threads)
@@ -181,6 +187,7 @@ rotate_kernel(const RotateArgs a)
         float *const to = turned + buffer * size + place<V>(i);
         to[0] = c.x;
         to[kSine<V>] = c.y;
+        if (V == 8) to[16] = -c.y;
     };
     auto turn = [&](int group, int buffer, int at) {
         if (own < entries) keep(buffer, own, (uint64_t)((long long)at + a.shift) * own_turn);
@@ -195,22 +202,19 @@ rotate_kernel(const RotateArgs a)
     for (int i = 0; i < U; ++i)
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-            const bool has = mine && p.weight && lane + i * a.per < units;
-            wa[i][e] = has ? p.weight[ia[i] + e] : 1.0f;
-            wb[i][e] = has ? p.weight[ib[i] + e] : 1.0f;
+            const bool has = mine && weight && lane + i * a.per < units;
+            wa[i][e] = has ? weight[ia[i] + e] : 1.0f;
+            wb[i][e] = has ? weight[ib[i] + e] : 1.0f;
         }
-    const int stride = (int)gridDim.x;
-    int coming = (int)blockIdx.x;        // the group that is fetched next
 #pragma unroll
-    for (int i = 0; i < ROT_DEPTH - 1; ++i, coming += stride) fetch(coming, i);
+    for (int i = 0; i < ROT_DEPTH - 1; ++i) fetch(i);
     turn((int)blockIdx.x, 0, position((int)blockIdx.x));
     int ahead = position((int)blockIdx.x + stride);
     int buffer = 0, at = 0;
-    for (int group = (int)blockIdx.x; group < a.groups; group += stride, buffer ^= 1, at = (at + 1) % ROT_DEPTH) {
-        const long long t = (long long)group * a.tokens + tok;
-        take(group, at);
-        fetch(coming, (at + ROT_DEPTH - 1) % ROT_DEPTH);
-        coming += stride;
+    for (int group = (int)blockIdx.x; group < a.groups;
+         group += stride, buffer ^= 1, at = (at + 1) % ROT_DEPTH, t += t_step, y += y_step) {
+        take(at);
+        fetch((at + ROT_DEPTH - 1) % ROT_DEPTH);
         __syncthreads();                 // the group's turns are there; the other buffer's have been used
         if (group + stride < a.groups) {
             turn(group + stride, buffer ^ 1, ahead);
@@ -218,16 +222,19 @@ rotate_kernel(const RotateArgs a)
         }
         float scale = 1.0f;
         if (a.norm) {
-            auto squares = [&](float by) {
+            auto squares = [&](auto small) {
+                const float by = decltype(small)::value ? 0x1p-80f : 1.0f;
                 float2 s = make_float2(0.0f, 0.0f);
 #pragma unroll
                 for (int i = 0; i < U; ++i) {
                     if constexpr (V == 8) {
 #pragma unroll
                         for (int e = 0; e < V; e += 2) {
-                            const float2 k = make_float2(by, by);
-                            const float2 fa = mul2(make_float2(va[i][e], va[i][e + 1]), k);
-                            const float2 fb = mul2(make_float2(vb[i][e], vb[i][e + 1]), k);
+                            float2 fa = make_float2(va[i][e], va[i][e + 1]), fb = make_float2(vb[i][e], vb[i][e + 1]);
+                            if (decltype(small)::value) {
+                                fa = mul2(fa, make_float2(by, by));
+                                fb = mul2(fb, make_float2(by, by));
+                            }
                             s = fma2(fa, fa, s);
                             s = fma2(fb, fb, s);
                         }
@@ -240,12 +247,12 @@ rotate_kernel(const RotateArgs a)
                 for (int o = 1; o < a.per; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
                 return sum;
             };
-            const float mean = fmaf(squares(1.0f), a.inv_dim, a.eps);
+            const float mean = fmaf(squares(std::false_type()), a.inv_dim, a.eps);
             scale = __frsqrt_rn(mean);
             // squares beyond fp32's range (elements above 2^60): again, of 2^-80 of them
             const bool big = isinf(mean);
             if (__any_sync(0xffffffffu, big)) {
-                const float small = fmaf(squares(0x1p-80f), a.inv_dim, a.eps * 0x1p-80f * 0x1p-80f);
+                const float small = fmaf(squares(std::true_type()), a.inv_dim, a.eps * 0x1p-80f * 0x1p-80f);
                 if (big) scale = __frsqrt_rn(small) * 0x1p-80f;
             }
         }
@@ -255,15 +262,23 @@ rotate_kernel(const RotateArgs a)
             const int u = lane + i * a.per;
             if (u >= units) continue;
             if (a.norm) {
+                if constexpr (V == 8) {
+                    const float2 k = make_float2(scale, scale);
 #pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    va[i][e] = __fmul_rn(__fmul_rn(va[i][e], scale), wa[i][e]);
-                    vb[i][e] = __fmul_rn(__fmul_rn(vb[i][e], scale), wb[i][e]);
+                    for (int e = 0; e < V; e += 2) {
+                        const float2 l = mul2(mul2(make_float2(va[i][e], va[i][e + 1]), k), make_float2(wa[i][e], wa[i][e + 1]));
+                        const float2 r = mul2(mul2(make_float2(vb[i][e], vb[i][e + 1]), k), make_float2(wb[i][e], wb[i][e + 1]));
+                        va[i][e] = l.x, va[i][e + 1] = l.y;
+                        vb[i][e] = r.x, vb[i][e + 1] = r.y;
+                    }
+                } else {
+                    va[i][0] = __fmul_rn(__fmul_rn(va[i][0], scale), wa[i][0]);
+                    vb[i][0] = __fmul_rn(__fmul_rn(vb[i][0], scale), wb[i][0]);
                 }
             }
             if (u < half / V) {
                 const float *const cs = turned + buffer * size + place<V>(tok * half + u * V);
-                float c[V], sn[V];
+                float c[V], sn[V], ns[V];         // (cosines, sines, their negatives)
                 if constexpr (V == 8) {
 #pragma unroll
                     for (int e = 0; e < 8; e += 4) {
@@ -271,6 +286,8 @@ rotate_kernel(const RotateArgs a)
                         const float4 h = *reinterpret_cast<const float4 *>(cs + 8 + e);
                         c[e] = f.x, c[e + 1] = f.y, c[e + 2] = f.z, c[e + 3] = f.w;
                         sn[e] = h.x, sn[e + 1] = h.y, sn[e + 2] = h.z, sn[e + 3] = h.w;
+                        const float4 n = *reinterpret_cast<const float4 *>(cs + 16 + e);
+                        ns[e] = n.x, ns[e + 1] = n.y, ns[e + 2] = n.z, ns[e + 3] = n.w;
                     }
                 } else {
                     c[0] = cs[0];
@@ -288,7 +305,7 @@ rotate_kernel(const RotateArgs a)
                     for (int e = 0; e < V; e += 2) {     // turn_pair's roundings, two at once
                         const float2 l = make_float2(va[i][e], va[i][e + 1]), r = make_float2(vb[i][e], vb[i][e + 1]);
                         const float2 k = make_float2(c[e], c[e + 1]), h = make_float2(sn[e], sn[e + 1]);
-                        const float2 m = fma2(r, make_float2(-h.x, -h.y), mul2(l, k)), n = fma2(l, h, mul2(r, k));
+                        const float2 m = fma2(r, make_float2(ns[e], ns[e + 1]), mul2(l, k)), n = fma2(l, h, mul2(r, k));
                         va[i][e] = m.x, va[i][e + 1] = m.y;
                         vb[i][e] = n.x, vb[i][e + 1] = n.y;
                     }
@@ -297,15 +314,14 @@ rotate_kernel(const RotateArgs a)
                 }
             }
             if (!MPQ_CHECK(t < a.T && ia[i] + V <= a.dim && ib[i] + V <= a.dim)) continue;
-            T *const to = y + p.ldy_token * t;
             if constexpr (VEC) {
-                store8(to + ia[i], va[i]);
-                store8(to + ib[i], vb[i]);
+                store8(y + ia[i], va[i]);
+                store8(y + ib[i], vb[i]);
             } else {
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    to[ia[i] + e] = from_f32<T>(va[i][e]);
-                    to[ib[i] + e] = from_f32<T>(vb[i][e]);
+                    y[ia[i] + e] = from_f32<T>(va[i][e]);
+                    y[ib[i] + e] = from_f32<T>(vb[i][e]);
                 }
             }
         }
@@ -351,7 +367,9 @@ mpq_status launch_rotate(const mpq_rotate_rows *q, const mpq_rotate_rows *k, int
     a.tokens = (int)std::max(1LL, std::min<long long>(256 / (a.rows * a.per), T));
     a.groups = (int)((T + (long long)a.tokens - 1) / a.tokens);
     const int threads = (a.tokens * a.rows * a.per + 31) / 32 * 32, ys = (heads + a.rows - 1) / a.rows;
-    const int resident = std::max(1, 1536 / threads) * sm_count();
+    // CTAs that are resident at once: 64 registers a thread in the wide 16-bit form, 128 in the others
+    const int regs = wide && vec && type != MPQ_F32 ? 64 : 128;
+    const int resident = std::max(1, 65536 / (regs * threads)) * sm_count();
     const dim3 grid((unsigned)std::min(a.groups, std::max(1, resident / ys)), (unsigned)ys);
     const int entries = a.tokens * (rot / 2);
     size_t smem = 2 * (size_t)(wide ? place<8>(entries) : place<1>(entries)) * sizeof(float);
