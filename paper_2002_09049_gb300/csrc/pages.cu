@@ -102,16 +102,26 @@ __device__ __forceinline__ bool last_cta(int *counter)
     return last != 0;
 }
 
-// What request b asks of the pool: pages, and whether its length and numbers allow it.
+// Every request's want and length into shared memory (where `start` and `len` will be), a warp's consecutive.
+__device__ __forceinline__ void load_requests(const PageArgs &a, int *want, int *len)
+{
+    for (int b = (int)threadIdx.x; b < a.B; b += (int)blockDim.x) {
+        want[b] = a.want[b];
+        len[b] = a.lens[b];
+    }
+    __syncthreads();
+}
+
+// What a request asks of the pool: pages, and whether its length and numbers allow it.
 struct Ask {
     int len, add, need;
     bool fits;
 };
-__device__ __forceinline__ Ask ask(const PageArgs &a, int b)
+__device__ __forceinline__ Ask ask(const PageArgs &a, int want, int len)
 {
     Ask r;
-    r.len = a.lens[b];
-    r.add = max(a.want[b], 0);
+    r.len = len;
+    r.add = max(want, 0);
     r.need = 0;
     r.fits = r.len >= 0 && (long long)r.len + r.add <= (long long)a.page * a.cols;
     if (r.fits) r.need = pages_of(a, r.len + r.add) - pages_of(a, r.len);
@@ -127,17 +137,18 @@ __global__ void pages_extend_kernel(const PageArgs a, int *table, const int *poo
     sm100::griddep_launch();
     sm100::griddep_wait();
     const int have = min(max(a.count[0], 0), a.pages);
+    load_requests(a, k.start, k.len);
     // the thread's requests: their tokens, then (which of them fit in N is known) their pages
     const int per = (a.B + (int)blockDim.x - 1) / (int)blockDim.x;
     const int b0 = min((int)threadIdx.x * per, a.B), b1 = min(b0 + per, a.B);
     uint2 total;
     unsigned tokens = 0;
-    for (int b = b0; b < b1; ++b) tokens = add_most(tokens, (unsigned)max(a.want[b], 0));
+    for (int b = b0; b < b1; ++b) tokens = add_most(tokens, (unsigned)max(k.start[b], 0));
     const unsigned t0 = block_scan(make_uint2(tokens, 0), total, warps).x;
     const unsigned N = (unsigned)a.N, all = total.x;
     unsigned at = t0, need = 0;
     for (int b = b0; b < b1; ++b) {
-        const Ask r = ask(a, b);
+        const Ask r = ask(a, k.start[b], k.len[b]);
         at = add_most(at, (unsigned)r.add);
         if (r.fits && at <= N) need = add_most(need, (unsigned)r.need);
     }
@@ -148,7 +159,7 @@ __global__ void pages_extend_kernel(const PageArgs a, int *table, const int *poo
     const bool writer = !a.in_place && blockIdx.x == 0;
     at = t0;
     for (int b = b0; b < b1; ++b) {
-        const Ask r = ask(a, b);
+        const Ask r = ask(a, k.start[b], k.len[b]);
         const unsigned end = add_most(at, (unsigned)r.add);
         const bool fits = r.fits && end <= N;
         const unsigned upto = add_most(before, fits ? (unsigned)r.need : 0u);
@@ -236,17 +247,18 @@ __global__ void pages_trim_kernel(const PageArgs a, const int *table, int *pool)
     sm100::griddep_launch();
     sm100::griddep_wait();
     const int have = min(max(a.count[0], 0), a.pages);
+    load_requests(a, k.start, k.len);
     const int per = (a.B + (int)blockDim.x - 1) / (int)blockDim.x;
     const int b0 = min((int)threadIdx.x * per, a.B), b1 = min(b0 + per, a.B);
     const int longest = a.page * a.cols;     // up to 2^30
-    auto cut = [&](int b, int &len, int &keep) {
-        len = min(max(a.lens[b], 0), longest);
-        keep = min(max(a.want[b], 0), len);
+    auto cut = [&](int want, int n, int &len, int &keep) {
+        len = min(max(n, 0), longest);
+        keep = min(max(want, 0), len);
     };
     unsigned back = 0;
     for (int b = b0; b < b1; ++b) {
         int len, keep;
-        cut(b, len, keep);
+        cut(k.start[b], k.len[b], len, keep);
         back = add_most(back, (unsigned)(pages_of(a, len) - pages_of(a, keep)));
     }
     uint2 total;
@@ -254,7 +266,7 @@ __global__ void pages_trim_kernel(const PageArgs a, const int *table, int *pool)
     const bool writer = !a.in_place && blockIdx.x == 0;
     for (int b = b0; b < b1; ++b) {
         int len, keep;
-        cut(b, len, keep);
+        cut(k.start[b], k.len[b], len, keep);
         k.start[b] = (int)before;
         k.len[b] = pages_of(a, keep);
         before = add_most(before, (unsigned)(pages_of(a, len) - pages_of(a, keep)));
@@ -283,7 +295,7 @@ __global__ void pages_trim_kernel(const PageArgs a, const int *table, int *pool)
     __syncthreads();
     for (int b = (int)threadIdx.x; b < a.B; b += (int)blockDim.x) {
         int len, keep;
-        cut(b, len, keep);
+        cut(a.want[b], a.lens[b], len, keep);
         a.new_lens[b] = keep;
     }
     if (threadIdx.x == 0) {
