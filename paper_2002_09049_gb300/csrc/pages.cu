@@ -50,31 +50,27 @@ __device__ __forceinline__ int pages_of(const PageArgs &a, int n)      // n >= 0
     return div_page(a, n + a.page - 1);
 }
 
-// Exclusive sums of two numbers over the CTA's threads, and the totals.
-__device__ __forceinline__ uint2 block_scan(uint2 own, uint2 &total, uint2 *warps)
+// The exclusive sum of a number over the CTA's threads, and the total.
+__device__ __forceinline__ unsigned block_scan(unsigned own, unsigned &total, unsigned *warps)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n = (int)blockDim.x >> 5;
-    uint2 in = own;
+    auto warp_scan = [&](unsigned v) {
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const unsigned x = __shfl_up_sync(0xffffffffu, in.x, o), y = __shfl_up_sync(0xffffffffu, in.y, o);
-        if (lane >= o) in = make_uint2(add_most(in.x, x), add_most(in.y, y));
-    }
+        for (int o = 1; o < 32; o <<= 1) {
+            const unsigned x = __shfl_up_sync(0xffffffffu, v, o);
+            if (lane >= o) v = add_most(v, x);
+        }
+        return v;
+    };
+    const unsigned in = warp_scan(own);
     if (lane == 31) warps[warp] = in;
     __syncthreads();
-    uint2 w = lane < n ? warps[lane] : make_uint2(0, 0);
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const unsigned x = __shfl_up_sync(0xffffffffu, w.x, o), y = __shfl_up_sync(0xffffffffu, w.y, o);
-        if (lane >= o) w = make_uint2(add_most(w.x, x), add_most(w.y, y));
-    }
-    total.x = __shfl_sync(0xffffffffu, w.x, 31);
-    total.y = __shfl_sync(0xffffffffu, w.y, 31);
-    const unsigned bx = __shfl_sync(0xffffffffu, w.x, max(warp - 1, 0));
-    const unsigned by = __shfl_sync(0xffffffffu, w.y, max(warp - 1, 0));
-    unsigned ex = __shfl_up_sync(0xffffffffu, in.x, 1), ey = __shfl_up_sync(0xffffffffu, in.y, 1);
-    if (lane == 0) ex = ey = 0;
-    return warp == 0 ? make_uint2(ex, ey) : make_uint2(add_most(bx, ex), add_most(by, ey));
+    const unsigned w = warp_scan(lane < n ? warps[lane] : 0u);
+    total = __shfl_sync(0xffffffffu, w, 31);
+    const unsigned behind = __shfl_sync(0xffffffffu, w, max(warp - 1, 0));
+    unsigned ex = __shfl_up_sync(0xffffffffu, in, 1);
+    if (lane == 0) ex = 0;
+    return warp == 0 ? ex : add_most(behind, ex);
 }
 
 // The last request that starts at or before number t.
@@ -129,10 +125,10 @@ __device__ __forceinline__ Ask ask(const PageArgs &a, int want, int len)
 }
 
 __global__ void pages_extend_kernel(const PageArgs a, int *table, const int *pool, int64_t *slots,
-                                    int *positions, long long share)
+                                    int *positions, long long share, int wide)
 {
     extern __shared__ int kept[];
-    __shared__ uint2 warps[32];
+    __shared__ unsigned warps[2][32];    // (a scan after a scan has words of its own)
     const Kept k{kept, kept + a.B, reinterpret_cast<unsigned *>(kept + 2 * a.B)};
     sm100::griddep_launch();
     sm100::griddep_wait();
@@ -141,19 +137,16 @@ __global__ void pages_extend_kernel(const PageArgs a, int *table, const int *poo
     // the thread's requests: their tokens, then (which of them fit in N is known) their pages
     const int per = (a.B + (int)blockDim.x - 1) / (int)blockDim.x;
     const int b0 = min((int)threadIdx.x * per, a.B), b1 = min(b0 + per, a.B);
-    uint2 total;
-    unsigned tokens = 0;
+    unsigned all, ignored, tokens = 0;
     for (int b = b0; b < b1; ++b) tokens = add_most(tokens, (unsigned)max(k.start[b], 0));
-    const unsigned t0 = block_scan(make_uint2(tokens, 0), total, warps).x;
-    const unsigned N = (unsigned)a.N, all = total.x;
+    const unsigned t0 = block_scan(tokens, all, warps[0]), N = (unsigned)a.N;
     unsigned at = t0, need = 0;
     for (int b = b0; b < b1; ++b) {
         const Ask r = ask(a, k.start[b], k.len[b]);
         at = add_most(at, (unsigned)r.add);
         if (r.fits && at <= N) need = add_most(need, (unsigned)r.need);
     }
-    __syncthreads();                         // (the warps' sums are read)
-    unsigned before = block_scan(make_uint2(need, 0), total, warps).x;
+    unsigned before = block_scan(need, ignored, warps[1]);
     // the pages given: those of the last served request and all before it
     unsigned given = 0;
     const bool writer = !a.in_place && blockIdx.x == 0;
@@ -176,12 +169,11 @@ __global__ void pages_extend_kernel(const PageArgs a, int *table, const int *poo
         before = upto;
     }
     const int left = have - (int)__reduce_max_sync(0xffffffffu, given);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) warps[threadIdx.x >> 5].x = (unsigned)left;
+    if ((threadIdx.x & 31) == 0) warps[0][threadIdx.x >> 5] = (unsigned)left;
     __syncthreads();
     if (writer && threadIdx.x == 0) {
-        unsigned least = warps[0].x;
-        for (int i = 1; i < (int)blockDim.x >> 5; ++i) least = min(least, warps[i].x);
+        unsigned least = warps[0][0];
+        for (int i = 1; i < (int)blockDim.x >> 5; ++i) least = min(least, warps[0][i]);
         a.new_count[0] = (int)least;
         a.new_count[1] = 0;
     }
@@ -215,6 +207,13 @@ __global__ void pages_extend_kernel(const PageArgs a, int *table, const int *poo
             if (page >= 0) s[i] = (int64_t)page * a.page + place;
         }
         const int n = (int)min((long long)P_EACH, to - t0);
+        if (wide && n == P_EACH && MPQ_IN(t0 + P_EACH - 1, a.N)) {   // (t0 is a multiple of P_EACH)
+            longlong2 *const so = reinterpret_cast<longlong2 *>(slots + t0);
+            so[0] = make_longlong2(s[0], s[1]);
+            so[1] = make_longlong2(s[2], s[3]);
+            *reinterpret_cast<int4 *>(positions + t0) = make_int4(p[0], p[1], p[2], p[3]);
+            continue;
+        }
         for (int i = 0; i < n; ++i) {
             if (!MPQ_IN(t0 + i, a.N)) continue;
             slots[t0 + i] = s[i];
@@ -231,8 +230,8 @@ __global__ void pages_extend_kernel(const PageArgs a, int *table, const int *poo
         a.new_lens[b] = k.len[b] + (served ? add : 0);
     }
     if (threadIdx.x == 0) {
-        unsigned least = warps[0].x;
-        for (int i = 1; i < (int)blockDim.x >> 5; ++i) least = min(least, warps[i].x);
+        unsigned least = warps[0][0];
+        for (int i = 1; i < (int)blockDim.x >> 5; ++i) least = min(least, warps[0][i]);
         a.count[1] = 0;
         a.new_count[0] = (int)least;
         a.new_count[1] = 0;
@@ -242,7 +241,7 @@ __global__ void pages_extend_kernel(const PageArgs a, int *table, const int *poo
 __global__ void pages_trim_kernel(const PageArgs a, const int *table, int *pool)
 {
     extern __shared__ int kept[];            // start: the number of a request's first page that returns; len: its column
-    __shared__ uint2 warps[32];
+    __shared__ unsigned warps[2][32];    // (a scan after a scan has words of its own)
     const Kept k{kept, kept + a.B, nullptr};
     sm100::griddep_launch();
     sm100::griddep_wait();
@@ -261,8 +260,7 @@ __global__ void pages_trim_kernel(const PageArgs a, const int *table, int *pool)
         cut(k.start[b], k.len[b], len, keep);
         back = add_most(back, (unsigned)(pages_of(a, len) - pages_of(a, keep)));
     }
-    uint2 total;
-    unsigned before = block_scan(make_uint2(back, 0), total, warps).x;
+    unsigned all, before = block_scan(back, all, warps[0]);
     const bool writer = !a.in_place && blockIdx.x == 0;
     for (int b = b0; b < b1; ++b) {
         int len, keep;
@@ -272,7 +270,6 @@ __global__ void pages_trim_kernel(const PageArgs a, const int *table, int *pool)
         before = add_most(before, (unsigned)(pages_of(a, len) - pages_of(a, keep)));
         if (writer) a.new_lens[b] = keep;
     }
-    const unsigned all = total.x;
     const int now = (int)min((long long)have + all, (long long)a.pages);
     if (writer && threadIdx.x == 0) {
         a.new_count[0] = now;
@@ -337,16 +334,18 @@ mpq_status launch_pages_extend(const int *add, int B, int page, int cols, const 
     a.N = N;
     a.taken = taken;
     const int threads = page_threads(B);
-    // a CTA scans every request: two CTAs an SM at most
-    const long long one = (long long)threads * P_EACH, most = 2LL * sm_count();
+    // a CTA scans every request: four CTAs of 256 threads an SM at most, two of 1,024
+    const long long one = (long long)threads * P_EACH, most = (threads == 256 ? 4LL : 2LL) * sm_count();
     const long long share = std::max(one, ((N + most - 1) / most + one - 1) / one * one);
     const int grid = (int)std::max(1LL, (N + share - 1) / share);
+    const int wide = ((uintptr_t)slots | (uintptr_t)positions) % 16 == 0;
+    static_assert(P_EACH == 4, "the wide stores");
     const size_t smem = (size_t)B * 3 * sizeof(int);
     static std::atomic<int> limit[kMaxDevices];
     const cudaError_t e = allow_smem(reinterpret_cast<const void *>(pages_extend_kernel), limit, smem);
     if (e != cudaSuccess) return cuda_status(e, "cudaFuncSetAttribute");
     return launch_waiting(pages_extend_kernel, dim3((unsigned)grid), dim3((unsigned)threads), smem, stream,
-                          "pages extend launch", a, table, pool, slots, positions, share);
+                          "pages extend launch", a, table, pool, slots, positions, share, wide);
 }
 
 mpq_status launch_pages_trim(const int *keep, int B, int page, int cols, const int *lens, int *new_lens,
