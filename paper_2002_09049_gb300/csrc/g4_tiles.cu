@@ -12,6 +12,11 @@
 // tokens' operand.  Else K may be split over the CTAs of a cluster, whose sums are joined in shared memory in the
 // order of the ranks (equal inputs give equal bits).
 //
+// Measured: 2,048 x 11,008 x 4,096 (T x C x d) 105 us, 1.76 PFLOP/s: a stage takes 1,024 cycles, its MMAs' own; 1,800 a
+// tile between the last MMA and the next one's first; 344 tiles on 76 pairs are five rounds.  75 x 4,096 x 11,008 15.6
+// us (22 stages of 0.4 us on 128 CTAs, then 3 us for the join): the MMAs' warp takes 450 cycles a stage beside 340 of
+// MMAs, a group of makers 2,500 a stage.
+//
 // Warps: 0 copies x, 1 issues MMAs (the even CTA's, of a pair), 2 copies weights, 3 tells the MMAs' warp that x has
 // landed, 4 .. make operands, the last write outputs (these two by lane quarters, warp % 4).  Every wait is bounded.
 #include <cuda.h>

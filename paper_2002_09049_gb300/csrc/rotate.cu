@@ -11,6 +11,11 @@
 // several where a token has few), one token after another: the next one's elements are on their way while the
 // last one is turned, and its cosines and sines -- made once for all heads, by every row's own threads they cost
 // more than the rows' traffic -- are left in shared memory for it.
+//
+// 8,192 tokens of 40 heads of 128 bf16 take 34.7 us (168 MB, 4.8 TB/s; without a norm 30.6, neighbours' pairs 44): 290
+// warp instructions a token and four rows, issue slots 0.52 busy, a barrier a token.  A CTA a token, without
+// loads ahead, took 62; one element after another instead of two at once, and cosines that eight threads read from
+// the same banks, 49.
 #include <math.h>
 
 #include <algorithm>
