@@ -600,7 +600,8 @@ mpq_status mpq_g4_dequantize(const void *packed, const mpq_g4_matrix *layout, vo
  *         multiple of 8 elements are faster).
  *   bias  [C] fp32 or NULL.
  *   Y     out [T][C] of type y_type, rows ldy elements apart (ldy >= C).
- * T = 0 or C = 0 is an empty call; T above 2^20 is MPQ_ERR_UNSUPPORTED.  Equal inputs give equal bits from call
+ * Y overlaps no input.  T = 0 or C = 0 is an empty call; T above 2^20 is MPQ_ERR_UNSUPPORTED.  Rows of X off the 16-byte
+ * boundary are copied to scratch of the stream-ordered pool first where T is more than a few.  Equal inputs give equal bits from call
  * to call (sums of several CTAs are joined in a fixed order); another T may take another order of the sums.
  */
 mpq_status mpq_g4_linear(const void *X, int x_type, long long ldx, int T, const mpq_g4_matrix *w_layout,

@@ -305,6 +305,9 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
         for (int i = max(0, n - a.stages); lane == 0 && i < n; ++i)
             drain_wait(PAIR ? &ctl.x_full[i % a.stages] : &ctl.ready[i % a.stages], (uint32_t)(i / a.stages) & 1u, wc,
                        MPQ_TIMEOUT_G4);
+        // ... nor an arrival for the pair's MMAs
+        for (int i = max(0, n - a.stages); PAIR && lane == 0 && i < n && !*abort_flag; ++i)
+            drain_wait(&ctl.empty[i % a.stages], (uint32_t)(i / a.stages) & 1u, wc, MPQ_TIMEOUT_G4);
         __syncwarp();
     } else if (warp == 2) {
         // -------------------------------------------------------------------- copies of weights

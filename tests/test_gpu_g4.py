@@ -155,7 +155,8 @@ def within(y, want, tol):
     (16, 4096, 512), (17, 640, 1000), (33, 500, 64), (31, 127, 2176), (63, 256, 384), (65, 130, 512),
     (75, 520, 4096), (128, 128, 256), (129, 384, 640), (200, 64, 2560), (256, 256, 1024), (257, 129, 136),
     (700, 300, 776), (1030, 1030, 304), (3, 20000, 128), (513, 3001, 1000), (2100, 2050, 512), (5000, 300, 128),
-    (256, 4096, 4096), (208, 200, 9000), (250, 2000, 11008), (30, 600, 11000), (600, 700, 8200)])
+    (256, 4096, 4096), (208, 200, 9000), (250, 2000, 11008), (30, 600, 11000), (600, 700, 8200),
+    (300, 100, 1), (150, 20, 7), (200, 1, 4096), (129, 17, 65), (1000, 129, 33), (4000, 40, 200)])
 @pytest.mark.parametrize("group,zeros", [(32, True), (64, False), (128, True)])
 def test_linear(gpu, T, C, d, group, zeros):
     dtype, out = ("bf16", "fp16")[(T + C) % 2], list(TYPES)[(T + C + group // 32) % 3]
