@@ -6,7 +6,8 @@
 // lane; x comes by TMA into 128-byte-swizzled shared memory.  (Operands in shared memory too, 141 us
 // for 2,048 x 11,008 x 4,096: 64 KB in and out per 64 elements of K of a pair's CTA are 512 cycles at 128 bytes each,
 // as many as the MMAs take.)  Eight warps write the outputs.  Roles run over their CTA's tiles without a
-// pause; up to 128 tokens two accumulators take turns, and a tile's outputs leave while the next one is summed.
+// pause.  Up to 128 tokens two warps issue the MMAs of every other stage, into accumulators of their own whose sums are
+// added on the way out (one warp's waits and issue took 800 cycles a stage, 340 of them the MMAs').
 //
 // PAIR: CTA pairs (cta_group::2) take 256 channels x 256 tokens, each CTA its own channels and half of the
 // tokens' operand.  Else K may be split over the CTAs of a cluster, whose sums are joined in shared memory in the
@@ -44,11 +45,14 @@ constexpr int H_K = 128;                 // elements of K in a stage: a packed t
 constexpr int H_A_COLS = H_K / 2;        // TMEM columns of a stage's weights, two elements each
 constexpr int H_MAX_STAGES = 8;
 constexpr int H_MAX_PACKED = 8;
+// PAIRS: CTA pairs, 256 tokens.  NARROW: up to 128 tokens, two warps that issue MMAs, each with an accumulator of its own.
+// WIDE: up to 256, one.
+enum Shape { PAIRS, WIDE, NARROW };
 constexpr int H_MAKE0 = 4;               // first of the warps that make operands, in groups of four
-__host__ __device__ constexpr int makers(bool pair) { return pair ? 2 : 3; }
 constexpr int H_OUTS = 8;                // warps that write outputs, behind them
-__host__ __device__ constexpr int first_out(bool pair) { return H_MAKE0 + 4 * makers(pair); }
-__host__ __device__ constexpr int tile_threads(bool pair) { return (first_out(pair) + H_OUTS) * 32; }
+__host__ __device__ constexpr int makers(int shape) { return shape == PAIRS ? 2 : shape == WIDE ? 3 : 4; }
+__host__ __device__ constexpr int first_out(int shape) { return H_MAKE0 + 4 * makers(shape); }
+__host__ __device__ constexpr int tile_threads(int shape) { return (first_out(shape) + H_OUTS) * 32; }
 // Shared memory of a CTA, at least: more than half of an SM's, since each takes all tensor memory (a second one would
 // wait for it, and two clusters whose CTAs wait on each other's SMs would never begin)
 constexpr size_t H_MIN_SMEM = 120 * 1024;
@@ -59,8 +63,8 @@ struct TileCtrl {
     uint64_t empty[H_MAX_STAGES];        // the MMAs that read it completed
     uint64_t p_full[H_MAX_PACKED];       // packed weights have landed
     uint64_t p_empty[H_MAX_PACKED];      // and been read
-    uint64_t d_full[2];                  // a tile's MMAs completed
-    uint64_t d_empty[2];                 // its sums have been read
+    uint64_t d_full;                     // a tile's MMAs completed
+    uint64_t d_empty;                    // its sums have been read
     uint64_t done;                       // every MMA completed
     uint32_t tmem_base;
     int abort;
@@ -77,7 +81,7 @@ struct TileArgs {
     int n_tiles, tiles;                  // tiles along the tokens; all (of a pair, or a cluster)
     int split;                           // CTAs that share a tile's K
     int stages, packed;                  // depths of the rings
-    int acc_cols, accs;                  // TMEM columns of an accumulator; accumulators: 1 or 2
+    int acc_cols;                        // TMEM columns of an accumulator
 };
 
 __host__ __device__ inline int tile_stage_bytes(int held) { return held * H_K * 2; }
@@ -87,10 +91,11 @@ __host__ __device__ inline int packed_bytes(const mpq_g4_matrix &L) { return 8 *
 struct Place {
     int at = 0;
     uint32_t phase = 0;
-    __device__ __forceinline__ void pass(int slots)
+    __device__ __forceinline__ void pass(int slots, int count = 1)   // count <= slots
     {
-        if (++at == slots) {
-            at = 0;
+        at += count;
+        if (at >= slots) {
+            at -= slots;
             phase ^= 1u;
         }
     }
@@ -201,11 +206,12 @@ __device__ __forceinline__ uint32_t pack16(int type, float a, float b)
     return type == MPQ_F16 ? pack2(a, b, __half()) : pack2(a, b, __nv_bfloat16());
 }
 
-template <typename T, bool PAIR>
-__global__ void __launch_bounds__(tile_threads(PAIR), 1)
+template <typename T, int SHAPE>
+__global__ void __launch_bounds__(tile_threads(SHAPE), 1)
 g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ CUtensorMap tmX,
                 const __grid_constant__ CUtensorMap tmW)
 {
+    constexpr bool PAIR = SHAPE == PAIRS;
     extern __shared__ unsigned char raw[];
     unsigned char *const base = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
     TileCtrl &ctl = *reinterpret_cast<TileCtrl *>(base);
@@ -254,11 +260,9 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
             mbar_init(&ctl.p_full[i], 1);
             mbar_init(&ctl.p_empty[i], 4);
         }
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(&ctl.d_full[i], 1);
-            mbar_init(&ctl.d_empty[i], (PAIR ? 2 : 1) * H_OUTS);
-        }
-        mbar_init(&ctl.done, 1);
+        mbar_init(&ctl.d_full, SHAPE == NARROW ? 2 : 1);
+        mbar_init(&ctl.d_empty, (PAIR ? 2 : 1) * H_OUTS);
+        mbar_init(&ctl.done, SHAPE == NARROW ? 2 : 1);
         ctl.abort = 0;
         fence_barrier_init();
         if (!MPQ_CHECK_SMEM_END(packed - raw + (size_t)a.packed * pb)) ctl.abort = 1;
@@ -275,7 +279,7 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
     __syncthreads();
     if (PAIR) cluster_sync();            // the barriers that the other CTA arrives on are ready
     tc_fence_after();
-    const uint32_t tmem = ctl.tmem_base, operands = tmem + (uint32_t)(a.accs * a.acc_cols);
+    const uint32_t tmem = ctl.tmem_base, operands = tmem + (uint32_t)((SHAPE == NARROW ? 2 : 1) * a.acc_cols);
     griddep_wait();
 
     if (warp == 0) {
@@ -336,10 +340,10 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
         for (int i = max(0, n - a.packed); lane == 0 && i < n; ++i)
             drain_wait(&ctl.p_full[i % a.packed], (uint32_t)(i / a.packed) & 1u, wc, MPQ_TIMEOUT_G4);
         __syncwarp();
-    } else if (warp == 3) {
+    } else if (PAIR && warp == 3) {
         // -------------------------------------------------------------------- x has landed
         Place s;
-        bool stop = !PAIR;
+        bool stop = false;
         for (int tile = first; tile < a.tiles && !stop; tile += step)
             for (int k = k0; k < k1; ++k, s.pass(a.stages)) {
                 stop = warp_failed(&ctl.x_full[s.at], s.phase);
@@ -347,22 +351,24 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
                 if (elected()) arrive(&ctl.ready[s.at]);
                 __syncwarp();
             }
-    } else if (warp == 1) {
+    } else if (warp == 1 || (SHAPE == NARROW && warp == 3)) {
         // -------------------------------------------------------------------- MMAs
         // (the warp waits as one; a thread that waits alone keeps its warp's others at the next meeting point, which
         // costs it a hundred cycles a wait)
         if (!PAIR || rank == 0) {
-            int t = 0;                   // tiles so far
+            const int own = warp >> 1;   // NARROW: of two, which takes every other stage
+            int t = 0, n = 0;            // tiles, stages so far
             Place s;
             bool stop = false;
             for (int tile = first; tile < a.tiles && !stop; tile += step, ++t) {
                 const int real = (int)min((long long)a.n_tile, a.rows.tokens - token0(tile));
                 const int m = PAIR ? 2 * H_M : H_M, cols = PAIR ? 256 : (real + 15) / 16 * 16;
-                const int b = t & (a.accs - 1), use = a.accs == 2 ? t >> 1 : t;
                 const uint32_t id = G4Pairs<T>::kBf16 ? idesc_bf16(m, cols) : idesc_f16(m, cols);
-                const uint32_t d = tmem + (uint32_t)(b * a.acc_cols);
-                if (use > 0 && warp_failed(&ctl.d_empty[b], (uint32_t)(use - 1) & 1u, true)) break;
-                for (int k = k0; k < k1; ++k, s.pass(a.stages)) {
+                const uint32_t d = tmem + (uint32_t)(SHAPE == NARROW ? own * a.acc_cols : 0);
+                uint32_t more = 0;
+                if (t > 0 && warp_failed(&ctl.d_empty, (uint32_t)(t - 1) & 1u, true)) break;
+                for (int k = k0; k < k1; ++k, ++n, s.pass(a.stages)) {
+                    if (SHAPE == NARROW && (n & 1) != own) continue;
                     if (warp_failed(&ctl.ready[s.at], s.phase, true)) {
                         stop = true;
                         break;
@@ -376,13 +382,15 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
                             const uint64_t bh = bd + (uint64_t)(h * a.held * 8);     // in 16 B units
 #pragma unroll
                             for (int j = 0; j < 4; ++j)
-                                mma_f16_ts<PAIR>(d, at + 32 * h + 8 * j, bh + 2 * j, id, k > k0 || h + j > 0 ? 1u : 0u);
+                                mma_f16_ts<PAIR>(d, at + 32 * h + 8 * j, bh + 2 * j, id, more | (uint32_t)(h + j > 0));
                         }
                         commit(&ctl.empty[s.at]);
-                        if (k == k1 - 1) commit(&ctl.d_full[b]);
                     }
+                    more = 1;
                     __syncwarp();
                 }
+                if (!stop && elected()) commit(&ctl.d_full);
+                __syncwarp();
             }
             // every MMA issued above completes before tensor memory is released
             if (elected()) {
@@ -391,7 +399,9 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
             }
         }
         __syncwarp();
-    } else if (warp < first_out(PAIR)) {
+    } else if (warp < H_MAKE0) {
+        // -------------------------------------------------------------------- (WIDE: no work for warp 3)
+    } else if (warp < first_out(SHAPE)) {
         // -------------------------------------------------------------------- operands from packed weights
         // A thread has a channel: its 64 bytes of a packed tile, by quarters in an order in which eight lanes
         // (what shared memory serves at once) meet no bank twice, put right in registers.
@@ -399,104 +409,92 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
         const int groups = 128 / a.L.group;
         const uint32_t to = operands + ((uint32_t)(q * 32) << 16);
         const unsigned char *const mine_at = packed + (row >> 4) * a.L.tile_bytes;
-        int turn = 0;                    // of the groups
-        bool again = false;              // every stage has been filled once
+        // of all the stages of all the CTA's tiles, every makers(SHAPE)-th
+        const long long stages = first < a.tiles ? (long long)((a.tiles - first - 1) / step + 1) * (k1 - k0) : 0;
         Place p, s;
-        bool stop = false;
-        for (int tile = first; tile < a.tiles && !stop; tile += step) {
-            for (int k = k0; k < k1; ++k, p.pass(a.packed)) {
-                const bool mine = turn == own;
-                turn = turn == makers(PAIR) - 1 ? 0 : turn + 1;
-                if (!mine) {
-                    again |= s.at + 1 == a.stages;
-                    s.pass(a.stages);
-                    continue;
-                }
-                if (warp_failed(&ctl.p_full[p.at], p.phase)) {
-                    stop = true;
-                    break;
-                }
-                const unsigned char *const t = mine_at + p.at * pb;
-                uint4 w[4];
+        p.pass(a.packed, own);
+        s.pass(a.stages, own);
+        for (long long n = own; n < stages; n += makers(SHAPE), p.pass(a.packed, makers(SHAPE)), s.pass(a.stages, makers(SHAPE))) {
+            if (warp_failed(&ctl.p_full[p.at], p.phase)) break;
+            const unsigned char *const t = mine_at + p.at * pb;
+            uint4 w[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    w[i] = *reinterpret_cast<const uint4 *>(t + (row & 15) * 64 + (i ^ x) * 16);
-                uint2 sc;                // the row's scales of the tile's quarters, two a word
-                uint32_t z = 0x08080808u;            // and zero points
-                const unsigned char *const ss = t + G4_CODES + (row & 15) * 2 * groups;
-                const unsigned char *const zs = t + G4_CODES + 32 * groups + (row & 15) * groups;
-                if (groups == 1) {
-                    sc.x = sc.y = *reinterpret_cast<const uint16_t *>(ss) * 0x10001u;
-                    if (a.L.zeros) z = __byte_perm(*zs, 0, 0x0000);
-                } else if (groups == 2) {
-                    const uint32_t two = *reinterpret_cast<const uint32_t *>(ss);
-                    sc = make_uint2(__byte_perm(two, 0, 0x1010), __byte_perm(two, 0, 0x3232));
-                    if (a.L.zeros) z = __byte_perm(*reinterpret_cast<const uint16_t *>(zs), 0, 0x1100);
-                } else {
-                    sc = *reinterpret_cast<const uint2 *>(ss);
-                    if (a.L.zeros) z = *reinterpret_cast<const uint32_t *>(zs);
-                }
-                __syncwarp();
-                if (elected()) mbar_arrive(&ctl.p_empty[p.at]);
-                swap_if(x & 1, w[0], w[1]);
-                swap_if(x & 1, w[2], w[3]);
-                swap_if(x & 2, w[0], w[2]);
-                swap_if(x & 2, w[1], w[3]);
-                const uint32_t scales[2] = {sc.x, sc.y};
-                const bool far = g4_far<T>(scales);
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {            // (behind the row's end: zeros, whose MMAs are left out)
-                    uint32_t v[32];
-                    auto convert = [&](auto f) {
-#pragma unroll
-                        for (int m = 0; m < 2; ++m) {
-                            const uint32_t two = scales[h];
-                            const G4Scale g = g4_scale<T>(m ? two >> 16 : two & 0xffffu, z >> (8 * (2 * h + m)) & 255u);
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const uint32_t word = h ? (m ? w[i].w : w[i].z) : (m ? w[i].y : w[i].x);
-                                uint32_t p4[4];
-                                g4_values<T, decltype(f)::value>(word, g, p4);
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) v[16 * m + 4 * i + e] = p4[e];
-                            }
-                        }
-                    };
-                    if (far)
-                        convert(std::true_type());
-                    else
-                        convert(std::false_type());
-                    if (h == 0) {
-                        if (again && warp_failed(&ctl.empty[s.at], s.phase ^ 1u)) {
-                            stop = true;
-                            break;
-                        }
-                        tc_fence_after();
-                    }
-                    tmem_st_32(to + (uint32_t)(s.at * H_A_COLS + 32 * h), v);
-                }
-                if (stop) break;
-                tmem_wait_st();
-                tc_fence_before();
-                __syncwarp();
-                if (elected()) arrive(&ctl.ready[s.at]);
-                again |= s.at + 1 == a.stages;
-                s.pass(a.stages);
+            for (int i = 0; i < 4; ++i)
+                w[i] = *reinterpret_cast<const uint4 *>(t + (row & 15) * 64 + (i ^ x) * 16);
+            uint2 sc;                // the row's scales of the tile's quarters, two a word
+            uint32_t z = 0x08080808u;            // and zero points
+            const unsigned char *const ss = t + G4_CODES + (row & 15) * 2 * groups;
+            const unsigned char *const zs = t + G4_CODES + 32 * groups + (row & 15) * groups;
+            if (groups == 1) {
+                sc.x = sc.y = *reinterpret_cast<const uint16_t *>(ss) * 0x10001u;
+                if (a.L.zeros) z = __byte_perm(*zs, 0, 0x0000);
+            } else if (groups == 2) {
+                const uint32_t two = *reinterpret_cast<const uint32_t *>(ss);
+                sc = make_uint2(__byte_perm(two, 0, 0x1010), __byte_perm(two, 0, 0x3232));
+                if (a.L.zeros) z = __byte_perm(*reinterpret_cast<const uint16_t *>(zs), 0, 0x1100);
+            } else {
+                sc = *reinterpret_cast<const uint2 *>(ss);
+                if (a.L.zeros) z = *reinterpret_cast<const uint32_t *>(zs);
             }
+            __syncwarp();
+            if (elected()) mbar_arrive(&ctl.p_empty[p.at]);
+            swap_if(x & 1, w[0], w[1]);
+            swap_if(x & 1, w[2], w[3]);
+            swap_if(x & 2, w[0], w[2]);
+            swap_if(x & 2, w[1], w[3]);
+            bool stop = false;
+            const uint32_t scales[2] = {sc.x, sc.y};
+            const bool far = g4_far<T>(scales);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {            // (behind the row's end: zeros, whose MMAs are left out)
+                uint32_t v[32];
+                auto convert = [&](auto f) {
+#pragma unroll
+                    for (int m = 0; m < 2; ++m) {
+                        const uint32_t two = scales[h];
+                        const G4Scale g = g4_scale<T>(m ? two >> 16 : two & 0xffffu, z >> (8 * (2 * h + m)) & 255u);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const uint32_t word = h ? (m ? w[i].w : w[i].z) : (m ? w[i].y : w[i].x);
+                            uint32_t p4[4];
+                            g4_values<T, decltype(f)::value>(word, g, p4);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) v[16 * m + 4 * i + e] = p4[e];
+                        }
+                    }
+                };
+                if (far)
+                    convert(std::true_type());
+                else
+                    convert(std::false_type());
+                if (h == 0) {
+                    stop = n >= a.stages && warp_failed(&ctl.empty[s.at], s.phase ^ 1u);
+                    if (stop) break;
+                    tc_fence_after();
+                }
+                tmem_st_32(to + (uint32_t)(s.at * H_A_COLS + 32 * h), v);
+            }
+            if (stop) break;
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (elected()) arrive(&ctl.ready[s.at]);
         }
     } else {
         // -------------------------------------------------------------------- outputs
-        const int q = warp & 3, row = q * 32 + lane, half = (warp - first_out(PAIR)) >> 2;
+        const int q = warp & 3, row = q * 32 + lane, half = (warp - first_out(SHAPE)) >> 2;
         int t = 0;
         for (int tile = first; tile < a.tiles; tile += step, ++t) {
             const long long n0 = token0(tile);
             const int real = (int)min((long long)a.n_tile, a.rows.tokens - n0);
-            const int b = t & (a.accs - 1), use = a.accs == 2 ? t >> 1 : t;
+            // NARROW: both accumulators have sums, but for a tile of one stage
+            const int whose = k1 - k0 == 1 ? t & 1 : 0;
+            const bool both = SHAPE == NARROW && k1 - k0 > 1;
             const int c = row_tile(tile) * H_M + row;
             const float bias = a.split == 1 && a.rows.bias && c < a.rows.channels ? a.rows.bias[c] : 0.0f;
-            if (warp_failed(&ctl.d_full[b], (uint32_t)use & 1u)) break;
+            if (warp_failed(&ctl.d_full, (uint32_t)t & 1u)) break;
             tc_fence_after();
-            const uint32_t from = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(b * a.acc_cols);
+            const uint32_t from = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(SHAPE == NARROW ? whose * a.acc_cols : 0);
             const Column at{c, lane, n0, real};
             uint16_t *const y16 = static_cast<uint16_t *>(Y);
             if constexpr (PAIR) {
@@ -514,7 +512,7 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
                     }
                     tc_fence_before();
                     __syncwarp();
-                    if (elected()) arrive(&ctl.d_empty[b]);
+                    if (elected()) arrive(&ctl.d_empty);
 #pragma unroll
                     for (int j = 0; j < 64; ++j)
                         if (j0 + 2 * j < real) store_two(a.rows, y16, two[j], at, j0 + 2 * j);
@@ -525,6 +523,12 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
                 float v[16];
                 __syncwarp();
                 tmem_ld_32x32b_x16(from + (uint32_t)j0, v);
+                if (both) {
+                    float o[16];
+                    tmem_ld_32x32b_x16(from + (uint32_t)(a.acc_cols + j0), o);
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) v[j] += o[j];
+                }
                 if (!PAIR && a.split > 1) {          // [token][128 channels]; the MMAs have read the ring
                     float *const part = reinterpret_cast<float *>(ring) + row;
 #pragma unroll
@@ -544,7 +548,7 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
             }
             tc_fence_before();
             __syncwarp();
-            if (elected()) arrive(&ctl.d_empty[b]);
+            if (elected()) arrive(&ctl.d_empty);
         }
     }
 
@@ -593,40 +597,41 @@ g4_rows_kernel(const uint16_t *X, long long ldx, int T, int d, uint16_t *to, int
     }
 }
 
-template <typename T, bool PAIR>
+template <typename T, int SHAPE>
 mpq_status launch_tiles(const TileArgs &a, const CUtensorMap &tmX, const CUtensorMap &tmW, void *Y, int ctas, cudaStream_t stream)
 {
     const size_t smem = std::max(H_MIN_SMEM, 1024 + H_CTRL_BYTES + (size_t)a.stages * tile_stage_bytes(a.held) +
                                                  (size_t)a.packed * packed_bytes(a.L));
     static std::atomic<int> limit[kMaxDevices];
-    cudaError_t e = allow_smem(reinterpret_cast<const void *>(g4_tiles_kernel<T, PAIR>), limit, smem);
+    cudaError_t e = allow_smem(reinterpret_cast<const void *>(g4_tiles_kernel<T, SHAPE>), limit, smem);
     if (e != cudaSuccess) return cuda_status(e, "cudaFuncSetAttribute");
     WaitCtl wc;
     const mpq_status ws = wait_ctl(&wc);
     if (ws != MPQ_OK) return ws;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)ctas);
-    cfg.blockDim = dim3(tile_threads(PAIR));
+    cfg.blockDim = dim3(tile_threads(SHAPE));
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     attr[0] = after_previous_kernel();
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = PAIR ? 2u : (unsigned)a.split;
+    attr[1].val.clusterDim.x = SHAPE == PAIRS ? 2u : (unsigned)a.split;
     attr[1].val.clusterDim.y = 1;
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    e = cudaLaunchKernelEx(&cfg, g4_tiles_kernel<T, PAIR>, a, Y, wc, tmX, tmW);
+    e = cudaLaunchKernelEx(&cfg, g4_tiles_kernel<T, SHAPE>, a, Y, wc, tmX, tmW);
     return cuda_status(e != cudaSuccess ? e : cudaGetLastError(), "g4 linear launch");
 }
 
 template <typename T>
-mpq_status launch_form(const TileArgs &a, bool pair, const CUtensorMap &tmX, const CUtensorMap &tmW, void *Y, int ctas,
+mpq_status launch_form(const TileArgs &a, int shape, const CUtensorMap &tmX, const CUtensorMap &tmW, void *Y, int ctas,
                        cudaStream_t stream)
 {
-    return pair ? launch_tiles<T, true>(a, tmX, tmW, Y, ctas, stream)
-                : launch_tiles<T, false>(a, tmX, tmW, Y, ctas, stream);
+    return shape == PAIRS  ? launch_tiles<T, PAIRS>(a, tmX, tmW, Y, ctas, stream)
+           : shape == WIDE ? launch_tiles<T, WIDE>(a, tmX, tmW, Y, ctas, stream)
+                           : launch_tiles<T, NARROW>(a, tmX, tmW, Y, ctas, stream);
 }
 
 struct Form {
@@ -706,17 +711,17 @@ mpq_status launch_g4_tiles(const void *X, int x_type, long long ldx, int T, cons
                      : f.split > 1 ? a.tiles * f.split
                                    : std::min(a.tiles, sms);
 
-    // an accumulator, or two that take turns where a CTA has several tiles of up to 128 tokens; the other columns are
-    // stages of operands
-    a.accs = a.acc_cols <= 128 && f.split == 1 && a.tiles > ctas ? 2 : 1;
-    // three tiles' packed weights or more, as many stages as fit beside them, then more packed tiles
+    const int shape = f.pair ? PAIRS : f.n > 128 ? WIDE : NARROW;
+    // as many packed tiles as groups or more, as many stages as fit beside them, then more packed tiles
     const int room = max_smem_optin() - 1024 - H_CTRL_BYTES, pb = packed_bytes(*L), sb = tile_stage_bytes(a.held);
-    a.stages = std::min({H_MAX_STAGES, (room - 3 * pb) / sb, (512 - a.accs * a.acc_cols) / H_A_COLS});
+    const int groups = makers(shape), accs = shape == NARROW ? 2 : 1;
+    a.stages = std::min({H_MAX_STAGES, (room - groups * pb) / sb, (512 - accs * a.acc_cols) / H_A_COLS});
     // A barrier's parity tells two phases apart, not more.  A group of makers that has made a stage knows that the MMAs
     // took the stage `stages` before it, and its next one is `groups` on: it meets a phase that is at most one behind if
-    // there are as many stages as groups.  Packed tiles may land out of order, so that a group knows only of its
-    // own: a slot is always the same group's.
-    const int groups = makers(f.pair);
+    // there are as many stages as groups (NARROW: an even number of both, so that what one warp's MMAs took
+    // says that it took the earlier ones; a stage's place is always the same warp's).  Packed tiles may land out of
+    // order, so that a group knows only of its own: a slot is always the same group's.
+    if (shape == NARROW) a.stages &= ~1;
     a.packed = std::min(H_MAX_PACKED, (room - a.stages * sb) / pb) / groups * groups;
     if (a.stages < groups || a.packed < groups) {
         set_error("g4 linear: shared memory has no room for %d stages", groups);
@@ -758,9 +763,9 @@ mpq_status launch_g4_tiles(const void *X, int x_type, long long ldx, int T, cons
         set_error("g4 linear: tensor map encoding failed");
         st = MPQ_ERR_CUDA;
     } else if (x_type == MPQ_F16) {
-        st = launch_form<__half>(a, f.pair, tmX, tmW, Y, ctas, stream);
+        st = launch_form<__half>(a, shape, tmX, tmW, Y, ctas, stream);
     } else {
-        st = launch_form<__nv_bfloat16>(a, f.pair, tmX, tmW, Y, ctas, stream);
+        st = launch_form<__nv_bfloat16>(a, shape, tmX, tmW, Y, ctas, stream);
     }
     if (scratch) {
         const cudaError_t e = cudaFreeAsync(scratch, stream);

@@ -65,15 +65,18 @@ __device__ __forceinline__ void join(const TokenRows &a, T *Y, const JoinAt &at)
     for (int i0 = (int)threadIdx.x + at.rank * (int)blockDim.x; i0 < quads; i0 += U * step) {
         float4 p[U][R];
 #pragma unroll
-        for (int u = 0; u < U; ++u)
+        for (int u = 0; u < U; ++u) {
+            if (i0 + u * step >= quads) break;
 #pragma unroll
             for (int r = 0; r < R; ++r)
-                p[u][r] = sm100::ld_dsmem_f32x4(at.part + min(i0 + u * step, quads - 1) * 4, (uint32_t)r);
+                p[u][r] = sm100::ld_dsmem_f32x4(at.part + (i0 + u * step) * 4, (uint32_t)r);
+        }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int i = i0 + u * step;
+            if (i >= quads) break;
             const int t = i / (TOKEN_M / 4), c = at.tile * TOKEN_M + (i % (TOKEN_M / 4)) * 4;
-            if (i >= quads || c >= a.channels) continue;
+            if (c >= a.channels) continue;
             float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int r = 0; r < R; ++r)
