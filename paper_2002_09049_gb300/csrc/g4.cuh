@@ -81,14 +81,14 @@ __device__ __forceinline__ void g4_values(uint32_t w, const G4Scale &g, uint32_t
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             p[j] = pack2((float)((int)(w >> (4 * j) & 15u) - z) * s, (float)((int)(w >> (4 * j + 16) & 15u) - z) * s, T());
-        return;
-    }
+    } else {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        uint32_t v;                          // (w >> 4 j) & 0x000f000f | the power: one operation of three inputs
-        asm("lop3.b32 %0, %1, %2, %3, 0xea;"
-            : "=r"(v) : "r"(w >> (4 * j)), "n"(0x000f000f), "n"(G4Pairs<T>::kPower));
-        p[j] = G4Pairs<T>::value(v, g.from, g.s);
+        for (int j = 0; j < 4; ++j) {
+            uint32_t v;                          // (w >> 4 j) & 0x000f000f | the power: one operation of three inputs
+            asm("lop3.b32 %0, %1, %2, %3, 0xea;"
+                : "=r"(v) : "r"(w >> (4 * j)), "n"(0x000f000f), "n"(G4Pairs<T>::kPower));
+            p[j] = G4Pairs<T>::value(v, g.from, g.s);
+        }
     }
 }
 

@@ -5,21 +5,22 @@
 // ahead), and groups of four warps turn them by turns into operands in tensor memory, a channel to a
 // lane; x comes by TMA into 128-byte-swizzled shared memory.  (Operands in shared memory too, 141 us
 // for 2,048 x 11,008 x 4,096: 64 KB in and out per 64 elements of K of a pair's CTA are 512 cycles at 128 bytes each,
-// as many as the MMAs take.)  Eight warps write the outputs.  Roles run over their CTA's tiles without a
-// pause.  Up to 128 tokens two warps issue the MMAs of every other stage, into accumulators of their own whose sums are
-// added on the way out (one warp's waits and issue took 800 cycles a stage, 340 of them the MMAs').
+// as many as the MMAs take.)  Eight warps write the outputs.  Roles run over their CTA's tiles without a pause.
 //
-// PAIR: CTA pairs (cta_group::2) take 256 channels x 256 tokens, each CTA its own channels and half of the
-// tokens' operand.  Else K may be split over the CTAs of a cluster, whose sums are joined in shared memory in the
-// order of the ranks (equal inputs give equal bits).
+// PAIRS: CTA pairs (cta_group::2) take 256 channels x 256 tokens, each CTA its own channels and half of the tokens'
+// operand.  WIDE, NARROW: a CTA's 128 channels x up to 256 or 128 tokens; K may be split over the CTAs of a cluster,
+// whose sums are joined in shared memory in the order of the ranks (equal inputs give equal bits).  NARROW: two
+// warps issue the MMAs of every other stage, into accumulators of their own whose sums are added on the way out (one
+// warp's waits and issue took 800 cycles a stage, 340 of them the MMAs').
 //
 // Measured: 2,048 x 11,008 x 4,096 (T x C x d) 105 us, 1.76 PFLOP/s: a stage takes 1,024 cycles, its MMAs' own; 1,800 a
-// tile between the last MMA and the next one's first; 344 tiles on 76 pairs are five rounds.  75 x 4,096 x 11,008 15.6
-// us (22 stages of 0.4 us on 128 CTAs, then 3 us for the join): the MMAs' warp takes 450 cycles a stage beside 340 of
-// MMAs, a group of makers 2,500 a stage.
+// tile between the last MMA and the next one's first; 344 tiles on 76 pairs are five rounds.  75 x 4,096 x 11,008 14.8
+// us: 2 to the first MMA, 22 stages of 0.35 on 128 CTAs (1,700 warp instructions a stage to make its operands), 3 for
+// the join of four ranks; without any of the work, roles waiting on each other alone, 10.3.
 //
-// Warps: 0 copies x, 1 issues MMAs (the even CTA's, of a pair), 2 copies weights, 3 tells the MMAs' warp that x has
-// landed, 4 .. make operands, the last write outputs (these two by lane quarters, warp % 4).  Every wait is bounded.
+// Warps: 0 copies x, 1 issues MMAs (the even CTA's, of a pair; NARROW: 3 too), 2 copies weights, PAIRS: 3 tells the MMAs'
+// warp that x has landed, 4 .. make operands, the last eight write outputs (these two by lane quarters, warp % 4).
+// Every wait is bounded.
 #include <cuda.h>
 #include <math.h>
 #include <string.h>
@@ -645,12 +646,12 @@ struct Form {
 int resident(int split, int sms) { return split == 1 ? sms : split == 2 ? sms / 2 : split == 4 ? sms * 36 / 152 : sms * 14 / 152; }
 
 // The form with the least modelled time (us): a start, and for each round of resident CTAs its stages, by their tokens
-// (up to 128 the operands' making bounds them, 0.37 to 0.41 us; from 192 on the MMAs), the tile's way out, and the
-// joining of a split.  Fitted to 960 timings of 102 sizes (8 <= T <= 2,048, 448 <= C <= 14,000, 500 <= d <= 11,008): the
-// choice costs 2% on average against the best form; 14,000 x 500 with 2,048 tokens 8%, and 1,024 x 1,024 up to 30%,
-// where a few tokens' kernel is taken.  Some of them, us, with 32 / 64 / 128 / 256 tokens a tile, pairs:
-// 40 x 4,096 x 4,096 (T x C x d; split by 4) 9.3, -, -, -, -; 256 x 11,008 x 4,096 45, 31, 33, 25.5, 27.7;
-// 2,048 x 11,008 x 4,096 -, 254, 145, 121, 107; 512 x 4,096 x 11,008 -, -, 41, 33 (split by 2), 55.
+// (up to 128 the operands' making bounds them, 0.34 to 0.36 us; from 192 on the MMAs), the tile's way out, and the
+// joining of a split.  Fitted to 919 timings of 91 sizes (16 <= T <= 2,048, 448 <= C <= 14,000, 500 <= d <= 11,008): the
+// choice costs 1% on average against the best form, 15% at worst (16 x 1,024 x 1,024, where the few tokens' kernel is
+// taken).  Some of them, us, with 32 / 64 / 128 / 256 tokens a tile, pairs: 32 x 4,096 x 4,096 (T x C x d; split by 4)
+// 9.4, -, -, -, -; 256 x 11,008 x 4,096 -, -, 32.5, 25.4, 27.4; 2,048 x 11,008 x 4,096 -, 238, 148, 121, 105;
+// 512 x 4,096 x 4,096 -, -, 18.8, 18.5 (split by 2), 26.7.
 Form choose_form(int T, int C, int k_tiles, int sms, double &least)
 {
     auto rounds = [](long long n, long long at_once) { return (double)((n + at_once - 1) / at_once); };
@@ -663,8 +664,8 @@ Form choose_form(int T, int C, int k_tiles, int sms, double &least)
         for (int split = 1; split <= TOKEN_MAX_SPLIT && split * 2 <= std::max(2, k_tiles); split *= 2) {
             const int stages = (k_tiles + split - 1) / split;
             const double r = rounds(tiles, std::max(1, resident(split, sms)));
-            const double t = 2.3 + r * (stages * std::max(0.374 + 0.0003 * n, 0.002 * n) + 0.54 +
-                                        (n > 128 ? 0.0226 : 0.0187) * n + (split > 1 ? 2.7 - 0.008 * n : 0.0));
+            const double t = 1.9 + r * (stages * std::max(0.3435 + 0.0001 * n, 0.0021 * n) + 0.46 +
+                                        (n > 128 ? 0.0246 : 0.0283) * n + (split > 1 ? 2.9 - 0.0091 * n : 0.0));
             if (t < least) {
                 best = {n, false, split};
                 least = t;
