@@ -8,9 +8,8 @@
 // and x's registers are 16 consecutive bytes of its row.  Warps of a CTA take a row tile's tiles in turn and
 // their sums are joined in shared memory in the warps' order.
 //
-// Measured: 1 x 4,096 x 4,096 (T x C x d) 4.1 us (a launch, one round of loads, the join; the weights' bytes would take
-// 1.3), 5 x 11,008 x 4,096 bf16 9.1, fp16 with zero points 10.8 (issue: 15 instructions for eight weights; 688 CTAs, two
-// an SM -- three or four an SM were slower for one token's 256, 4.9 to 6.7 us).
+// Measured: 1 x 4,096 x 4,096 (T x C x d) 4.0 us (a launch, one round of loads, the join; the weights' bytes would take
+// 1.3), 5 x 11,008 x 4,096 bf16 8.2, fp16 with zero points 9.6 (issue: 15 instructions for eight weights).
 #include <math.h>
 
 #include <algorithm>
@@ -98,9 +97,12 @@ struct Groups {
     }
 };
 
-// NT: tiles of eight tokens; GROUP: elements of a group; VEC: x's rows are 16-byte aligned, d a multiple of 8.
-template <typename T, int NT, int GROUP, bool VEC>
-__global__ void __launch_bounds__(FEW_WARPS * 32)
+// NT: tiles of eight tokens; GROUP: elements of a group; VEC: x's rows are 16-byte aligned, d a multiple of 8.  CROWD: more
+// CTAs than two an SM, so three are to fit, with fewer loads ahead (5 x 11,008 x 4,096 9.1 -> 8.1 us; one token's 256 CTAs
+// of 4,096 x 4,096 took 4.9 that way instead of 4.0).  Two fit otherwise: left to 255 registers, 64 x 4,096 x 4,096 took
+// 19.4 us instead of 14.2.
+template <typename T, int NT, int GROUP, bool VEC, bool CROWD>
+__global__ void __launch_bounds__(FEW_WARPS * 32, CROWD ? 3 : 2)
 g4_few_kernel(const G4Args a, const T *X, void *Y)
 {
     constexpr int N = 128 / GROUP;           // groups of a tile's row
@@ -116,7 +118,7 @@ g4_few_kernel(const G4Args a, const T *X, void *Y)
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[n][e] = 0.0f;
     // U tiles' codes, scales and zero points are on their way before the first is used
-    constexpr int U = NT == 1 ? 4 : 2;
+    constexpr int U = NT == 1 && !CROWD ? 4 : 2;
     const unsigned char *const codes = strip + g * 64 + i * 16;
     for (int k0 = warp; k0 < a.L.k_tiles; k0 += U * FEW_WARPS) {
         uint4 wa[U], wb[U];
@@ -179,34 +181,43 @@ g4_few_kernel(const G4Args a, const T *X, void *Y)
     }
 }
 
-template <typename T, int NT, bool VEC>
+template <typename T, int NT, bool VEC, bool CROWD>
 mpq_status launch_few(const G4Args &a, const T *X, void *Y, cudaStream_t stream)
 {
     const dim3 grid((unsigned)a.L.row_tiles, (unsigned)((a.T + NT * 8 - 1) / (NT * 8)));
-    auto *const kernel = a.L.group == 32   ? g4_few_kernel<T, NT, 32, VEC>
-                         : a.L.group == 64 ? g4_few_kernel<T, NT, 64, VEC>
-                                           : g4_few_kernel<T, NT, 128, VEC>;
+    auto *const kernel = a.L.group == 32   ? g4_few_kernel<T, NT, 32, VEC, CROWD>
+                         : a.L.group == 64 ? g4_few_kernel<T, NT, 64, VEC, CROWD>
+                                           : g4_few_kernel<T, NT, 128, VEC, CROWD>;
     return launch_waiting(kernel, grid, dim3(FEW_WARPS * 32), 0, stream, "g4 linear launch", a, X, Y);
+}
+
+template <typename T, int NT>
+mpq_status launch_tokens(const G4Args &a, const T *X, bool vec, void *Y, cudaStream_t stream)
+{
+    const bool crowd = NT < 4 && a.L.row_tiles > 2 * sm_count();
+    if (crowd) return vec ? launch_few<T, NT, true, NT < 4>(a, X, Y, stream) : launch_few<T, NT, false, NT < 4>(a, X, Y, stream);
+    return vec ? launch_few<T, NT, true, false>(a, X, Y, stream) : launch_few<T, NT, false, false>(a, X, Y, stream);
 }
 
 template <typename T>
 mpq_status launch_typed(const G4Args &a, const T *X, int x_type, void *Y, cudaStream_t stream)
 {
     const bool vec = rows_aligned(X, x_type, a.T > 1 ? a.ldx : 0) && a.L.d % 8 == 0;
-    if (a.T <= 8) return vec ? launch_few<T, 1, true>(a, X, Y, stream) : launch_few<T, 1, false>(a, X, Y, stream);
-    if (a.T <= 16) return vec ? launch_few<T, 2, true>(a, X, Y, stream) : launch_few<T, 2, false>(a, X, Y, stream);
-    return vec ? launch_few<T, 4, true>(a, X, Y, stream) : launch_few<T, 4, false>(a, X, Y, stream);
+    if (a.T <= 8) return launch_tokens<T, 1>(a, X, vec, Y, stream);
+    if (a.T <= 16) return launch_tokens<T, 2>(a, X, vec, Y, stream);
+    return launch_tokens<T, 4>(a, X, vec, Y, stream);
 }
 
 // Whether this kernel's modelled time (us) is less than the tiles': a start, and what is longer of a warp's tiles one
 // after another and of all tiles and CTAs, by the tokens of a CTA (8, 16 or 32).  Some timings, us, this kernel's and
-// the tiles': 8 x 4,096 x 4,096 (T x C x d) 4.9, 8.7; 32 x 4,096 x 4,096 8.2, 9.4; 48 x 4,096 x 4,096 13.4, 9.9;
-// 16 x 11,008 x 4,096 13.4, 16.5; 128 x 1,024 x 1,024 4.1, 7.2; 24 x 448 x 8,064 9.1, 9.0; 16 x 14,000 x 500 9.5, 7.7.
+// the tiles': 8 x 4,096 x 4,096 (T x C x d) 4.3, 8.2; 32 x 4,096 x 4,096 7.8, 9.0; 64 x 4,096 x 4,096 14.2, 9.3;
+// 16 x 11,008 x 4,096 11.8, 14.9; 24 x 11,008 x 4,096 17.6, 14.9; 64 x 2,048 x 2,048 5.1, 7.4; 16 x 32,768 x 4,096
+// 30.8, 27.5; 24 x 512 x 8,192 7.7, 8.4; 96 x 512 x 8,192 11.2, 9.6 (where the model is wrong).
 bool few_tokens(int T, const mpq_g4_matrix *L)
 {
     if (T > 128) return false;
     const int c = T <= 8 ? 0 : T <= 16 ? 1 : 2;
-    constexpr double one[3] = {0.4, 0.6, 0.9}, tile[3] = {0.25e-3, 0.4e-3, 0.45e-3}, cta[3] = {3.4e-3, 6.2e-3, 12e-3};
+    constexpr double one[3] = {0.4, 0.6, 0.75}, tile[3] = {0.27e-3, 0.36e-3, 0.6e-3}, cta[3] = {0.6e-3, 1.5e-3, 2.3e-3};
     const double ctas = (double)L->row_tiles * ((T + 31) / 32);
     const double t = 2.0 + std::max((L->k_tiles + FEW_WARPS - 1) / FEW_WARPS * one[c], ctas * (L->k_tiles * tile[c] + cta[c]));
     return t < g4_tiles_time(T, L->rows, L->d);
