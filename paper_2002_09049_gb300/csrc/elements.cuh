@@ -46,6 +46,29 @@ __device__ __forceinline__ uint32_t pack2(float a, float b, __nv_bfloat16)
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 
+// Two floats at once, each rounded as one alone.
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(*reinterpret_cast<const uint64_t *>(&a)),
+        "l"(*reinterpret_cast<const uint64_t *>(&b)));
+    return *reinterpret_cast<const float2 *>(&r);
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(*reinterpret_cast<const uint64_t *>(&a)),
+        "l"(*reinterpret_cast<const uint64_t *>(&b)), "l"(*reinterpret_cast<const uint64_t *>(&c)));
+    return *reinterpret_cast<const float2 *>(&r);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(*reinterpret_cast<const uint64_t *>(&a)),
+        "l"(*reinterpret_cast<const uint64_t *>(&b)));
+    return *reinterpret_cast<const float2 *>(&r);
+}
+
 // Eight elements from p (16-byte aligned).  Ordinary loads: in a kernel that begins with griddep_wait
 // what they read may have been written by the kernel before.
 __device__ __forceinline__ void load8(const float *p, float (&v)[8])
@@ -114,6 +137,22 @@ __device__ __forceinline__ void store8(T *p, const float (&v)[8])
                    pack2(v[6], v[7], T()));
 }
 
+// Eight words from p on (16-byte aligned).
+__device__ __forceinline__ void load_words(const uint32_t *p, uint32_t (&w)[8])
+{
+    if (((uintptr_t)p & 31) == 0) {
+        asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]),
+                       "=r"(w[6]), "=r"(w[7])
+                     : "l"(__cvta_generic_to_global(p)) : "memory");
+    } else {
+        const uint4 a = reinterpret_cast<const uint4 *>(p)[0];
+        const uint4 b = reinterpret_cast<const uint4 *>(p)[1];
+        w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w;
+        w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
+    }
+}
+
 // Sixteen elements from p on, to p on (16-byte aligned): 32-byte accesses where p is 32-byte aligned.
 template <typename T>
 __device__ __forceinline__ void load16(const T *p, float (&v)[16])
@@ -126,17 +165,7 @@ __device__ __forceinline__ void load16(const T *p, float (&v)[16])
         for (int i = 0; i < 8; ++i) v[i] = a[i], v[8 + i] = b[i];
     } else {
         uint32_t w[8];
-        if (((uintptr_t)p & 31) == 0) {
-            asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                         : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]),
-                           "=r"(w[6]), "=r"(w[7])
-                         : "l"(__cvta_generic_to_global(p)) : "memory");
-        } else {
-            const uint4 a = reinterpret_cast<const uint4 *>(p)[0];
-            const uint4 b = reinterpret_cast<const uint4 *>(p)[1];
-            w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w;
-            w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
-        }
+        load_words(reinterpret_cast<const uint32_t *>(p), w);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float2 f = unpack2(w[i], T());

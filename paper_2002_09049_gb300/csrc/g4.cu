@@ -7,12 +7,14 @@
 // Res. Dev. 34(1), 1990), a division where the scale is so small or large that a remainder could leave the
 // normal range.
 //
-// Memory-bound where elements are fp32: 11,008 x 4,096 is quantised in 33.0 us and read back in 31.4 (204 MB each, 6.2 and
-// 6.5 TB/s).  4,096 x 4,096 bf16 with zero points in groups of 64 takes 13.6 and 7.8 (42 MB each): quantising, 250
-// warp instructions for 512 elements (two words a thread took 13 shuffles for 16 elements' range; with one word a
-// thread, and a division's two corrections, 19.2 us).
+// Memory-bound where elements are fp32: 11,008 x 4,096 is quantised in 31.3 us and read back in 31.4 (204 MB each, 6.5
+// TB/s).  4,096 x 4,096 bf16 with zero points in groups of 64 takes 10.5 and 7.8 (42 MB each): quantising is bound by issue.
+// 16-bit types' ranges are found two elements an instruction, and quotients and their rounding too (one by one 13.6 us; with
+// one word of codes a thread and a division's two corrections 19.2); two tiles a thread instead of four took 10.9.
 #include <math.h>
 #include <string.h>
+
+#include <type_traits>
 
 #include "g4.cuh"
 #include "sm100.cuh"
@@ -44,11 +46,112 @@ __device__ __forceinline__ float near_reciprocal(float s)
     return r;
 }
 
+// For scales that quotient() is not for.  Functions of their own: a division's code among the quotients cost 2 of 11 us.
+__device__ __noinline__ float divided(float x, float s) { return __fdiv_rn(x, s); }
+__device__ __noinline__ uint32_t divided_codes(float2 a, float2 b, float2 c, float2 d, float s, int z, float least, float most)
+{
+    const float x[8] = {a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
+    uint32_t w = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        w |= (uint32_t)(z + (int)rintf(fminf(fmaxf(__fdiv_rn(x[i], s), least), most))) << g4_shift(i);
+    return w;
+}
+
 // The nearest whole number (|y| below 2^22, ties to even).
 __device__ __forceinline__ int whole(float y)
 {
     return __float_as_int(__fadd_rn(y, 12582912.0f)) - __float_as_int(12582912.0f);
 }
+
+// A thread's 16 elements as they were read, and their range: the largest |x| (0 beside it), or with ZEROS the largest of x
+// and 0 and the largest of -x and 0; NaN if an element is.
+template <typename T>
+struct Sixteen {
+    uint32_t w[8];                           // two elements each
+
+    using Two = std::conditional_t<std::is_same_v<T, __half>, __half2, __nv_bfloat162>;
+    __device__ static __forceinline__ uint32_t more(uint32_t a, uint32_t b)
+    {
+        const Two m = __hmax2_nan(as(a), as(b));
+        return *reinterpret_cast<const uint32_t *>(&m);
+    }
+    __device__ static __forceinline__ uint32_t less(uint32_t a, uint32_t b)
+    {
+        const Two m = __hmin2_nan(as(a), as(b));
+        return *reinterpret_cast<const uint32_t *>(&m);
+    }
+    __device__ static __forceinline__ Two as(uint32_t v) { return *reinterpret_cast<Two *>(&v); }
+
+    __device__ __forceinline__ void load(const T *x) { load_words(reinterpret_cast<const uint32_t *>(x), w); }
+    __device__ __forceinline__ void pair(int i, float a, float b) { w[i] = pack2(a, b, T()); }
+    __device__ __forceinline__ float2 pair(int i) const { return unpack2(w[i], T()); }
+
+    template <bool ZEROS>
+    __device__ __forceinline__ float2 range(int threads) const
+    {
+        constexpr uint32_t off = ZEROS ? 0xffffffffu : 0x7fff7fffu;
+        uint32_t m = w[0] & off;
+#pragma unroll
+        for (int i = 1; i < 8; ++i) m = more(m, w[i] & off);
+        if (ZEROS) {                         // the pairs' largest, and their least with its sign turned
+            uint32_t l = w[0];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) l = less(l, w[i]);
+            m = more(__byte_perm(m, l, 0x5410) ^ 0x80000000u, __byte_perm(m, l, 0x7632) ^ 0x80000000u);
+        }
+#pragma unroll
+        for (int o = 1; o < 8; o <<= 1) {
+            if (o >= threads) break;
+            m = more(m, __shfl_xor_sync(0xffffffffu, m, o));
+        }
+        if (ZEROS) return unpack2(more(m, 0u), T());
+        return {unpack2(more(m, m >> 16), T()).x, 0.0f};
+    }
+};
+
+template <>
+struct Sixteen<float> {
+    float v[16];
+
+    __device__ static __forceinline__ float more(float a, float b, float c)
+    {
+        float m;
+        asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(a), "f"(b), "f"(c));
+        return m;
+    }
+    __device__ static __forceinline__ float less(float a, float b, float c)
+    {
+        float m;
+        asm("min.NaN.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(a), "f"(b), "f"(c));
+        return m;
+    }
+
+    __device__ __forceinline__ void load(const float *x) { load16(x, v); }
+    __device__ __forceinline__ void pair(int i, float a, float b) { v[2 * i] = a, v[2 * i + 1] = b; }
+    __device__ __forceinline__ float2 pair(int i) const { return {v[2 * i], v[2 * i + 1]}; }
+
+    template <bool ZEROS>
+    __device__ __forceinline__ float2 range(int threads) const
+    {
+        float m = ZEROS ? 0.0f : __uint_as_float(top_bits(v)), l = 0.0f;
+        if (ZEROS) {
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+                m = more(m, v[i], v[i + 1]);
+                l = less(l, v[i], v[i + 1]);
+            }
+        }
+        l = -l;
+#pragma unroll
+        for (int o = 1; o < 8; o <<= 1) {
+            if (o >= threads) break;
+            m = more(m, __shfl_xor_sync(0xffffffffu, m, o), 0.0f);
+            if (ZEROS) l = more(l, __shfl_xor_sync(0xffffffffu, l, o), 0.0f);
+        }
+        return {m, l};
+    }
+};
 
 struct G4Group {
     float s, r;
@@ -56,61 +159,51 @@ struct G4Group {
     bool plain;                              // s lies where quotient() is exact; r is its reciprocal
 };
 
-// The scale and zero point of a group of `threads` threads (2, 4 or 8 lanes of a warp) of 16 elements.
-template <bool ZEROS>
-__device__ __forceinline__ G4Group group_of(const float (&v)[16], int threads)
+// The scale and zero point of a group of `threads` threads (2, 4 or 8 lanes of a warp) of 16 elements.  The scale before its
+// rounding is finite where all elements are.
+template <bool ZEROS, typename T>
+__device__ __forceinline__ G4Group group_of(const Sixteen<T> &v, int threads)
 {
-    uint32_t top = top_bits(v);
-    float hi = 0.0f, lo = 0.0f;
-    if (ZEROS) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            hi = fmaxf(hi, v[i]);
-            lo = fminf(lo, v[i]);
-        }
-    }
-#pragma unroll
-    for (int o = 1; o < 8; o <<= 1) {
-        if (o >= threads) break;
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-        if (ZEROS) {
-            hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-            lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-        }
-    }
+    const float2 m = v.template range<ZEROS>(threads);
     constexpr float seventh = 1.0f / 7.0f, fifteenth = 1.0f / 15.0f;
+    const float s = ZEROS ? __fadd_rn(__fmul_rn(m.x, fifteenth), __fmul_rn(m.y, fifteenth)) : __fmul_rn(m.x, seventh);
     G4Group g;
-    g.s = bf16_rn(ZEROS ? __fsub_rn(__fmul_rn(hi, fifteenth), __fmul_rn(lo, fifteenth))
-                        : __fmul_rn(__uint_as_float(top), seventh));
-    if (top >= 0x7f800000u) g.s = NAN;
+    g.s = s < INFINITY ? bf16_rn(s) : NAN;
     g.plain = g.s >= 0x1p-100f && g.s <= 0x1p100f;
     g.r = near_reciprocal(g.s);
     g.z = G4_ZERO;
     if (ZEROS && g.s > 0.0f) {
-        const float z = g.plain ? quotient(-lo, g.s, g.r) : __fdiv_rn(-lo, g.s);
+        const float z = g.plain ? quotient(m.y, g.s, g.r) : divided(m.y, g.s);
         g.z = min(max(whole(fminf(z, 32.0f)), 0), 15);
     }
     return g;
 }
 
-// The word of eight codes.  A quotient is clamped to the codes' range, and 1.5 * 2^23 added, which rounds it to the
-// whole number in the sum's low bits; the word is the sum of those bits in their places, less what the bits of
-// 1.5 * 2^23 themselves and z come to (all modulo 2^32).
-template <bool ZEROS>
-__device__ __forceinline__ uint32_t codes_of(const float *v, const G4Group &g)
+// The word of the eight codes of pairs p .. p + 3.  1.5 * 2^23 + 16 is added to a quotient, which rounds it to the whole
+// number in the sum's low bits, plus 16.  A scale that is a normal number is less than 2^-8 below its group's
+// range / 7 or / 15, so |x / s| <= 7.03, or x / s in [-15.06, 15.06]: without zero points all codes are in the range.  With
+// them z is the least element's quotient rounded, and no other rounds to less than -z, while the largest may come
+// to 16.  Two sums' low halves lie in a word as two elements' codes do, so a word is four such pairs in their places,
+// less what the 16s and z come to (all modulo 2^32).
+template <bool ZEROS, typename T>
+__device__ __forceinline__ uint32_t codes_of(const Sixteen<T> &v, int p, const G4Group &g)
 {
-    constexpr float big = 12582912.0f;
+    constexpr float big = 12582912.0f + 16.0f;
     if (!(g.s > 0.0f)) return (uint32_t)g.z * 0x11111111u;
-    const float least = ZEROS ? (float)-g.z : -7.0f, most = ZEROS ? (float)(15 - g.z) : 7.0f;
-    uint32_t w = (uint32_t)(g.z - __float_as_int(big)) * 0x11111111u;
-    if (g.plain) {
+    if (!g.plain)
+        return divided_codes(v.pair(p), v.pair(p + 1), v.pair(p + 2), v.pair(p + 3), g.s, g.z,
+                             ZEROS ? (float)-g.z : -7.0f, ZEROS ? (float)(15 - g.z) : 7.0f);
+    uint32_t w = (uint32_t)(g.z - 16) * 0x11111111u;
+    const uint32_t most = (uint32_t)(31 - g.z) * 0x10001u;
+    const float2 s = {-g.s, -g.s}, r = {g.r, g.r};
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            w += __float_as_uint(__fadd_rn(fminf(fmaxf(quotient(v[i], g.s, g.r), least), most), big)) << g4_shift(i);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            w += __float_as_uint(__fadd_rn(fminf(fmaxf(__fdiv_rn(v[i], g.s), least), most), big)) << g4_shift(i);
+    for (int i = 0; i < 4; ++i) {
+        const float2 x = v.pair(p + i);
+        float2 y = mul2(x, r);               // quotient()
+        y = fma2(fma2(y, s, x), r, y);
+        y = add2(y, {big, big});
+        const uint32_t two = __byte_perm(__float_as_uint(y.x), __float_as_uint(y.y), 0x5410);
+        w += (ZEROS ? __vmins2(two, most) : two) << (4 * i);
     }
     return w;
 }
@@ -129,9 +222,10 @@ __device__ __forceinline__ TileRun tile_run(const mpq_g4_matrix &L, int most)
 
 // A thread has 16 elements of U tiles, and 128 threads a tile's 16 rows; the CTA's two halves take U tiles each.  VEC: rows
 // are 16-byte aligned, and all of a thread's elements are on their way before the first is used; else (U = 1) rows
-// pass through shared memory, a warp's accesses consecutive.
+// pass through shared memory, a warp's accesses consecutive.  Four CTAs an SM: fp32 with zero points, 11,008 x 4,096, is
+// 36.4 us with the two registers more that leave three, 33.6 with four.
 template <typename T, bool VEC, bool ZEROS, int U>
-__global__ void __launch_bounds__(G4_THREADS)
+__global__ void __launch_bounds__(G4_THREADS, U > 1 ? 4 : 1)
 g4_quantize_kernel(const T *X, long long ldx, mpq_g4_matrix L, unsigned char *packed)
 {
     static_assert(VEC || U == 1, "one staged tile of a half");
@@ -141,7 +235,7 @@ g4_quantize_kernel(const T *X, long long ldx, mpq_g4_matrix L, unsigned char *pa
     const TileRun run = tile_run(L, 2 * U);
     const int part = (int)threadIdx.x >> 7, in_tile = ((int)threadIdx.x >> 3) & 15, n = 2 * (threadIdx.x & 7);
     const int k0 = run.kt0 + part * U;
-    float v[U][16];
+    Sixteen<T> v[U];
     if constexpr (VEC) {
         const long long row = run.row0 + in_tile;
         const bool real = row < L.rows;
@@ -150,10 +244,12 @@ g4_quantize_kernel(const T *X, long long ldx, mpq_g4_matrix L, unsigned char *pa
         for (int u = 0; u < U; ++u) {
             const int j = (k0 + u) * 128 + n * 8;
             if (real && j + 16 <= L.d) {
-                load16(x + j, v[u]);
+                v[u].load(x + j);
             } else {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) v[u][i] = real && j + i < L.d ? to_f32(x[j + i]) : 0.0f;
+                for (int i = 0; i < 8; ++i)
+                    v[u].pair(i, real && j + 2 * i < L.d ? to_f32(x[j + 2 * i]) : 0.0f,
+                              real && j + 2 * i + 1 < L.d ? to_f32(x[j + 2 * i + 1]) : 0.0f);
             }
         }
     } else {
@@ -166,13 +262,16 @@ g4_quantize_kernel(const T *X, long long ldx, mpq_g4_matrix L, unsigned char *pa
         }
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[0][i] = stage[(part * 16 + in_tile) * G4_PITCH + n * 8 + i];
+        for (int i = 0; i < 8; ++i) {
+            const float *const at = stage + (part * 16 + in_tile) * G4_PITCH + n * 8 + 2 * i;
+            v[0].pair(i, at[0], at[1]);
+        }
     }
     const int threads = L.group >> 4, groups = 128 / L.group;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const G4Group g = group_of<ZEROS>(v[u], threads);
-        const uint32_t w0 = codes_of<ZEROS>(v[u], g), w1 = codes_of<ZEROS>(v[u] + 8, g);
+        const uint32_t w0 = codes_of<ZEROS>(v[u], 0, g), w1 = codes_of<ZEROS>(v[u], 4, g);
         const size_t at = ((size_t)run.rt * L.k_tiles + k0 + u) * L.tile_bytes;
         if (part * U + u >= run.here || !MPQ_IN(at + L.tile_bytes - 1, L.bytes)) return;
         unsigned char *const tile = packed + at;
@@ -239,10 +338,10 @@ g4_dequantize_kernel(const unsigned char *packed, mpq_g4_matrix L, T *Y, long lo
     }
 }
 
-// Whether four tiles to a CTA leave every SM its fill of CTAs (eight).
-bool by_fours(const mpq_g4_matrix *L, bool vec)
+// Whether `each` tiles to a CTA leave every SM its fill of CTAs (`fill`).
+bool by_many(const mpq_g4_matrix *L, bool vec, int each, int fill)
 {
-    return vec && (long long)L->row_tiles * ((L->k_tiles + 3) / 4) >= 8LL * sm_count();
+    return vec && (long long)L->row_tiles * ((L->k_tiles + each - 1) / each) >= (long long)fill * sm_count();
 }
 dim3 tile_grid(const mpq_g4_matrix *L, int each)
 {
@@ -252,11 +351,12 @@ dim3 tile_grid(const mpq_g4_matrix *L, int each)
 template <typename T, bool ZEROS>
 mpq_status quantize_typed(const void *X, bool vec, long long ldx, const mpq_g4_matrix *L, void *packed, cudaStream_t stream)
 {
-    const bool four = by_fours(L, vec);
-    return launch_waiting(four  ? g4_quantize_kernel<T, true, ZEROS, 2>
+    constexpr int U = sizeof(T) == 2 ? 4 : 2;                // 128 bytes a thread on their way
+    const bool many = by_many(L, vec, 2 * U, 16 / U);
+    return launch_waiting(many  ? g4_quantize_kernel<T, true, ZEROS, U>
                           : vec ? g4_quantize_kernel<T, true, ZEROS, 1>
                                 : g4_quantize_kernel<T, false, ZEROS, 1>,
-                          tile_grid(L, four ? 4 : 2), dim3(G4_THREADS), 0, stream, "g4 quantize launch",
+                          tile_grid(L, many ? 2 * U : 2), dim3(G4_THREADS), 0, stream, "g4 quantize launch",
                           static_cast<const T *>(X), ldx, *L, static_cast<unsigned char *>(packed));
 }
 
@@ -295,7 +395,7 @@ mpq_status launch_g4_dequantize(const void *packed, const mpq_g4_matrix *L, void
     const bool vec = aligned(Y, y_type, ldy, L->rows);
     return by_type(y_type, [&](auto t) {
         using T = decltype(t);
-        const int each = by_fours(L, vec) ? 4 : 1;
+        const int each = by_many(L, vec, 4, 8) ? 4 : 1;
         return launch_waiting(each > 1 ? g4_dequantize_kernel<T, true, 4>
                               : vec    ? g4_dequantize_kernel<T, true, 1>
                                        : g4_dequantize_kernel<T, false, 1>,

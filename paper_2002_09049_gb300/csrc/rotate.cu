@@ -80,22 +80,6 @@ __host__ __device__ constexpr int place(int i) { return V == 8 ? (i >> 3) * 28 +
 template <int V>
 constexpr int kSine = V == 8 ? 8 : 1;
 
-// Two floats at once, each rounded as one alone.
-__device__ __forceinline__ float2 mul2(float2 a, float2 b)
-{
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(*reinterpret_cast<const uint64_t *>(&a)),
-        "l"(*reinterpret_cast<const uint64_t *>(&b)));
-    return *reinterpret_cast<const float2 *>(&r);
-}
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
-{
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(*reinterpret_cast<const uint64_t *>(&a)),
-        "l"(*reinterpret_cast<const uint64_t *>(&b)), "l"(*reinterpret_cast<const uint64_t *>(&c)));
-    return *reinterpret_cast<const float2 *>(&r);
-}
-
 // (l, r) -> (l c - r s, r c + l s)
 __device__ __forceinline__ void turn_pair(float &l, float &r, float c, float s)
 {

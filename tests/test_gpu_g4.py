@@ -100,6 +100,37 @@ def test_quantize_special_values(gpu, group, zeros):
     assert torch.equal(again.cpu(), want)
 
 
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("group,zeros", KINDS)
+def test_quantize_every_16_bit_float(gpu, group, zeros, dtype):
+    """Every 16-bit float -- both zeros, subnormals, infinities, NaN -- in order and out of it, and ranges whose two
+    ends both round away from zero: as the definition has them, and as the same floats in fp32."""
+    bits = np.arange(65536, dtype=np.uint16)
+    mixed = np.random.default_rng(9).permutation(bits)
+    x = torch.from_numpy(np.concatenate([bits, mixed, mixed | 0x8000]).view(np.int16)).view(TYPES[dtype]).view(-1, 128)
+    ends = torch.zeros(512, 128, dtype=TYPES[dtype])
+    ends[:, ::2] = (1 + torch.arange(512) / 512)[:, None] * 5.5
+    ends[:, 1::2] = -9.5
+    x = torch.cat([x, ends])
+    lay = binding.mpq_g4_layout(*x.shape, group, zeros)
+    packed = binding.mpq_g4_quantize(x.to(DEV), lay)
+    assert torch.equal(packed, binding.mpq_g4_quantize(x.float().to(DEV), lay))
+    q, z, s = ref.g4_encode(x.float().numpy(), group, zeros)
+    got = binding.mpq_g4_dequantize(packed, lay).cpu().numpy()
+    with np.errstate(over="ignore", invalid="ignore"):
+        want = ref.g4_values(q, z, s, 128).astype(np.float32)
+    assert np.array_equal(got, want, equal_nan=True)
+    wide = torch.empty(x.shape[0], 129, dtype=TYPES[dtype], device=DEV)[:, 1:]        # rows off the 16-byte boundary
+    assert torch.equal(binding.mpq_g4_quantize(wide.copy_(x), lay), packed)
+    many = x.view(16, -1).repeat(80, 1).to(DEV)                                       # several tiles a thread
+    lay = binding.mpq_g4_layout(*many.shape, group, zeros)
+    packed = binding.mpq_g4_quantize(many, lay)
+    assert torch.equal(packed, binding.mpq_g4_quantize(many.float(), lay))
+    assert torch.equal(packed.view(80, -1), packed[:packed.numel() // 80].expand(80, -1))
+    assert torch.equal(binding.mpq_g4_dequantize(packed, lay)[:16].nan_to_num(7.0).cpu(),
+                       torch.from_numpy(got).view(16, -1).nan_to_num(7.0))
+
+
 @pytest.mark.parametrize("group,zeros", KINDS)
 def test_every_code(gpu, group, zeros):
     """Buffers made elsewhere: every code with every zero point, scales of either sign."""
