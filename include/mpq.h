@@ -594,8 +594,15 @@ mpq_status mpq_g4_dequantize(const void *packed, const mpq_g4_matrix *layout, vo
 
 /*
  * mpq_g4_linear -- Y[t][c] = sum_j x_tj w_cj + bias_c for inputs X [T][d] and packed weights W [C][d]: w is a weight's
- * value s (q - z) rounded once to X's type, what mpq_g4_dequantize gives in it (bf16: by 2^-9 of it at most; fp16: by
- * 2^-12, infinite from 65,520 on); exact products, fp32 sums, the bias added in fp32, one rounding to y_type.
+ * value s (q - z) rounded once to X's type, what mpq_g4_dequantize gives in it; exact products, fp32 sums, the bias
+ * added in fp32, one rounding to y_type.  The weight's rounding is 2^-9 of it at most in bf16 (as much as the rounding
+ * of outputs in that type), in fp16 2^-12 of it or 2^-25, whichever is more: values below 2^-25 vanish, those from
+ * 65,520 on are infinite.
+ * mpq_g4_linear_exact -- the same with w = s (q - z) itself, for matrices and sums where that rounding counts: up to
+ * twice the time where there are many tokens, no more where there are few.  Products and sums in fp32: few tokens' (as many
+ * as are faster so) are sums of x (q - z) for each group, which |x| below 2^112 keeps finite, times s; many tokens'
+ * weights are two terms of X's type, exact where |w| is below bf16's largest number.  With fp16 inputs a scale less than
+ * 2^-28 of its row's largest may be off by 2^-36 of that one.
  *   X     [T][d] of type x_type (MPQ_F16 or MPQ_BF16), rows ldx elements apart (ldx >= d; 16-byte aligned rows of a
  *         multiple of 8 elements are faster).
  *   bias  [C] fp32 or NULL.
@@ -606,6 +613,8 @@ mpq_status mpq_g4_dequantize(const void *packed, const mpq_g4_matrix *layout, vo
  */
 mpq_status mpq_g4_linear(const void *X, int x_type, long long ldx, int T, const mpq_g4_matrix *w_layout,
                          const void *W, const float *bias, void *Y, int y_type, long long ldy, void *stream);
+mpq_status mpq_g4_linear_exact(const void *X, int x_type, long long ldx, int T, const mpq_g4_matrix *w_layout,
+                               const void *W, const float *bias, void *Y, int y_type, long long ldy, void *stream);
 
 /*
  * Positions.  mpq_rotation_turns -- HOST only: the frequencies freq[n] (radians a position, finite) as turns a

@@ -125,6 +125,7 @@ SIGNATURES = {
     "mpq_g4_quantize": ([_P, _I, _LL, _G4, _P, _P], _I),
     "mpq_g4_dequantize": ([_P, _G4, _P, _I, _LL, _P], _I),
     "mpq_g4_linear": ([_P, _I, _LL, _I, _G4, _P, _P, _P, _I, _LL, _P], _I),
+    "mpq_g4_linear_exact": ([_P, _I, _LL, _I, _G4, _P, _P, _P, _I, _LL, _P], _I),
     "mpq_rotation_turns": ([_P, _I, _P], _I),
     "mpq_rotate": ([_R, _R, _I, _I, _I, _P, _I, _P, _I, _I, _I, ctypes.c_float, _P], _I),
     "mpq_pages_extend": ([_P, _I, _I, _I, _P, _P, _P, _P, _I, _P, _P, _P, _P, _LL, _P, _P], _I),
@@ -607,10 +608,11 @@ def mpq_g4_dequantize(packed, layout: G4Matrix, dtype=torch.float32, Y=None, str
     return _native.g4_dequantize(packed, layout, dtype, Y, stream)
 
 
-def mpq_g4_linear(X, W, w_layout: G4Matrix, bias=None, dtype=None, Y=None, stream=None):
+def mpq_g4_linear(X, W, w_layout: G4Matrix, bias=None, dtype=None, Y=None, stream=None, exact: bool = False):
     """Y [T][C] = X W^T + bias for inputs X [T][d] (fp16 or bf16; rows may lie apart) and packed weights W
-    [C][d]; bias fp32 [C].  dtype: that of Y, X's by default."""
-    return _native.g4_linear(X, W, w_layout, bias, dtype, Y, stream)
+    [C][d]; bias fp32 [C].  dtype: that of Y, X's by default.  The weights' values are rounded to X's type first;
+    exact: they are not (mpq_g4_linear_exact; up to twice the time for many tokens)."""
+    return _native.g4_linear(X, W, w_layout, bias, dtype, Y, stream, exact)
 
 
 def mpq_rotation(freq, device="cuda"):

@@ -29,7 +29,7 @@ decltype(&mpq_cache_read) f_cache_read;
 decltype(&mpq_cache_attention) f_cache_attention;
 decltype(&mpq_g4_quantize) f_g4_quantize;
 decltype(&mpq_g4_dequantize) f_g4_dequantize;
-decltype(&mpq_g4_linear) f_g4_linear;
+decltype(&mpq_g4_linear) f_g4_linear, f_g4_linear_exact;
 decltype(&mpq_rotate) f_rotate;
 decltype(&mpq_pages_extend) f_pages_extend;
 decltype(&mpq_pages_trim) f_pages_trim;
@@ -412,9 +412,17 @@ PyObject *g4_dequantize(PyObject *const *v)   // packed, layout, dtype, Y, strea
     return own ? THPVariable_Wrap(Y) : same(v[3]);
 }
 
-PyObject *g4_linear(PyObject *const *v)       // X, W, w_layout, bias, dtype, Y, stream
+bool flag(PyObject *o)
+{
+    const int r = PyObject_IsTrue(o);
+    if (r < 0) throw Refused();
+    return r != 0;
+}
+
+PyObject *g4_linear(PyObject *const *v)       // X, W, w_layout, bias, dtype, Y, stream, exact
 {
     Call call;
+    const bool exact = flag(v[7]);
     const at::Tensor &X = call.tensor(v[0], "X");
     const mpq_g4_matrix &L = layout<mpq_g4_matrix>(v[2], "w_layout");
     if (X.dim() != 2) refuse(PyExc_ValueError, "%s must be [T][d]", "X");
@@ -429,16 +437,9 @@ PyObject *g4_linear(PyObject *const *v)       // X, W, w_layout, bias, dtype, Y,
     const at::Tensor Y = own ? call.empty({T, L.rows}, v[4] == Py_None ? X.scalar_type() : dtype_arg(v[4]))
                              : THPVariable_Unpack(v[5]);
     const long long ldy = rows_of(Y, "Y", T, L.rows);
-    run("mpq_g4_linear", f_g4_linear, X.data_ptr(), type, ldx, (int)T, &L, W.data_ptr(),
+    run(exact ? "mpq_g4_linear_exact" : "mpq_g4_linear", exact ? f_g4_linear_exact : f_g4_linear, X.data_ptr(), type, ldx, (int)T, &L, W.data_ptr(),
         bias ? bias->data_ptr<float>() : nullptr, Y.data_ptr(), type_of(Y.scalar_type(), "Y"), ldy, stream);
     return own ? THPVariable_Wrap(Y) : same(v[5]);
-}
-
-bool flag(PyObject *o)
-{
-    const int r = PyObject_IsTrue(o);
-    if (r < 0) throw Refused();
-    return r != 0;
 }
 
 // Q or K [T][heads][dim] of a rotation, and where its output goes (None: allocated later).
@@ -619,6 +620,7 @@ PyObject *init(PyObject *, PyObject *args)
     take(f_g4_quantize, "mpq_g4_quantize");
     take(f_g4_dequantize, "mpq_g4_dequantize");
     take(f_g4_linear, "mpq_g4_linear");
+    take(f_g4_linear_exact, "mpq_g4_linear_exact");
     take(f_rotate, "mpq_rotate");
     take(f_pages_extend, "mpq_pages_extend");
     take(f_pages_trim, "mpq_pages_trim");
@@ -648,7 +650,7 @@ PyMethodDef methods[] = {{"init", init, METH_VARARGS, nullptr},
                          method<cache_attention, 12>("cache_attention"),
                          method<g4_quantize, 4>("g4_quantize"),
                          method<g4_dequantize, 5>("g4_dequantize"),
-                         method<g4_linear, 7>("g4_linear"),
+                         method<g4_linear, 8>("g4_linear"),
                          method<rotate, 13>("rotate"),
                          method<pages_extend, 13>("pages_extend"),
                          method<pages_trim, 9>("pages_trim"),

@@ -31,11 +31,18 @@ struct G4Pairs<__nv_bfloat16> {
     // s twice; its bits are a bf16's
     __device__ static __forceinline__ uint32_t scale(uint32_t bits) { return __byte_perm(bits, 0, 0x1010); }
     __device__ static __forceinline__ bool plain(uint32_t) { return true; }
+    __device__ static __forceinline__ uint32_t whole(uint32_t v, uint32_t from) { return bits(__hsub2(as(v), as(from))); }
     __device__ static __forceinline__ uint32_t value(uint32_t v, uint32_t from, uint32_t s)
     {
-        const __nv_bfloat162 r = __hmul2(__hsub2(as(v), as(from)), as(s));
-        return *reinterpret_cast<const uint32_t *>(&r);
+        return bits(__hmul2(__hsub2(as(v), as(from)), as(s)));
     }
+    // what value() rounds off, exact
+    __device__ static __forceinline__ uint32_t rest(uint32_t v, uint32_t from, uint32_t s)
+    {
+        const __nv_bfloat162 q = __hsub2(as(v), as(from));
+        return bits(__hfma2(q, as(s), __hneg2(__hmul2(q, as(s)))));
+    }
+    __device__ static __forceinline__ uint32_t bits(__nv_bfloat162 r) { return *reinterpret_cast<const uint32_t *>(&r); }
     __device__ static __forceinline__ __nv_bfloat162 as(uint32_t v) { return *reinterpret_cast<__nv_bfloat162 *>(&v); }
 };
 template <>
@@ -44,19 +51,24 @@ struct G4Pairs<__half> {
     static constexpr uint32_t kPower = 0x64006400u;      // 1024
     __device__ static __forceinline__ uint32_t scale(uint32_t bits)
     {
-        const __half2 h = __float2half2_rn(bf16_bits(bits));
-        return *reinterpret_cast<const uint32_t *>(&h);
+        return G4Pairs::bits(__float2half2_rn(bf16_bits(bits)));
     }
     __device__ static __forceinline__ bool plain(uint32_t bits)      // |s| in [2^-17, 2^15], or 0
     {
         const uint32_t m = bits & 0x7fffu;
         return m - 0x3700u <= 0x4700u - 0x3700u || m == 0;
     }
+    __device__ static __forceinline__ uint32_t whole(uint32_t v, uint32_t from) { return bits(__hsub2(as(v), as(from))); }
     __device__ static __forceinline__ uint32_t value(uint32_t v, uint32_t from, uint32_t s)
     {
-        const __half2 r = __hmul2(__hsub2(as(v), as(from)), as(s));
-        return *reinterpret_cast<const uint32_t *>(&r);
+        return bits(__hmul2(__hsub2(as(v), as(from)), as(s)));
     }
+    __device__ static __forceinline__ uint32_t rest(uint32_t v, uint32_t from, uint32_t s)
+    {
+        const __half2 q = __hsub2(as(v), as(from));
+        return bits(__hfma2(q, as(s), __hneg2(__hmul2(q, as(s)))));
+    }
+    __device__ static __forceinline__ uint32_t bits(__half2 r) { return *reinterpret_cast<const uint32_t *>(&r); }
     __device__ static __forceinline__ __half2 as(uint32_t v) { return *reinterpret_cast<__half2 *>(&v); }
 };
 
@@ -68,6 +80,32 @@ template <typename T>
 __device__ __forceinline__ G4Scale g4_scale(uint32_t bits, uint32_t z)
 {
     return {G4Pairs<T>::scale(bits), G4Pairs<T>::kPower | z | z << 16, bits};
+}
+
+// A pair of a word's codes as the bits of the power plus each.
+template <typename T>
+__device__ __forceinline__ uint32_t g4_pair(uint32_t w, int j)
+{
+    uint32_t v;                                  // (w >> 4 j) & 0x000f000f | the power: one operation of three inputs
+    asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(v) : "r"(w >> (4 * j)), "n"(0x000f000f), "n"(G4Pairs<T>::kPower));
+    return v;
+}
+
+// A word's eight q - z, whole numbers that either type holds.
+template <typename T>
+__device__ __forceinline__ void g4_whole(uint32_t w, uint32_t from, uint32_t (&p)[4])
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) p[j] = G4Pairs<T>::whole(g4_pair<T>(w, j), from);
+}
+
+// What the word's eight values lose to their rounding: s and q - z have 8 and 4 bits, their product 12, of which bf16 keeps
+// 8 and fp16 11, so what is left is a T again (where it is not below T's least place: bf16's 2^-133, fp16's 2^-24).
+template <typename T>
+__device__ __forceinline__ void g4_rest(uint32_t w, const G4Scale &g, uint32_t (&p)[4])
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) p[j] = G4Pairs<T>::rest(g4_pair<T>(w, j), g.from, g.s);
 }
 
 // FAR: scales that G4Pairs<T>::plain does not hold for are among a warp's (hardly a matrix has such), so all of them
@@ -83,12 +121,7 @@ __device__ __forceinline__ void g4_values(uint32_t w, const G4Scale &g, uint32_t
             p[j] = pack2((float)((int)(w >> (4 * j) & 15u) - z) * s, (float)((int)(w >> (4 * j + 16) & 15u) - z) * s, T());
     } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            uint32_t v;                          // (w >> 4 j) & 0x000f000f | the power: one operation of three inputs
-            asm("lop3.b32 %0, %1, %2, %3, 0xea;"
-                : "=r"(v) : "r"(w >> (4 * j)), "n"(0x000f000f), "n"(G4Pairs<T>::kPower));
-            p[j] = G4Pairs<T>::value(v, g.from, g.s);
-        }
+        for (int j = 0; j < 4; ++j) p[j] = G4Pairs<T>::value(g4_pair<T>(w, j), g.from, g.s);
     }
 }
 

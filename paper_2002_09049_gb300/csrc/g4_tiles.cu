@@ -13,6 +13,15 @@
 // warps issue the MMAs of every other stage, into accumulators of their own whose sums are added on the way out (one
 // warp's waits and issue took 800 cycles a stage, 340 of them the MMAs').
 //
+// EXACT: no weight is rounded.  s (q - z) has 12 significant bits, so it is a term of bf16 and what that leaves, a second
+// one: all of K goes by twice, once for either term, into the same sums.  fp16 holds 11 bits, all there are without
+// zero points, but not every size: a channel's scales are taken times a power of two that brings the largest of them (of
+// the CTA's share of K) to 2^11 or more, and its sums divided by it.  A scale of 2^-28 of that largest one or more is
+// held as it is, a smaller one to 2^-36 of it.
+//
+// Measured, beside the rounded values': 2,048 x 11,008 x 4,096 bf16 191 us (102), fp16 without zero points 110 (104), with
+// them 200 (105); 256 x 11,008 x 4,096 bf16 41.8 (24.4); 75 x 4,096 x 11,008 bf16 23.7 (14.3).
+//
 // Measured: 2,048 x 11,008 x 4,096 (T x C x d) 105 us, 1.76 PFLOP/s: a stage takes 1,024 cycles, its MMAs' own; 1,800 a
 // tile between the last MMA and the next one's first; 344 tiles on 76 pairs are five rounds.  75 x 4,096 x 11,008 14.8
 // us: 2 to the first MMA, 22 stages of 0.35 on 128 CTAs (1,700 warp instructions a stage to make its operands), 3 for
@@ -81,6 +90,7 @@ struct TileArgs {
     int n_tile, held;                    // tokens of a tile; of them, in one CTA's shared memory
     int n_tiles, tiles;                  // tiles along the tokens; all (of a pair, or a cluster)
     int split;                           // CTAs that share a tile's K
+    int terms;                           // of a weight's value: times that K goes by
     int stages, packed;                  // depths of the rings
     int acc_cols;                        // TMEM columns of an accumulator
 };
@@ -207,12 +217,42 @@ __device__ __forceinline__ uint32_t pack16(int type, float a, float b)
     return type == MPQ_F16 ? pack2(a, b, __half()) : pack2(a, b, __nv_bfloat16());
 }
 
-template <typename T, int SHAPE>
+// A channel's power of two (EXACT, fp16): its scales are taken times 2^n, n = a + b, and its sums 2^-n times.
+struct Power {
+    int a, b;
+    __device__ __forceinline__ float scaled(float s) const { return s * pow2f(a) * pow2f(b); }
+    __device__ __forceinline__ float back(float v) const { return v * pow2f(-a) * pow2f(-b); }
+};
+// Of channel `row` of a row tile, by the scales of its packed tiles k0 .. k1 - 1.  (Bits above the exponent's of infinity
+// too: such a channel's outputs are no numbers anyway.)
+__device__ __forceinline__ Power power_of(const TileArgs &a, int row_tile, int row, int k0, int k1)
+{
+    const int strip = row_tile * (H_M / 16) + (row >> 4), groups = 128 / a.L.group;
+    uint32_t most = 0;
+    if (strip < a.L.row_tiles) {
+        const unsigned char *p = a.w + ((size_t)strip * a.L.k_tiles + k0) * a.L.tile_bytes + G4_CODES + (row & 15) * 2 * groups;
+#pragma unroll 8
+        for (int k = k0; k < k1; ++k, p += a.L.tile_bytes) {
+            if (groups == 1) {
+                most = __vmaxu2(most, *reinterpret_cast<const uint16_t *>(p) & 0x7fffu);
+            } else if (groups == 2) {
+                most = __vmaxu2(most, *reinterpret_cast<const uint32_t *>(p) & 0x7fff7fffu);
+            } else {
+                const uint2 s = *reinterpret_cast<const uint2 *>(p);
+                most = __vmaxu2(most, __vmaxu2(s.x & 0x7fff7fffu, s.y & 0x7fff7fffu));
+            }
+        }
+    }
+    const int n = 127 + 11 - max((int)(max(most & 0xffffu, most >> 16) >> 7), 1);     // -117 .. 137
+    return {n / 2, n - n / 2};
+}
+
+template <typename T, int SHAPE, bool EXACT>
 __global__ void __launch_bounds__(tile_threads(SHAPE), 1)
 g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ CUtensorMap tmX,
                 const __grid_constant__ CUtensorMap tmW)
 {
-    constexpr bool PAIR = SHAPE == PAIRS;
+    constexpr bool PAIR = SHAPE == PAIRS, POWERS = EXACT && !G4Pairs<T>::kBf16;
     extern __shared__ unsigned char raw[];
     unsigned char *const base = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
     TileCtrl &ctl = *reinterpret_cast<TileCtrl *>(base);
@@ -229,6 +269,9 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
     // this CTA's share of the row
     const int k0 = PAIR ? 0 : (int)((long long)k_tiles * rank / a.split);
     const int k1 = PAIR ? k_tiles : (int)((long long)k_tiles * (rank + 1) / a.split);
+    // stages of a tile: its packed tiles, for each term of the weights
+    const int span = (k1 - k0) * (EXACT ? a.terms : 1);
+    auto k_of = [&](int i) { return k0 + (EXACT && i >= k1 - k0 ? i - (k1 - k0) : i); };
     // halves of a stage (64 elements, a row of the swizzle) that the row reaches
     auto halves = [&](int k) { return k * H_K + 64 < a.L.d ? 2 : 1; };
     auto row_tile = [&](int tile) { return PAIR ? tile / a.n_tiles * 2 + rank : tile / a.n_tiles; };
@@ -290,7 +333,8 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
         bool stop = wc.withhold || *abort_flag;
         for (int tile = first; tile < a.tiles && !stop; tile += step) {
             const int y0 = (int)token0(tile) + (PAIR ? rank * a.held : 0);
-            for (int k = k0; k < k1; ++k, ++n, s.pass(a.stages)) {
+            for (int i = 0; i < span; ++i, ++n, s.pass(a.stages)) {
+                const int k = k_of(i);
                 const uint32_t at = ring_u32 + (uint32_t)(s.at * sb);
                 if ((n >= a.stages && warp_failed(&ctl.empty[s.at], s.phase ^ 1u)) || !MPQ_CHECK((at & 1023u) == 0u)) {
                     stop = true;
@@ -321,7 +365,7 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
         bool stop = wc.withhold || *abort_flag;
         for (int tile = first; tile < a.tiles && !stop; tile += step) {
             const int r0 = row_tile(tile) * 8;
-            for (int k = k0; k < k1; ++k, ++n, p.pass(a.packed)) {
+            for (int i = 0; i < span; ++i, ++n, p.pass(a.packed)) {
                 if (n >= a.packed && warp_failed(&ctl.p_empty[p.at], p.phase ^ 1u)) {
                     stop = true;
                     break;
@@ -333,7 +377,7 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
                 }
                 if (elected()) {         // (strips of 16 channels past the last are filled with zeros)
                     mbar_arrive_expect_tx(&ctl.p_full[p.at], (uint32_t)pb);
-                    tma_load_3d(at, &tmW, 0, k, r0, &ctl.p_full[p.at]);
+                    tma_load_3d(at, &tmW, 0, k_of(i), r0, &ctl.p_full[p.at]);
                 }
                 __syncwarp();
             }
@@ -346,7 +390,7 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
         Place s;
         bool stop = false;
         for (int tile = first; tile < a.tiles && !stop; tile += step)
-            for (int k = k0; k < k1; ++k, s.pass(a.stages)) {
+            for (int i = 0; i < span; ++i, s.pass(a.stages)) {
                 stop = warp_failed(&ctl.x_full[s.at], s.phase);
                 if (stop) break;
                 if (elected()) arrive(&ctl.ready[s.at]);
@@ -368,7 +412,7 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
                 const uint32_t d = tmem + (uint32_t)(SHAPE == NARROW ? own * a.acc_cols : 0);
                 uint32_t more = 0;
                 if (t > 0 && warp_failed(&ctl.d_empty, (uint32_t)(t - 1) & 1u, true)) break;
-                for (int k = k0; k < k1; ++k, ++n, s.pass(a.stages)) {
+                for (int i = 0; i < span; ++i, ++n, s.pass(a.stages)) {
                     if (SHAPE == NARROW && (n & 1) != own) continue;
                     if (warp_failed(&ctl.ready[s.at], s.phase, true)) {
                         stop = true;
@@ -378,7 +422,7 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
                     const uint64_t bd = smem_desc_sw128(ring_u32 + (uint32_t)(s.at * sb));
                     const uint32_t at = operands + (uint32_t)(s.at * H_A_COLS);
                     if (elected()) {
-                        const int count = halves(k);
+                        const int count = halves(k_of(i));
                         for (int h = 0; h < count; ++h) {
                             const uint64_t bh = bd + (uint64_t)(h * a.held * 8);     // in 16 B units
 #pragma unroll
@@ -411,11 +455,24 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
         const uint32_t to = operands + ((uint32_t)(q * 32) << 16);
         const unsigned char *const mine_at = packed + (row >> 4) * a.L.tile_bytes;
         // of all the stages of all the CTA's tiles, every makers(SHAPE)-th
-        const long long stages = first < a.tiles ? (long long)((a.tiles - first - 1) / step + 1) * (k1 - k0) : 0;
+        const long long stages = first < a.tiles ? (long long)((a.tiles - first - 1) / step + 1) * span : 0;
         Place p, s;
         p.pass(a.packed, own);
         s.pass(a.stages, own);
+        int tile = first, at_stage = own;    // EXACT: of which tile this is which stage
+        Power power = {0, 0};
+        int power_tile = -1;                 // whose
         for (long long n = own; n < stages; n += makers(SHAPE), p.pass(a.packed, makers(SHAPE)), s.pass(a.stages, makers(SHAPE))) {
+            bool second = false;             // the values' second term
+            if constexpr (EXACT) {
+                while (at_stage >= span) at_stage -= span, tile += step;
+                second = at_stage >= k1 - k0;
+                at_stage += makers(SHAPE);
+                if (POWERS && power_tile != tile) {
+                    power = power_of(a, row_tile(tile), row, k0, k1);
+                    power_tile = tile;
+                }
+            }
             if (warp_failed(&ctl.p_full[p.at], p.phase)) break;
             const unsigned char *const t = mine_at + p.at * pb;
             uint4 w[4];
@@ -445,7 +502,7 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
             swap_if(x & 2, w[1], w[3]);
             bool stop = false;
             const uint32_t scales[2] = {sc.x, sc.y};
-            const bool far = g4_far<T>(scales);
+            const bool far = !EXACT && g4_far<T>(scales);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {            // (behind the row's end: zeros, whose MMAs are left out)
                 uint32_t v[32];
@@ -453,21 +510,25 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
 #pragma unroll
                     for (int m = 0; m < 2; ++m) {
                         const uint32_t two = scales[h];
-                        const G4Scale g = g4_scale<T>(m ? two >> 16 : two & 0xffffu, z >> (8 * (2 * h + m)) & 255u);
+                        G4Scale g = g4_scale<T>(m ? two >> 16 : two & 0xffffu, z >> (8 * (2 * h + m)) & 255u);
+                        if constexpr (POWERS) g.s = G4Pairs<T>::bits(__float2half2_rn(power.scaled(bf16_bits(g.bits))));
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             const uint32_t word = h ? (m ? w[i].w : w[i].z) : (m ? w[i].y : w[i].x);
                             uint32_t p4[4];
-                            g4_values<T, decltype(f)::value>(word, g, p4);
+                            if constexpr (decltype(f)::value == 2)
+                                g4_rest<T>(word, g, p4);
+                            else
+                                g4_values<T, decltype(f)::value != 0>(word, g, p4);
 #pragma unroll
                             for (int e = 0; e < 4; ++e) v[16 * m + 4 * i + e] = p4[e];
                         }
                     }
                 };
-                if (far)
-                    convert(std::true_type());
+                if (EXACT ? second : far)
+                    convert(std::integral_constant<int, EXACT ? 2 : 1>());
                 else
-                    convert(std::false_type());
+                    convert(std::integral_constant<int, 0>());
                 if (h == 0) {
                     stop = n >= a.stages && warp_failed(&ctl.empty[s.at], s.phase ^ 1u);
                     if (stop) break;
@@ -489,10 +550,13 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
             const long long n0 = token0(tile);
             const int real = (int)min((long long)a.n_tile, a.rows.tokens - n0);
             // NARROW: both accumulators have sums, but for a tile of one stage
-            const int whose = k1 - k0 == 1 ? t & 1 : 0;
-            const bool both = SHAPE == NARROW && k1 - k0 > 1;
+            const int whose = span == 1 ? t & 1 : 0;
+            const bool both = SHAPE == NARROW && span > 1;
             const int c = row_tile(tile) * H_M + row;
             const float bias = a.split == 1 && a.rows.bias && c < a.rows.channels ? a.rows.bias[c] : 0.0f;
+            Power power = {0, 0};
+            if (POWERS) power = power_of(a, row_tile(tile), row, k0, k1);
+            auto value = [&](float v) { return POWERS ? power.back(v) : v; };
             if (warp_failed(&ctl.d_full, (uint32_t)t & 1u)) break;
             tc_fence_after();
             const uint32_t from = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(SHAPE == NARROW ? whose * a.acc_cols : 0);
@@ -509,7 +573,7 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
                         tmem_ld_32x32b_x32(from + (uint32_t)(j0 + 32 * u), v);
 #pragma unroll
                         for (int j = 0; j < 16; ++j)
-                            two[16 * u + j] = pack16(a.y_type, v[2 * j] + bias, v[2 * j + 1] + bias);
+                            two[16 * u + j] = pack16(a.y_type, value(v[2 * j]) + bias, value(v[2 * j + 1]) + bias);
                     }
                     tc_fence_before();
                     __syncwarp();
@@ -529,6 +593,10 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
                     tmem_ld_32x32b_x16(from + (uint32_t)(a.acc_cols + j0), o);
 #pragma unroll
                     for (int j = 0; j < 16; ++j) v[j] += o[j];
+                }
+                if (POWERS) {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) v[j] = value(v[j]);
                 }
                 if (!PAIR && a.split > 1) {          // [token][128 channels]; the MMAs have read the ring
                     float *const part = reinterpret_cast<float *>(ring) + row;
@@ -598,13 +666,13 @@ g4_rows_kernel(const uint16_t *X, long long ldx, int T, int d, uint16_t *to, int
     }
 }
 
-template <typename T, int SHAPE>
+template <typename T, int SHAPE, bool EXACT>
 mpq_status launch_tiles(const TileArgs &a, const CUtensorMap &tmX, const CUtensorMap &tmW, void *Y, int ctas, cudaStream_t stream)
 {
     const size_t smem = std::max(H_MIN_SMEM, 1024 + H_CTRL_BYTES + (size_t)a.stages * tile_stage_bytes(a.held) +
                                                  (size_t)a.packed * packed_bytes(a.L));
     static std::atomic<int> limit[kMaxDevices];
-    cudaError_t e = allow_smem(reinterpret_cast<const void *>(g4_tiles_kernel<T, SHAPE>), limit, smem);
+    cudaError_t e = allow_smem(reinterpret_cast<const void *>(g4_tiles_kernel<T, SHAPE, EXACT>), limit, smem);
     if (e != cudaSuccess) return cuda_status(e, "cudaFuncSetAttribute");
     WaitCtl wc;
     const mpq_status ws = wait_ctl(&wc);
@@ -622,17 +690,17 @@ mpq_status launch_tiles(const TileArgs &a, const CUtensorMap &tmX, const CUtenso
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    e = cudaLaunchKernelEx(&cfg, g4_tiles_kernel<T, SHAPE>, a, Y, wc, tmX, tmW);
+    e = cudaLaunchKernelEx(&cfg, g4_tiles_kernel<T, SHAPE, EXACT>, a, Y, wc, tmX, tmW);
     return cuda_status(e != cudaSuccess ? e : cudaGetLastError(), "g4 linear launch");
 }
 
-template <typename T>
+template <typename T, bool EXACT>
 mpq_status launch_form(const TileArgs &a, int shape, const CUtensorMap &tmX, const CUtensorMap &tmW, void *Y, int ctas,
                        cudaStream_t stream)
 {
-    return shape == PAIRS  ? launch_tiles<T, PAIRS>(a, tmX, tmW, Y, ctas, stream)
-           : shape == WIDE ? launch_tiles<T, WIDE>(a, tmX, tmW, Y, ctas, stream)
-                           : launch_tiles<T, NARROW>(a, tmX, tmW, Y, ctas, stream);
+    return shape == PAIRS  ? launch_tiles<T, PAIRS, EXACT>(a, tmX, tmW, Y, ctas, stream)
+           : shape == WIDE ? launch_tiles<T, WIDE, EXACT>(a, tmX, tmW, Y, ctas, stream)
+                           : launch_tiles<T, NARROW, EXACT>(a, tmX, tmW, Y, ctas, stream);
 }
 
 struct Form {
@@ -652,17 +720,17 @@ int resident(int split, int sms) { return split == 1 ? sms : split == 2 ? sms / 
 // taken).  Some of them, us, with 32 / 64 / 128 / 256 tokens a tile, pairs: 32 x 4,096 x 4,096 (T x C x d; split by 4)
 // 9.4, -, -, -, -; 256 x 11,008 x 4,096 -, -, 32.5, 25.4, 27.4; 2,048 x 11,008 x 4,096 -, 238, 148, 121, 105;
 // 512 x 4,096 x 4,096 -, -, 18.8, 18.5 (split by 2), 26.7.
-Form choose_form(int T, int C, int k_tiles, int sms, double &least)
+Form choose_form(int T, int C, int k_tiles, int terms, int sms, double &least)
 {
     auto rounds = [](long long n, long long at_once) { return (double)((n + at_once - 1) / at_once); };
     Form best = {256, true, 1};
-    least = 6.8 + rounds((C + 255LL) / 256 * ((T + 255LL) / 256), std::max(1, sms / 2)) * (0.512 * k_tiles + 3.7);
+    least = 6.8 + rounds((C + 255LL) / 256 * ((T + 255LL) / 256), std::max(1, sms / 2)) * (0.512 * k_tiles * terms + 3.7);
     if (T <= 128) least = HUGE_VAL;
     for (int most = 32; most <= 256; most += most < 128 ? 32 : 64) {
         const int n = std::min(most, (T + 15) / 16 * 16);
         const long long tiles = (C + H_M - 1LL) / H_M * ((T + n - 1LL) / n);
         for (int split = 1; split <= TOKEN_MAX_SPLIT && split * 2 <= std::max(2, k_tiles); split *= 2) {
-            const int stages = (k_tiles + split - 1) / split;
+            const int stages = (k_tiles + split - 1) / split * terms;
             const double r = rounds(tiles, std::max(1, resident(split, sms)));
             const double t = 1.9 + r * (stages * std::max(0.3435 + 0.0001 * n, 0.0021 * n) + 0.46 +
                                         (n > 128 ? 0.0246 : 0.0283) * n + (split > 1 ? 2.9 - 0.0091 * n : 0.0));
@@ -678,15 +746,17 @@ Form choose_form(int T, int C, int k_tiles, int sms, double &least)
 
 }  // namespace
 
-double g4_tiles_time(int T, int C, int d)
+int g4_terms(int x_type, const mpq_g4_matrix *L) { return x_type == MPQ_BF16 || L->zeros ? 2 : 1; }
+
+double g4_tiles_time(int T, int C, int d, int terms)
 {
     double t;
-    choose_form(T, C, (d + H_K - 1) / H_K, sm_count(), t);
+    choose_form(T, C, (d + H_K - 1) / H_K, terms, sm_count(), t);
     return t;
 }
 
 mpq_status launch_g4_tiles(const void *X, int x_type, long long ldx, int T, const mpq_g4_matrix *L, const void *W,
-                           const float *bias, void *Y, int y_type, long long ldy, cudaStream_t stream)
+                           const float *bias, void *Y, int y_type, long long ldy, int exact, cudaStream_t stream)
 {
     TileArgs a = {};
     a.L = *L;
@@ -695,7 +765,8 @@ mpq_status launch_g4_tiles(const void *X, int x_type, long long ldx, int T, cons
     const int C = L->rows, four = 4 * type_size(y_type), sms = sm_count();
     a.rows = {T, C, C % 4 == 0 && ldy % 4 == 0 && (uintptr_t)Y % four == 0, bias, ldy};
     double modelled;
-    const Form f = choose_form(T, C, L->k_tiles, sms, modelled);
+    a.terms = exact ? g4_terms(x_type, L) : 1;
+    const Form f = choose_form(T, C, L->k_tiles, a.terms, sms, modelled);
     a.n_tile = f.n;
     a.held = f.pair ? f.n / 2 : f.n;
     a.split = f.pair ? 1 : f.split;
@@ -764,9 +835,11 @@ mpq_status launch_g4_tiles(const void *X, int x_type, long long ldx, int T, cons
         set_error("g4 linear: tensor map encoding failed");
         st = MPQ_ERR_CUDA;
     } else if (x_type == MPQ_F16) {
-        st = launch_form<__half>(a, shape, tmX, tmW, Y, ctas, stream);
+        st = exact ? launch_form<__half, true>(a, shape, tmX, tmW, Y, ctas, stream)
+                   : launch_form<__half, false>(a, shape, tmX, tmW, Y, ctas, stream);
     } else {
-        st = launch_form<__nv_bfloat16>(a, shape, tmX, tmW, Y, ctas, stream);
+        st = exact ? launch_form<__nv_bfloat16, true>(a, shape, tmX, tmW, Y, ctas, stream)
+                   : launch_form<__nv_bfloat16, false>(a, shape, tmX, tmW, Y, ctas, stream);
     }
     if (scratch) {
         const cudaError_t e = cudaFreeAsync(scratch, stream);

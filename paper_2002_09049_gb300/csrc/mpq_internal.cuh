@@ -158,12 +158,14 @@ mpq_status launch_g4_quantize(const void *X, int x_type, long long ldx, const mp
 mpq_status launch_g4_dequantize(const void *packed, const mpq_g4_matrix *L, void *Y, int y_type,
                                 long long ldy, cudaStream_t stream);
 mpq_status launch_g4_linear(const void *X, int x_type, long long ldx, int T, const mpq_g4_matrix *L,
-                            const void *W, const float *bias, void *Y, int y_type, long long ldy,
+                            const void *W, const float *bias, void *Y, int y_type, long long ldy, int exact,
                             cudaStream_t stream);
-// The form for many tokens (g4_tiles.cu), and the time (us) that its model gives a call.
-double g4_tiles_time(int T, int C, int d);
+// The form for many tokens (g4_tiles.cu), how many 16-bit terms it takes to hold a weight's value, and the time (us)
+// that its model gives a call of so many.
+int g4_terms(int x_type, const mpq_g4_matrix *L);
+double g4_tiles_time(int T, int C, int d, int terms);
 mpq_status launch_g4_tiles(const void *X, int x_type, long long ldx, int T, const mpq_g4_matrix *L,
-                           const void *W, const float *bias, void *Y, int y_type, long long ldy,
+                           const void *W, const float *bias, void *Y, int y_type, long long ldy, int exact,
                            cudaStream_t stream);
 mpq_status launch_rotate(const mpq_rotate_rows *q, const mpq_rotate_rows *k, int type, int T, int dim,
                          const int *positions, int shift, const uint64_t *turns, int rot, int neighbours,

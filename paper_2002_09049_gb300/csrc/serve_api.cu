@@ -289,11 +289,10 @@ extern "C" mpq_status mpq_g4_dequantize(const void *packed, const mpq_g4_matrix 
     return launch_g4_dequantize(packed, layout, Y, y_type, ldy, (cudaStream_t)stream);
 }
 
-extern "C" mpq_status mpq_g4_linear(const void *X, int x_type, long long ldx, int T,
-                                    const mpq_g4_matrix *w_layout, const void *W, const float *bias, void *Y,
-                                    int y_type, long long ldy, void *stream)
+static mpq_status g4_linear(const void *X, int x_type, long long ldx, int T, const mpq_g4_matrix *w_layout,
+                            const void *W, const float *bias, void *Y, int y_type, long long ldy, int exact,
+                            void *stream)
 {
-    CallRange range_("mpq_g4_linear");
     clear_error();
     mpq_status st = check_g4(w_layout, "w_layout");
     if (st == MPQ_OK) st = check_type(x_type, "x_type");
@@ -309,7 +308,23 @@ extern "C" mpq_status mpq_g4_linear(const void *X, int x_type, long long ldx, in
     REQUIRE(aligned16(W), MPQ_ERR_INVALID_ARG, "W must be 16-byte aligned");
     REQUIRE(on(X, type_size(x_type)) && on(bias, sizeof(float)) && on(Y, type_size(y_type)), MPQ_ERR_INVALID_ARG,
             "X, bias and Y must be aligned to their elements");
-    return launch_g4_linear(X, x_type, ldx, T, w_layout, W, bias, Y, y_type, ldy, (cudaStream_t)stream);
+    return launch_g4_linear(X, x_type, ldx, T, w_layout, W, bias, Y, y_type, ldy, exact, (cudaStream_t)stream);
+}
+
+extern "C" mpq_status mpq_g4_linear(const void *X, int x_type, long long ldx, int T,
+                                    const mpq_g4_matrix *w_layout, const void *W, const float *bias, void *Y,
+                                    int y_type, long long ldy, void *stream)
+{
+    CallRange range_("mpq_g4_linear");
+    return g4_linear(X, x_type, ldx, T, w_layout, W, bias, Y, y_type, ldy, 0, stream);
+}
+
+extern "C" mpq_status mpq_g4_linear_exact(const void *X, int x_type, long long ldx, int T,
+                                          const mpq_g4_matrix *w_layout, const void *W, const float *bias,
+                                          void *Y, int y_type, long long ldy, void *stream)
+{
+    CallRange range_("mpq_g4_linear_exact");
+    return g4_linear(X, x_type, ldx, T, w_layout, W, bias, Y, y_type, ldy, 1, stream);
 }
 
 extern "C" mpq_status mpq_rotation_turns(const double *freq, int n, uint64_t *turns)
