@@ -407,7 +407,7 @@ def run(state):
     if k == "linear":
         lay = binding.mpq_g4_layout(case["C"], case["d"], case["group"], case["zeros"])
         return binding.mpq_g4_linear(state["x"], state["w"], lay, bias=state["bias"],
-                                     dtype=TYPES[case["dtype"]])
+                                     dtype=TYPES[case["dtype"]], exact=True)
     if k == "rotate":
         q, key = binding.mpq_rotate(state["q"], state["k"], state["pos"], state["turns"],
                                     norm=case["norm"], q_weight=state["q_weight"],
