@@ -763,6 +763,20 @@ mpq_status mpq_set_wait_limit(long long clocks);
  */
 mpq_status mpq_test_withhold_copies(int on);
 
+/*
+ * mpq_test_g4_form -- TEST HOOK, process-wide: the form in which later mpq_g4_linear and mpq_g4_linear_exact calls run,
+ * which their sizes choose otherwise (form 0, the default):
+ *   MPQ_G4_FEW     the few tokens' kernel (tokens and split are not looked at);
+ *   MPQ_G4_TILES   tiles of 128 channels and `tokens` tokens (a multiple of 16 up to 256; calls of fewer: as
+ *                  many as they have), K split over `split` CTAs (1, 2, 4 or 8);
+ *   MPQ_G4_PAIRS   CTA pairs, 256 channels and 256 tokens.
+ * A call with fewer than two packed tiles of 128 elements for each of `split` CTAs is MPQ_ERR_UNSUPPORTED meanwhile.
+ */
+#define MPQ_G4_FEW 1
+#define MPQ_G4_TILES 2
+#define MPQ_G4_PAIRS 3
+mpq_status mpq_test_g4_form(int form, int tokens, int split);
+
 /* MPQ_BUILD_* bits of the options this library was compiled with (0 for the normal build). */
 unsigned mpq_build_options(void);
 

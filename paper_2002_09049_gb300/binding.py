@@ -34,6 +34,8 @@ MPQ_TIMEOUT_DRAIN = 0x100
 MPQ_FAULT_BOUNDS = 0x10000            # mpq_device_status: the checked build skipped accesses
 MPQ_BUILD_CHECK_BOUNDS = 0x1          # mpq_build_options: the checked build
 
+MPQ_G4_FEW, MPQ_G4_TILES, MPQ_G4_PAIRS = 1, 2, 3       # mpq_test_g4_form
+
 MPQ_CACHE_WORKSPACE = 1 << 25         # bytes of mpq_cache_attention's workspace
 MPQ_PAGES_MAX_REQUESTS = 8192         # most requests of mpq_pages_extend and mpq_pages_trim
 
@@ -133,6 +135,7 @@ SIGNATURES = {
     "mpq_device_status": ([_P, _P], _I),
     "mpq_set_wait_limit": ([ctypes.c_longlong], _I),
     "mpq_test_withhold_copies": ([_I], _I),
+    "mpq_test_g4_form": ([_I, _I, _I], _I),
     "mpq_build_options": ([], ctypes.c_uint),
     "mpq_status_string": ([_I], ctypes.c_char_p),
     "mpq_last_error": ([], ctypes.c_char_p),
@@ -688,3 +691,9 @@ def mpq_set_wait_limit(clocks: int):
 def mpq_test_withhold_copies(on: bool):
     """Test hook: the output-error contraction's copy thread issues no copies while on."""
     _check(load().mpq_test_withhold_copies(1 if on else 0), "mpq_test_withhold_copies")
+
+
+def mpq_test_g4_form(form: int = 0, tokens: int = 256, split: int = 1):
+    """Test hook: the form of later mpq_g4_linear calls (MPQ_G4_*; 0: by their sizes), the tokens of a tile and
+    the CTAs that K is split over."""
+    _check(load().mpq_test_g4_form(form, tokens, split), "mpq_test_g4_form")

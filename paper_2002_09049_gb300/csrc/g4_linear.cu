@@ -11,6 +11,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "g4_few.cuh"
 
@@ -34,13 +35,26 @@ bool few_tokens(int T, const mpq_g4_matrix *L, int terms)
     return t < g4_tiles_time(T, L->rows, L->d, terms);
 }
 
+std::atomic<int> g_form{0};                  // a test's: form + 8 tokens + 4,096 split
+
 }  // namespace
+
+G4Form g4_test_form()
+{
+    const int f = g_form.load(std::memory_order_relaxed);
+    return {f & 7, f >> 3 & 511, f >> 12};
+}
+void set_g4_test_form(const G4Form &f)
+{
+    g_form.store(f.form | f.tokens << 3 | f.split << 12, std::memory_order_relaxed);
+}
 
 mpq_status launch_g4_linear(const void *X, int x_type, long long ldx, int T, const mpq_g4_matrix *L,
                             const void *W, const float *bias, void *Y, int y_type, long long ldy, int exact,
                             cudaStream_t stream)
 {
-    if (!few_tokens(T, L, exact ? g4_terms(x_type, L) : 1))
+    const int form = g4_test_form().form;
+    if (form ? form != MPQ_G4_FEW : !few_tokens(T, L, exact ? g4_terms(x_type, L) : 1))
         return launch_g4_tiles(X, x_type, ldx, T, L, W, bias, Y, y_type, ldy, exact, stream);
     const G4Args a = {*L, static_cast<const unsigned char *>(W), bias, ldx, ldy, T, y_type};
     return exact ? launch_few_exact(a, X, x_type, Y, stream) : launch_few_tokens<false>(a, X, x_type, Y, stream);

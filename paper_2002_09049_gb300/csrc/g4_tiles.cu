@@ -766,7 +766,16 @@ mpq_status launch_g4_tiles(const void *X, int x_type, long long ldx, int T, cons
     a.rows = {T, C, C % 4 == 0 && ldy % 4 == 0 && (uintptr_t)Y % four == 0, bias, ldy};
     double modelled;
     a.terms = exact ? g4_terms(x_type, L) : 1;
-    const Form f = choose_form(T, C, L->k_tiles, a.terms, sms, modelled);
+    Form f = choose_form(T, C, L->k_tiles, a.terms, sms, modelled);
+    const G4Form asked = g4_test_form();
+    if (asked.form == MPQ_G4_PAIRS) f = {256, true, 1};
+    if (asked.form == MPQ_G4_TILES) {
+        f = {std::min(asked.tokens, (T + 15) / 16 * 16), false, asked.split};
+        if (f.split > 1 && f.split * 2 > L->k_tiles) {
+            set_error("g4 linear: %d tiles of K are too few for %d CTAs", L->k_tiles, f.split);
+            return MPQ_ERR_UNSUPPORTED;
+        }
+    }
     a.n_tile = f.n;
     a.held = f.pair ? f.n / 2 : f.n;
     a.split = f.pair ? 1 : f.split;

@@ -163,6 +163,12 @@ mpq_status launch_g4_linear(const void *X, int x_type, long long ldx, int T, con
 // The form for many tokens (g4_tiles.cu), how many 16-bit terms it takes to hold a weight's value, and the time (us)
 // that its model gives a call of so many.
 int g4_terms(int x_type, const mpq_g4_matrix *L);
+// The form that a test asks for (form 0: none), and its setter (mpq_test_g4_form).
+struct G4Form {
+    int form, tokens, split;
+};
+G4Form g4_test_form();
+void set_g4_test_form(const G4Form &f);
 double g4_tiles_time(int T, int C, int d, int terms);
 mpq_status launch_g4_tiles(const void *X, int x_type, long long ldx, int T, const mpq_g4_matrix *L,
                            const void *W, const float *bias, void *Y, int y_type, long long ldy, int exact,

@@ -327,6 +327,19 @@ extern "C" mpq_status mpq_g4_linear_exact(const void *X, int x_type, long long l
     return g4_linear(X, x_type, ldx, T, w_layout, W, bias, Y, y_type, ldy, 1, stream);
 }
 
+extern "C" mpq_status mpq_test_g4_form(int form, int tokens, int split)
+{
+    clear_error();
+    REQUIRE(form >= 0 && form <= MPQ_G4_PAIRS, MPQ_ERR_INVALID_ARG, "form = %d is not one of MPQ_G4_*", form);
+    const bool tiles = form == MPQ_G4_TILES;
+    REQUIRE(!tiles || (tokens >= 16 && tokens <= 256 && tokens % 16 == 0), MPQ_ERR_INVALID_ARG,
+            "tokens = %d is not a multiple of 16, 16..256", tokens);
+    REQUIRE(!tiles || split == 1 || split == 2 || split == 4 || split == 8, MPQ_ERR_INVALID_ARG,
+            "split = %d is not 1, 2, 4 or 8", split);
+    set_g4_test_form({form, tiles ? tokens : 0, tiles ? split : 1});
+    return MPQ_OK;
+}
+
 extern "C" mpq_status mpq_rotation_turns(const double *freq, int n, uint64_t *turns)
 {
     clear_error();

@@ -24,3 +24,9 @@ def test_refuses(lib):
         assert f(**bad) == 1, bad
     assert f(t=F32) == 3 and f(T=(1 << 20) + 1) == 3
     assert f(T=0, X=None, Y=None) == 0 and f(lay=binding.mpq_g4_layout(0, 64, 32), ldy=0, W=None, Y=None) == 0
+
+
+def test_forms_are_refused(lib):
+    for bad in ((-1, 16, 1), (4, 16, 1), (2, 0, 1), (2, 8, 1), (2, 24, 1), (2, 272, 1), (2, 256, 0), (2, 256, 3), (2, 256, 16)):
+        assert lib.mpq_test_g4_form(*bad) == 1, bad
+    assert lib.mpq_test_g4_form(0, 0, 0) == 0

@@ -29,14 +29,14 @@ SHAPES = [(1, 1, 1), (1, 300, 4096), (5, 77, 333), (9, 129, 1000), (20, 40, 333)
           (1100, 5003, 333), (2100, 9001, 257), (1500, 9000, 140), (2300, 6001, 1100)]
 
 
-def packed_matrix(gen, C, d, group, zeros, exponents):
-    """(layout, packed buffer, values in 64 bits): every code, every zero point, scales m 2^e with m in [128, 255] and an e a
-    row; made on the device, where elements past the rows' ends have the value 0."""
+def packed_matrix(gen, C, d, group, zeros, exponents, most=256):
+    """(layout, packed buffer, values in 64 bits): every code, every zero point, scales m 2^e with m from 128 to most - 1 and
+    an e a row; made on the device, where elements past the rows' ends have the value 0."""
     lay = binding.mpq_g4_layout(C, d, group, zeros)
     rt, kt, n = lay.row_tiles, lay.k_tiles, 128 // group
     rnd = lambda lo, hi, *s: torch.randint(lo, hi, s, generator=gen, device=DEV)
     rows, wide = rt * 16, kt * 128
-    q, m = rnd(0, 16, rows, wide), rnd(128, 256, rows, kt * n)
+    q, m = rnd(0, 16, rows, wide), rnd(128, most, rows, kt * n)
     z = rnd(0, 16, rows, kt * n) if zeros else torch.full((rows, kt * n), 8, device=DEV)
     e = torch.zeros(rows, dtype=torch.float64, device=DEV)
     e[:C] = exponents
