@@ -55,7 +55,6 @@ constexpr int H_K = 128;                 // elements of K in a stage: a packed t
 constexpr int H_A_COLS = H_K / 2;        // TMEM columns of a stage's weights, two elements each
 constexpr int H_MAX_STAGES = 8;
 constexpr int H_MAX_PACKED = 8;
-constexpr int H_COLS = TOKEN_COLS;       // of tensor memory, all
 // PAIRS: CTA pairs, 256 tokens.  NARROW: up to 128 tokens, two warps that issue MMAs, each with an accumulator of its own.
 // WIDE: up to 256, one.
 enum Shape { PAIRS, WIDE, NARROW };
@@ -64,10 +63,13 @@ constexpr int H_OUTS = 8;                // warps that write outputs, behind the
 __host__ __device__ constexpr int makers(int shape) { return shape == PAIRS ? 2 : shape == WIDE ? 3 : 4; }
 __host__ __device__ constexpr int first_out(int shape) { return H_MAKE0 + 4 * makers(shape); }
 __host__ __device__ constexpr int tile_threads(int shape) { return (first_out(shape) + H_OUTS) * 32; }
+// Shared memory of a CTA, at least: more than half of an SM's, since each takes all tensor memory (a second one would
+// wait for it, and two clusters whose CTAs wait on each other's SMs would never begin)
+constexpr size_t H_MIN_SMEM = 120 * 1024;
 
 struct TileCtrl {
-    uint64_t x_full[H_MAX_STAGES];       // a stage's x has landed in this CTA
-    uint64_t ready[H_MAX_STAGES];        // a stage's weights are operands (PAIR: in both CTAs, and its x has landed there)
+    uint64_t x_full[H_MAX_STAGES];       // PAIR: a stage's x has landed in this CTA
+    uint64_t ready[H_MAX_STAGES];        // a stage's x has landed and its weights are operands (PAIR: in both CTAs)
     uint64_t empty[H_MAX_STAGES];        // the MMAs that read it completed
     uint64_t p_full[H_MAX_PACKED];       // packed weights have landed
     uint64_t p_empty[H_MAX_PACKED];      // and been read
@@ -287,15 +289,15 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
     auto arrive = [&](uint64_t *bar) {   // at the CTA whose thread issues MMAs
         if (PAIR) mbar_arrive_cluster(bar, 0); else mbar_arrive(bar);
     };
-    auto commit = [&](uint64_t *bar) {       // PAIR: in both CTAs
-        if (PAIR) mma_commit_pair(bar, (uint16_t)3); else mma_commit(bar);
+    auto commit = [&](uint64_t *bar, int ctas = 3) {
+        if (PAIR) mma_commit_pair(bar, (uint16_t)ctas); else mma_commit(bar);
     };
 
     griddep_launch();
     if (threadIdx.x == 0) {
         for (int i = 0; i < a.stages; ++i) {
             mbar_init(&ctl.x_full[i], 1);
-            mbar_init(&ctl.ready[i], PAIR ? 10 : 4);
+            mbar_init(&ctl.ready[i], PAIR ? 10 : 5);
             mbar_init(&ctl.empty[i], 1);
         }
         for (int i = 0; i < a.packed; ++i) {
@@ -313,9 +315,9 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
     }
     if (warp == 1) {
         if (PAIR)
-            tmem_alloc_pair(&ctl.tmem_base, H_COLS);
+            tmem_alloc_pair(&ctl.tmem_base, 512u);
         else
-            tmem_alloc(&ctl.tmem_base, H_COLS);
+            tmem_alloc(&ctl.tmem_base, 512u);
     }
     tc_fence_before();
     __syncthreads();
@@ -328,7 +330,7 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
         // -------------------------------------------------------------------- copies of x
         int n = 0;
         Place s;
-        bool stop = wc.withhold == 1 || *abort_flag;
+        bool stop = wc.withhold || *abort_flag;
         for (int tile = first; tile < a.tiles && !stop; tile += step) {
             const int y0 = (int)token0(tile) + (PAIR ? rank * a.held : 0);
             for (int i = 0; i < span; ++i, ++n, s.pass(a.stages)) {
@@ -340,7 +342,7 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
                 }
                 if (elected()) {
                     const int count = halves(k);
-                    uint64_t *const bar = &ctl.x_full[s.at];
+                    uint64_t *const bar = PAIR ? &ctl.x_full[s.at] : &ctl.ready[s.at];
                     mbar_arrive_expect_tx(bar, (uint32_t)(count * a.held * 128));
                     for (int h = 0; h < count; ++h)
                         tma_load_2d(at + (uint32_t)(h * a.held * 128), &tmX, k * H_K + h * 64, y0, bar);
@@ -348,16 +350,13 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
                 __syncwarp();
             }
         }
-        // no copy may land after the CTA is gone (whatever became of the other roles: a barrier that these complete too
-        // would never be full behind one that gave up)
+        // no copy may land after the CTA is gone (a stage that has weights too is full when they are made)
         for (int i = max(0, n - a.stages); lane == 0 && i < n; ++i)
-            drain_wait(&ctl.x_full[i % a.stages], (uint32_t)(i / a.stages) & 1u, wc, MPQ_TIMEOUT_G4);
-        // ... nor an arrival for the pair's MMAs: their end comes in any case, the last stages' arrivals if no role gave up
-        if (PAIR && lane == 0) {
-            drain_wait_cluster(&ctl.done, 0, wc, MPQ_TIMEOUT_G4);
-            for (int i = max(0, n - a.stages); i < n; ++i)
-                if (*abort_flag || failed(&ctl.empty[i % a.stages], (uint32_t)(i / a.stages) & 1u, false)) break;
-        }
+            drain_wait(PAIR ? &ctl.x_full[i % a.stages] : &ctl.ready[i % a.stages], (uint32_t)(i / a.stages) & 1u, wc,
+                       MPQ_TIMEOUT_G4);
+        // ... nor an arrival for the pair's MMAs
+        for (int i = max(0, n - a.stages); PAIR && lane == 0 && i < n && !*abort_flag; ++i)
+            drain_wait(&ctl.empty[i % a.stages], (uint32_t)(i / a.stages) & 1u, wc, MPQ_TIMEOUT_G4);
         __syncwarp();
     } else if (warp == 2) {
         // -------------------------------------------------------------------- copies of weights
@@ -415,7 +414,7 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
                 if (t > 0 && warp_failed(&ctl.d_empty, (uint32_t)(t - 1) & 1u, true)) break;
                 for (int i = 0; i < span; ++i, ++n, s.pass(a.stages)) {
                     if (SHAPE == NARROW && (n & 1) != own) continue;
-                    if ((!PAIR && warp_failed(&ctl.x_full[s.at], s.phase)) || warp_failed(&ctl.ready[s.at], s.phase, true)) {
+                    if (warp_failed(&ctl.ready[s.at], s.phase, true)) {
                         stop = true;
                         break;
                     }
@@ -440,7 +439,7 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
             }
             // every MMA issued above completes before tensor memory is released
             if (elected()) {
-                commit(&ctl.done);
+                commit(&ctl.done, 1);
                 drain_wait_cluster(&ctl.done, 0, wc, MPQ_TIMEOUT_G4);
             }
         }
@@ -641,9 +640,9 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
     if (warp == 1) {
         tc_fence_after();
         if (PAIR)
-            tmem_dealloc_pair(tmem, H_COLS);
+            tmem_dealloc_pair(tmem, 512u);
         else
-            tmem_dealloc(tmem, H_COLS);
+            tmem_dealloc(tmem, 512u);
     }
 }
 
@@ -670,10 +669,8 @@ g4_rows_kernel(const uint16_t *X, long long ldx, int T, int d, uint16_t *to, int
 template <typename T, int SHAPE, bool EXACT>
 mpq_status launch_tiles(const TileArgs &a, const CUtensorMap &tmX, const CUtensorMap &tmW, void *Y, int ctas, cudaStream_t stream)
 {
-    const size_t smem = token_smem(1024 + H_CTRL_BYTES + (size_t)a.stages * tile_stage_bytes(a.held) +
-                                       (size_t)a.packed * packed_bytes(a.L), H_COLS);
-    const mpq_status sm = token_check_sm();
-    if (sm != MPQ_OK) return sm;
+    const size_t smem = std::max(H_MIN_SMEM, 1024 + H_CTRL_BYTES + (size_t)a.stages * tile_stage_bytes(a.held) +
+                                                 (size_t)a.packed * packed_bytes(a.L));
     static std::atomic<int> limit[kMaxDevices];
     cudaError_t e = allow_smem(reinterpret_cast<const void *>(g4_tiles_kernel<T, SHAPE, EXACT>), limit, smem);
     if (e != cudaSuccess) return cuda_status(e, "cudaFuncSetAttribute");
@@ -799,7 +796,7 @@ mpq_status launch_g4_tiles(const void *X, int x_type, long long ldx, int T, cons
     // as many packed tiles as groups or more, as many stages as fit beside them, then more packed tiles
     const int room = max_smem_optin() - 1024 - H_CTRL_BYTES, pb = packed_bytes(*L), sb = tile_stage_bytes(a.held);
     const int groups = makers(shape), accs = shape == NARROW ? 2 : 1;
-    a.stages = std::min({H_MAX_STAGES, (room - groups * pb) / sb, (H_COLS - accs * a.acc_cols) / H_A_COLS});
+    a.stages = std::min({H_MAX_STAGES, (room - groups * pb) / sb, (512 - accs * a.acc_cols) / H_A_COLS});
     // A barrier's parity tells two phases apart, not more.  A group of makers that has made a stage knows that the MMAs
     // took the stage `stages` before it, and its next one is `groups` on: it meets a phase that is at most one behind if
     // there are as many stages as groups (NARROW: an even number of both, so that what one warp's MMAs took
