@@ -759,7 +759,9 @@ mpq_status mpq_set_wait_limit(long long clocks);
  * output-error contraction (mpq_output_error's tensor-core path) issues no copies, so that every
  * wait of that kernel runs out with nothing in flight and the call reports MPQ_TIMEOUT_OUTPUT_ERROR
  * through mpq_device_status; likewise mpq_mx_linear's (MPQ_TIMEOUT_MX), mpq_g4_linear's
- * (MPQ_TIMEOUT_G4) and mpq_cache_attention's warps (MPQ_TIMEOUT_ATTENTION).  Off (0) by default; never on outside tests of the timeout path.
+ * (MPQ_TIMEOUT_G4) and mpq_cache_attention's warps (MPQ_TIMEOUT_ATTENTION).  2: mpq_g4_linear's copies of
+ * weights alone, so that its waits run out with copies of x landed.  Off (0) by default; never on outside tests of the
+ * timeout path.
  */
 mpq_status mpq_test_withhold_copies(int on);
 

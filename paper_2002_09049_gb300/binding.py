@@ -688,9 +688,10 @@ def mpq_set_wait_limit(clocks: int):
     _check(load().mpq_set_wait_limit(int(clocks)), "mpq_set_wait_limit")
 
 
-def mpq_test_withhold_copies(on: bool):
-    """Test hook: the output-error contraction's copy thread issues no copies while on."""
-    _check(load().mpq_test_withhold_copies(1 if on else 0), "mpq_test_withhold_copies")
+def mpq_test_withhold_copies(on: int):
+    """Test hook: the output-error contraction's copy thread issues no copies while on (2: mpq_g4_linear's copies
+    of x go on)."""
+    _check(load().mpq_test_withhold_copies(2 if on == 2 else 1 if on else 0), "mpq_test_withhold_copies")
 
 
 def mpq_test_g4_form(form: int = 0, tokens: int = 256, split: int = 1):

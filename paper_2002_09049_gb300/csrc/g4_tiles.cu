@@ -68,8 +68,8 @@ __host__ __device__ constexpr int tile_threads(int shape) { return (first_out(sh
 constexpr size_t H_MIN_SMEM = 120 * 1024;
 
 struct TileCtrl {
-    uint64_t x_full[H_MAX_STAGES];       // PAIR: a stage's x has landed in this CTA
-    uint64_t ready[H_MAX_STAGES];        // a stage's x has landed and its weights are operands (PAIR: in both CTAs)
+    uint64_t x_full[H_MAX_STAGES];       // a stage's x has landed in this CTA
+    uint64_t ready[H_MAX_STAGES];        // a stage's weights are operands (PAIR: in both CTAs, and its x has landed there)
     uint64_t empty[H_MAX_STAGES];        // the MMAs that read it completed
     uint64_t p_full[H_MAX_PACKED];       // packed weights have landed
     uint64_t p_empty[H_MAX_PACKED];      // and been read
@@ -289,15 +289,15 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
     auto arrive = [&](uint64_t *bar) {   // at the CTA whose thread issues MMAs
         if (PAIR) mbar_arrive_cluster(bar, 0); else mbar_arrive(bar);
     };
-    auto commit = [&](uint64_t *bar, int ctas = 3) {
-        if (PAIR) mma_commit_pair(bar, (uint16_t)ctas); else mma_commit(bar);
+    auto commit = [&](uint64_t *bar) {       // PAIR: in both CTAs
+        if (PAIR) mma_commit_pair(bar, (uint16_t)3); else mma_commit(bar);
     };
 
     griddep_launch();
     if (threadIdx.x == 0) {
         for (int i = 0; i < a.stages; ++i) {
             mbar_init(&ctl.x_full[i], 1);
-            mbar_init(&ctl.ready[i], PAIR ? 10 : 5);
+            mbar_init(&ctl.ready[i], PAIR ? 10 : 4);
             mbar_init(&ctl.empty[i], 1);
         }
         for (int i = 0; i < a.packed; ++i) {
@@ -330,7 +330,7 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
         // -------------------------------------------------------------------- copies of x
         int n = 0;
         Place s;
-        bool stop = wc.withhold || *abort_flag;
+        bool stop = wc.withhold == 1 || *abort_flag;
         for (int tile = first; tile < a.tiles && !stop; tile += step) {
             const int y0 = (int)token0(tile) + (PAIR ? rank * a.held : 0);
             for (int i = 0; i < span; ++i, ++n, s.pass(a.stages)) {
@@ -342,7 +342,7 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
                 }
                 if (elected()) {
                     const int count = halves(k);
-                    uint64_t *const bar = PAIR ? &ctl.x_full[s.at] : &ctl.ready[s.at];
+                    uint64_t *const bar = &ctl.x_full[s.at];
                     mbar_arrive_expect_tx(bar, (uint32_t)(count * a.held * 128));
                     for (int h = 0; h < count; ++h)
                         tma_load_2d(at + (uint32_t)(h * a.held * 128), &tmX, k * H_K + h * 64, y0, bar);
@@ -350,13 +350,16 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
                 __syncwarp();
             }
         }
-        // no copy may land after the CTA is gone (a stage that has weights too is full when they are made)
+        // no copy may land after the CTA is gone (whatever became of the other roles: a barrier that these complete too
+        // would never be full behind one that gave up)
         for (int i = max(0, n - a.stages); lane == 0 && i < n; ++i)
-            drain_wait(PAIR ? &ctl.x_full[i % a.stages] : &ctl.ready[i % a.stages], (uint32_t)(i / a.stages) & 1u, wc,
-                       MPQ_TIMEOUT_G4);
-        // ... nor an arrival for the pair's MMAs
-        for (int i = max(0, n - a.stages); PAIR && lane == 0 && i < n && !*abort_flag; ++i)
-            drain_wait(&ctl.empty[i % a.stages], (uint32_t)(i / a.stages) & 1u, wc, MPQ_TIMEOUT_G4);
+            drain_wait(&ctl.x_full[i % a.stages], (uint32_t)(i / a.stages) & 1u, wc, MPQ_TIMEOUT_G4);
+        // ... nor an arrival for the pair's MMAs: their end comes in any case, the last stages' arrivals if no role gave up
+        if (PAIR && lane == 0) {
+            drain_wait_cluster(&ctl.done, 0, wc, MPQ_TIMEOUT_G4);
+            for (int i = max(0, n - a.stages); i < n; ++i)
+                if (*abort_flag || failed(&ctl.empty[i % a.stages], (uint32_t)(i / a.stages) & 1u, false)) break;
+        }
         __syncwarp();
     } else if (warp == 2) {
         // -------------------------------------------------------------------- copies of weights
@@ -414,7 +417,7 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
                 if (t > 0 && warp_failed(&ctl.d_empty, (uint32_t)(t - 1) & 1u, true)) break;
                 for (int i = 0; i < span; ++i, ++n, s.pass(a.stages)) {
                     if (SHAPE == NARROW && (n & 1) != own) continue;
-                    if (warp_failed(&ctl.ready[s.at], s.phase, true)) {
+                    if ((!PAIR && warp_failed(&ctl.x_full[s.at], s.phase)) || warp_failed(&ctl.ready[s.at], s.phase, true)) {
                         stop = true;
                         break;
                     }
@@ -439,7 +442,7 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
             }
             // every MMA issued above completes before tensor memory is released
             if (elected()) {
-                commit(&ctl.done, 1);
+                commit(&ctl.done);
                 drain_wait_cluster(&ctl.done, 0, wc, MPQ_TIMEOUT_G4);
             }
         }

@@ -135,6 +135,6 @@ extern "C" mpq_status mpq_set_wait_limit(long long clocks)
 
 extern "C" mpq_status mpq_test_withhold_copies(int on)
 {
-    g_withhold.store(on ? 1 : 0, std::memory_order_relaxed);
+    g_withhold.store(on == 2 ? 2 : on != 0, std::memory_order_relaxed);
     return MPQ_OK;
 }

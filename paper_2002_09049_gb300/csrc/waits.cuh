@@ -18,7 +18,7 @@ namespace mpq {
 struct WaitCtl {
     unsigned *status;    // this device's timeout word (MPQ_TIMEOUT_* bits, atomicOr)
     long long budget;    // SM clocks one wait may take before it gives up
-    int withhold;        // test hook: the contraction's copy thread issues no copies
+    int withhold;        // test hook: the contraction's copy thread issues no copies (2: a part of a kernel's)
 };
 
 // Host: the control block for a launch on the current device (the word's address is looked up

@@ -184,6 +184,29 @@ def test_withheld_copies_time_out(gpu, f, exact):
     assert binding.mpq_device_status() == 0
 
 
+@pytest.mark.parametrize("f", [*TILES, PAIRS], ids=ids)
+@pytest.mark.parametrize("T,d", [(40, 2100), (600, 2100), (300, 200)])
+def test_withheld_weights_time_out(gpu, f, T, d):
+    """With copies of x landed and the weights' withheld, the kernel ends as soon: its copies need no other role's work to
+    be waited for, so no drain gives up."""
+    d = least(f, d)
+    gen = torch.Generator(device=DEV).manual_seed(4)
+    lay, packed, w = packed_matrix(gen, 700, d, 64, False, torch.zeros(700, dtype=torch.float64, device=DEV), 129)
+    x = ones(gen, T, d, "bf16")
+    with form(f):
+        try:
+            binding.mpq_set_wait_limit(1 << 18)
+            binding.mpq_test_withhold_copies(2)
+            binding.mpq_g4_linear(x, packed, lay, dtype=torch.float32)
+            flags = binding.mpq_device_status()
+        finally:
+            binding.mpq_test_withhold_copies(0)
+            binding.mpq_set_wait_limit(0)
+        assert flags == binding.MPQ_TIMEOUT_G4
+        assert torch.equal(binding.mpq_g4_linear(x, packed, lay, dtype=torch.float32), (x.double() @ w.T).float())
+    assert binding.mpq_device_status() == 0
+
+
 def test_a_form_that_a_call_cannot_take(gpu):
     lay = binding.mpq_g4_layout(16, 512, 64)
     p = binding.mpq_g4_quantize(torch.ones(16, 512, device=DEV), lay)
