@@ -55,6 +55,7 @@ constexpr int H_K = 128;                 // elements of K in a stage: a packed t
 constexpr int H_A_COLS = H_K / 2;        // TMEM columns of a stage's weights, two elements each
 constexpr int H_MAX_STAGES = 8;
 constexpr int H_MAX_PACKED = 8;
+constexpr int H_COLS = TOKEN_COLS;       // of tensor memory, all
 // PAIRS: CTA pairs, 256 tokens.  NARROW: up to 128 tokens, two warps that issue MMAs, each with an accumulator of its own.
 // WIDE: up to 256, one.
 enum Shape { PAIRS, WIDE, NARROW };
@@ -63,9 +64,6 @@ constexpr int H_OUTS = 8;                // warps that write outputs, behind the
 __host__ __device__ constexpr int makers(int shape) { return shape == PAIRS ? 2 : shape == WIDE ? 3 : 4; }
 __host__ __device__ constexpr int first_out(int shape) { return H_MAKE0 + 4 * makers(shape); }
 __host__ __device__ constexpr int tile_threads(int shape) { return (first_out(shape) + H_OUTS) * 32; }
-// Shared memory of a CTA, at least: more than half of an SM's, since each takes all tensor memory (a second one would
-// wait for it, and two clusters whose CTAs wait on each other's SMs would never begin)
-constexpr size_t H_MIN_SMEM = 120 * 1024;
 
 struct TileCtrl {
     uint64_t x_full[H_MAX_STAGES];       // a stage's x has landed in this CTA
@@ -315,9 +313,9 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
     }
     if (warp == 1) {
         if (PAIR)
-            tmem_alloc_pair(&ctl.tmem_base, 512u);
+            tmem_alloc_pair(&ctl.tmem_base, H_COLS);
         else
-            tmem_alloc(&ctl.tmem_base, 512u);
+            tmem_alloc(&ctl.tmem_base, H_COLS);
     }
     tc_fence_before();
     __syncthreads();
@@ -643,9 +641,9 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
     if (warp == 1) {
         tc_fence_after();
         if (PAIR)
-            tmem_dealloc_pair(tmem, 512u);
+            tmem_dealloc_pair(tmem, H_COLS);
         else
-            tmem_dealloc(tmem, 512u);
+            tmem_dealloc(tmem, H_COLS);
     }
 }
 
@@ -672,8 +670,10 @@ g4_rows_kernel(const uint16_t *X, long long ldx, int T, int d, uint16_t *to, int
 template <typename T, int SHAPE, bool EXACT>
 mpq_status launch_tiles(const TileArgs &a, const CUtensorMap &tmX, const CUtensorMap &tmW, void *Y, int ctas, cudaStream_t stream)
 {
-    const size_t smem = std::max(H_MIN_SMEM, 1024 + H_CTRL_BYTES + (size_t)a.stages * tile_stage_bytes(a.held) +
-                                                 (size_t)a.packed * packed_bytes(a.L));
+    const size_t smem = token_smem(1024 + H_CTRL_BYTES + (size_t)a.stages * tile_stage_bytes(a.held) +
+                                       (size_t)a.packed * packed_bytes(a.L), H_COLS);
+    const mpq_status sm = token_check_sm();
+    if (sm != MPQ_OK) return sm;
     static std::atomic<int> limit[kMaxDevices];
     cudaError_t e = allow_smem(reinterpret_cast<const void *>(g4_tiles_kernel<T, SHAPE, EXACT>), limit, smem);
     if (e != cudaSuccess) return cuda_status(e, "cudaFuncSetAttribute");
@@ -799,7 +799,7 @@ mpq_status launch_g4_tiles(const void *X, int x_type, long long ldx, int T, cons
     // as many packed tiles as groups or more, as many stages as fit beside them, then more packed tiles
     const int room = max_smem_optin() - 1024 - H_CTRL_BYTES, pb = packed_bytes(*L), sb = tile_stage_bytes(a.held);
     const int groups = makers(shape), accs = shape == NARROW ? 2 : 1;
-    a.stages = std::min({H_MAX_STAGES, (room - groups * pb) / sb, (512 - accs * a.acc_cols) / H_A_COLS});
+    a.stages = std::min({H_MAX_STAGES, (room - groups * pb) / sb, (H_COLS - accs * a.acc_cols) / H_A_COLS});
     // A barrier's parity tells two phases apart, not more.  A group of makers that has made a stage knows that the MMAs
     // took the stage `stages` before it, and its next one is `groups` on: it meets a phase that is at most one behind if
     // there are as many stages as groups (NARROW: an even number of both, so that what one warp's MMAs took

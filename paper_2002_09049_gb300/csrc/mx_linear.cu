@@ -389,7 +389,9 @@ mpq_status launch_typed(const MxArgs &a, const void *A, const void *B, int row_b
         set_error("mx linear: tensor map encoding failed");
         return MPQ_ERR_CUDA;
     }
-    const size_t smem = 1024 + X_CTRL_BYTES + (size_t)a.stages * stage_bytes(a);
+    const size_t smem = token_smem(1024 + X_CTRL_BYTES + (size_t)a.stages * stage_bytes(a), a.cols);
+    const mpq_status sm = token_check_sm();
+    if (sm != MPQ_OK) return sm;
     static std::atomic<int> limit[kMaxDevices];
     cudaError_t e = allow_smem(reinterpret_cast<const void *>(mx_linear_kernel<T, MANY>), limit, smem);
     if (e != cudaSuccess) return cuda_status(e, "cudaFuncSetAttribute");

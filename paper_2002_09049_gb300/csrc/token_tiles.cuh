@@ -4,6 +4,7 @@
 #pragma once
 
 #include <algorithm>
+#include <atomic>
 
 #include "elements.cuh"
 #include "mpq_internal.cuh"
@@ -13,6 +14,41 @@ namespace mpq {
 
 constexpr int TOKEN_M = 128;             // channels of a tile
 constexpr int TOKEN_MAX_SPLIT = 8;       // CTAs of a cluster that splits K
+
+// tcgen05.alloc waits until the columns that it asks for are free, without a limit.  So CTAs whose columns do not fit
+// beside one another must not come to one SM: two clusters that each hold what the other's CTA waits for would never
+// end, nor would a kernel launched ahead that holds what the one before it waits for.  Shared memory keeps them apart: a
+// CTA that takes more than half of the columns asks for TOKEN_ALONE_SMEM or more, one that takes half or less for
+// TOKEN_HALF_SMEM or more, which two of them leave no third and none of the others room beside.  (The SM keeps
+// 1 KB a CTA for itself.)
+constexpr size_t TOKEN_SM_SMEM = 228 * 1024, TOKEN_KEPT_SMEM = 1024;
+constexpr size_t TOKEN_HALF_SMEM = 96 * 1024, TOKEN_ALONE_SMEM = 132 * 1024;
+constexpr int TOKEN_COLS = 512;          // columns of tensor memory
+static_assert(TOKEN_ALONE_SMEM + TOKEN_HALF_SMEM + 2 * TOKEN_KEPT_SMEM > TOKEN_SM_SMEM, "one alone and half");
+static_assert(3 * (TOKEN_HALF_SMEM + TOKEN_KEPT_SMEM) > TOKEN_SM_SMEM, "three halves");
+
+// What a launch asks for: `smem` bytes and `cols` columns are what its CTA uses.
+inline size_t token_smem(size_t smem, int cols)
+{
+    return std::max(smem, 2 * cols > TOKEN_COLS ? TOKEN_ALONE_SMEM : TOKEN_HALF_SMEM);
+}
+// Refuses a device whose SMs have other shared memory than this reckons with.
+inline mpq_status token_check_sm()
+{
+    static std::atomic<int> good[kMaxDevices];
+    int dev = 0, most = 0, kept = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess && dev < kMaxDevices && good[dev].load(std::memory_order_relaxed)) return MPQ_OK;
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&most, cudaDevAttrMaxSharedMemoryPerMultiprocessor, dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&kept, cudaDevAttrReservedSharedMemoryPerBlock, dev);
+    if (e != cudaSuccess) return cuda_status(e, "shared memory of an SM");
+    if ((size_t)most > TOKEN_SM_SMEM || (size_t)kept < TOKEN_KEPT_SMEM) {
+        set_error("SMs of %d bytes of shared memory, %d kept a CTA, are not supported", most, kept);
+        return MPQ_ERR_UNSUPPORTED;
+    }
+    if (dev < kMaxDevices) good[dev].store(1, std::memory_order_relaxed);
+    return MPQ_OK;
+}
 
 // Outputs [tokens][channels], rows ldy apart; wide: they take 4 at a time.
 struct TokenRows {

@@ -207,6 +207,32 @@ def test_withheld_weights_time_out(gpu, f, T, d):
     assert binding.mpq_device_status() == 0
 
 
+@pytest.mark.parametrize("f", [(binding.MPQ_G4_TILES, 48, 8), (binding.MPQ_G4_TILES, 256, 2), PAIRS], ids=ids)
+def test_beside_the_microscaled_layer(gpu, f):
+    """The two layers whose clusters' CTAs allocate tensor memory, on two streams and one after another on one: each ends,
+    with the result of the call made alone (an SM has no room for CTAs of both)."""
+    gen = torch.Generator(device=DEV).manual_seed(7)
+    rand = lambda *s: torch.randn(*s, generator=gen, device=DEV)
+    d, T = 4096, 48
+    lay, xl, wl = binding.mpq_g4_layout(4096, d, 64), binding.mpq_mx_layout(T, d), binding.mpq_mx_layout(1500, d)
+    g, w = binding.mpq_g4_quantize(rand(4096, d), lay), binding.mpq_mx_quantize(rand(1500, d), wl)
+    x = rand(T, d).bfloat16()
+    q = binding.mpq_mx_quantize(x, xl)
+    one, two = lambda: binding.mpq_g4_linear(x, g, lay), lambda: binding.mpq_mx_linear(q, xl, w, wl)
+    with form(f):
+        y, v = one(), two()
+        torch.cuda.synchronize()
+        streams = torch.cuda.Stream(), torch.cuda.Stream()
+        for _ in range(40):
+            got = []
+            for s, calls in zip(streams, ((one, two, one), (two, one, two))):
+                with torch.cuda.stream(s):
+                    got += [(c, c()) for c in calls]
+            torch.cuda.synchronize()
+            assert all(torch.equal(r, y if c is one else v) for c, r in got)
+    assert binding.mpq_device_status() == 0
+
+
 def test_a_form_that_a_call_cannot_take(gpu):
     lay = binding.mpq_g4_layout(16, 512, 64)
     p = binding.mpq_g4_quantize(torch.ones(16, 512, device=DEV), lay)
