@@ -628,11 +628,11 @@ g4_tiles_kernel(const TileArgs a, void *Y, WaitCtl wc, const __grid_constant__ C
         const JoinAt at{reinterpret_cast<const float *>(ring), n0,
                         (int)min((long long)a.n_tile, a.rows.tokens - n0), row_tile(first), rank};
         if (a.y_type == MPQ_F32)
-            join_split(a.rows, static_cast<float *>(Y), at, a.split);
+            join_split<false>(a.rows, static_cast<float *>(Y), at, a.split);
         else if (a.y_type == MPQ_F16)
-            join_split(a.rows, static_cast<__half *>(Y), at, a.split);
+            join_split<false>(a.rows, static_cast<__half *>(Y), at, a.split);
         else
-            join_split(a.rows, static_cast<__nv_bfloat16 *>(Y), at, a.split);
+            join_split<false>(a.rows, static_cast<__nv_bfloat16 *>(Y), at, a.split);
     }
     if (cluster)
         cluster_sync();                  // no CTA leaves while its sums are read, or arrivals to it are on their way

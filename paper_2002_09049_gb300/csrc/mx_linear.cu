@@ -349,7 +349,7 @@ mx_linear_kernel(const MxArgs a, T *Y, WaitCtl wc, const __grid_constant__ CUten
         cluster_sync();                  // every rank's sums are in its shared memory
         const TokenRows rows{a.b_rows, a.a_rows, a.wide, a.bias, a.ldy};
         const JoinAt at{reinterpret_cast<const float *>(ring), n0, n_real, tile, rank};
-        join_split(rows, Y, at, a.split);
+        join_split<true>(rows, Y, at, a.split);
     }
     if (cluster)
         cluster_sync();                  // no rank leaves while its sums are read, or copies to it land

@@ -90,8 +90,12 @@ struct JoinAt {
     int n_real, tile, rank;
 };
 
-// The sums of a cluster's R ranks, in rank order; four channels to a thread, eight loads in flight.
-template <typename T, int R>
+// The sums of a cluster's R ranks, in rank order; four channels to a thread, eight loads in flight.  WHOLE: a thread's
+// loads past the last are of the last again, so that none of them waits for a comparison.  The microscaled layer's up to
+// 320 threads have few such (75 x 4,096 x 11,008, T x C x d, 9.9 us instead of 10.05, 256 x 4,096 x 4,096 8.5 instead
+// of 9.1); of the 896 that the 4-bit integer layer has, most would load for nothing (75 x 4,096 x 11,008 14.4 us instead of
+// 14.2, 500 x 1,024 x 4,096 10.8 instead of 10.55).
+template <typename T, int R, bool WHOLE>
 __device__ __forceinline__ void join(const TokenRows &a, T *Y, const JoinAt &at)
 {
     constexpr int U = 8 / R;
@@ -102,17 +106,18 @@ __device__ __forceinline__ void join(const TokenRows &a, T *Y, const JoinAt &at)
         float4 p[U][R];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (i0 + u * step >= quads) break;
+            const int i = i0 + u * step;
+            if (!WHOLE && i >= quads) break;
 #pragma unroll
             for (int r = 0; r < R; ++r)
-                p[u][r] = sm100::ld_dsmem_f32x4(at.part + (i0 + u * step) * 4, (uint32_t)r);
+                p[u][r] = sm100::ld_dsmem_f32x4(at.part + (WHOLE ? min(i, quads - 1) : i) * 4, (uint32_t)r);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int i = i0 + u * step;
-            if (i >= quads) break;
+            if (!WHOLE && i >= quads) break;
             const int t = i / (TOKEN_M / 4), c = at.tile * TOKEN_M + (i % (TOKEN_M / 4)) * 4;
-            if (c >= a.channels) continue;
+            if (i >= quads || c >= a.channels) continue;
             float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int r = 0; r < R; ++r)
@@ -133,15 +138,15 @@ __device__ __forceinline__ void join(const TokenRows &a, T *Y, const JoinAt &at)
     }
 }
 
-template <typename T>
+template <bool WHOLE, typename T>
 __device__ __forceinline__ void join_split(const TokenRows &a, T *Y, const JoinAt &at, int split)
 {
     if (split == 2)
-        join<T, 2>(a, Y, at);
+        join<T, 2, WHOLE>(a, Y, at);
     else if (split == 4)
-        join<T, 4>(a, Y, at);
+        join<T, 4, WHOLE>(a, Y, at);
     else
-        join<T, 8>(a, Y, at);
+        join<T, 8, WHOLE>(a, Y, at);
 }
 
 }  // namespace mpq
