@@ -694,7 +694,7 @@ mpq_status mpq_pages_extend(const int *add, int B, int page, int cols, const int
  * beyond return to the pool, in the order in which mpq_pages_extend would give them out again (a step that is
  * taken back whole leaves the pool as it was).  Table entries past a request's end are left as they were.  If
  * more pages return than the pool has room for, those past its end are dropped (and its count is `pages`):
- * a state that extend and trim alone have changed has room for all.  Lengths are taken as within 0 .. page *
+ * a state that extend and trim alone have changed has room for all.  (Sums of pages stop at 2^31 - 1.)  Lengths are taken as within 0 .. page *
  * cols; new_lens and new_count as mpq_pages_extend's.
  */
 mpq_status mpq_pages_trim(const int *keep, int B, int page, int cols, const int *lens, int *new_lens,
@@ -702,7 +702,7 @@ mpq_status mpq_pages_trim(const int *keep, int B, int page, int cols, const int 
 
 /*
  * Bounded device-side waits.  The tensor-core kernels (mpq_output_error and its _noalloc variant,
- * mpq_clip_search, mpq_multipoint_linear, mpq_mx_linear, mpq_g4_linear) hand work between their warps, and
+ * mpq_clip_search, mpq_multipoint_linear, mpq_mx_linear, mpq_g4_linear and its _exact) hand work between their warps, and
  * mpq_cache_attention's warps take their copies, through shared-memory barriers, and every wait on
  * one is bounded by a clock budget.  A kernel whose wait gives up
  * stops issuing work, waits for the copies and MMAs it has already issued to finish, releases its

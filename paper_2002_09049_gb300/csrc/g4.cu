@@ -8,7 +8,7 @@
 // normal range.
 //
 // Memory-bound where elements are fp32: 11,008 x 4,096 is quantised in 31.3 us and read back in 31.4 (204 MB each, 6.5
-// TB/s).  4,096 x 4,096 bf16 with zero points in groups of 64 takes 10.5 and 7.8 (42 MB each): quantising is bound by issue.
+// TB/s).  4,096 x 4,096 bf16 with zero points in groups of 64 takes 10.5 and 7.8 (42 MB each): quantising by its instructions.
 // 16-bit types' ranges are found two elements an instruction, and quotients and their rounding too (one by one 13.6 us; with
 // one word of codes a thread and a division's two corrections 19.2); two tiles a thread instead of four took 10.9.
 #include <math.h>
@@ -223,7 +223,8 @@ __device__ __forceinline__ TileRun tile_run(const mpq_g4_matrix &L, int most)
 // A thread has 16 elements of U tiles, and 128 threads a tile's 16 rows; the CTA's two halves take U tiles each.  VEC: rows
 // are 16-byte aligned, and all of a thread's elements are on their way before the first is used; else (U = 1) rows
 // pass through shared memory, a warp's accesses consecutive.  Four CTAs an SM: fp32 with zero points, 11,008 x 4,096, is
-// 36.4 us with the two registers more that leave three, 33.6 with four.
+// 36.4 us with the two registers more that leave three, 33.6 with four.  (Four cost 16-bit rows with zero points two spilled
+// words.)
 template <typename T, bool VEC, bool ZEROS, int U>
 __global__ void __launch_bounds__(G4_THREADS, U > 1 ? 4 : 1)
 g4_quantize_kernel(const T *X, long long ldx, mpq_g4_matrix L, unsigned char *packed)

@@ -82,7 +82,8 @@ __device__ __forceinline__ G4Scale g4_scale(uint32_t bits, uint32_t z)
     return {G4Pairs<T>::scale(bits), G4Pairs<T>::kPower | z | z << 16, bits};
 }
 
-// A pair of a word's codes as the bits of the power plus each.
+// A pair of a word's codes as the bits of the power plus each: a whole number set into the last places of a power's
+// significand, the conversion of Warren, Hacker's Delight, 2nd ed., 17-2.
 template <typename T>
 __device__ __forceinline__ uint32_t g4_pair(uint32_t w, int j)
 {

@@ -4,7 +4,7 @@
 // A tile's 16 rows are A, eight tokens B.  A lane's 16 bytes of a row hold, for each 32 elements, the eight that it
 // multiplies in two MMAs: the codes become A's registers where they are, and x's registers are 16 consecutive bytes of
 // its row.  Warps of a CTA take a row tile's tiles in turn and their sums are joined in shared memory in the
-// warps' order.
+// warps' order.  (EXACT with 32 tokens spills up to 19 words: it has its groups' sums beside all of K's.)
 #pragma once
 
 #include <type_traits>

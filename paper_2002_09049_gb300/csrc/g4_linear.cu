@@ -6,8 +6,10 @@
 // in the tensor cores' fp32.)  In bf16 that is as much again as the rounding of 16-bit outputs, so the exact call has no
 // rounding of weights at all.
 //
-// Measured: 1 x 4,096 x 4,096 (T x C x d) 4.0 us (a launch, one round of loads, the join; the weights' bytes would take
-// 1.3), 5 x 11,008 x 4,096 bf16 8.2, fp16 with zero points 9.6 (issue: 15 instructions for eight weights).
+// Measured (weights in L2, as they are from call to call; in brackets 20 layers' weights by turns, which come from memory),
+// few tokens: 1 x 4,096 x 4,096 (T x C x d) 3.7 us (4.6: a launch, one round of loads, the join; the weights' bytes would
+// take 1.3), 5 x 11,008 x 4,096 fp16 with zero points 9.1 (11.2: loads' latency, issue slots 0.45 busy with 15 instructions
+// for eight weights, 688 CTAs on places for 456).  The models below were fitted to calls with weights in L2.
 #include <math.h>
 
 #include <algorithm>

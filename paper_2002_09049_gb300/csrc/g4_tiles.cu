@@ -20,11 +20,12 @@
 // held as it is, a smaller one to 2^-36 of it.
 //
 // Measured, beside the rounded values': 2,048 x 11,008 x 4,096 bf16 191 us (102), fp16 without zero points 110 (104), with
-// them 200 (105); 256 x 11,008 x 4,096 bf16 41.8 (24.4); 75 x 4,096 x 11,008 bf16 23.7 (14.3).
+// them 200 (105); 256 x 11,008 x 4,096 bf16 41.8 (24.4); 75 x 4,096 x 11,008 bf16 23.8 (14.3: its makers make both terms,
+// 14.8 M warp instructions for 7.4).  fp16's powers spill 7 words in the pairs' form.
 //
-// Measured: 2,048 x 11,008 x 4,096 (T x C x d) 105 us, 1.76 PFLOP/s: a stage takes 1,024 cycles, its MMAs' own; 1,800 a
-// tile between the last MMA and the next one's first; 344 tiles on 76 pairs are five rounds.  75 x 4,096 x 11,008 14.8
-// us: 2 to the first MMA, 22 stages of 0.35 on 128 CTAs (1,700 warp instructions a stage to make its operands), 3 for
+// Measured: 2,048 x 11,008 x 4,096 (T x C x d) 102 us, 1.81 PFLOP/s: a stage takes 1,024 cycles, its MMAs' own; 1,800 a
+// tile between the last MMA and the next one's first; 344 tiles on 76 pairs are five rounds.  75 x 4,096 x 11,008 14.3
+// us (weights from memory 15.0): 2 to the first MMA, 22 stages of 0.35 on 128 CTAs (1,700 warp instructions a stage to make its operands), 3 for
 // the join of four ranks; without any of the work, roles waiting on each other alone, 10.3.
 //
 // Warps: 0 copies x, 1 issues MMAs (the even CTA's, of a pair; NARROW: 3 too), 2 copies weights, PAIRS: 3 tells the MMAs'
@@ -718,7 +719,7 @@ int resident(int split, int sms) { return split == 1 ? sms : split == 2 ? sms / 
 
 // The form with the least modelled time (us): a start, and for each round of resident CTAs its stages, by their tokens
 // (up to 128 the operands' making bounds them, 0.34 to 0.36 us; from 192 on the MMAs), the tile's way out, and the
-// joining of a split.  Fitted to 919 timings of 91 sizes (16 <= T <= 2,048, 448 <= C <= 14,000, 500 <= d <= 11,008): the
+// joining of a split; `terms`: K goes by so many times.  Fitted to 919 timings, weights in L2, of 91 sizes (16 <= T <= 2,048, 448 <= C <= 14,000, 500 <= d <= 11,008): the
 // choice costs 1% on average against the best form, 15% at worst (16 x 1,024 x 1,024, where the few tokens' kernel is
 // taken).  Some of them, us, with 32 / 64 / 128 / 256 tokens a tile, pairs: 32 x 4,096 x 4,096 (T x C x d; split by 4)
 // 9.4, -, -, -, -; 256 x 11,008 x 4,096 -, -, 32.5, 25.4, 27.4; 2,048 x 11,008 x 4,096 -, 238, 148, 121, 105;

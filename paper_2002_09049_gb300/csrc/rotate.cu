@@ -12,8 +12,9 @@
 // last one is turned, and its cosines and sines -- made once for all heads, by every row's own threads they cost
 // more than the rows' traffic -- are left in shared memory for it.
 //
-// 8,192 tokens of 40 heads of 128 bf16 take 34.7 us (168 MB, 4.8 TB/s; without a norm 30.6, neighbours' pairs 44): 290
-// warp instructions a token and four rows, issue slots 0.52 busy, a barrier a token.  A CTA a token, without
+// 8,192 tokens of 40 heads of 128 bf16 take 34.7 us (168 MB, 4.8 TB/s; without a norm 30.6, neighbours' pairs 44): a
+// barrier a token, at which warps wait for the slowest (issue slots are 0.52 busy, with 290 warp instructions a token and
+// four rows).  The 16-bit forms' 64 registers, for two CTAs of 512 threads, leave 12 to 16 bytes spilled.  A CTA a token, without
 // loads ahead, took 62; one element after another instead of two at once, and cosines that eight threads read from
 // the same banks, 49.
 #include <math.h>
